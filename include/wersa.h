@@ -219,6 +219,86 @@ int64_t wersa_block_saved_offset(const wersa_desc *desc, int which);
  * (B, n, hidden)). -1 on a bad argument. */
 int64_t wersa_block_workspace_offset(const wersa_desc *desc, int which);
 
+/*
+ * Causal linear attention with a decay for each head (the causal counterpart of step 8 without a normaliser, for decoders):
+ *   S_t = lambda_h S_{t-1} + k_t v_t^T  (dk x dv, float32),  o_t = scale q_t^T S_t,  lambda_h = exp(log_decay[h])
+ * over a whole sequence (wersa_decay_forward), its derivative (wersa_decay_backward), and one token at a time on a
+ * cache of states (wersa_decay_step).  q and k are (B, H, n, dk), v and out (B, H, n, dv), each at strides of its own
+ * (batch, head, row; in elements; columns contiguous); dq, dk, dv and dout are laid out like q, k, v and out.  Any
+ * element-aligned pointer is taken.
+ *   packed   0: B sequences of n rows each; offsets is NULL.
+ *            1: B sequences of any lengths (zero among them) one behind the other in tensors with one batch entry of n
+ *               rows: sequence b is rows offsets[b] .. offsets[b + 1] - 1 (B + 1 device integers that do not decrease; the
+ *               batch strides are not read).  Offsets are clamped to 0 .. n on the device; rows of no sequence are not written.
+ *   log_decay  float32 [H], at most 0 for a state that stays bounded; -inf is a decay of zero.  A fixed parameter: it
+ *            has no gradient.
+ *   states   float32 [state_slots][H][dk][dv], contiguous, 16-byte aligned.  initial_state NULL: zeros; final_state
+ *            NULL: not wanted; the two may be the same buffer.  slots NULL: sequence b has state b.  Otherwise sequence b has
+ *            state slots[b] (device integers, no two alike); one below 0 or from state_slots on has none: its initial state is
+ *            zero, its final state is not written, and wersa_decay_step gives it zeros.
+ *   saved    what the forward leaves for the backward (wersa_decay_saved_bytes, 256-byte aligned); NULL: no backward
+ *            follows, and the workspace takes it.  A forward that is given `saved` needs no workspace.
+ * wersa_decay_backward: the gradients of a scalar loss given those with respect to out and (dfinal_state, by sequence, may be
+ * NULL) the final states; initial_state is by sequence; dinitial_state may be NULL.
+ * Supported: dk, dv multiples of 16 up to 128; n up to 2^30 (0: the final state is the initial one); B, H up to 65535.
+ * Arithmetic: states and every sum in float32.  The other conventions are those above.
+ */
+typedef struct {
+  int32_t B, H, n, dk, dv;
+  int32_t dtype;           /* wersa_dtype of q, k, v, out and their gradients */
+  int32_t packed;
+  float scale;
+  int64_t stride_q[3], stride_k[3], stride_v[3], stride_o[3];
+} wersa_decay_desc;
+
+size_t wersa_decay_workspace_bytes(const wersa_decay_desc *desc, int for_backward);
+size_t wersa_decay_saved_bytes(const wersa_decay_desc *desc);
+
+wersa_status wersa_decay_forward(const wersa_decay_desc *desc, const void *q, const void *k, const void *v,
+                                 const float *log_decay, const int32_t *offsets, const float *initial_state,
+                                 float *final_state, const int32_t *slots, int32_t state_slots, void *out, void *saved,
+                                 void *workspace, size_t workspace_bytes, void *hip_stream);
+
+wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, const void *k, const void *v,
+                                  const float *log_decay, const int32_t *offsets, const float *initial_state,
+                                  const void *dout, const float *dfinal_state, const void *saved, void *dq, void *dk,
+                                  void *dv, float *dinitial_state, void *workspace, size_t workspace_bytes,
+                                  void *hip_stream);
+
+/* One token of each of B sequences (desc->n = 1, not packed): the states are updated in place. */
+wersa_status wersa_decay_step(const wersa_decay_desc *desc, const void *q, const void *k, const void *v,
+                              const float *log_decay, float *state, const int32_t *slots, int32_t state_slots, void *out,
+                              void *hip_stream);
+
+/*
+ * Root-mean-square norm over the columns of a row, with the residual's addition before it:
+ *   r = x + residual (kept in the tensors' type; with residual NULL r is x itself and nothing is written),
+ *   y = r * rstd * weight,  rstd = 1 / sqrt(mean(r^2) + eps)
+ * The norm reads the stream r as it is kept.  x and residual are (rows, cols) at row strides of their own, columns
+ * contiguous; r, y, dy, dr and dx are dense.  weight is float32 [cols] or NULL (ones); rstd float32 [rows], NULL:
+ * not wanted.  wersa_rms_norm_eight_bit writes y in 8 bits (e4m3, largest value 448) and float32 scales [rows]:
+ *   scale = max|y| / 448,  y8 = e4m3(y * (448 / max|y|)) to the nearest, ties to even;  a row of zeros has scale 1.
+ * wersa_rms_norm_backward: r is the forward's stream (x where no residual was added, at stride_x), dr the gradient that
+ * reaches r from elsewhere (NULL: none); dx is the gradient of x and of the residual, dweight (float32 [cols], NULL: not
+ * wanted) that of the weight, for which the workspace is needed.  Supported: cols up to 8192, rows up to 2^31 (0: nothing is done but
+ * dweight = 0).
+ */
+typedef struct {
+  int64_t rows;
+  int32_t cols, dtype;
+  float eps;
+  int64_t stride_x, stride_residual;
+} wersa_norm_desc;
+
+wersa_status wersa_rms_norm_forward(const wersa_norm_desc *desc, const void *x, const void *residual, const float *weight,
+                                    void *r, void *y, float *rstd, void *hip_stream);
+wersa_status wersa_rms_norm_eight_bit(const wersa_norm_desc *desc, const void *x, const void *residual,
+                                      const float *weight, void *r, void *y, float *scales, void *hip_stream);
+size_t wersa_rms_norm_workspace_bytes(const wersa_norm_desc *desc);
+wersa_status wersa_rms_norm_backward(const wersa_norm_desc *desc, const void *r, const float *weight, const float *rstd,
+                                     const void *dy, const void *dr, void *dx, float *dweight, void *workspace,
+                                     size_t workspace_bytes, void *hip_stream);
+
 /* 1 if this descriptor runs on the MFMA path, 0 if on the generic path, -1 if rejected. */
 int32_t wersa_selected_path(const wersa_desc *desc);
 

@@ -7,6 +7,13 @@ the HIP kernels behind the C ABI).
 q, k, v: (B, H, n, d) with a shared layout (any strides, last dimension contiguous); gradients
 flow to q, k, v, sigma, gate_w, gate_b, scale_w (omega_rf is a fixed random matrix) and, for the
 block, to x and the four weight matrices (float32 gradients cast to the weights' dtype).
+
+    out, final_state = wersa_decay_attention(q, k, v, log_decay, scale, initial_state, offsets)
+    y = wersa_rms_norm(x, weight, eps=eps)
+    y, r = wersa_rms_norm(x, weight, residual, eps)
+
+q, k (B, H, n, dk), v (B, H, n, dv), each with strides of its own; gradients flow to q, k, v and initial_state (log_decay
+is fixed).  x, residual (..., cols), weight float32 (cols) or None; gradients flow to all three.
 """
 import ctypes
 import warnings
@@ -95,3 +102,63 @@ class _WersaBlock(torch.autograd.Function):
 def wersa_attention_block(x, wq, wk, wv, wo, H, omega_rf, sigma, gate_w, gate_b, scale_w, L, eps=1e-6,
                           bw_floor=1e-6):
     return _WersaBlock.apply(x, wq, wk, wv, wo, H, omega_rf, sigma, gate_w, gate_b, scale_w, L, eps, bw_floor)
+
+
+class _DecayAttention(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, v, log_decay, scale, initial_state, offsets):
+        out, final_state, saved = binding.wersa_decay_forward(q, k, v, log_decay, scale=scale, offsets=offsets, initial_state=initial_state,
+                                                              want_state=True, want_saved=True)
+        ctx.save_for_backward(q, k, v, log_decay, initial_state, offsets, saved)
+        ctx.scale = scale
+        ctx.set_materialize_grads(False)
+        return out, final_state
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dfinal):
+        q, k, v, log_decay, initial_state, offsets, saved = ctx.saved_tensors
+        dout = torch.zeros_like(v) if dout is None else _rows_apart(dout)
+        g = binding.wersa_decay_backward(q, k, v, log_decay, dout, saved, scale=ctx.scale, offsets=offsets, initial_state=initial_state,
+                                         dfinal_state=None if dfinal is None else dfinal.contiguous(), want_dinitial=ctx.needs_input_grad[5])
+        return g["dq"], g["dk"], g["dv"], None, None, g["dinitial_state"], None
+
+
+def _rows_apart(x):
+    """x with contiguous columns and rows that do not share memory (an expanded tensor is copied)."""
+    apart = x.stride(3) == 1 and all(x.stride(i) > 0 or x.shape[i] == 1 for i in range(2)) and (x.stride(2) >= x.shape[3] or x.shape[2] <= 1)
+    return x if apart else x.contiguous()
+
+
+def wersa_decay_attention(q, k, v, log_decay, scale=None, initial_state=None, offsets=None):
+    """Causal linear attention with a decay for each head.  Returns (out, final states (B, H, dk, dv) in float32)."""
+    return _DecayAttention.apply(_rows_apart(q), _rows_apart(k), _rows_apart(v), log_decay, scale, initial_state, offsets)
+
+
+class _RmsNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, residual, eps):
+        y, r, rstd = binding.wersa_rms_norm_forward(x, weight, residual=residual, eps=eps, want_rstd=True)
+        ctx.save_for_backward(x if residual is None else r, weight, rstd)
+        ctx.set_materialize_grads(False)
+        return y if residual is None else (y, r)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dr=None):
+        r, weight, rstd = ctx.saved_tensors
+        dense = lambda t: None if t is None else t.contiguous()
+        if dy is None:
+            dy = torch.zeros(r.shape, dtype=r.dtype, device=r.device)
+        dx, dw = binding.wersa_rms_norm_backward(r, rstd, dense(dy), weight, dense(dr), want_dweight=weight is not None and ctx.needs_input_grad[1])
+        return dx, dw, dx if ctx.needs_input_grad[2] else None, None
+
+
+def wersa_rms_norm(x, weight=None, residual=None, eps=1e-6):
+    """RMS norm over the last dimension: y, or (y, x + residual)."""
+    shape = x.shape
+    x = x.reshape(-1, shape[-1])
+    if residual is None:
+        return _RmsNorm.apply(x, weight, None, eps).view(shape)
+    y, r = _RmsNorm.apply(x, weight, residual.reshape(-1, shape[-1]), eps)
+    return y.view(shape), r.view(shape)

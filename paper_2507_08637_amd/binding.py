@@ -22,7 +22,9 @@ EXPORTS = ["wersa_workspace_bytes", "wersa_saved_bytes", "wersa_forward", "wersa
            "wersa_peak_copy", "wersa_peak_mfma",
            "wersa_block_workspace_bytes", "wersa_block_saved_bytes", "wersa_block_saved_offset",
            "wersa_block_workspace_offset",
-           "wersa_block_forward", "wersa_block_backward"]
+           "wersa_block_forward", "wersa_block_backward",
+           "wersa_decay_workspace_bytes", "wersa_decay_saved_bytes", "wersa_decay_forward", "wersa_decay_backward", "wersa_decay_step",
+           "wersa_rms_norm_forward", "wersa_rms_norm_eight_bit", "wersa_rms_norm_workspace_bytes", "wersa_rms_norm_backward"]
 
 
 class WersaDesc(ctypes.Structure):
@@ -31,6 +33,17 @@ class WersaDesc(ctypes.Structure):
                 ("dtype", ctypes.c_int32), ("eps", ctypes.c_float), ("bw_floor", ctypes.c_float),
                 ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
                 ("stride_n", ctypes.c_int64), ("flags", ctypes.c_int32)]
+
+
+class WersaDecayDesc(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("n", ctypes.c_int32), ("dk", ctypes.c_int32),
+                ("dv", ctypes.c_int32), ("dtype", ctypes.c_int32), ("packed", ctypes.c_int32), ("scale", ctypes.c_float)] + \
+               [(name, ctypes.c_int64 * 3) for name in ("stride_q", "stride_k", "stride_v", "stride_o")]
+
+
+class WersaNormDesc(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float),
+                ("stride_x", ctypes.c_int64), ("stride_residual", ctypes.c_int64)]
 
 
 class WersaError(RuntimeError):
@@ -88,6 +101,25 @@ def load_library():
     lib.wersa_block_backward.restype = ctypes.c_int
     lib.wersa_block_backward.argtypes = [dp] + [vp] * 6 + [fp] * 4 + [vp, vp, vp] + [fp] * 8 + \
         [vp, ctypes.c_size_t, vp]
+    ddp, ndp = ctypes.POINTER(WersaDecayDesc), ctypes.POINTER(WersaNormDesc)
+    lib.wersa_decay_workspace_bytes.restype = ctypes.c_size_t
+    lib.wersa_decay_workspace_bytes.argtypes = [ddp, ctypes.c_int]
+    lib.wersa_decay_saved_bytes.restype = ctypes.c_size_t
+    lib.wersa_decay_saved_bytes.argtypes = [ddp]
+    lib.wersa_decay_forward.restype = ctypes.c_int
+    lib.wersa_decay_forward.argtypes = [ddp] + [vp] * 8 + [ctypes.c_int32] + [vp] * 3 + [ctypes.c_size_t, vp]
+    lib.wersa_decay_backward.restype = ctypes.c_int
+    lib.wersa_decay_backward.argtypes = [ddp] + [vp] * 14 + [ctypes.c_size_t, vp]
+    lib.wersa_decay_step.restype = ctypes.c_int
+    lib.wersa_decay_step.argtypes = [ddp] + [vp] * 6 + [ctypes.c_int32, vp, vp]
+    lib.wersa_rms_norm_forward.restype = ctypes.c_int
+    lib.wersa_rms_norm_forward.argtypes = [ndp] + [vp] * 7
+    lib.wersa_rms_norm_eight_bit.restype = ctypes.c_int
+    lib.wersa_rms_norm_eight_bit.argtypes = [ndp] + [vp] * 7
+    lib.wersa_rms_norm_workspace_bytes.restype = ctypes.c_size_t
+    lib.wersa_rms_norm_workspace_bytes.argtypes = [ndp]
+    lib.wersa_rms_norm_backward.restype = ctypes.c_int
+    lib.wersa_rms_norm_backward.argtypes = [ndp] + [vp] * 8 + [ctypes.c_size_t, vp]
     lib.wersa_status_string.restype = ctypes.c_char_p
     lib.wersa_status_string.argtypes = [ctypes.c_int]
     lib.wersa_version.restype = ctypes.c_int32
@@ -428,6 +460,180 @@ def wersa_block_backward(x, wq, wk, wv, wo, H, omega_rf, sigma, gate_w, gate_b, 
                                     _ptr(g["dscale_w"]), _ptr(g["dsigma"]), _ptr(workspace),
                                     _nbytes(workspace), _stream(stream)))
     return grads
+
+
+# ---- causal linear attention with a decay for each head -------------------------------------------
+
+def _dtype_code(x):
+    if x.dtype == torch.float32:
+        return WERSA_F32
+    if x.dtype == torch.bfloat16:
+        return WERSA_BF16
+    raise TypeError("dtype must be float32 or bfloat16")
+
+
+def make_decay_desc(q, k, v, out, scale=None, offsets=None):
+    """Descriptor for q, k (B, H, n, dk) and v, out (B, H, n, dv), last dimension contiguous; with offsets (B + 1) the tensors
+    have one batch entry that holds the rows of all B sequences.  scale: 1 / sqrt(dk) by default."""
+    assert q.dim() == 4 and v.dim() == 4 and k.shape == q.shape and v.shape[:3] == q.shape[:3] and out.shape == v.shape, \
+        "expect q, k (B, H, n, dk) and v, out (B, H, n, dv)"
+    assert k.dtype == q.dtype and v.dtype == q.dtype and out.dtype == q.dtype, "q, k, v and out must share a dtype"
+    assert all(x.stride(3) == 1 for x in (q, k, v, out)), "expect a contiguous last dim"
+    N, H, n, dk = q.shape
+    B = N
+    if offsets is not None:
+        assert N == 1 and offsets.dim() == 1 and offsets.numel() >= 2 and offsets.dtype == torch.int32 and offsets.is_contiguous(), \
+            "packed sequences: tensors of one batch entry and int32 offsets (B + 1)"
+        B = offsets.numel() - 1
+    three = ctypes.c_int64 * 3
+    return WersaDecayDesc(B, H, n, dk, v.shape[3], _dtype_code(q), int(offsets is not None), dk ** -0.5 if scale is None else scale,
+                          *(three(*x.stride()[:3]) for x in (q, k, v, out)))
+
+
+def _check_states(desc, slots, *states):
+    """float32 (rows, H, dk, dv); rows = B, or any number with slots (B).  Returns the rows."""
+    rows = desc.B
+    if slots is not None:
+        assert slots.dtype == torch.int32 and slots.is_contiguous() and slots.numel() == desc.B, "slots: int32, one per sequence"
+        rows = max([s.shape[0] for s in states if s is not None], default=0)
+    for s in states:
+        if s is not None:
+            assert s.shape == (rows, desc.H, desc.dk, desc.dv) and s.is_contiguous() and s.dtype == torch.float32, \
+                "states are contiguous float32 (sequences or slots, H, dk, dv)"
+    return rows
+
+
+def _check_log_decay(log_decay, desc):
+    assert log_decay.dtype == torch.float32 and log_decay.is_contiguous() and log_decay.numel() == desc.H, "log_decay: float32, one per head"
+
+
+def wersa_decay_forward(q, k, v, log_decay, scale=None, offsets=None, initial_state=None, final_state=None, slots=None, out=None,
+                        want_state=False, want_saved=False, saved=None, workspace=None, stream=None):
+    """Returns (out, final_state, saved).  final_state: a buffer to write, or want_state=True for a new one (else None);
+    want_saved=True leaves what wersa_decay_backward needs (else None)."""
+    lib = load_library()
+    if out is None:
+        out = torch.empty_strided(v.shape, v.stride(), dtype=v.dtype, device=v.device)
+    desc = make_decay_desc(q, k, v, out, scale, offsets)
+    _check_log_decay(log_decay, desc)
+    if want_state and final_state is None:
+        assert slots is None, "with slots the states lie in a buffer of the caller's"
+        final_state = torch.empty(desc.B, desc.H, desc.dk, desc.dv, dtype=torch.float32, device=q.device)
+    rows = _check_states(desc, slots, initial_state, final_state)
+    sb = lib.wersa_decay_saved_bytes(ctypes.byref(desc))
+    if saved is not None:
+        assert _nbytes(saved) >= sb, f"saved buffer holds {_nbytes(saved)} bytes, wersa_decay_saved_bytes asks for {sb}"
+    elif want_saved:
+        saved = torch.empty(max(sb // 4, 64), dtype=torch.float32, device=q.device)
+    elif workspace is None:
+        wb = lib.wersa_decay_workspace_bytes(ctypes.byref(desc), 0)
+        workspace = _scratch(wb, q, stream) if wb > 256 else None   # (256: no scratch in it)
+    _check(lib.wersa_decay_forward(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(offsets), _ptr(initial_state),
+                                   _ptr(final_state), _ptr(slots), rows, _ptr(out), _ptr(saved), _ptr(workspace),
+                                   0 if workspace is None else _nbytes(workspace), _stream(stream)))
+    return out, final_state, saved
+
+
+def wersa_decay_backward(q, k, v, log_decay, dout, saved, scale=None, offsets=None, initial_state=None, dfinal_state=None,
+                         want_dinitial=False, workspace=None, stream=None, grads=None):
+    """Returns dict(dq, dk, dv, dinitial_state).  `grads` may be a dict from an earlier call: its tensors are then overwritten."""
+    lib = load_library()
+    desc = make_decay_desc(q, k, v, dout, scale, offsets)
+    _check_log_decay(log_decay, desc)
+    _check_states(desc, None, initial_state, dfinal_state)
+    sb = lib.wersa_decay_saved_bytes(ctypes.byref(desc))
+    assert _nbytes(saved) >= sb, f"saved buffer holds {_nbytes(saved)} bytes, wersa_decay_saved_bytes asks for {sb}"
+    if grads is None:
+        grads = {name: torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device) for name, x in (("dq", q), ("dk", k), ("dv", v))}
+        grads["dinitial_state"] = torch.empty(desc.B, desc.H, desc.dk, desc.dv, dtype=torch.float32, device=q.device) if want_dinitial else None
+    for name, x in (("dq", q), ("dk", k), ("dv", v)):
+        _same_layout(x, grads[name])
+    _check_states(desc, None, grads["dinitial_state"])
+    if workspace is None:
+        workspace = _scratch(lib.wersa_decay_workspace_bytes(ctypes.byref(desc), 1), q, stream)
+    _check(lib.wersa_decay_backward(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(offsets), _ptr(initial_state),
+                                    _ptr(dout), _ptr(dfinal_state), _ptr(saved), _ptr(grads["dq"]), _ptr(grads["dk"]), _ptr(grads["dv"]),
+                                    _ptr(grads["dinitial_state"]), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    return grads
+
+
+def wersa_decay_step(q, k, v, log_decay, state, scale=None, slots=None, out=None, stream=None):
+    """One token of each of B sequences: q, k (B, H, dk), v (B, H, dv), state (B or slots, H, dk, dv) float32, updated in place.  Returns out."""
+    lib = load_library()
+    if out is None:
+        out = torch.empty(v.shape, dtype=v.dtype, device=v.device)
+    desc = make_decay_desc(q.unsqueeze(2), k.unsqueeze(2), v.unsqueeze(2), out.unsqueeze(2), scale)
+    _check_log_decay(log_decay, desc)
+    rows = _check_states(desc, slots, state)
+    _check(lib.wersa_decay_step(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(state), _ptr(slots), rows, _ptr(out),
+                                _stream(stream)))
+    return out
+
+
+# ---- root-mean-square norm with the residual's addition --------------------------------------------
+
+def _norm_args(x, weight, residual, eps, r):
+    """(rows, cols) tensors, columns contiguous; returns the descriptor and the stream's buffer (None without a residual)."""
+    assert x.dim() == 2 and x.stride(1) == 1, "expect (rows, cols) with contiguous columns"
+    rows, cols = x.shape
+    if weight is not None:
+        assert weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == cols, "weight: float32, one per column"
+    if residual is not None:
+        assert residual.shape == x.shape and residual.dtype == x.dtype and residual.stride(1) == 1, "the residual has x's shape and dtype"
+        if r is None:
+            r = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        assert r.shape == x.shape and r.dtype == x.dtype and r.is_contiguous()
+    strides = (x.stride(0), cols if residual is None else residual.stride(0))
+    return WersaNormDesc(rows, cols, _dtype_code(x), eps, *strides), r if residual is not None else None
+
+
+def wersa_rms_norm_forward(x, weight=None, residual=None, eps=1e-6, r=None, y=None, rstd=None, want_rstd=False, stream=None):
+    """Returns (y, r, rstd): r = x + residual (x itself without one), rstd (rows) float32 or None."""
+    desc, stream_out = _norm_args(x, weight, residual, eps, r)
+    if y is None:
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    assert y.shape == x.shape and y.dtype == x.dtype and y.is_contiguous()
+    if want_rstd and rstd is None:
+        rstd = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    assert rstd is None or (rstd.numel() == x.shape[0] and rstd.dtype == torch.float32 and rstd.is_contiguous())
+    _check(load_library().wersa_rms_norm_forward(ctypes.byref(desc), _ptr(x), _ptr(residual), _ptr(weight), _ptr(stream_out), _ptr(y), _ptr(rstd),
+                                                 _stream(stream)))
+    return y, x if residual is None else stream_out, rstd
+
+
+def wersa_rms_norm_eight_bit(x, weight=None, residual=None, eps=1e-6, r=None, y=None, scales=None, stream=None):
+    """Returns (y, r, scales): y (rows, cols) float8_e4m3fn, to be multiplied by scales (rows) float32."""
+    desc, stream_out = _norm_args(x, weight, residual, eps, r)
+    if y is None:
+        y = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+    if scales is None:
+        scales = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
+    assert y.shape == x.shape and y.dtype == torch.float8_e4m3fn and y.is_contiguous()
+    assert scales.numel() == x.shape[0] and scales.dtype == torch.float32 and scales.is_contiguous()
+    _check(load_library().wersa_rms_norm_eight_bit(ctypes.byref(desc), _ptr(x), _ptr(residual), _ptr(weight), _ptr(stream_out), _ptr(y),
+                                                   _ptr(scales), _stream(stream)))
+    return y, x if residual is None else stream_out, scales
+
+
+def wersa_rms_norm_backward(r, rstd, dy, weight=None, dr=None, dx=None, want_dweight=True, dweight=None, workspace=None, stream=None):
+    """Returns (dx, dweight): dx is the gradient of x and of the residual; dr: what reaches the stream r from elsewhere."""
+    lib = load_library()
+    desc, _ = _norm_args(r, weight, None, 0.0, None)
+    for t in (dy, dr):
+        assert t is None or (t.shape == r.shape and t.dtype == r.dtype and t.is_contiguous()), "dy and dr are dense, of r's shape and dtype"
+    assert rstd.numel() == r.shape[0] and rstd.dtype == torch.float32 and rstd.is_contiguous()
+    if dx is None:
+        dx = torch.empty(r.shape, dtype=r.dtype, device=r.device)
+    assert dx.shape == r.shape and dx.dtype == r.dtype and dx.is_contiguous()
+    if want_dweight and dweight is None:
+        dweight = torch.empty(r.shape[1], dtype=torch.float32, device=r.device)
+    if dweight is not None:
+        assert dweight.numel() == r.shape[1] and dweight.dtype == torch.float32 and dweight.is_contiguous()
+        if workspace is None:
+            workspace = _scratch(lib.wersa_rms_norm_workspace_bytes(ctypes.byref(desc)), r, stream)
+    _check(lib.wersa_rms_norm_backward(ctypes.byref(desc), _ptr(r), _ptr(weight), _ptr(rstd), _ptr(dy), _ptr(dr), _ptr(dx), _ptr(dweight),
+                                       _ptr(workspace), 0 if workspace is None else _nbytes(workspace), _stream(stream)))
+    return dx, dweight
 
 
 def wersa_profile_enable(on, only=None):

@@ -10,7 +10,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libwersa.so")
 NODE = os.path.join(HERE, "_wersa_torch.so")
 SOURCES = ["wersa_api.hip", "wersa_generic.hip", "wersa_profile.hip", "wersa_fast.hip",
-           "wersa_block.hip", "wersa_split.hip"]
+           "wersa_block.hip", "wersa_split.hip", "wersa_decay.hip", "wersa_norm.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

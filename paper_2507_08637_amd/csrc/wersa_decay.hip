@@ -1,0 +1,601 @@
+// Causal linear attention with a decay for each head: per (sequence, head)
+//   S_t = lambda S_{t-1} + k_t v_t^T  (dk x dv),   o_t = scale q_t^T S_t,   lambda = exp(log_decay[h])
+//
+// Whole sequences go in chunks of 64 rows.  With D_ts = lambda^(t-s) for s <= t, else 0, and S the state before the chunk
+//   O  = (scale (Q K^T) o D) V + scale diag(lambda^(t+1)) Q S,     S' = lambda^64 S + (K o lambda^(63-s))^T V
+// A workgroup walks the chunks of one segment of a sequence with S in registers.  Where (sequence, head) pairs alone do not
+// fill the device, sequences are split into segments: one launch forms what every segment adds to the state, one
+// adds these up to the states that the segments begin with, and the walk starts everywhere at once.
+//
+// The derivative is three more walks.  With G_t = dL/dS_t, G_t = lambda G_{t+1} + scale q_t do_t^T:
+//   dq_t = scale S_t do_t     the walk with (do, v, k) in the place of (q, k, v)
+//   dk_t = G_t v_t            the walk from the last row to the first, with (v, do, q)
+//   dv_t = G_t^T k_t          the same with (k, q, do)
+// The walk back multiplies with lambda after a row where the walk forward does before it: `shift` below.
+#include "wersa_internal.h"
+
+#include <type_traits>
+
+namespace wersa {
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+// Rows of a tensor may begin at any element: vector accesses to global memory need no more than the element's alignment on this device.
+template <typename V> struct Any {
+  typedef V type __attribute__((aligned(2)));
+};
+
+constexpr int kChunk = 64;
+
+// lambda^e for e >= 0.  The clamp keeps 0 * log_decay apart from 0 * inf: a decay of zero (log_decay = -inf) leaves lambda^0 = 1.
+__device__ __forceinline__ float log2_decay(const float *log_decay, int h) { return (log_decay[h] < -1e4f ? -1e4f : log_decay[h]) * 1.44269504f; }
+__device__ __forceinline__ float decay_pow(float l2, int e) { return exp2f(l2 * (float)e); }
+
+struct Strides {
+  int64_t b, h, n;
+};
+
+// The rows of one sequence, and of one segment of it.  Packed sequences lie in rows offsets[b] .. offsets[b + 1] of one tensor.  Segment s of
+// sequence b has slot floor(begin / seg) + b + s: the slots of a sequence lie behind those of the one before it whatever the lengths are, so that the grid
+// is known without them; some slots stay empty.  Offsets are clamped into the tensor: no value of theirs leads out of it.
+struct Sequences {
+  const int32_t *offsets;   // null: B sequences of n rows each
+  int B, n, seg, segs;      // segs: segments of a sequence that is not packed
+  __host__ __device__ int slots() const { return offsets ? n / seg + B : B * segs; }
+  __device__ __forceinline__ int begin(int b) const { return offsets ? min(max(offsets[b], 0), n) : 0; }
+  __device__ __forceinline__ int rows(int b) const { return offsets ? max(min(offsets[b + 1], n) - begin(b), 0) : n; }
+  __device__ __forceinline__ int first_slot(int b) const { return offsets ? begin(b) / seg + b : b * segs; }
+  __device__ __forceinline__ int segments(int b) const { return offsets ? max(1, (rows(b) + seg - 1) / seg) : segs; }
+};
+struct Segment {
+  int b, s, rows;           // rows == -1: nothing here
+  int64_t row0;
+};
+__device__ __forceinline__ Segment segment_of(const Sequences &q, int slot) {
+  Segment r;
+  if (!q.offsets) {
+    r.b = slot / q.segs;
+    r.s = slot % q.segs;
+  } else {
+    int lo = 0, hi = q.B - 1;   // the last sequence that does not begin behind this slot
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) >> 1;
+      if (q.first_slot(mid) <= slot) lo = mid; else hi = mid - 1;
+    }
+    r.b = lo;
+    r.s = slot - q.first_slot(lo);
+  }
+  const int have = q.rows(r.b);
+  r.row0 = (int64_t)q.begin(r.b) + (int64_t)r.s * q.seg;
+  r.rows = r.s < 0 || r.s >= q.segments(r.b) ? -1 : min(q.seg, have - r.s * q.seg);
+  return r;
+}
+
+struct Walk {
+  const void *q, *k, *v;
+  void *o;
+  Strides sq, sk, sv, so;
+  const float *log_decay;
+  const float *init;        // states that the walk begins with: by slot (by_slot) or by sequence; null: zeros
+  float *fin;               // states that it ends with, by sequence (or local sums by slot: STATES)
+  const int32_t *cache;     // rows of init and fin (by sequence) that the sequences have, null: sequence b has row b
+  int cache_rows;
+  Sequences seq;
+  int H, kw, vw;            // widths of k and v
+  int64_t si, sj;           // strides of a state's rows (k) and columns (v)
+  float intra, inter, gain; // factors of the chunk's products, of the state's part and of what goes into the state
+  bool by_slot, reverse;
+};
+
+__device__ __forceinline__ int cache_row(const Walk &a, int b) {   // -1: none
+  const int r = a.cache ? a.cache[b] : b;
+  return r < 0 || r >= a.cache_rows ? -1 : r;
+}
+
+// Raw pieces of a row: 16 bytes for the tiles, four elements for queries and outputs.
+template <typename T> struct Raw;
+template <> struct Raw<float> {
+  static constexpr int PIECE = 4;
+  typedef u32x4 Four;
+  static __device__ __forceinline__ void spread(const u32x4 &p, float *out) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[i] = __uint_as_float(p[i]);
+  }
+  static __device__ __forceinline__ f32x4 four(const Four &p) {
+    return f32x4{__uint_as_float(p[0]), __uint_as_float(p[1]), __uint_as_float(p[2]), __uint_as_float(p[3])};
+  }
+  static __device__ __forceinline__ Four pack(f32x4 v) {
+    return Four{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
+  }
+};
+template <> struct Raw<bf16_t> {
+  static constexpr int PIECE = 8;
+  typedef u32x2 Four;
+  static __device__ __forceinline__ void spread(const u32x4 &p, float *out) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      out[2 * i] = __uint_as_float(p[i] << 16);
+      out[2 * i + 1] = __uint_as_float(p[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ f32x4 four(const Four &p) {
+    return f32x4{__uint_as_float(p[0] << 16), __uint_as_float(p[0] & 0xffff0000u), __uint_as_float(p[1] << 16), __uint_as_float(p[1] & 0xffff0000u)};
+  }
+  static __device__ __forceinline__ Four pack(f32x4 v) {
+    return Four{(uint32_t)f32_to_bf16(v[0]) | (uint32_t)f32_to_bf16(v[1]) << 16, (uint32_t)f32_to_bf16(v[2]) | (uint32_t)f32_to_bf16(v[3]) << 16};
+  }
+};
+template <typename V, typename T> __device__ __forceinline__ V load_raw(const T *p, bool ok) {
+  V r{};
+  if (ok) r = *reinterpret_cast<const typename Any<V>::type *>(p);
+  return r;
+}
+template <typename V, typename T> __device__ __forceinline__ void store_raw(T *p, const V &v) { *reinterpret_cast<typename Any<V>::type *>(p) = v; }
+
+// ---- float32 matrix instructions -----------------------------------------------------------------
+// v_mfma_f32_16x16x4_f32 (c = lane % 16, g = lane / 16): A row c, k = g;  B column c, k = g;  C/D: acc[i] is row 4 g + i, column c.
+// Four of them take k = 4 g + i of a 16-wide slice: four consecutive values per lane.
+__device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
+
+// Four waves.  Wave w has rows 16 w .. of the chunk for the output and rows (DK / 4) w .. of the state.  P is formed as its transpose (key
+// rows down the registers, query rows on the lanes), which is the layout that the product with V takes it in.
+template <typename T, int DK, int DV, bool STATES>
+__global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
+  constexpr int LK = DK + 4, LV = DV + 4, PIECE = Raw<T>::PIECE;
+  constexpr int PK = kChunk * DK / PIECE / 256, PV = kChunk * DV / PIECE / 256;   // pieces of a thread
+  constexpr int RT = DK / 64, CT = DV / 16;                                         // state: row tiles of a wave, column tiles
+  extern __shared__ __align__(16) float lds[];
+  float *Ks = lds, *Vs = Ks + kChunk * LK, *weight = Vs + kChunk * LV, *St = weight + kChunk;
+  const Segment seg = segment_of(a.seq, blockIdx.x);
+  if (seg.rows < 0) return;
+  const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const bool last = a.reverse ? seg.s == 0 : seg.s == a.seq.segments(seg.b) - 1;
+  if (STATES && last) return;   // nothing begins with what the last one adds
+  const int64_t b_at = a.seq.offsets ? 0 : seg.b;
+  // logical row r of the segment is row at + r * dir
+  const int64_t at = a.reverse ? seg.row0 + seg.rows - 1 : seg.row0, dir = a.reverse ? -1 : 1;
+  const int shift = a.reverse ? 1 : 0;
+  const T *q = (const T *)a.q + b_at * a.sq.b + h * a.sq.h + at * a.sq.n, *k = (const T *)a.k + b_at * a.sk.b + h * a.sk.h + at * a.sk.n,
+          *v = (const T *)a.v + b_at * a.sv.b + h * a.sv.h + at * a.sv.n;
+  T *o = (T *)a.o + b_at * a.so.b + h * a.so.h + at * a.so.n;
+  const float l2 = log2_decay(a.log_decay, h);
+  const int64_t state_size = (int64_t)a.kw * a.vw;
+
+  // state: S[rt][ct][i] is row 16 (RT w + rt) + 4 g + i, column 16 ct + c
+  f32x4 S[RT][CT];
+  const int own = cache_row(a, seg.b);
+  const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
+  const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 16 * (RT * w + rt) + 4 * g + i, col = 16 * ct + c;
+        S[rt][ct][i] = init && r < a.kw && col < a.vw ? init[r * a.si + col * a.sj] : 0.f;
+      }
+
+  float factor[4][4];   // of P, by key tile
+#pragma unroll
+  for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = 16 * (w - jt) + c - 4 * g - i;
+      factor[jt][i] = e >= 0 ? a.intra * decay_pow(l2, e) : 0.f;
+    }
+  const float reach = a.inter * decay_pow(l2, 16 * w + c + 1 - shift);
+
+  u32x4 rk[PK], rv[PV];
+  typename Raw<T>::Four rq[DK / 16];
+  auto request = [&](int r0) {
+#pragma unroll
+    for (int i = 0; i < PK; ++i) {
+      const int p = tid + 256 * i, row = r0 + p / (DK / PIECE), col = p % (DK / PIECE) * PIECE;
+      rk[i] = load_raw<u32x4>(k + row * dir * a.sk.n + col, row < seg.rows && col < a.kw);
+    }
+#pragma unroll
+    for (int i = 0; i < PV; ++i) {
+      const int p = tid + 256 * i, row = r0 + p / (DV / PIECE), col = p % (DV / PIECE) * PIECE;
+      rv[i] = load_raw<u32x4>(v + row * dir * a.sv.n + col, row < seg.rows && col < a.vw);
+    }
+    if (!STATES) {
+      const int row = r0 + 16 * w + c;
+#pragma unroll
+      for (int j = 0; j < DK / 16; ++j)
+        rq[j] = load_raw<typename Raw<T>::Four>(q + row * dir * a.sq.n + 16 * j + 4 * g, row < seg.rows && 16 * j + 4 * g < a.kw);
+    }
+  };
+
+  request(0);
+  for (int r0 = 0; r0 < seg.rows; r0 += kChunk) {
+    const int rows = min(kChunk, seg.rows - r0);
+    // what was requested, and the state, into LDS
+#pragma unroll
+    for (int i = 0; i < PK; ++i) {
+      const int p = tid + 256 * i;
+      float e[PIECE];
+      Raw<T>::spread(rk[i], e);
+#pragma unroll
+      for (int j = 0; j < PIECE; j += 4)
+        *(f32x4 *)(Ks + p / (DK / PIECE) * LK + p % (DK / PIECE) * PIECE + j) = f32x4{e[j], e[j + 1], e[j + 2], e[j + 3]};
+    }
+#pragma unroll
+    for (int i = 0; i < PV; ++i) {
+      const int p = tid + 256 * i;
+      float e[PIECE];
+      Raw<T>::spread(rv[i], e);
+#pragma unroll
+      for (int j = 0; j < PIECE; j += 4)
+        *(f32x4 *)(Vs + p / (DV / PIECE) * LV + p % (DV / PIECE) * PIECE + j) = f32x4{e[j], e[j + 1], e[j + 2], e[j + 3]};
+    }
+    if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + shift);
+    f32x4 Q[DK / 16];
+    if (!STATES) {
+#pragma unroll
+      for (int j = 0; j < DK / 16; ++j) Q[j] = Raw<T>::four(rq[j]);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct) *(f32x4 *)(St + (16 * ct + c) * LK + 16 * (RT * w + rt) + 4 * g) = S[rt][ct];
+    }
+    __syncthreads();
+    request(r0 + kChunk);
+
+    f32x4 O[CT];
+    if (!STATES) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) {
+        O[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < DK / 16; ++j) {
+          const f32x4 s = *(const f32x4 *)(St + (16 * ct + c) * LK + 16 * j + 4 * g);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) O[ct] = mfma_f32(s[i], Q[j][i], O[ct]);
+        }
+        O[ct] *= reach;
+      }
+    }
+    const float keep = decay_pow(l2, rows);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct) S[rt][ct] *= keep;
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt) {
+      float V[CT][4];
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) V[ct][i] = Vs[(16 * jt + 4 * g + i) * LV + 16 * ct + c];
+      if (!STATES && jt <= w) {
+        f32x4 P = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < DK / 16; ++j) {
+          const f32x4 s = *(const f32x4 *)(Ks + (16 * jt + c) * LK + 16 * j + 4 * g);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) P = mfma_f32(s[i], Q[j][i], P);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) P[i] = jt < w || c >= 4 * g + i ? P[i] * factor[jt][i] : 0.f;
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) O[ct] = mfma_f32(V[ct][i], P[i], O[ct]);
+      }
+      const f32x4 wt = *(const f32x4 *)(weight + 16 * jt + 4 * g);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float kt = Ks[(16 * jt + 4 * g + i) * LK + 16 * (RT * w + rt) + c] * wt[i];
+#pragma unroll
+          for (int ct = 0; ct < CT; ++ct) S[rt][ct] = mfma_f32(kt, V[ct][i], S[rt][ct]);
+        }
+    }
+    if (!STATES && 16 * w + c < rows) {
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+        if (16 * ct + 4 * g < a.vw) store_raw(o + (r0 + 16 * w + c) * dir * a.so.n + 16 * ct + 4 * g, Raw<T>::pack(O[ct]));
+    }
+    __syncthreads();
+  }
+
+  float *fin = nullptr;
+  if (STATES) fin = a.fin + ((int64_t)blockIdx.x * a.H + h) * state_size;
+  else if (last && a.fin && own >= 0) fin = a.fin + ((int64_t)own * a.H + h) * state_size;
+  if (fin) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 16 * (RT * w + rt) + 4 * g + i, col = 16 * ct + c;
+          if (r < a.kw && col < a.vw) fin[r * a.si + col * a.sj] = S[rt][ct][i];
+        }
+  }
+}
+
+// What the segments of a sequence add to the state, in place, to the states that they begin with: four values of a state per thread, over all
+// segments in their order (from the last one with `reverse`), eight of them requested at a time.
+__global__ __launch_bounds__(64) void scan_kernel(Walk a, float *local) {
+  const int h = blockIdx.y, b = blockIdx.z;
+  const int64_t state_size = (int64_t)a.kw * a.vw, e = ((int64_t)blockIdx.x * 64 + threadIdx.x) * 4;
+  if (e >= state_size) return;
+  const int segs = a.seq.segments(b), have = a.seq.rows(b), own = cache_row(a, b);
+  const float l2 = log2_decay(a.log_decay, h);
+  f32x4 run = a.init && own >= 0 ? *(const f32x4 *)(a.init + ((int64_t)own * a.H + h) * state_size + e) : f32x4{0.f, 0.f, 0.f, 0.f};
+  const int64_t step = a.H * state_size;
+  float *p = local + ((int64_t)a.seq.first_slot(b) * a.H + h) * state_size + e;
+  const float full = decay_pow(l2, a.seq.seg), tail = decay_pow(l2, have - (segs - 1) * a.seq.seg);
+  for (int s0 = 0; s0 < segs; s0 += 8) {
+    f32x4 x[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const int s = a.reverse ? segs - 1 - s0 - u : s0 + u;
+      if (s0 + u < segs - 1) x[u] = *(const f32x4 *)(p + s * step);   // the last one has added nothing
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      if (s0 + u >= segs) break;
+      const int s = a.reverse ? segs - 1 - s0 - u : s0 + u;
+      *(f32x4 *)(p + s * step) = run;
+      if (s0 + u < segs - 1) run = run * (s == segs - 1 ? tail : full) + x[u];
+    }
+  }
+}
+
+// ---- one token -------------------------------------------------------------------------------------
+// S <- lambda S + k v^T, o = scale q^T S.  Bound by the state's way through memory.  A workgroup has W columns of a state, W / 4 threads to a
+// row (16 bytes each), all rows of a thread requested before the first is used.
+struct Step {
+  const void *q, *k, *v;
+  void *o;
+  Strides sq, sk, sv, so;
+  const float *log_decay;
+  float *state;
+  const int32_t *cache;
+  int cache_rows, H, kw, vw;
+  float scale;
+};
+template <typename T, int W>
+__global__ __launch_bounds__(256) void step_kernel(Step a) {
+  constexpr int TPR = W / 4, ROWS = 256 / TPR, PASS = (128 + ROWS - 1) / ROWS;
+  const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, col = blockIdx.x * W + tid % TPR * 4, r0 = tid / TPR;
+  __shared__ f32x4 part[4][TPR];
+  const int own0 = a.cache ? a.cache[b] : b, own = own0 < 0 || own0 >= a.cache_rows ? -1 : own0;
+  const T *q = (const T *)a.q + b * a.sq.b + h * a.sq.h, *k = (const T *)a.k + b * a.sk.b + h * a.sk.h, *v = (const T *)a.v + b * a.sv.b + h * a.sv.h;
+  T *o = (T *)a.o + b * a.so.b + h * a.so.h;
+  f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+  if (own >= 0 && col < a.vw) {
+    float *s = a.state + ((int64_t)own * a.H + h) * a.kw * a.vw + col;
+    f32x4 x[PASS];
+#pragma unroll
+    for (int u = 0; u < PASS; ++u)
+      if (r0 + u * ROWS < a.kw) x[u] = *(const f32x4 *)(s + (r0 + u * ROWS) * a.vw);
+    const float lambda = decay_pow(log2_decay(a.log_decay, h), 1);
+    f32x4 vv;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) vv[i] = ld(v + col + i);
+#pragma unroll
+    for (int u = 0; u < PASS; ++u)
+      if (r0 + u * ROWS < a.kw) {
+        const float kk = ld(k + r0 + u * ROWS), qq = ld(q + r0 + u * ROWS);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[u][i] = x[u][i] * lambda + kk * vv[i];
+          sum[i] += qq * x[u][i];
+        }
+        *(f32x4 *)(s + (r0 + u * ROWS) * a.vw) = x[u];
+      }
+  }
+  // over the rows: lanes of a wave, then the four waves
+#pragma unroll
+  for (int d = TPR; d < 64; d *= 2)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += __shfl_xor(sum[i], d);
+  if ((tid & 63) < TPR) part[tid >> 6][tid & 63] = sum;
+  __syncthreads();
+  if (tid < TPR && col < a.vw) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) st(o + col + i, a.scale * ((part[0][tid][i] + part[1][tid][i]) + (part[2][tid][i] + part[3][tid][i])));
+  }
+}
+
+// ---- host ------------------------------------------------------------------------------------------
+constexpr int kSegmentsWanted = 768;   // workgroups that a walk should have
+
+int segment_rows(const wersa_decay_desc &c) {
+  const int64_t slices = (int64_t)c.H * (c.packed ? 1 : c.B);
+  const int64_t want = kSegmentsWanted / slices;   // segments of a slice
+  if (want <= 1) return c.packed ? INT32_MAX / 2 : (c.n + kChunk - 1) / kChunk * kChunk + kChunk;
+  int64_t rows = ((int64_t)c.n + want - 1) / want;
+  rows = (rows + kChunk - 1) / kChunk * kChunk;
+  return (int)(rows < 4 * kChunk ? 4 * kChunk : rows);
+}
+Sequences sequences(const wersa_decay_desc &c, const int32_t *offsets) {
+  Sequences s;
+  s.offsets = offsets;
+  s.B = c.B;
+  s.n = c.n;
+  s.seg = segment_rows(c);
+  s.segs = c.n > 0 ? (c.n + s.seg - 1) / s.seg : 1;
+  return s;
+}
+int64_t state_slots_of(const wersa_decay_desc &c) {   // 0: every sequence is one segment
+  const int seg = segment_rows(c);
+  if (c.n <= seg) return 0;
+  return c.packed ? (int64_t)c.n / seg + c.B : (int64_t)c.B * ((c.n + seg - 1) / seg);
+}
+size_t states_bytes(const wersa_decay_desc &c) { return (size_t)state_slots_of(c) * c.H * c.dk * c.dv * sizeof(float); }
+
+bool strides_ok(const int64_t *s, const wersa_decay_desc &c, int width) {
+  if (s[0] < 0 || s[1] < 0 || s[2] < 0) return false;
+  if (!c.packed && c.B > 1 && s[0] == 0) return false;
+  if (c.H > 1 && s[1] == 0) return false;
+  return c.n <= 1 || s[2] >= width;
+}
+wersa_status validate(const wersa_decay_desc *c) {
+  if (!c) return WERSA_ERR_INVALID_ARG;
+  if (c->B < 1 || c->H < 1 || c->n < 0 || c->dk < 1 || c->dv < 1) return WERSA_ERR_INVALID_ARG;
+  if (c->dtype != WERSA_F32 && c->dtype != WERSA_BF16) return WERSA_ERR_INVALID_ARG;
+  if (c->packed != 0 && c->packed != 1) return WERSA_ERR_INVALID_ARG;
+  if (!(c->scale - c->scale == 0.f)) return WERSA_ERR_INVALID_ARG;   // not finite
+  if (!strides_ok(c->stride_q, *c, c->dk) || !strides_ok(c->stride_k, *c, c->dk) || !strides_ok(c->stride_v, *c, c->dv) ||
+      !strides_ok(c->stride_o, *c, c->dv))
+    return WERSA_ERR_INVALID_ARG;
+  if (c->dk % 16 != 0 || c->dv % 16 != 0 || c->dk > 128 || c->dv > 128) return WERSA_ERR_UNSUPPORTED;
+  if (c->H > 65535 || c->B > 65535 || c->n > (1 << 30)) return WERSA_ERR_UNSUPPORTED;
+  return WERSA_OK;
+}
+bool misaligned(const void *p, size_t a) { return ((uintptr_t)p % a) != 0; }
+Strides strides(const int64_t *s) { return Strides{s[0], s[1], s[2]}; }
+template <typename T, int DK, int DV, bool STATES>
+bool launch_walk_as(const Walk &a, hipStream_t st) {
+  constexpr size_t smem = sizeof(float) * (kChunk * (DK + 4 + DV + 4 + 1) + (STATES ? 0 : DV * (DK + 4)));
+  auto kern = &walk_f32_kernel<T, DK, DV, STATES>;
+  if (smem > 65536 &&
+      hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess)
+    return false;
+  WERSA_STAGE(STATES ? "wersa_decay_states" : "wersa_decay_walk", st, kern<<<dim3(a.seq.slots(), a.H), 256, smem, st>>>(a));
+  return true;
+}
+template <bool STATES> bool launch_walk(const wersa_decay_desc &c, const Walk &a, hipStream_t st) {
+  const bool f32 = c.dtype == WERSA_F32;
+  if (a.kw <= 64 && a.vw <= 64) return f32 ? launch_walk_as<float, 64, 64, STATES>(a, st) : launch_walk_as<bf16_t, 64, 64, STATES>(a, st);
+  if (a.kw <= 64) return f32 ? launch_walk_as<float, 64, 128, STATES>(a, st) : launch_walk_as<bf16_t, 64, 128, STATES>(a, st);
+  if (a.vw <= 64) return f32 ? launch_walk_as<float, 128, 64, STATES>(a, st) : launch_walk_as<bf16_t, 128, 64, STATES>(a, st);
+  return f32 ? launch_walk_as<float, 128, 128, STATES>(a, st) : launch_walk_as<bf16_t, 128, 128, STATES>(a, st);
+}
+void launch_scan(const Walk &a, float *local, hipStream_t st) {
+  WERSA_STAGE("wersa_decay_scan", st, scan_kernel<<<dim3((a.kw * a.vw / 4 + 63) / 64, a.H, a.seq.B), 64, 0, st>>>(a, local));
+}
+
+}  // namespace
+}  // namespace wersa
+
+using namespace wersa;
+
+extern "C" {
+
+size_t wersa_decay_workspace_bytes(const wersa_decay_desc *desc, int for_backward) {
+  (void)for_backward;
+  return validate(desc) == WERSA_OK ? states_bytes(*desc) + 256 : 0;
+}
+
+size_t wersa_decay_saved_bytes(const wersa_decay_desc *desc) { return validate(desc) == WERSA_OK ? states_bytes(*desc) + 256 : 0; }
+
+wersa_status wersa_decay_forward(const wersa_decay_desc *desc, const void *q, const void *k, const void *v, const float *log_decay,
+                                 const int32_t *offsets, const float *initial_state, float *final_state, const int32_t *slots,
+                                 int32_t state_slots, void *out, void *saved, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  const wersa_status vs = validate(desc);
+  if (vs != WERSA_OK) return vs;
+  const wersa_decay_desc &c = *desc;
+  if (c.n > 0 && (!q || !k || !v || !out)) return WERSA_ERR_INVALID_ARG;
+  if (!log_decay || (c.packed != 0) != (offsets != nullptr)) return WERSA_ERR_INVALID_ARG;
+  if ((initial_state || final_state) && state_slots < (slots ? 1 : c.B)) return WERSA_ERR_INVALID_ARG;
+  if (misaligned(initial_state, 16) || misaligned(final_state, 16)) return WERSA_ERR_INVALID_ARG;
+  const bool split = state_slots_of(c) > 0;
+  if (split && !saved && (!workspace || workspace_bytes < states_bytes(c) || misaligned(workspace, 256))) return WERSA_ERR_WORKSPACE;
+  if (misaligned(saved, 256)) return WERSA_ERR_WORKSPACE;
+  hipStream_t st = (hipStream_t)hip_stream;
+  Walk a{};
+  a.q = q, a.k = k, a.v = v, a.o = out;
+  a.sq = strides(c.stride_q), a.sk = strides(c.stride_k), a.sv = strides(c.stride_v), a.so = strides(c.stride_o);
+  a.log_decay = log_decay;
+  a.init = initial_state, a.cache = slots, a.cache_rows = state_slots;
+  a.seq = sequences(c, offsets);
+  a.H = c.H, a.kw = c.dk, a.vw = c.dv, a.si = c.dv, a.sj = 1;
+  a.intra = a.inter = c.scale, a.gain = 1.f;
+  if (split) {
+    float *local = (float *)(saved ? saved : workspace);
+    a.fin = local;
+    if (!launch_walk<true>(c, a, st)) return WERSA_ERR_LAUNCH;
+    launch_scan(a, local, st);
+    a.init = local, a.by_slot = true;
+  }
+  a.fin = final_state;
+  if (!launch_walk<false>(c, a, st)) return WERSA_ERR_LAUNCH;
+  return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
+}
+
+wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, const void *k, const void *v, const float *log_decay,
+                                  const int32_t *offsets, const float *initial_state, const void *dout, const float *dfinal_state,
+                                  const void *saved, void *dq, void *dk, void *dv, float *dinitial_state, void *workspace,
+                                  size_t workspace_bytes, void *hip_stream) {
+  const wersa_status vs = validate(desc);
+  if (vs != WERSA_OK) return vs;
+  const wersa_decay_desc &c = *desc;
+  if (c.n > 0 && (!q || !k || !v || !dout || !dq || !dk || !dv)) return WERSA_ERR_INVALID_ARG;
+  if (!log_decay || (c.packed != 0) != (offsets != nullptr)) return WERSA_ERR_INVALID_ARG;
+  if (misaligned(initial_state, 16) || misaligned(dfinal_state, 16) || misaligned(dinitial_state, 16)) return WERSA_ERR_INVALID_ARG;
+  const bool split = state_slots_of(c) > 0;
+  if (split && !saved) return WERSA_ERR_INVALID_ARG;
+  if (misaligned(saved, 256) || (split && (!workspace || workspace_bytes < states_bytes(c) || misaligned(workspace, 256))))
+    return WERSA_ERR_WORKSPACE;
+  hipStream_t st = (hipStream_t)hip_stream;
+  Walk a{};
+  a.log_decay = log_decay;
+  a.cache_rows = c.B;
+  a.seq = sequences(c, offsets);
+  a.H = c.H;
+  const Strides sq = strides(c.stride_q), sk = strides(c.stride_k), sv = strides(c.stride_v), so = strides(c.stride_o);
+  // dq: states transposed
+  Walk f = a;
+  f.q = dout, f.k = v, f.v = k, f.o = dq;
+  f.sq = so, f.sk = sv, f.sv = sk, f.so = sq;
+  f.kw = c.dv, f.vw = c.dk, f.si = 1, f.sj = c.dv;
+  f.intra = f.inter = c.scale, f.gain = 1.f;
+  f.init = split ? (const float *)saved : initial_state;
+  f.by_slot = split;
+  if (!launch_walk<false>(c, f, st)) return WERSA_ERR_LAUNCH;
+  // dv, and the gradient of the state
+  a.reverse = true;
+  a.intra = c.scale, a.inter = 1.f, a.gain = c.scale;
+  a.init = dfinal_state;
+  Walk r = a;
+  r.q = k, r.k = q, r.v = dout, r.o = dv;
+  r.sq = sk, r.sk = sq, r.sv = so, r.so = sv;
+  r.kw = c.dk, r.vw = c.dv, r.si = c.dv, r.sj = 1;
+  if (split) {
+    r.fin = (float *)workspace;
+    if (!launch_walk<true>(c, r, st)) return WERSA_ERR_LAUNCH;
+    launch_scan(r, (float *)workspace, st);
+    a.init = r.init = (const float *)workspace;
+    a.by_slot = r.by_slot = true;
+  }
+  r.fin = dinitial_state;
+  if (!launch_walk<false>(c, r, st)) return WERSA_ERR_LAUNCH;
+  a.q = v, a.k = dout, a.v = q, a.o = dk;
+  a.sq = sv, a.sk = so, a.sv = sq, a.so = sk;
+  a.kw = c.dv, a.vw = c.dk, a.si = 1, a.sj = c.dv;
+  if (!launch_walk<false>(c, a, st)) return WERSA_ERR_LAUNCH;
+  return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
+}
+
+wersa_status wersa_decay_step(const wersa_decay_desc *desc, const void *q, const void *k, const void *v, const float *log_decay,
+                              float *state, const int32_t *slots, int32_t state_slots, void *out, void *hip_stream) {
+  const wersa_status vs = validate(desc);
+  if (vs != WERSA_OK) return vs;
+  const wersa_decay_desc &c = *desc;
+  if (c.n != 1 || c.packed || !q || !k || !v || !log_decay || !state || !out) return WERSA_ERR_INVALID_ARG;
+  if (state_slots < (slots ? 1 : c.B) || misaligned(state, 16)) return WERSA_ERR_INVALID_ARG;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const Step a{q, k, v, out, strides(c.stride_q), strides(c.stride_k), strides(c.stride_v), strides(c.stride_o), log_decay, state, slots,
+               state_slots, c.H, c.dk, c.dv, c.scale};
+  auto launch = [&](auto w) {
+    constexpr int W = decltype(w)::value;
+    const dim3 grid((c.dv + W - 1) / W, c.H, c.B);
+    if (c.dtype == WERSA_F32) WERSA_STAGE("wersa_decay_step", st, (step_kernel<float, W><<<grid, 256, 0, st>>>(a)));
+    else WERSA_STAGE("wersa_decay_step", st, (step_kernel<bf16_t, W><<<grid, 256, 0, st>>>(a)));
+  };
+  const int64_t states = (int64_t)c.B * c.H;
+  if (states >= 256) c.dv <= 64 ? launch(std::integral_constant<int, 64>{}) : launch(std::integral_constant<int, 128>{});
+  else launch(std::integral_constant<int, 16>{});
+  return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
+}
+
+}  // extern "C"
