@@ -141,8 +141,9 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __
 
 // Four waves.  Wave w has rows 16 w .. of the chunk for the output and rows (DK / 4) w .. of the state.  P is formed as its transpose (key
 // rows down the registers, query rows on the lanes), which is the layout that the product with V takes it in.
-template <typename T, int DK, int DV, bool STATES>
+template <int DK, int DV, bool STATES>
 __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
+  typedef float T;
   constexpr int LK = DK + 4, LV = DV + 4, PIECE = Raw<T>::PIECE;
   constexpr int PK = kChunk * DK / PIECE / 256, PV = kChunk * DV / PIECE / 256;   // pieces of a thread
   constexpr int RT = DK / 64, CT = DV / 16;                                         // state: row tiles of a wave, column tiles
@@ -319,6 +320,218 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
   }
 }
 
+// ---- bf16 matrix instructions --------------------------------------------------------------------
+// v_mfma_f32_16x16x32_bf16 (c = lane % 16, g = lane / 16): A row c, k = 8 g + q;  B column c, k = 8 g + q;  C/D: acc[i] is row 4 g + i, column c.
+// The order of k is free as long as both operands have the same: in products over the chunk's rows, slot q of lane group g is row 4 g + q (q < 4) or
+// 16 + 4 g + q - 4 of 32.  That is what two tiles of P leave in a lane's registers, and what two transposing reads bring.
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ f32x4 mfma_bf16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+// ds_read_b64_tr_b16: within each group of 16 lanes, lane i passes the address of four consecutive 16-bit values, taken as row i / 4,
+// columns 4 (i % 4) .. + 3 of a 4 x 16 block, and receives column i of that block.
+__device__ __forceinline__ bf16x8 read_transposed(const bf16_t *lo, const bf16_t *hi) {
+  typedef __attribute__((address_space(3))) s16x4 *lds_s16x4_ptr;
+  const bf16x4 a = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)lo));
+  const bf16x4 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)hi));
+  return bf16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+}
+// x as the sum of three bf16 values, 24 bits of it: keys times their weight enter the state like float32.
+struct Three {
+  bf16x8 t[3];
+  __device__ __forceinline__ explicit Three(f32x8 x) {
+    t[0] = __builtin_convertvector(x, bf16x8);
+    x -= __builtin_convertvector(t[0], f32x8);
+    t[1] = __builtin_convertvector(x, bf16x8);
+    x -= __builtin_convertvector(t[1], f32x8);
+    t[2] = __builtin_convertvector(x, bf16x8);
+  }
+};
+
+// As walk_f32_kernel, for bf16 tensors.  P and the state as an operand of the output are rounded to bf16, like the output; what goes into the
+// state is not.  Rows of LDS are 32 bytes longer than the data: eight rows then begin in eight different groups of banks, for both kinds of reads.
+// Column tiles of V are dealt in pairs: lane c of tile 2 u + e is column 32 u + 8 (c / 4) + 4 e + c % 4, so that a lane of the output holds eight
+// columns in a row.
+template <int DK, int DV, bool STATES>
+__global__ __launch_bounds__(256) void walk_bf16_kernel(Walk a) {
+  constexpr int LK = DK + 16, LV = DV + 16;
+  constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;   // pieces of a thread
+  constexpr int RT = DK / 64, CT = DV / 16, QJ = DK / 32;
+  extern __shared__ __align__(16) unsigned char lds_bytes[];
+  bf16_t *Ks = (bf16_t *)lds_bytes, *Vs = Ks + kChunk * LK;
+  float *weight = (float *)(Vs + kChunk * LV);
+  bf16_t *St = (bf16_t *)(weight + kChunk);
+  const Segment seg = segment_of(a.seq, blockIdx.x);
+  if (seg.rows < 0) return;
+  const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const bool last = a.reverse ? seg.s == 0 : seg.s == a.seq.segments(seg.b) - 1;
+  if (STATES && last) return;
+  const int64_t b_at = a.seq.offsets ? 0 : seg.b;
+  const int64_t at = a.reverse ? seg.row0 + seg.rows - 1 : seg.row0, dir = a.reverse ? -1 : 1;
+  const int shift = a.reverse ? 1 : 0;
+  const bf16_t *q = (const bf16_t *)a.q + b_at * a.sq.b + h * a.sq.h + at * a.sq.n, *k = (const bf16_t *)a.k + b_at * a.sk.b + h * a.sk.h + at * a.sk.n,
+               *v = (const bf16_t *)a.v + b_at * a.sv.b + h * a.sv.h + at * a.sv.n;
+  bf16_t *o = (bf16_t *)a.o + b_at * a.so.b + h * a.so.h + at * a.so.n;
+  const float l2 = log2_decay(a.log_decay, h);
+  const int64_t state_size = (int64_t)a.kw * a.vw;
+  auto vcol = [&](int ct) { return 32 * (ct >> 1) + 8 * (c >> 2) + 4 * (ct & 1) + (c & 3); };
+
+  // state: S[rt][ct][i] is row 16 (RT w + rt) + 4 g + i, column vcol(ct)
+  f32x4 S[RT][CT];
+  const int own = cache_row(a, seg.b);
+  const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
+  const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = 16 * (RT * w + rt) + 4 * g + i, col = vcol(ct);
+        S[rt][ct][i] = init && r < a.kw && col < a.vw ? init[r * a.si + col * a.sj] : 0.f;
+      }
+
+  float factor[4][4];   // of P, by key tile
+#pragma unroll
+  for (int jt = 0; jt < 4; ++jt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int e = 16 * (w - jt) + c - 4 * g - i;
+      factor[jt][i] = e >= 0 ? a.intra * decay_pow(l2, e) : 0.f;
+    }
+  const float reach = a.inter * decay_pow(l2, 16 * w + c + 1 - shift);
+
+  u32x4 rk[PK], rv[PV], rq[QJ];
+  auto request = [&](int r0) {
+#pragma unroll
+    for (int i = 0; i < PK; ++i) {
+      const int p = tid + 256 * i, row = r0 + p / (DK / 8), col = p % (DK / 8) * 8;
+      rk[i] = load_raw<u32x4>(k + row * dir * a.sk.n + col, row < seg.rows && col < a.kw);
+    }
+#pragma unroll
+    for (int i = 0; i < PV; ++i) {
+      const int p = tid + 256 * i, row = r0 + p / (DV / 8), col = p % (DV / 8) * 8;
+      rv[i] = load_raw<u32x4>(v + row * dir * a.sv.n + col, row < seg.rows && col < a.vw);
+    }
+    if (!STATES) {
+      const int row = r0 + 16 * w + c;
+#pragma unroll
+      for (int j = 0; j < QJ; ++j) rq[j] = load_raw<u32x4>(q + row * dir * a.sq.n + 32 * j + 8 * g, row < seg.rows && 32 * j + 8 * g < a.kw);
+    }
+  };
+
+  request(0);
+  for (int r0 = 0; r0 < seg.rows; r0 += kChunk) {
+    const int rows = min(kChunk, seg.rows - r0);
+#pragma unroll
+    for (int i = 0; i < PK; ++i) {
+      const int p = tid + 256 * i;
+      *(u32x4 *)(Ks + p / (DK / 8) * LK + p % (DK / 8) * 8) = rk[i];
+    }
+#pragma unroll
+    for (int i = 0; i < PV; ++i) {
+      const int p = tid + 256 * i;
+      *(u32x4 *)(Vs + p / (DV / 8) * LV + p % (DV / 8) * 8) = rv[i];
+    }
+    if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + shift);
+    bf16x8 Q[QJ];
+    if (!STATES) {
+#pragma unroll
+      for (int j = 0; j < QJ; ++j) Q[j] = __builtin_bit_cast(bf16x8, rq[j]);
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+          *(bf16x4 *)(St + vcol(ct) * LK + 16 * (RT * w + rt) + 4 * g) = __builtin_convertvector(S[rt][ct], bf16x4);
+    }
+    __syncthreads();
+    request(r0 + kChunk);
+
+    bf16x8 P[2];   // weights of 32 key rows each
+    if (!STATES) {
+#pragma unroll
+      for (int jt = 0; jt < 4; ++jt) {
+        f32x4 p = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (jt <= w) {
+#pragma unroll
+          for (int j = 0; j < QJ; ++j) p = mfma_bf16(*(const bf16x8 *)(Ks + (16 * jt + c) * LK + 32 * j + 8 * g), Q[j], p);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) p[i] = jt < w || c >= 4 * g + i ? p[i] * factor[jt][i] : 0.f;
+        }
+        const bf16x4 b = __builtin_convertvector(p, bf16x4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) P[jt >> 1][4 * (jt & 1) + i] = b[i];
+      }
+    }
+    // keys of the wave's state rows, weighted, in three terms
+    const float keep = decay_pow(l2, rows);
+    bf16x8 K[RT][2][3];
+#pragma unroll
+    for (int jj = 0; jj < 2; ++jj) {
+      const f32x4 w0 = *(const f32x4 *)(weight + 32 * jj + 4 * g), w1 = *(const f32x4 *)(weight + 32 * jj + 16 + 4 * g);
+      const f32x8 wt = f32x8{w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const bf16_t *p = Ks + (32 * jj + 4 * g + (c >> 2)) * LK + 16 * (RT * w + rt) + 4 * (c & 3);
+        const Three t(__builtin_convertvector(read_transposed(p, p + 16 * LK), f32x8) * wt);
+#pragma unroll
+        for (int u = 0; u < 3; ++u) K[rt][jj][u] = t.t[u];
+      }
+    }
+    const int row = r0 + 16 * w + c;
+    f32x4 O[2];
+#pragma unroll
+    for (int ct = 0; ct < CT; ++ct) {
+      bf16x8 V[2];
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        const bf16_t *p = Vs + (32 * jj + 4 * g + (c >> 2)) * LV + 32 * (ct >> 1) + 8 * (c & 3) + 4 * (ct & 1);
+        V[jj] = read_transposed(p, p + 16 * LV);
+      }
+      if (!STATES) {
+        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < QJ; ++j) acc = mfma_bf16(*(const bf16x8 *)(St + vcol(ct) * LK + 32 * j + 8 * g), Q[j], acc);
+        acc *= reach;
+#pragma unroll
+        for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(V[jj], P[jj], acc);
+        O[ct & 1] = acc;
+        if ((ct & 1) && row < seg.rows && 32 * (ct >> 1) + 8 * g < a.vw) {
+          const bf16x8 b = __builtin_convertvector(f32x8{O[0][0], O[0][1], O[0][2], O[0][3], O[1][0], O[1][1], O[1][2], O[1][3]}, bf16x8);
+          store_raw(o + row * dir * a.so.n + 32 * (ct >> 1) + 8 * g, __builtin_bit_cast(u32x4, b));
+        }
+      }
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        f32x4 x = S[rt][ct] * keep;
+#pragma unroll
+        for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+          for (int u = 2; u >= 0; --u) x = mfma_bf16(K[rt][jj][u], V[jj], x);
+        S[rt][ct] = x;
+      }
+    }
+    __syncthreads();
+  }
+
+  float *fin = nullptr;
+  if (STATES) fin = a.fin + ((int64_t)blockIdx.x * a.H + h) * state_size;
+  else if (last && a.fin && own >= 0) fin = a.fin + ((int64_t)own * a.H + h) * state_size;
+  if (fin) {
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+      for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = 16 * (RT * w + rt) + 4 * g + i, col = vcol(ct);
+          if (r < a.kw && col < a.vw) fin[r * a.si + col * a.sj] = S[rt][ct][i];
+        }
+  }
+}
+
 // What the segments of a sequence add to the state, in place, to the states that they begin with: four values of a state per thread, over all
 // segments in their order (from the last one with `reverse`), eight of them requested at a time.
 __global__ __launch_bounds__(64) void scan_kernel(Walk a, float *local) {
@@ -453,22 +666,23 @@ wersa_status validate(const wersa_decay_desc *c) {
 }
 bool misaligned(const void *p, size_t a) { return ((uintptr_t)p % a) != 0; }
 Strides strides(const int64_t *s) { return Strides{s[0], s[1], s[2]}; }
-template <typename T, int DK, int DV, bool STATES>
-bool launch_walk_as(const Walk &a, hipStream_t st) {
-  constexpr size_t smem = sizeof(float) * (kChunk * (DK + 4 + DV + 4 + 1) + (STATES ? 0 : DV * (DK + 4)));
-  auto kern = &walk_f32_kernel<T, DK, DV, STATES>;
+template <typename K> bool launch_walk_kernel(K kern, size_t smem, bool states, const Walk &a, hipStream_t st) {
   if (smem > 65536 &&
       hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess)
     return false;
-  WERSA_STAGE(STATES ? "wersa_decay_states" : "wersa_decay_walk", st, kern<<<dim3(a.seq.slots(), a.H), 256, smem, st>>>(a));
+  WERSA_STAGE(states ? "wersa_decay_states" : "wersa_decay_walk", st, kern<<<dim3(a.seq.slots(), a.H), 256, smem, st>>>(a));
   return true;
 }
+template <int DK, int DV, bool STATES> bool launch_walk_as(const wersa_decay_desc &c, const Walk &a, hipStream_t st) {
+  if (c.dtype == WERSA_F32)
+    return launch_walk_kernel(&walk_f32_kernel<DK, DV, STATES>,
+                              sizeof(float) * (kChunk * (DK + 4 + DV + 4 + 1) + (STATES ? 0 : DV * (DK + 4))), STATES, a, st);
+  return launch_walk_kernel(&walk_bf16_kernel<DK, DV, STATES>,
+                            sizeof(bf16_t) * (kChunk * (DK + 16 + DV + 16) + (STATES ? 0 : DV * (DK + 16))) + sizeof(float) * kChunk, STATES, a, st);
+}
 template <bool STATES> bool launch_walk(const wersa_decay_desc &c, const Walk &a, hipStream_t st) {
-  const bool f32 = c.dtype == WERSA_F32;
-  if (a.kw <= 64 && a.vw <= 64) return f32 ? launch_walk_as<float, 64, 64, STATES>(a, st) : launch_walk_as<bf16_t, 64, 64, STATES>(a, st);
-  if (a.kw <= 64) return f32 ? launch_walk_as<float, 64, 128, STATES>(a, st) : launch_walk_as<bf16_t, 64, 128, STATES>(a, st);
-  if (a.vw <= 64) return f32 ? launch_walk_as<float, 128, 64, STATES>(a, st) : launch_walk_as<bf16_t, 128, 64, STATES>(a, st);
-  return f32 ? launch_walk_as<float, 128, 128, STATES>(a, st) : launch_walk_as<bf16_t, 128, 128, STATES>(a, st);
+  if (a.kw <= 64) return a.vw <= 64 ? launch_walk_as<64, 64, STATES>(c, a, st) : launch_walk_as<64, 128, STATES>(c, a, st);
+  return a.vw <= 64 ? launch_walk_as<128, 64, STATES>(c, a, st) : launch_walk_as<128, 128, STATES>(c, a, st);
 }
 void launch_scan(const Walk &a, float *local, hipStream_t st) {
   WERSA_STAGE("wersa_decay_scan", st, scan_kernel<<<dim3((a.kw * a.vw / 4 + 63) / 64, a.H, a.seq.B), 64, 0, st>>>(a, local));
