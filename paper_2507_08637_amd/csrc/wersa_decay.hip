@@ -21,11 +21,6 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
-// Rows of a tensor may begin at any element: vector accesses to global memory need no more than the element's alignment on this device.
-template <typename V> struct Any {
-  typedef V type __attribute__((aligned(2)));
-};
 
 constexpr int kChunk = 64;
 
@@ -94,45 +89,42 @@ __device__ __forceinline__ int cache_row(const Walk &a, int b) {   // -1: none
   return r < 0 || r >= a.cache_rows ? -1 : r;
 }
 
-// Raw pieces of a row: 16 bytes for the tiles, four elements for queries and outputs.
-template <typename T> struct Raw;
-template <> struct Raw<float> {
-  static constexpr int PIECE = 4;
-  typedef u32x4 Four;
-  static __device__ __forceinline__ void spread(const u32x4 &p, float *out) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) out[i] = __uint_as_float(p[i]);
+// The rows of a segment in one tensor, chunk by chunk in the walk's order, as buffers that end at the last row: loads of rows that are not there, or
+// of columns past the width, return zeros, stores to them do nothing, by the bounds check of the buffer instructions.
+constexpr int64_t kMostRowStride = 1 << 24;   // elements: 63 rows of 4 bytes stay below 2^32
+typedef __amdgpu_buffer_rsrc_t Buffer;
+struct Rows {
+  const char *low;    // of the segment's rows, the first in memory
+  int64_t step;       // bytes from row to row
+  int rows, width;    // width: bytes of a row
+  bool reverse;
+  struct Chunk {
+    Buffer b;
+    uint32_t missing; // the walk back: bytes by which a partial chunk's rows lie lower
+  };
+  __device__ __forceinline__ Chunk chunk(int r0) const {
+    const int have = max(0, min(kChunk, rows - r0));
+    const uint64_t p = (uint64_t)(low + (reverse ? rows - r0 - have : r0) * step);
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)p), hi = __builtin_amdgcn_readfirstlane((uint32_t)(p >> 32));
+    const uint32_t bytes = __builtin_amdgcn_readfirstlane(have ? (uint32_t)(have - 1) * (uint32_t)step + width : 0);
+    return Chunk{__builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)hi << 32 | lo), 0, (int)bytes, 0x00020000),
+                 reverse ? (uint32_t)(kChunk - have) * (uint32_t)step : 0};
   }
-  static __device__ __forceinline__ f32x4 four(const Four &p) {
-    return f32x4{__uint_as_float(p[0]), __uint_as_float(p[1]), __uint_as_float(p[2]), __uint_as_float(p[3])};
-  }
-  static __device__ __forceinline__ Four pack(f32x4 v) {
-    return Four{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-  }
+  // Of a row of a chunk.  Bytes past the width are none of the buffer's (`outside`, joined in by `or` at the access).
+  __device__ __forceinline__ uint32_t offset(int row, int byte) const { return (uint32_t)(reverse ? kChunk - 1 - row : row) * (uint32_t)step + byte; }
+  __device__ __forceinline__ uint32_t outside(int byte) const { return byte < width ? 0u : 0xffffffc0u; }
 };
-template <> struct Raw<bf16_t> {
-  static constexpr int PIECE = 8;
-  typedef u32x2 Four;
-  static __device__ __forceinline__ void spread(const u32x4 &p, float *out) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      out[2 * i] = __uint_as_float(p[i] << 16);
-      out[2 * i + 1] = __uint_as_float(p[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ f32x4 four(const Four &p) {
-    return f32x4{__uint_as_float(p[0] << 16), __uint_as_float(p[0] & 0xffff0000u), __uint_as_float(p[1] << 16), __uint_as_float(p[1] & 0xffff0000u)};
-  }
-  static __device__ __forceinline__ Four pack(f32x4 v) {
-    return Four{(uint32_t)f32_to_bf16(v[0]) | (uint32_t)f32_to_bf16(v[1]) << 16, (uint32_t)f32_to_bf16(v[2]) | (uint32_t)f32_to_bf16(v[3]) << 16};
-  }
-};
-template <typename V, typename T> __device__ __forceinline__ V load_raw(const T *p, bool ok) {
-  V r{};
-  if (ok) r = *reinterpret_cast<const typename Any<V>::type *>(p);
-  return r;
+__device__ __forceinline__ u32x4 load_piece(const Rows::Chunk &c, uint32_t offset, uint32_t outside) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(c.b, (int)((offset - c.missing) | outside), 0, 0));
 }
-template <typename V, typename T> __device__ __forceinline__ void store_raw(T *p, const V &v) { *reinterpret_cast<typename Any<V>::type *>(p) = v; }
+__device__ __forceinline__ void store_piece(const Rows::Chunk &c, uint32_t offset, uint32_t outside, u32x4 v) {
+  __builtin_amdgcn_raw_buffer_store_b128(v, c.b, (int)((offset - c.missing) | outside), 0, 0);
+}
+// Rows of `seg` for head h of a tensor.
+__device__ __forceinline__ Rows rows_of(const void *p, const Strides &s, const Segment &seg, const Walk &a, int h, int cols, int element) {
+  const int64_t at = (a.seq.offsets ? 0 : seg.b * s.b) + h * s.h + seg.row0 * s.n;
+  return Rows{(const char *)p + at * element, s.n * element, seg.rows, cols * element, a.reverse};
+}
 
 // ---- float32 matrix instructions -----------------------------------------------------------------
 // v_mfma_f32_16x16x4_f32 (c = lane % 16, g = lane / 16): A row c, k = g;  B column c, k = g;  C/D: acc[i] is row 4 g + i, column c.
@@ -143,9 +135,8 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __
 // rows down the registers, query rows on the lanes), which is the layout that the product with V takes it in.
 template <int DK, int DV, bool STATES>
 __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
-  typedef float T;
-  constexpr int LK = DK + 4, LV = DV + 4, PIECE = Raw<T>::PIECE;
-  constexpr int PK = kChunk * DK / PIECE / 256, PV = kChunk * DV / PIECE / 256;   // pieces of a thread
+  constexpr int LK = DK + 4, LV = DV + 4;
+  constexpr int PK = kChunk * DK / 4 / 256, PV = kChunk * DV / 4 / 256;   // pieces of a thread
   constexpr int RT = DK / 64, CT = DV / 16;                                         // state: row tiles of a wave, column tiles
   extern __shared__ __align__(16) float lds[];
   float *Ks = lds, *Vs = Ks + kChunk * LK, *weight = Vs + kChunk * LV, *St = weight + kChunk;
@@ -154,13 +145,9 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
   const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const bool last = a.reverse ? seg.s == 0 : seg.s == a.seq.segments(seg.b) - 1;
   if (STATES && last) return;   // nothing begins with what the last one adds
-  const int64_t b_at = a.seq.offsets ? 0 : seg.b;
-  // logical row r of the segment is row at + r * dir
-  const int64_t at = a.reverse ? seg.row0 + seg.rows - 1 : seg.row0, dir = a.reverse ? -1 : 1;
   const int shift = a.reverse ? 1 : 0;
-  const T *q = (const T *)a.q + b_at * a.sq.b + h * a.sq.h + at * a.sq.n, *k = (const T *)a.k + b_at * a.sk.b + h * a.sk.h + at * a.sk.n,
-          *v = (const T *)a.v + b_at * a.sv.b + h * a.sv.h + at * a.sv.n;
-  T *o = (T *)a.o + b_at * a.so.b + h * a.so.h + at * a.so.n;
+  const Rows qr = rows_of(a.q, a.sq, seg, a, h, a.kw, 4), kr = rows_of(a.k, a.sk, seg, a, h, a.kw, 4), vr = rows_of(a.v, a.sv, seg, a, h, a.vw, 4),
+             orow = rows_of(a.o, a.so, seg, a, h, a.vw, 4);
   const float l2 = log2_decay(a.log_decay, h);
   const int64_t state_size = (int64_t)a.kw * a.vw;
 
@@ -189,24 +176,19 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
     }
   const float reach = a.inter * decay_pow(l2, 16 * w + c + 1 - shift);
 
-  u32x4 rk[PK], rv[PV];
-  typename Raw<T>::Four rq[DK / 16];
+  f32x4 rk[PK], rv[PV], rq[DK / 16];
+  const int krow = tid / (DK / 4), kcol = tid % (DK / 4) * 4, vrow = tid / (DV / 4), vcol = tid % (DV / 4) * 4;   // a thread's first piece
   auto request = [&](int r0) {
+    const Rows::Chunk kc = kr.chunk(r0), vc = vr.chunk(r0);
 #pragma unroll
-    for (int i = 0; i < PK; ++i) {
-      const int p = tid + 256 * i, row = r0 + p / (DK / PIECE), col = p % (DK / PIECE) * PIECE;
-      rk[i] = load_raw<u32x4>(k + row * dir * a.sk.n + col, row < seg.rows && col < a.kw);
-    }
+    for (int i = 0; i < PK; ++i) rk[i] = __builtin_bit_cast(f32x4, load_piece(kc, kr.offset(krow + 1024 / DK * i, 4 * kcol), kr.outside(4 * kcol)));
 #pragma unroll
-    for (int i = 0; i < PV; ++i) {
-      const int p = tid + 256 * i, row = r0 + p / (DV / PIECE), col = p % (DV / PIECE) * PIECE;
-      rv[i] = load_raw<u32x4>(v + row * dir * a.sv.n + col, row < seg.rows && col < a.vw);
-    }
+    for (int i = 0; i < PV; ++i) rv[i] = __builtin_bit_cast(f32x4, load_piece(vc, vr.offset(vrow + 1024 / DV * i, 4 * vcol), vr.outside(4 * vcol)));
     if (!STATES) {
-      const int row = r0 + 16 * w + c;
+      const Rows::Chunk qc = qr.chunk(r0);
 #pragma unroll
       for (int j = 0; j < DK / 16; ++j)
-        rq[j] = load_raw<typename Raw<T>::Four>(q + row * dir * a.sq.n + 16 * j + 4 * g, row < seg.rows && 16 * j + 4 * g < a.kw);
+        rq[j] = __builtin_bit_cast(f32x4, load_piece(qc, qr.offset(16 * w + c, 64 * j + 16 * g), qr.outside(64 * j + 16 * g)));
     }
   };
 
@@ -215,28 +197,14 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
     const int rows = min(kChunk, seg.rows - r0);
     // what was requested, and the state, into LDS
 #pragma unroll
-    for (int i = 0; i < PK; ++i) {
-      const int p = tid + 256 * i;
-      float e[PIECE];
-      Raw<T>::spread(rk[i], e);
+    for (int i = 0; i < PK; ++i) *(f32x4 *)(Ks + (krow + 1024 / DK * i) * LK + kcol) = rk[i];
 #pragma unroll
-      for (int j = 0; j < PIECE; j += 4)
-        *(f32x4 *)(Ks + p / (DK / PIECE) * LK + p % (DK / PIECE) * PIECE + j) = f32x4{e[j], e[j + 1], e[j + 2], e[j + 3]};
-    }
-#pragma unroll
-    for (int i = 0; i < PV; ++i) {
-      const int p = tid + 256 * i;
-      float e[PIECE];
-      Raw<T>::spread(rv[i], e);
-#pragma unroll
-      for (int j = 0; j < PIECE; j += 4)
-        *(f32x4 *)(Vs + p / (DV / PIECE) * LV + p % (DV / PIECE) * PIECE + j) = f32x4{e[j], e[j + 1], e[j + 2], e[j + 3]};
-    }
+    for (int i = 0; i < PV; ++i) *(f32x4 *)(Vs + (vrow + 1024 / DV * i) * LV + vcol) = rv[i];
     if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + shift);
     f32x4 Q[DK / 16];
     if (!STATES) {
 #pragma unroll
-      for (int j = 0; j < DK / 16; ++j) Q[j] = Raw<T>::four(rq[j]);
+      for (int j = 0; j < DK / 16; ++j) Q[j] = rq[j];
 #pragma unroll
       for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -296,10 +264,11 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
           for (int ct = 0; ct < CT; ++ct) S[rt][ct] = mfma_f32(kt, V[ct][i], S[rt][ct]);
         }
     }
-    if (!STATES && 16 * w + c < rows) {
+    if (!STATES) {
+      const Rows::Chunk oc = orow.chunk(r0);
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
-        if (16 * ct + 4 * g < a.vw) store_raw(o + (r0 + 16 * w + c) * dir * a.so.n + 16 * ct + 4 * g, Raw<T>::pack(O[ct]));
+        store_piece(oc, orow.offset(16 * w + c, 64 * ct + 16 * g), orow.outside(64 * ct + 16 * g), __builtin_bit_cast(u32x4, O[ct]));
     }
     __syncthreads();
   }
@@ -350,213 +319,313 @@ struct Three {
   }
 };
 
+// The decays of a wave's part of a chunk's weights: 16 own rows on the lanes, 16 other rows down the registers.  lambda^(c - 4 g - i) on the diagonal tile,
+// lambda^(16 + c - 4 g - i) times a power of lambda^16, the same for the whole wave, on those before it.
+struct Weights {
+  float on[4], before[4], apart[3], reach;
+  int w, ahead;   // ahead: c - 4 g
+  __device__ __forceinline__ Weights(const Walk &a, float l2, int w, int g, int c) : w(w), ahead(c - 4 * g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      on[i] = ahead >= i ? a.intra * decay_pow(l2, ahead - i) : 0.f;
+      before[i] = a.intra * decay_pow(l2, 16 + ahead - i);
+    }
+#pragma unroll
+    for (int jt = 0; jt < 3; ++jt) apart[jt] = decay_pow(l2, 16 * max(w - jt - 1, 0));
+    reach = a.inter * decay_pow(l2, 16 * w + c + (a.reverse ? 0 : 1));
+  }
+  // Products of the own rows `b` with the chunk's rows in LDS, weighted: operands of the products with the other tensor's rows.
+  template <int D> __device__ __forceinline__ void products(const bf16_t *rows, const bf16x8 (&b)[D / 32], int g, int c, bf16x8 (&P)[2]) const {
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt) {
+      f32x4 p = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (jt <= w) {
+#pragma unroll
+        for (int j = 0; j < D / 32; ++j) p = mfma_bf16(*(const bf16x8 *)(rows + (16 * jt + c) * (D + 16) + 32 * j + 8 * g), b[j], p);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) p[i] = jt < w ? p[i] * before[i] * apart[jt < 3 ? jt : 0] : ahead >= i ? p[i] * on[i] : 0.f;
+      }
+      const bf16x4 r = __builtin_convertvector(p, bf16x4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) P[jt >> 1][4 * (jt & 1) + i] = r[i];
+    }
+  }
+};
+// Column tiles are dealt in pairs: lane c of tile 2 u + e is column 32 u + 8 (c / 4) + 4 e + c % 4, so that a lane of the output (whose rows down the
+// registers these are) holds eight columns in a row.
+__device__ __forceinline__ int tile_column(int ct, int c) { return 32 * (ct >> 1) + 8 * (c >> 2) + 4 * (ct & 1) + (c & 3); }
+// The tile's columns of 32 rows of LDS from `row` on, down the slots of k: rows 4 g + q and 16 + 4 g + q - 4 (see above), or 8 g + q with NATURAL.
+template <int D, bool NATURAL> __device__ __forceinline__ bf16x8 tile_operand(const bf16_t *rows, int row, int ct, int g, int c) {
+  const bf16_t *p = rows + (row + (NATURAL ? 8 : 4) * g + (c >> 2)) * (D + 16) + 32 * (ct >> 1) + 8 * (c & 3) + 4 * (ct & 1);
+  return read_transposed(p, p + (NATURAL ? 4 : 16) * (D + 16));
+}
+__device__ __forceinline__ u32x4 pack_pair(f32x4 x, f32x4 y) {
+  return __builtin_bit_cast(u32x4, __builtin_convertvector(f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]}, bf16x8));
+}
+// S <- keep S + (K o weight)^T V over the chunk's rows in LDS: RT row tiles of the wave from `row0` on, all column tiles.
+template <int DK, int DV>
+__device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float keep, const bf16_t *Ks, const bf16_t *Vs, const float *weight, int row0, int g, int c) {
+  constexpr int RT = DK / 64, CT = DV / 16, LK = DK + 16;
+  bf16x8 K[RT][2][3];
+#pragma unroll
+  for (int jj = 0; jj < 2; ++jj) {
+    const f32x4 w0 = *(const f32x4 *)(weight + 32 * jj + 4 * g), w1 = *(const f32x4 *)(weight + 32 * jj + 16 + 4 * g);
+    const f32x8 wt = f32x8{w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const bf16_t *p = Ks + (32 * jj + 4 * g + (c >> 2)) * LK + row0 + 16 * rt + 4 * (c & 3);
+      const Three t(__builtin_convertvector(read_transposed(p, p + 16 * LK), f32x8) * wt);
+#pragma unroll
+      for (int u = 0; u < 3; ++u) K[rt][jj][u] = t.t[u];
+    }
+  }
+#pragma unroll
+  for (int ct = 0; ct < CT; ++ct) {
+    const bf16x8 V[2] = {tile_operand<DV, false>(Vs, 0, ct, g, c), tile_operand<DV, false>(Vs, 32, ct, g, c)};
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      f32x4 x = S[rt][ct] * keep;
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+        for (int u = 2; u >= 0; --u) x = mfma_bf16(K[rt][jj][u], V[jj], x);
+      S[rt][ct] = x;
+    }
+  }
+}
+// A wave's rows of a state, from memory or to it.
+template <int DK, int DV, typename F> __device__ __forceinline__ void each_of_state(const Walk &a, f32x4 (&S)[DK / 64][DV / 16], int row0, int g, int c, F f) {
+#pragma unroll
+  for (int rt = 0; rt < DK / 64; ++rt)
+#pragma unroll
+    for (int ct = 0; ct < DV / 16; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = row0 + 16 * rt + 4 * g + i, col = tile_column(ct, c);
+        S[rt][ct][i] = f(S[rt][ct][i], r < a.kw && col < a.vw, r * a.si + col * a.sj);
+      }
+}
+
 // As walk_f32_kernel, for bf16 tensors.  P and the state as an operand of the output are rounded to bf16, like the output; what goes into the
 // state is not.  Rows of LDS are 32 bytes longer than the data: eight rows then begin in eight different groups of banks, for both kinds of reads.
-// Column tiles of V are dealt in pairs: lane c of tile 2 u + e is column 32 u + 8 (c / 4) + 4 e + c % 4, so that a lane of the output holds eight
-// columns in a row.
 template <int DK, int DV, bool STATES>
-__global__ __launch_bounds__(256) void walk_bf16_kernel(Walk a) {
+__global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(Walk a) {
   constexpr int LK = DK + 16, LV = DV + 16;
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;   // pieces of a thread
-  constexpr int RT = DK / 64, CT = DV / 16, QJ = DK / 32;
+  constexpr int CT = DV / 16, QJ = DK / 32;
   extern __shared__ __align__(16) unsigned char lds_bytes[];
   bf16_t *Ks = (bf16_t *)lds_bytes, *Vs = Ks + kChunk * LK;
   float *weight = (float *)(Vs + kChunk * LV);
-  bf16_t *St = (bf16_t *)(weight + kChunk);
+  bf16_t *St = (bf16_t *)(weight + kChunk);   // columns of the state, as rows
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
   const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int row0 = DK / 4 * w;   // of the wave's rows of the state
   const bool last = a.reverse ? seg.s == 0 : seg.s == a.seq.segments(seg.b) - 1;
   if (STATES && last) return;
-  const int64_t b_at = a.seq.offsets ? 0 : seg.b;
-  const int64_t at = a.reverse ? seg.row0 + seg.rows - 1 : seg.row0, dir = a.reverse ? -1 : 1;
-  const int shift = a.reverse ? 1 : 0;
-  const bf16_t *q = (const bf16_t *)a.q + b_at * a.sq.b + h * a.sq.h + at * a.sq.n, *k = (const bf16_t *)a.k + b_at * a.sk.b + h * a.sk.h + at * a.sk.n,
-               *v = (const bf16_t *)a.v + b_at * a.sv.b + h * a.sv.h + at * a.sv.n;
-  bf16_t *o = (bf16_t *)a.o + b_at * a.so.b + h * a.so.h + at * a.so.n;
+  const Rows qr = rows_of(a.q, a.sq, seg, a, h, a.kw, 2), kr = rows_of(a.k, a.sk, seg, a, h, a.kw, 2), vr = rows_of(a.v, a.sv, seg, a, h, a.vw, 2),
+             orow = rows_of(a.o, a.so, seg, a, h, a.vw, 2);
   const float l2 = log2_decay(a.log_decay, h);
   const int64_t state_size = (int64_t)a.kw * a.vw;
-  auto vcol = [&](int ct) { return 32 * (ct >> 1) + 8 * (c >> 2) + 4 * (ct & 1) + (c & 3); };
 
-  // state: S[rt][ct][i] is row 16 (RT w + rt) + 4 g + i, column vcol(ct)
-  f32x4 S[RT][CT];
+  f32x4 S[DK / 64][CT];   // S[rt][ct][i] is row row0 + 16 rt + 4 g + i, column tile_column(ct, c)
   const int own = cache_row(a, seg.b);
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
   const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = 16 * (RT * w + rt) + 4 * g + i, col = vcol(ct);
-        S[rt][ct][i] = init && r < a.kw && col < a.vw ? init[r * a.si + col * a.sj] : 0.f;
-      }
+  each_of_state<DK, DV>(a, S, row0, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  const Weights weights(a, l2, w, g, c);
 
-  float factor[4][4];   // of P, by key tile
-#pragma unroll
-  for (int jt = 0; jt < 4; ++jt)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = 16 * (w - jt) + c - 4 * g - i;
-      factor[jt][i] = e >= 0 ? a.intra * decay_pow(l2, e) : 0.f;
-    }
-  const float reach = a.inter * decay_pow(l2, 16 * w + c + 1 - shift);
-
-  u32x4 rk[PK], rv[PV], rq[QJ];
+  u32x4 rk[PK], rv[PV];
+  bf16x8 Q[QJ];
+  const int krow = tid / (DK / 8), kcol = tid % (DK / 8) * 8, vrow = tid / (DV / 8), vcol = tid % (DV / 8) * 8;   // a thread's first piece
   auto request = [&](int r0) {
+    const Rows::Chunk kc = kr.chunk(r0), vc = vr.chunk(r0);
 #pragma unroll
-    for (int i = 0; i < PK; ++i) {
-      const int p = tid + 256 * i, row = r0 + p / (DK / 8), col = p % (DK / 8) * 8;
-      rk[i] = load_raw<u32x4>(k + row * dir * a.sk.n + col, row < seg.rows && col < a.kw);
-    }
+    for (int i = 0; i < PK; ++i) rk[i] = load_piece(kc, kr.offset(krow + 2048 / DK * i, 2 * kcol), kr.outside(2 * kcol));
 #pragma unroll
-    for (int i = 0; i < PV; ++i) {
-      const int p = tid + 256 * i, row = r0 + p / (DV / 8), col = p % (DV / 8) * 8;
-      rv[i] = load_raw<u32x4>(v + row * dir * a.sv.n + col, row < seg.rows && col < a.vw);
-    }
-    if (!STATES) {
-      const int row = r0 + 16 * w + c;
+    for (int i = 0; i < PV; ++i) rv[i] = load_piece(vc, vr.offset(vrow + 2048 / DV * i, 2 * vcol), vr.outside(2 * vcol));
+  };
+  auto request_own = [&](int r0) {   // the wave's 16 queries
+    const Rows::Chunk qc = qr.chunk(r0);
 #pragma unroll
-      for (int j = 0; j < QJ; ++j) rq[j] = load_raw<u32x4>(q + row * dir * a.sq.n + 32 * j + 8 * g, row < seg.rows && 32 * j + 8 * g < a.kw);
-    }
+    for (int j = 0; j < QJ; ++j)
+      Q[j] = __builtin_bit_cast(bf16x8, load_piece(qc, qr.offset(16 * w + c, 64 * j + 16 * g), qr.outside(64 * j + 16 * g)));
   };
 
   request(0);
+  if (!STATES) request_own(0);
   for (int r0 = 0; r0 < seg.rows; r0 += kChunk) {
     const int rows = min(kChunk, seg.rows - r0);
 #pragma unroll
-    for (int i = 0; i < PK; ++i) {
-      const int p = tid + 256 * i;
-      *(u32x4 *)(Ks + p / (DK / 8) * LK + p % (DK / 8) * 8) = rk[i];
-    }
+    for (int i = 0; i < PK; ++i) *(u32x4 *)(Ks + (krow + 2048 / DK * i) * LK + kcol) = rk[i];
 #pragma unroll
-    for (int i = 0; i < PV; ++i) {
-      const int p = tid + 256 * i;
-      *(u32x4 *)(Vs + p / (DV / 8) * LV + p % (DV / 8) * 8) = rv[i];
-    }
-    if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + shift);
-    bf16x8 Q[QJ];
+    for (int i = 0; i < PV; ++i) *(u32x4 *)(Vs + (vrow + 2048 / DV * i) * LV + vcol) = rv[i];
+    if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + (a.reverse ? 1 : 0));
     if (!STATES) {
 #pragma unroll
-      for (int j = 0; j < QJ; ++j) Q[j] = __builtin_bit_cast(bf16x8, rq[j]);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+      for (int rt = 0; rt < DK / 64; ++rt)
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
-          *(bf16x4 *)(St + vcol(ct) * LK + 16 * (RT * w + rt) + 4 * g) = __builtin_convertvector(S[rt][ct], bf16x4);
+          *(bf16x4 *)(St + tile_column(ct, c) * LK + row0 + 16 * rt + 4 * g) = __builtin_convertvector(S[rt][ct], bf16x4);
     }
     __syncthreads();
     request(r0 + kChunk);
-
-    bf16x8 P[2];   // weights of 32 key rows each
     if (!STATES) {
+      bf16x8 P[2];
+      weights.products<DK>(Ks, Q, g, c, P);
+      const Rows::Chunk oc = orow.chunk(r0);
+      f32x4 O[2];
 #pragma unroll
-      for (int jt = 0; jt < 4; ++jt) {
-        f32x4 p = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (jt <= w) {
-#pragma unroll
-          for (int j = 0; j < QJ; ++j) p = mfma_bf16(*(const bf16x8 *)(Ks + (16 * jt + c) * LK + 32 * j + 8 * g), Q[j], p);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) p[i] = jt < w || c >= 4 * g + i ? p[i] * factor[jt][i] : 0.f;
-        }
-        const bf16x4 b = __builtin_convertvector(p, bf16x4);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) P[jt >> 1][4 * (jt & 1) + i] = b[i];
-      }
-    }
-    // keys of the wave's state rows, weighted, in three terms
-    const float keep = decay_pow(l2, rows);
-    bf16x8 K[RT][2][3];
-#pragma unroll
-    for (int jj = 0; jj < 2; ++jj) {
-      const f32x4 w0 = *(const f32x4 *)(weight + 32 * jj + 4 * g), w1 = *(const f32x4 *)(weight + 32 * jj + 16 + 4 * g);
-      const f32x8 wt = f32x8{w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        const bf16_t *p = Ks + (32 * jj + 4 * g + (c >> 2)) * LK + 16 * (RT * w + rt) + 4 * (c & 3);
-        const Three t(__builtin_convertvector(read_transposed(p, p + 16 * LK), f32x8) * wt);
-#pragma unroll
-        for (int u = 0; u < 3; ++u) K[rt][jj][u] = t.t[u];
-      }
-    }
-    const int row = r0 + 16 * w + c;
-    f32x4 O[2];
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      bf16x8 V[2];
-#pragma unroll
-      for (int jj = 0; jj < 2; ++jj) {
-        const bf16_t *p = Vs + (32 * jj + 4 * g + (c >> 2)) * LV + 32 * (ct >> 1) + 8 * (c & 3) + 4 * (ct & 1);
-        V[jj] = read_transposed(p, p + 16 * LV);
-      }
-      if (!STATES) {
+      for (int ct = 0; ct < CT; ++ct) {
         f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < QJ; ++j) acc = mfma_bf16(*(const bf16x8 *)(St + vcol(ct) * LK + 32 * j + 8 * g), Q[j], acc);
-        acc *= reach;
+        for (int j = 0; j < QJ; ++j) acc = mfma_bf16(*(const bf16x8 *)(St + tile_column(ct, c) * LK + 32 * j + 8 * g), Q[j], acc);
+        acc *= weights.reach;
 #pragma unroll
-        for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(V[jj], P[jj], acc);
+        for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(tile_operand<DV, false>(Vs, 32 * jj, ct, g, c), P[jj], acc);
         O[ct & 1] = acc;
-        if ((ct & 1) && row < seg.rows && 32 * (ct >> 1) + 8 * g < a.vw) {
-          const bf16x8 b = __builtin_convertvector(f32x8{O[0][0], O[0][1], O[0][2], O[0][3], O[1][0], O[1][1], O[1][2], O[1][3]}, bf16x8);
-          store_raw(o + row * dir * a.so.n + 32 * (ct >> 1) + 8 * g, __builtin_bit_cast(u32x4, b));
-        }
+        if (ct & 1) store_piece(oc, orow.offset(16 * w + c, 32 * ct - 32 + 16 * g), orow.outside(32 * ct - 32 + 16 * g), pack_pair(O[0], O[1]));
       }
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt) {
-        f32x4 x = S[rt][ct] * keep;
-#pragma unroll
-        for (int jj = 0; jj < 2; ++jj)
-#pragma unroll
-          for (int u = 2; u >= 0; --u) x = mfma_bf16(K[rt][jj][u], V[jj], x);
-        S[rt][ct] = x;
-      }
+      request_own(r0 + kChunk);   // (into the registers of this chunk's, which are done with)
     }
+    update_state<DK, DV>(S, decay_pow(l2, rows), Ks, Vs, weight, row0, g, c);
     __syncthreads();
   }
 
   float *fin = nullptr;
   if (STATES) fin = a.fin + ((int64_t)blockIdx.x * a.H + h) * state_size;
   else if (last && a.fin && own >= 0) fin = a.fin + ((int64_t)own * a.H + h) * state_size;
-  if (fin) {
+  if (fin) each_of_state<DK, DV>(a, S, row0, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
+}
+
+// The two walks back of the derivative as one, k and v of `a` being q and dout: own rows of keys and values, G^T k and the weighted rows of dout give dv, G v and the
+// weighted rows of q give dk.  Reads four tensors and writes two, where two walks read three and write one each, and forms G once.
+struct Back {
+  const void *k, *v;
+  void *dk, *dv;
+  Strides sk, sv;
+};
+template <int DK, int DV>
+__global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
+  constexpr int LK = DK + 16, LV = DV + 16;
+  constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;
+  constexpr int KT = DK / 16, CT = DV / 16, KJ = DK / 32, VJ = DV / 32;
+  extern __shared__ __align__(16) unsigned char lds_bytes[];
+  bf16_t *Qs = (bf16_t *)lds_bytes, *Ds = Qs + kChunk * LK;
+  float *weight = (float *)(Ds + kChunk * LV);
+  bf16_t *Gt = (bf16_t *)(weight + kChunk);
+  const Segment seg = segment_of(a.seq, blockIdx.x);
+  if (seg.rows < 0) return;
+  const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int row0 = DK / 4 * w;
+  const Rows qr = rows_of(a.k, a.sk, seg, a, h, a.kw, 2), dr = rows_of(a.v, a.sv, seg, a, h, a.vw, 2), kr = rows_of(b.k, b.sk, seg, a, h, a.kw, 2),
+             vr = rows_of(b.v, b.sv, seg, a, h, a.vw, 2), dkr = rows_of(b.dk, b.sk, seg, a, h, a.kw, 2), dvr = rows_of(b.dv, b.sv, seg, a, h, a.vw, 2);
+  const float l2 = log2_decay(a.log_decay, h);
+  const int64_t state_size = (int64_t)a.kw * a.vw;
+
+  f32x4 G[DK / 64][CT];
+  const int64_t from = a.by_slot ? (int64_t)blockIdx.x : seg.b;
+  const float *init = a.init ? a.init + (from * a.H + h) * state_size : nullptr;
+  each_of_state<DK, DV>(a, G, row0, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  const Weights weights(a, l2, w, g, c);
+
+  u32x4 rq[PK], rd[PV];
+  bf16x8 K[KJ], V[VJ];
+  const int qrow = tid / (DK / 8), qcol = tid % (DK / 8) * 8, drow = tid / (DV / 8), dcol = tid % (DV / 8) * 8;
+  auto request = [&](int r0) {
+    const Rows::Chunk qc = qr.chunk(r0), dc = dr.chunk(r0);
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+    for (int i = 0; i < PK; ++i) rq[i] = load_piece(qc, qr.offset(qrow + 2048 / DK * i, 2 * qcol), qr.outside(2 * qcol));
+#pragma unroll
+    for (int i = 0; i < PV; ++i) rd[i] = load_piece(dc, dr.offset(drow + 2048 / DV * i, 2 * dcol), dr.outside(2 * dcol));
+  };
+  auto request_own = [&](int r0) {
+    const Rows::Chunk kc = kr.chunk(r0), vc = vr.chunk(r0);
+#pragma unroll
+    for (int j = 0; j < KJ; ++j)
+      K[j] = __builtin_bit_cast(bf16x8, load_piece(kc, kr.offset(16 * w + c, 64 * j + 16 * g), kr.outside(64 * j + 16 * g)));
+#pragma unroll
+    for (int j = 0; j < VJ; ++j)
+      V[j] = __builtin_bit_cast(bf16x8, load_piece(vc, vr.offset(16 * w + c, 64 * j + 16 * g), vr.outside(64 * j + 16 * g)));
+  };
+
+  request(0);
+  request_own(0);
+  for (int r0 = 0; r0 < seg.rows; r0 += kChunk) {
+    const int rows = min(kChunk, seg.rows - r0);
+#pragma unroll
+    for (int i = 0; i < PK; ++i) *(u32x4 *)(Qs + (qrow + 2048 / DK * i) * LK + qcol) = rq[i];
+#pragma unroll
+    for (int i = 0; i < PV; ++i) *(u32x4 *)(Ds + (drow + 2048 / DV * i) * LV + dcol) = rd[i];
+    if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + 1);
+#pragma unroll
+    for (int rt = 0; rt < DK / 64; ++rt)
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
+        *(bf16x4 *)(Gt + tile_column(ct, c) * LK + row0 + 16 * rt + 4 * g) = __builtin_convertvector(G[rt][ct], bf16x4);
+    __syncthreads();
+    request(r0 + kChunk);
+    f32x4 O[2];
+    bf16x8 P[2];
+    weights.products<DK>(Qs, K, g, c, P);
+    const Rows::Chunk vc = dvr.chunk(r0), kc = dkr.chunk(r0);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 16 * (RT * w + rt) + 4 * g + i, col = vcol(ct);
-          if (r < a.kw && col < a.vw) fin[r * a.si + col * a.sj] = S[rt][ct][i];
-        }
+    for (int ct = 0; ct < CT; ++ct) {
+      f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < KJ; ++j) acc = mfma_bf16(*(const bf16x8 *)(Gt + tile_column(ct, c) * LK + 32 * j + 8 * g), K[j], acc);
+      acc *= weights.reach;
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(tile_operand<DV, false>(Ds, 32 * jj, ct, g, c), P[jj], acc);
+      O[ct & 1] = acc;
+      if (ct & 1) store_piece(vc, dvr.offset(16 * w + c, 32 * ct - 32 + 16 * g), dvr.outside(32 * ct - 32 + 16 * g), pack_pair(O[0], O[1]));
+    }
+    weights.products<DV>(Ds, V, g, c, P);
+#pragma unroll
+    for (int kt = 0; kt < KT; ++kt) {
+      f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int j = 0; j < VJ; ++j) acc = mfma_bf16(tile_operand<DK, true>(Gt, 32 * j, kt, g, c), V[j], acc);
+      acc *= weights.reach;
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(tile_operand<DK, false>(Qs, 32 * jj, kt, g, c), P[jj], acc);
+      O[kt & 1] = acc;
+      if (kt & 1) store_piece(kc, dkr.offset(16 * w + c, 32 * kt - 32 + 16 * g), dkr.outside(32 * kt - 32 + 16 * g), pack_pair(O[0], O[1]));
+    }
+    request_own(r0 + kChunk);
+    update_state<DK, DV>(G, decay_pow(l2, rows), Qs, Ds, weight, row0, g, c);
+    __syncthreads();
+  }
+  if (a.fin && seg.s == 0) {
+    float *fin = a.fin + ((int64_t)seg.b * a.H + h) * state_size;
+    each_of_state<DK, DV>(a, G, row0, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
   }
 }
 
-// What the segments of a sequence add to the state, in place, to the states that they begin with: four values of a state per thread, over all
-// segments in their order (from the last one with `reverse`), eight of them requested at a time.
+// What the segments of a sequence add to the state, in place, to the states that they begin with: one value of a state per thread, over all
+// segments in their order (from the last one with `reverse`).  Bound by the way to memory and back of each round of requests, so that a round has many.
+constexpr int kScanRound = 16;
 __global__ __launch_bounds__(64) void scan_kernel(Walk a, float *local) {
   const int h = blockIdx.y, b = blockIdx.z;
-  const int64_t state_size = (int64_t)a.kw * a.vw, e = ((int64_t)blockIdx.x * 64 + threadIdx.x) * 4;
-  if (e >= state_size) return;
+  const int64_t state_size = (int64_t)a.kw * a.vw, e = (int64_t)blockIdx.x * 64 + threadIdx.x;   // (a multiple of 64)
   const int segs = a.seq.segments(b), have = a.seq.rows(b), own = cache_row(a, b);
   const float l2 = log2_decay(a.log_decay, h);
-  f32x4 run = a.init && own >= 0 ? *(const f32x4 *)(a.init + ((int64_t)own * a.H + h) * state_size + e) : f32x4{0.f, 0.f, 0.f, 0.f};
+  float run = a.init && own >= 0 ? a.init[((int64_t)own * a.H + h) * state_size + e] : 0.f;
   const int64_t step = a.H * state_size;
   float *p = local + ((int64_t)a.seq.first_slot(b) * a.H + h) * state_size + e;
   const float full = decay_pow(l2, a.seq.seg), tail = decay_pow(l2, have - (segs - 1) * a.seq.seg);
-  for (int s0 = 0; s0 < segs; s0 += 8) {
-    f32x4 x[8];
+  for (int s0 = 0; s0 < segs; s0 += kScanRound) {
+    float x[kScanRound];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
+    for (int u = 0; u < kScanRound; ++u) {
       const int s = a.reverse ? segs - 1 - s0 - u : s0 + u;
-      if (s0 + u < segs - 1) x[u] = *(const f32x4 *)(p + s * step);   // the last one has added nothing
+      x[u] = s0 + u < segs - 1 ? p[s * step] : 0.f;   // the last one has added nothing
     }
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      if (s0 + u >= segs) break;
+    for (int u = 0; u < kScanRound; ++u) {
       const int s = a.reverse ? segs - 1 - s0 - u : s0 + u;
-      *(f32x4 *)(p + s * step) = run;
-      if (s0 + u < segs - 1) run = run * (s == segs - 1 ? tail : full) + x[u];
+      if (s0 + u < segs) p[s * step] = run;
+      run = run * (s == segs - 1 ? tail : full) + x[u];
     }
   }
 }
@@ -661,6 +730,8 @@ wersa_status validate(const wersa_decay_desc *c) {
       !strides_ok(c->stride_o, *c, c->dv))
     return WERSA_ERR_INVALID_ARG;
   if (c->dk % 16 != 0 || c->dv % 16 != 0 || c->dk > 128 || c->dv > 128) return WERSA_ERR_UNSUPPORTED;
+  for (const int64_t *s : {c->stride_q, c->stride_k, c->stride_v, c->stride_o})
+    if (c->n > 1 && s[2] > kMostRowStride) return WERSA_ERR_UNSUPPORTED;
   if (c->H > 65535 || c->B > 65535 || c->n > (1 << 30)) return WERSA_ERR_UNSUPPORTED;
   return WERSA_OK;
 }
@@ -684,8 +755,21 @@ template <bool STATES> bool launch_walk(const wersa_decay_desc &c, const Walk &a
   if (a.kw <= 64) return a.vw <= 64 ? launch_walk_as<64, 64, STATES>(c, a, st) : launch_walk_as<64, 128, STATES>(c, a, st);
   return a.vw <= 64 ? launch_walk_as<128, 64, STATES>(c, a, st) : launch_walk_as<128, 128, STATES>(c, a, st);
 }
+template <int DK, int DV> bool launch_back_as(const Walk &a, const Back &b, hipStream_t st) {
+  constexpr size_t smem = sizeof(bf16_t) * (kChunk * (DK + 16 + DV + 16) + DV * (DK + 16)) + sizeof(float) * kChunk;
+  auto kern = &back_bf16_kernel<DK, DV>;
+  if (smem > 65536 &&
+      hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess)
+    return false;
+  WERSA_STAGE("wersa_decay_back", st, kern<<<dim3(a.seq.slots(), a.H), 256, smem, st>>>(a, b));
+  return true;
+}
+bool launch_back(const Walk &a, const Back &b, hipStream_t st) {
+  if (a.kw <= 64) return a.vw <= 64 ? launch_back_as<64, 64>(a, b, st) : launch_back_as<64, 128>(a, b, st);
+  return a.vw <= 64 ? launch_back_as<128, 64>(a, b, st) : launch_back_as<128, 128>(a, b, st);
+}
 void launch_scan(const Walk &a, float *local, hipStream_t st) {
-  WERSA_STAGE("wersa_decay_scan", st, scan_kernel<<<dim3((a.kw * a.vw / 4 + 63) / 64, a.H, a.seq.B), 64, 0, st>>>(a, local));
+  WERSA_STAGE("wersa_decay_scan", st, scan_kernel<<<dim3(a.kw * a.vw / 64, a.H, a.seq.B), 64, 0, st>>>(a, local));
 }
 
 }  // namespace
@@ -782,6 +866,10 @@ wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, c
     a.by_slot = r.by_slot = true;
   }
   r.fin = dinitial_state;
+  if (c.dtype == WERSA_BF16) {
+    if (!launch_back(r, Back{k, v, dk, dv, sk, sv}, st)) return WERSA_ERR_LAUNCH;
+    return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
+  }
   if (!launch_walk<false>(c, r, st)) return WERSA_ERR_LAUNCH;
   a.q = v, a.k = dout, a.v = q, a.o = dk;
   a.sq = sv, a.sk = so, a.sv = sq, a.so = sk;
