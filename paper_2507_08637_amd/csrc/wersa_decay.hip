@@ -95,8 +95,9 @@ constexpr int64_t kMostRowStride = 1 << 24;   // elements: 63 rows of 4 bytes st
 typedef __amdgpu_buffer_rsrc_t Buffer;
 struct Rows {
   const char *low;    // of the segment's rows, the first in memory
-  int64_t step;       // bytes from row to row
-  int rows, width;    // width: bytes of a row
+  uint32_t step;      // bytes from row to row
+  int width;          // bytes of a row
+  int rows;
   bool reverse;
   struct Chunk {
     Buffer b;
@@ -104,26 +105,46 @@ struct Rows {
   };
   __device__ __forceinline__ Chunk chunk(int r0) const {
     const int have = max(0, min(kChunk, rows - r0));
-    const uint64_t p = (uint64_t)(low + (reverse ? rows - r0 - have : r0) * step);
+    const uint64_t p = (uint64_t)low + (uint64_t)(uint32_t)(reverse ? rows - r0 - have : r0) * step;
     const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)p), hi = __builtin_amdgcn_readfirstlane((uint32_t)(p >> 32));
-    const uint32_t bytes = __builtin_amdgcn_readfirstlane(have ? (uint32_t)(have - 1) * (uint32_t)step + width : 0);
+    const uint32_t bytes = __builtin_amdgcn_readfirstlane(have ? (uint32_t)(have - 1) * step + width : 0);
     return Chunk{__builtin_amdgcn_make_buffer_rsrc((void *)((uint64_t)hi << 32 | lo), 0, (int)bytes, 0x00020000),
-                 reverse ? (uint32_t)(kChunk - have) * (uint32_t)step : 0};
+                 reverse ? (uint32_t)(kChunk - have) * step : 0};
   }
-  // Of a row of a chunk.  Bytes past the width are none of the buffer's (`outside`, joined in by `or` at the access).
-  __device__ __forceinline__ uint32_t offset(int row, int byte) const { return (uint32_t)(reverse ? kChunk - 1 - row : row) * (uint32_t)step + byte; }
-  __device__ __forceinline__ uint32_t outside(int byte) const { return byte < width ? 0u : 0xffffffc0u; }
+  // Of a byte of a row of a chunk; `rows` further on in the chunk.
+  __device__ __forceinline__ uint32_t offset(int row, int byte) const { return (uint32_t)(reverse ? kChunk - 1 - row : row) * step + byte; }
+  __device__ __forceinline__ uint32_t further(int rows) const { return (uint32_t)(reverse ? -rows : rows) * step; }
 };
-__device__ __forceinline__ u32x4 load_piece(const Rows::Chunk &c, uint32_t offset, uint32_t outside) {
-  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(c.b, (int)((offset - c.missing) | outside), 0, 0));
-}
-__device__ __forceinline__ void store_piece(const Rows::Chunk &c, uint32_t offset, uint32_t outside, u32x4 v) {
-  __builtin_amdgcn_raw_buffer_store_b128(v, c.b, (int)((offset - c.missing) | outside), 0, 0);
-}
+// Bytes past the width are none of the buffer's: joined in by `or` at the access.
+__device__ __forceinline__ uint32_t outside(int byte, int width) { return byte < width ? 0u : 0xffffffc0u; }
+__device__ __forceinline__ u32x4 load_piece(const Rows::Chunk &c, uint32_t at) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(c.b, (int)at, 0, 0)); }
+__device__ __forceinline__ void store_piece(const Rows::Chunk &c, uint32_t at, u32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(v, c.b, (int)at, 0, 0); }
 // Rows of `seg` for head h of a tensor.
 __device__ __forceinline__ Rows rows_of(const void *p, const Strides &s, const Segment &seg, const Walk &a, int h, int cols, int element) {
   const int64_t at = (a.seq.offsets ? 0 : seg.b * s.b) + h * s.h + seg.row0 * s.n;
-  return Rows{(const char *)p + at * element, s.n * element, seg.rows, cols * element, a.reverse};
+  return Rows{(const char *)p + at * element, (uint32_t)(s.n * element), cols * element, seg.rows, a.reverse};
+}
+// The same value, of which the compiler knows nothing: what follows from it is formed where it is used, not kept in registers around a loop.
+__device__ __forceinline__ uint32_t opaque(uint32_t x) {
+  asm volatile("" : "+v"(x));
+  return x;
+}
+// A thread's pieces of a tile of D values a row (PIECES of them, 256 threads), and the pieces 16 g + 64 j of the row of a lane (J of them).  FULL: no columns past the width.
+template <int D, int E, int PIECES, bool FULL> struct TilePieces {
+  uint32_t at, out;
+  __device__ __forceinline__ TilePieces(const Rows &r, int tid) : at(r.offset(tid / (D / E), tid % (D / E) * 16)), out(outside(tid % (D / E) * 16, r.width)) {}
+  __device__ __forceinline__ void load(const Rows &r, int r0, u32x4 (&p)[PIECES]) const {
+    const Rows::Chunk c = r.chunk(r0);
+    uint32_t x = opaque(at) - c.missing;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i, x += r.further(256 * E / D)) p[i] = load_piece(c, FULL ? x : x | out);
+  }
+};
+template <int J, bool FULL, typename V> __device__ __forceinline__ void load_own(const Rows &r, int r0, uint32_t at, int g, V (&p)[J]) {
+  const Rows::Chunk c = r.chunk(r0);
+  const uint32_t x = opaque(at) - c.missing;
+#pragma unroll
+  for (int j = 0; j < J; ++j) p[j] = __builtin_bit_cast(V, load_piece(c, FULL ? x + 64 * j : (x + 64 * j) | outside(64 * j + 16 * g, r.width)));
 }
 
 // ---- float32 matrix instructions -----------------------------------------------------------------
@@ -176,20 +197,16 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
     }
   const float reach = a.inter * decay_pow(l2, 16 * w + c + 1 - shift);
 
-  f32x4 rk[PK], rv[PV], rq[DK / 16];
+  u32x4 rk[PK], rv[PV];
+  f32x4 rq[DK / 16];
   const int krow = tid / (DK / 4), kcol = tid % (DK / 4) * 4, vrow = tid / (DV / 4), vcol = tid % (DV / 4) * 4;   // a thread's first piece
+  const TilePieces<DK, 4, PK, false> kp(kr, tid);
+  const TilePieces<DV, 4, PV, false> vp(vr, tid);
+  const uint32_t qat = qr.offset(16 * w + c, 16 * g);
   auto request = [&](int r0) {
-    const Rows::Chunk kc = kr.chunk(r0), vc = vr.chunk(r0);
-#pragma unroll
-    for (int i = 0; i < PK; ++i) rk[i] = __builtin_bit_cast(f32x4, load_piece(kc, kr.offset(krow + 1024 / DK * i, 4 * kcol), kr.outside(4 * kcol)));
-#pragma unroll
-    for (int i = 0; i < PV; ++i) rv[i] = __builtin_bit_cast(f32x4, load_piece(vc, vr.offset(vrow + 1024 / DV * i, 4 * vcol), vr.outside(4 * vcol)));
-    if (!STATES) {
-      const Rows::Chunk qc = qr.chunk(r0);
-#pragma unroll
-      for (int j = 0; j < DK / 16; ++j)
-        rq[j] = __builtin_bit_cast(f32x4, load_piece(qc, qr.offset(16 * w + c, 64 * j + 16 * g), qr.outside(64 * j + 16 * g)));
-    }
+    kp.load(kr, r0, rk);
+    vp.load(vr, r0, rv);
+    if (!STATES) load_own<DK / 16, false>(qr, r0, qat, g, rq);
   };
 
   request(0);
@@ -197,9 +214,9 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
     const int rows = min(kChunk, seg.rows - r0);
     // what was requested, and the state, into LDS
 #pragma unroll
-    for (int i = 0; i < PK; ++i) *(f32x4 *)(Ks + (krow + 1024 / DK * i) * LK + kcol) = rk[i];
+    for (int i = 0; i < PK; ++i) *(u32x4 *)(Ks + (krow + 1024 / DK * i) * LK + kcol) = rk[i];
 #pragma unroll
-    for (int i = 0; i < PV; ++i) *(f32x4 *)(Vs + (vrow + 1024 / DV * i) * LV + vcol) = rv[i];
+    for (int i = 0; i < PV; ++i) *(u32x4 *)(Vs + (vrow + 1024 / DV * i) * LV + vcol) = rv[i];
     if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + shift);
     f32x4 Q[DK / 16];
     if (!STATES) {
@@ -268,7 +285,7 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
       const Rows::Chunk oc = orow.chunk(r0);
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct)
-        store_piece(oc, orow.offset(16 * w + c, 64 * ct + 16 * g), orow.outside(64 * ct + 16 * g), __builtin_bit_cast(u32x4, O[ct]));
+        store_piece(oc, (orow.offset(16 * w + c, 64 * ct + 16 * g) - oc.missing) | outside(64 * ct + 16 * g, orow.width), __builtin_bit_cast(u32x4, O[ct]));
     }
     __syncthreads();
   }
@@ -301,12 +318,30 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ f32x4 mfma_bf16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 // ds_read_b64_tr_b16: within each group of 16 lanes, lane i passes the address of four consecutive 16-bit values, taken as row i / 4,
 // columns 4 (i % 4) .. + 3 of a 4 x 16 block, and receives column i of that block.
-__device__ __forceinline__ bf16x8 read_transposed(const bf16_t *lo, const bf16_t *hi) {
+__device__ __forceinline__ bf16x8 read_transposed(uint32_t lo, uint32_t hi) {
   typedef __attribute__((address_space(3))) s16x4 *lds_s16x4_ptr;
   const bf16x4 a = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)lo));
   const bf16x4 b = __builtin_bit_cast(bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4_ptr)hi));
   return bf16x8{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
 }
+// Rows of D values in LDS, their 16-byte pieces permuted by the row so that no read or write meets another in a bank (64 banks of 4 bytes): 16-byte accesses by one
+// column of 16 rows, and transposing reads of 32 bytes of 8 rows: rows 4 g + .. of two lane groups, or with NATURAL rows 8 g + ...  Against rows 32 bytes longer
+// than the data, at width 128: half of the cycles of LDS were conflicts.  The permutation goes by the row's last four bits and is an exclusive or, so that a lane needs
+// one address for all tiles of a kind: other rows are a constant further on, other columns one `or` away.
+template <int D, bool NATURAL> __device__ __forceinline__ uint32_t lds_at(int row, int col) {   // in bytes
+  int f;
+  if (D == 128) f = NATURAL ? (row & 3) << 1 | (row & 8) | (row >> 2 & 1) : (row & 7) << 1 | (row >> 3 & 1);
+  else f = NATURAL ? (row & 2) | (row & 8) >> 1 | (row >> 2 & 1) : (row & 6) | (row >> 3 & 1);
+  return 2 * (row * D + ((col >> 3 ^ f) << 3 | (col & 7)));
+}
+template <typename V> __device__ __forceinline__ V lds_read(uint32_t at) { return *(__attribute__((address_space(3))) const V *)at; }
+template <typename V> __device__ __forceinline__ void lds_write(uint32_t at, V v) { *(__attribute__((address_space(3))) V *)at = v; }
+// What a lane reads: the operand with a row of LDS per lane (rows 16 t + c, columns 32 j + 8 g ..), and the transposed one (below).
+template <int D, bool NATURAL> struct RowOperand {
+  uint32_t at;
+  __device__ __forceinline__ RowOperand(int g, int c) : at(opaque(lds_at<D, NATURAL>(c, 8 * g))) {}
+  __device__ __forceinline__ bf16x8 operator()(uint32_t rows, int t, int j) const { return lds_read<bf16x8>((at ^ 64 * j) + rows + 32 * t * D); }
+};
 // x as the sum of three bf16 values, 24 bits of it: keys times their weight enter the state like float32.
 struct Three {
   bf16x8 t[3];
@@ -335,13 +370,14 @@ struct Weights {
     reach = a.inter * decay_pow(l2, 16 * w + c + (a.reverse ? 0 : 1));
   }
   // Products of the own rows `b` with the chunk's rows in LDS, weighted: operands of the products with the other tensor's rows.
-  template <int D> __device__ __forceinline__ void products(const bf16_t *rows, const bf16x8 (&b)[D / 32], int g, int c, bf16x8 (&P)[2]) const {
+  template <int D> __device__ __forceinline__ void products(uint32_t rows, const bf16x8 (&b)[D / 32], int g, int c, bf16x8 (&P)[2]) const {
+    const RowOperand<D, false> operand(g, c);
 #pragma unroll
     for (int jt = 0; jt < 4; ++jt) {
       f32x4 p = f32x4{0.f, 0.f, 0.f, 0.f};
       if (jt <= w) {
 #pragma unroll
-        for (int j = 0; j < D / 32; ++j) p = mfma_bf16(*(const bf16x8 *)(rows + (16 * jt + c) * (D + 16) + 32 * j + 8 * g), b[j], p);
+        for (int j = 0; j < D / 32; ++j) p = mfma_bf16(operand(rows, jt, j), b[j], p);
 #pragma unroll
         for (int i = 0; i < 4; ++i) p[i] = jt < w ? p[i] * before[i] * apart[jt < 3 ? jt : 0] : ahead >= i ? p[i] * on[i] : 0.f;
       }
@@ -351,21 +387,43 @@ struct Weights {
     }
   }
 };
-// Column tiles are dealt in pairs: lane c of tile 2 u + e is column 32 u + 8 (c / 4) + 4 e + c % 4, so that a lane of the output (whose rows down the
-// registers these are) holds eight columns in a row.
-__device__ __forceinline__ int tile_column(int ct, int c) { return 32 * (ct >> 1) + 8 * (c >> 2) + 4 * (ct & 1) + (c & 3); }
-// The tile's columns of 32 rows of LDS from `row` on, down the slots of k: rows 4 g + q and 16 + 4 g + q - 4 (see above), or 8 g + q with NATURAL.
-template <int D, bool NATURAL> __device__ __forceinline__ bf16x8 tile_operand(const bf16_t *rows, int row, int ct, int g, int c) {
-  const bf16_t *p = rows + (row + (NATURAL ? 8 : 4) * g + (c >> 2)) * (D + 16) + 32 * (ct >> 1) + 8 * (c & 3) + 4 * (ct & 1);
-  return read_transposed(p, p + (NATURAL ? 4 : 16) * (D + 16));
-}
+// A tile's 16 columns of 32 rows of LDS from `row` (a multiple of 32) on, down the slots of k: rows 4 g + q and 16 + 4 g + q - 4 (see above), or 8 g + q with NATURAL.
+template <int D, bool NATURAL> struct ColumnOperand {
+  uint32_t at;
+  __device__ __forceinline__ ColumnOperand(int g, int c) : at(opaque(lds_at<D, NATURAL>((NATURAL ? 8 : 4) * g + (c >> 2), 4 * (c & 3)))) {}
+  __device__ __forceinline__ bf16x8 operator()(uint32_t rows, int row, int ct) const {
+    const uint32_t lo = (at ^ 32 * ct) + rows + 2 * row * D;
+    return read_transposed(lo, NATURAL ? (at ^ (32 * ct + 16)) + rows + 2 * (row + 4) * D : lo + 2 * 16 * D);
+  }
+};
+// Two tiles of an output, whose 16 columns each lie four to a lane, as eight columns in a row per lane: from column 16 (g % 2) + 8 (g / 2) of the 32 on
+// (pair_byte).
 __device__ __forceinline__ u32x4 pack_pair(f32x4 x, f32x4 y) {
-  return __builtin_bit_cast(u32x4, __builtin_convertvector(f32x8{x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]}, bf16x8));
+  typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+  const u32x2 a = __builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4)), b = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
+  const auto r0 = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), r1 = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
+  return u32x4{r0[0], r1[0], r0[1], r1[1]};
+}
+__device__ __forceinline__ int pair_byte(int g) { return 32 * (g & 1) + 16 * (g >> 1); }
+// A thread's pieces of a tile into LDS (rows 2048 / D apart, a multiple of 16), and a wave's rows of a state, as columns and rounded to bf16.
+template <int D, int PIECES> __device__ __forceinline__ void put_tile(uint32_t at, const u32x4 (&p)[PIECES]) {
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) lds_write(at + 4096 * i, p[i]);
+}
+template <int DK, int DV, bool NATURAL>
+__device__ __forceinline__ void put_state(uint32_t St, const f32x4 (&S)[DK / 64][DV / 16], int row0, int g, int c) {
+  const uint32_t at = opaque(lds_at<DK, NATURAL>(c, row0 + 4 * g));
+#pragma unroll
+  for (int rt = 0; rt < DK / 64; ++rt)
+#pragma unroll
+    for (int ct = 0; ct < DV / 16; ++ct) lds_write((at ^ 32 * rt) + St + 32 * ct * DK, __builtin_convertvector(S[rt][ct], bf16x4));
 }
 // S <- keep S + (K o weight)^T V over the chunk's rows in LDS: RT row tiles of the wave from `row0` on, all column tiles.
 template <int DK, int DV>
-__device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float keep, const bf16_t *Ks, const bf16_t *Vs, const float *weight, int row0, int g, int c) {
-  constexpr int RT = DK / 64, CT = DV / 16, LK = DK + 16;
+__device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float keep, uint32_t Ks, uint32_t Vs, const float *weight, int row0, int g, int c) {
+  constexpr int RT = DK / 64, CT = DV / 16;
+  const ColumnOperand<DK, false> keys(g, c);
+  const ColumnOperand<DV, false> values(g, c);
   bf16x8 K[RT][2][3];
 #pragma unroll
   for (int jj = 0; jj < 2; ++jj) {
@@ -373,15 +431,14 @@ __device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float
     const f32x8 wt = f32x8{w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const bf16_t *p = Ks + (32 * jj + 4 * g + (c >> 2)) * LK + row0 + 16 * rt + 4 * (c & 3);
-      const Three t(__builtin_convertvector(read_transposed(p, p + 16 * LK), f32x8) * wt);
+      const Three t(__builtin_convertvector(keys(Ks, 32 * jj, row0 / 16 + rt), f32x8) * wt);
 #pragma unroll
       for (int u = 0; u < 3; ++u) K[rt][jj][u] = t.t[u];
     }
   }
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
-    const bf16x8 V[2] = {tile_operand<DV, false>(Vs, 0, ct, g, c), tile_operand<DV, false>(Vs, 32, ct, g, c)};
+    const bf16x8 V[2] = {values(Vs, 0, ct), values(Vs, 32, ct)};
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       f32x4 x = S[rt][ct] * keep;
@@ -394,29 +451,29 @@ __device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float
   }
 }
 // A wave's rows of a state, from memory or to it.
-template <int DK, int DV, typename F> __device__ __forceinline__ void each_of_state(const Walk &a, f32x4 (&S)[DK / 64][DV / 16], int row0, int g, int c, F f) {
+template <int DK, int DV, typename F> __device__ __forceinline__ void each_of_state(const Walk &a, f32x4 (&S)[DK / 64][DV / 16], int row0, int g, int lane_c, F f) {
+  const int c = (int)opaque((uint32_t)lane_c);
 #pragma unroll
   for (int rt = 0; rt < DK / 64; ++rt)
 #pragma unroll
     for (int ct = 0; ct < DV / 16; ++ct)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const int r = row0 + 16 * rt + 4 * g + i, col = tile_column(ct, c);
+        const int r = row0 + 16 * rt + 4 * g + i, col = 16 * ct + c;
         S[rt][ct][i] = f(S[rt][ct][i], r < a.kw && col < a.vw, r * a.si + col * a.sj);
       }
 }
 
 // As walk_f32_kernel, for bf16 tensors.  P and the state as an operand of the output are rounded to bf16, like the output; what goes into the
-// state is not.  Rows of LDS are 32 bytes longer than the data: eight rows then begin in eight different groups of banks, for both kinds of reads.
-template <int DK, int DV, bool STATES>
+// state is not.
+template <int DK, int DV, bool FULL, bool STATES>
 __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(Walk a) {
-  constexpr int LK = DK + 16, LV = DV + 16;
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;   // pieces of a thread
   constexpr int CT = DV / 16, QJ = DK / 32;
   extern __shared__ __align__(16) unsigned char lds_bytes[];
-  bf16_t *Ks = (bf16_t *)lds_bytes, *Vs = Ks + kChunk * LK;
-  float *weight = (float *)(Vs + kChunk * LV);
-  bf16_t *St = (bf16_t *)(weight + kChunk);   // columns of the state, as rows
+  // in LDS: K, V, the columns of the state as rows, the keys' weights
+  const uint32_t Ks = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes, Vs = Ks + 2 * kChunk * DK, St = Vs + 2 * kChunk * DV;
+  float *weight = (float *)(lds_bytes + 2 * (kChunk * (DK + DV) + (STATES ? 0 : DV * DK)));
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
   const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
@@ -428,7 +485,7 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
   const float l2 = log2_decay(a.log_decay, h);
   const int64_t state_size = (int64_t)a.kw * a.vw;
 
-  f32x4 S[DK / 64][CT];   // S[rt][ct][i] is row row0 + 16 rt + 4 g + i, column tile_column(ct, c)
+  f32x4 S[DK / 64][CT];   // S[rt][ct][i] is row row0 + 16 rt + 4 g + i, column 16 ct + c
   const int own = cache_row(a, seg.b);
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
   const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
@@ -437,36 +494,24 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
 
   u32x4 rk[PK], rv[PV];
   bf16x8 Q[QJ];
-  const int krow = tid / (DK / 8), kcol = tid % (DK / 8) * 8, vrow = tid / (DV / 8), vcol = tid % (DV / 8) * 8;   // a thread's first piece
+  const TilePieces<DK, 8, PK, FULL> kp(kr, tid);
+  const TilePieces<DV, 8, PV, FULL> vp(vr, tid);
+  const uint32_t qat = qr.offset(16 * w + c, 16 * g), oat = orow.offset(16 * w + c, pair_byte(g));
+  const uint32_t kput = Ks + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), vput = Vs + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
   auto request = [&](int r0) {
-    const Rows::Chunk kc = kr.chunk(r0), vc = vr.chunk(r0);
-#pragma unroll
-    for (int i = 0; i < PK; ++i) rk[i] = load_piece(kc, kr.offset(krow + 2048 / DK * i, 2 * kcol), kr.outside(2 * kcol));
-#pragma unroll
-    for (int i = 0; i < PV; ++i) rv[i] = load_piece(vc, vr.offset(vrow + 2048 / DV * i, 2 * vcol), vr.outside(2 * vcol));
-  };
-  auto request_own = [&](int r0) {   // the wave's 16 queries
-    const Rows::Chunk qc = qr.chunk(r0);
-#pragma unroll
-    for (int j = 0; j < QJ; ++j)
-      Q[j] = __builtin_bit_cast(bf16x8, load_piece(qc, qr.offset(16 * w + c, 64 * j + 16 * g), qr.outside(64 * j + 16 * g)));
+    kp.load(kr, r0, rk);
+    vp.load(vr, r0, rv);
   };
 
   request(0);
-  if (!STATES) request_own(0);
+  if (!STATES) load_own<QJ, FULL>(qr, 0, qat, g, Q);
   for (int r0 = 0; r0 < seg.rows; r0 += kChunk) {
     const int rows = min(kChunk, seg.rows - r0);
-#pragma unroll
-    for (int i = 0; i < PK; ++i) *(u32x4 *)(Ks + (krow + 2048 / DK * i) * LK + kcol) = rk[i];
-#pragma unroll
-    for (int i = 0; i < PV; ++i) *(u32x4 *)(Vs + (vrow + 2048 / DV * i) * LV + vcol) = rv[i];
+    put_tile<DK, PK>(kput, rk);
+    put_tile<DV, PV>(vput, rv);
     if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + (a.reverse ? 1 : 0));
     if (!STATES) {
-#pragma unroll
-      for (int rt = 0; rt < DK / 64; ++rt)
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-          *(bf16x4 *)(St + tile_column(ct, c) * LK + row0 + 16 * rt + 4 * g) = __builtin_convertvector(S[rt][ct], bf16x4);
+      put_state<DK, DV, false>(St, S, row0, g, c);
     }
     __syncthreads();
     request(r0 + kChunk);
@@ -474,19 +519,22 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
       bf16x8 P[2];
       weights.products<DK>(Ks, Q, g, c, P);
       const Rows::Chunk oc = orow.chunk(r0);
+      const uint32_t x = opaque(oat) - oc.missing;
+      const RowOperand<DK, false> state(g, c);
+      const ColumnOperand<DV, false> values(g, c);
       f32x4 O[2];
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
         f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int j = 0; j < QJ; ++j) acc = mfma_bf16(*(const bf16x8 *)(St + tile_column(ct, c) * LK + 32 * j + 8 * g), Q[j], acc);
+        for (int j = 0; j < QJ; ++j) acc = mfma_bf16(state(St, ct, j), Q[j], acc);
         acc *= weights.reach;
 #pragma unroll
-        for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(tile_operand<DV, false>(Vs, 32 * jj, ct, g, c), P[jj], acc);
+        for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(values(Vs, 32 * jj, ct), P[jj], acc);
         O[ct & 1] = acc;
-        if (ct & 1) store_piece(oc, orow.offset(16 * w + c, 32 * ct - 32 + 16 * g), orow.outside(32 * ct - 32 + 16 * g), pack_pair(O[0], O[1]));
+        if (ct & 1) store_piece(oc, FULL ? x + 32 * (ct - 1) : (x + 32 * (ct - 1)) | outside(32 * (ct - 1) + pair_byte(g), orow.width), pack_pair(O[0], O[1]));
       }
-      request_own(r0 + kChunk);   // (into the registers of this chunk's, which are done with)
+      load_own<QJ, FULL>(qr, r0 + kChunk, qat, g, Q);   // (into the registers of this chunk's, which are done with)
     }
     update_state<DK, DV>(S, decay_pow(l2, rows), Ks, Vs, weight, row0, g, c);
     __syncthreads();
@@ -505,15 +553,13 @@ struct Back {
   void *dk, *dv;
   Strides sk, sv;
 };
-template <int DK, int DV>
+template <int DK, int DV, bool FULL>
 __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
-  constexpr int LK = DK + 16, LV = DV + 16;
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;
   constexpr int KT = DK / 16, CT = DV / 16, KJ = DK / 32, VJ = DV / 32;
   extern __shared__ __align__(16) unsigned char lds_bytes[];
-  bf16_t *Qs = (bf16_t *)lds_bytes, *Ds = Qs + kChunk * LK;
-  float *weight = (float *)(Ds + kChunk * LV);
-  bf16_t *Gt = (bf16_t *)(weight + kChunk);
+  const uint32_t Qs = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes, Ds = Qs + 2 * kChunk * DK, Gt = Ds + 2 * kChunk * DV;
+  float *weight = (float *)(lds_bytes + 2 * (kChunk * (DK + DV) + DV * DK));
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
   const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
@@ -531,66 +577,67 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
 
   u32x4 rq[PK], rd[PV];
   bf16x8 K[KJ], V[VJ];
-  const int qrow = tid / (DK / 8), qcol = tid % (DK / 8) * 8, drow = tid / (DV / 8), dcol = tid % (DV / 8) * 8;
+  const TilePieces<DK, 8, PK, FULL> qp(qr, tid);
+  const TilePieces<DV, 8, PV, FULL> dp(dr, tid);
+  const uint32_t kat = kr.offset(16 * w + c, 16 * g), vat = vr.offset(16 * w + c, 16 * g);
+  const uint32_t dkat = dkr.offset(16 * w + c, pair_byte(g)), dvat = dvr.offset(16 * w + c, pair_byte(g));
+  const uint32_t qput = Qs + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), dput = Ds + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
   auto request = [&](int r0) {
-    const Rows::Chunk qc = qr.chunk(r0), dc = dr.chunk(r0);
-#pragma unroll
-    for (int i = 0; i < PK; ++i) rq[i] = load_piece(qc, qr.offset(qrow + 2048 / DK * i, 2 * qcol), qr.outside(2 * qcol));
-#pragma unroll
-    for (int i = 0; i < PV; ++i) rd[i] = load_piece(dc, dr.offset(drow + 2048 / DV * i, 2 * dcol), dr.outside(2 * dcol));
+    qp.load(qr, r0, rq);
+    dp.load(dr, r0, rd);
   };
   auto request_own = [&](int r0) {
-    const Rows::Chunk kc = kr.chunk(r0), vc = vr.chunk(r0);
-#pragma unroll
-    for (int j = 0; j < KJ; ++j)
-      K[j] = __builtin_bit_cast(bf16x8, load_piece(kc, kr.offset(16 * w + c, 64 * j + 16 * g), kr.outside(64 * j + 16 * g)));
-#pragma unroll
-    for (int j = 0; j < VJ; ++j)
-      V[j] = __builtin_bit_cast(bf16x8, load_piece(vc, vr.offset(16 * w + c, 64 * j + 16 * g), vr.outside(64 * j + 16 * g)));
+    load_own<KJ, FULL>(kr, r0, kat, g, K);
+    load_own<VJ, FULL>(vr, r0, vat, g, V);
   };
 
   request(0);
   request_own(0);
   for (int r0 = 0; r0 < seg.rows; r0 += kChunk) {
     const int rows = min(kChunk, seg.rows - r0);
-#pragma unroll
-    for (int i = 0; i < PK; ++i) *(u32x4 *)(Qs + (qrow + 2048 / DK * i) * LK + qcol) = rq[i];
-#pragma unroll
-    for (int i = 0; i < PV; ++i) *(u32x4 *)(Ds + (drow + 2048 / DV * i) * LV + dcol) = rd[i];
+    put_tile<DK, PK>(qput, rq);
+    put_tile<DV, PV>(dput, rd);
     if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + 1);
-#pragma unroll
-    for (int rt = 0; rt < DK / 64; ++rt)
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-        *(bf16x4 *)(Gt + tile_column(ct, c) * LK + row0 + 16 * rt + 4 * g) = __builtin_convertvector(G[rt][ct], bf16x4);
+    put_state<DK, DV, true>(Gt, G, row0, g, c);
     __syncthreads();
     request(r0 + kChunk);
     f32x4 O[2];
     bf16x8 P[2];
     weights.products<DK>(Qs, K, g, c, P);
-    const Rows::Chunk vc = dvr.chunk(r0), kc = dkr.chunk(r0);
+    {
+      const Rows::Chunk oc = dvr.chunk(r0);
+      const uint32_t x = opaque(dvat) - oc.missing;
+      const RowOperand<DK, true> state(g, c);
+      const ColumnOperand<DV, false> douts(g, c);
 #pragma unroll
-    for (int ct = 0; ct < CT; ++ct) {
-      f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int ct = 0; ct < CT; ++ct) {
+        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < KJ; ++j) acc = mfma_bf16(*(const bf16x8 *)(Gt + tile_column(ct, c) * LK + 32 * j + 8 * g), K[j], acc);
-      acc *= weights.reach;
+        for (int j = 0; j < KJ; ++j) acc = mfma_bf16(state(Gt, ct, j), K[j], acc);
+        acc *= weights.reach;
 #pragma unroll
-      for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(tile_operand<DV, false>(Ds, 32 * jj, ct, g, c), P[jj], acc);
-      O[ct & 1] = acc;
-      if (ct & 1) store_piece(vc, dvr.offset(16 * w + c, 32 * ct - 32 + 16 * g), dvr.outside(32 * ct - 32 + 16 * g), pack_pair(O[0], O[1]));
+        for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(douts(Ds, 32 * jj, ct), P[jj], acc);
+        O[ct & 1] = acc;
+        if (ct & 1) store_piece(oc, FULL ? x + 32 * (ct - 1) : (x + 32 * (ct - 1)) | outside(32 * (ct - 1) + pair_byte(g), dvr.width), pack_pair(O[0], O[1]));
+      }
     }
     weights.products<DV>(Ds, V, g, c, P);
+    {
+      const Rows::Chunk oc = dkr.chunk(r0);
+      const uint32_t x = opaque(dkat) - oc.missing;
+      const ColumnOperand<DK, true> state(g, c);
+      const ColumnOperand<DK, false> queries(g, c);
 #pragma unroll
-    for (int kt = 0; kt < KT; ++kt) {
-      f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int kt = 0; kt < KT; ++kt) {
+        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int j = 0; j < VJ; ++j) acc = mfma_bf16(tile_operand<DK, true>(Gt, 32 * j, kt, g, c), V[j], acc);
-      acc *= weights.reach;
+        for (int j = 0; j < VJ; ++j) acc = mfma_bf16(state(Gt, 32 * j, kt), V[j], acc);
+        acc *= weights.reach;
 #pragma unroll
-      for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(tile_operand<DK, false>(Qs, 32 * jj, kt, g, c), P[jj], acc);
-      O[kt & 1] = acc;
-      if (kt & 1) store_piece(kc, dkr.offset(16 * w + c, 32 * kt - 32 + 16 * g), dkr.outside(32 * kt - 32 + 16 * g), pack_pair(O[0], O[1]));
+        for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(queries(Qs, 32 * jj, kt), P[jj], acc);
+        O[kt & 1] = acc;
+        if (kt & 1) store_piece(oc, FULL ? x + 32 * (kt - 1) : (x + 32 * (kt - 1)) | outside(32 * (kt - 1) + pair_byte(g), dkr.width), pack_pair(O[0], O[1]));
+      }
     }
     request_own(r0 + kChunk);
     update_state<DK, DV>(G, decay_pow(l2, rows), Qs, Ds, weight, row0, g, c);
@@ -604,7 +651,7 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
 
 // What the segments of a sequence add to the state, in place, to the states that they begin with: one value of a state per thread, over all
 // segments in their order (from the last one with `reverse`).  Bound by the way to memory and back of each round of requests, so that a round has many.
-constexpr int kScanRound = 16;
+constexpr int kScanRound = 32;
 __global__ __launch_bounds__(64) void scan_kernel(Walk a, float *local) {
   const int h = blockIdx.y, b = blockIdx.z;
   const int64_t state_size = (int64_t)a.kw * a.vw, e = (int64_t)blockIdx.x * 64 + threadIdx.x;   // (a multiple of 64)
@@ -688,11 +735,10 @@ __global__ __launch_bounds__(256) void step_kernel(Step a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-constexpr int kSegmentsWanted = 768;   // workgroups that a walk should have
-
+// Workgroups that a walk should have: those that the device holds at a time, three to a compute unit at widths up to 64 in bf16, else two.
 int segment_rows(const wersa_decay_desc &c) {
   const int64_t slices = (int64_t)c.H * (c.packed ? 1 : c.B);
-  const int64_t want = kSegmentsWanted / slices;   // segments of a slice
+  const int64_t want = (c.dk <= 64 && c.dv <= 64 ? 768 : 512) / slices;   // segments of a slice
   if (want <= 1) return c.packed ? INT32_MAX / 2 : (c.n + kChunk - 1) / kChunk * kChunk + kChunk;
   int64_t rows = ((int64_t)c.n + want - 1) / want;
   rows = (rows + kChunk - 1) / kChunk * kChunk;
@@ -737,32 +783,29 @@ wersa_status validate(const wersa_decay_desc *c) {
 }
 bool misaligned(const void *p, size_t a) { return ((uintptr_t)p % a) != 0; }
 Strides strides(const int64_t *s) { return Strides{s[0], s[1], s[2]}; }
-template <typename K> bool launch_walk_kernel(K kern, size_t smem, bool states, const Walk &a, hipStream_t st) {
+template <typename K, typename... Args> bool launch(const char *name, K kern, size_t smem, const Walk &a, hipStream_t st, Args... more) {
   if (smem > 65536 &&
       hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess)
     return false;
-  WERSA_STAGE(states ? "wersa_decay_states" : "wersa_decay_walk", st, kern<<<dim3(a.seq.slots(), a.H), 256, smem, st>>>(a));
+  WERSA_STAGE(name, st, kern<<<dim3(a.seq.slots(), a.H), 256, smem, st>>>(a, more...));
   return true;
 }
 template <int DK, int DV, bool STATES> bool launch_walk_as(const wersa_decay_desc &c, const Walk &a, hipStream_t st) {
+  const char *name = STATES ? "wersa_decay_states" : "wersa_decay_walk";
   if (c.dtype == WERSA_F32)
-    return launch_walk_kernel(&walk_f32_kernel<DK, DV, STATES>,
-                              sizeof(float) * (kChunk * (DK + 4 + DV + 4 + 1) + (STATES ? 0 : DV * (DK + 4))), STATES, a, st);
-  return launch_walk_kernel(&walk_bf16_kernel<DK, DV, STATES>,
-                            sizeof(bf16_t) * (kChunk * (DK + 16 + DV + 16) + (STATES ? 0 : DV * (DK + 16))) + sizeof(float) * kChunk, STATES, a, st);
+    return launch(name, &walk_f32_kernel<DK, DV, STATES>, sizeof(float) * (kChunk * (DK + 4 + DV + 4 + 1) + (STATES ? 0 : DV * (DK + 4))), a, st);
+  constexpr size_t smem = sizeof(bf16_t) * (kChunk * (DK + DV) + (STATES ? 0 : DV * DK)) + sizeof(float) * kChunk;
+  return a.kw == DK && a.vw == DV ? launch(name, &walk_bf16_kernel<DK, DV, true, STATES>, smem, a, st)
+                                  : launch(name, &walk_bf16_kernel<DK, DV, false, STATES>, smem, a, st);
 }
 template <bool STATES> bool launch_walk(const wersa_decay_desc &c, const Walk &a, hipStream_t st) {
   if (a.kw <= 64) return a.vw <= 64 ? launch_walk_as<64, 64, STATES>(c, a, st) : launch_walk_as<64, 128, STATES>(c, a, st);
   return a.vw <= 64 ? launch_walk_as<128, 64, STATES>(c, a, st) : launch_walk_as<128, 128, STATES>(c, a, st);
 }
 template <int DK, int DV> bool launch_back_as(const Walk &a, const Back &b, hipStream_t st) {
-  constexpr size_t smem = sizeof(bf16_t) * (kChunk * (DK + 16 + DV + 16) + DV * (DK + 16)) + sizeof(float) * kChunk;
-  auto kern = &back_bf16_kernel<DK, DV>;
-  if (smem > 65536 &&
-      hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess)
-    return false;
-  WERSA_STAGE("wersa_decay_back", st, kern<<<dim3(a.seq.slots(), a.H), 256, smem, st>>>(a, b));
-  return true;
+  constexpr size_t smem = sizeof(bf16_t) * (kChunk * (DK + DV) + DV * DK) + sizeof(float) * kChunk;
+  return a.kw == DK && a.vw == DV ? launch("wersa_decay_back", &back_bf16_kernel<DK, DV, true>, smem, a, st, b)
+                                  : launch("wersa_decay_back", &back_bf16_kernel<DK, DV, false>, smem, a, st, b);
 }
 bool launch_back(const Walk &a, const Back &b, hipStream_t st) {
   if (a.kw <= 64) return a.vw <= 64 ? launch_back_as<64, 64>(a, b, st) : launch_back_as<64, 128>(a, b, st);

@@ -17,20 +17,37 @@ typedef u32x2 u32x2_any __attribute__((aligned(1)));
 typedef uint32_t u32_any __attribute__((aligned(1)));
 
 // E values of a row from column `col` on, 16 bytes; columns past the end are zeros.
-template <typename T, int E> __device__ __forceinline__ void load_piece(const T *row, int col, int cols, float (&v)[E]) {
+template <typename T> __device__ __forceinline__ u32x4 load_raw(const T *row, int col, int cols) {
+  constexpr int E = 16 / sizeof(T);
+  u32x4 p = u32x4{0, 0, 0, 0};
   if (col + E <= cols) {
-    const u32x4 p = *reinterpret_cast<const u32x4_any *>(row + col);
+    p = *reinterpret_cast<const u32x4_any *>(row + col);
+  } else if (col < cols) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (E == 4) v[i] = __uint_as_float(p[i]);
-      else {
-        v[2 * i] = __uint_as_float(p[i] << 16);
-        v[2 * i + 1] = __uint_as_float(p[i] & 0xffff0000u);
-      }
+    for (int i = 0; i < E; ++i)
+      if (col + i < cols) p[i * (int)sizeof(T) / 4] |= sizeof(T) == 4 ? __float_as_uint(ld(row + col + i)) : (__float_as_uint(ld(row + col + i)) >> 16) << 16 * (i & 1);
+  }
+  return p;
+}
+template <typename T, int E> __device__ __forceinline__ void spread(const u32x4 &p, float (&v)[E]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (E == 4) v[i] = __uint_as_float(p[i]);
+    else {
+      v[2 * i] = __uint_as_float(p[i] << 16);
+      v[2 * i + 1] = __uint_as_float(p[i] & 0xffff0000u);
     }
-  } else {
+  }
+}
+template <typename T, int E> __device__ __forceinline__ void load_piece(const T *row, int col, int cols, float (&v)[E]) { spread<T, E>(load_raw(row, col, cols), v); }
+// E weights from column `col` on; ones where there are none.
+template <int E> __device__ __forceinline__ void load_weights(const float *weight, int col, int cols, float (&w)[E]) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = col + i < cols ? ld(row + col + i) : 0.f;
+  for (int i0 = 0; i0 < E; i0 += 4) {
+    float u[4] = {1.f, 1.f, 1.f, 1.f};
+    if (weight) load_piece<float, 4>(weight, col + i0, cols, u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i0 + i] = u[i];
   }
 }
 template <typename T, int E> __device__ __forceinline__ void store_piece(T *row, int col, int cols, const float (&v)[E]) {
@@ -123,10 +140,9 @@ __global__ __launch_bounds__(256) void norm_kernel(NormJob a) {
 #pragma unroll
   for (int p = 0; p < PIECES; ++p) {
     float w[E];
-    if (a.weight) load_piece<float, 4>(a.weight, (t + LANES * p) * E, a.cols, *reinterpret_cast<float(*)[4]>(w));
-    if (a.weight && E == 8) load_piece<float, 4>(a.weight, (t + LANES * p) * E + 4, a.cols, *reinterpret_cast<float(*)[4]>(w + E - 4));
+    load_weights(a.weight, (t + LANES * p) * E, a.cols, w);
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[p][i] = a.weight ? v[p][i] * rstd * w[i] : v[p][i] * rstd;
+    for (int i = 0; i < E; ++i) v[p][i] = v[p][i] * rstd * w[i];
   }
   if (!EIGHT) {
     T *y = (T *)a.y + (ok ? row : 0) * a.cols;
@@ -164,6 +180,11 @@ __global__ __launch_bounds__(256) void norm_kernel(NormJob a) {
   }
 }
 
+// Workgroups of the backward at most: three to a compute unit, two where a thread holds 32 columns (weights, sums and three tensors' values in registers).
+// 131072 rows of 2048 in bf16: 413 us with 512, 433 with 768, 719 with three to a unit and registers in scratch; 128000 rows of 128 in float32: 44.4 with 768, 47.2 with 512.
+constexpr int kBackGroups = 768;
+template <typename T, int PIECES> constexpr int back_groups() { return PIECES * 16 / sizeof(T) >= 32 ? 512 : kBackGroups; }
+
 struct NormBackJob {
   const void *r, *dy, *dr;
   const float *weight, *rstd;
@@ -173,57 +194,64 @@ struct NormBackJob {
   int cols;
 };
 
-// dx = rstd (g - xhat mean(g xhat)) + dr with g = dy weight.  A workgroup takes rows from its index on, as many at a time as it holds, and keeps its columns'
-// sums of dy xhat in registers until the end.
+// dx = rstd (g - xhat mean(g xhat)) + dr with g = dy weight.  A workgroup takes rows from its index on, as many at a time as it holds, with the weights of its
+// columns and their sums of dy xhat in registers throughout.  All that a row needs is requested before the first of it is used; it stays as it came, and is taken apart twice.
 template <typename T, int LANES, int PIECES>
-__global__ __launch_bounds__(256) void norm_back_kernel(NormBackJob a) {
+__global__ __launch_bounds__(256, back_groups<T, PIECES>() / 256) void norm_back_kernel(NormBackJob a) {
   constexpr int E = 16 / sizeof(T), ROWS = 256 / LANES;
   __shared__ float part[4];
   __shared__ float sums[LANES == 256 ? 1 : 256 * 4];
   const int t = threadIdx.x % LANES;
-  float dw[PIECES][E];
+  float w[PIECES][E], dw[PIECES][E];
 #pragma unroll
-  for (int p = 0; p < PIECES; ++p)
+  for (int p = 0; p < PIECES; ++p) {
+    load_weights(a.weight, (t + LANES * p) * E, a.cols, w[p]);
 #pragma unroll
     for (int i = 0; i < E; ++i) dw[p][i] = 0.f;
+  }
   for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS) {
     const int64_t row = row0 + threadIdx.x / LANES, at = row < a.rows ? row : 0;
     const int cols = row < a.rows ? a.cols : 0;
-    float v[PIECES][E], g[PIECES][E];
-    const T *r = (const T *)a.r + at * a.stride_r, *dy = (const T *)a.dy + at * a.cols;
+    const T *r = (const T *)a.r + at * a.stride_r, *dy = (const T *)a.dy + at * a.cols, *dr = (const T *)a.dr + at * a.cols;
+    u32x4 rr[PIECES], rd[PIECES], ru[PIECES];
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) load_piece<T, E>(r, (t + LANES * p) * E, cols, v[p]);
+    for (int p = 0; p < PIECES; ++p) {
+      rr[p] = load_raw(r, (t + LANES * p) * E, cols);
+      rd[p] = load_raw(dy, (t + LANES * p) * E, cols);
+    }
+    if (a.dr) {
 #pragma unroll
-    for (int p = 0; p < PIECES; ++p) load_piece<T, E>(dy, (t + LANES * p) * E, cols, g[p]);
+      for (int p = 0; p < PIECES; ++p) ru[p] = load_raw(dr, (t + LANES * p) * E, cols);
+    }
     const float rstd = a.rstd[at];
     float dot = 0.f;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      float w[E], s = 0.f;
-      if (a.weight) load_piece<float, 4>(a.weight, (t + LANES * p) * E, a.cols, *reinterpret_cast<float(*)[4]>(w));
-      if (a.weight && E == 8) load_piece<float, 4>(a.weight, (t + LANES * p) * E + 4, a.cols, *reinterpret_cast<float(*)[4]>(w + E - 4));
+      float v[E], g[E], s = 0.f;
+      spread<T, E>(rr[p], v);
+      spread<T, E>(rd[p], g);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        v[p][i] *= rstd;
-        dw[p][i] += g[p][i] * v[p][i];
-        if (a.weight) g[p][i] *= w[i];
-        s += g[p][i] * v[p][i];
+        v[i] *= rstd;
+        dw[p][i] += g[i] * v[i];
+        s += g[i] * w[p][i] * v[i];
       }
       dot += s;
     }
     const float mean = row_sum<LANES>(dot, part) / (float)a.cols;
     T *dx = (T *)a.dx + at * a.cols;
-    const T *dr = (const T *)a.dr + at * a.cols;
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      float u[E];
-      if (a.dr) load_piece<T, E>(dr, (t + LANES * p) * E, cols, u);
+      float v[E], g[E], u[E];
+      spread<T, E>(rr[p], v);
+      spread<T, E>(rd[p], g);
+      if (a.dr) spread<T, E>(ru[p], u);
 #pragma unroll
       for (int i = 0; i < E; ++i) {
-        g[p][i] = rstd * (g[p][i] - v[p][i] * mean);
-        if (a.dr) g[p][i] += u[i];
+        g[i] = rstd * (g[i] * w[p][i] - v[i] * rstd * mean);
+        if (a.dr) g[i] += u[i];
       }
-      store_piece<T, E>(dx, (t + LANES * p) * E, cols, g[p]);
+      store_piece<T, E>(dx, (t + LANES * p) * E, cols, g);
     }
   }
   if (!a.partial) return;
@@ -253,28 +281,26 @@ __global__ __launch_bounds__(256) void norm_back_kernel(NormBackJob a) {
     }
 }
 
-// Sum over the workgroups, in their order: 16 columns, 16 shares of the workgroups.
-__global__ __launch_bounds__(256) void norm_reduce_kernel(const float *partial, int groups, int cols, float *dweight) {
-  __shared__ float part[16][17];
+// Sum over the workgroups: 16 columns, 64 shares of the workgroups, all requests of a share at once.
+__global__ __launch_bounds__(1024) void norm_reduce_kernel(const float *partial, int groups, int cols, float *dweight) {
+  constexpr int SHARES = 64, EACH = kBackGroups / SHARES;
+  __shared__ float part[SHARES][17];
   const int c = threadIdx.x % 16, s = threadIdx.x / 16, col = blockIdx.x * 16 + c;
+  float v[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) v[i] = col < cols && s + SHARES * i < groups ? partial[(int64_t)(s + SHARES * i) * cols + col] : 0.f;
   float sum = 0.f;
-  if (col < cols)
-    for (int i = s; i < groups; i += 16) sum += partial[(int64_t)i * cols + col];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) sum += v[i];
   part[s][c] = sum;
-  __syncthreads();
-  if (s == 0 && col < cols) {
-    float v[16];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) v[i] = part[i][c];
-#pragma unroll
-    for (int d = 8; d > 0; d /= 2)
-#pragma unroll
-      for (int i = 0; i < d; ++i) v[i] += v[i + d];
-    dweight[col] = v[0];
+  for (int d = SHARES / 2; d > 0; d /= 2) {
+    __syncthreads();
+    if (s < d) part[s][c] += part[s + d][c];
   }
+  if (s == 0 && col < cols) dweight[col] = part[0][c];
 }
 
-constexpr int kBackGroups = 1024;   // workgroups of the backward at most: four to a compute unit
 
 bool misaligned(const void *p, size_t a) { return ((uintptr_t)p % a) != 0; }
 
@@ -367,11 +393,11 @@ wersa_status wersa_rms_norm_backward(const wersa_norm_desc *desc, const void *r,
   by_width(*desc, [&](auto *type, auto lanes, auto pieces) {
     typedef typename std::remove_pointer<decltype(type)>::type T;
     constexpr int L = decltype(lanes)::value, P = decltype(pieces)::value;
-    groups = (int)std::min<int64_t>(kBackGroups, (desc->rows + 256 / L - 1) / (256 / L));
+    groups = (int)std::min<int64_t>(back_groups<T, P>(), (desc->rows + 256 / L - 1) / (256 / L));
     if (groups > 0) WERSA_STAGE("wersa_rms_norm_back", st, (norm_back_kernel<T, L, P><<<groups, 256, 0, st>>>(a)));
   });
   if (dweight)
-    WERSA_STAGE("wersa_rms_norm_reduce", st, norm_reduce_kernel<<<(desc->cols + 15) / 16, 256, 0, st>>>((const float *)workspace, groups, desc->cols, dweight));
+    WERSA_STAGE("wersa_rms_norm_reduce", st, norm_reduce_kernel<<<(desc->cols + 15) / 16, 1024, 0, st>>>((const float *)workspace, groups, desc->cols, dweight));
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
 
