@@ -183,7 +183,7 @@ __global__ __launch_bounds__(256) void norm_kernel(NormJob a) {
 // Workgroups of the backward at most: three to a compute unit, two where a thread holds 32 columns (weights, sums and three tensors' values in registers).
 // 131072 rows of 2048 in bf16: 413 us with 512, 433 with 768, 719 with three to a unit and registers in scratch; 128000 rows of 128 in float32: 44.4 with 768, 47.2 with 512.
 constexpr int kBackGroups = 768;
-template <typename T, int PIECES> constexpr int back_groups() { return PIECES * 16 / sizeof(T) >= 32 ? 512 : kBackGroups; }
+__host__ __device__ constexpr int back_groups(int columns) { return columns >= 32 ? 512 : kBackGroups; }   // columns of a thread
 
 struct NormBackJob {
   const void *r, *dy, *dr;
@@ -197,7 +197,7 @@ struct NormBackJob {
 // dx = rstd (g - xhat mean(g xhat)) + dr with g = dy weight.  A workgroup takes rows from its index on, as many at a time as it holds, with the weights of its
 // columns and their sums of dy xhat in registers throughout.  All that a row needs is requested before the first of it is used; it stays as it came, and is taken apart twice.
 template <typename T, int LANES, int PIECES>
-__global__ __launch_bounds__(256, back_groups<T, PIECES>() / 256) void norm_back_kernel(NormBackJob a) {
+__global__ __launch_bounds__(256, back_groups(PIECES * 16 / sizeof(T)) / 256) void norm_back_kernel(NormBackJob a) {
   constexpr int E = 16 / sizeof(T), ROWS = 256 / LANES;
   __shared__ float part[4];
   __shared__ float sums[LANES == 256 ? 1 : 256 * 4];
@@ -393,7 +393,7 @@ wersa_status wersa_rms_norm_backward(const wersa_norm_desc *desc, const void *r,
   by_width(*desc, [&](auto *type, auto lanes, auto pieces) {
     typedef typename std::remove_pointer<decltype(type)>::type T;
     constexpr int L = decltype(lanes)::value, P = decltype(pieces)::value;
-    groups = (int)std::min<int64_t>(back_groups<T, P>(), (desc->rows + 256 / L - 1) / (256 / L));
+    groups = (int)std::min<int64_t>(back_groups(P * 16 / sizeof(T)), (desc->rows + 256 / L - 1) / (256 / L));
     if (groups > 0) WERSA_STAGE("wersa_rms_norm_back", st, (norm_back_kernel<T, L, P><<<groups, 256, 0, st>>>(a)));
   });
   if (dweight)
