@@ -336,23 +336,40 @@ template <int D, bool NATURAL> __device__ __forceinline__ uint32_t lds_at(int ro
 }
 template <typename V> __device__ __forceinline__ V lds_read(uint32_t at) { return *(__attribute__((address_space(3))) const V *)at; }
 template <typename V> __device__ __forceinline__ void lds_write(uint32_t at, V v) { *(__attribute__((address_space(3))) V *)at = v; }
-// What a lane reads: the operand with a row of LDS per lane (rows 16 t + c, columns 32 j + 8 g ..), and the transposed one (below).
+// What a lane reads: the operand with a row of LDS per lane (rows 16 t + c, columns 32 j + 8 g ..), and the transposed one (below).  `lds`: where LDS begins (a multiple of
+// 256); `rows`, a tile's place from there, is a constant, and so part of the instruction.
 template <int D, bool NATURAL> struct RowOperand {
   uint32_t at;
-  __device__ __forceinline__ RowOperand(int g, int c) : at(opaque(lds_at<D, NATURAL>(c, 8 * g))) {}
-  __device__ __forceinline__ bf16x8 operator()(uint32_t rows, int t, int j) const { return lds_read<bf16x8>((at ^ 64 * j) + rows + 32 * t * D); }
+  __device__ __forceinline__ RowOperand(uint32_t lds, int g, int c) : at(opaque(lds + lds_at<D, NATURAL>(c, 8 * g))) {}
+  __device__ __forceinline__ bf16x8 operator()(uint32_t rows, int t, int j) const { return lds_read<bf16x8>((at ^ 64 * j) + (rows + 32 * t * D)); }
 };
-// x as the sum of three bf16 values, 24 bits of it: keys times their weight enter the state like float32.
-struct Three {
-  bf16x8 t[3];
-  __device__ __forceinline__ explicit Three(f32x8 x) {
-    t[0] = __builtin_convertvector(x, bf16x8);
-    x -= __builtin_convertvector(t[0], f32x8);
-    t[1] = __builtin_convertvector(x, bf16x8);
-    x -= __builtin_convertvector(t[1], f32x8);
-    t[2] = __builtin_convertvector(x, bf16x8);
+__device__ __forceinline__ uint32_t pack2(float x, float y) {
+  typedef float f32x2 __attribute__((ext_vector_type(2)));
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x, y}, bf16x2));
+}
+// x w as the sum of three bf16 values, 24 bits of it: keys times their weight enter the state like float32.  (The packed values are hidden from the compiler, which
+// would round every element a second time to take it apart.)
+__device__ __forceinline__ void three_terms(bf16x8 x, f32x4 w0, f32x4 w1, bf16x8 (&t)[3]) {
+  const u32x4 p = __builtin_bit_cast(u32x4, x);
+  u32x4 q[3];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float lo = __uint_as_float(p[i] << 16) * (i < 2 ? w0[2 * i] : w1[2 * i - 4]), hi = __uint_as_float(p[i] & 0xffff0000u) * (i < 2 ? w0[2 * i + 1] : w1[2 * i - 3]);
+#pragma unroll
+    for (int u = 0; u < 3; ++u) {
+      uint32_t r = pack2(lo, hi);
+      if (u < 2) {
+        asm("" : "+v"(r));
+        lo -= __uint_as_float(r << 16);
+        hi -= __uint_as_float(r & 0xffff0000u);
+      }
+      q[u][i] = r;
+    }
   }
-};
+#pragma unroll
+  for (int u = 0; u < 3; ++u) t[u] = __builtin_bit_cast(bf16x8, q[u]);
+}
 
 // The decays of a wave's part of a chunk's weights: 16 own rows on the lanes, 16 other rows down the registers.  lambda^(c - 4 g - i) on the diagonal tile,
 // lambda^(16 + c - 4 g - i) times a power of lambda^16, the same for the whole wave, on those before it.
@@ -370,8 +387,8 @@ struct Weights {
     reach = a.inter * decay_pow(l2, 16 * w + c + (a.reverse ? 0 : 1));
   }
   // Products of the own rows `b` with the chunk's rows in LDS, weighted: operands of the products with the other tensor's rows.
-  template <int D> __device__ __forceinline__ void products(uint32_t rows, const bf16x8 (&b)[D / 32], int g, int c, bf16x8 (&P)[2]) const {
-    const RowOperand<D, false> operand(g, c);
+  template <int D> __device__ __forceinline__ void products(uint32_t lds, uint32_t rows, const bf16x8 (&b)[D / 32], int g, int c, bf16x8 (&P)[2]) const {
+    const RowOperand<D, false> operand(lds, g, c);
 #pragma unroll
     for (int jt = 0; jt < 4; ++jt) {
       f32x4 p = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -390,10 +407,10 @@ struct Weights {
 // A tile's 16 columns of 32 rows of LDS from `row` (a multiple of 32) on, down the slots of k: rows 4 g + q and 16 + 4 g + q - 4 (see above), or 8 g + q with NATURAL.
 template <int D, bool NATURAL> struct ColumnOperand {
   uint32_t at;
-  __device__ __forceinline__ ColumnOperand(int g, int c) : at(opaque(lds_at<D, NATURAL>((NATURAL ? 8 : 4) * g + (c >> 2), 4 * (c & 3)))) {}
+  __device__ __forceinline__ ColumnOperand(uint32_t lds, int g, int c) : at(opaque(lds + lds_at<D, NATURAL>((NATURAL ? 8 : 4) * g + (c >> 2), 4 * (c & 3)))) {}
   __device__ __forceinline__ bf16x8 operator()(uint32_t rows, int row, int ct) const {
-    const uint32_t lo = (at ^ 32 * ct) + rows + 2 * row * D;
-    return read_transposed(lo, NATURAL ? (at ^ (32 * ct + 16)) + rows + 2 * (row + 4) * D : lo + 2 * 16 * D);
+    const uint32_t lo = (at ^ 32 * ct) + (rows + 2 * row * D);
+    return read_transposed(lo, NATURAL ? (at ^ (32 * ct + 16)) + (rows + 2 * (row + 4) * D) : (at ^ 32 * ct) + (rows + 2 * (row + 16) * D));
   }
 };
 // Two tiles of an output, whose 16 columns each lie four to a lane, as eight columns in a row per lane: from column 16 (g % 2) + 8 (g / 2) of the 32 on
@@ -411,43 +428,38 @@ template <int D, int PIECES> __device__ __forceinline__ void put_tile(uint32_t a
   for (int i = 0; i < PIECES; ++i) lds_write(at + 4096 * i, p[i]);
 }
 template <int DK, int DV, bool NATURAL>
-__device__ __forceinline__ void put_state(uint32_t St, const f32x4 (&S)[DK / 64][DV / 16], int row0, int g, int c) {
-  const uint32_t at = opaque(lds_at<DK, NATURAL>(c, row0 + 4 * g));
+__device__ __forceinline__ void put_state(uint32_t lds, uint32_t St, const f32x4 (&S)[DK / 64][DV / 16], int row0, int g, int c) {
+  const uint32_t at = opaque(lds + lds_at<DK, NATURAL>(c, row0 + 4 * g));
 #pragma unroll
   for (int rt = 0; rt < DK / 64; ++rt)
 #pragma unroll
-    for (int ct = 0; ct < DV / 16; ++ct) lds_write((at ^ 32 * rt) + St + 32 * ct * DK, __builtin_convertvector(S[rt][ct], bf16x4));
+    for (int ct = 0; ct < DV / 16; ++ct) lds_write((at ^ 32 * rt) + (St + 32 * ct * DK), __builtin_convertvector(S[rt][ct], bf16x4));
 }
-// S <- keep S + (K o weight)^T V over the chunk's rows in LDS: RT row tiles of the wave from `row0` on, all column tiles.
+// S <- keep S + (K o weight)^T V over the chunk's rows in LDS: RT row tiles of the wave (`row0` elements into a row, part of `keys`), all column tiles.
 template <int DK, int DV>
-__device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float keep, uint32_t Ks, uint32_t Vs, const float *weight, int row0, int g, int c) {
+__device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float keep, uint32_t lds, uint32_t Ks, uint32_t Vs, const float *weight, int row0, int g, int c) {
   constexpr int RT = DK / 64, CT = DV / 16;
-  const ColumnOperand<DK, false> keys(g, c);
-  const ColumnOperand<DV, false> values(g, c);
+  ColumnOperand<DK, false> keys(lds, g, c);
+  keys.at ^= 2 * row0;
+  const ColumnOperand<DV, false> values(lds, g, c);
   bf16x8 K[RT][2][3];
 #pragma unroll
   for (int jj = 0; jj < 2; ++jj) {
     const f32x4 w0 = *(const f32x4 *)(weight + 32 * jj + 4 * g), w1 = *(const f32x4 *)(weight + 32 * jj + 16 + 4 * g);
-    const f32x8 wt = f32x8{w0[0], w0[1], w0[2], w0[3], w1[0], w1[1], w1[2], w1[3]};
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const Three t(__builtin_convertvector(keys(Ks, 32 * jj, row0 / 16 + rt), f32x8) * wt);
-#pragma unroll
-      for (int u = 0; u < 3; ++u) K[rt][jj][u] = t.t[u];
-    }
+    for (int rt = 0; rt < RT; ++rt) three_terms(keys(Ks, 32 * jj, rt), w0, w1, K[rt][jj]);
   }
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     const bf16x8 V[2] = {values(Vs, 0, ct), values(Vs, 32, ct)};
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      f32x4 x = S[rt][ct] * keep;
+    for (int rt = 0; rt < RT; ++rt) S[rt][ct] *= keep;
 #pragma unroll
-      for (int jj = 0; jj < 2; ++jj)
+    for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
-        for (int u = 2; u >= 0; --u) x = mfma_bf16(K[rt][jj][u], V[jj], x);
-      S[rt][ct] = x;
-    }
+      for (int u = 2; u >= 0; --u)
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) S[rt][ct] = mfma_bf16(K[rt][jj][u], V[jj], S[rt][ct]);
   }
 }
 // A wave's rows of a state, from memory or to it.
@@ -470,10 +482,13 @@ template <int DK, int DV, bool FULL, bool STATES>
 __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(Walk a) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;   // pieces of a thread
   constexpr int CT = DV / 16, QJ = DK / 32;
+  // The walk that forms states only waits for memory alone: it has tiles twice, in LDS and under way.
+  constexpr int SETS = STATES ? 2 : 1, SET = 2 * kChunk * (DK + DV);
   extern __shared__ __align__(16) unsigned char lds_bytes[];
   // in LDS: K, V, the columns of the state as rows, the keys' weights
-  const uint32_t Ks = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes, Vs = Ks + 2 * kChunk * DK, St = Vs + 2 * kChunk * DV;
-  float *weight = (float *)(lds_bytes + 2 * (kChunk * (DK + DV) + (STATES ? 0 : DV * DK)));
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes;
+  constexpr uint32_t Ks = 0, Vs = 2 * kChunk * DK, St = SETS * SET;
+  float *weight = (float *)(lds_bytes + SETS * SET + (STATES ? 0 : 2 * DV * DK));
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
   const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
@@ -492,52 +507,55 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
   each_of_state<DK, DV>(a, S, row0, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const Weights weights(a, l2, w, g, c);
 
-  u32x4 rk[PK], rv[PV];
+  u32x4 rk[SETS][PK], rv[SETS][PV];
   bf16x8 Q[QJ];
   const TilePieces<DK, 8, PK, FULL> kp(kr, tid);
   const TilePieces<DV, 8, PV, FULL> vp(vr, tid);
   const uint32_t qat = qr.offset(16 * w + c, 16 * g), oat = orow.offset(16 * w + c, pair_byte(g));
-  const uint32_t kput = Ks + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), vput = Vs + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
-  auto request = [&](int r0) {
-    kp.load(kr, r0, rk);
-    vp.load(vr, r0, rv);
+  const uint32_t kput = lds + Ks + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), vput = lds + Vs + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
+  auto request = [&](int r0, int set) {
+    kp.load(kr, r0, rk[set]);
+    vp.load(vr, r0, rv[set]);
   };
 
-  request(0);
+#pragma unroll
+  for (int set = 0; set < SETS; ++set) request(set * kChunk, set);
   if (!STATES) load_own<QJ, FULL>(qr, 0, qat, g, Q);
-  for (int r0 = 0; r0 < seg.rows; r0 += kChunk) {
-    const int rows = min(kChunk, seg.rows - r0);
-    put_tile<DK, PK>(kput, rk);
-    put_tile<DV, PV>(vput, rv);
-    if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + (a.reverse ? 1 : 0));
-    if (!STATES) {
-      put_state<DK, DV, false>(St, S, row0, g, c);
-    }
-    __syncthreads();
-    request(r0 + kChunk);
-    if (!STATES) {
-      bf16x8 P[2];
-      weights.products<DK>(Ks, Q, g, c, P);
-      const Rows::Chunk oc = orow.chunk(r0);
-      const uint32_t x = opaque(oat) - oc.missing;
-      const RowOperand<DK, false> state(g, c);
-      const ColumnOperand<DV, false> values(g, c);
-      f32x4 O[2];
+  for (int r1 = 0; r1 < seg.rows; r1 += SETS * kChunk) {
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int set = 0; set < SETS; ++set) {
+      const int r0 = r1 + set * kChunk, rows = min(kChunk, seg.rows - r0);
+      if (set && rows <= 0) break;
+      put_tile<DK, PK>(kput + set * SET, rk[set]);
+      put_tile<DV, PV>(vput + set * SET, rv[set]);
+      if (tid < kChunk) weight[set * kChunk + tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + (a.reverse ? 1 : 0));
+      if (!STATES) put_state<DK, DV, false>(lds, St, S, row0, g, c);
+      __syncthreads();
+      request(r0 + SETS * kChunk, set);
+      if (!STATES) {
+        bf16x8 P[2];
+        weights.products<DK>(lds, Ks, Q, g, c, P);
+        const Rows::Chunk oc = orow.chunk(r0);
+        const uint32_t x = opaque(oat) - oc.missing;
+        const RowOperand<DK, false> state(lds, g, c);
+        const ColumnOperand<DV, false> values(lds, g, c);
+        f32x4 O[2];
 #pragma unroll
-        for (int j = 0; j < QJ; ++j) acc = mfma_bf16(state(St, ct, j), Q[j], acc);
-        acc *= weights.reach;
+        for (int ct = 0; ct < CT; ++ct) {
+          f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-        for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(values(Vs, 32 * jj, ct), P[jj], acc);
-        O[ct & 1] = acc;
-        if (ct & 1) store_piece(oc, FULL ? x + 32 * (ct - 1) : (x + 32 * (ct - 1)) | outside(32 * (ct - 1) + pair_byte(g), orow.width), pack_pair(O[0], O[1]));
+          for (int j = 0; j < QJ; ++j) acc = mfma_bf16(state(St, ct, j), Q[j], acc);
+          acc *= weights.reach;
+#pragma unroll
+          for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(values(Vs, 32 * jj, ct), P[jj], acc);
+          O[ct & 1] = acc;
+          if (ct & 1) store_piece(oc, FULL ? x + 32 * (ct - 1) : (x + 32 * (ct - 1)) | outside(32 * (ct - 1) + pair_byte(g), orow.width), pack_pair(O[0], O[1]));
+        }
+        load_own<QJ, FULL>(qr, r0 + kChunk, qat, g, Q);   // (into the registers of this chunk's, which are done with)
       }
-      load_own<QJ, FULL>(qr, r0 + kChunk, qat, g, Q);   // (into the registers of this chunk's, which are done with)
+      update_state<DK, DV>(S, decay_pow(l2, rows), lds, Ks + set * SET, Vs + set * SET, weight + set * kChunk, row0, g, c);
+      if (SETS == 1) __syncthreads();   // (with two sets every wave is past this one's reads at the next set's barrier)
     }
-    update_state<DK, DV>(S, decay_pow(l2, rows), Ks, Vs, weight, row0, g, c);
-    __syncthreads();
   }
 
   float *fin = nullptr;
@@ -558,7 +576,8 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;
   constexpr int KT = DK / 16, CT = DV / 16, KJ = DK / 32, VJ = DV / 32;
   extern __shared__ __align__(16) unsigned char lds_bytes[];
-  const uint32_t Qs = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes, Ds = Qs + 2 * kChunk * DK, Gt = Ds + 2 * kChunk * DV;
+  const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes;
+  constexpr uint32_t Qs = 0, Ds = 2 * kChunk * DK, Gt = Ds + 2 * kChunk * DV;
   float *weight = (float *)(lds_bytes + 2 * (kChunk * (DK + DV) + DV * DK));
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
@@ -581,7 +600,7 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
   const TilePieces<DV, 8, PV, FULL> dp(dr, tid);
   const uint32_t kat = kr.offset(16 * w + c, 16 * g), vat = vr.offset(16 * w + c, 16 * g);
   const uint32_t dkat = dkr.offset(16 * w + c, pair_byte(g)), dvat = dvr.offset(16 * w + c, pair_byte(g));
-  const uint32_t qput = Qs + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), dput = Ds + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
+  const uint32_t qput = lds + Qs + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), dput = lds + Ds + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
   auto request = [&](int r0) {
     qp.load(qr, r0, rq);
     dp.load(dr, r0, rd);
@@ -598,17 +617,17 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
     put_tile<DK, PK>(qput, rq);
     put_tile<DV, PV>(dput, rd);
     if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + 1);
-    put_state<DK, DV, true>(Gt, G, row0, g, c);
+    put_state<DK, DV, true>(lds, Gt, G, row0, g, c);
     __syncthreads();
     request(r0 + kChunk);
     f32x4 O[2];
     bf16x8 P[2];
-    weights.products<DK>(Qs, K, g, c, P);
+    weights.products<DK>(lds, Qs, K, g, c, P);
     {
       const Rows::Chunk oc = dvr.chunk(r0);
       const uint32_t x = opaque(dvat) - oc.missing;
-      const RowOperand<DK, true> state(g, c);
-      const ColumnOperand<DV, false> douts(g, c);
+      const RowOperand<DK, true> state(lds, g, c);
+      const ColumnOperand<DV, false> douts(lds, g, c);
 #pragma unroll
       for (int ct = 0; ct < CT; ++ct) {
         f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -621,12 +640,12 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
         if (ct & 1) store_piece(oc, FULL ? x + 32 * (ct - 1) : (x + 32 * (ct - 1)) | outside(32 * (ct - 1) + pair_byte(g), dvr.width), pack_pair(O[0], O[1]));
       }
     }
-    weights.products<DV>(Ds, V, g, c, P);
+    weights.products<DV>(lds, Ds, V, g, c, P);
     {
       const Rows::Chunk oc = dkr.chunk(r0);
       const uint32_t x = opaque(dkat) - oc.missing;
-      const ColumnOperand<DK, true> state(g, c);
-      const ColumnOperand<DK, false> queries(g, c);
+      const ColumnOperand<DK, true> state(lds, g, c);
+      const ColumnOperand<DK, false> queries(lds, g, c);
 #pragma unroll
       for (int kt = 0; kt < KT; ++kt) {
         f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -640,7 +659,7 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
       }
     }
     request_own(r0 + kChunk);
-    update_state<DK, DV>(G, decay_pow(l2, rows), Qs, Ds, weight, row0, g, c);
+    update_state<DK, DV>(G, decay_pow(l2, rows), lds, Qs, Ds, weight, row0, g, c);
     __syncthreads();
   }
   if (a.fin && seg.s == 0) {
@@ -794,7 +813,7 @@ template <int DK, int DV, bool STATES> bool launch_walk_as(const wersa_decay_des
   const char *name = STATES ? "wersa_decay_states" : "wersa_decay_walk";
   if (c.dtype == WERSA_F32)
     return launch(name, &walk_f32_kernel<DK, DV, STATES>, sizeof(float) * (kChunk * (DK + 4 + DV + 4 + 1) + (STATES ? 0 : DV * (DK + 4))), a, st);
-  constexpr size_t smem = sizeof(bf16_t) * (kChunk * (DK + DV) + (STATES ? 0 : DV * DK)) + sizeof(float) * kChunk;
+  constexpr size_t sets = STATES ? 2 : 1, smem = sizeof(bf16_t) * (sets * kChunk * (DK + DV) + (STATES ? 0 : DV * DK)) + sizeof(float) * sets * kChunk;
   return a.kw == DK && a.vw == DV ? launch(name, &walk_bf16_kernel<DK, DV, true, STATES>, smem, a, st)
                                   : launch(name, &walk_bf16_kernel<DK, DV, false, STATES>, smem, a, st);
 }
