@@ -117,8 +117,11 @@ struct Rows {
 };
 // Bytes past the width are none of the buffer's: joined in by `or` at the access.
 __device__ __forceinline__ uint32_t outside(int byte, int width) { return byte < width ? 0u : 0xffffffc0u; }
-__device__ __forceinline__ u32x4 load_piece(const Rows::Chunk &c, uint32_t at) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(c.b, (int)at, 0, 0)); }
-__device__ __forceinline__ void store_piece(const Rows::Chunk &c, uint32_t at, u32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(v, c.b, (int)at, 0, 0); }
+// Outputs, and what the states alone are formed from, pass by the caches (aux 2: non-temporal).
+template <bool NT = false> __device__ __forceinline__ u32x4 load_piece(const Rows::Chunk &c, uint32_t at) {
+  return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(c.b, (int)at, 0, NT ? 2 : 0));
+}
+__device__ __forceinline__ void store_piece(const Rows::Chunk &c, uint32_t at, u32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(v, c.b, (int)at, 0, 2); }
 // Rows of `seg` for head h of a tensor.
 __device__ __forceinline__ Rows rows_of(const void *p, const Strides &s, const Segment &seg, const Walk &a, int h, int cols, int element) {
   const int64_t at = (a.seq.offsets ? 0 : seg.b * s.b) + h * s.h + seg.row0 * s.n;
@@ -129,23 +132,24 @@ __device__ __forceinline__ uint32_t opaque(uint32_t x) {
   asm volatile("" : "+v"(x));
   return x;
 }
-// A thread's pieces of a tile of D values a row (PIECES of them, 256 threads), and the pieces 16 g + 64 j of the row of a lane (J of them).  FULL: no columns past the width.
-template <int D, int E, int PIECES, bool FULL> struct TilePieces {
+// A thread's pieces of a tile of D values a row of E per piece, PIECES of them: THREADS threads take whole rows one behind the other from `row0` on.  FULL: no columns past the
+// width.
+template <int D, int E, int PIECES, int THREADS, bool FULL> struct TilePieces {
   uint32_t at, out;
-  __device__ __forceinline__ TilePieces(const Rows &r, int tid) : at(r.offset(tid / (D / E), tid % (D / E) * 16)), out(outside(tid % (D / E) * 16, r.width)) {}
-  __device__ __forceinline__ void load(const Rows &r, int r0, u32x4 (&p)[PIECES]) const {
+  __device__ __forceinline__ TilePieces(const Rows &r, int row0, int t) : at(r.offset(row0 + t / (D / E), t % (D / E) * 16)), out(outside(t % (D / E) * 16, r.width)) {}
+  template <bool NT> __device__ __forceinline__ void load(const Rows &r, int r0, u32x4 (&p)[PIECES]) const {
     const Rows::Chunk c = r.chunk(r0);
     uint32_t x = opaque(at) - c.missing;
 #pragma unroll
-    for (int i = 0; i < PIECES; ++i, x += r.further(256 * E / D)) p[i] = load_piece(c, FULL ? x : x | out);
+    for (int i = 0; i < PIECES; ++i, x += r.further(THREADS * E / D)) p[i] = load_piece<NT>(c, FULL ? x : x | out);
+  }
+  __device__ __forceinline__ void store(const Rows &r, int r0, const u32x4 (&p)[PIECES]) const {
+    const Rows::Chunk c = r.chunk(r0);
+    uint32_t x = opaque(at) - c.missing;
+#pragma unroll
+    for (int i = 0; i < PIECES; ++i, x += r.further(THREADS * E / D)) store_piece(c, FULL ? x : x | out, p[i]);
   }
 };
-template <int J, bool FULL, typename V> __device__ __forceinline__ void load_own(const Rows &r, int r0, uint32_t at, int g, V (&p)[J]) {
-  const Rows::Chunk c = r.chunk(r0);
-  const uint32_t x = opaque(at) - c.missing;
-#pragma unroll
-  for (int j = 0; j < J; ++j) p[j] = __builtin_bit_cast(V, load_piece(c, FULL ? x + 64 * j : (x + 64 * j) | outside(64 * j + 16 * g, r.width)));
-}
 
 // ---- float32 matrix instructions -----------------------------------------------------------------
 // v_mfma_f32_16x16x4_f32 (c = lane % 16, g = lane / 16): A row c, k = g;  B column c, k = g;  C/D: acc[i] is row 4 g + i, column c.
@@ -200,13 +204,18 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
   u32x4 rk[PK], rv[PV];
   f32x4 rq[DK / 16];
   const int krow = tid / (DK / 4), kcol = tid % (DK / 4) * 4, vrow = tid / (DV / 4), vcol = tid % (DV / 4) * 4;   // a thread's first piece
-  const TilePieces<DK, 4, PK, false> kp(kr, tid);
-  const TilePieces<DV, 4, PV, false> vp(vr, tid);
+  const TilePieces<DK, 4, PK, 256, false> kp(kr, 0, tid);
+  const TilePieces<DV, 4, PV, 256, false> vp(vr, 0, tid);
   const uint32_t qat = qr.offset(16 * w + c, 16 * g);
   auto request = [&](int r0) {
-    kp.load(kr, r0, rk);
-    vp.load(vr, r0, rv);
-    if (!STATES) load_own<DK / 16, false>(qr, r0, qat, g, rq);
+    kp.template load<false>(kr, r0, rk);
+    vp.template load<false>(vr, r0, rv);
+    if (!STATES) {
+      const Rows::Chunk qc = qr.chunk(r0);
+#pragma unroll
+      for (int j = 0; j < DK / 16; ++j)
+        rq[j] = __builtin_bit_cast(f32x4, load_piece(qc, (qat + 64 * j - qc.missing) | outside(64 * j + 16 * g, qr.width)));
+    }
   };
 
   request(0);
@@ -413,15 +422,13 @@ template <int D, bool NATURAL> struct ColumnOperand {
     return read_transposed(lo, NATURAL ? (at ^ (32 * ct + 16)) + (rows + 2 * (row + 4) * D) : (at ^ 32 * ct) + (rows + 2 * (row + 16) * D));
   }
 };
-// Two tiles of an output, whose 16 columns each lie four to a lane, as eight columns in a row per lane: from column 16 (g % 2) + 8 (g / 2) of the 32 on
-// (pair_byte).
+// Two tiles of an output, whose 16 columns each lie four to a lane, as eight columns in a row per lane: from column 16 (g % 2) + 8 (g / 2) of the 32 on.
 __device__ __forceinline__ u32x4 pack_pair(f32x4 x, f32x4 y) {
   typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
   const u32x2 a = __builtin_bit_cast(u32x2, __builtin_convertvector(x, bf16x4)), b = __builtin_bit_cast(u32x2, __builtin_convertvector(y, bf16x4));
   const auto r0 = __builtin_amdgcn_permlane16_swap(a[0], b[0], false, false), r1 = __builtin_amdgcn_permlane16_swap(a[1], b[1], false, false);
   return u32x4{r0[0], r1[0], r0[1], r1[1]};
 }
-__device__ __forceinline__ int pair_byte(int g) { return 32 * (g & 1) + 16 * (g >> 1); }
 // A thread's pieces of a tile into LDS (rows 2048 / D apart, a multiple of 16), and a wave's rows of a state, as columns and rounded to bf16.
 template <int D, int PIECES> __device__ __forceinline__ void put_tile(uint32_t at, const u32x4 (&p)[PIECES]) {
 #pragma unroll
@@ -435,9 +442,49 @@ __device__ __forceinline__ void put_state(uint32_t lds, uint32_t St, const f32x4
 #pragma unroll
     for (int ct = 0; ct < DV / 16; ++ct) lds_write((at ^ 32 * rt) + (St + 32 * ct * DK), __builtin_convertvector(S[rt][ct], bf16x4));
 }
+// What a wave has written to LDS for itself is read after this: LDS takes a wave's accesses in their order, and the compiler keeps it.
+__device__ __forceinline__ void own_lds() {
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+// A wave's 16 rows of a tensor on their way between memory, where whole lines of them are read and written, and the operands' layout: through 32 D bytes of LDS of its own.
+template <int D, bool FULL> struct OwnRows {
+  static constexpr int J = D / 32;
+  TilePieces<D, 8, J, 64, FULL> pieces;
+  uint32_t put;
+  __device__ __forceinline__ OwnRows(const Rows &r, uint32_t stage, int w, int lane) : pieces(r, 16 * w, lane), put(stage + lds_at<D, false>(lane / (D / 8), lane % (D / 8) * 8)) {}
+  // (rows 512 / D further on: the permutation by the row is another constant)
+  __device__ __forceinline__ static uint32_t piece(uint32_t at, int i) { return (at ^ 16 * (D == 128 ? (i & 1) * 8 + (i >> 1) : i)) + 1024 * i; }
+  __device__ __forceinline__ void operands(const u32x4 (&raw)[J], uint32_t stage, int g, int c, bf16x8 (&b)[J]) const {
+    const uint32_t at = opaque(put);
+#pragma unroll
+    for (int i = 0; i < J; ++i) lds_write(piece(at, i), raw[i]);
+    own_lds();
+    const RowOperand<D, false> operand(stage, g, c);
+#pragma unroll
+    for (int j = 0; j < J; ++j) b[j] = operand(0, 0, j);
+    own_lds();
+  }
+  __device__ __forceinline__ void out(const Rows &r, int r0) const {   // what pair_at's places hold
+    own_lds();
+    const uint32_t at = opaque(put);
+    u32x4 raw[J];
+#pragma unroll
+    for (int i = 0; i < J; ++i) raw[i] = lds_read<u32x4>(piece(at, i));
+    pieces.store(r, r0, raw);
+    own_lds();
+  }
+};
+// Where a lane's eight columns of a pair of tiles (the first one, the others an exclusive or of 64 bytes apart) lie in the wave's own LDS.
+template <int D> __device__ __forceinline__ uint32_t pair_at(uint32_t stage, int g, int c) { return opaque(stage + lds_at<D, false>(c, 16 * (g & 1) + 8 * (g >> 1))); }
+__device__ __forceinline__ void put_weights(uint32_t stage, int lane, const Walk &a, float l2, int behind) {   // behind: rows after the chunk's first one
+  lds_write(stage + 4 * lane, a.gain * decay_pow(l2, max(behind - lane, 0) + (a.reverse ? 1 : 0)));
+  own_lds();
+}
 // S <- keep S + (K o weight)^T V over the chunk's rows in LDS: RT row tiles of the wave (`row0` elements into a row, part of `keys`), all column tiles.
-template <int DK, int DV>
-__device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float keep, uint32_t lds, uint32_t Ks, uint32_t Vs, const float *weight, int row0, int g, int c) {
+// weight: the wave's own table of the chunk's rows.  SUM: keep is 1.
+template <int DK, int DV, bool SUM>
+__device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float keep, uint32_t lds, uint32_t Ks, uint32_t Vs, uint32_t weight, int row0, int g, int c) {
   constexpr int RT = DK / 64, CT = DV / 16;
   ColumnOperand<DK, false> keys(lds, g, c);
   keys.at ^= 2 * row0;
@@ -445,15 +492,17 @@ __device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float
   bf16x8 K[RT][2][3];
 #pragma unroll
   for (int jj = 0; jj < 2; ++jj) {
-    const f32x4 w0 = *(const f32x4 *)(weight + 32 * jj + 4 * g), w1 = *(const f32x4 *)(weight + 32 * jj + 16 + 4 * g);
+    const f32x4 w0 = lds_read<f32x4>(weight + 128 * jj + 16 * g), w1 = lds_read<f32x4>(weight + 128 * jj + 64 + 16 * g);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) three_terms(keys(Ks, 32 * jj, rt), w0, w1, K[rt][jj]);
   }
 #pragma unroll
   for (int ct = 0; ct < CT; ++ct) {
     const bf16x8 V[2] = {values(Vs, 0, ct), values(Vs, 32, ct)};
+    if (!SUM) {
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt) S[rt][ct] *= keep;
+      for (int rt = 0; rt < RT; ++rt) S[rt][ct] *= keep;
+    }
 #pragma unroll
     for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
@@ -481,18 +530,18 @@ template <int DK, int DV, typename F> __device__ __forceinline__ void each_of_st
 template <int DK, int DV, bool FULL, bool STATES>
 __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(Walk a) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;   // pieces of a thread
-  constexpr int CT = DV / 16, QJ = DK / 32;
+  constexpr int CT = DV / 16, QJ = DK / 32, STAGE = STATES ? 256 : 32 * (DK > DV ? DK : DV);   // bytes of LDS that a wave has for itself
   // The walk that forms states only waits for memory alone: it has tiles twice, in LDS and under way.
   constexpr int SETS = STATES ? 2 : 1, SET = 2 * kChunk * (DK + DV);
   extern __shared__ __align__(16) unsigned char lds_bytes[];
-  // in LDS: K, V, the columns of the state as rows, the keys' weights
+  // in LDS: K, V, the columns of the state as rows, the waves' own parts
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes;
   constexpr uint32_t Ks = 0, Vs = 2 * kChunk * DK, St = SETS * SET;
-  float *weight = (float *)(lds_bytes + SETS * SET + (STATES ? 0 : 2 * DV * DK));
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
   const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int row0 = DK / 4 * w;   // of the wave's rows of the state
+  const uint32_t stage = lds + SETS * SET + (STATES ? 0 : 2 * DV * DK) + STAGE * w;
   const bool last = a.reverse ? seg.s == 0 : seg.s == a.seq.segments(seg.b) - 1;
   if (STATES && last) return;
   const Rows qr = rows_of(a.q, a.sq, seg, a, h, a.kw, 2), kr = rows_of(a.k, a.sk, seg, a, h, a.kw, 2), vr = rows_of(a.v, a.sv, seg, a, h, a.vw, 2),
@@ -507,20 +556,20 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
   each_of_state<DK, DV>(a, S, row0, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const Weights weights(a, l2, w, g, c);
 
-  u32x4 rk[SETS][PK], rv[SETS][PV];
-  bf16x8 Q[QJ];
-  const TilePieces<DK, 8, PK, FULL> kp(kr, tid);
-  const TilePieces<DV, 8, PV, FULL> vp(vr, tid);
-  const uint32_t qat = qr.offset(16 * w + c, 16 * g), oat = orow.offset(16 * w + c, pair_byte(g));
+  u32x4 rk[SETS][PK], rv[SETS][PV], rq[QJ];
+  const TilePieces<DK, 8, PK, 256, FULL> kp(kr, 0, tid);
+  const TilePieces<DV, 8, PV, 256, FULL> vp(vr, 0, tid);
+  const OwnRows<DK, FULL> qo(qr, stage, w, lane);
+  const OwnRows<DV, FULL> oo(orow, stage, w, lane);
   const uint32_t kput = lds + Ks + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), vput = lds + Vs + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
   auto request = [&](int r0, int set) {
-    kp.load(kr, r0, rk[set]);
-    vp.load(vr, r0, rv[set]);
+    kp.template load<STATES>(kr, r0, rk[set]);
+    vp.template load<STATES>(vr, r0, rv[set]);
   };
 
 #pragma unroll
   for (int set = 0; set < SETS; ++set) request(set * kChunk, set);
-  if (!STATES) load_own<QJ, FULL>(qr, 0, qat, g, Q);
+  if (!STATES) qo.pieces.template load<false>(qr, 0, rq);
   for (int r1 = 0; r1 < seg.rows; r1 += SETS * kChunk) {
 #pragma unroll
     for (int set = 0; set < SETS; ++set) {
@@ -528,15 +577,17 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
       if (set && rows <= 0) break;
       put_tile<DK, PK>(kput + set * SET, rk[set]);
       put_tile<DV, PV>(vput + set * SET, rv[set]);
-      if (tid < kChunk) weight[set * kChunk + tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + (a.reverse ? 1 : 0));
-      if (!STATES) put_state<DK, DV, false>(lds, St, S, row0, g, c);
+      bf16x8 Q[QJ];
+      if (!STATES) {
+        put_state<DK, DV, false>(lds, St, S, row0, g, c);
+        qo.operands(rq, stage, g, c, Q);
+      }
       __syncthreads();
       request(r0 + SETS * kChunk, set);
       if (!STATES) {
         bf16x8 P[2];
         weights.products<DK>(lds, Ks, Q, g, c, P);
-        const Rows::Chunk oc = orow.chunk(r0);
-        const uint32_t x = opaque(oat) - oc.missing;
+        const uint32_t pair = pair_at<DV>(stage, g, c);
         const RowOperand<DK, false> state(lds, g, c);
         const ColumnOperand<DV, false> values(lds, g, c);
         f32x4 O[2];
@@ -549,11 +600,14 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
 #pragma unroll
           for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(values(Vs, 32 * jj, ct), P[jj], acc);
           O[ct & 1] = acc;
-          if (ct & 1) store_piece(oc, FULL ? x + 32 * (ct - 1) : (x + 32 * (ct - 1)) | outside(32 * (ct - 1) + pair_byte(g), orow.width), pack_pair(O[0], O[1]));
+          if (ct & 1) lds_write(pair ^ 32 * (ct - 1), pack_pair(O[0], O[1]));
         }
-        load_own<QJ, FULL>(qr, r0 + kChunk, qat, g, Q);   // (into the registers of this chunk's, which are done with)
+        oo.out(orow, r0);
+        qo.pieces.template load<false>(qr, r0 + kChunk, rq);
       }
-      update_state<DK, DV>(S, decay_pow(l2, rows), lds, Ks + set * SET, Vs + set * SET, weight + set * kChunk, row0, g, c);
+      // the walk that forms states only weights rows by the segment's end, and has no sum to scale
+      put_weights(stage, lane, a, l2, STATES ? seg.rows - 1 - r0 : rows - 1);
+      update_state<DK, DV, STATES>(S, decay_pow(l2, rows), lds, Ks + set * SET, Vs + set * SET, stage, row0, g, c);
       if (SETS == 1) __syncthreads();   // (with two sets every wave is past this one's reads at the next set's barrier)
     }
   }
@@ -574,15 +628,15 @@ struct Back {
 template <int DK, int DV, bool FULL>
 __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;
-  constexpr int KT = DK / 16, CT = DV / 16, KJ = DK / 32, VJ = DV / 32;
+  constexpr int KT = DK / 16, CT = DV / 16, KJ = DK / 32, VJ = DV / 32, STAGE = 32 * (DK > DV ? DK : DV);
   extern __shared__ __align__(16) unsigned char lds_bytes[];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes;
   constexpr uint32_t Qs = 0, Ds = 2 * kChunk * DK, Gt = Ds + 2 * kChunk * DV;
-  float *weight = (float *)(lds_bytes + 2 * (kChunk * (DK + DV) + DV * DK));
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
   const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const int row0 = DK / 4 * w;
+  const uint32_t stage = lds + Gt + 2 * DV * DK + STAGE * w;
   const Rows qr = rows_of(a.k, a.sk, seg, a, h, a.kw, 2), dr = rows_of(a.v, a.sv, seg, a, h, a.vw, 2), kr = rows_of(b.k, b.sk, seg, a, h, a.kw, 2),
              vr = rows_of(b.v, b.sv, seg, a, h, a.vw, 2), dkr = rows_of(b.dk, b.sk, seg, a, h, a.kw, 2), dvr = rows_of(b.dv, b.sv, seg, a, h, a.vw, 2);
   const float l2 = log2_decay(a.log_decay, h);
@@ -594,20 +648,19 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
   each_of_state<DK, DV>(a, G, row0, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const Weights weights(a, l2, w, g, c);
 
-  u32x4 rq[PK], rd[PV];
-  bf16x8 K[KJ], V[VJ];
-  const TilePieces<DK, 8, PK, FULL> qp(qr, tid);
-  const TilePieces<DV, 8, PV, FULL> dp(dr, tid);
-  const uint32_t kat = kr.offset(16 * w + c, 16 * g), vat = vr.offset(16 * w + c, 16 * g);
-  const uint32_t dkat = dkr.offset(16 * w + c, pair_byte(g)), dvat = dvr.offset(16 * w + c, pair_byte(g));
+  u32x4 rq[PK], rd[PV], rk[KJ], rv[VJ];
+  const TilePieces<DK, 8, PK, 256, FULL> qp(qr, 0, tid);
+  const TilePieces<DV, 8, PV, 256, FULL> dp(dr, 0, tid);
+  const OwnRows<DK, FULL> ko(kr, stage, w, lane), dko(dkr, stage, w, lane);
+  const OwnRows<DV, FULL> vo(vr, stage, w, lane), dvo(dvr, stage, w, lane);
   const uint32_t qput = lds + Qs + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), dput = lds + Ds + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
   auto request = [&](int r0) {
-    qp.load(qr, r0, rq);
-    dp.load(dr, r0, rd);
+    qp.template load<false>(qr, r0, rq);
+    dp.template load<false>(dr, r0, rd);
   };
   auto request_own = [&](int r0) {
-    load_own<KJ, FULL>(kr, r0, kat, g, K);
-    load_own<VJ, FULL>(vr, r0, vat, g, V);
+    ko.pieces.template load<false>(kr, r0, rk);
+    vo.pieces.template load<false>(vr, r0, rv);
   };
 
   request(0);
@@ -616,16 +669,17 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
     const int rows = min(kChunk, seg.rows - r0);
     put_tile<DK, PK>(qput, rq);
     put_tile<DV, PV>(dput, rd);
-    if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + 1);
     put_state<DK, DV, true>(lds, Gt, G, row0, g, c);
+    bf16x8 K[KJ], V[VJ];
+    ko.operands(rk, stage, g, c, K);
+    vo.operands(rv, stage, g, c, V);
     __syncthreads();
     request(r0 + kChunk);
     f32x4 O[2];
     bf16x8 P[2];
     weights.products<DK>(lds, Qs, K, g, c, P);
     {
-      const Rows::Chunk oc = dvr.chunk(r0);
-      const uint32_t x = opaque(dvat) - oc.missing;
+      const uint32_t pair = pair_at<DV>(stage, g, c);
       const RowOperand<DK, true> state(lds, g, c);
       const ColumnOperand<DV, false> douts(lds, g, c);
 #pragma unroll
@@ -637,13 +691,13 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
 #pragma unroll
         for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(douts(Ds, 32 * jj, ct), P[jj], acc);
         O[ct & 1] = acc;
-        if (ct & 1) store_piece(oc, FULL ? x + 32 * (ct - 1) : (x + 32 * (ct - 1)) | outside(32 * (ct - 1) + pair_byte(g), dvr.width), pack_pair(O[0], O[1]));
+        if (ct & 1) lds_write(pair ^ 32 * (ct - 1), pack_pair(O[0], O[1]));
       }
+      dvo.out(dvr, r0);
     }
     weights.products<DV>(lds, Ds, V, g, c, P);
     {
-      const Rows::Chunk oc = dkr.chunk(r0);
-      const uint32_t x = opaque(dkat) - oc.missing;
+      const uint32_t pair = pair_at<DK>(stage, g, c);
       const ColumnOperand<DK, true> state(lds, g, c);
       const ColumnOperand<DK, false> queries(lds, g, c);
 #pragma unroll
@@ -655,11 +709,13 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
 #pragma unroll
         for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(queries(Qs, 32 * jj, kt), P[jj], acc);
         O[kt & 1] = acc;
-        if (kt & 1) store_piece(oc, FULL ? x + 32 * (kt - 1) : (x + 32 * (kt - 1)) | outside(32 * (kt - 1) + pair_byte(g), dkr.width), pack_pair(O[0], O[1]));
+        if (kt & 1) lds_write(pair ^ 32 * (kt - 1), pack_pair(O[0], O[1]));
       }
+      dko.out(dkr, r0);
     }
     request_own(r0 + kChunk);
-    update_state<DK, DV>(G, decay_pow(l2, rows), lds, Qs, Ds, weight, row0, g, c);
+    put_weights(stage, lane, a, l2, rows - 1);
+    update_state<DK, DV, false>(G, decay_pow(l2, rows), lds, Qs, Ds, stage, row0, g, c);
     __syncthreads();
   }
   if (a.fin && seg.s == 0) {
@@ -813,7 +869,7 @@ template <int DK, int DV, bool STATES> bool launch_walk_as(const wersa_decay_des
   const char *name = STATES ? "wersa_decay_states" : "wersa_decay_walk";
   if (c.dtype == WERSA_F32)
     return launch(name, &walk_f32_kernel<DK, DV, STATES>, sizeof(float) * (kChunk * (DK + 4 + DV + 4 + 1) + (STATES ? 0 : DV * (DK + 4))), a, st);
-  constexpr size_t sets = STATES ? 2 : 1, smem = sizeof(bf16_t) * (sets * kChunk * (DK + DV) + (STATES ? 0 : DV * DK)) + sizeof(float) * sets * kChunk;
+  constexpr size_t sets = STATES ? 2 : 1, smem = 2 * (sets * kChunk * (DK + DV) + (STATES ? 0 : DV * DK)) + 4 * (STATES ? 256 : 32 * (DK > DV ? DK : DV));
   return a.kw == DK && a.vw == DV ? launch(name, &walk_bf16_kernel<DK, DV, true, STATES>, smem, a, st)
                                   : launch(name, &walk_bf16_kernel<DK, DV, false, STATES>, smem, a, st);
 }
@@ -822,7 +878,7 @@ template <bool STATES> bool launch_walk(const wersa_decay_desc &c, const Walk &a
   return a.vw <= 64 ? launch_walk_as<128, 64, STATES>(c, a, st) : launch_walk_as<128, 128, STATES>(c, a, st);
 }
 template <int DK, int DV> bool launch_back_as(const Walk &a, const Back &b, hipStream_t st) {
-  constexpr size_t smem = sizeof(bf16_t) * (kChunk * (DK + DV) + DV * DK) + sizeof(float) * kChunk;
+  constexpr size_t smem = 2 * (kChunk * (DK + DV) + DV * DK) + 4 * 32 * (DK > DV ? DK : DV);
   return a.kw == DK && a.vw == DV ? launch("wersa_decay_back", &back_bf16_kernel<DK, DV, true>, smem, a, st, b)
                                   : launch("wersa_decay_back", &back_bf16_kernel<DK, DV, false>, smem, a, st, b);
 }
