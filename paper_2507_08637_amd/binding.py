@@ -7,6 +7,7 @@ raises.
 """
 import ctypes
 import os
+import struct
 
 import torch
 
@@ -472,22 +473,31 @@ def _dtype_code(x):
     raise TypeError("dtype must be float32 or bfloat16")
 
 
+_DECAY_DESC = struct.Struct("7if12q")   # (a structure of ctypes takes several times as long to fill in field by field)
+
+
 def make_decay_desc(q, k, v, out, scale=None, offsets=None):
     """Descriptor for q, k (B, H, n, dk) and v, out (B, H, n, dv), last dimension contiguous; with offsets (B + 1) the tensors
     have one batch entry that holds the rows of all B sequences.  scale: 1 / sqrt(dk) by default."""
-    assert q.dim() == 4 and v.dim() == 4 and k.shape == q.shape and v.shape[:3] == q.shape[:3] and out.shape == v.shape, \
-        "expect q, k (B, H, n, dk) and v, out (B, H, n, dv)"
-    assert k.dtype == q.dtype and v.dtype == q.dtype and out.dtype == q.dtype, "q, k, v and out must share a dtype"
-    assert all(x.stride(3) == 1 for x in (q, k, v, out)), "expect a contiguous last dim"
-    N, H, n, dk = q.shape
+    assert q.dim() == 4 and v.dim() == 4, "expect q, k (B, H, n, dk) and v, out (B, H, n, dv)"
+    (N, H, n, dk), dv = q.shape, v.shape[3]
+    assert k.shape == q.shape and v.shape == (N, H, n, dv) and out.shape == v.shape, "expect q, k (B, H, n, dk) and v, out (B, H, n, dv)"
+    dtype = q.dtype
+    assert k.dtype == dtype and v.dtype == dtype and out.dtype == dtype, "q, k, v and out must share a dtype"
+    (qb, qh, qn, q1), (kb, kh, kn, k1), (vb, vh, vn, v1), (ob, oh, on, o1) = q.stride(), k.stride(), v.stride(), out.stride()
+    assert q1 == k1 == v1 == o1 == 1, "expect a contiguous last dim"
     B = N
     if offsets is not None:
         assert N == 1 and offsets.dim() == 1 and offsets.numel() >= 2 and offsets.dtype == torch.int32 and offsets.is_contiguous(), \
             "packed sequences: tensors of one batch entry and int32 offsets (B + 1)"
         B = offsets.numel() - 1
-    three = ctypes.c_int64 * 3
-    return WersaDecayDesc(B, H, n, dk, v.shape[3], _dtype_code(q), int(offsets is not None), dk ** -0.5 if scale is None else scale,
-                          *(three(*x.stride()[:3]) for x in (q, k, v, out)))
+    return WersaDecayDesc.from_buffer_copy(_DECAY_DESC.pack(
+        B, H, n, dk, dv, _dtype_code(q), offsets is not None, dk ** -0.5 if scale is None else scale,
+        qb, qh, qn, kb, kh, kn, vb, vh, vn, ob, oh, on))
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
 
 
 def _check_states(desc, slots, *states):
@@ -528,8 +538,8 @@ def wersa_decay_forward(q, k, v, log_decay, scale=None, offsets=None, initial_st
     elif workspace is None:
         wb = lib.wersa_decay_workspace_bytes(ctypes.byref(desc), 0)
         workspace = _scratch(wb, q, stream) if wb > 256 else None   # (256: no scratch in it)
-    _check(lib.wersa_decay_forward(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(offsets), _ptr(initial_state),
-                                   _ptr(final_state), _ptr(slots), rows, _ptr(out), _ptr(saved), _ptr(workspace),
+    _check(lib.wersa_decay_forward(ctypes.byref(desc), _addr(q), _addr(k), _addr(v), _addr(log_decay), _addr(offsets), _addr(initial_state),
+                                   _addr(final_state), _addr(slots), rows, _addr(out), _addr(saved), _addr(workspace),
                                    0 if workspace is None else _nbytes(workspace), _stream(stream)))
     return out, final_state, saved
 
@@ -551,9 +561,9 @@ def wersa_decay_backward(q, k, v, log_decay, dout, saved, scale=None, offsets=No
     _check_states(desc, None, grads["dinitial_state"])
     if workspace is None:
         workspace = _scratch(lib.wersa_decay_workspace_bytes(ctypes.byref(desc), 1), q, stream)
-    _check(lib.wersa_decay_backward(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(offsets), _ptr(initial_state),
-                                    _ptr(dout), _ptr(dfinal_state), _ptr(saved), _ptr(grads["dq"]), _ptr(grads["dk"]), _ptr(grads["dv"]),
-                                    _ptr(grads["dinitial_state"]), _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    _check(lib.wersa_decay_backward(ctypes.byref(desc), _addr(q), _addr(k), _addr(v), _addr(log_decay), _addr(offsets), _addr(initial_state),
+                                    _addr(dout), _addr(dfinal_state), _addr(saved), _addr(grads["dq"]), _addr(grads["dk"]), _addr(grads["dv"]),
+                                    _addr(grads["dinitial_state"]), _addr(workspace), _nbytes(workspace), _stream(stream)))
     return grads
 
 
@@ -562,15 +572,25 @@ def wersa_decay_step(q, k, v, log_decay, state, scale=None, slots=None, out=None
     lib = load_library()
     if out is None:
         out = torch.empty(v.shape, dtype=v.dtype, device=v.device)
-    desc = make_decay_desc(q.unsqueeze(2), k.unsqueeze(2), v.unsqueeze(2), out.unsqueeze(2), scale)
+    assert q.dim() == 3 and v.dim() == 3, "expect q, k (B, H, dk) and v, out (B, H, dv)"
+    (B, H, dk), dv, dtype = q.shape, v.shape[2], q.dtype
+    assert k.shape == q.shape and v.shape == (B, H, dv) and out.shape == v.shape, "expect q, k (B, H, dk) and v, out (B, H, dv)"
+    assert k.dtype == dtype and v.dtype == dtype and out.dtype == dtype, "q, k, v and out must share a dtype"
+    (qb, qh, q1), (kb, kh, k1), (vb, vh, v1), (ob, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
+    assert q1 == k1 == v1 == o1 == 1, "expect a contiguous last dim"
+    desc = WersaDecayDesc.from_buffer_copy(_DECAY_DESC.pack(B, H, 1, dk, dv, _dtype_code(q), 0, dk ** -0.5 if scale is None else scale,
+                                                            qb, qh, 0, kb, kh, 0, vb, vh, 0, ob, oh, 0))
     _check_log_decay(log_decay, desc)
     rows = _check_states(desc, slots, state)
-    _check(lib.wersa_decay_step(ctypes.byref(desc), _ptr(q), _ptr(k), _ptr(v), _ptr(log_decay), _ptr(state), _ptr(slots), rows, _ptr(out),
-                                _stream(stream)))
+    _check(lib.wersa_decay_step(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), state.data_ptr(), _addr(slots),
+                                rows, out.data_ptr(), _stream(stream)))
     return out
 
 
 # ---- root-mean-square norm with the residual's addition --------------------------------------------
+
+_NORM_DESC = struct.Struct("qiif4xqq")
+
 
 def _norm_args(x, weight, residual, eps, r):
     """(rows, cols) tensors, columns contiguous; returns the descriptor and the stream's buffer (None without a residual)."""
@@ -578,40 +598,42 @@ def _norm_args(x, weight, residual, eps, r):
     rows, cols = x.shape
     if weight is not None:
         assert weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == cols, "weight: float32, one per column"
+    step = cols
     if residual is not None:
         assert residual.shape == x.shape and residual.dtype == x.dtype and residual.stride(1) == 1, "the residual has x's shape and dtype"
+        step = residual.stride(0)
         if r is None:
-            r = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-        assert r.shape == x.shape and r.dtype == x.dtype and r.is_contiguous()
-    strides = (x.stride(0), cols if residual is None else residual.stride(0))
-    return WersaNormDesc(rows, cols, _dtype_code(x), eps, *strides), r if residual is not None else None
+            r = x.new_empty((rows, cols))
+        else:
+            _dense(r, x.shape, x.dtype, "r")
+    return WersaNormDesc.from_buffer_copy(_NORM_DESC.pack(rows, cols, _dtype_code(x), eps, x.stride(0), step)), r if residual is not None else None
+
+
+def _dense(t, shape, dtype, name):
+    assert t.shape == shape and t.dtype == dtype and t.is_contiguous(), f"{name} is dense, {tuple(shape)} of {dtype}"
+    return t
 
 
 def wersa_rms_norm_forward(x, weight=None, residual=None, eps=1e-6, r=None, y=None, rstd=None, want_rstd=False, stream=None):
     """Returns (y, r, rstd): r = x + residual (x itself without one), rstd (rows) float32 or None."""
     desc, stream_out = _norm_args(x, weight, residual, eps, r)
-    if y is None:
-        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
-    assert y.shape == x.shape and y.dtype == x.dtype and y.is_contiguous()
-    if want_rstd and rstd is None:
-        rstd = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-    assert rstd is None or (rstd.numel() == x.shape[0] and rstd.dtype == torch.float32 and rstd.is_contiguous())
-    _check(load_library().wersa_rms_norm_forward(ctypes.byref(desc), _ptr(x), _ptr(residual), _ptr(weight), _ptr(stream_out), _ptr(y), _ptr(rstd),
-                                                 _stream(stream)))
+    y = x.new_empty(x.shape) if y is None else _dense(y, x.shape, x.dtype, "y")
+    if rstd is not None:
+        _dense(rstd, x.shape[:1], torch.float32, "rstd")
+    elif want_rstd:
+        rstd = x.new_empty(x.shape[0], dtype=torch.float32)
+    _check(load_library().wersa_rms_norm_forward(ctypes.byref(desc), x.data_ptr(), _addr(residual), _addr(weight), _addr(stream_out), y.data_ptr(),
+                                                 _addr(rstd), _stream(stream)))
     return y, x if residual is None else stream_out, rstd
 
 
 def wersa_rms_norm_eight_bit(x, weight=None, residual=None, eps=1e-6, r=None, y=None, scales=None, stream=None):
     """Returns (y, r, scales): y (rows, cols) float8_e4m3fn, to be multiplied by scales (rows) float32."""
     desc, stream_out = _norm_args(x, weight, residual, eps, r)
-    if y is None:
-        y = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
-    if scales is None:
-        scales = torch.empty(x.shape[0], dtype=torch.float32, device=x.device)
-    assert y.shape == x.shape and y.dtype == torch.float8_e4m3fn and y.is_contiguous()
-    assert scales.numel() == x.shape[0] and scales.dtype == torch.float32 and scales.is_contiguous()
-    _check(load_library().wersa_rms_norm_eight_bit(ctypes.byref(desc), _ptr(x), _ptr(residual), _ptr(weight), _ptr(stream_out), _ptr(y),
-                                                   _ptr(scales), _stream(stream)))
+    y = x.new_empty(x.shape, dtype=torch.float8_e4m3fn) if y is None else _dense(y, x.shape, torch.float8_e4m3fn, "y")
+    scales = x.new_empty(x.shape[0], dtype=torch.float32) if scales is None else _dense(scales, x.shape[:1], torch.float32, "scales")
+    _check(load_library().wersa_rms_norm_eight_bit(ctypes.byref(desc), x.data_ptr(), _addr(residual), _addr(weight), _addr(stream_out), y.data_ptr(),
+                                                   scales.data_ptr(), _stream(stream)))
     return y, x if residual is None else stream_out, scales
 
 
@@ -631,8 +653,8 @@ def wersa_rms_norm_backward(r, rstd, dy, weight=None, dr=None, dx=None, want_dwe
         assert dweight.numel() == r.shape[1] and dweight.dtype == torch.float32 and dweight.is_contiguous()
         if workspace is None:
             workspace = _scratch(lib.wersa_rms_norm_workspace_bytes(ctypes.byref(desc)), r, stream)
-    _check(lib.wersa_rms_norm_backward(ctypes.byref(desc), _ptr(r), _ptr(weight), _ptr(rstd), _ptr(dy), _ptr(dr), _ptr(dx), _ptr(dweight),
-                                       _ptr(workspace), 0 if workspace is None else _nbytes(workspace), _stream(stream)))
+    _check(lib.wersa_rms_norm_backward(ctypes.byref(desc), _addr(r), _addr(weight), _addr(rstd), _addr(dy), _addr(dr), _addr(dx), _addr(dweight),
+                                       _addr(workspace), 0 if workspace is None else _nbytes(workspace), _stream(stream)))
     return dx, dweight
 
 

@@ -156,85 +156,152 @@ template <int D, int E, int PIECES, int THREADS, bool FULL> struct TilePieces {
 // Four of them take k = 4 g + i of a 16-wide slice: four consecutive values per lane.
 __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0); }
 
-// Four waves.  Wave w has rows 16 w .. of the chunk for the output and rows (DK / 4) w .. of the state.  P is formed as its transpose (key
-// rows down the registers, query rows on the lanes), which is the layout that the product with V takes it in.
+// A wave's part of a chunk's work and of the state.  Rows 16 t .. of the chunk: the weights of a later tile have more rows to them, so that which wave has which goes by the
+// workgroup (all first waves of a compute unit's workgroups share a SIMD).  Of the state RT row tiles from row0 on and CW column tiles from col0 on: at width 32 a wave has one
+// row tile and half of the columns.
+template <int DK, int DV> struct Part {
+  static constexpr int RT = DK < 64 ? 1 : DK / 64, CT = DV / 16, CW = DK < 64 ? CT / 2 : CT;
+  int t, row0, col0;
+  __device__ __forceinline__ Part(int wave) : t((wave + blockIdx.x + blockIdx.y) & 3), row0(DK < 64 ? 16 * (wave & 1) : DK / 4 * wave), col0(DK < 64 ? DV / 2 * (wave >> 1) : 0) {}
+};
+// Products of a wave's 16 own rows (four consecutive values of a row in a lane) with rows 16 jt .. of the chunk in LDS.
+template <int D> __device__ __forceinline__ f32x4 products_f32(const float *rows, int jt, const f32x4 (&own)[D / 16], int g, int c) {
+  f32x4 p = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+  for (int j = 0; j < D / 16; ++j) {
+    const f32x4 s = *(const f32x4 *)(rows + (16 * jt + c) * (D + 4) + 16 * j + 4 * g);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p = mfma_f32(s[i], own[j][i], p);
+  }
+  return p;
+}
+// The own 16 rows of a tensor in that layout.
+template <int D> __device__ __forceinline__ void load_own_f32(const Rows &r, int r0, uint32_t at, int g, f32x4 (&own)[D / 16]) {
+  const Rows::Chunk c = r.chunk(r0);
+#pragma unroll
+  for (int j = 0; j < D / 16; ++j) own[j] = __builtin_bit_cast(f32x4, load_piece(c, (at + 64 * j - c.missing) | outside(64 * j + 16 * g, r.width)));
+}
+template <int D> __device__ __forceinline__ void store_own_f32(const Rows &r, int r0, uint32_t at, int g, const f32x4 (&o)[D / 16]) {
+  const Rows::Chunk c = r.chunk(r0);
+#pragma unroll
+  for (int j = 0; j < D / 16; ++j) store_piece(c, (at + 64 * j - c.missing) | outside(64 * j + 16 * g, r.width), __builtin_bit_cast(u32x4, o[j]));
+}
+template <int D, int PIECES> __device__ __forceinline__ void put_tile_f32(float *rows, int tid, const u32x4 (&p)[PIECES]) {
+#pragma unroll
+  for (int i = 0; i < PIECES; ++i) *(u32x4 *)(rows + (tid / (D / 4) + 1024 / D * i) * (D + 4) + tid % (D / 4) * 4) = p[i];
+}
+template <int DK, int DV, typename F>
+__device__ __forceinline__ void each_of_state_f32(const Walk &a, f32x4 (&S)[Part<DK, DV>::RT][Part<DK, DV>::CW], const Part<DK, DV> &part, int g, int lane_c, F f) {
+  const int c = (int)opaque((uint32_t)lane_c);
+#pragma unroll
+  for (int rt = 0; rt < Part<DK, DV>::RT; ++rt)
+#pragma unroll
+    for (int ct = 0; ct < Part<DK, DV>::CW; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = part.row0 + 16 * rt + 4 * g + i, col = part.col0 + 16 * ct + c;
+        S[rt][ct][i] = f(S[rt][ct][i], r < a.kw && col < a.vw, r * a.si + col * a.sj);
+      }
+}
+// Of the weights of own rows 16 t + c against rows 16 jt + 4 g + i of the chunk: lambda to the distance; the rest of the row is masked.
+struct WeightsF32 {
+  float on[4], before[4], apart[3], reach;
+  int t, ahead;
+  __device__ __forceinline__ WeightsF32(const Walk &a, float l2, int t, int g, int c) : t(t), ahead(c - 4 * g) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      on[i] = ahead >= i ? a.intra * decay_pow(l2, ahead - i) : 0.f;
+      before[i] = a.intra * decay_pow(l2, 16 + ahead - i);
+    }
+#pragma unroll
+    for (int jt = 0; jt < 3; ++jt) apart[jt] = decay_pow(l2, 16 * max(t - jt - 1, 0));
+    reach = a.inter * decay_pow(l2, 16 * t + c + (a.reverse ? 0 : 1));
+  }
+  __device__ __forceinline__ f32x4 operator()(f32x4 p, int jt) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) p[i] = jt < t ? p[i] * before[i] * apart[jt < 3 ? jt : 0] : ahead >= i ? p[i] * on[i] : 0.f;
+    return p;
+  }
+};
+// S += (K o weight)^T V over rows 16 jt .. of the chunk; V: the rows' values in the layout below.
+template <int DK, int DV>
+__device__ __forceinline__ void add_to_state_f32(const Part<DK, DV> &part, f32x4 (&S)[Part<DK, DV>::RT][Part<DK, DV>::CW], const float *Ks, const float *Vs, const float *weight, int jt,
+                                                 const float (&V)[DV / 16][4], int g, int c) {
+  constexpr int LK = DK + 4, LV = DV + 4, RT = Part<DK, DV>::RT, CW = Part<DK, DV>::CW;
+  const f32x4 wt = *(const f32x4 *)(weight + 16 * jt + 4 * g);
+  float U[CW][4];
+#pragma unroll
+  for (int ct = 0; ct < CW; ++ct)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) U[ct][i] = DK < 64 ? Vs[(16 * jt + 4 * g + i) * LV + part.col0 + 16 * ct + c] : V[ct][i];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float kt = Ks[(16 * jt + 4 * g + i) * LK + part.row0 + 16 * rt + c] * wt[i];
+#pragma unroll
+      for (int ct = 0; ct < CW; ++ct) S[rt][ct] = mfma_f32(kt, U[ct][i], S[rt][ct]);
+    }
+}
+template <int D> __device__ __forceinline__ void columns_f32(const float *rows, int jt, int g, int c, float (&v)[D / 16][4]) {
+#pragma unroll
+  for (int ct = 0; ct < D / 16; ++ct)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[ct][i] = rows[(16 * jt + 4 * g + i) * (D + 4) + 16 * ct + c];
+}
+
+// Four waves.  Weights are formed as their transpose (the chunk's rows down the registers, own rows on the lanes), which is the layout that the product with V takes them in.
 template <int DK, int DV, bool STATES>
 __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
-  constexpr int LK = DK + 4, LV = DV + 4;
-  constexpr int PK = kChunk * DK / 4 / 256, PV = kChunk * DV / 4 / 256;   // pieces of a thread
-  constexpr int RT = DK / 64, CT = DV / 16;                                         // state: row tiles of a wave, column tiles
+  constexpr int LK = DK + 4, LV = DV + 4, PK = kChunk * DK / 4 / 256, PV = kChunk * DV / 4 / 256;   // pieces of a thread
+  typedef Part<DK, DV> P4;
+  constexpr int CT = P4::CT;
   extern __shared__ __align__(16) float lds[];
   float *Ks = lds, *Vs = Ks + kChunk * LK, *weight = Vs + kChunk * LV, *St = weight + kChunk;
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
-  const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int h = blockIdx.y, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const bool last = a.reverse ? seg.s == 0 : seg.s == a.seq.segments(seg.b) - 1;
   if (STATES && last) return;   // nothing begins with what the last one adds
-  const int shift = a.reverse ? 1 : 0;
+  const P4 part(wave);
   const Rows qr = rows_of(a.q, a.sq, seg, a, h, a.kw, 4), kr = rows_of(a.k, a.sk, seg, a, h, a.kw, 4), vr = rows_of(a.v, a.sv, seg, a, h, a.vw, 4),
              orow = rows_of(a.o, a.so, seg, a, h, a.vw, 4);
   const float l2 = log2_decay(a.log_decay, h);
   const int64_t state_size = (int64_t)a.kw * a.vw;
 
-  // state: S[rt][ct][i] is row 16 (RT w + rt) + 4 g + i, column 16 ct + c
-  f32x4 S[RT][CT];
+  f32x4 S[P4::RT][P4::CW];   // S[rt][ct][i] is row row0 + 16 rt + 4 g + i, column col0 + 16 ct + c
   const int own = cache_row(a, seg.b);
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
   const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
-#pragma unroll
-  for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-    for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = 16 * (RT * w + rt) + 4 * g + i, col = 16 * ct + c;
-        S[rt][ct][i] = init && r < a.kw && col < a.vw ? init[r * a.si + col * a.sj] : 0.f;
-      }
-
-  float factor[4][4];   // of P, by key tile
-#pragma unroll
-  for (int jt = 0; jt < 4; ++jt)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int e = 16 * (w - jt) + c - 4 * g - i;
-      factor[jt][i] = e >= 0 ? a.intra * decay_pow(l2, e) : 0.f;
-    }
-  const float reach = a.inter * decay_pow(l2, 16 * w + c + 1 - shift);
+  each_of_state_f32<DK, DV>(a, S, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  const WeightsF32 weights(a, l2, part.t, g, c);
 
   u32x4 rk[PK], rv[PV];
   f32x4 rq[DK / 16];
-  const int krow = tid / (DK / 4), kcol = tid % (DK / 4) * 4, vrow = tid / (DV / 4), vcol = tid % (DV / 4) * 4;   // a thread's first piece
   const TilePieces<DK, 4, PK, 256, false> kp(kr, 0, tid);
   const TilePieces<DV, 4, PV, 256, false> vp(vr, 0, tid);
-  const uint32_t qat = qr.offset(16 * w + c, 16 * g);
+  const uint32_t qat = qr.offset(16 * part.t + c, 16 * g), oat = orow.offset(16 * part.t + c, 16 * g);
   auto request = [&](int r0) {
     kp.template load<false>(kr, r0, rk);
     vp.template load<false>(vr, r0, rv);
-    if (!STATES) {
-      const Rows::Chunk qc = qr.chunk(r0);
-#pragma unroll
-      for (int j = 0; j < DK / 16; ++j)
-        rq[j] = __builtin_bit_cast(f32x4, load_piece(qc, (qat + 64 * j - qc.missing) | outside(64 * j + 16 * g, qr.width)));
-    }
+    if (!STATES) load_own_f32<DK>(qr, r0, qat, g, rq);
   };
 
   request(0);
   for (int r0 = 0; r0 < seg.rows; r0 += kChunk) {
     const int rows = min(kChunk, seg.rows - r0);
     // what was requested, and the state, into LDS
-#pragma unroll
-    for (int i = 0; i < PK; ++i) *(u32x4 *)(Ks + (krow + 1024 / DK * i) * LK + kcol) = rk[i];
-#pragma unroll
-    for (int i = 0; i < PV; ++i) *(u32x4 *)(Vs + (vrow + 1024 / DV * i) * LV + vcol) = rv[i];
-    if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + shift);
+    put_tile_f32<DK>(Ks, tid, rk);
+    put_tile_f32<DV>(Vs, tid, rv);
+    if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + (a.reverse ? 1 : 0));
     f32x4 Q[DK / 16];
     if (!STATES) {
 #pragma unroll
       for (int j = 0; j < DK / 16; ++j) Q[j] = rq[j];
 #pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
+      for (int rt = 0; rt < P4::RT; ++rt)
 #pragma unroll
-        for (int ct = 0; ct < CT; ++ct) *(f32x4 *)(St + (16 * ct + c) * LK + 16 * (RT * w + rt) + 4 * g) = S[rt][ct];
+        for (int ct = 0; ct < P4::CW; ++ct) *(f32x4 *)(St + (part.col0 + 16 * ct + c) * LK + part.row0 + 16 * rt + 4 * g) = S[rt][ct];
     }
     __syncthreads();
     request(r0 + kChunk);
@@ -242,76 +309,150 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
     f32x4 O[CT];
     if (!STATES) {
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
-        O[ct] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < DK / 16; ++j) {
-          const f32x4 s = *(const f32x4 *)(St + (16 * ct + c) * LK + 16 * j + 4 * g);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) O[ct] = mfma_f32(s[i], Q[j][i], O[ct]);
-        }
-        O[ct] *= reach;
-      }
+      for (int ct = 0; ct < CT; ++ct) O[ct] = products_f32<DK>(St, ct, Q, g, c) * weights.reach;
     }
     const float keep = decay_pow(l2, rows);
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+    for (int rt = 0; rt < P4::RT; ++rt)
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) S[rt][ct] *= keep;
+      for (int ct = 0; ct < P4::CW; ++ct) S[rt][ct] *= keep;
 #pragma unroll
     for (int jt = 0; jt < 4; ++jt) {
       float V[CT][4];
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) V[ct][i] = Vs[(16 * jt + 4 * g + i) * LV + 16 * ct + c];
-      if (!STATES && jt <= w) {
-        f32x4 P = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < DK / 16; ++j) {
-          const f32x4 s = *(const f32x4 *)(Ks + (16 * jt + c) * LK + 16 * j + 4 * g);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) P = mfma_f32(s[i], Q[j][i], P);
-        }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) P[i] = jt < w || c >= 4 * g + i ? P[i] * factor[jt][i] : 0.f;
+      if (DK >= 64 || jt <= part.t) columns_f32<DV>(Vs, jt, g, c, V);
+      if (!STATES && jt <= part.t) {
+        const f32x4 P = weights(products_f32<DK>(Ks, jt, Q, g, c), jt);
 #pragma unroll
         for (int ct = 0; ct < CT; ++ct)
 #pragma unroll
           for (int i = 0; i < 4; ++i) O[ct] = mfma_f32(V[ct][i], P[i], O[ct]);
       }
-      const f32x4 wt = *(const f32x4 *)(weight + 16 * jt + 4 * g);
-#pragma unroll
-      for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float kt = Ks[(16 * jt + 4 * g + i) * LK + 16 * (RT * w + rt) + c] * wt[i];
-#pragma unroll
-          for (int ct = 0; ct < CT; ++ct) S[rt][ct] = mfma_f32(kt, V[ct][i], S[rt][ct]);
-        }
+      add_to_state_f32<DK, DV>(part, S, Ks, Vs, weight, jt, V, g, c);
     }
-    if (!STATES) {
-      const Rows::Chunk oc = orow.chunk(r0);
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
-        store_piece(oc, (orow.offset(16 * w + c, 64 * ct + 16 * g) - oc.missing) | outside(64 * ct + 16 * g, orow.width), __builtin_bit_cast(u32x4, O[ct]));
-    }
+    if (!STATES) store_own_f32<DV>(orow, r0, oat, g, O);
     __syncthreads();
   }
 
   float *fin = nullptr;
   if (STATES) fin = a.fin + ((int64_t)blockIdx.x * a.H + h) * state_size;
   else if (last && a.fin && own >= 0) fin = a.fin + ((int64_t)own * a.H + h) * state_size;
-  if (fin) {
+  if (fin) each_of_state_f32<DK, DV>(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
+}
+
+// The two walks back of the derivative as one, k and v of `a` being q and dout: own rows of keys and values, G^T k and the weighted rows of dout give dv, G v and the
+// weighted rows of q give dk.  Reads four tensors and writes two, where two walks read three and write one each, and forms G once.
+struct Back {
+  const void *k, *v;
+  void *dk, *dv;
+  Strides sk, sv;
+};
+template <int DK, int DV>
+__global__ __launch_bounds__(256) void back_f32_kernel(Walk a, Back b) {
+  constexpr int LK = DK + 4, LV = DV + 4, PK = kChunk * DK / 4 / 256, PV = kChunk * DV / 4 / 256;
+  typedef Part<DK, DV> P4;
+  constexpr int KT = DK / 16, CT = P4::CT;
+  extern __shared__ __align__(16) float lds[];
+  float *Qs = lds, *Ds = Qs + kChunk * LK, *weight = Ds + kChunk * LV, *Gt = weight + kChunk;
+  const Segment seg = segment_of(a.seq, blockIdx.x);
+  if (seg.rows < 0) return;
+  const int h = blockIdx.y, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const P4 part(wave);
+  const Rows qr = rows_of(a.k, a.sk, seg, a, h, a.kw, 4), dr = rows_of(a.v, a.sv, seg, a, h, a.vw, 4), kr = rows_of(b.k, b.sk, seg, a, h, a.kw, 4),
+             vr = rows_of(b.v, b.sv, seg, a, h, a.vw, 4), dkr = rows_of(b.dk, b.sk, seg, a, h, a.kw, 4), dvr = rows_of(b.dv, b.sv, seg, a, h, a.vw, 4);
+  const float l2 = log2_decay(a.log_decay, h);
+  const int64_t state_size = (int64_t)a.kw * a.vw;
+
+  f32x4 G[P4::RT][P4::CW];
+  const int64_t from = a.by_slot ? (int64_t)blockIdx.x : seg.b;
+  const float *init = a.init ? a.init + (from * a.H + h) * state_size : nullptr;
+  each_of_state_f32<DK, DV>(a, G, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  const WeightsF32 weights(a, l2, part.t, g, c);
+
+  u32x4 rq[PK], rd[PV];
+  f32x4 K[KT], V[CT];
+  const TilePieces<DK, 4, PK, 256, false> qp(qr, 0, tid);
+  const TilePieces<DV, 4, PV, 256, false> dp(dr, 0, tid);
+  const uint32_t kat = kr.offset(16 * part.t + c, 16 * g), vat = vr.offset(16 * part.t + c, 16 * g);
+  const uint32_t dkat = dkr.offset(16 * part.t + c, 16 * g), dvat = dvr.offset(16 * part.t + c, 16 * g);
+  auto request = [&](int r0) {
+    qp.template load<false>(qr, r0, rq);
+    dp.template load<false>(dr, r0, rd);
+  };
+  auto request_own = [&](int r0) {
+    load_own_f32<DK>(kr, r0, kat, g, K);
+    load_own_f32<DV>(vr, r0, vat, g, V);
+  };
+  request(0);
+  request_own(0);
+  for (int r0 = 0; r0 < seg.rows; r0 += kChunk) {
+    const int rows = min(kChunk, seg.rows - r0);
+    put_tile_f32<DK>(Qs, tid, rq);
+    put_tile_f32<DV>(Ds, tid, rd);
+    if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + 1);
 #pragma unroll
-    for (int rt = 0; rt < RT; ++rt)
+    for (int rt = 0; rt < P4::RT; ++rt)
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct)
+      for (int ct = 0; ct < P4::CW; ++ct) *(f32x4 *)(Gt + (part.col0 + 16 * ct + c) * LK + part.row0 + 16 * rt + 4 * g) = G[rt][ct];
+    __syncthreads();
+    request(r0 + kChunk);
+    {
+      f32x4 O[CT];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = 16 * (RT * w + rt) + 4 * g + i, col = 16 * ct + c;
-          if (r < a.kw && col < a.vw) fin[r * a.si + col * a.sj] = S[rt][ct][i];
-        }
+      for (int ct = 0; ct < CT; ++ct) O[ct] = products_f32<DK>(Gt, ct, K, g, c) * weights.reach;
+#pragma unroll
+      for (int jt = 0; jt < 4; ++jt) {
+        if (jt > part.t) break;
+        float D[CT][4];
+        columns_f32<DV>(Ds, jt, g, c, D);
+        const f32x4 P = weights(products_f32<DK>(Qs, jt, K, g, c), jt);
+#pragma unroll
+        for (int ct = 0; ct < CT; ++ct)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) O[ct] = mfma_f32(D[ct][i], P[i], O[ct]);
+      }
+      store_own_f32<DV>(dvr, r0, dvat, g, O);
+    }
+    {
+      f32x4 O[KT];
+#pragma unroll
+      for (int kt = 0; kt < KT; ++kt) {   // G v: rows of G down the lanes, its columns four values apart in Gt
+        O[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int j = 0; j < CT; ++j)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) O[kt] = mfma_f32(Gt[(16 * j + 4 * g + i) * LK + 16 * kt + c], V[j][i], O[kt]);
+        O[kt] *= weights.reach;
+      }
+#pragma unroll
+      for (int jt = 0; jt < 4; ++jt) {
+        if (jt > part.t) break;
+        float U[KT][4];
+        columns_f32<DK>(Qs, jt, g, c, U);
+        const f32x4 P = weights(products_f32<DV>(Ds, jt, V, g, c), jt);
+#pragma unroll
+        for (int kt = 0; kt < KT; ++kt)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) O[kt] = mfma_f32(U[kt][i], P[i], O[kt]);
+      }
+      store_own_f32<DK>(dkr, r0, dkat, g, O);
+    }
+    request_own(r0 + kChunk);
+    const float keep = decay_pow(l2, rows);
+#pragma unroll
+    for (int rt = 0; rt < P4::RT; ++rt)
+#pragma unroll
+      for (int ct = 0; ct < P4::CW; ++ct) G[rt][ct] *= keep;
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt) {
+      float D[CT][4];
+      if (DK >= 64) columns_f32<DV>(Ds, jt, g, c, D);
+      add_to_state_f32<DK, DV>(part, G, Qs, Ds, weight, jt, D, g, c);
+    }
+    __syncthreads();
+  }
+  if (a.fin && seg.s == 0) {
+    float *fin = a.fin + ((int64_t)seg.b * a.H + h) * state_size;
+    each_of_state_f32<DK, DV>(a, G, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
   }
 }
 
@@ -618,13 +759,7 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
   if (fin) each_of_state<DK, DV>(a, S, row0, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
 }
 
-// The two walks back of the derivative as one, k and v of `a` being q and dout: own rows of keys and values, G^T k and the weighted rows of dout give dv, G v and the
-// weighted rows of q give dk.  Reads four tensors and writes two, where two walks read three and write one each, and forms G once.
-struct Back {
-  const void *k, *v;
-  void *dk, *dv;
-  Strides sk, sv;
-};
+// As back_f32_kernel, for bf16 tensors.
 template <int DK, int DV, bool FULL>
 __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;
@@ -724,29 +859,34 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
   }
 }
 
-// What the segments of a sequence add to the state, in place, to the states that they begin with: one value of a state per thread, over all
-// segments in their order (from the last one with `reverse`).  Bound by the way to memory and back of each round of requests, so that a round has many.
-constexpr int kScanRound = 32;
-__global__ __launch_bounds__(64) void scan_kernel(Walk a, float *local) {
+// What the segments of a sequence add to the state, in place, to the states that they begin with: E values of a state per thread, over all
+// segments in their order (from the last one with `reverse`).  Few states are bound by the way to memory and back of each round of requests: rounds have many,
+// and a thread has one value, so that there are threads; many states (packed prompts) by the launch of their workgroups: four values then.  24 packed prompts, 16 heads
+// of 128 x 128: 77 us with one value; 8 slices of 64 x 64, 96 segments: 31 us with four values and rounds of eight.
+template <int E, int ROUND>
+__global__ __launch_bounds__(256) void scan_kernel(Walk a, float *local) {
+  typedef float V __attribute__((ext_vector_type(E)));
   const int h = blockIdx.y, b = blockIdx.z;
-  const int64_t state_size = (int64_t)a.kw * a.vw, e = (int64_t)blockIdx.x * 64 + threadIdx.x;   // (a multiple of 64)
+  const int64_t state_size = (int64_t)a.kw * a.vw, e = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * E;
+  if (e >= state_size) return;
   const int segs = a.seq.segments(b), have = a.seq.rows(b), own = cache_row(a, b);
   const float l2 = log2_decay(a.log_decay, h);
-  float run = a.init && own >= 0 ? a.init[((int64_t)own * a.H + h) * state_size + e] : 0.f;
+  V run = V(0.f);
+  if (a.init && own >= 0) run = *(const V *)(a.init + ((int64_t)own * a.H + h) * state_size + e);
   const int64_t step = a.H * state_size;
   float *p = local + ((int64_t)a.seq.first_slot(b) * a.H + h) * state_size + e;
   const float full = decay_pow(l2, a.seq.seg), tail = decay_pow(l2, have - (segs - 1) * a.seq.seg);
-  for (int s0 = 0; s0 < segs; s0 += kScanRound) {
-    float x[kScanRound];
+  for (int s0 = 0; s0 < segs; s0 += ROUND) {
+    V x[ROUND];
 #pragma unroll
-    for (int u = 0; u < kScanRound; ++u) {
+    for (int u = 0; u < ROUND; ++u) {
       const int s = a.reverse ? segs - 1 - s0 - u : s0 + u;
-      x[u] = s0 + u < segs - 1 ? p[s * step] : 0.f;   // the last one has added nothing
+      x[u] = s0 + u < segs - 1 ? *(const V *)(p + s * step) : V(0.f);   // the last one has added nothing
     }
 #pragma unroll
-    for (int u = 0; u < kScanRound; ++u) {
+    for (int u = 0; u < ROUND; ++u) {
       const int s = a.reverse ? segs - 1 - s0 - u : s0 + u;
-      if (s0 + u < segs) p[s * step] = run;
+      if (s0 + u < segs) *(V *)(p + s * step) = run;
       run = run * (s == segs - 1 ? tail : full) + x[u];
     }
   }
@@ -810,14 +950,18 @@ __global__ __launch_bounds__(256) void step_kernel(Step a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-// Workgroups that a walk should have: those that the device holds at a time, three to a compute unit at widths up to 64 in bf16, else two.
+// Rows of a segment.  Segments are as many as the device holds workgroups at a time, three to a compute unit at widths up to 64 in bf16, else two: a walk over more
+// of them has a last round that is partly idle (32 slices of 65536 rows, width 128, 768 instead of 512: walk 615 us, 519 with 512).  Packed sequences have a
+// partial segment each on top, and three quarters as many whole ones (24 prompts, 16 heads, 65536 rows: 476 us in all, 507 without this).  Two chunks at least: 8 slices
+// of 1000 rows 22 us with segments of one, two or four chunks, 32 with eight or in one launch.
 int segment_rows(const wersa_decay_desc &c) {
   const int64_t slices = (int64_t)c.H * (c.packed ? 1 : c.B);
-  const int64_t want = (c.dk <= 64 && c.dv <= 64 ? 768 : 512) / slices;   // segments of a slice
+  const int64_t held = c.dtype == WERSA_BF16 && c.dk <= 64 && c.dv <= 64 ? 768 : 512;
+  const int64_t want = (c.packed ? held * 3 / 4 : held) / slices;   // segments of a slice
   if (want <= 1) return c.packed ? INT32_MAX / 2 : (c.n + kChunk - 1) / kChunk * kChunk + kChunk;
   int64_t rows = ((int64_t)c.n + want - 1) / want;
   rows = (rows + kChunk - 1) / kChunk * kChunk;
-  return (int)(rows < 4 * kChunk ? 4 * kChunk : rows);
+  return (int)(rows < 2 * kChunk ? 2 * kChunk : rows);
 }
 Sequences sequences(const wersa_decay_desc &c, const int32_t *offsets) {
   Sequences s;
@@ -865,29 +1009,37 @@ template <typename K, typename... Args> bool launch(const char *name, K kern, si
   WERSA_STAGE(name, st, kern<<<dim3(a.seq.slots(), a.H), 256, smem, st>>>(a, more...));
   return true;
 }
+constexpr size_t f32_lds(int dk, int dv, bool state) { return sizeof(float) * (kChunk * (dk + 4 + dv + 4 + 1) + (state ? dv * (dk + 4) : 0)); }
 template <int DK, int DV, bool STATES> bool launch_walk_as(const wersa_decay_desc &c, const Walk &a, hipStream_t st) {
   const char *name = STATES ? "wersa_decay_states" : "wersa_decay_walk";
-  if (c.dtype == WERSA_F32)
-    return launch(name, &walk_f32_kernel<DK, DV, STATES>, sizeof(float) * (kChunk * (DK + 4 + DV + 4 + 1) + (STATES ? 0 : DV * (DK + 4))), a, st);
+  if (c.dtype == WERSA_F32) return launch(name, &walk_f32_kernel<DK, DV, STATES>, f32_lds(DK, DV, !STATES), a, st);
   constexpr size_t sets = STATES ? 2 : 1, smem = 2 * (sets * kChunk * (DK + DV) + (STATES ? 0 : DV * DK)) + 4 * (STATES ? 256 : 32 * (DK > DV ? DK : DV));
   return a.kw == DK && a.vw == DV ? launch(name, &walk_bf16_kernel<DK, DV, true, STATES>, smem, a, st)
                                   : launch(name, &walk_bf16_kernel<DK, DV, false, STATES>, smem, a, st);
 }
 template <bool STATES> bool launch_walk(const wersa_decay_desc &c, const Walk &a, hipStream_t st) {
+  if (c.dtype == WERSA_F32 && a.kw <= 32 && a.vw <= 32)
+    return launch(STATES ? "wersa_decay_states" : "wersa_decay_walk", &walk_f32_kernel<32, 32, STATES>, f32_lds(32, 32, !STATES), a, st);
   if (a.kw <= 64) return a.vw <= 64 ? launch_walk_as<64, 64, STATES>(c, a, st) : launch_walk_as<64, 128, STATES>(c, a, st);
   return a.vw <= 64 ? launch_walk_as<128, 64, STATES>(c, a, st) : launch_walk_as<128, 128, STATES>(c, a, st);
 }
-template <int DK, int DV> bool launch_back_as(const Walk &a, const Back &b, hipStream_t st) {
+template <int DK, int DV> bool launch_back_as(const wersa_decay_desc &c, const Walk &a, const Back &b, hipStream_t st) {
+  if (c.dtype == WERSA_F32) return launch("wersa_decay_back", &back_f32_kernel<DK, DV>, f32_lds(DK, DV, true), a, st, b);
   constexpr size_t smem = 2 * (kChunk * (DK + DV) + DV * DK) + 4 * 32 * (DK > DV ? DK : DV);
   return a.kw == DK && a.vw == DV ? launch("wersa_decay_back", &back_bf16_kernel<DK, DV, true>, smem, a, st, b)
                                   : launch("wersa_decay_back", &back_bf16_kernel<DK, DV, false>, smem, a, st, b);
 }
-bool launch_back(const Walk &a, const Back &b, hipStream_t st) {
-  if (a.kw <= 64) return a.vw <= 64 ? launch_back_as<64, 64>(a, b, st) : launch_back_as<64, 128>(a, b, st);
-  return a.vw <= 64 ? launch_back_as<128, 64>(a, b, st) : launch_back_as<128, 128>(a, b, st);
+bool launch_back(const wersa_decay_desc &c, const Walk &a, const Back &b, hipStream_t st) {
+  if (c.dtype == WERSA_F32 && a.kw <= 32 && a.vw <= 32) return launch("wersa_decay_back", &back_f32_kernel<32, 32>, f32_lds(32, 32, true), a, st, b);
+  if (a.kw <= 64) return a.vw <= 64 ? launch_back_as<64, 64>(c, a, b, st) : launch_back_as<64, 128>(c, a, b, st);
+  return a.vw <= 64 ? launch_back_as<128, 64>(c, a, b, st) : launch_back_as<128, 128>(c, a, b, st);
 }
 void launch_scan(const Walk &a, float *local, hipStream_t st) {
-  WERSA_STAGE("wersa_decay_scan", st, scan_kernel<<<dim3(a.kw * a.vw / 64, a.H, a.seq.B), 64, 0, st>>>(a, local));
+  const int size = a.kw * a.vw;
+  if ((int64_t)size * a.H * a.seq.B >= 1 << 21)   // eight waves of four values to a SIMD
+    WERSA_STAGE("wersa_decay_scan", st, (scan_kernel<4, 8><<<dim3((size / 4 + 255) / 256, a.H, a.seq.B), 256, 0, st>>>(a, local)));
+  else
+    WERSA_STAGE("wersa_decay_scan", st, (scan_kernel<1, 32><<<dim3((size + 63) / 64, a.H, a.seq.B), 64, 0, st>>>(a, local)));
 }
 
 }  // namespace
@@ -980,19 +1132,11 @@ wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, c
     r.fin = (float *)workspace;
     if (!launch_walk<true>(c, r, st)) return WERSA_ERR_LAUNCH;
     launch_scan(r, (float *)workspace, st);
-    a.init = r.init = (const float *)workspace;
-    a.by_slot = r.by_slot = true;
+    r.init = (const float *)workspace;
+    r.by_slot = true;
   }
   r.fin = dinitial_state;
-  if (c.dtype == WERSA_BF16) {
-    if (!launch_back(r, Back{k, v, dk, dv, sk, sv}, st)) return WERSA_ERR_LAUNCH;
-    return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
-  }
-  if (!launch_walk<false>(c, r, st)) return WERSA_ERR_LAUNCH;
-  a.q = v, a.k = dout, a.v = q, a.o = dk;
-  a.sq = sv, a.sk = so, a.sv = sq, a.so = sk;
-  a.kw = c.dv, a.vw = c.dk, a.si = 1, a.sj = c.dv;
-  if (!launch_walk<false>(c, a, st)) return WERSA_ERR_LAUNCH;
+  if (!launch_back(c, r, Back{k, v, dk, dv, sk, sv}, st)) return WERSA_ERR_LAUNCH;
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
 
