@@ -219,7 +219,7 @@ struct WeightsF32 {
   }
   __device__ __forceinline__ f32x4 operator()(f32x4 p, int jt) const {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) p[i] = jt < t ? p[i] * before[i] * apart[jt < 3 ? jt : 0] : ahead >= i ? p[i] * on[i] : 0.f;
+    for (int i = 0; i < 4; ++i) p[i] = jt < t ? p[i] * before[i] * (jt == 0 ? apart[0] : jt == 1 ? apart[1] : apart[2]) : ahead >= i ? p[i] * on[i] : 0.f;
     return p;
   }
 };
@@ -248,6 +248,56 @@ template <int D> __device__ __forceinline__ void columns_f32(const float *rows, 
   for (int ct = 0; ct < D / 16; ++ct)
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[ct][i] = rows[(16 * jt + 4 * g + i) * (D + 4) + 16 * ct + c];
+}
+
+// The output of a wave's 16 own rows: what the state gives (`inter`, a tile of columns at a time) and the weighted rows of the chunk, `weight` their weights for rows 16 jt ..
+// A weight that is masked is a zero, and in a product of matrices a zero times what is not a number or not finite is not a number: rows that come later would reach back.  So results that
+// are not finite are formed again, with such values left out; where none of a row's own reach is among them, that is the result.
+template <int D, typename Inter, typename Weight>
+__device__ __forceinline__ void weighted_rows_f32(const float *rows, const Rows &out, int r0, uint32_t at, int t, int g, int c, Inter inter, Weight weight) {
+  float probe = 0.f;
+  {
+    f32x4 O[D / 16];
+#pragma unroll
+    for (int ct = 0; ct < D / 16; ++ct) O[ct] = inter(ct);
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt) {
+      if (jt > t) break;
+      float V[D / 16][4];
+      columns_f32<D>(rows, jt, g, c, V);
+      const f32x4 P = weight(jt);
+#pragma unroll
+      for (int ct = 0; ct < D / 16; ++ct)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) O[ct] = mfma_f32(V[ct][i], P[i], O[ct]);
+    }
+#pragma unroll
+    for (int ct = 0; ct < D / 16; ++ct)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) probe = fmaf(O[ct][i], 0.f, probe);   // not a number if one is not finite
+    store_own_f32<D>(out, r0, at, g, O);
+  }
+  if (!__any(!(probe == 0.f))) return;
+  const Rows::Chunk oc = out.chunk(r0);
+#pragma unroll 1
+  for (int ct = 0; ct < D / 16; ++ct) {
+    f32x4 all = inter(ct), finite = all, met = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int jt = 0; jt <= t; ++jt) {
+      const f32x4 P = weight(jt);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float v = rows[(16 * jt + 4 * g + i) * (D + 4) + 16 * ct + c];
+        const bool fine = fabsf(v) < __builtin_inff();
+        all = mfma_f32(v, P[i], all);
+        finite = mfma_f32(fine ? v : 0.f, P[i], finite);
+        met = mfma_f32(fine ? 0.f : 1.f, 16 * jt + 4 * g + i <= 16 * t + c ? 1.f : 0.f, met);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) all[i] = met[i] > 0.f ? all[i] : finite[i];
+    store_piece(oc, (at + 64 * ct - oc.missing) | outside(64 * ct + 16 * g, out.width), __builtin_bit_cast(u32x4, all));
+  }
 }
 
 // Four waves.  Weights are formed as their transpose (the chunk's rows down the registers, own rows on the lanes), which is the layout that the product with V takes them in.
@@ -306,11 +356,9 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
     __syncthreads();
     request(r0 + kChunk);
 
-    f32x4 O[CT];
-    if (!STATES) {
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) O[ct] = products_f32<DK>(St, ct, Q, g, c) * weights.reach;
-    }
+    if (!STATES)
+      weighted_rows_f32<DV>(Vs, orow, r0, oat, part.t, g, c, [&](int ct) { return products_f32<DK>(St, ct, Q, g, c) * weights.reach; },
+                            [&](int jt) { return weights(products_f32<DK>(Ks, jt, Q, g, c), jt); });
     const float keep = decay_pow(l2, rows);
 #pragma unroll
     for (int rt = 0; rt < P4::RT; ++rt)
@@ -319,17 +367,9 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
 #pragma unroll
     for (int jt = 0; jt < 4; ++jt) {
       float V[CT][4];
-      if (DK >= 64 || jt <= part.t) columns_f32<DV>(Vs, jt, g, c, V);
-      if (!STATES && jt <= part.t) {
-        const f32x4 P = weights(products_f32<DK>(Ks, jt, Q, g, c), jt);
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) O[ct] = mfma_f32(V[ct][i], P[i], O[ct]);
-      }
+      if (DK >= 64) columns_f32<DV>(Vs, jt, g, c, V);
       add_to_state_f32<DK, DV>(part, S, Ks, Vs, weight, jt, V, g, c);
     }
-    if (!STATES) store_own_f32<DV>(orow, r0, oat, g, O);
     __syncthreads();
   }
 
@@ -395,47 +435,16 @@ __global__ __launch_bounds__(256) void back_f32_kernel(Walk a, Back b) {
       for (int ct = 0; ct < P4::CW; ++ct) *(f32x4 *)(Gt + (part.col0 + 16 * ct + c) * LK + part.row0 + 16 * rt + 4 * g) = G[rt][ct];
     __syncthreads();
     request(r0 + kChunk);
-    {
-      f32x4 O[CT];
+    weighted_rows_f32<DV>(Ds, dvr, r0, dvat, part.t, g, c, [&](int ct) { return products_f32<DK>(Gt, ct, K, g, c) * weights.reach; },
+                          [&](int jt) { return weights(products_f32<DK>(Qs, jt, K, g, c), jt); });
+    weighted_rows_f32<DK>(Qs, dkr, r0, dkat, part.t, g, c, [&](int kt) {   // G v: rows of G down the lanes, its columns four values apart in Gt
+      f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int ct = 0; ct < CT; ++ct) O[ct] = products_f32<DK>(Gt, ct, K, g, c) * weights.reach;
+      for (int j = 0; j < CT; ++j)
 #pragma unroll
-      for (int jt = 0; jt < 4; ++jt) {
-        if (jt > part.t) break;
-        float D[CT][4];
-        columns_f32<DV>(Ds, jt, g, c, D);
-        const f32x4 P = weights(products_f32<DK>(Qs, jt, K, g, c), jt);
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) O[ct] = mfma_f32(D[ct][i], P[i], O[ct]);
-      }
-      store_own_f32<DV>(dvr, r0, dvat, g, O);
-    }
-    {
-      f32x4 O[KT];
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {   // G v: rows of G down the lanes, its columns four values apart in Gt
-        O[kt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < CT; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) O[kt] = mfma_f32(Gt[(16 * j + 4 * g + i) * LK + 16 * kt + c], V[j][i], O[kt]);
-        O[kt] *= weights.reach;
-      }
-#pragma unroll
-      for (int jt = 0; jt < 4; ++jt) {
-        if (jt > part.t) break;
-        float U[KT][4];
-        columns_f32<DK>(Qs, jt, g, c, U);
-        const f32x4 P = weights(products_f32<DV>(Ds, jt, V, g, c), jt);
-#pragma unroll
-        for (int kt = 0; kt < KT; ++kt)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) O[kt] = mfma_f32(U[kt][i], P[i], O[kt]);
-      }
-      store_own_f32<DK>(dkr, r0, dkat, g, O);
-    }
+        for (int i = 0; i < 4; ++i) acc = mfma_f32(Gt[(16 * j + 4 * g + i) * LK + 16 * kt + c], V[j][i], acc);
+      return acc * weights.reach;
+    }, [&](int jt) { return weights(products_f32<DV>(Ds, jt, V, g, c), jt); });
     request_own(r0 + kChunk);
     const float keep = decay_pow(l2, rows);
 #pragma unroll
@@ -622,6 +631,58 @@ __device__ __forceinline__ void put_weights(uint32_t stage, int lane, const Walk
   lds_write(stage + 4 * lane, a.gain * decay_pow(l2, max(behind - lane, 0) + (a.reverse ? 1 : 0)));
   own_lds();
 }
+// The output of a wave's 16 own rows into its own LDS: tile by tile what the state gives (`inter`) and the weights P times the chunk's rows.
+// A weight that is masked is a zero, and in a product of matrices a zero times what is not a number or not finite is not a number: rows that come later would reach back.  So results that
+// are not finite are formed again, with such values left out; where none of a row's own reach is among them, that is the result.
+template <int D, typename Inter>
+__device__ __forceinline__ void weighted_rows(uint32_t lds, uint32_t rows, uint32_t pair, const bf16x8 (&P)[2], int t, int g, int c, Inter inter) {
+  const ColumnOperand<D, false> columns(lds, g, c);
+  float probe = 0.f;
+  {
+    f32x4 O[2];
+#pragma unroll
+    for (int ct = 0; ct < D / 16; ++ct) {
+      f32x4 acc = inter(ct);
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(columns(rows, 32 * jj, ct), P[jj], acc);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) probe = fmaf(acc[i], 0.f, probe);   // not a number if one is not finite
+      O[ct & 1] = acc;
+      if (ct & 1) lds_write(pair ^ 32 * (ct - 1), pack_pair(O[0], O[1]));
+    }
+  }
+  if (!__any(!(probe == 0.f))) return;
+  bf16x8 reach[2];   // one for the rows that a row has weights for
+#pragma unroll
+  for (int jj = 0; jj < 2; ++jj)
+#pragma unroll
+    for (int q = 0; q < 8; ++q) reach[jj][q] = 32 * jj + 4 * g + (q < 4 ? q : 12 + q) <= 16 * t + c ? (__bf16)1.f : (__bf16)0.f;
+#pragma unroll 1
+  for (int ct0 = 0; ct0 < D / 16; ct0 += 2) {
+    f32x4 O[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      f32x4 all = inter(ct0 + e), finite = all, met = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int jj = 0; jj < 2; ++jj) {
+        const bf16x8 v = columns(rows, 32 * jj, ct0 + e);
+        u32x4 clean = __builtin_bit_cast(u32x4, v), ones;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const bool lo = (clean[i] & 0x7f80u) == 0x7f80u, hi = (clean[i] & 0x7f800000u) == 0x7f800000u;
+          ones[i] = (lo ? 0x3f80u : 0u) | (hi ? 0x3f800000u : 0u);
+          clean[i] &= (lo ? 0u : 0xffffu) | (hi ? 0u : 0xffff0000u);
+        }
+        all = mfma_bf16(v, P[jj], all);
+        finite = mfma_bf16(__builtin_bit_cast(bf16x8, clean), P[jj], finite);
+        met = mfma_bf16(__builtin_bit_cast(bf16x8, ones), reach[jj], met);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) O[e][i] = met[i] > 0.f ? all[i] : finite[i];
+    }
+    lds_write(pair ^ 32 * ct0, pack_pair(O[0], O[1]));
+  }
+}
 // S <- keep S + (K o weight)^T V over the chunk's rows in LDS: RT row tiles of the wave (`row0` elements into a row, part of `keys`), all column tiles.
 // weight: the wave's own table of the chunk's rows.  SUM: keep is 1.
 template <int DK, int DV, bool SUM>
@@ -728,21 +789,13 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
       if (!STATES) {
         bf16x8 P[2];
         weights.products<DK>(lds, Ks, Q, g, c, P);
-        const uint32_t pair = pair_at<DV>(stage, g, c);
         const RowOperand<DK, false> state(lds, g, c);
-        const ColumnOperand<DV, false> values(lds, g, c);
-        f32x4 O[2];
-#pragma unroll
-        for (int ct = 0; ct < CT; ++ct) {
+        weighted_rows<DV>(lds, Vs, pair_at<DV>(stage, g, c), P, w, g, c, [&](int ct) {
           f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int j = 0; j < QJ; ++j) acc = mfma_bf16(state(St, ct, j), Q[j], acc);
-          acc *= weights.reach;
-#pragma unroll
-          for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(values(Vs, 32 * jj, ct), P[jj], acc);
-          O[ct & 1] = acc;
-          if (ct & 1) lds_write(pair ^ 32 * (ct - 1), pack_pair(O[0], O[1]));
-        }
+          return acc * weights.reach;
+        });
         oo.out(orow, r0);
         qo.pieces.template load<false>(qr, r0 + kChunk, rq);
       }
@@ -763,7 +816,7 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
 template <int DK, int DV, bool FULL>
 __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;
-  constexpr int KT = DK / 16, CT = DV / 16, KJ = DK / 32, VJ = DV / 32, STAGE = 32 * (DK > DV ? DK : DV);
+  constexpr int CT = DV / 16, KJ = DK / 32, VJ = DV / 32, STAGE = 32 * (DK > DV ? DK : DV);
   extern __shared__ __align__(16) unsigned char lds_bytes[];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes;
   constexpr uint32_t Qs = 0, Ds = 2 * kChunk * DK, Gt = Ds + 2 * kChunk * DV;
@@ -810,42 +863,27 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
     vo.operands(rv, stage, g, c, V);
     __syncthreads();
     request(r0 + kChunk);
-    f32x4 O[2];
     bf16x8 P[2];
     weights.products<DK>(lds, Qs, K, g, c, P);
     {
-      const uint32_t pair = pair_at<DV>(stage, g, c);
       const RowOperand<DK, true> state(lds, g, c);
-      const ColumnOperand<DV, false> douts(lds, g, c);
-#pragma unroll
-      for (int ct = 0; ct < CT; ++ct) {
+      weighted_rows<DV>(lds, Ds, pair_at<DV>(stage, g, c), P, w, g, c, [&](int ct) {
         f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < KJ; ++j) acc = mfma_bf16(state(Gt, ct, j), K[j], acc);
-        acc *= weights.reach;
-#pragma unroll
-        for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(douts(Ds, 32 * jj, ct), P[jj], acc);
-        O[ct & 1] = acc;
-        if (ct & 1) lds_write(pair ^ 32 * (ct - 1), pack_pair(O[0], O[1]));
-      }
+        return acc * weights.reach;
+      });
       dvo.out(dvr, r0);
     }
     weights.products<DV>(lds, Ds, V, g, c, P);
     {
-      const uint32_t pair = pair_at<DK>(stage, g, c);
       const ColumnOperand<DK, true> state(lds, g, c);
-      const ColumnOperand<DK, false> queries(lds, g, c);
-#pragma unroll
-      for (int kt = 0; kt < KT; ++kt) {
+      weighted_rows<DK>(lds, Qs, pair_at<DK>(stage, g, c), P, w, g, c, [&](int kt) {
         f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < VJ; ++j) acc = mfma_bf16(state(Gt, 32 * j, kt), V[j], acc);
-        acc *= weights.reach;
-#pragma unroll
-        for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(queries(Qs, 32 * jj, kt), P[jj], acc);
-        O[kt & 1] = acc;
-        if (kt & 1) lds_write(pair ^ 32 * (kt - 1), pack_pair(O[0], O[1]));
-      }
+        return acc * weights.reach;
+      });
       dko.out(dkr, r0);
     }
     request_own(r0 + kChunk);
@@ -909,25 +947,30 @@ template <typename T, int W>
 __global__ __launch_bounds__(256) void step_kernel(Step a) {
   constexpr int TPR = W / 4, ROWS = 256 / TPR, PASS = (128 + ROWS - 1) / ROWS;
   const int h = blockIdx.y, b = blockIdx.z, tid = threadIdx.x, col = blockIdx.x * W + tid % TPR * 4, r0 = tid / TPR;
+  __shared__ float key[128], query[128];
   __shared__ f32x4 part[4][TPR];
   const int own0 = a.cache ? a.cache[b] : b, own = own0 < 0 || own0 >= a.cache_rows ? -1 : own0;
   const T *q = (const T *)a.q + b * a.sq.b + h * a.sq.h, *k = (const T *)a.k + b * a.sk.b + h * a.sk.h, *v = (const T *)a.v + b * a.sv.b + h * a.sv.h;
   T *o = (T *)a.o + b * a.so.b + h * a.so.h;
-  f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (own >= 0 && col < a.vw) {
-    float *s = a.state + ((int64_t)own * a.H + h) * a.kw * a.vw + col;
-    f32x4 x[PASS];
-#pragma unroll
-    for (int u = 0; u < PASS; ++u)
-      if (r0 + u * ROWS < a.kw) x[u] = *(const f32x4 *)(s + (r0 + u * ROWS) * a.vw);
-    const float lambda = decay_pow(log2_decay(a.log_decay, h), 1);
-    f32x4 vv;
+  const bool there = own >= 0 && col < a.vw;
+  const float mine = tid % 128 < a.kw ? ld((tid < 128 ? k : q) + tid % 128) : 0.f;
+  f32x4 vv = f32x4{0.f, 0.f, 0.f, 0.f}, sum = vv, x[PASS];
+  float *s = a.state + ((int64_t)own * a.H + h) * a.kw * a.vw + col;
+  if (there) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) vv[i] = ld(v + col + i);
 #pragma unroll
     for (int u = 0; u < PASS; ++u)
+      if (r0 + u * ROWS < a.kw) x[u] = *(const f32x4 *)(s + (r0 + u * ROWS) * a.vw);
+  }
+  (tid < 128 ? key : query)[tid % 128] = mine;
+  const float lambda = decay_pow(log2_decay(a.log_decay, h), 1);
+  __syncthreads();
+  if (there) {
+#pragma unroll
+    for (int u = 0; u < PASS; ++u)
       if (r0 + u * ROWS < a.kw) {
-        const float kk = ld(k + r0 + u * ROWS), qq = ld(q + r0 + u * ROWS);
+        const float kk = key[r0 + u * ROWS], qq = query[r0 + u * ROWS];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           x[u][i] = x[u][i] * lambda + kk * vv[i];
@@ -950,13 +993,14 @@ __global__ __launch_bounds__(256) void step_kernel(Step a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-// Rows of a segment.  Segments are as many as the device holds workgroups at a time, three to a compute unit at widths up to 64 in bf16, else two: a walk over more
+// Rows of a segment.  Segments are as many as the device holds workgroups at a time, three to a compute unit at widths up to 64 in bf16 and 32 in float32, else two: a walk over more
 // of them has a last round that is partly idle (32 slices of 65536 rows, width 128, 768 instead of 512: walk 615 us, 519 with 512).  Packed sequences have a
 // partial segment each on top, and three quarters as many whole ones (24 prompts, 16 heads, 65536 rows: 476 us in all, 507 without this).  Two chunks at least: 8 slices
 // of 1000 rows 22 us with segments of one, two or four chunks, 32 with eight or in one launch.
 int segment_rows(const wersa_decay_desc &c) {
   const int64_t slices = (int64_t)c.H * (c.packed ? 1 : c.B);
-  const int64_t held = c.dtype == WERSA_BF16 && c.dk <= 64 && c.dv <= 64 ? 768 : 512;
+  const int narrow = c.dtype == WERSA_BF16 ? 64 : 32;
+  const int64_t held = c.dk <= narrow && c.dv <= narrow ? 768 : 512;
   const int64_t want = (c.packed ? held * 3 / 4 : held) / slices;   // segments of a slice
   if (want <= 1) return c.packed ? INT32_MAX / 2 : (c.n + kChunk - 1) / kChunk * kChunk + kChunk;
   int64_t rows = ((int64_t)c.n + want - 1) / want;

@@ -360,3 +360,38 @@ def test_autograd(dtype):
     out, final = autograd.wersa_decay_attention(q, k, v1.expand(B, H, n, d), g["ld"], scale=0.1)
     dq, dk = torch.autograd.grad(final, (q, k), g["dfinal"])
     assert (dq == 0).all() and torch.isfinite(dk).all() and (dk != 0).any()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n,dk,dv", [(60, 32, 32), (130, 64, 64), (150, 128, 128), (130, 48, 112), (700, 64, 64)])
+def test_what_is_not_finite_stays_on_its_side_of_the_mask(n, dk, dv, dtype):
+    """Keys and values that are not numbers or not finite in later rows, queries and gradients in earlier ones: rows that do not reach them are as without them."""
+    from paper_2507_08637_amd import binding
+    p = to(make(1, 2, n, dk, dv, dtype, seed=6, grads=True))
+    def run():
+        out, final, saved = binding.wersa_decay_forward(p["q"], p["k"], p["v"], p["ld"], want_state=True, want_saved=True)
+        g = binding.wersa_decay_backward(p["q"], p["k"], p["v"], p["ld"], p["dout"], saved, dfinal_state=p["dfinal"], want_dinitial=True)
+        return dict(out=out, **{x: g[x] for x in ("dq", "dk", "dv")})
+    cut = n - 37
+    clean = {x: p[x].clone() for x in ("q", "k", "v", "dout")}
+    for x, bad in (("v", float("nan")), ("v", float("inf")), ("k", float("inf")), ("k", float("nan"))):
+        p.update({x: t.clone() for x, t in clean.items()})
+        p[x][:, :, cut + 3] = 0
+        want = run()
+        p[x][:, :, cut + 3] = bad
+        got = run()
+        rows = slice(0, cut + 3)
+        assert torch.equal(got["out"][:, :, rows], want["out"][:, :, rows]), (x, bad)
+        assert torch.equal(got["dq"][:, :, rows], want["dq"][:, :, rows]), (x, bad)
+        if x == "v":
+            assert not torch.isfinite(got["out"][:, :, cut + 3]).any()
+    for x, bad in (("dout", float("nan")), ("dout", -float("inf")), ("q", float("nan")), ("q", float("inf"))):
+        p.update({x: t.clone() for x, t in clean.items()})
+        p[x][:, :, 21] = 0
+        want = run()
+        p[x][:, :, 21] = bad
+        got = run()
+        for name in ("dk", "dv"):
+            assert torch.equal(got[name][:, :, 22:], want[name][:, :, 22:]), (x, bad, name)
+        if x == "dout":
+            assert not torch.isfinite(got["dv"][:, :, 21]).any()
