@@ -638,19 +638,21 @@ template <int D, typename Inter>
 __device__ __forceinline__ void weighted_rows(uint32_t lds, uint32_t rows, uint32_t pair, const bf16x8 (&P)[2], int t, int g, int c, Inter inter) {
   const ColumnOperand<D, false> columns(lds, g, c);
   float probe = 0.f;
-  {
+  auto tiles = [&](auto halves) {   // of the chunk's rows: the first 32 rows have no weights for the others
     f32x4 O[2];
 #pragma unroll
     for (int ct = 0; ct < D / 16; ++ct) {
       f32x4 acc = inter(ct);
 #pragma unroll
-      for (int jj = 0; jj < 2; ++jj) acc = mfma_bf16(columns(rows, 32 * jj, ct), P[jj], acc);
+      for (int jj = 0; jj < decltype(halves)::value; ++jj) acc = mfma_bf16(columns(rows, 32 * jj, ct), P[jj], acc);
 #pragma unroll
       for (int i = 0; i < 4; ++i) probe = fmaf(acc[i], 0.f, probe);   // not a number if one is not finite
       O[ct & 1] = acc;
       if (ct & 1) lds_write(pair ^ 32 * (ct - 1), pack_pair(O[0], O[1]));
     }
-  }
+  };
+  if (t < 2) tiles(std::integral_constant<int, 1>{});
+  else tiles(std::integral_constant<int, 2>{});
   if (!__any(!(probe == 0.f))) return;
   bf16x8 reach[2];   // one for the rows that a row has weights for
 #pragma unroll
@@ -742,7 +744,7 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
   const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
-  const int row0 = DK / 4 * w;   // of the wave's rows of the state
+  const int t = (w + blockIdx.x + blockIdx.y) & 3, row0 = DK / 4 * w;   // rows 16 t .. of the chunk (see Part), rows row0 .. of the state
   const uint32_t stage = lds + SETS * SET + (STATES ? 0 : 2 * DV * DK) + STAGE * w;
   const bool last = a.reverse ? seg.s == 0 : seg.s == a.seq.segments(seg.b) - 1;
   if (STATES && last) return;
@@ -756,13 +758,13 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
   const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
   each_of_state<DK, DV>(a, S, row0, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
-  const Weights weights(a, l2, w, g, c);
+  const Weights weights(a, l2, t, g, c);
 
   u32x4 rk[SETS][PK], rv[SETS][PV], rq[QJ];
   const TilePieces<DK, 8, PK, 256, FULL> kp(kr, 0, tid);
   const TilePieces<DV, 8, PV, 256, FULL> vp(vr, 0, tid);
-  const OwnRows<DK, FULL> qo(qr, stage, w, lane);
-  const OwnRows<DV, FULL> oo(orow, stage, w, lane);
+  const OwnRows<DK, FULL> qo(qr, stage, t, lane);
+  const OwnRows<DV, FULL> oo(orow, stage, t, lane);
   const uint32_t kput = lds + Ks + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), vput = lds + Vs + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
   auto request = [&](int r0, int set) {
     kp.template load<STATES>(kr, r0, rk[set]);
@@ -790,7 +792,7 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
         bf16x8 P[2];
         weights.products<DK>(lds, Ks, Q, g, c, P);
         const RowOperand<DK, false> state(lds, g, c);
-        weighted_rows<DV>(lds, Vs, pair_at<DV>(stage, g, c), P, w, g, c, [&](int ct) {
+        weighted_rows<DV>(lds, Vs, pair_at<DV>(stage, g, c), P, t, g, c, [&](int ct) {
           f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int j = 0; j < QJ; ++j) acc = mfma_bf16(state(St, ct, j), Q[j], acc);
@@ -823,7 +825,7 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
   const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
-  const int row0 = DK / 4 * w;
+  const int t = (w + blockIdx.x + blockIdx.y) & 3, row0 = DK / 4 * w;
   const uint32_t stage = lds + Gt + 2 * DV * DK + STAGE * w;
   const Rows qr = rows_of(a.k, a.sk, seg, a, h, a.kw, 2), dr = rows_of(a.v, a.sv, seg, a, h, a.vw, 2), kr = rows_of(b.k, b.sk, seg, a, h, a.kw, 2),
              vr = rows_of(b.v, b.sv, seg, a, h, a.vw, 2), dkr = rows_of(b.dk, b.sk, seg, a, h, a.kw, 2), dvr = rows_of(b.dv, b.sv, seg, a, h, a.vw, 2);
@@ -834,13 +836,13 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : seg.b;
   const float *init = a.init ? a.init + (from * a.H + h) * state_size : nullptr;
   each_of_state<DK, DV>(a, G, row0, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
-  const Weights weights(a, l2, w, g, c);
+  const Weights weights(a, l2, t, g, c);
 
   u32x4 rq[PK], rd[PV], rk[KJ], rv[VJ];
   const TilePieces<DK, 8, PK, 256, FULL> qp(qr, 0, tid);
   const TilePieces<DV, 8, PV, 256, FULL> dp(dr, 0, tid);
-  const OwnRows<DK, FULL> ko(kr, stage, w, lane), dko(dkr, stage, w, lane);
-  const OwnRows<DV, FULL> vo(vr, stage, w, lane), dvo(dvr, stage, w, lane);
+  const OwnRows<DK, FULL> ko(kr, stage, t, lane), dko(dkr, stage, t, lane);
+  const OwnRows<DV, FULL> vo(vr, stage, t, lane), dvo(dvr, stage, t, lane);
   const uint32_t qput = lds + Qs + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), dput = lds + Ds + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
   auto request = [&](int r0) {
     qp.template load<false>(qr, r0, rq);
@@ -867,7 +869,7 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
     weights.products<DK>(lds, Qs, K, g, c, P);
     {
       const RowOperand<DK, true> state(lds, g, c);
-      weighted_rows<DV>(lds, Ds, pair_at<DV>(stage, g, c), P, w, g, c, [&](int ct) {
+      weighted_rows<DV>(lds, Ds, pair_at<DV>(stage, g, c), P, t, g, c, [&](int ct) {
         f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < KJ; ++j) acc = mfma_bf16(state(Gt, ct, j), K[j], acc);
@@ -878,7 +880,7 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
     weights.products<DV>(lds, Ds, V, g, c, P);
     {
       const ColumnOperand<DK, true> state(lds, g, c);
-      weighted_rows<DK>(lds, Qs, pair_at<DK>(stage, g, c), P, w, g, c, [&](int kt) {
+      weighted_rows<DK>(lds, Qs, pair_at<DK>(stage, g, c), P, t, g, c, [&](int kt) {
         f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < VJ; ++j) acc = mfma_bf16(state(Gt, 32 * j, kt), V[j], acc);
