@@ -27,7 +27,7 @@ _node = None   # (False: it does not load)
 
 
 def _load_node():
-    """The extension that holds the attention core's node of the autograd graph (csrc/wersa_torch.cpp), on the library that the
+    """The extension that holds the operators' nodes of the autograd graph (csrc/wersa_torch.cpp), on the library that the
     binding has loaded.  It is bound to one version of torch where the library is not: without it the node in Python makes the same
     calls, and a warning says that its host path is the slower one."""
     global _node
@@ -42,6 +42,9 @@ def _load_node():
             return _node
         node.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.wersa_forward, lib.wersa_backward, lib.wersa_workspace_bytes,
                                                                     lib.wersa_saved_bytes, lib.wersa_selected_path)))
+        node.bind_causal([ctypes.cast(f, ctypes.c_void_p).value for f in (
+            lib.wersa_decay_forward, lib.wersa_decay_backward, lib.wersa_decay_workspace_bytes, lib.wersa_decay_saved_bytes,
+            lib.wersa_rms_norm_forward, lib.wersa_rms_norm_backward, lib.wersa_rms_norm_workspace_bytes)])
         _node = node
     return _node
 
@@ -132,7 +135,12 @@ def _rows_apart(x):
 
 def wersa_decay_attention(q, k, v, log_decay, scale=None, initial_state=None, offsets=None):
     """Causal linear attention with a decay for each head.  Returns (out, final states (B, H, dk, dv) in float32)."""
-    return _DecayAttention.apply(_rows_apart(q), _rows_apart(k), _rows_apart(v), log_decay, scale, initial_state, offsets)
+    q, k, v = _rows_apart(q), _rows_apart(k), _rows_apart(v)
+    node = _load_node() if _node is None else _node
+    if not node or torch.jit.is_tracing():
+        return _DecayAttention.apply(q, k, v, log_decay, scale, initial_state, offsets)
+    desc, saved_bytes = binding.checked_decay_desc(q, k, v, log_decay, scale, offsets, initial_state)
+    return tuple(node.decay_attention(q, k, v, log_decay, initial_state, offsets, bytes(desc), saved_bytes))
 
 
 class _RmsNorm(torch.autograd.Function):
@@ -157,8 +165,16 @@ class _RmsNorm(torch.autograd.Function):
 def wersa_rms_norm(x, weight=None, residual=None, eps=1e-6):
     """RMS norm over the last dimension: y, or (y, x + residual)."""
     shape = x.shape
-    x = x.reshape(-1, shape[-1])
-    if residual is None:
-        return _RmsNorm.apply(x, weight, None, eps).view(shape)
-    y, r = _RmsNorm.apply(x, weight, residual.reshape(-1, shape[-1]), eps)
-    return y.view(shape), r.view(shape)
+    if len(shape) != 2:
+        x = x.reshape(-1, shape[-1])
+        residual = None if residual is None else residual.reshape(-1, shape[-1])
+    node = _load_node() if _node is None else _node
+    if not node or torch.jit.is_tracing():
+        outs = _RmsNorm.apply(x, weight, residual, eps)
+        outs = (outs,) if residual is None else outs
+    else:
+        binding.checked_norm_args(x, weight, residual)
+        outs = node.rms_norm(x, weight, residual, eps)
+    if len(shape) != 2:
+        outs = [t.view(shape) for t in outs]
+    return outs[0] if residual is None else tuple(outs)

@@ -517,6 +517,17 @@ def _check_log_decay(log_decay, desc):
     assert log_decay.dtype == torch.float32 and log_decay.is_contiguous() and log_decay.numel() == desc.H, "log_decay: float32, one per head"
 
 
+def checked_decay_desc(q, k, v, log_decay, scale, offsets, initial_state):
+    """(descriptor, bytes of saved) of a forward call whose output is laid out like v; the arguments are checked."""
+    desc = make_decay_desc(q, k, v, v, scale, offsets)
+    _check_log_decay(log_decay, desc)
+    _check_states(desc, None, initial_state)
+    sb = load_library().wersa_decay_saved_bytes(ctypes.byref(desc))
+    if sb == 0:   # the precise status
+        _check(load_library().wersa_decay_forward(ctypes.byref(desc), *([None] * 8), 0, *([None] * 3), 0, None))
+    return desc, sb
+
+
 def wersa_decay_forward(q, k, v, log_decay, scale=None, offsets=None, initial_state=None, final_state=None, slots=None, out=None,
                         want_state=False, want_saved=False, saved=None, workspace=None, stream=None):
     """Returns (out, final_state, saved).  final_state: a buffer to write, or want_state=True for a new one (else None);
@@ -592,15 +603,22 @@ def wersa_decay_step(q, k, v, log_decay, state, scale=None, slots=None, out=None
 _NORM_DESC = struct.Struct("qiif4xqq")
 
 
-def _norm_args(x, weight, residual, eps, r):
-    """(rows, cols) tensors, columns contiguous; returns the descriptor and the stream's buffer (None without a residual)."""
+def checked_norm_args(x, weight, residual):
+    """(rows, cols) tensors, columns contiguous."""
     assert x.dim() == 2 and x.stride(1) == 1, "expect (rows, cols) with contiguous columns"
-    rows, cols = x.shape
     if weight is not None:
-        assert weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == cols, "weight: float32, one per column"
-    step = cols
+        assert weight.dtype == torch.float32 and weight.is_contiguous() and weight.numel() == x.shape[1], "weight: float32, one per column"
     if residual is not None:
         assert residual.shape == x.shape and residual.dtype == x.dtype and residual.stride(1) == 1, "the residual has x's shape and dtype"
+    _dtype_code(x)
+
+
+def _norm_args(x, weight, residual, eps, r):
+    """Returns the descriptor and the stream's buffer (None without a residual)."""
+    checked_norm_args(x, weight, residual)
+    rows, cols = x.shape
+    step = cols
+    if residual is not None:
         step = residual.stride(0)
         if r is None:
             r = x.new_empty((rows, cols))

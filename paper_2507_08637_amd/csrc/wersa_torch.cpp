@@ -1,4 +1,4 @@
-// The attention core as a node of torch's autograd graph, in C++: what a training step pays for on the host beyond the launches.  The engine runs
+// The attention core, and the causal operators, as nodes of torch's autograd graph, in C++: what a training step pays for on the host beyond the launches.  The engine runs
 // a backward on a thread of its own, and interpreter state, reference counts and runtime structures that both threads touch move between their
 // caches at every change.  2 x 4 slices of 1000 tokens, d 64, m 256, bf16, forward and backward: 235 to 246 us where the engine's thread runs far from
 // the caller's and 128 to 136 where near with a node written in Python, 128 to 138 and 98 with this one; its kernels take 97.
@@ -132,6 +132,134 @@ Tensor attention(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor
   return Attention::apply(q, k, v, omega, sigma, gate_w, gate_b, scale_w, d, saved_bytes, workspace);
 }
 
+// ---- the causal operators ------------------------------------------------------------------------------
+// Decay attention and the RMS norm, whose kernels for some thousand tokens take less than the host's part of a step.  128000 rows of 128, float32, forward and backward of the norm: 95 us
+// with a node in Python where the engine's thread runs near the caller's, 175 where it runs far; its kernels take 97.
+decltype(&wersa_decay_forward) decay_forward_fn = nullptr;
+decltype(&wersa_decay_backward) decay_backward_fn = nullptr;
+decltype(&wersa_decay_workspace_bytes) decay_workspace_bytes_fn = nullptr;
+decltype(&wersa_decay_saved_bytes) decay_saved_bytes_fn = nullptr;
+decltype(&wersa_rms_norm_forward) norm_forward_fn = nullptr;
+decltype(&wersa_rms_norm_backward) norm_backward_fn = nullptr;
+decltype(&wersa_rms_norm_workspace_bytes) norm_workspace_bytes_fn = nullptr;
+
+Tensor or_none(const std::optional<Tensor> &t) { return t ? *t : Tensor(); }
+const void *in(const Tensor &t) { return t.defined() ? t.const_data_ptr() : nullptr; }
+void *out_of(const Tensor &t) { return t.defined() ? t.mutable_data_ptr() : nullptr; }
+int32_t dtype_of(const Tensor &t) { return t.scalar_type() == at::kFloat ? WERSA_F32 : t.scalar_type() == at::kBFloat16 ? WERSA_BF16 : -1; }
+// A backward runs with gradients enabled where a graph of it is wanted: there is none of what the kernels do.
+void once() { TORCH_CHECK(!at::GradMode::is_enabled(), "the causal operators are differentiable once"); }
+
+// Rows with contiguous columns that do not share memory.
+bool rows_apart(const Tensor &t) {
+  return t.stride(3) == 1 && (t.stride(0) > 0 || t.size(0) == 1) && (t.stride(1) > 0 || t.size(1) == 1) && (t.stride(2) >= t.size(3) || t.size(2) <= 1);
+}
+void put_strides(int64_t *to, const Tensor &t) {
+  for (int i = 0; i < 3; ++i) to[i] = t.stride(i);
+}
+
+struct DecayAttention : torch::autograd::Function<DecayAttention> {
+  static variable_list forward(AutogradContext *ctx, const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &log_decay, const std::optional<Tensor> &initial_state,
+                               const std::optional<Tensor> &sequences, const std::string &desc, int64_t saved_bytes) {
+    const Tensor initial = or_none(initial_state), offsets = or_none(sequences);
+    wersa_decay_desc d;
+    TORCH_CHECK(desc.size() == sizeof(d), "descriptor of another size");
+    std::memcpy(&d, desc.data(), sizeof(d));
+    const Tensor out = at::empty_strided(v.sizes(), v.strides(), v.options());
+    const auto f32 = q.options().dtype(at::kFloat);
+    const Tensor final_state = at::empty({d.B, d.H, d.dk, d.dv}, f32), saved = at::empty({saved_bytes / 4}, f32);
+    check(decay_forward_fn(&d, in(q), in(k), in(v), floats(log_decay), (const int32_t *)in(offsets), (const float *)in(initial), floats_out(final_state), nullptr,
+                           d.B, out.mutable_data_ptr(), saved.mutable_data_ptr(), nullptr, 0, stream(q)));
+    ctx->save_for_backward({q, k, v, log_decay, initial, offsets, saved});
+    ctx->saved_data["desc"] = desc;
+    ctx->set_materialize_grads(false);
+    return {out, final_state};
+  }
+
+  // As above, the call is described by the tensors that are there now.  `saved` does not depend on their strides.
+  static variable_list backward(AutogradContext *ctx, const variable_list &grads) {
+    once();
+    const variable_list t = ctx->get_saved_variables();
+    const Tensor &q = t[0], &k = t[1], &v = t[2], &log_decay = t[3], &initial = t[4], &offsets = t[5], &saved = t[6];
+    wersa_decay_desc d;
+    std::memcpy(&d, ctx->saved_data["desc"].toStringRef().data(), sizeof(d));
+    const int64_t N = d.packed ? 1 : d.B;
+    for (const Tensor *x : {&q, &k, &v})
+      require(x->dim() == 4 && x->sizes() == at::IntArrayRef({N, d.H, d.n, x == &v ? d.dv : d.dk}) && dtype_of(*x) == d.dtype && rows_apart(*x),
+              "expect q, k and v as they were saved: (B, H, n, d) with contiguous last dim");
+    auto states = [&](const Tensor &x) { return !x.defined() || (holds_floats(x, (int64_t)d.B * d.H * d.dk * d.dv)); };
+    require(holds_floats(log_decay, d.H) && states(initial) && holds_floats(saved, (int64_t)decay_saved_bytes_fn(&d) / 4) &&
+                (offsets.defined() ? d.packed && offsets.scalar_type() == at::kInt && offsets.is_contiguous() && offsets.numel() == d.B + 1 : !d.packed),
+            "expect log_decay, the states and the offsets as they were saved");
+    Tensor dout = grads[0], dfinal = grads[1];
+    if (!dout.defined()) dout = at::zeros(v.sizes(), v.options());
+    if (!rows_apart(dout)) dout = dout.contiguous();
+    if (dfinal.defined()) dfinal = dfinal.contiguous();
+    require(dout.sizes() == v.sizes() && dout.dtype() == v.dtype() && states(dfinal), "gradients of other shapes or types than the outputs");
+    for (const Tensor &x : t) require(!x.defined() || x.device() == dout.device(), "saved tensors on another device");
+    put_strides(d.stride_q, q);
+    put_strides(d.stride_k, k);
+    put_strides(d.stride_v, v);
+    put_strides(d.stride_o, dout);
+    auto like = [](const Tensor &x) { return at::empty_strided(x.sizes(), x.strides(), x.options()); };
+    const Tensor dq = like(q), dk = like(k), dv = like(v), dinitial = initial.defined() && ctx->needs_input_grad(4) ? at::empty_like(initial) : Tensor();
+    const Tensor ws = scratch((int64_t)decay_workspace_bytes_fn(&d, 1), q);
+    check(decay_backward_fn(&d, in(q), in(k), in(v), floats(log_decay), (const int32_t *)in(offsets), (const float *)in(initial), in(dout),
+                            (const float *)in(dfinal), saved.const_data_ptr(), out_of(dq), out_of(dk), out_of(dv), (float *)out_of(dinitial),
+                            ws.mutable_data_ptr(), ws.nbytes(), stream(q)));
+    return {dq, dk, dv, Tensor(), dinitial, Tensor(), Tensor(), Tensor()};
+  }
+};
+
+struct RmsNorm : torch::autograd::Function<RmsNorm> {
+  static variable_list forward(AutogradContext *ctx, const Tensor &x, const std::optional<Tensor> &weights, const std::optional<Tensor> &added, double eps) {
+    const Tensor weight = or_none(weights), residual = or_none(added);
+    const int64_t rows = x.size(0), cols = x.size(1);
+    const wersa_norm_desc d{rows, (int32_t)cols, dtype_of(x), (float)eps, x.stride(0), residual.defined() ? residual.stride(0) : cols};
+    const Tensor y = at::empty({rows, cols}, x.options()), r = residual.defined() ? at::empty({rows, cols}, x.options()) : Tensor(),
+                 rstd = at::empty({rows}, x.options().dtype(at::kFloat));
+    check(norm_forward_fn(&d, in(x), in(residual), (const float *)in(weight), out_of(r), out_of(y), floats_out(rstd), stream(x)));
+    ctx->save_for_backward({r.defined() ? r : x, weight, rstd});
+    ctx->set_materialize_grads(false);
+    return r.defined() ? variable_list{y, r} : variable_list{y};
+  }
+
+  static variable_list backward(AutogradContext *ctx, const variable_list &grads) {
+    once();
+    const variable_list t = ctx->get_saved_variables();
+    const Tensor &r = t[0], &weight = t[1], &rstd = t[2];
+    require(r.dim() == 2 && r.stride(1) == 1 && dtype_of(r) >= 0 && (r.size(0) <= 1 || r.stride(0) >= r.size(1)) && holds_floats(rstd, r.size(0)) &&
+                (!weight.defined() || holds_floats(weight, r.size(1))),
+            "expect the stream, the weight and the statistics as they were saved");
+    const int64_t rows = r.size(0), cols = r.size(1);
+    const Tensor dy = grads[0].defined() ? grads[0].contiguous() : at::zeros({rows, cols}, r.options());
+    const Tensor dr = grads.size() > 1 && grads[1].defined() ? grads[1].contiguous() : Tensor();
+    for (const Tensor *x : {&dy, &dr})
+      require(!x->defined() || (x->sizes() == r.sizes() && x->dtype() == r.dtype()), "gradients of other shapes or types than the outputs");
+    for (const Tensor &x : t) require(!x.defined() || x.device() == dy.device(), "saved tensors on another device");
+    const wersa_norm_desc d{rows, (int32_t)cols, dtype_of(r), 0.f, r.stride(0), cols};
+    const bool wants = weight.defined() && ctx->needs_input_grad(1);
+    const Tensor dx = at::empty({rows, cols}, r.options()), dw = wants ? at::empty_like(weight) : Tensor(),
+                 ws = wants ? scratch((int64_t)norm_workspace_bytes_fn(&d), r) : Tensor();
+    check(norm_backward_fn(&d, in(r), (const float *)in(weight), floats(rstd), in(dy), in(dr), out_of(dx), (float *)out_of(dw), out_of(ws),
+                           wants ? ws.nbytes() : 0, stream(r)));
+    // (gradients are asked for by the tensors that there are)
+    return {dx, dw, grads.size() > 1 && ctx->needs_input_grad(weight.defined() ? 2 : 1) ? dx : Tensor(), Tensor()};
+  }
+};
+
+variable_list decay_attention(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &log_decay, const std::optional<Tensor> &initial,
+                              const std::optional<Tensor> &offsets, const pybind11::bytes &desc, int64_t saved_bytes) {
+  const std::string d = desc;
+  pybind11::gil_scoped_release nogil;
+  return DecayAttention::apply(q, k, v, log_decay, initial, offsets, d, saved_bytes);
+}
+
+variable_list rms_norm(const Tensor &x, const std::optional<Tensor> &weight, const std::optional<Tensor> &residual, double eps) {
+  pybind11::gil_scoped_release nogil;
+  return RmsNorm::apply(x, weight, residual, eps);
+}
+
 }  // namespace
 
 PYBIND11_MODULE(_wersa_torch, m) {
@@ -143,4 +271,16 @@ PYBIND11_MODULE(_wersa_torch, m) {
     selected_path_fn = reinterpret_cast<decltype(selected_path_fn)>(selected_path);
   });
   m.def("attention", &attention);
+  m.def("bind_causal", [](const std::vector<uintptr_t> &at) {
+    TORCH_CHECK(at.size() == 7, "seven entry points");
+    decay_forward_fn = reinterpret_cast<decltype(decay_forward_fn)>(at[0]);
+    decay_backward_fn = reinterpret_cast<decltype(decay_backward_fn)>(at[1]);
+    decay_workspace_bytes_fn = reinterpret_cast<decltype(decay_workspace_bytes_fn)>(at[2]);
+    decay_saved_bytes_fn = reinterpret_cast<decltype(decay_saved_bytes_fn)>(at[3]);
+    norm_forward_fn = reinterpret_cast<decltype(norm_forward_fn)>(at[4]);
+    norm_backward_fn = reinterpret_cast<decltype(norm_backward_fn)>(at[5]);
+    norm_workspace_bytes_fn = reinterpret_cast<decltype(norm_workspace_bytes_fn)>(at[6]);
+  });
+  m.def("decay_attention", &decay_attention);
+  m.def("rms_norm", &rms_norm);
 }
