@@ -191,7 +191,7 @@ template <int D, int PIECES> __device__ __forceinline__ void put_tile_f32(float 
   for (int i = 0; i < PIECES; ++i) *(u32x4 *)(rows + (tid / (D / 4) + 1024 / D * i) * (D + 4) + tid % (D / 4) * 4) = p[i];
 }
 template <int DK, int DV, typename F>
-__device__ __forceinline__ void each_of_state_f32(const Walk &a, f32x4 (&S)[Part<DK, DV>::RT][Part<DK, DV>::CW], const Part<DK, DV> &part, int g, int lane_c, F f) {
+__device__ __forceinline__ void each_of_state(const Walk &a, f32x4 (&S)[Part<DK, DV>::RT][Part<DK, DV>::CW], const Part<DK, DV> &part, int g, int lane_c, F f) {
   const int c = (int)opaque((uint32_t)lane_c);
 #pragma unroll
   for (int rt = 0; rt < Part<DK, DV>::RT; ++rt)
@@ -323,7 +323,7 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
   const int own = cache_row(a, seg.b);
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
   const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
-  each_of_state_f32<DK, DV>(a, S, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  each_of_state<DK, DV>(a, S, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const WeightsF32 weights(a, l2, part.t, g, c);
 
   u32x4 rk[PK], rv[PV];
@@ -376,7 +376,7 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
   float *fin = nullptr;
   if (STATES) fin = a.fin + ((int64_t)blockIdx.x * a.H + h) * state_size;
   else if (last && a.fin && own >= 0) fin = a.fin + ((int64_t)own * a.H + h) * state_size;
-  if (fin) each_of_state_f32<DK, DV>(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
+  if (fin) each_of_state<DK, DV>(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
 }
 
 // The two walks back of the derivative as one, k and v of `a` being q and dout: own rows of keys and values, G^T k and the weighted rows of dout give dv, G v and the
@@ -405,7 +405,7 @@ __global__ __launch_bounds__(256) void back_f32_kernel(Walk a, Back b) {
   f32x4 G[P4::RT][P4::CW];
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : seg.b;
   const float *init = a.init ? a.init + (from * a.H + h) * state_size : nullptr;
-  each_of_state_f32<DK, DV>(a, G, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  each_of_state<DK, DV>(a, G, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const WeightsF32 weights(a, l2, part.t, g, c);
 
   u32x4 rq[PK], rd[PV];
@@ -461,7 +461,7 @@ __global__ __launch_bounds__(256) void back_f32_kernel(Walk a, Back b) {
   }
   if (a.fin && seg.s == 0) {
     float *fin = a.fin + ((int64_t)seg.b * a.H + h) * state_size;
-    each_of_state_f32<DK, DV>(a, G, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
+    each_of_state<DK, DV>(a, G, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
   }
 }
 
@@ -490,6 +490,7 @@ __device__ __forceinline__ bf16x8 read_transposed(uint32_t lo, uint32_t hi) {
 template <int D, bool NATURAL> __device__ __forceinline__ uint32_t lds_at(int row, int col) {   // in bytes
   int f;
   if (D == 128) f = NATURAL ? (row & 3) << 1 | (row & 8) | (row >> 2 & 1) : (row & 7) << 1 | (row >> 3 & 1);
+  else if (D == 32) f = NATURAL ? row >> 2 & 3 : (row >> 1 & 2) | (row >> 3 & 1);
   else f = NATURAL ? (row & 2) | (row & 8) >> 1 | (row >> 2 & 1) : (row & 6) | (row >> 3 & 1);
   return 2 * (row * D + ((col >> 3 ^ f) << 3 | (col & 7)));
 }
@@ -585,12 +586,12 @@ template <int D, int PIECES> __device__ __forceinline__ void put_tile(uint32_t a
   for (int i = 0; i < PIECES; ++i) lds_write(at + 4096 * i, p[i]);
 }
 template <int DK, int DV, bool NATURAL>
-__device__ __forceinline__ void put_state(uint32_t lds, uint32_t St, const f32x4 (&S)[DK / 64][DV / 16], int row0, int g, int c) {
-  const uint32_t at = opaque(lds + lds_at<DK, NATURAL>(c, row0 + 4 * g));
+__device__ __forceinline__ void put_state(uint32_t lds, uint32_t St, const Part<DK, DV> &part, const f32x4 (&S)[Part<DK, DV>::RT][Part<DK, DV>::CW], int g, int c) {
+  const uint32_t at = opaque(lds + 2 * part.col0 * DK + lds_at<DK, NATURAL>(c, part.row0 + 4 * g));
 #pragma unroll
-  for (int rt = 0; rt < DK / 64; ++rt)
+  for (int rt = 0; rt < Part<DK, DV>::RT; ++rt)
 #pragma unroll
-    for (int ct = 0; ct < DV / 16; ++ct) lds_write((at ^ 32 * rt) + (St + 32 * ct * DK), __builtin_convertvector(S[rt][ct], bf16x4));
+    for (int ct = 0; ct < Part<DK, DV>::CW; ++ct) lds_write((at ^ 32 * rt) + (St + 32 * ct * DK), __builtin_convertvector(S[rt][ct], bf16x4));
 }
 // What a wave has written to LDS for itself is read after this: LDS takes a wave's accesses in their order, and the compiler keeps it.
 __device__ __forceinline__ void own_lds() {
@@ -685,14 +686,15 @@ __device__ __forceinline__ void weighted_rows(uint32_t lds, uint32_t rows, uint3
     lds_write(pair ^ 32 * ct0, pack_pair(O[0], O[1]));
   }
 }
-// S <- keep S + (K o weight)^T V over the chunk's rows in LDS: RT row tiles of the wave (`row0` elements into a row, part of `keys`), all column tiles.
-// weight: the wave's own table of the chunk's rows.  SUM: keep is 1.
+// S <- keep S + (K o weight)^T V over the chunk's rows in LDS.  weight: the wave's own table of the chunk's rows.  SUM: keep is 1.
 template <int DK, int DV, bool SUM>
-__device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float keep, uint32_t lds, uint32_t Ks, uint32_t Vs, uint32_t weight, int row0, int g, int c) {
-  constexpr int RT = DK / 64, CT = DV / 16;
+__device__ __forceinline__ void update_state(const Part<DK, DV> &part, f32x4 (&S)[Part<DK, DV>::RT][Part<DK, DV>::CW], float keep, uint32_t lds, uint32_t Ks, uint32_t Vs,
+                                             uint32_t weight, int g, int c) {
+  constexpr int RT = Part<DK, DV>::RT, CW = Part<DK, DV>::CW;
   ColumnOperand<DK, false> keys(lds, g, c);
-  keys.at ^= 2 * row0;
-  const ColumnOperand<DV, false> values(lds, g, c);
+  keys.at ^= 2 * part.row0;
+  ColumnOperand<DV, false> values(lds, g, c);
+  if (DK < 64) values.at ^= 2 * part.col0;
   bf16x8 K[RT][2][3];
 #pragma unroll
   for (int jj = 0; jj < 2; ++jj) {
@@ -701,7 +703,7 @@ __device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float
     for (int rt = 0; rt < RT; ++rt) three_terms(keys(Ks, 32 * jj, rt), w0, w1, K[rt][jj]);
   }
 #pragma unroll
-  for (int ct = 0; ct < CT; ++ct) {
+  for (int ct = 0; ct < CW; ++ct) {
     const bf16x8 V[2] = {values(Vs, 0, ct), values(Vs, 32, ct)};
     if (!SUM) {
 #pragma unroll
@@ -715,26 +717,14 @@ __device__ __forceinline__ void update_state(f32x4 (&S)[DK / 64][DV / 16], float
         for (int rt = 0; rt < RT; ++rt) S[rt][ct] = mfma_bf16(K[rt][jj][u], V[jj], S[rt][ct]);
   }
 }
-// A wave's rows of a state, from memory or to it.
-template <int DK, int DV, typename F> __device__ __forceinline__ void each_of_state(const Walk &a, f32x4 (&S)[DK / 64][DV / 16], int row0, int g, int lane_c, F f) {
-  const int c = (int)opaque((uint32_t)lane_c);
-#pragma unroll
-  for (int rt = 0; rt < DK / 64; ++rt)
-#pragma unroll
-    for (int ct = 0; ct < DV / 16; ++ct)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = row0 + 16 * rt + 4 * g + i, col = 16 * ct + c;
-        S[rt][ct][i] = f(S[rt][ct][i], r < a.kw && col < a.vw, r * a.si + col * a.sj);
-      }
-}
 
 // As walk_f32_kernel, for bf16 tensors.  P and the state as an operand of the output are rounded to bf16, like the output; what goes into the
 // state is not.
 template <int DK, int DV, bool FULL, bool STATES>
-__global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(Walk a) {
+__global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(Walk a) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;   // pieces of a thread
-  constexpr int CT = DV / 16, QJ = DK / 32, STAGE = STATES ? 256 : 32 * (DK > DV ? DK : DV);   // bytes of LDS that a wave has for itself
+  typedef Part<DK, DV> P4;
+  constexpr int QJ = DK / 32, STAGE = STATES ? 256 : 32 * (DK > DV ? DK : DV);   // bytes of LDS that a wave has for itself
   // The walk that forms states only waits for memory alone: it has tiles twice, in LDS and under way.
   constexpr int SETS = STATES ? 2 : 1, SET = 2 * kChunk * (DK + DV);
   extern __shared__ __align__(16) unsigned char lds_bytes[];
@@ -744,7 +734,8 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
   const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
-  const int t = (w + blockIdx.x + blockIdx.y) & 3, row0 = DK / 4 * w;   // rows 16 t .. of the chunk (see Part), rows row0 .. of the state
+  const P4 part(w);
+  const int t = part.t;
   const uint32_t stage = lds + SETS * SET + (STATES ? 0 : 2 * DV * DK) + STAGE * w;
   const bool last = a.reverse ? seg.s == 0 : seg.s == a.seq.segments(seg.b) - 1;
   if (STATES && last) return;
@@ -753,11 +744,11 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
   const float l2 = log2_decay(a.log_decay, h);
   const int64_t state_size = (int64_t)a.kw * a.vw;
 
-  f32x4 S[DK / 64][CT];   // S[rt][ct][i] is row row0 + 16 rt + 4 g + i, column 16 ct + c
+  f32x4 S[P4::RT][P4::CW];   // S[rt][ct][i] is row row0 + 16 rt + 4 g + i, column col0 + 16 ct + c
   const int own = cache_row(a, seg.b);
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
   const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
-  each_of_state<DK, DV>(a, S, row0, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  each_of_state<DK, DV>(a, S, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const Weights weights(a, l2, t, g, c);
 
   u32x4 rk[SETS][PK], rv[SETS][PV], rq[QJ];
@@ -783,7 +774,7 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
       put_tile<DV, PV>(vput + set * SET, rv[set]);
       bf16x8 Q[QJ];
       if (!STATES) {
-        put_state<DK, DV, false>(lds, St, S, row0, g, c);
+        put_state<DK, DV, false>(lds, St, part, S, g, c);
         qo.operands(rq, stage, g, c, Q);
       }
       __syncthreads();
@@ -803,7 +794,7 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
       }
       // the walk that forms states only weights rows by the segment's end, and has no sum to scale
       put_weights(stage, lane, a, l2, STATES ? seg.rows - 1 - r0 : rows - 1);
-      update_state<DK, DV, STATES>(S, decay_pow(l2, rows), lds, Ks + set * SET, Vs + set * SET, stage, row0, g, c);
+      update_state<DK, DV, STATES>(part, S, decay_pow(l2, rows), lds, Ks + set * SET, Vs + set * SET, stage, g, c);
       if (SETS == 1) __syncthreads();   // (with two sets every wave is past this one's reads at the next set's barrier)
     }
   }
@@ -811,31 +802,33 @@ __global__ __launch_bounds__(256, DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(
   float *fin = nullptr;
   if (STATES) fin = a.fin + ((int64_t)blockIdx.x * a.H + h) * state_size;
   else if (last && a.fin && own >= 0) fin = a.fin + ((int64_t)own * a.H + h) * state_size;
-  if (fin) each_of_state<DK, DV>(a, S, row0, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
+  if (fin) each_of_state<DK, DV>(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
 }
 
 // As back_f32_kernel, for bf16 tensors.
 template <int DK, int DV, bool FULL>
-__global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
+__global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : 2) void back_bf16_kernel(Walk a, Back b) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;
-  constexpr int CT = DV / 16, KJ = DK / 32, VJ = DV / 32, STAGE = 32 * (DK > DV ? DK : DV);
+  typedef Part<DK, DV> P4;
+  constexpr int KJ = DK / 32, VJ = DV / 32, STAGE = 32 * (DK > DV ? DK : DV);
   extern __shared__ __align__(16) unsigned char lds_bytes[];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes;
   constexpr uint32_t Qs = 0, Ds = 2 * kChunk * DK, Gt = Ds + 2 * kChunk * DV;
   const Segment seg = segment_of(a.seq, blockIdx.x);
   if (seg.rows < 0) return;
   const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
-  const int t = (w + blockIdx.x + blockIdx.y) & 3, row0 = DK / 4 * w;
+  const P4 part(w);
+  const int t = part.t;
   const uint32_t stage = lds + Gt + 2 * DV * DK + STAGE * w;
   const Rows qr = rows_of(a.k, a.sk, seg, a, h, a.kw, 2), dr = rows_of(a.v, a.sv, seg, a, h, a.vw, 2), kr = rows_of(b.k, b.sk, seg, a, h, a.kw, 2),
              vr = rows_of(b.v, b.sv, seg, a, h, a.vw, 2), dkr = rows_of(b.dk, b.sk, seg, a, h, a.kw, 2), dvr = rows_of(b.dv, b.sv, seg, a, h, a.vw, 2);
   const float l2 = log2_decay(a.log_decay, h);
   const int64_t state_size = (int64_t)a.kw * a.vw;
 
-  f32x4 G[DK / 64][CT];
+  f32x4 G[P4::RT][P4::CW];
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : seg.b;
   const float *init = a.init ? a.init + (from * a.H + h) * state_size : nullptr;
-  each_of_state<DK, DV>(a, G, row0, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  each_of_state<DK, DV>(a, G, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const Weights weights(a, l2, t, g, c);
 
   u32x4 rq[PK], rd[PV], rk[KJ], rv[VJ];
@@ -859,7 +852,7 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
     const int rows = min(kChunk, seg.rows - r0);
     put_tile<DK, PK>(qput, rq);
     put_tile<DV, PV>(dput, rd);
-    put_state<DK, DV, true>(lds, Gt, G, row0, g, c);
+    put_state<DK, DV, true>(lds, Gt, part, G, g, c);
     bf16x8 K[KJ], V[VJ];
     ko.operands(rk, stage, g, c, K);
     vo.operands(rv, stage, g, c, V);
@@ -890,12 +883,12 @@ __global__ __launch_bounds__(256, 2) void back_bf16_kernel(Walk a, Back b) {
     }
     request_own(r0 + kChunk);
     put_weights(stage, lane, a, l2, rows - 1);
-    update_state<DK, DV, false>(G, decay_pow(l2, rows), lds, Qs, Ds, stage, row0, g, c);
+    update_state<DK, DV, false>(part, G, decay_pow(l2, rows), lds, Qs, Ds, stage, g, c);
     __syncthreads();
   }
   if (a.fin && seg.s == 0) {
     float *fin = a.fin + ((int64_t)seg.b * a.H + h) * state_size;
-    each_of_state<DK, DV>(a, G, row0, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
+    each_of_state<DK, DV>(a, G, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
   }
 }
 
@@ -995,14 +988,14 @@ __global__ __launch_bounds__(256) void step_kernel(Step a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-// Rows of a segment.  Segments are as many as the device holds workgroups at a time, three to a compute unit at widths up to 64 in bf16 and 32 in float32, else two: a walk over more
+// Rows of a segment.  Segments are as many as the device holds workgroups at a time, four to a compute unit at widths up to 32 in bf16, three up to 64 (float32: up to 32), else two: a walk over more
 // of them has a last round that is partly idle (32 slices of 65536 rows, width 128, 768 instead of 512: walk 615 us, 519 with 512).  Packed sequences have a
 // partial segment each on top, and three quarters as many whole ones (24 prompts, 16 heads, 65536 rows: 476 us in all, 507 without this).  Two chunks at least: 8 slices
 // of 1000 rows 22 us with segments of one, two or four chunks, 32 with eight or in one launch.
 int segment_rows(const wersa_decay_desc &c) {
   const int64_t slices = (int64_t)c.H * (c.packed ? 1 : c.B);
-  const int narrow = c.dtype == WERSA_BF16 ? 64 : 32;
-  const int64_t held = c.dk <= narrow && c.dv <= narrow ? 768 : 512;
+  const int width = (c.dk > c.dv ? c.dk : c.dv) * (c.dtype == WERSA_BF16 ? 1 : 2);
+  const int64_t held = width <= 32 ? 1024 : width <= 64 ? 768 : 512;
   const int64_t want = (c.packed ? held * 3 / 4 : held) / slices;   // segments of a slice
   if (want <= 1) return c.packed ? INT32_MAX / 2 : (c.n + kChunk - 1) / kChunk * kChunk + kChunk;
   int64_t rows = ((int64_t)c.n + want - 1) / want;
@@ -1064,8 +1057,7 @@ template <int DK, int DV, bool STATES> bool launch_walk_as(const wersa_decay_des
                                   : launch(name, &walk_bf16_kernel<DK, DV, false, STATES>, smem, a, st);
 }
 template <bool STATES> bool launch_walk(const wersa_decay_desc &c, const Walk &a, hipStream_t st) {
-  if (c.dtype == WERSA_F32 && a.kw <= 32 && a.vw <= 32)
-    return launch(STATES ? "wersa_decay_states" : "wersa_decay_walk", &walk_f32_kernel<32, 32, STATES>, f32_lds(32, 32, !STATES), a, st);
+  if (a.kw <= 32 && a.vw <= 32) return launch_walk_as<32, 32, STATES>(c, a, st);
   if (a.kw <= 64) return a.vw <= 64 ? launch_walk_as<64, 64, STATES>(c, a, st) : launch_walk_as<64, 128, STATES>(c, a, st);
   return a.vw <= 64 ? launch_walk_as<128, 64, STATES>(c, a, st) : launch_walk_as<128, 128, STATES>(c, a, st);
 }
@@ -1076,7 +1068,7 @@ template <int DK, int DV> bool launch_back_as(const wersa_decay_desc &c, const W
                                   : launch("wersa_decay_back", &back_bf16_kernel<DK, DV, false>, smem, a, st, b);
 }
 bool launch_back(const wersa_decay_desc &c, const Walk &a, const Back &b, hipStream_t st) {
-  if (c.dtype == WERSA_F32 && a.kw <= 32 && a.vw <= 32) return launch("wersa_decay_back", &back_f32_kernel<32, 32>, f32_lds(32, 32, true), a, st, b);
+  if (a.kw <= 32 && a.vw <= 32) return launch_back_as<32, 32>(c, a, b, st);
   if (a.kw <= 64) return a.vw <= 64 ? launch_back_as<64, 64>(c, a, b, st) : launch_back_as<64, 128>(c, a, b, st);
   return a.vw <= 64 ? launch_back_as<128, 64>(c, a, b, st) : launch_back_as<128, 128>(c, a, b, st);
 }
