@@ -108,7 +108,7 @@ __global__ __launch_bounds__(256) void norm_kernel(NormJob a) {
   constexpr int E = 16 / sizeof(T);
   __shared__ float part[4];
   const int t = threadIdx.x % LANES;
-  const int64_t row = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
   const bool ok = row < a.rows;   // (every thread stays for the sums)
   const T *x = (const T *)a.x + (ok ? row : 0) * a.stride_x;
   float v[PIECES][E];
@@ -343,7 +343,8 @@ wersa_status forward(const wersa_norm_desc &c, const NormJob &a, bool eight, hip
   by_width(c, [&](auto *type, auto lanes, auto pieces) {
     typedef typename std::remove_pointer<decltype(type)>::type T;
     constexpr int L = decltype(lanes)::value, P = decltype(pieces)::value;
-    const unsigned grid = (unsigned)((c.rows + 256 / L - 1) / (256 / L));
+    const int64_t groups = (c.rows + 256 / L - 1) / (256 / L), across = std::min<int64_t>(groups, 1 << 20);   // (a dimension has fewer than 2^32 threads)
+    const dim3 grid((unsigned)across, (unsigned)((groups + across - 1) / across));
     if (eight) WERSA_STAGE("wersa_rms_norm_eight_bit", st, (norm_kernel<T, L, P, true><<<grid, 256, 0, st>>>(a)));
     else WERSA_STAGE("wersa_rms_norm", st, (norm_kernel<T, L, P, false><<<grid, 256, 0, st>>>(a)));
   });

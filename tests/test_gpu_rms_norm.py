@@ -146,3 +146,14 @@ def test_leading_dimensions_and_unused_outputs():
     (dx,) = torch.autograd.grad(y, x, one.expand_as(y))
     (want,) = torch.autograd.grad(y_of := autograd.wersa_rms_norm(x, w, residual=res)[0], x, torch.ones_like(y))
     assert torch.equal(dx, want)
+
+
+def test_more_rows_than_one_dimension_of_a_grid_has_threads_for():
+    """2^29 rows of one column: 2^24 workgroups, 2^32 threads."""
+    from paper_2507_08637_amd import binding
+    rows = (1 << 29) + 5
+    x = torch.full((rows, 1), 2.0, dtype=torch.bfloat16, device="cuda")
+    x[-1], x[-7], x[rows // 2] = -3.0, 0.0, -1.0
+    y, _, _ = binding.wersa_rms_norm_forward(x, eps=0.0)
+    y[-7] = 1
+    assert (y[-1] == -1).all() and (y[rows // 2] == -1).all() and int((y == 1).sum()) == rows - 2
