@@ -158,11 +158,13 @@ __device__ __forceinline__ f32x4 mfma_f32(float a, float b, f32x4 c) { return __
 
 // A wave's part of a chunk's work and of the state.  Rows 16 t .. of the chunk: the weights of a later tile have more rows to them, so that which wave has which goes by the
 // workgroup (all first waves of a compute unit's workgroups share a SIMD).  Of the state RT row tiles from row0 on and CW column tiles from col0 on: at width 32 a wave has one
-// row tile and half of the columns.
-template <int DK, int DV> struct Part {
-  static constexpr int RT = DK < 64 ? 1 : DK / 64, CT = DV / 16, CW = DK < 64 ? CT / 2 : CT;
-  int t, row0, col0;
-  __device__ __forceinline__ Part(int wave) : t((wave + blockIdx.x + blockIdx.y) & 3), row0(DK < 64 ? 16 * (wave & 1) : DK / 4 * wave), col0(DK < 64 ? DV / 2 * (wave >> 1) : 0) {}
+// row tile and half of the columns; with eight waves two of them share rows and rows of the state, and each has half of the columns, of the outputs too.
+template <int DK, int DV, int WAVES = 4> struct Part {
+  static constexpr int HALVES = WAVES / 4, RT = DK < 64 ? 1 : DK / 64, CT = DV / 16, CW = DK < 64 ? CT / 2 : CT / HALVES;
+  int t, half, row0, col0;
+  __device__ __forceinline__ Part(int wave)
+      : t((wave + blockIdx.x + blockIdx.y) & 3), half(wave >> 2), row0(DK < 64 ? 16 * (wave & 1) : DK / 4 * (wave & 3)),
+        col0(DK < 64 ? DV / 2 * (wave >> 1) : DV / HALVES * half) {}
 };
 // Products of a wave's 16 own rows (four consecutive values of a row in a lane) with rows 16 jt .. of the chunk in LDS.
 template <int D> __device__ __forceinline__ f32x4 products_f32(const float *rows, int jt, const f32x4 (&own)[D / 16], int g, int c) {
@@ -181,22 +183,17 @@ template <int D> __device__ __forceinline__ void load_own_f32(const Rows &r, int
 #pragma unroll
   for (int j = 0; j < D / 16; ++j) own[j] = __builtin_bit_cast(f32x4, load_piece(c, (at + 64 * j - c.missing) | outside(64 * j + 16 * g, r.width)));
 }
-template <int D> __device__ __forceinline__ void store_own_f32(const Rows &r, int r0, uint32_t at, int g, const f32x4 (&o)[D / 16]) {
-  const Rows::Chunk c = r.chunk(r0);
+template <int D, int THREADS, int PIECES> __device__ __forceinline__ void put_tile_f32(float *rows, int tid, const u32x4 (&p)[PIECES]) {
 #pragma unroll
-  for (int j = 0; j < D / 16; ++j) store_piece(c, (at + 64 * j - c.missing) | outside(64 * j + 16 * g, r.width), __builtin_bit_cast(u32x4, o[j]));
+  for (int i = 0; i < PIECES; ++i) *(u32x4 *)(rows + (tid / (D / 4) + 4 * THREADS / D * i) * (D + 4) + tid % (D / 4) * 4) = p[i];
 }
-template <int D, int PIECES> __device__ __forceinline__ void put_tile_f32(float *rows, int tid, const u32x4 (&p)[PIECES]) {
-#pragma unroll
-  for (int i = 0; i < PIECES; ++i) *(u32x4 *)(rows + (tid / (D / 4) + 1024 / D * i) * (D + 4) + tid % (D / 4) * 4) = p[i];
-}
-template <int DK, int DV, typename F>
-__device__ __forceinline__ void each_of_state(const Walk &a, f32x4 (&S)[Part<DK, DV>::RT][Part<DK, DV>::CW], const Part<DK, DV> &part, int g, int lane_c, F f) {
+template <typename P, int RT, int CW, typename F>
+__device__ __forceinline__ void each_of_state(const Walk &a, f32x4 (&S)[RT][CW], const P &part, int g, int lane_c, F f) {
   const int c = (int)opaque((uint32_t)lane_c);
 #pragma unroll
-  for (int rt = 0; rt < Part<DK, DV>::RT; ++rt)
+  for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-    for (int ct = 0; ct < Part<DK, DV>::CW; ++ct)
+    for (int ct = 0; ct < CW; ++ct)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int r = part.row0 + 16 * rt + 4 * g + i, col = part.col0 + 16 * ct + c;
@@ -223,71 +220,80 @@ struct WeightsF32 {
     return p;
   }
 };
-// S += (K o weight)^T V over rows 16 jt .. of the chunk; V: the rows' values in the layout below.
-template <int DK, int DV>
-__device__ __forceinline__ void add_to_state_f32(const Part<DK, DV> &part, f32x4 (&S)[Part<DK, DV>::RT][Part<DK, DV>::CW], const float *Ks, const float *Vs, const float *weight, int jt,
-                                                 const float (&V)[DV / 16][4], int g, int c) {
-  constexpr int LK = DK + 4, LV = DV + 4, RT = Part<DK, DV>::RT, CW = Part<DK, DV>::CW;
-  const f32x4 wt = *(const f32x4 *)(weight + 16 * jt + 4 * g);
-  float U[CW][4];
+// Columns 16 ct + c of rows 16 jt + 4 g + i of the chunk in LDS, rows of D values.
+template <int D, int TILES> __device__ __forceinline__ void columns_f32(const float *rows, int jt, int g, int c, float (&v)[TILES][4]) {
 #pragma unroll
-  for (int ct = 0; ct < CW; ++ct)
+  for (int ct = 0; ct < TILES; ++ct)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) U[ct][i] = DK < 64 ? Vs[(16 * jt + 4 * g + i) * LV + part.col0 + 16 * ct + c] : V[ct][i];
+    for (int i = 0; i < 4; ++i) v[ct][i] = rows[(16 * jt + 4 * g + i) * (D + 4) + 16 * ct + c];
+}
+// S <- keep S + (K o weight)^T V over the chunk's rows.
+template <int DK, int DV, typename P, int RT, int CW>
+__device__ __forceinline__ void update_state_f32(const P &part, f32x4 (&S)[RT][CW], float keep, const float *Ks, const float *Vs, const float *weight, int g, int c) {
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float kt = Ks[(16 * jt + 4 * g + i) * LK + part.row0 + 16 * rt + c] * wt[i];
+    for (int ct = 0; ct < CW; ++ct) S[rt][ct] *= keep;
 #pragma unroll
-      for (int ct = 0; ct < CW; ++ct) S[rt][ct] = mfma_f32(kt, U[ct][i], S[rt][ct]);
-    }
-}
-template <int D> __device__ __forceinline__ void columns_f32(const float *rows, int jt, int g, int c, float (&v)[D / 16][4]) {
+  for (int jt = 0; jt < 4; ++jt) {
+    const f32x4 wt = *(const f32x4 *)(weight + 16 * jt + 4 * g);
+    float V[CW][4];
+    columns_f32<DV>(Vs + part.col0, jt, g, c, V);
 #pragma unroll
-  for (int ct = 0; ct < D / 16; ++ct)
+    for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) v[ct][i] = rows[(16 * jt + 4 * g + i) * (D + 4) + 16 * ct + c];
+      for (int i = 0; i < 4; ++i) {
+        const float kt = Ks[(16 * jt + 4 * g + i) * (DK + 4) + part.row0 + 16 * rt + c] * wt[i];
+#pragma unroll
+        for (int ct = 0; ct < CW; ++ct) S[rt][ct] = mfma_f32(kt, V[ct][i], S[rt][ct]);
+      }
+  }
 }
 
 // The output of a wave's 16 own rows: what the state gives (`inter`, a tile of columns at a time) and the weighted rows of the chunk, `weight` their weights for rows 16 jt ..
 // A weight that is masked is a zero, and in a product of matrices a zero times what is not a number or not finite is not a number: rows that come later would reach back.  So results that
 // are not finite are formed again, with such values left out; where none of a row's own reach is among them, that is the result.
-template <int D, typename Inter, typename Weight>
-__device__ __forceinline__ void weighted_rows_f32(const float *rows, const Rows &out, int r0, uint32_t at, int t, int g, int c, Inter inter, Weight weight) {
+// D / HALVES columns of the output, from `col` on.
+template <int D, int HALVES, typename Inter, typename Weight>
+__device__ __forceinline__ void weighted_rows_f32(const float *rows, const Rows &out, int r0, uint32_t at, int col, int t, int g, int c, Inter inter, Weight weight) {
+  constexpr int TILES = D / 16 / HALVES;
   float probe = 0.f;
+  const Rows::Chunk oc = out.chunk(r0);
+  auto store = [&](int ct, f32x4 x) {
+    store_piece(oc, (at + 4 * col + 64 * ct - oc.missing) | outside(4 * col + 64 * ct + 16 * g, out.width), __builtin_bit_cast(u32x4, x));
+  };
   {
-    f32x4 O[D / 16];
+    f32x4 O[TILES];
 #pragma unroll
-    for (int ct = 0; ct < D / 16; ++ct) O[ct] = inter(ct);
+    for (int ct = 0; ct < TILES; ++ct) O[ct] = inter(ct);
 #pragma unroll
     for (int jt = 0; jt < 4; ++jt) {
       if (jt > t) break;
-      float V[D / 16][4];
-      columns_f32<D>(rows, jt, g, c, V);
+      float V[TILES][4];
+      columns_f32<D>(rows + col, jt, g, c, V);
       const f32x4 P = weight(jt);
 #pragma unroll
-      for (int ct = 0; ct < D / 16; ++ct)
+      for (int ct = 0; ct < TILES; ++ct)
 #pragma unroll
         for (int i = 0; i < 4; ++i) O[ct] = mfma_f32(V[ct][i], P[i], O[ct]);
     }
 #pragma unroll
-    for (int ct = 0; ct < D / 16; ++ct)
+    for (int ct = 0; ct < TILES; ++ct) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) probe = fmaf(O[ct][i], 0.f, probe);   // not a number if one is not finite
-    store_own_f32<D>(out, r0, at, g, O);
+      store(ct, O[ct]);
+    }
   }
   if (!__any(!(probe == 0.f))) return;
-  const Rows::Chunk oc = out.chunk(r0);
 #pragma unroll 1
-  for (int ct = 0; ct < D / 16; ++ct) {
+  for (int ct = 0; ct < TILES; ++ct) {
     f32x4 all = inter(ct), finite = all, met = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
     for (int jt = 0; jt <= t; ++jt) {
       const f32x4 P = weight(jt);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        const float v = rows[(16 * jt + 4 * g + i) * (D + 4) + 16 * ct + c];
+        const float v = rows[(16 * jt + 4 * g + i) * (D + 4) + col + 16 * ct + c];
         const bool fine = fabsf(v) < __builtin_inff();
         all = mfma_f32(v, P[i], all);
         finite = mfma_f32(fine ? v : 0.f, P[i], finite);
@@ -296,16 +302,17 @@ __device__ __forceinline__ void weighted_rows_f32(const float *rows, const Rows 
     }
 #pragma unroll
     for (int i = 0; i < 4; ++i) all[i] = met[i] > 0.f ? all[i] : finite[i];
-    store_piece(oc, (at + 64 * ct - oc.missing) | outside(64 * ct + 16 * g, out.width), __builtin_bit_cast(u32x4, all));
+    store(ct, all);
   }
 }
 
-// Four waves.  Weights are formed as their transpose (the chunk's rows down the registers, own rows on the lanes), which is the layout that the product with V takes them in.
+// Weights are formed as their transpose (the chunk's rows down the registers, own rows on the lanes), which is the layout that the product with V takes them in.
+// Eight waves at width 128, where LDS holds one workgroup to a compute unit: two to a SIMD, which form their rows' weights twice.
+constexpr int f32_waves(int dk, int dv) { return dk > 64 || dv > 64 ? 8 : 4; }
 template <int DK, int DV, bool STATES>
-__global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
-  constexpr int LK = DK + 4, LV = DV + 4, PK = kChunk * DK / 4 / 256, PV = kChunk * DV / 4 / 256;   // pieces of a thread
-  typedef Part<DK, DV> P4;
-  constexpr int CT = P4::CT;
+__global__ __launch_bounds__(64 * f32_waves(DK, DV)) void walk_f32_kernel(Walk a) {
+  constexpr int WAVES = f32_waves(DK, DV), THREADS = 64 * WAVES, LK = DK + 4, LV = DV + 4, PK = kChunk * DK / 4 / THREADS, PV = kChunk * DV / 4 / THREADS;   // pieces of a thread
+  typedef Part<DK, DV, WAVES> P4;
   extern __shared__ __align__(16) float lds[];
   float *Ks = lds, *Vs = Ks + kChunk * LK, *weight = Vs + kChunk * LV, *St = weight + kChunk;
   const Segment seg = segment_of(a.seq, blockIdx.x);
@@ -314,6 +321,7 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
   const bool last = a.reverse ? seg.s == 0 : seg.s == a.seq.segments(seg.b) - 1;
   if (STATES && last) return;   // nothing begins with what the last one adds
   const P4 part(wave);
+  const int col = DV / P4::HALVES * part.half;   // of the outputs
   const Rows qr = rows_of(a.q, a.sq, seg, a, h, a.kw, 4), kr = rows_of(a.k, a.sk, seg, a, h, a.kw, 4), vr = rows_of(a.v, a.sv, seg, a, h, a.vw, 4),
              orow = rows_of(a.o, a.so, seg, a, h, a.vw, 4);
   const float l2 = log2_decay(a.log_decay, h);
@@ -323,13 +331,13 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
   const int own = cache_row(a, seg.b);
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
   const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
-  each_of_state<DK, DV>(a, S, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  each_of_state(a, S, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const WeightsF32 weights(a, l2, part.t, g, c);
 
   u32x4 rk[PK], rv[PV];
   f32x4 rq[DK / 16];
-  const TilePieces<DK, 4, PK, 256, false> kp(kr, 0, tid);
-  const TilePieces<DV, 4, PV, 256, false> vp(vr, 0, tid);
+  const TilePieces<DK, 4, PK, THREADS, false> kp(kr, 0, tid);
+  const TilePieces<DV, 4, PV, THREADS, false> vp(vr, 0, tid);
   const uint32_t qat = qr.offset(16 * part.t + c, 16 * g), oat = orow.offset(16 * part.t + c, 16 * g);
   auto request = [&](int r0) {
     kp.template load<false>(kr, r0, rk);
@@ -341,8 +349,8 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
   for (int r0 = 0; r0 < seg.rows; r0 += kChunk) {
     const int rows = min(kChunk, seg.rows - r0);
     // what was requested, and the state, into LDS
-    put_tile_f32<DK>(Ks, tid, rk);
-    put_tile_f32<DV>(Vs, tid, rv);
+    put_tile_f32<DK, THREADS>(Ks, tid, rk);
+    put_tile_f32<DV, THREADS>(Vs, tid, rv);
     if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + (a.reverse ? 1 : 0));
     f32x4 Q[DK / 16];
     if (!STATES) {
@@ -355,28 +363,18 @@ __global__ __launch_bounds__(256) void walk_f32_kernel(Walk a) {
     }
     __syncthreads();
     request(r0 + kChunk);
-
     if (!STATES)
-      weighted_rows_f32<DV>(Vs, orow, r0, oat, part.t, g, c, [&](int ct) { return products_f32<DK>(St, ct, Q, g, c) * weights.reach; },
-                            [&](int jt) { return weights(products_f32<DK>(Ks, jt, Q, g, c), jt); });
-    const float keep = decay_pow(l2, rows);
-#pragma unroll
-    for (int rt = 0; rt < P4::RT; ++rt)
-#pragma unroll
-      for (int ct = 0; ct < P4::CW; ++ct) S[rt][ct] *= keep;
-#pragma unroll
-    for (int jt = 0; jt < 4; ++jt) {
-      float V[CT][4];
-      if (DK >= 64) columns_f32<DV>(Vs, jt, g, c, V);
-      add_to_state_f32<DK, DV>(part, S, Ks, Vs, weight, jt, V, g, c);
-    }
+      weighted_rows_f32<DV, P4::HALVES>(Vs, orow, r0, oat, col, part.t, g, c,
+                                        [&](int ct) { return products_f32<DK>(St + col * LK, ct, Q, g, c) * weights.reach; },
+                                        [&](int jt) { return weights(products_f32<DK>(Ks, jt, Q, g, c), jt); });
+    update_state_f32<DK, DV>(part, S, decay_pow(l2, rows), Ks, Vs, weight, g, c);
     __syncthreads();
   }
 
   float *fin = nullptr;
   if (STATES) fin = a.fin + ((int64_t)blockIdx.x * a.H + h) * state_size;
   else if (last && a.fin && own >= 0) fin = a.fin + ((int64_t)own * a.H + h) * state_size;
-  if (fin) each_of_state<DK, DV>(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
+  if (fin) each_of_state(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
 }
 
 // The two walks back of the derivative as one, k and v of `a` being q and dout: own rows of keys and values, G^T k and the weighted rows of dout give dv, G v and the
@@ -387,9 +385,9 @@ struct Back {
   Strides sk, sv;
 };
 template <int DK, int DV>
-__global__ __launch_bounds__(256) void back_f32_kernel(Walk a, Back b) {
-  constexpr int LK = DK + 4, LV = DV + 4, PK = kChunk * DK / 4 / 256, PV = kChunk * DV / 4 / 256;
-  typedef Part<DK, DV> P4;
+__global__ __launch_bounds__(64 * f32_waves(DK, DV)) void back_f32_kernel(Walk a, Back b) {
+  constexpr int WAVES = f32_waves(DK, DV), THREADS = 64 * WAVES, LK = DK + 4, LV = DV + 4, PK = kChunk * DK / 4 / THREADS, PV = kChunk * DV / 4 / THREADS;
+  typedef Part<DK, DV, WAVES> P4;
   constexpr int KT = DK / 16, CT = P4::CT;
   extern __shared__ __align__(16) float lds[];
   float *Qs = lds, *Ds = Qs + kChunk * LK, *weight = Ds + kChunk * LV, *Gt = weight + kChunk;
@@ -397,6 +395,7 @@ __global__ __launch_bounds__(256) void back_f32_kernel(Walk a, Back b) {
   if (seg.rows < 0) return;
   const int h = blockIdx.y, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const P4 part(wave);
+  const int vcol = DV / P4::HALVES * part.half, kcol = DK / P4::HALVES * part.half;   // of dv and of dk
   const Rows qr = rows_of(a.k, a.sk, seg, a, h, a.kw, 4), dr = rows_of(a.v, a.sv, seg, a, h, a.vw, 4), kr = rows_of(b.k, b.sk, seg, a, h, a.kw, 4),
              vr = rows_of(b.v, b.sv, seg, a, h, a.vw, 4), dkr = rows_of(b.dk, b.sk, seg, a, h, a.kw, 4), dvr = rows_of(b.dv, b.sv, seg, a, h, a.vw, 4);
   const float l2 = log2_decay(a.log_decay, h);
@@ -405,13 +404,13 @@ __global__ __launch_bounds__(256) void back_f32_kernel(Walk a, Back b) {
   f32x4 G[P4::RT][P4::CW];
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : seg.b;
   const float *init = a.init ? a.init + (from * a.H + h) * state_size : nullptr;
-  each_of_state<DK, DV>(a, G, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  each_of_state(a, G, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const WeightsF32 weights(a, l2, part.t, g, c);
 
   u32x4 rq[PK], rd[PV];
   f32x4 K[KT], V[CT];
-  const TilePieces<DK, 4, PK, 256, false> qp(qr, 0, tid);
-  const TilePieces<DV, 4, PV, 256, false> dp(dr, 0, tid);
+  const TilePieces<DK, 4, PK, THREADS, false> qp(qr, 0, tid);
+  const TilePieces<DV, 4, PV, THREADS, false> dp(dr, 0, tid);
   const uint32_t kat = kr.offset(16 * part.t + c, 16 * g), vat = vr.offset(16 * part.t + c, 16 * g);
   const uint32_t dkat = dkr.offset(16 * part.t + c, 16 * g), dvat = dvr.offset(16 * part.t + c, 16 * g);
   auto request = [&](int r0) {
@@ -426,8 +425,8 @@ __global__ __launch_bounds__(256) void back_f32_kernel(Walk a, Back b) {
   request_own(0);
   for (int r0 = 0; r0 < seg.rows; r0 += kChunk) {
     const int rows = min(kChunk, seg.rows - r0);
-    put_tile_f32<DK>(Qs, tid, rq);
-    put_tile_f32<DV>(Ds, tid, rd);
+    put_tile_f32<DK, THREADS>(Qs, tid, rq);
+    put_tile_f32<DV, THREADS>(Ds, tid, rd);
     if (tid < kChunk) weight[tid] = a.gain * decay_pow(l2, max(rows - 1 - tid, 0) + 1);
 #pragma unroll
     for (int rt = 0; rt < P4::RT; ++rt)
@@ -435,33 +434,23 @@ __global__ __launch_bounds__(256) void back_f32_kernel(Walk a, Back b) {
       for (int ct = 0; ct < P4::CW; ++ct) *(f32x4 *)(Gt + (part.col0 + 16 * ct + c) * LK + part.row0 + 16 * rt + 4 * g) = G[rt][ct];
     __syncthreads();
     request(r0 + kChunk);
-    weighted_rows_f32<DV>(Ds, dvr, r0, dvat, part.t, g, c, [&](int ct) { return products_f32<DK>(Gt, ct, K, g, c) * weights.reach; },
-                          [&](int jt) { return weights(products_f32<DK>(Qs, jt, K, g, c), jt); });
-    weighted_rows_f32<DK>(Qs, dkr, r0, dkat, part.t, g, c, [&](int kt) {   // G v: rows of G down the lanes, its columns four values apart in Gt
+    weighted_rows_f32<DV, P4::HALVES>(Ds, dvr, r0, dvat, vcol, part.t, g, c, [&](int ct) { return products_f32<DK>(Gt + vcol * LK, ct, K, g, c) * weights.reach; },
+                                      [&](int jt) { return weights(products_f32<DK>(Qs, jt, K, g, c), jt); });
+    weighted_rows_f32<DK, P4::HALVES>(Qs, dkr, r0, dkat, kcol, part.t, g, c, [&](int kt) {   // G v: rows of G down the lanes, its columns four values apart in Gt
       f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < CT; ++j)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc = mfma_f32(Gt[(16 * j + 4 * g + i) * LK + 16 * kt + c], V[j][i], acc);
+        for (int i = 0; i < 4; ++i) acc = mfma_f32(Gt[(16 * j + 4 * g + i) * LK + kcol + 16 * kt + c], V[j][i], acc);
       return acc * weights.reach;
     }, [&](int jt) { return weights(products_f32<DV>(Ds, jt, V, g, c), jt); });
     request_own(r0 + kChunk);
-    const float keep = decay_pow(l2, rows);
-#pragma unroll
-    for (int rt = 0; rt < P4::RT; ++rt)
-#pragma unroll
-      for (int ct = 0; ct < P4::CW; ++ct) G[rt][ct] *= keep;
-#pragma unroll
-    for (int jt = 0; jt < 4; ++jt) {
-      float D[CT][4];
-      if (DK >= 64) columns_f32<DV>(Ds, jt, g, c, D);
-      add_to_state_f32<DK, DV>(part, G, Qs, Ds, weight, jt, D, g, c);
-    }
+    update_state_f32<DK, DV>(part, G, decay_pow(l2, rows), Qs, Ds, weight, g, c);
     __syncthreads();
   }
   if (a.fin && seg.s == 0) {
     float *fin = a.fin + ((int64_t)seg.b * a.H + h) * state_size;
-    each_of_state<DK, DV>(a, G, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
+    each_of_state(a, G, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
   }
 }
 
@@ -748,7 +737,7 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) vo
   const int own = cache_row(a, seg.b);
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
   const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
-  each_of_state<DK, DV>(a, S, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  each_of_state(a, S, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const Weights weights(a, l2, t, g, c);
 
   u32x4 rk[SETS][PK], rv[SETS][PV], rq[QJ];
@@ -802,7 +791,7 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) vo
   float *fin = nullptr;
   if (STATES) fin = a.fin + ((int64_t)blockIdx.x * a.H + h) * state_size;
   else if (last && a.fin && own >= 0) fin = a.fin + ((int64_t)own * a.H + h) * state_size;
-  if (fin) each_of_state<DK, DV>(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
+  if (fin) each_of_state(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
 }
 
 // As back_f32_kernel, for bf16 tensors.
@@ -828,7 +817,7 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : 2) void back_bf16_kernel(W
   f32x4 G[P4::RT][P4::CW];
   const int64_t from = a.by_slot ? (int64_t)blockIdx.x : seg.b;
   const float *init = a.init ? a.init + (from * a.H + h) * state_size : nullptr;
-  each_of_state<DK, DV>(a, G, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
+  each_of_state(a, G, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const Weights weights(a, l2, t, g, c);
 
   u32x4 rq[PK], rd[PV], rk[KJ], rv[VJ];
@@ -888,7 +877,7 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : 2) void back_bf16_kernel(W
   }
   if (a.fin && seg.s == 0) {
     float *fin = a.fin + ((int64_t)seg.b * a.H + h) * state_size;
-    each_of_state<DK, DV>(a, G, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
+    each_of_state(a, G, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
   }
 }
 
@@ -988,14 +977,14 @@ __global__ __launch_bounds__(256) void step_kernel(Step a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-// Rows of a segment.  Segments are as many as the device holds workgroups at a time, four to a compute unit at widths up to 32 in bf16, three up to 64 (float32: up to 32), else two: a walk over more
-// of them has a last round that is partly idle (32 slices of 65536 rows, width 128, 768 instead of 512: walk 615 us, 519 with 512).  Packed sequences have a
+// Rows of a segment.  Segments are as many as the device holds workgroups at a time, four to a compute unit at widths up to 32 in bf16, three up to 64 (float32: up to 32), then two, and one at width
+// 128 in float32: a walk over more of them has a last round that is partly idle (32 slices of 65536 rows, width 128, 768 instead of 512: walk 615 us, 519 with 512).  Packed sequences have a
 // partial segment each on top, and three quarters as many whole ones (24 prompts, 16 heads, 65536 rows: 476 us in all, 507 without this).  Two chunks at least: 8 slices
 // of 1000 rows 22 us with segments of one, two or four chunks, 32 with eight or in one launch.
 int segment_rows(const wersa_decay_desc &c) {
   const int64_t slices = (int64_t)c.H * (c.packed ? 1 : c.B);
   const int width = (c.dk > c.dv ? c.dk : c.dv) * (c.dtype == WERSA_BF16 ? 1 : 2);
-  const int64_t held = width <= 32 ? 1024 : width <= 64 ? 768 : 512;
+  const int64_t held = width <= 32 ? 1024 : width <= 64 ? 768 : width <= 128 ? 512 : 256;
   const int64_t want = (c.packed ? held * 3 / 4 : held) / slices;   // segments of a slice
   if (want <= 1) return c.packed ? INT32_MAX / 2 : (c.n + kChunk - 1) / kChunk * kChunk + kChunk;
   int64_t rows = ((int64_t)c.n + want - 1) / want;
@@ -1041,20 +1030,20 @@ wersa_status validate(const wersa_decay_desc *c) {
 }
 bool misaligned(const void *p, size_t a) { return ((uintptr_t)p % a) != 0; }
 Strides strides(const int64_t *s) { return Strides{s[0], s[1], s[2]}; }
-template <typename K, typename... Args> bool launch(const char *name, K kern, size_t smem, const Walk &a, hipStream_t st, Args... more) {
+template <typename K, typename... Args> bool launch(const char *name, K kern, int threads, size_t smem, const Walk &a, hipStream_t st, Args... more) {
   if (smem > 65536 &&
       hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess)
     return false;
-  WERSA_STAGE(name, st, kern<<<dim3(a.seq.slots(), a.H), 256, smem, st>>>(a, more...));
+  WERSA_STAGE(name, st, kern<<<dim3(a.seq.slots(), a.H), threads, smem, st>>>(a, more...));
   return true;
 }
 constexpr size_t f32_lds(int dk, int dv, bool state) { return sizeof(float) * (kChunk * (dk + 4 + dv + 4 + 1) + (state ? dv * (dk + 4) : 0)); }
 template <int DK, int DV, bool STATES> bool launch_walk_as(const wersa_decay_desc &c, const Walk &a, hipStream_t st) {
   const char *name = STATES ? "wersa_decay_states" : "wersa_decay_walk";
-  if (c.dtype == WERSA_F32) return launch(name, &walk_f32_kernel<DK, DV, STATES>, f32_lds(DK, DV, !STATES), a, st);
+  if (c.dtype == WERSA_F32) return launch(name, &walk_f32_kernel<DK, DV, STATES>, 64 * f32_waves(DK, DV), f32_lds(DK, DV, !STATES), a, st);
   constexpr size_t sets = STATES ? 2 : 1, smem = 2 * (sets * kChunk * (DK + DV) + (STATES ? 0 : DV * DK)) + 4 * (STATES ? 256 : 32 * (DK > DV ? DK : DV));
-  return a.kw == DK && a.vw == DV ? launch(name, &walk_bf16_kernel<DK, DV, true, STATES>, smem, a, st)
-                                  : launch(name, &walk_bf16_kernel<DK, DV, false, STATES>, smem, a, st);
+  return a.kw == DK && a.vw == DV ? launch(name, &walk_bf16_kernel<DK, DV, true, STATES>, 256, smem, a, st)
+                                  : launch(name, &walk_bf16_kernel<DK, DV, false, STATES>, 256, smem, a, st);
 }
 template <bool STATES> bool launch_walk(const wersa_decay_desc &c, const Walk &a, hipStream_t st) {
   if (a.kw <= 32 && a.vw <= 32) return launch_walk_as<32, 32, STATES>(c, a, st);
@@ -1062,10 +1051,10 @@ template <bool STATES> bool launch_walk(const wersa_decay_desc &c, const Walk &a
   return a.vw <= 64 ? launch_walk_as<128, 64, STATES>(c, a, st) : launch_walk_as<128, 128, STATES>(c, a, st);
 }
 template <int DK, int DV> bool launch_back_as(const wersa_decay_desc &c, const Walk &a, const Back &b, hipStream_t st) {
-  if (c.dtype == WERSA_F32) return launch("wersa_decay_back", &back_f32_kernel<DK, DV>, f32_lds(DK, DV, true), a, st, b);
+  if (c.dtype == WERSA_F32) return launch("wersa_decay_back", &back_f32_kernel<DK, DV>, 64 * f32_waves(DK, DV), f32_lds(DK, DV, true), a, st, b);
   constexpr size_t smem = 2 * (kChunk * (DK + DV) + DV * DK) + 4 * 32 * (DK > DV ? DK : DV);
-  return a.kw == DK && a.vw == DV ? launch("wersa_decay_back", &back_bf16_kernel<DK, DV, true>, smem, a, st, b)
-                                  : launch("wersa_decay_back", &back_bf16_kernel<DK, DV, false>, smem, a, st, b);
+  return a.kw == DK && a.vw == DV ? launch("wersa_decay_back", &back_bf16_kernel<DK, DV, true>, 256, smem, a, st, b)
+                                  : launch("wersa_decay_back", &back_bf16_kernel<DK, DV, false>, 256, smem, a, st, b);
 }
 bool launch_back(const wersa_decay_desc &c, const Walk &a, const Back &b, hipStream_t st) {
   if (a.kw <= 32 && a.vw <= 32) return launch_back_as<32, 32>(c, a, b, st);
