@@ -395,3 +395,17 @@ def test_what_is_not_finite_stays_on_its_side_of_the_mask(n, dk, dv, dtype):
             assert torch.equal(got[name][:, :, 22:], want[name][:, :, 22:]), (x, bad, name)
         if x == "dout":
             assert not torch.isfinite(got["dv"][:, :, 21]).any()
+
+
+@pytest.mark.parametrize("B,H,dk,dv", [(128, 17, 128, 128), (600, 14, 64, 64)])
+def test_step_of_many_states(B, H, dk, dv):
+    """More states than the last-level cache keeps: the variant that passes it by."""
+    from paper_2507_08637_amd import binding
+    g = torch.Generator(device="cuda").manual_seed(1)
+    normal = lambda *shape: torch.randn(shape, generator=g, device="cuda")
+    q, k, v, state = normal(B, H, dk), normal(B, H, dk), normal(B, H, dv), normal(B, H, dk, dv)
+    ld = decays(H).cuda()
+    want = ld.exp().double().view(H, 1, 1) * state.double() + k.double().unsqueeze(3) * v.double().unsqueeze(2)
+    out = binding.wersa_decay_step(q, k, v, ld, state, scale=0.5)
+    close(state, want.cpu(), torch.float32, "state")
+    close(out, (0.5 * (q.double().unsqueeze(3) * want).sum(2)).cpu(), torch.float32, "out")
