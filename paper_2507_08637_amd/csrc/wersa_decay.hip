@@ -1191,11 +1191,11 @@ wersa_status wersa_decay_step(const wersa_decay_desc *desc, const void *q, const
     if (c.dtype == WERSA_F32) WERSA_STAGE("wersa_decay_step", st, (step_kernel<float, W, NT><<<grid, 256, 0, st>>>(a)));
     else WERSA_STAGE("wersa_decay_step", st, (step_kernel<bf16_t, W, NT><<<grid, 256, 0, st>>>(a)));
   };
-  // From 256 states on there is a workgroup for every compute unit with whole rows; fewer are dealt out in 16 columns each.
-  const int64_t states = (int64_t)c.B * c.H, bytes = states * c.dk * c.dv * 4;
+  // Whole rows to a workgroup, however few states there are: 16 columns to one instead take 3.0 us for 8 states of 64 x 64 (3.2 with whole rows), 5.4 for 64 of 128 x 128 (4.5), 13.3
+  // for 256 (8.3).
+  const int64_t bytes = (int64_t)c.B * c.H * c.dk * c.dv * 4;
   auto by_width = [&](auto nt) { c.dv <= 64 ? launch(std::integral_constant<int, 64>{}, nt) : launch(std::integral_constant<int, 128>{}, nt); };
-  if (states < 256) launch(std::integral_constant<int, 16>{}, std::false_type{});
-  else if (bytes < kCachedStates) by_width(std::false_type{});
+  if (bytes < kCachedStates) by_width(std::false_type{});
   else by_width(std::true_type{});
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
