@@ -14,6 +14,8 @@
 // The walk back multiplies with lambda after a row where the walk forward does before it: `shift` below.
 #include "wersa_internal.h"
 
+#include <algorithm>
+#include <cmath>
 #include <type_traits>
 
 namespace wersa {
@@ -984,19 +986,49 @@ __global__ __launch_bounds__(256) void step_kernel(Step a) {
 }
 
 // ---- host ------------------------------------------------------------------------------------------
-// Rows of a segment.  Segments are as many as the device holds workgroups at a time, four to a compute unit at widths up to 32 in bf16, three up to 64 (float32: up to 32), then two, and one at width
-// 128 in float32: a walk over more of them has a last round that is partly idle (32 slices of 65536 rows, width 128, 768 instead of 512: walk 615 us, 519 with 512).  Packed sequences have a
-// partial segment each on top, and three quarters as many whole ones (24 prompts, 16 heads, 65536 rows: 476 us in all, 507 without this).  Two chunks at least: 8 slices
-// of 1000 rows 22 us with segments of one, two or four chunks, 32 with eight or in one launch.
+// Rows of a segment, by what a forward pass takes.  The device holds `held` workgroups of a walk at a time; with all of them a chunk takes `full` us of each, a workgroup alone needs
+// `alone`.  More than one segment to a sequence costs the launch that forms states (about 0.45 of a walk without the last segments), the scan's traffic and two launches.
+// us of a recorded forward pass with this rule, in parentheses with as many segments as the device holds: 48 x 8 slices of 501 rows, width 64, 28 (54); 16 x 16 of 300 16 (35); 8 x 8 of 500
+// 20 (22); 16 x 16 of 1000, width 128, 77 (104); 8 of 2000, width 64, 18 in segments of two chunks, 65 in one; 64 of 2048, width 128, 84, 128 in one; 32 of 65536, walk alone:
+// 519 in 512 segments, 615 in 768.
+struct Pace {
+  int held;
+  float full, alone;
+};
+Pace pace(const wersa_decay_desc &c) {
+  const int width = c.dk > c.dv ? c.dk : c.dv;
+  if (c.dtype == WERSA_BF16) return width <= 32 ? Pace{1024, 3.7f, 1.7f} : width <= 64 ? Pace{768, 5.0f, 2.1f} : Pace{512, 7.8f, 4.2f};
+  return width <= 32 ? Pace{768, 6.2f, 2.5f} : width <= 64 ? Pace{512, 10.2f, 5.0f} : Pace{256, 17.f, 17.f};
+}
 int segment_rows(const wersa_decay_desc &c) {
-  const int64_t slices = (int64_t)c.H * (c.packed ? 1 : c.B);
-  const int width = (c.dk > c.dv ? c.dk : c.dv) * (c.dtype == WERSA_BF16 ? 1 : 2);
-  const int64_t held = width <= 32 ? 1024 : width <= 64 ? 768 : width <= 128 ? 512 : 256;
-  const int64_t want = (c.packed ? held * 3 / 4 : held) / slices;   // segments of a slice
-  if (want <= 1) return c.packed ? INT32_MAX / 2 : (c.n + kChunk - 1) / kChunk * kChunk + kChunk;
-  int64_t rows = ((int64_t)c.n + want - 1) / want;
-  rows = (rows + kChunk - 1) / kChunk * kChunk;
-  return (int)(rows < 2 * kChunk ? 2 * kChunk : rows);
+  const Pace p = pace(c);
+  if (c.packed) {
+    // Lengths are not known here.  Three quarters as many whole segments as the device holds: every sequence has a partial one on top (24 prompts, 16 heads, 65536 rows: 476 us in all,
+    // 507 with as many).  Two chunks at least.
+    const int64_t want = (int64_t)p.held * 3 / 4 / c.H;
+    if (want <= 1) return INT32_MAX / 2;
+    const int64_t rows = ((c.n + want - 1) / want + kChunk - 1) / kChunk * kChunk;
+    return (int)(rows < 2 * kChunk ? 2 * kChunk : rows);
+  }
+  const int64_t slices = (int64_t)c.H * c.B, chunks = ((int64_t)c.n + kChunk - 1) / kChunk;
+  auto walk = [&](int64_t each, int64_t segments) {   // us of `segments` workgroups per slice over `each` chunks
+    const double load = (double)slices * segments / p.held;
+    return each * (load <= 1 ? std::max<double>(p.alone, p.full * load) : p.full * std::ceil(load));
+  };
+  int64_t best = chunks + 1;   // more than there are: one segment
+  double least = walk(chunks, 1);
+  auto consider = [&](int64_t each) {
+    const int64_t k = each < 1 ? 1 : (chunks + each - 1) / each;
+    if (k < 2) return;
+    const double us = walk(each, k) * (1 + 0.45 * (k - 1) / k) + 12 + (double)slices * k * c.dk * c.dv * 8 / 5e6;
+    if (us < least) least = us, best = each;
+  };
+  for (const int64_t each : {1, 2, 3, 4, 6, 8}) consider(each);
+  for (int64_t rounds = 1; rounds <= 3; ++rounds) {
+    const int64_t k = p.held * rounds / slices;
+    if (k >= 2) consider((chunks + k - 1) / k);
+  }
+  return (int)(best * kChunk);
 }
 Sequences sequences(const wersa_decay_desc &c, const int32_t *offsets) {
   Sequences s;
