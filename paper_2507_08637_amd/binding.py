@@ -500,6 +500,14 @@ def _addr(t):
     return None if t is None else t.data_ptr()
 
 
+def _on_one_gpu(first, *others):
+    """An address of host memory, or of another device's, would fault on the GPU."""
+    device = first.get_device()
+    assert device >= 0, "expect tensors on the GPU"
+    for t in others:
+        assert t is None or t.get_device() == device, "expect all tensors on one GPU"
+
+
 def _check_states(desc, slots, *states):
     """float32 (rows, H, dk, dv); rows = B, or any number with slots (B).  Returns the rows."""
     rows = desc.B
@@ -522,6 +530,7 @@ def checked_decay_desc(q, k, v, log_decay, scale, offsets, initial_state):
     desc = make_decay_desc(q, k, v, v, scale, offsets)
     _check_log_decay(log_decay, desc)
     _check_states(desc, None, initial_state)
+    _on_one_gpu(q, k, v, log_decay, offsets, initial_state)
     sb = load_library().wersa_decay_saved_bytes(ctypes.byref(desc))
     if sb == 0:   # the precise status
         _check(load_library().wersa_decay_forward(ctypes.byref(desc), *([None] * 8), 0, *([None] * 3), 0, None))
@@ -541,6 +550,7 @@ def wersa_decay_forward(q, k, v, log_decay, scale=None, offsets=None, initial_st
         assert slots is None, "with slots the states lie in a buffer of the caller's"
         final_state = torch.empty(desc.B, desc.H, desc.dk, desc.dv, dtype=torch.float32, device=q.device)
     rows = _check_states(desc, slots, initial_state, final_state)
+    _on_one_gpu(q, k, v, log_decay, offsets, initial_state, final_state, slots, out, saved, workspace)
     sb = lib.wersa_decay_saved_bytes(ctypes.byref(desc))
     if saved is not None:
         assert _nbytes(saved) >= sb, f"saved buffer holds {_nbytes(saved)} bytes, wersa_decay_saved_bytes asks for {sb}"
@@ -570,6 +580,7 @@ def wersa_decay_backward(q, k, v, log_decay, dout, saved, scale=None, offsets=No
     for name, x in (("dq", q), ("dk", k), ("dv", v)):
         _same_layout(x, grads[name])
     _check_states(desc, None, grads["dinitial_state"])
+    _on_one_gpu(q, k, v, log_decay, offsets, initial_state, dout, dfinal_state, saved, workspace, *grads.values())
     if workspace is None:
         workspace = _scratch(lib.wersa_decay_workspace_bytes(ctypes.byref(desc), 1), q, stream)
     _check(lib.wersa_decay_backward(ctypes.byref(desc), _addr(q), _addr(k), _addr(v), _addr(log_decay), _addr(offsets), _addr(initial_state),
@@ -593,6 +604,7 @@ def wersa_decay_step(q, k, v, log_decay, state, scale=None, slots=None, out=None
                                                             qb, qh, 0, kb, kh, 0, vb, vh, 0, ob, oh, 0))
     _check_log_decay(log_decay, desc)
     rows = _check_states(desc, slots, state)
+    _on_one_gpu(q, k, v, log_decay, state, slots, out)
     _check(lib.wersa_decay_step(ctypes.byref(desc), q.data_ptr(), k.data_ptr(), v.data_ptr(), log_decay.data_ptr(), state.data_ptr(), _addr(slots),
                                 rows, out.data_ptr(), _stream(stream)))
     return out
@@ -611,6 +623,7 @@ def checked_norm_args(x, weight, residual):
     if residual is not None:
         assert residual.shape == x.shape and residual.dtype == x.dtype and residual.stride(1) == 1, "the residual has x's shape and dtype"
     _dtype_code(x)
+    _on_one_gpu(x, weight, residual)
 
 
 def _norm_args(x, weight, residual, eps, r):
@@ -623,11 +636,12 @@ def _norm_args(x, weight, residual, eps, r):
         if r is None:
             r = x.new_empty((rows, cols))
         else:
-            _dense(r, x.shape, x.dtype, "r")
+            _dense(x, r, x.shape, x.dtype, "r")
     return WersaNormDesc.from_buffer_copy(_NORM_DESC.pack(rows, cols, _dtype_code(x), eps, x.stride(0), step)), r if residual is not None else None
 
 
-def _dense(t, shape, dtype, name):
+def _dense(like, t, shape, dtype, name):
+    _on_one_gpu(like, t)
     assert t.shape == shape and t.dtype == dtype and t.is_contiguous(), f"{name} is dense, {tuple(shape)} of {dtype}"
     return t
 
@@ -635,9 +649,9 @@ def _dense(t, shape, dtype, name):
 def wersa_rms_norm_forward(x, weight=None, residual=None, eps=1e-6, r=None, y=None, rstd=None, want_rstd=False, stream=None):
     """Returns (y, r, rstd): r = x + residual (x itself without one), rstd (rows) float32 or None."""
     desc, stream_out = _norm_args(x, weight, residual, eps, r)
-    y = x.new_empty(x.shape) if y is None else _dense(y, x.shape, x.dtype, "y")
+    y = x.new_empty(x.shape) if y is None else _dense(x, y, x.shape, x.dtype, "y")
     if rstd is not None:
-        _dense(rstd, x.shape[:1], torch.float32, "rstd")
+        _dense(x, rstd, x.shape[:1], torch.float32, "rstd")
     elif want_rstd:
         rstd = x.new_empty(x.shape[0], dtype=torch.float32)
     _check(load_library().wersa_rms_norm_forward(ctypes.byref(desc), x.data_ptr(), _addr(residual), _addr(weight), _addr(stream_out), y.data_ptr(),
@@ -648,8 +662,8 @@ def wersa_rms_norm_forward(x, weight=None, residual=None, eps=1e-6, r=None, y=No
 def wersa_rms_norm_eight_bit(x, weight=None, residual=None, eps=1e-6, r=None, y=None, scales=None, stream=None):
     """Returns (y, r, scales): y (rows, cols) float8_e4m3fn, to be multiplied by scales (rows) float32."""
     desc, stream_out = _norm_args(x, weight, residual, eps, r)
-    y = x.new_empty(x.shape, dtype=torch.float8_e4m3fn) if y is None else _dense(y, x.shape, torch.float8_e4m3fn, "y")
-    scales = x.new_empty(x.shape[0], dtype=torch.float32) if scales is None else _dense(scales, x.shape[:1], torch.float32, "scales")
+    y = x.new_empty(x.shape, dtype=torch.float8_e4m3fn) if y is None else _dense(x, y, x.shape, torch.float8_e4m3fn, "y")
+    scales = x.new_empty(x.shape[0], dtype=torch.float32) if scales is None else _dense(x, scales, x.shape[:1], torch.float32, "scales")
     _check(load_library().wersa_rms_norm_eight_bit(ctypes.byref(desc), x.data_ptr(), _addr(residual), _addr(weight), _addr(stream_out), y.data_ptr(),
                                                    scales.data_ptr(), _stream(stream)))
     return y, x if residual is None else stream_out, scales
@@ -665,6 +679,7 @@ def wersa_rms_norm_backward(r, rstd, dy, weight=None, dr=None, dx=None, want_dwe
     if dx is None:
         dx = torch.empty(r.shape, dtype=r.dtype, device=r.device)
     assert dx.shape == r.shape and dx.dtype == r.dtype and dx.is_contiguous()
+    _on_one_gpu(r, rstd, dy, weight, dr, dx, dweight, workspace)
     if want_dweight and dweight is None:
         dweight = torch.empty(r.shape[1], dtype=torch.float32, device=r.device)
     if dweight is not None:

@@ -130,3 +130,16 @@ def test_binding_refuses():
         binding.wersa_rms_norm_forward(x.t())
     with pytest.raises(TypeError):
         binding.wersa_rms_norm_forward(x.half())
+
+
+def test_tensors_of_the_host_are_refused():
+    """Their addresses would fault on the GPU."""
+    from paper_2507_08637_amd import autograd, binding
+    q, v, ld = torch.zeros(2, 3, 10, 32), torch.zeros(2, 3, 10, 16), torch.zeros(3)
+    for call in (lambda: binding.wersa_decay_forward(q, q, v, ld), lambda: autograd.wersa_decay_attention(q, q, v, ld),
+                 lambda: binding.wersa_decay_step(q[:, :, 0], q[:, :, 0], v[:, :, 0], ld, torch.zeros(2, 3, 32, 16)),
+                 lambda: binding.wersa_decay_backward(q, q, v, ld, v, torch.zeros(64)),
+                 lambda: binding.wersa_rms_norm_forward(q.view(-1, 32)), lambda: binding.wersa_rms_norm_eight_bit(q.view(-1, 32)),
+                 lambda: autograd.wersa_rms_norm(q), lambda: binding.wersa_rms_norm_backward(q.view(-1, 32), torch.zeros(60), q.view(-1, 32))):
+        with pytest.raises(AssertionError, match="GPU"):
+            call()

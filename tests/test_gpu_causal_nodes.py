@@ -111,3 +111,17 @@ def test_refusals(node):
         node.wersa_rms_norm(torch.zeros(2, 64, device="cuda"), torch.ones(63, device="cuda"))
     with pytest.raises(TypeError):
         node.wersa_rms_norm(torch.zeros(2, 64, device="cuda", dtype=torch.float16))
+
+
+def test_one_tensor_of_the_host_among_others_is_refused():
+    from paper_2507_08637_amd import binding
+    q, k, v = (x.detach() for x in leaves((1, 2, 10, 32), (1, 2, 10, 32), (1, 2, 10, 32)))
+    ld, offsets, slots = torch.zeros(2), torch.tensor([0, 4, 10], dtype=torch.int32), torch.tensor([0], dtype=torch.int32)
+    state = torch.zeros(1, 2, 32, 32, device="cuda")
+    for call in (lambda: binding.wersa_decay_forward(q, k, v, ld), lambda: binding.wersa_decay_forward(q, k, v, ld.cuda(), offsets=offsets),
+                 lambda: binding.wersa_decay_forward(q, k, v, ld.cuda(), final_state=state, slots=slots),
+                 lambda: binding.wersa_decay_forward(q, k, v, ld.cuda(), initial_state=state.cpu()),
+                 lambda: binding.wersa_decay_step(q[:, :, 0], k[:, :, 0], v[:, :, 0], ld.cuda(), state, slots=slots),
+                 lambda: binding.wersa_rms_norm_forward(q[0, 0], torch.ones(32)), lambda: binding.wersa_rms_norm_forward(q[0, 0], residual=q[0, 0].cpu())):
+        with pytest.raises(AssertionError, match="GPU"):
+            call()
