@@ -84,7 +84,12 @@ struct Walk {
   int64_t si, sj;           // strides of a state's rows (k) and columns (v)
   float intra, inter, gain; // factors of the chunk's products, of the state's part and of what goes into the state
   bool by_slot, reverse;
+  bool heads_first;         // the grid's order
 };
+
+// Heads that lie side by side in memory go side by side through the grid.
+__device__ __forceinline__ int slot_of(const Walk &a) { return a.heads_first ? blockIdx.y : blockIdx.x; }
+__device__ __forceinline__ int head_of(const Walk &a) { return a.heads_first ? blockIdx.x : blockIdx.y; }
 
 __device__ __forceinline__ int cache_row(const Walk &a, int b) {   // -1: none
   const int r = a.cache ? a.cache[b] : b;
@@ -119,8 +124,8 @@ struct Rows {
 };
 // Bytes past the width are none of the buffer's: joined in by `or` at the access.
 __device__ __forceinline__ uint32_t outside(int byte, int width) { return byte < width ? 0u : 0xffffffc0u; }
-// Outputs, and what the states alone are formed from, pass by the caches (aux 2: non-temporal).
-template <bool NT = false> __device__ __forceinline__ u32x4 load_piece(const Rows::Chunk &c, uint32_t at) {
+// Aux 2: non-temporal, by the caches, which keep what comes after.
+template <bool NT> __device__ __forceinline__ u32x4 load_piece(const Rows::Chunk &c, uint32_t at) {
   return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(c.b, (int)at, 0, NT ? 2 : 0));
 }
 __device__ __forceinline__ void store_piece(const Rows::Chunk &c, uint32_t at, u32x4 v) { __builtin_amdgcn_raw_buffer_store_b128(v, c.b, (int)at, 0, 2); }
@@ -183,7 +188,7 @@ template <int D> __device__ __forceinline__ f32x4 products_f32(const float *rows
 template <int D> __device__ __forceinline__ void load_own_f32(const Rows &r, int r0, uint32_t at, int g, f32x4 (&own)[D / 16]) {
   const Rows::Chunk c = r.chunk(r0);
 #pragma unroll
-  for (int j = 0; j < D / 16; ++j) own[j] = __builtin_bit_cast(f32x4, load_piece(c, (at + 64 * j - c.missing) | outside(64 * j + 16 * g, r.width)));
+  for (int j = 0; j < D / 16; ++j) own[j] = __builtin_bit_cast(f32x4, load_piece<false>(c, (at + 64 * j - c.missing) | outside(64 * j + 16 * g, r.width)));
 }
 template <int D, int THREADS, int PIECES> __device__ __forceinline__ void put_tile_f32(float *rows, int tid, const u32x4 (&p)[PIECES]) {
 #pragma unroll
@@ -319,9 +324,10 @@ __global__ __launch_bounds__(64 * f32_waves(DK, DV)) void walk_f32_kernel(Walk a
   typedef Part<DK, DV, WAVES> P4;
   extern __shared__ __align__(16) float lds[];
   float *Ks = lds, *Vs = Ks + kChunk * LK, *weight = Vs + kChunk * LV, *St = weight + kChunk;
-  const Segment seg = segment_of(a.seq, blockIdx.x);
+  const int slot = slot_of(a), h = head_of(a);
+  const Segment seg = segment_of(a.seq, slot);
   if (seg.rows < 0) return;
-  const int h = blockIdx.y, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const bool last = a.reverse ? seg.s == 0 : seg.s == a.seq.segments(seg.b) - 1;
   if (STATES && last) return;   // nothing begins with what the last one adds
   const P4 part(wave);
@@ -333,7 +339,7 @@ __global__ __launch_bounds__(64 * f32_waves(DK, DV)) void walk_f32_kernel(Walk a
 
   f32x4 S[P4::RT][P4::CW];   // S[rt][ct][i] is row row0 + 16 rt + 4 g + i, column col0 + 16 ct + c
   const int own = cache_row(a, seg.b);
-  const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
+  const int64_t from = a.by_slot ? (int64_t)slot : own;
   const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
   each_of_state(a, S, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const WeightsF32 weights(a, l2, part.t, g, c);
@@ -376,7 +382,7 @@ __global__ __launch_bounds__(64 * f32_waves(DK, DV)) void walk_f32_kernel(Walk a
   }
 
   float *fin = nullptr;
-  if (STATES) fin = a.fin + ((int64_t)blockIdx.x * a.H + h) * state_size;
+  if (STATES) fin = a.fin + ((int64_t)slot * a.H + h) * state_size;
   else if (last && a.fin && own >= 0) fin = a.fin + ((int64_t)own * a.H + h) * state_size;
   if (fin) each_of_state(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
 }
@@ -395,9 +401,10 @@ __global__ __launch_bounds__(64 * f32_waves(DK, DV)) void back_f32_kernel(Walk a
   constexpr int KT = DK / 16, CT = P4::CT;
   extern __shared__ __align__(16) float lds[];
   float *Qs = lds, *Ds = Qs + kChunk * LK, *weight = Ds + kChunk * LV, *Gt = weight + kChunk;
-  const Segment seg = segment_of(a.seq, blockIdx.x);
+  const int slot = slot_of(a), h = head_of(a);
+  const Segment seg = segment_of(a.seq, slot);
   if (seg.rows < 0) return;
-  const int h = blockIdx.y, tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const P4 part(wave);
   const int vcol = DV / P4::HALVES * part.half, kcol = DK / P4::HALVES * part.half;   // of dv and of dk
   const Rows qr = rows_of(a.k, a.sk, seg, a, h, a.kw, 4), dr = rows_of(a.v, a.sv, seg, a, h, a.vw, 4), kr = rows_of(b.k, b.sk, seg, a, h, a.kw, 4),
@@ -406,7 +413,7 @@ __global__ __launch_bounds__(64 * f32_waves(DK, DV)) void back_f32_kernel(Walk a
   const int64_t state_size = (int64_t)a.kw * a.vw;
 
   f32x4 G[P4::RT][P4::CW];
-  const int64_t from = a.by_slot ? (int64_t)blockIdx.x : seg.b;
+  const int64_t from = a.by_slot ? (int64_t)slot : seg.b;
   const float *init = a.init ? a.init + (from * a.H + h) * state_size : nullptr;
   each_of_state(a, G, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const WeightsF32 weights(a, l2, part.t, g, c);
@@ -715,7 +722,7 @@ __device__ __forceinline__ void update_state(const Part<DK, DV> &part, f32x4 (&S
 // take the error of a result from 0.0023 to 0.0020 of it, for 4 %); what goes into the state is not.  Bound by memory: width 128, 32 slices of 65536 rows, 465 us, 4.6 TB/s; width 64, 8
 // slices of 131072, 110 us, 4.9 TB/s; forming states alone 213 us, 4.7 TB/s, and 57 us, 4.5 TB/s.  A build that only loads and stores takes as long: every workgroup streams through a place of
 // its own in four tensors, which a copy (5.7 TB/s) does not.
-template <int DK, int DV, bool FULL, bool STATES>
+template <int DK, int DV, bool FULL, bool STATES, bool NT>
 __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(Walk a) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;   // pieces of a thread
   typedef Part<DK, DV> P4;
@@ -726,9 +733,10 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) vo
   // in LDS: K, V, the columns of the state as rows, the waves' own parts
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes;
   constexpr uint32_t Ks = 0, Vs = 2 * kChunk * DK, St = SETS * SET;
-  const Segment seg = segment_of(a.seq, blockIdx.x);
+  const int slot = slot_of(a), h = head_of(a);
+  const Segment seg = segment_of(a.seq, slot);
   if (seg.rows < 0) return;
-  const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const P4 part(w);
   const int t = part.t;
   const uint32_t stage = lds + SETS * SET + (STATES ? 0 : 2 * DV * DK) + STAGE * w;
@@ -741,7 +749,7 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) vo
 
   f32x4 S[P4::RT][P4::CW];   // S[rt][ct][i] is row row0 + 16 rt + 4 g + i, column col0 + 16 ct + c
   const int own = cache_row(a, seg.b);
-  const int64_t from = a.by_slot ? (int64_t)blockIdx.x : own;
+  const int64_t from = a.by_slot ? (int64_t)slot : own;
   const float *init = STATES || !a.init || from < 0 ? nullptr : a.init + (from * a.H + h) * state_size;
   each_of_state(a, S, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const Weights weights(a, l2, t, g, c);
@@ -753,13 +761,13 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) vo
   const OwnRows<DV, FULL> oo(orow, stage, t, lane);
   const uint32_t kput = lds + Ks + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), vput = lds + Vs + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
   auto request = [&](int r0, int set) {
-    kp.template load<STATES>(kr, r0, rk[set]);
-    vp.template load<STATES>(vr, r0, rv[set]);
+    kp.template load<NT>(kr, r0, rk[set]);
+    vp.template load<NT>(vr, r0, rv[set]);
   };
 
 #pragma unroll
   for (int set = 0; set < SETS; ++set) request(set * kChunk, set);
-  if (!STATES) qo.pieces.template load<false>(qr, 0, rq);
+  if (!STATES) qo.pieces.template load<NT>(qr, 0, rq);
   for (int r1 = 0; r1 < seg.rows; r1 += SETS * kChunk) {
 #pragma unroll
     for (int set = 0; set < SETS; ++set) {
@@ -785,7 +793,7 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) vo
           return acc * weights.reach;
         });
         oo.out(orow, r0);
-        qo.pieces.template load<false>(qr, r0 + kChunk, rq);
+        qo.pieces.template load<NT>(qr, r0 + kChunk, rq);
       }
       // the walk that forms states only weights rows by the segment's end, and has no sum to scale
       put_weights(stage, lane, a, l2, STATES ? seg.rows - 1 - r0 : rows - 1);
@@ -795,13 +803,13 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) vo
   }
 
   float *fin = nullptr;
-  if (STATES) fin = a.fin + ((int64_t)blockIdx.x * a.H + h) * state_size;
+  if (STATES) fin = a.fin + ((int64_t)slot * a.H + h) * state_size;
   else if (last && a.fin && own >= 0) fin = a.fin + ((int64_t)own * a.H + h) * state_size;
   if (fin) each_of_state(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
 }
 
 // As back_f32_kernel, for bf16 tensors.  Width 128, 32 slices of 65536 rows: 680 us, 4.7 TB/s; two walks took 2 x 502.
-template <int DK, int DV, bool FULL>
+template <int DK, int DV, bool FULL, bool NT>
 __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : 2) void back_bf16_kernel(Walk a, Back b) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;
   typedef Part<DK, DV> P4;
@@ -809,9 +817,10 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : 2) void back_bf16_kernel(W
   extern __shared__ __align__(16) unsigned char lds_bytes[];
   const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) unsigned char *)lds_bytes;
   constexpr uint32_t Qs = 0, Ds = 2 * kChunk * DK, Gt = Ds + 2 * kChunk * DV;
-  const Segment seg = segment_of(a.seq, blockIdx.x);
+  const int slot = slot_of(a), h = head_of(a);
+  const Segment seg = segment_of(a.seq, slot);
   if (seg.rows < 0) return;
-  const int h = blockIdx.y, tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, g = lane >> 4, c = lane & 15;
   const P4 part(w);
   const int t = part.t;
   const uint32_t stage = lds + Gt + 2 * DV * DK + STAGE * w;
@@ -821,7 +830,7 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : 2) void back_bf16_kernel(W
   const int64_t state_size = (int64_t)a.kw * a.vw;
 
   f32x4 G[P4::RT][P4::CW];
-  const int64_t from = a.by_slot ? (int64_t)blockIdx.x : seg.b;
+  const int64_t from = a.by_slot ? (int64_t)slot : seg.b;
   const float *init = a.init ? a.init + (from * a.H + h) * state_size : nullptr;
   each_of_state(a, G, part, g, c, [&](float, bool there, int64_t at) { return init && there ? init[at] : 0.f; });
   const Weights weights(a, l2, t, g, c);
@@ -833,12 +842,12 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : 2) void back_bf16_kernel(W
   const OwnRows<DV, FULL> vo(vr, stage, t, lane), dvo(dvr, stage, t, lane);
   const uint32_t qput = lds + Qs + lds_at<DK, false>(tid / (DK / 8), tid % (DK / 8) * 8), dput = lds + Ds + lds_at<DV, false>(tid / (DV / 8), tid % (DV / 8) * 8);
   auto request = [&](int r0) {
-    qp.template load<false>(qr, r0, rq);
-    dp.template load<false>(dr, r0, rd);
+    qp.template load<NT>(qr, r0, rq);
+    dp.template load<NT>(dr, r0, rd);
   };
   auto request_own = [&](int r0) {
-    ko.pieces.template load<false>(kr, r0, rk);
-    vo.pieces.template load<false>(vr, r0, rv);
+    ko.pieces.template load<NT>(kr, r0, rk);
+    vo.pieces.template load<NT>(vr, r0, rv);
   };
 
   request(0);
@@ -1043,6 +1052,20 @@ Sequences sequences(const wersa_decay_desc &c, const int32_t *offsets) {
   s.segs = c.n > 0 ? (c.n + s.seg - 1) / s.seg : 1;
   return s;
 }
+// How walks go through memory, where a head's rows are whole lines of 128 bytes (others share lines with their neighbours, and take up to twice as long either way).
+bool whole_lines(const wersa_decay_desc &c) {
+  const int e = c.dtype == WERSA_F32 ? 4 : 2;
+  return c.dk * e % 128 == 0 && c.dv * e % 128 == 0;
+}
+// Heads that lie side by side in a row go side by side through the grid: 24 packed prompts, 16 heads, 65536 rows, width 128 in bf16: walk 336 us, 304 so; float32, width 32, 128 slices of
+// 4000 rows: 68, 65.  With heads apart in memory the walks would take longer so (loads and stores alone: 380, 448).
+bool heads_first(const wersa_decay_desc &c, const Sequences &s) { return c.stride_v[1] < c.stride_v[2] && whole_lines(c) && s.slots() <= 65535; }   // (blockIdx.y)
+// Walks in bf16 read by the caches what these would not keep to the next kernel: 8 slices of 131072 rows, width 64 (134 MB a tensor), walk 112 us, 100 so; 1024 of 500 rows (65 MB) would take
+// 66 for 61.  The walk that forms states never does: the next one finds part of what it read (the same 8 slices: 117 us for 112).
+constexpr int64_t kLastLevelCache = 256 << 20;
+bool passes_caches(const wersa_decay_desc &c) {
+  return whole_lines(c) && ((int64_t)c.packed * c.n + (1 - c.packed) * (int64_t)c.B * c.n) * c.H * (2 * c.dk + c.dv) * 2 > kLastLevelCache;
+}
 int64_t state_slots_of(const wersa_decay_desc &c) {   // 0: every sequence is one segment
   const int seg = segment_rows(c);
   if (c.n <= seg) return 0;
@@ -1077,7 +1100,7 @@ template <typename K, typename... Args> bool launch(const char *name, K kern, in
   if (smem > 65536 &&
       hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess)
     return false;
-  WERSA_STAGE(name, st, kern<<<dim3(a.seq.slots(), a.H), threads, smem, st>>>(a, more...));
+  WERSA_STAGE(name, st, kern<<<a.heads_first ? dim3(a.H, a.seq.slots()) : dim3(a.seq.slots(), a.H), threads, smem, st>>>(a, more...));
   return true;
 }
 constexpr size_t f32_lds(int dk, int dv, bool state) { return sizeof(float) * (kChunk * (dk + 4 + dv + 4 + 1) + (state ? dv * (dk + 4) : 0)); }
@@ -1085,8 +1108,9 @@ template <int DK, int DV, bool STATES> bool launch_walk_as(const wersa_decay_des
   const char *name = STATES ? "wersa_decay_states" : "wersa_decay_walk";
   if (c.dtype == WERSA_F32) return launch(name, &walk_f32_kernel<DK, DV, STATES>, 64 * f32_waves(DK, DV), f32_lds(DK, DV, !STATES), a, st);
   constexpr size_t sets = STATES ? 2 : 1, smem = 2 * (sets * kChunk * (DK + DV) + (STATES ? 0 : DV * DK)) + 4 * (STATES ? 256 : 32 * (DK > DV ? DK : DV));
-  return a.kw == DK && a.vw == DV ? launch(name, &walk_bf16_kernel<DK, DV, true, STATES>, 256, smem, a, st)
-                                  : launch(name, &walk_bf16_kernel<DK, DV, false, STATES>, 256, smem, a, st);
+  if (a.kw != DK || a.vw != DV) return launch(name, &walk_bf16_kernel<DK, DV, false, STATES, false>, 256, smem, a, st);
+  return !STATES && DK > 32 && passes_caches(c) ? launch(name, &walk_bf16_kernel<DK, DV, true, STATES, !STATES && (DK > 32)>, 256, smem, a, st)
+                                                : launch(name, &walk_bf16_kernel<DK, DV, true, STATES, false>, 256, smem, a, st);
 }
 template <bool STATES> bool launch_walk(const wersa_decay_desc &c, const Walk &a, hipStream_t st) {
   if (a.kw <= 32 && a.vw <= 32) return launch_walk_as<32, 32, STATES>(c, a, st);
@@ -1096,8 +1120,9 @@ template <bool STATES> bool launch_walk(const wersa_decay_desc &c, const Walk &a
 template <int DK, int DV> bool launch_back_as(const wersa_decay_desc &c, const Walk &a, const Back &b, hipStream_t st) {
   if (c.dtype == WERSA_F32) return launch("wersa_decay_back", &back_f32_kernel<DK, DV>, 64 * f32_waves(DK, DV), f32_lds(DK, DV, true), a, st, b);
   constexpr size_t smem = 2 * (kChunk * (DK + DV) + DV * DK) + 4 * 32 * (DK > DV ? DK : DV);
-  return a.kw == DK && a.vw == DV ? launch("wersa_decay_back", &back_bf16_kernel<DK, DV, true>, 256, smem, a, st, b)
-                                  : launch("wersa_decay_back", &back_bf16_kernel<DK, DV, false>, 256, smem, a, st, b);
+  if (a.kw != DK || a.vw != DV) return launch("wersa_decay_back", &back_bf16_kernel<DK, DV, false, false>, 256, smem, a, st, b);
+  return DK > 32 && passes_caches(c) ? launch("wersa_decay_back", &back_bf16_kernel<DK, DV, true, (DK > 32)>, 256, smem, a, st, b)
+                                     : launch("wersa_decay_back", &back_bf16_kernel<DK, DV, true, false>, 256, smem, a, st, b);
 }
 bool launch_back(const wersa_decay_desc &c, const Walk &a, const Back &b, hipStream_t st) {
   if (a.kw <= 32 && a.vw <= 32) return launch_back_as<32, 32>(c, a, b, st);
@@ -1146,6 +1171,7 @@ wersa_status wersa_decay_forward(const wersa_decay_desc *desc, const void *q, co
   a.log_decay = log_decay;
   a.init = initial_state, a.cache = slots, a.cache_rows = state_slots;
   a.seq = sequences(c, offsets);
+  a.heads_first = heads_first(c, a.seq);
   a.H = c.H, a.kw = c.dk, a.vw = c.dv, a.si = c.dv, a.sj = 1;
   a.intra = a.inter = c.scale, a.gain = 1.f;
   if (split) {
@@ -1179,6 +1205,7 @@ wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, c
   a.log_decay = log_decay;
   a.cache_rows = c.B;
   a.seq = sequences(c, offsets);
+  a.heads_first = heads_first(c, a.seq);
   a.H = c.H;
   const Strides sq = strides(c.stride_q), sk = strides(c.stride_k), sv = strides(c.stride_v), so = strides(c.stride_o);
   // dq: states transposed

@@ -409,3 +409,57 @@ def test_step_of_many_states(B, H, dk, dv):
     out = binding.wersa_decay_step(q, k, v, ld, state, scale=0.5)
     close(state, want.cpu(), torch.float32, "state")
     close(out, (0.5 * (q.double().unsqueeze(3) * want).sum(2)).cpu(), torch.float32, "out")
+
+
+@pytest.mark.parametrize("layout", ["bhnd", "bnhd"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_orders_of_the_grid(dtype, layout):
+    """Heads apart in memory or side by side, in several segments."""
+    from paper_2507_08637_amd import binding
+    p = make(2, 3, 700, 64, 64, dtype, seed=31, layout=layout, state=True, grads=True)
+    g, ref = to(p), reference(p, 0.125, grads=True)
+    out, final, saved = binding.wersa_decay_forward(g["q"], g["k"], g["v"], g["ld"], 0.125, initial_state=g["S0"], want_state=True, want_saved=True)
+    got = binding.wersa_decay_backward(g["q"], g["k"], g["v"], g["ld"], g["dout"], saved, 0.125, initial_state=g["S0"], dfinal_state=g["dfinal"], want_dinitial=True)
+    close(out, ref["out"], dtype, "out")
+    close(final, ref["final"], torch.float32, "final")
+    for name in ("dq", "dk", "dv"):
+        close(got[name], ref[name], dtype, name)
+    close(got["dinitial_state"], ref["dS0"], torch.float32, "dS0")
+
+
+def test_more_sequences_than_a_grid_has_in_its_second_dimension():
+    """65535 packed sequences of no, one or two rows, heads side by side."""
+    from paper_2507_08637_amd import binding
+    H, d, B = 2, 64, 65535
+    g = torch.Generator().manual_seed(32)
+    lengths = torch.randint(0, 3, (B,), generator=g)
+    ends = torch.cumsum(lengths, 0)
+    n = int(ends[-1])
+    q, k, v = (torch.randn(1, n, H, d, generator=g).cuda().permute(0, 2, 1, 3) for _ in range(3))
+    ld = decays(H).cuda()
+    offsets = torch.cat([torch.zeros(1, dtype=torch.int64), ends]).int().cuda()
+    out = binding.wersa_decay_forward(q, k, v, ld, 0.125, offsets=offsets)[0]
+    second = torch.zeros(n, dtype=torch.bool)
+    second[ends[lengths == 2] - 1] = True
+    wide = [x.double().cpu()[0] for x in (q, k, v)]
+    want = (wide[0] * wide[1]).sum(-1, keepdim=True) * wide[2]
+    before = [x.roll(1, 1) for x in wide]
+    want += torch.where(second[None, :, None], ld.double().cpu().exp()[:, None, None] * (wide[0] * before[1]).sum(-1, keepdim=True) * before[2], 0.)
+    close(out[0], 0.125 * want, torch.float32, "out")
+
+
+def test_tensors_that_pass_the_caches():
+    """A batch whose q, k and v together are larger than the last-level cache against its halves, which are not."""
+    from paper_2507_08637_amd import autograd
+    g = torch.Generator(device="cuda").manual_seed(33)
+    x = [torch.randn(2, 70000, 8, 64, generator=g, device="cuda", dtype=torch.bfloat16).permute(0, 2, 1, 3) for _ in range(4)]
+    ld = decays(8).cuda()
+
+    def step(*t):
+        leaves = [y.detach().requires_grad_() for y in t[:3]]
+        out = autograd.wersa_decay_attention(*leaves, ld, 0.125)[0]
+        return [out.detach()] + list(torch.autograd.grad(out, leaves, t[3]))
+
+    whole, halves = step(*x), [step(*(y[i:i + 1] for y in x)) for i in range(2)]
+    for a, b, what in zip(whole, zip(*halves), ("out", "dq", "dk", "dv")):
+        close(a, torch.cat(b).double().cpu(), torch.bfloat16, what)   # (both have the same roundings, up to the order of a state's sums and where the last chunks begin)
