@@ -315,7 +315,7 @@ __device__ __forceinline__ void weighted_rows_f32(const float *rows, const Rows 
 
 // Weights are formed as their transpose (the chunk's rows down the registers, own rows on the lanes), which is the layout that the product with V takes them in.
 // Eight waves at width 128, where LDS holds one workgroup to a compute unit: two to a SIMD, which form their rows' weights twice.
-// Up to width 32 near memory (128 slices of 4000 rows: 67 us, 3.9 TB/s), above by the matrix units: 32 slices of 8192 rows, width 64, 82 us, 3.3 TB/s; 16 slices, width 128, 136 us, 2.0 TB/s,
+// Up to width 32 near memory (128 slices of 4000 rows: 64 us, 4.1 TB/s), above by the matrix units: 32 slices of 8192 rows, width 64, 82 us, 3.3 TB/s; 16 slices, width 128, 136 us, 2.0 TB/s,
 // about 92 of the 157 TFLOP/s that float32 matrix instructions have at their nominal clock.
 constexpr int f32_waves(int dk, int dv) { return dk > 64 || dv > 64 ? 8 : 4; }
 template <int DK, int DV, bool STATES>
@@ -719,9 +719,8 @@ __device__ __forceinline__ void update_state(const Part<DK, DV> &part, f32x4 (&S
 }
 
 // As walk_f32_kernel, for bf16 tensors.  P and the state as an operand of the output are rounded to bf16, like the output (each 2^-9 of a result in the root mean square; P in two terms would
-// take the error of a result from 0.0023 to 0.0020 of it, for 4 %); what goes into the state is not.  Bound by memory: width 128, 32 slices of 65536 rows, 465 us, 4.6 TB/s; width 64, 8
-// slices of 131072, 110 us, 4.9 TB/s; forming states alone 213 us, 4.7 TB/s, and 57 us, 4.5 TB/s.  A build that only loads and stores takes as long: every workgroup streams through a place of
-// its own in four tensors, which a copy (5.7 TB/s) does not.
+// take the error of a result from 0.0023 to 0.0020 of it, for 4 %); what goes into the state is not.  Bound by memory: width 128, 32 slices of 65536 rows, 460 us, 4.7 TB/s (416 without the update
+// of the state; loads and stores alone 380 to 400); width 64, 8 slices of 131072, 100 us, 5.4 TB/s; forming states alone 213 us, 5.0 TB/s (199 without the products), and 57 us, 4.7 TB/s.
 template <int DK, int DV, bool FULL, bool STATES, bool NT>
 __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(Walk a) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;   // pieces of a thread
@@ -808,7 +807,7 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) vo
   if (fin) each_of_state(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
 }
 
-// As back_f32_kernel, for bf16 tensors.  Width 128, 32 slices of 65536 rows: 680 us, 4.7 TB/s; two walks took 2 x 502.
+// As back_f32_kernel, for bf16 tensors.  Width 128, 32 slices of 65536 rows: 670 us, 4.8 TB/s (630 without the update of the state); two walks took 2 x 502.
 template <int DK, int DV, bool FULL, bool NT>
 __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : 2) void back_bf16_kernel(Walk a, Back b) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;
@@ -1016,9 +1015,9 @@ Pace pace(const wersa_decay_desc &c) {
 int segment_rows(const wersa_decay_desc &c) {
   const Pace p = pace(c);
   if (c.packed) {
-    // Lengths are not known here.  Three quarters as many whole segments as the device holds: every sequence has a partial one on top (24 prompts, 16 heads, 65536 rows: 476 us in all,
-    // 507 with as many).  Two chunks at least.
-    const int64_t want = (int64_t)p.held * 3 / 4 / c.H;
+    // Lengths are not known here.  Seven eighths as many whole segments as the device holds: every sequence has a partial one on top.  Geometric mean of nine batches of 8 to 60 prompts, widths 32 to
+    // 128, with six draws of long-tailed lengths each: 125 us, 138 with five eighths, 129 with six, 135 with eight, 139 with nine, 132 with twelve.  Two chunks at least.
+    const int64_t want = (int64_t)p.held * 7 / 8 / c.H;
     if (want <= 1) return INT32_MAX / 2;
     const int64_t rows = ((c.n + want - 1) / want + kChunk - 1) / kChunk * kChunk;
     return (int)(rows < 2 * kChunk ? 2 * kChunk : rows);
