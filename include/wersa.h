@@ -225,7 +225,8 @@ int64_t wersa_block_workspace_offset(const wersa_desc *desc, int which);
  * over a whole sequence (wersa_decay_forward), its derivative (wersa_decay_backward), and one token at a time on a
  * cache of states (wersa_decay_step).  q and k are (B, H, n, dk), v and out (B, H, n, dv), each at strides of its own
  * (batch, head, row; in elements; columns contiguous); dq, dk, dv and dout are laid out like q, k, v and out.  Any
- * element-aligned pointer is taken.
+ * element-aligned pointer is taken.  Rows do not overlap: a row's stride is at least the width, and at most 2^24; with n = 1 it is
+ * not read.
  *   packed   0: B sequences of n rows each; offsets is NULL.
  *            1: B sequences of any lengths (zero among them) one behind the other in tensors with one batch entry of n
  *               rows: sequence b is rows offsets[b] .. offsets[b + 1] - 1 (B + 1 device integers that do not decrease; the

@@ -1094,7 +1094,8 @@ wersa_status validate(const wersa_decay_desc *c) {
   return WERSA_OK;
 }
 bool misaligned(const void *p, size_t a) { return ((uintptr_t)p % a) != 0; }
-Strides strides(const int64_t *s) { return Strides{s[0], s[1], s[2]}; }
+// A lone row's stride may be anything (0, one element, past 32 bits). Rows that are not there are told from it by their distance from it: they get the width.
+Strides strides(const int64_t *s, const wersa_decay_desc &c, int width) { return Strides{s[0], s[1], c.n > 1 ? s[2] : width}; }
 template <typename K, typename... Args> bool launch(const char *name, K kern, int threads, size_t smem, const Walk &a, hipStream_t st, Args... more) {
   if (smem > 65536 &&
       hipFuncSetAttribute(reinterpret_cast<const void *>(kern), hipFuncAttributeMaxDynamicSharedMemorySize, (int)smem) != hipSuccess)
@@ -1166,7 +1167,7 @@ wersa_status wersa_decay_forward(const wersa_decay_desc *desc, const void *q, co
   hipStream_t st = (hipStream_t)hip_stream;
   Walk a{};
   a.q = q, a.k = k, a.v = v, a.o = out;
-  a.sq = strides(c.stride_q), a.sk = strides(c.stride_k), a.sv = strides(c.stride_v), a.so = strides(c.stride_o);
+  a.sq = strides(c.stride_q, c, c.dk), a.sk = strides(c.stride_k, c, c.dk), a.sv = strides(c.stride_v, c, c.dv), a.so = strides(c.stride_o, c, c.dv);
   a.log_decay = log_decay;
   a.init = initial_state, a.cache = slots, a.cache_rows = state_slots;
   a.seq = sequences(c, offsets);
@@ -1206,7 +1207,7 @@ wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, c
   a.seq = sequences(c, offsets);
   a.heads_first = heads_first(c, a.seq);
   a.H = c.H;
-  const Strides sq = strides(c.stride_q), sk = strides(c.stride_k), sv = strides(c.stride_v), so = strides(c.stride_o);
+  const Strides sq = strides(c.stride_q, c, c.dk), sk = strides(c.stride_k, c, c.dk), sv = strides(c.stride_v, c, c.dv), so = strides(c.stride_o, c, c.dv);
   // dq: states transposed
   Walk f = a;
   f.q = dout, f.k = v, f.v = k, f.o = dq;
@@ -1244,8 +1245,8 @@ wersa_status wersa_decay_step(const wersa_decay_desc *desc, const void *q, const
   if (c.n != 1 || c.packed || !q || !k || !v || !log_decay || !state || !out) return WERSA_ERR_INVALID_ARG;
   if (state_slots < (slots ? 1 : c.B) || misaligned(state, 16)) return WERSA_ERR_INVALID_ARG;
   hipStream_t st = (hipStream_t)hip_stream;
-  const Step a{q, k, v, out, strides(c.stride_q), strides(c.stride_k), strides(c.stride_v), strides(c.stride_o), log_decay, state, slots,
-               state_slots, c.H, c.dk, c.dv, c.scale};
+  const Step a{q, k, v, out, strides(c.stride_q, c, c.dk), strides(c.stride_k, c, c.dk), strides(c.stride_v, c, c.dv), strides(c.stride_o, c, c.dv), log_decay,
+               state, slots, state_slots, c.H, c.dk, c.dv, c.scale};
   auto launch = [&](auto w, auto nt) {
     constexpr int W = decltype(w)::value;
     constexpr bool NT = decltype(nt)::value;
