@@ -260,6 +260,9 @@ wersa_status wersa_decay_forward(const wersa_decay_desc *desc, const void *q, co
                                  float *final_state, const int32_t *slots, int32_t state_slots, void *out, void *saved,
                                  void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* Zeros to the rows of out that are of no sequence. */
+wersa_status wersa_decay_clear(const wersa_decay_desc *desc, const int32_t *offsets, void *out, void *hip_stream);
+
 wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, const void *k, const void *v,
                                   const float *log_decay, const int32_t *offsets, const float *initial_state,
                                   const void *dout, const float *dfinal_state, const void *saved, void *dq, void *dk,

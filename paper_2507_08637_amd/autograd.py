@@ -43,7 +43,7 @@ def _load_node():
         node.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.wersa_forward, lib.wersa_backward, lib.wersa_workspace_bytes,
                                                                     lib.wersa_saved_bytes, lib.wersa_selected_path)))
         node.bind_causal([ctypes.cast(f, ctypes.c_void_p).value for f in (
-            lib.wersa_decay_forward, lib.wersa_decay_backward, lib.wersa_decay_workspace_bytes, lib.wersa_decay_saved_bytes,
+            lib.wersa_decay_forward, lib.wersa_decay_clear, lib.wersa_decay_backward, lib.wersa_decay_workspace_bytes, lib.wersa_decay_saved_bytes,
             lib.wersa_rms_norm_forward, lib.wersa_rms_norm_backward, lib.wersa_rms_norm_workspace_bytes)])
         _node = node
     return _node
@@ -134,7 +134,8 @@ def _rows_apart(x):
 
 
 def wersa_decay_attention(q, k, v, log_decay, scale=None, initial_state=None, offsets=None):
-    """Causal linear attention with a decay for each head.  Returns (out, final states (B, H, dk, dv) in float32)."""
+    """Causal linear attention with a decay for each head.  Returns (out, final states (B, H, dk, dv) in float32).  Rows of no sequence (offsets that
+    begin behind the first row or end before the last one) are zeros in out and in the gradients, whatever they hold in q, k, v and out's gradient."""
     q, k, v = _rows_apart(q), _rows_apart(k), _rows_apart(v)
     node = _load_node() if _node is None else _node
     if not node or torch.jit.is_tracing():

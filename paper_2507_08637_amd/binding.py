@@ -24,7 +24,8 @@ EXPORTS = ["wersa_workspace_bytes", "wersa_saved_bytes", "wersa_forward", "wersa
            "wersa_block_workspace_bytes", "wersa_block_saved_bytes", "wersa_block_saved_offset",
            "wersa_block_workspace_offset",
            "wersa_block_forward", "wersa_block_backward",
-           "wersa_decay_workspace_bytes", "wersa_decay_saved_bytes", "wersa_decay_forward", "wersa_decay_backward", "wersa_decay_step",
+           "wersa_decay_workspace_bytes", "wersa_decay_saved_bytes", "wersa_decay_forward", "wersa_decay_clear", "wersa_decay_backward",
+           "wersa_decay_step",
            "wersa_rms_norm_forward", "wersa_rms_norm_eight_bit", "wersa_rms_norm_workspace_bytes", "wersa_rms_norm_backward"]
 
 
@@ -109,6 +110,8 @@ def load_library():
     lib.wersa_decay_saved_bytes.argtypes = [ddp]
     lib.wersa_decay_forward.restype = ctypes.c_int
     lib.wersa_decay_forward.argtypes = [ddp] + [vp] * 8 + [ctypes.c_int32] + [vp] * 3 + [ctypes.c_size_t, vp]
+    lib.wersa_decay_clear.restype = ctypes.c_int
+    lib.wersa_decay_clear.argtypes = [ddp] + [vp] * 3
     lib.wersa_decay_backward.restype = ctypes.c_int
     lib.wersa_decay_backward.argtypes = [ddp] + [vp] * 14 + [ctypes.c_size_t, vp]
     lib.wersa_decay_step.restype = ctypes.c_int
@@ -540,8 +543,10 @@ def checked_decay_desc(q, k, v, log_decay, scale, offsets, initial_state):
 def wersa_decay_forward(q, k, v, log_decay, scale=None, offsets=None, initial_state=None, final_state=None, slots=None, out=None,
                         want_state=False, want_saved=False, saved=None, workspace=None, stream=None):
     """Returns (out, final_state, saved).  final_state: a buffer to write, or want_state=True for a new one (else None);
-    want_saved=True leaves what wersa_decay_backward needs (else None)."""
+    want_saved=True leaves what wersa_decay_backward needs (else None).  Rows of no sequence are zeros in a new out, and left as they are in
+    the caller's."""
     lib = load_library()
+    clear = out is None and offsets is not None
     if out is None:
         out = torch.empty_strided(v.shape, v.stride(), dtype=v.dtype, device=v.device)
     desc = make_decay_desc(q, k, v, out, scale, offsets)
@@ -562,12 +567,14 @@ def wersa_decay_forward(q, k, v, log_decay, scale=None, offsets=None, initial_st
     _check(lib.wersa_decay_forward(ctypes.byref(desc), _addr(q), _addr(k), _addr(v), _addr(log_decay), _addr(offsets), _addr(initial_state),
                                    _addr(final_state), _addr(slots), rows, _addr(out), _addr(saved), _addr(workspace),
                                    0 if workspace is None else _nbytes(workspace), _stream(stream)))
+    if clear:
+        _check(lib.wersa_decay_clear(ctypes.byref(desc), _addr(offsets), _addr(out), _stream(stream)))
     return out, final_state, saved
 
 
 def wersa_decay_backward(q, k, v, log_decay, dout, saved, scale=None, offsets=None, initial_state=None, dfinal_state=None,
                          want_dinitial=False, workspace=None, stream=None, grads=None):
-    """Returns dict(dq, dk, dv, dinitial_state).  `grads` may be a dict from an earlier call: its tensors are then overwritten."""
+    """Returns dict(dq, dk, dv, dinitial_state); rows of no sequence are zeros.  `grads` may be a dict from an earlier call: its tensors are then overwritten."""
     lib = load_library()
     desc = make_decay_desc(q, k, v, dout, scale, offsets)
     _check_log_decay(log_decay, desc)

@@ -928,6 +928,26 @@ __global__ __launch_bounds__(256) void scan_kernel(Walk a, float *local) {
   }
 }
 
+// Packed sequences lie one behind the other: rows of none are those before the first one and those behind the last one. Zeros to them, for
+// nothing else writes them: 16 bytes to a thread, so far as there are any.
+struct Outside {
+  void *to[3];
+  Strides stride[3];
+  int width[3];             // bytes
+  int element;
+};
+__global__ __launch_bounds__(256) void clear_kernel(Sequences seq, Outside a) {
+  typedef u32x4 u32x4_any __attribute__((aligned(2)));
+  const int which = blockIdx.z, h = blockIdx.y, per_row = a.width[which] / 16;
+  const int first = seq.begin(0), last = max(first, min(max(seq.offsets[seq.B], 0), seq.n));
+  const int64_t pieces = (int64_t)(first + seq.n - last) * per_row;
+  char *to = (char *)a.to[which] + h * a.stride[which].h * a.element;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
+    const int64_t at = i / per_row, row = at < first ? at : at + (last - first);
+    *(u32x4_any *)(to + row * a.stride[which].n * a.element + i % per_row * 16) = u32x4{0, 0, 0, 0};
+  }
+}
+
 // ---- one token -------------------------------------------------------------------------------------
 // S <- lambda S + k v^T, o = scale q^T S.  Bound by the state's way through memory.  A workgroup has W columns of a state, W / 4 threads to a
 // row (16 bytes each), all rows of a thread requested before the first is used.  NT: states that will not be in the last-level cache when their next token comes pass by it
@@ -1129,6 +1149,14 @@ bool launch_back(const wersa_decay_desc &c, const Walk &a, const Back &b, hipStr
   if (a.kw <= 64) return a.vw <= 64 ? launch_back_as<64, 64>(c, a, b, st) : launch_back_as<64, 128>(c, a, b, st);
   return a.vw <= 64 ? launch_back_as<128, 64>(c, a, b, st) : launch_back_as<128, 128>(c, a, b, st);
 }
+void launch_clear(const wersa_decay_desc &c, const Sequences &seq, int tensors, Outside a, hipStream_t st) {
+  if (!c.packed || c.n == 0) return;
+  a.element = c.dtype == WERSA_F32 ? 4 : 2;
+  const int64_t most = (int64_t)c.n * std::max(c.dk, c.dv) * a.element / 16;
+  const int64_t across = std::min<int64_t>((most + 255) / 256, std::max(1, 2048 / (c.H * tensors)));
+  for (int i = 0; i < tensors; ++i) a.width[i] *= a.element;
+  WERSA_STAGE("wersa_decay_clear", st, (clear_kernel<<<dim3((unsigned)across, c.H, tensors), 256, 0, st>>>(seq, a)));
+}
 void launch_scan(const Walk &a, float *local, hipStream_t st) {
   const int size = a.kw * a.vw;
   if ((int64_t)size * a.H * a.seq.B >= 1 << 21)   // eight waves of four values to a SIMD
@@ -1186,6 +1214,15 @@ wersa_status wersa_decay_forward(const wersa_decay_desc *desc, const void *q, co
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
 
+wersa_status wersa_decay_clear(const wersa_decay_desc *desc, const int32_t *offsets, void *out, void *hip_stream) {
+  const wersa_status vs = validate(desc);
+  if (vs != WERSA_OK) return vs;
+  const wersa_decay_desc &c = *desc;
+  if ((c.n > 0 && !out) || (c.packed != 0) != (offsets != nullptr)) return WERSA_ERR_INVALID_ARG;
+  launch_clear(c, sequences(c, offsets), 1, Outside{{out}, {strides(c.stride_o, c, c.dv)}, {c.dv}, 0}, (hipStream_t)hip_stream);
+  return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
+}
+
 wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, const void *k, const void *v, const float *log_decay,
                                   const int32_t *offsets, const float *initial_state, const void *dout, const float *dfinal_state,
                                   const void *saved, void *dq, void *dk, void *dv, float *dinitial_state, void *workspace,
@@ -1234,6 +1271,7 @@ wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, c
   }
   r.fin = dinitial_state;
   if (!launch_back(c, r, Back{k, v, dk, dv, sk, sv}, st)) return WERSA_ERR_LAUNCH;
+  launch_clear(c, a.seq, 3, Outside{{dq, dk, dv}, {sq, sk, sv}, {c.dk, c.dk, c.dv}, 0}, st);
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
 
