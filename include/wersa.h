@@ -224,9 +224,9 @@ int64_t wersa_block_workspace_offset(const wersa_desc *desc, int which);
  *   S_t = lambda_h S_{t-1} + k_t v_t^T  (dk x dv, float32),  o_t = scale q_t^T S_t,  lambda_h = exp(log_decay[h])
  * over a whole sequence (wersa_decay_forward), its derivative (wersa_decay_backward), and one token at a time on a
  * cache of states (wersa_decay_step).  q and k are (B, H, n, dk), v and out (B, H, n, dv), each at strides of its own
- * (batch, head, row; in elements; columns contiguous); dq, dk, dv and dout are laid out like q, k, v and out.  Any
- * element-aligned pointer is taken.  Rows do not overlap: a row's stride is at least the width, and at most 2^24; with n = 1 it is
- * not read.
+ * (batch, head, row; in elements; columns contiguous); dout is laid out like out.  Any element-aligned pointer is taken.  Rows do
+ * not overlap: a row's stride is at least the width, and at most 2^24; with n = 1 it is not read.  Sequences and heads of what is
+ * only read may overlap (strides above 0); in out, dq, dk and dv each dimension begins behind what those of smaller strides take.
  *   packed   0: B sequences of n rows each; offsets is NULL.
  *            1: B sequences of any lengths (zero among them) one behind the other in tensors with one batch entry of n
  *               rows: sequence b is rows offsets[b] .. offsets[b + 1] - 1 (B + 1 device integers that do not decrease; the
@@ -250,6 +250,7 @@ typedef struct {
   int32_t packed;
   float scale;
   int64_t stride_q[3], stride_k[3], stride_v[3], stride_o[3];
+  int64_t stride_dq[3], stride_dk[3], stride_dv[3];   /* of the gradients; three zeros: those of q, k, v */
 } wersa_decay_desc;
 
 size_t wersa_decay_workspace_bytes(const wersa_decay_desc *desc, int for_backward);

@@ -128,7 +128,8 @@ class _DecayAttention(torch.autograd.Function):
 
 
 def _rows_apart(x):
-    """x with contiguous columns and rows that do not share memory (an expanded tensor is copied)."""
+    """x with contiguous columns, and strides as the library reads them: rows that do not share memory, heads and sequences that are not one (an
+    expanded tensor is copied)."""
     apart = x.stride(3) == 1 and all(x.stride(i) > 0 or x.shape[i] == 1 for i in range(2)) and (x.stride(2) >= x.shape[3] or x.shape[2] <= 1)
     return x if apart else x.contiguous()
 

@@ -40,7 +40,7 @@ class WersaDesc(ctypes.Structure):
 class WersaDecayDesc(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("n", ctypes.c_int32), ("dk", ctypes.c_int32),
                 ("dv", ctypes.c_int32), ("dtype", ctypes.c_int32), ("packed", ctypes.c_int32), ("scale", ctypes.c_float)] + \
-               [(name, ctypes.c_int64 * 3) for name in ("stride_q", "stride_k", "stride_v", "stride_o")]
+               [(name, ctypes.c_int64 * 3) for name in ("stride_q", "stride_k", "stride_v", "stride_o", "stride_dq", "stride_dk", "stride_dv")]
 
 
 class WersaNormDesc(ctypes.Structure):
@@ -476,12 +476,15 @@ def _dtype_code(x):
     raise TypeError("dtype must be float32 or bfloat16")
 
 
-_DECAY_DESC = struct.Struct("7if12q")   # (a structure of ctypes takes several times as long to fill in field by field)
+_DECAY_DESC = struct.Struct("7if21q")   # (a structure of ctypes takes several times as long to fill in field by field)
 
 
-def make_decay_desc(q, k, v, out, scale=None, offsets=None):
+_AS_THEIR_TENSORS = (0,) * 9
+
+
+def make_decay_desc(q, k, v, out, scale=None, offsets=None, grad_strides=_AS_THEIR_TENSORS):
     """Descriptor for q, k (B, H, n, dk) and v, out (B, H, n, dv), last dimension contiguous; with offsets (B + 1) the tensors
-    have one batch entry that holds the rows of all B sequences.  scale: 1 / sqrt(dk) by default."""
+    have one batch entry that holds the rows of all B sequences.  scale: 1 / sqrt(dk) by default.  grad_strides: three of each of dq, dk, dv."""
     assert q.dim() == 4 and v.dim() == 4, "expect q, k (B, H, n, dk) and v, out (B, H, n, dv)"
     (N, H, n, dk), dv = q.shape, v.shape[3]
     assert k.shape == q.shape and v.shape == (N, H, n, dv) and out.shape == v.shape, "expect q, k (B, H, n, dk) and v, out (B, H, n, dv)"
@@ -496,7 +499,19 @@ def make_decay_desc(q, k, v, out, scale=None, offsets=None):
         B = offsets.numel() - 1
     return WersaDecayDesc.from_buffer_copy(_DECAY_DESC.pack(
         B, H, n, dk, dv, _dtype_code(q), offsets is not None, dk ** -0.5 if scale is None else scale,
-        qb, qh, qn, kb, kh, kn, vb, vh, vn, ob, oh, on))
+        qb, qh, qn, kb, kh, kn, vb, vh, vn, ob, oh, on, *grad_strides))
+
+
+def _dense_like(x):
+    """A new tensor of x's shape, with its dimensions in x's order in memory but none apart from or on another: x may be a slice, or windows that overlap."""
+    shape, strides = x.shape, x.stride()
+    (N, H, n, d), (b, h, r, _) = shape, strides
+    if not ((r == d and h == n * d or h == d and r == H * d) and b == H * n * d):   # (otherwise it is dense)
+        step, strides = d, [1] * 4
+        for i in sorted(range(3), key=x.stride):
+            strides[i] = step
+            step *= max(1, shape[i])
+    return torch.empty_strided(shape, strides, dtype=x.dtype, device=x.device)
 
 
 def _addr(t):
@@ -529,7 +544,7 @@ def _check_log_decay(log_decay, desc):
 
 
 def checked_decay_desc(q, k, v, log_decay, scale, offsets, initial_state):
-    """(descriptor, bytes of saved) of a forward call whose output is laid out like v; the arguments are checked."""
+    """(descriptor, bytes of saved) of a forward call, whose output's strides the caller fills in; the arguments are checked."""
     desc = make_decay_desc(q, k, v, v, scale, offsets)
     _check_log_decay(log_decay, desc)
     _check_states(desc, None, initial_state)
@@ -548,7 +563,7 @@ def wersa_decay_forward(q, k, v, log_decay, scale=None, offsets=None, initial_st
     lib = load_library()
     clear = out is None and offsets is not None
     if out is None:
-        out = torch.empty_strided(v.shape, v.stride(), dtype=v.dtype, device=v.device)
+        out = _dense_like(v)
     desc = make_decay_desc(q, k, v, out, scale, offsets)
     _check_log_decay(log_decay, desc)
     if want_state and final_state is None:
@@ -574,18 +589,22 @@ def wersa_decay_forward(q, k, v, log_decay, scale=None, offsets=None, initial_st
 
 def wersa_decay_backward(q, k, v, log_decay, dout, saved, scale=None, offsets=None, initial_state=None, dfinal_state=None,
                          want_dinitial=False, workspace=None, stream=None, grads=None):
-    """Returns dict(dq, dk, dv, dinitial_state); rows of no sequence are zeros.  `grads` may be a dict from an earlier call: its tensors are then overwritten."""
+    """Returns dict(dq, dk, dv, dinitial_state); rows of no sequence are zeros.  `grads` may be a dict from an earlier call, of any strides: its tensors are then
+    overwritten."""
     lib = load_library()
-    desc = make_decay_desc(q, k, v, dout, scale, offsets)
+    fresh = grads is None
+    if fresh:
+        grads = dict(dq=_dense_like(q), dk=_dense_like(k), dv=_dense_like(v))
+    for name, x in (("dq", q), ("dk", k), ("dv", v)):
+        g = grads[name]
+        assert g.shape == x.shape and g.dtype == x.dtype and g.stride(3) == 1, f"{name} has its tensor's shape and dtype, and a contiguous last dim"
+    desc = make_decay_desc(q, k, v, dout, scale, offsets, [s for name in ("dq", "dk", "dv") for s in grads[name].stride()[:3]])
     _check_log_decay(log_decay, desc)
     _check_states(desc, None, initial_state, dfinal_state)
     sb = lib.wersa_decay_saved_bytes(ctypes.byref(desc))
     assert _nbytes(saved) >= sb, f"saved buffer holds {_nbytes(saved)} bytes, wersa_decay_saved_bytes asks for {sb}"
-    if grads is None:
-        grads = {name: torch.empty_strided(x.shape, x.stride(), dtype=x.dtype, device=x.device) for name, x in (("dq", q), ("dk", k), ("dv", v))}
+    if fresh:
         grads["dinitial_state"] = torch.empty(desc.B, desc.H, desc.dk, desc.dv, dtype=torch.float32, device=q.device) if want_dinitial else None
-    for name, x in (("dq", q), ("dk", k), ("dv", v)):
-        _same_layout(x, grads[name])
     _check_states(desc, None, grads["dinitial_state"])
     _on_one_gpu(q, k, v, log_decay, offsets, initial_state, dout, dfinal_state, saved, workspace, *grads.values())
     if workspace is None:
@@ -608,7 +627,7 @@ def wersa_decay_step(q, k, v, log_decay, state, scale=None, slots=None, out=None
     (qb, qh, q1), (kb, kh, k1), (vb, vh, v1), (ob, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
     assert q1 == k1 == v1 == o1 == 1, "expect a contiguous last dim"
     desc = WersaDecayDesc.from_buffer_copy(_DECAY_DESC.pack(B, H, 1, dk, dv, _dtype_code(q), 0, dk ** -0.5 if scale is None else scale,
-                                                            qb, qh, 0, kb, kh, 0, vb, vh, 0, ob, oh, 0))
+                                                            qb, qh, 0, kb, kh, 0, vb, vh, 0, ob, oh, 0, *_AS_THEIR_TENSORS))
     _check_log_decay(log_decay, desc)
     rows = _check_states(desc, slots, state)
     _on_one_gpu(q, k, v, log_decay, state, slots, out)

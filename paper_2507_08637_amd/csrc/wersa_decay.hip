@@ -392,7 +392,7 @@ __global__ __launch_bounds__(64 * f32_waves(DK, DV)) void walk_f32_kernel(Walk a
 struct Back {
   const void *k, *v;
   void *dk, *dv;
-  Strides sk, sv;
+  Strides sk, sv, sdk, sdv;
 };
 template <int DK, int DV>
 __global__ __launch_bounds__(64 * f32_waves(DK, DV)) void back_f32_kernel(Walk a, Back b) {
@@ -408,7 +408,7 @@ __global__ __launch_bounds__(64 * f32_waves(DK, DV)) void back_f32_kernel(Walk a
   const P4 part(wave);
   const int vcol = DV / P4::HALVES * part.half, kcol = DK / P4::HALVES * part.half;   // of dv and of dk
   const Rows qr = rows_of(a.k, a.sk, seg, a, h, a.kw, 4), dr = rows_of(a.v, a.sv, seg, a, h, a.vw, 4), kr = rows_of(b.k, b.sk, seg, a, h, a.kw, 4),
-             vr = rows_of(b.v, b.sv, seg, a, h, a.vw, 4), dkr = rows_of(b.dk, b.sk, seg, a, h, a.kw, 4), dvr = rows_of(b.dv, b.sv, seg, a, h, a.vw, 4);
+             vr = rows_of(b.v, b.sv, seg, a, h, a.vw, 4), dkr = rows_of(b.dk, b.sdk, seg, a, h, a.kw, 4), dvr = rows_of(b.dv, b.sdv, seg, a, h, a.vw, 4);
   const float l2 = log2_decay(a.log_decay, h);
   const int64_t state_size = (int64_t)a.kw * a.vw;
 
@@ -824,7 +824,7 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : 2) void back_bf16_kernel(W
   const int t = part.t;
   const uint32_t stage = lds + Gt + 2 * DV * DK + STAGE * w;
   const Rows qr = rows_of(a.k, a.sk, seg, a, h, a.kw, 2), dr = rows_of(a.v, a.sv, seg, a, h, a.vw, 2), kr = rows_of(b.k, b.sk, seg, a, h, a.kw, 2),
-             vr = rows_of(b.v, b.sv, seg, a, h, a.vw, 2), dkr = rows_of(b.dk, b.sk, seg, a, h, a.kw, 2), dvr = rows_of(b.dv, b.sv, seg, a, h, a.vw, 2);
+             vr = rows_of(b.v, b.sv, seg, a, h, a.vw, 2), dkr = rows_of(b.dk, b.sdk, seg, a, h, a.kw, 2), dvr = rows_of(b.dv, b.sdv, seg, a, h, a.vw, 2);
   const float l2 = log2_decay(a.log_decay, h);
   const int64_t state_size = (int64_t)a.kw * a.vw;
 
@@ -1098,6 +1098,24 @@ bool strides_ok(const int64_t *s, const wersa_decay_desc &c, int width) {
   if (c.H > 1 && s[1] == 0) return false;
   return c.n <= 1 || s[2] >= width;
 }
+// What is written: heads and sequences must not lie on each other, as those that are only read may. Sorted by stride, a dimension begins anew behind what the ones before it take.
+bool apart(const int64_t *s, const wersa_decay_desc &c, int width) {
+  struct { int64_t stride, count; } dim[3] = {{s[0], c.packed ? 1 : c.B}, {s[1], c.H}, {s[2], c.n}};
+  std::sort(dim, dim + 3, [](auto &x, auto &y) { return x.stride < y.stride; });
+  __int128 taken = width;
+  for (const auto &d : dim)
+    if (d.count > 1) {
+      if (d.stride < taken) return false;
+      taken += (__int128)d.stride * (d.count - 1);
+    }
+  return true;
+}
+// A gradient's strides: those of its tensor where the descriptor has none.
+const int64_t *strides_of_gradient(const int64_t *own, const int64_t *tensor) { return own[0] == 0 && own[1] == 0 && own[2] == 0 ? tensor : own; }
+wersa_status written(const int64_t *s, const wersa_decay_desc &c, int width) {
+  if (s[0] < 0 || s[1] < 0 || s[2] < 0 || !apart(s, c, width)) return WERSA_ERR_INVALID_ARG;
+  return c.n > 1 && s[2] > kMostRowStride ? WERSA_ERR_UNSUPPORTED : WERSA_OK;
+}
 wersa_status validate(const wersa_decay_desc *c) {
   if (!c) return WERSA_ERR_INVALID_ARG;
   if (c->B < 1 || c->H < 1 || c->n < 0 || c->dk < 1 || c->dv < 1) return WERSA_ERR_INVALID_ARG;
@@ -1189,6 +1207,7 @@ wersa_status wersa_decay_forward(const wersa_decay_desc *desc, const void *q, co
   if (!log_decay || (c.packed != 0) != (offsets != nullptr)) return WERSA_ERR_INVALID_ARG;
   if ((initial_state || final_state) && state_slots < (slots ? 1 : c.B)) return WERSA_ERR_INVALID_ARG;
   if (misaligned(initial_state, 16) || misaligned(final_state, 16)) return WERSA_ERR_INVALID_ARG;
+  if (const wersa_status ws = written(c.stride_o, c, c.dv)) return ws;
   const bool split = state_slots_of(c) > 0;
   if (split && !saved && (!workspace || workspace_bytes < states_bytes(c) || misaligned(workspace, 256))) return WERSA_ERR_WORKSPACE;
   if (misaligned(saved, 256)) return WERSA_ERR_WORKSPACE;
@@ -1219,6 +1238,7 @@ wersa_status wersa_decay_clear(const wersa_decay_desc *desc, const int32_t *offs
   if (vs != WERSA_OK) return vs;
   const wersa_decay_desc &c = *desc;
   if ((c.n > 0 && !out) || (c.packed != 0) != (offsets != nullptr)) return WERSA_ERR_INVALID_ARG;
+  if (const wersa_status ws = written(c.stride_o, c, c.dv)) return ws;
   launch_clear(c, sequences(c, offsets), 1, Outside{{out}, {strides(c.stride_o, c, c.dv)}, {c.dv}, 0}, (hipStream_t)hip_stream);
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
@@ -1233,6 +1253,9 @@ wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, c
   if (c.n > 0 && (!q || !k || !v || !dout || !dq || !dk || !dv)) return WERSA_ERR_INVALID_ARG;
   if (!log_decay || (c.packed != 0) != (offsets != nullptr)) return WERSA_ERR_INVALID_ARG;
   if (misaligned(initial_state, 16) || misaligned(dfinal_state, 16) || misaligned(dinitial_state, 16)) return WERSA_ERR_INVALID_ARG;
+  const int64_t *gq = strides_of_gradient(c.stride_dq, c.stride_q), *gk = strides_of_gradient(c.stride_dk, c.stride_k), *gv = strides_of_gradient(c.stride_dv, c.stride_v);
+  for (const wersa_status ws : {written(gq, c, c.dk), written(gk, c, c.dk), written(gv, c, c.dv)})
+    if (ws != WERSA_OK) return ws;
   const bool split = state_slots_of(c) > 0;
   if (split && !saved) return WERSA_ERR_INVALID_ARG;
   if (misaligned(saved, 256) || (split && (!workspace || workspace_bytes < states_bytes(c) || misaligned(workspace, 256))))
@@ -1245,10 +1268,11 @@ wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, c
   a.heads_first = heads_first(c, a.seq);
   a.H = c.H;
   const Strides sq = strides(c.stride_q, c, c.dk), sk = strides(c.stride_k, c, c.dk), sv = strides(c.stride_v, c, c.dv), so = strides(c.stride_o, c, c.dv);
+  const Strides sdq = strides(gq, c, c.dk), sdk = strides(gk, c, c.dk), sdv = strides(gv, c, c.dv);
   // dq: states transposed
   Walk f = a;
   f.q = dout, f.k = v, f.v = k, f.o = dq;
-  f.sq = so, f.sk = sv, f.sv = sk, f.so = sq;
+  f.sq = so, f.sk = sv, f.sv = sk, f.so = sdq;
   f.kw = c.dv, f.vw = c.dk, f.si = 1, f.sj = c.dv;
   f.intra = f.inter = c.scale, f.gain = 1.f;
   f.init = split ? (const float *)saved : initial_state;
@@ -1260,7 +1284,7 @@ wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, c
   a.init = dfinal_state;
   Walk r = a;
   r.q = k, r.k = q, r.v = dout, r.o = dv;
-  r.sq = sk, r.sk = sq, r.sv = so, r.so = sv;
+  r.sq = sk, r.sk = sq, r.sv = so, r.so = sdv;
   r.kw = c.dk, r.vw = c.dv, r.si = c.dv, r.sj = 1;
   if (split) {
     r.fin = (float *)workspace;
@@ -1270,8 +1294,8 @@ wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, c
     r.by_slot = true;
   }
   r.fin = dinitial_state;
-  if (!launch_back(c, r, Back{k, v, dk, dv, sk, sv}, st)) return WERSA_ERR_LAUNCH;
-  launch_clear(c, a.seq, 3, Outside{{dq, dk, dv}, {sq, sk, sv}, {c.dk, c.dk, c.dv}, 0}, st);
+  if (!launch_back(c, r, Back{k, v, dk, dv, sk, sv, sdk, sdv}, st)) return WERSA_ERR_LAUNCH;
+  launch_clear(c, a.seq, 3, Outside{{dq, dk, dv}, {sdq, sdk, sdv}, {c.dk, c.dk, c.dv}, 0}, st);
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
 
@@ -1282,6 +1306,7 @@ wersa_status wersa_decay_step(const wersa_decay_desc *desc, const void *q, const
   const wersa_decay_desc &c = *desc;
   if (c.n != 1 || c.packed || !q || !k || !v || !log_decay || !state || !out) return WERSA_ERR_INVALID_ARG;
   if (state_slots < (slots ? 1 : c.B) || misaligned(state, 16)) return WERSA_ERR_INVALID_ARG;
+  if (const wersa_status ws = written(c.stride_o, c, c.dv)) return ws;
   hipStream_t st = (hipStream_t)hip_stream;
   const Step a{q, k, v, out, strides(c.stride_q, c, c.dk), strides(c.stride_k, c, c.dk), strides(c.stride_v, c, c.dv), strides(c.stride_o, c, c.dv), log_decay,
                state, slots, state_slots, c.H, c.dk, c.dv, c.scale};

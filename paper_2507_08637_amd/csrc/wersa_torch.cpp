@@ -12,6 +12,7 @@
 #include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/utils/pybind.h>
 
+#include <algorithm>
 #include <cstring>
 
 #include "../../include/wersa.h"
@@ -151,12 +152,23 @@ int32_t dtype_of(const Tensor &t) { return t.scalar_type() == at::kFloat ? WERSA
 // A backward runs with gradients enabled where a graph of it is wanted: there is none of what the kernels do.
 void once() { TORCH_CHECK(!at::GradMode::is_enabled(), "the causal operators are differentiable once"); }
 
-// Rows with contiguous columns that do not share memory.
+// Rows with contiguous columns that do not share memory, heads and sequences that are not one: as the library reads them.
 bool rows_apart(const Tensor &t) {
   return t.stride(3) == 1 && (t.stride(0) > 0 || t.size(0) == 1) && (t.stride(1) > 0 || t.size(1) == 1) && (t.stride(2) >= t.size(3) || t.size(2) <= 1);
 }
 void put_strides(int64_t *to, const Tensor &t) {
   for (int i = 0; i < 3; ++i) to[i] = t.stride(i);
+}
+// A new tensor of t's shape, with its dimensions in t's order in memory but none apart from or on another: t may be a slice, or windows that overlap.
+Tensor dense_like(const Tensor &t) {
+  int order[3] = {0, 1, 2};
+  std::stable_sort(order, order + 3, [&](int a, int b) { return t.stride(a) < t.stride(b); });
+  int64_t strides[4] = {1, 1, 1, 1}, step = t.size(3);
+  for (const int i : order) {
+    strides[i] = step;
+    step *= std::max<int64_t>(1, t.size(i));
+  }
+  return at::empty_strided(t.sizes(), strides, t.options());
 }
 
 struct DecayAttention : torch::autograd::Function<DecayAttention> {
@@ -166,7 +178,8 @@ struct DecayAttention : torch::autograd::Function<DecayAttention> {
     wersa_decay_desc d;
     TORCH_CHECK(desc.size() == sizeof(d), "descriptor of another size");
     std::memcpy(&d, desc.data(), sizeof(d));
-    const Tensor out = at::empty_strided(v.sizes(), v.strides(), v.options());
+    const Tensor out = dense_like(v);
+    put_strides(d.stride_o, out);
     const auto f32 = q.options().dtype(at::kFloat);
     const Tensor final_state = at::empty({d.B, d.H, d.dk, d.dv}, f32), saved = at::empty({saved_bytes / 4}, f32);
     check(decay_forward_fn(&d, in(q), in(k), in(v), floats(log_decay), (const int32_t *)in(offsets), (const float *)in(initial), floats_out(final_state), nullptr,
@@ -203,8 +216,10 @@ struct DecayAttention : torch::autograd::Function<DecayAttention> {
     put_strides(d.stride_k, k);
     put_strides(d.stride_v, v);
     put_strides(d.stride_o, dout);
-    auto like = [](const Tensor &x) { return at::empty_strided(x.sizes(), x.strides(), x.options()); };
-    const Tensor dq = like(q), dk = like(k), dv = like(v), dinitial = initial.defined() && ctx->needs_input_grad(4) ? at::empty_like(initial) : Tensor();
+    const Tensor dq = dense_like(q), dk = dense_like(k), dv = dense_like(v), dinitial = initial.defined() && ctx->needs_input_grad(4) ? at::empty_like(initial) : Tensor();
+    put_strides(d.stride_dq, dq);
+    put_strides(d.stride_dk, dk);
+    put_strides(d.stride_dv, dv);
     const Tensor ws = scratch((int64_t)decay_workspace_bytes_fn(&d, 1), q);
     check(decay_backward_fn(&d, in(q), in(k), in(v), floats(log_decay), (const int32_t *)in(offsets), (const float *)in(initial), in(dout),
                             (const float *)in(dfinal), saved.const_data_ptr(), out_of(dq), out_of(dk), out_of(dv), (float *)out_of(dinitial),

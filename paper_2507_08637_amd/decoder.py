@@ -93,8 +93,7 @@ class Decoder(torch.nn.Module):
     def prefill(self, tokens, offsets, cache, slots, weights):
         """Prompts one behind the other: tokens (all), offsets (prompts + 1) and slots (prompts) int32.  Leaves their states in the cache; logits of every token."""
         def attend(i, q, k, v):
-            return binding.wersa_decay_forward(q, k, v, self.log_decay, offsets=offsets, final_state=cache[i], slots=slots,
-                                               out=torch.empty_like(v, memory_format=torch.contiguous_format))[0]
+            return binding.wersa_decay_forward(q, k, v, self.log_decay, offsets=offsets, final_state=cache[i], slots=slots)[0]
         return self._serve(tokens, weights, attend)
 
     @torch.no_grad()

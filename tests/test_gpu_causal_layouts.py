@@ -75,3 +75,61 @@ def test_lone_rows_as_programs_have_them(node, dtype):
     close(final, ref["final"], torch.float32, "final")
     for name, x in zip(("dq", "dk", "dv"), grads):
         close(x, ref[name], dtype, name)
+
+
+def check_against_copies(node, leaves, ld, dout, dfinal, dtype):
+    """The operator on views against the definition of their values; returns out and the gradients."""
+    values = {x: t.detach().cpu().contiguous() for x, t in zip("qkv", leaves)}
+    p = dict(values, ld=ld.cpu(), S0=torch.zeros(dfinal.shape), dout=dout.detach().cpu(), dfinal=dfinal.cpu())
+    ref = reference(p, 0.125, grads=True)
+    out, final = node.wersa_decay_attention(*leaves, ld, 0.125)
+    grads = torch.autograd.grad((out, final), leaves, (dout, dfinal))
+    close(out, ref["out"], dtype, "out")
+    close(final, ref["final"], torch.float32, "final")
+    for name, x in zip(("dq", "dk", "dv"), grads):
+        close(x, ref[name], dtype, name)
+    return (out, *grads)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("n", [100, 700])
+def test_windows_that_overlap(node, n, dtype):
+    """Sliding windows over the rows of one tensor as the batch, and heads that share columns: outputs and gradients have memory of their own for each."""
+    H, d, B = 3, 64, 4
+    g = torch.Generator(device="cuda").manual_seed(22)
+    normal = lambda *shape: torch.randn(shape, generator=g, device="cuda").to(dtype)
+    ld = torch.tensor([-0.1, -0.02, -0.005], device="cuda")
+    windows = lambda: normal(n + (B - 1) * (n // 2), H, d).unfold(0, n, n // 2).permute(0, 1, 3, 2)
+    assert windows().shape == (B, H, n, d) and windows().stride(0) == n // 2 * H * d
+    shared = lambda: normal(B, n, d + 32 * (H - 1)).unfold(2, d, 32).transpose(1, 2)
+    assert shared().shape == (B, H, n, d) and shared().stride(1) == 32
+    for views in ([windows(), windows(), windows()], [shared(), shared(), shared()], [windows(), shared(), normal(B, H, n, d)]):
+        leaves = [x.detach().requires_grad_(True) for x in views]
+        for made in check_against_copies(node, leaves, ld, normal(B, H, n, d), torch.randn(B, H, d, d, generator=g, device="cuda"), dtype):
+            assert made.untyped_storage().nbytes() == made.numel() * made.element_size()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_slices_of_a_fused_projection(node, dtype):
+    """Outputs and gradients hold their own elements, not what lies between the slices, in the projection's order: the output is rows of heads without a copy."""
+    from paper_2507_08637_amd import binding
+    B, n, H, d = 2, 150, 3, 64
+    g = torch.Generator(device="cuda").manual_seed(23)
+    fused = torch.randn(B, n, 3, H, d, generator=g, device="cuda").to(dtype)
+    q, k, v = (x.detach().requires_grad_(True) for x in fused.permute(2, 0, 3, 1, 4).unbind(0))
+    ld = torch.tensor([-0.1, -0.02, -0.005], device="cuda")
+    dout, dfinal = torch.randn(B, n, H, d, generator=g, device="cuda").to(dtype).transpose(1, 2), torch.randn(B, H, d, d, generator=g, device="cuda")
+    made = check_against_copies(node, (q, k, v), ld, dout, dfinal, dtype)
+    for x in made:
+        assert x.untyped_storage().nbytes() == x.numel() * x.element_size()
+        assert x.transpose(1, 2).is_contiguous()
+    with torch.no_grad():
+        out, _, saved = binding.wersa_decay_forward(q, k, v, ld, 0.125, want_saved=True)
+        grads = binding.wersa_decay_backward(q, k, v, ld, dout, saved, 0.125, dfinal_state=dfinal)
+        # into gradients of other strides, slices of a gradient of the whole
+        whole = torch.full((B, n, 3, H, d), float("nan"), device="cuda", dtype=dtype)
+        into = dict(zip(("dq", "dk", "dv"), whole.permute(2, 0, 3, 1, 4).unbind(0)), dinitial_state=None)
+        binding.wersa_decay_backward(q, k, v, ld, dout, saved, 0.125, dfinal_state=dfinal, grads=into)
+    assert torch.equal(out, made[0]) and out.transpose(1, 2).is_contiguous()
+    for name, x, part in zip(("dq", "dk", "dv"), made[1:], whole.unbind(2)):
+        assert torch.equal(grads[name], x) and torch.equal(part.transpose(1, 2), x) and grads[name].transpose(1, 2).is_contiguous()
