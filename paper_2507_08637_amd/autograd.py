@@ -13,7 +13,7 @@ block, to x and the four weight matrices (float32 gradients cast to the weights'
     y, r = wersa_rms_norm(x, weight, residual, eps)
 
 q, k (B, H, n, dk), v (B, H, n, dv), each with strides of its own; gradients flow to q, k, v and initial_state (log_decay
-is fixed).  x, residual (..., cols), weight float32 (cols) or None; gradients flow to all three.
+is fixed: one that wants a gradient is refused).  x, residual (..., cols), weight float32 (cols) or None; gradients flow to all three.
 """
 import ctypes
 import warnings
@@ -137,6 +137,7 @@ def _rows_apart(x):
 def wersa_decay_attention(q, k, v, log_decay, scale=None, initial_state=None, offsets=None):
     """Causal linear attention with a decay for each head.  Returns (out, final states (B, H, dk, dv) in float32).  Rows of no sequence (offsets that
     begin behind the first row or end before the last one) are zeros in out and in the gradients, whatever they hold in q, k, v and out's gradient."""
+    assert not (log_decay.requires_grad and torch.is_grad_enabled()), "log_decay is fixed and has no gradient: pass log_decay.detach() if none is wanted"
     q, k, v = _rows_apart(q), _rows_apart(k), _rows_apart(v)
     node = _load_node() if _node is None else _node
     if not node or torch.jit.is_tracing():
