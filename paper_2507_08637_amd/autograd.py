@@ -168,6 +168,7 @@ class _RmsNorm(torch.autograd.Function):
 def wersa_rms_norm(x, weight=None, residual=None, eps=1e-6):
     """RMS norm over the last dimension: y, or (y, x + residual)."""
     shape = x.shape
+    assert residual is None or residual.shape == shape, "the residual has x's shape and dtype"
     if len(shape) != 2:
         x = x.reshape(-1, shape[-1])
         residual = None if residual is None else residual.reshape(-1, shape[-1])

@@ -35,3 +35,15 @@ def test_a_decay_that_wants_a_gradient(calls):
         autograd.wersa_decay_attention(q, q, q, ld)
     autograd.wersa_decay_attention(q, q, q, ld.detach())
     assert calls.count("wersa_decay_forward") == 2
+
+
+def test_a_residual_of_another_shape(calls):
+    """As many elements in other dimensions would be added row by row in the wrong order."""
+    from paper_2507_08637_amd import autograd
+    x = torch.zeros(4, 6, 32)
+    for shape in ((6, 4, 32), (24, 32), (2, 12, 32)):
+        with pytest.raises(AssertionError, match="x's shape"):
+            autograd.wersa_rms_norm(x, residual=torch.zeros(shape))
+    assert not calls
+    y, r = autograd.wersa_rms_norm(x, residual=torch.zeros(4, 6, 32))
+    assert y.shape == r.shape == x.shape and "wersa_rms_norm_forward" in calls
