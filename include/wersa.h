@@ -282,7 +282,8 @@ wersa_status wersa_decay_step(const wersa_decay_desc *desc, const void *q, const
  * The norm reads the stream r as it is kept.  x and residual are (rows, cols) at row strides of their own, columns
  * contiguous; r, y, dy, dr and dx are dense.  weight is float32 [cols] or NULL (ones); rstd float32 [rows], NULL:
  * not wanted.  wersa_rms_norm_eight_bit writes y in 8 bits (e4m3, largest value 448) and float32 scales [rows]:
- *   scale = max|y| / 448,  y8 = e4m3(y * (448 / max|y|)) to the nearest, ties to even;  a row of zeros has scale 1.
+ *   scale = max|y| / 448,  y8 = e4m3(y * (448 / max|y|)) to the nearest, ties to even;  a row of zeros has scale 1.  The bits are
+ *   right for rows of any size; below max|y| = 448 * 2^-126 = 5e-36 the scale has fewer than 24 bits, down to zero.
  * wersa_rms_norm_backward: r is the forward's stream (x where no residual was added, at stride_x), dr the gradient that
  * reaches r from elsewhere (NULL: none); dx is the gradient of x and of the residual, dweight (float32 [cols], NULL: not
  * wanted) that of the weight, for which the workspace is needed.  Supported: cols up to 8192, rows up to 2^31 (0: nothing is done but

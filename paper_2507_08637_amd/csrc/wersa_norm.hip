@@ -157,7 +157,14 @@ __global__ __launch_bounds__(256) void norm_kernel(NormJob a) {
 #pragma unroll
     for (int i = 0; i < E; ++i) most = max(most, __float_as_uint(v[p][i]) & 0x7fffffffu);
   const float top = __uint_as_float(row_most<LANES>(most, part));
-  const float inverse = top > 0.f ? 448.f / top : 1.f;
+  float inverse = top > 0.f ? 448.f / top : 1.f;
+  if (top > 0.f && top < 0x1p-100f) {   // a row so small that 448 / top may leave float32: its values are raised first
+    inverse = 448.f / (top * 0x1p64f);
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[p][i] *= 0x1p64f;
+  }
   if (ok && t == 0) a.scales[row] = top > 0.f ? top / 448.f : 1.f;
   unsigned char *y = (unsigned char *)a.y + (ok ? row : 0) * a.cols;
 #pragma unroll
