@@ -514,6 +514,16 @@ def _dense_like(x):
     return torch.empty_strided(shape, strides, dtype=x.dtype, device=x.device)
 
 
+def _not_broadcast(x, stream):
+    """x, or a copy where it is expanded over sequences, heads or rows: the library takes strides above 0."""
+    if 0 not in x.stride():
+        return x
+    if stream is None:
+        return x.contiguous()
+    with torch.cuda.stream(stream):
+        return x.contiguous()
+
+
 def _addr(t):
     return None if t is None else t.data_ptr()
 
@@ -562,6 +572,7 @@ def wersa_decay_forward(q, k, v, log_decay, scale=None, offsets=None, initial_st
     the caller's."""
     lib = load_library()
     clear = out is None and offsets is not None
+    q, k, v = _not_broadcast(q, stream), _not_broadcast(k, stream), _not_broadcast(v, stream)
     if out is None:
         out = _dense_like(v)
     desc = make_decay_desc(q, k, v, out, scale, offsets)
@@ -593,6 +604,7 @@ def wersa_decay_backward(q, k, v, log_decay, dout, saved, scale=None, offsets=No
     overwritten."""
     lib = load_library()
     fresh = grads is None
+    q, k, v, dout = (_not_broadcast(x, stream) for x in (q, k, v, dout))
     if fresh:
         grads = dict(dq=_dense_like(q), dk=_dense_like(k), dv=_dense_like(v))
     for name, x in (("dq", q), ("dk", k), ("dv", v)):
@@ -624,6 +636,7 @@ def wersa_decay_step(q, k, v, log_decay, state, scale=None, slots=None, out=None
     (B, H, dk), dv, dtype = q.shape, v.shape[2], q.dtype
     assert k.shape == q.shape and v.shape == (B, H, dv) and out.shape == v.shape, "expect q, k (B, H, dk) and v, out (B, H, dv)"
     assert k.dtype == dtype and v.dtype == dtype and out.dtype == dtype, "q, k, v and out must share a dtype"
+    q, k, v = _not_broadcast(q, stream), _not_broadcast(k, stream), _not_broadcast(v, stream)
     (qb, qh, q1), (kb, kh, k1), (vb, vh, v1), (ob, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
     assert q1 == k1 == v1 == o1 == 1, "expect a contiguous last dim"
     desc = WersaDecayDesc.from_buffer_copy(_DECAY_DESC.pack(B, H, 1, dk, dv, _dtype_code(q), 0, dk ** -0.5 if scale is None else scale,

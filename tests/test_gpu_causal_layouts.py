@@ -133,3 +133,28 @@ def test_slices_of_a_fused_projection(node, dtype):
     assert torch.equal(out, made[0]) and out.transpose(1, 2).is_contiguous()
     for name, x, part in zip(("dq", "dk", "dv"), made[1:], whole.unbind(2)):
         assert torch.equal(grads[name], x) and torch.equal(part.transpose(1, 2), x) and grads[name].transpose(1, 2).is_contiguous()
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_heads_that_share_keys_and_values(dtype):
+    """The binding on keys and values that are expanded over heads, sequences or rows: as on copies of them, gradients for each of the heads."""
+    from paper_2507_08637_amd import binding
+    B, H, n, d = 2, 4, 200, 64
+    p = to(make(B, H, n, d, d, dtype, seed=24, grads=True))
+    common = [p["k"][:, :1], p["v"][:1, :1], p["dout"][:, :, :1]]
+    k, v, dout = (x.expand(B, H, n, d) for x in common)
+    side = torch.cuda.Stream()
+
+    def run(k, v, dout, stream=None):
+        side.wait_stream(torch.cuda.current_stream())
+        out, final, saved = binding.wersa_decay_forward(p["q"], k, v, p["ld"], want_state=True, want_saved=True, stream=stream)
+        got = binding.wersa_decay_backward(p["q"], k, v, p["ld"], dout, saved, dfinal_state=p["dfinal"], want_dinitial=True, stream=stream)
+        state = p["dfinal"].clone()
+        side.wait_stream(torch.cuda.current_stream())
+        token = binding.wersa_decay_step(p["q"][:, :, 3], k[:, :, 3], v[:, :, 3], p["ld"], state, stream=stream)
+        torch.cuda.synchronize()
+        return [out, final, *got.values(), token, state]
+    want = run(k.contiguous(), v.contiguous(), dout.contiguous())
+    for stream in (None, side):
+        for a, b in zip(run(k, v, dout, stream), want):
+            assert torch.equal(a, b)
