@@ -165,13 +165,19 @@ class _RmsNorm(torch.autograd.Function):
         return dx, dw, dx if ctx.needs_input_grad[2] else None, None
 
 
+def _as_rows(x):
+    """(rows, cols), columns contiguous, rows that do not share memory: a view, or a copy of what is not laid out so (transposed, broadcast)."""
+    if x.dim() != 2:
+        x = x.reshape(-1, x.shape[-1])
+    apart = x.stride(1) == 1 and (x.stride(0) >= x.shape[1] or x.shape[0] <= 1)
+    return x if apart else x.clone(memory_format=torch.contiguous_format)
+
+
 def wersa_rms_norm(x, weight=None, residual=None, eps=1e-6):
     """RMS norm over the last dimension: y, or (y, x + residual)."""
     shape = x.shape
     assert residual is None or residual.shape == shape, "the residual has x's shape and dtype"
-    if len(shape) != 2:
-        x = x.reshape(-1, shape[-1])
-        residual = None if residual is None else residual.reshape(-1, shape[-1])
+    x, residual = _as_rows(x), None if residual is None else _as_rows(residual)
     node = _load_node() if _node is None else _node
     if not node or torch.jit.is_tracing():
         outs = _RmsNorm.apply(x, weight, residual, eps)
