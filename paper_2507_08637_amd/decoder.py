@@ -63,7 +63,8 @@ class Decoder(torch.nn.Module):
         def after_norm(w):
             if not eight_bit:
                 return w.to(self.dtype), None
-            scale = w.abs().amax(0) / 448
+            most = w.abs().amax(0)
+            scale = torch.where(most > 0, most / 448, 1.0)   # (a column of zeros)
             return (w / scale).to(torch.float8_e4m3fn).t().contiguous().t(), scale[None]
         return ([dict(qkv=after_norm(x.qkv), out=x.out.to(self.dtype), up=after_norm(x.up), down=x.down.to(self.dtype)) for x in self.layers],
                 after_norm(self.head))

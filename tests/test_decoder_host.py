@@ -1,0 +1,22 @@
+"""The host's part of the decoder example, without a GPU."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+
+def model():
+    from paper_2507_08637_amd.decoder import Decoder
+    torch.manual_seed(0)
+    return Decoder(vocabulary=16, hidden=64, heads=2, device="cpu", dtype=torch.float32)
+
+
+def test_weights_in_eight_bits_with_a_column_of_zeros():
+    """Every value within half a step of e4m3 of its weight (2^-4 of it, 2^-10 of the column's scale for the smallest), zeros zeros."""
+    m = model()
+    with torch.no_grad():
+        m.layers[0].qkv[:, 5] = 0
+        m.head[:, 3] = 0
+    layers, head = m.serving(eight_bit=True)
+    for (bits, scale), w in ((layers[0]["qkv"], m.layers[0].qkv), (layers[1]["up"], m.layers[1].up), (head, m.head)):
+        got = bits.float() * scale
+        assert torch.isfinite(got).all() and ((got - w).abs() <= (2.0 ** -4 * w.abs()).maximum(2.0 ** -10 * scale) * (1 + 2.0 ** -20)).all()
