@@ -131,6 +131,7 @@ def train(model, steps, sequences=16, n=128, period=2, seed=0, report=None):
 
 def generate(model, prompts, tokens, eight_bit=False):
     """The most likely continuation, `tokens` long, of each prompt (a list of 1-D tensors): (prompts, tokens)."""
+    assert prompts and all(len(p) > 0 for p in prompts), "a prompt has at least one token to go on from"
     device, B = model.log_decay.device, len(prompts)
     lengths = torch.tensor([len(p) for p in prompts])
     offsets = torch.cat([torch.zeros(1, dtype=torch.long), lengths.cumsum(0)]).to(torch.int32).to(device)

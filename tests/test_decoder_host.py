@@ -20,3 +20,12 @@ def test_weights_in_eight_bits_with_a_column_of_zeros():
     for (bits, scale), w in ((layers[0]["qkv"], m.layers[0].qkv), (layers[1]["up"], m.layers[1].up), (head, m.head)):
         got = bits.float() * scale
         assert torch.isfinite(got).all() and ((got - w).abs() <= (2.0 ** -4 * w.abs()).maximum(2.0 ** -10 * scale) * (1 + 2.0 ** -20)).all()
+
+
+def test_prompts_of_no_tokens():
+    """There is no token to go on from: the logits of the prompt beside it were taken."""
+    from paper_2507_08637_amd.decoder import generate
+    one, none = torch.tensor([3]), torch.zeros(0, dtype=torch.long)
+    for prompts in ([none], [one, none], [none, one], []):
+        with pytest.raises(AssertionError, match="at least one token"):
+            generate(model(), prompts, 2)
