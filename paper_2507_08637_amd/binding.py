@@ -636,8 +636,10 @@ def wersa_decay_step(q, k, v, log_decay, state, scale=None, slots=None, out=None
     (B, H, dk), dv, dtype = q.shape, v.shape[2], q.dtype
     assert k.shape == q.shape and v.shape == (B, H, dv) and out.shape == v.shape, "expect q, k (B, H, dk) and v, out (B, H, dv)"
     assert k.dtype == dtype and v.dtype == dtype and out.dtype == dtype, "q, k, v and out must share a dtype"
-    q, k, v = _not_broadcast(q, stream), _not_broadcast(k, stream), _not_broadcast(v, stream)
     (qb, qh, q1), (kb, kh, k1), (vb, vh, v1), (ob, oh, o1) = q.stride(), k.stride(), v.stride(), out.stride()
+    if not (qb and qh and kb and kh and vb and vh):
+        q, k, v = _not_broadcast(q, stream), _not_broadcast(k, stream), _not_broadcast(v, stream)
+        (qb, qh, q1), (kb, kh, k1), (vb, vh, v1) = q.stride(), k.stride(), v.stride()
     assert q1 == k1 == v1 == o1 == 1, "expect a contiguous last dim"
     desc = WersaDecayDesc.from_buffer_copy(_DECAY_DESC.pack(B, H, 1, dk, dv, _dtype_code(q), 0, dk ** -0.5 if scale is None else scale,
                                                             qb, qh, 0, kb, kh, 0, vb, vh, 0, ob, oh, 0, *_AS_THEIR_TENSORS))
