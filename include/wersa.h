@@ -230,7 +230,9 @@ int64_t wersa_block_workspace_offset(const wersa_desc *desc, int which);
  *   packed   0: B sequences of n rows each; offsets is NULL.
  *            1: B sequences of any lengths (zero among them) one behind the other in tensors with one batch entry of n
  *               rows: sequence b is rows offsets[b] .. offsets[b + 1] - 1 (B + 1 device integers that do not decrease; the
- *               batch strides are not read).  Offsets are clamped to 0 .. n on the device; rows of no sequence are not written.
+ *               batch strides are not read).  Offsets are clamped to 0 .. n on the device.  Rows of no sequence,
+ *            before the first one's or behind the last one's, are not read; the forward leaves them in out as they are, or with
+ *            clear = 1 writes zeros to them; in dq, dk and dv they are zeros.
  *   log_decay  float32 [H], at most 0 for a state that stays bounded; -inf is a decay of zero.  A fixed parameter: it
  *            has no gradient.
  *   states   float32 [state_slots][H][dk][dv], contiguous, 16-byte aligned.  initial_state NULL: zeros; final_state
@@ -251,6 +253,7 @@ typedef struct {
   float scale;
   int64_t stride_q[3], stride_k[3], stride_v[3], stride_o[3];
   int64_t stride_dq[3], stride_dk[3], stride_dv[3];   /* of the gradients; three zeros: those of q, k, v */
+  int32_t clear;           /* packed: 1: the forward writes zeros to the rows of out that are of no sequence */
 } wersa_decay_desc;
 
 size_t wersa_decay_workspace_bytes(const wersa_decay_desc *desc, int for_backward);
@@ -260,9 +263,6 @@ wersa_status wersa_decay_forward(const wersa_decay_desc *desc, const void *q, co
                                  const float *log_decay, const int32_t *offsets, const float *initial_state,
                                  float *final_state, const int32_t *slots, int32_t state_slots, void *out, void *saved,
                                  void *workspace, size_t workspace_bytes, void *hip_stream);
-
-/* Zeros to the rows of out that are of no sequence. */
-wersa_status wersa_decay_clear(const wersa_decay_desc *desc, const int32_t *offsets, void *out, void *hip_stream);
 
 wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, const void *k, const void *v,
                                   const float *log_decay, const int32_t *offsets, const float *initial_state,

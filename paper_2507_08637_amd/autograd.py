@@ -43,7 +43,7 @@ def _load_node():
         node.bind(*(ctypes.cast(f, ctypes.c_void_p).value for f in (lib.wersa_forward, lib.wersa_backward, lib.wersa_workspace_bytes,
                                                                     lib.wersa_saved_bytes, lib.wersa_selected_path)))
         node.bind_causal([ctypes.cast(f, ctypes.c_void_p).value for f in (
-            lib.wersa_decay_forward, lib.wersa_decay_clear, lib.wersa_decay_backward, lib.wersa_decay_workspace_bytes, lib.wersa_decay_saved_bytes,
+            lib.wersa_decay_forward, lib.wersa_decay_backward, lib.wersa_decay_workspace_bytes, lib.wersa_decay_saved_bytes,
             lib.wersa_rms_norm_forward, lib.wersa_rms_norm_backward, lib.wersa_rms_norm_workspace_bytes)])
         _node = node
     return _node

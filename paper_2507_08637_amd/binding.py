@@ -24,8 +24,7 @@ EXPORTS = ["wersa_workspace_bytes", "wersa_saved_bytes", "wersa_forward", "wersa
            "wersa_block_workspace_bytes", "wersa_block_saved_bytes", "wersa_block_saved_offset",
            "wersa_block_workspace_offset",
            "wersa_block_forward", "wersa_block_backward",
-           "wersa_decay_workspace_bytes", "wersa_decay_saved_bytes", "wersa_decay_forward", "wersa_decay_clear", "wersa_decay_backward",
-           "wersa_decay_step",
+           "wersa_decay_workspace_bytes", "wersa_decay_saved_bytes", "wersa_decay_forward", "wersa_decay_backward", "wersa_decay_step",
            "wersa_rms_norm_forward", "wersa_rms_norm_eight_bit", "wersa_rms_norm_workspace_bytes", "wersa_rms_norm_backward"]
 
 
@@ -40,7 +39,8 @@ class WersaDesc(ctypes.Structure):
 class WersaDecayDesc(ctypes.Structure):
     _fields_ = [("B", ctypes.c_int32), ("H", ctypes.c_int32), ("n", ctypes.c_int32), ("dk", ctypes.c_int32),
                 ("dv", ctypes.c_int32), ("dtype", ctypes.c_int32), ("packed", ctypes.c_int32), ("scale", ctypes.c_float)] + \
-               [(name, ctypes.c_int64 * 3) for name in ("stride_q", "stride_k", "stride_v", "stride_o", "stride_dq", "stride_dk", "stride_dv")]
+               [(name, ctypes.c_int64 * 3) for name in ("stride_q", "stride_k", "stride_v", "stride_o", "stride_dq", "stride_dk", "stride_dv")] + \
+               [("clear", ctypes.c_int32)]
 
 
 class WersaNormDesc(ctypes.Structure):
@@ -110,8 +110,6 @@ def load_library():
     lib.wersa_decay_saved_bytes.argtypes = [ddp]
     lib.wersa_decay_forward.restype = ctypes.c_int
     lib.wersa_decay_forward.argtypes = [ddp] + [vp] * 8 + [ctypes.c_int32] + [vp] * 3 + [ctypes.c_size_t, vp]
-    lib.wersa_decay_clear.restype = ctypes.c_int
-    lib.wersa_decay_clear.argtypes = [ddp] + [vp] * 3
     lib.wersa_decay_backward.restype = ctypes.c_int
     lib.wersa_decay_backward.argtypes = [ddp] + [vp] * 14 + [ctypes.c_size_t, vp]
     lib.wersa_decay_step.restype = ctypes.c_int
@@ -476,15 +474,14 @@ def _dtype_code(x):
     raise TypeError("dtype must be float32 or bfloat16")
 
 
-_DECAY_DESC = struct.Struct("7if21q")   # (a structure of ctypes takes several times as long to fill in field by field)
+# (a structure of ctypes takes several times as long to fill in field by field)
+_DECAY_DESC = struct.Struct("7if12q72xi4x")   # without the gradients' strides
+_GRAD_STRIDES = struct.Struct("9q")
 
 
-_AS_THEIR_TENSORS = (0,) * 9
-
-
-def make_decay_desc(q, k, v, out, scale=None, offsets=None, grad_strides=_AS_THEIR_TENSORS):
+def make_decay_desc(q, k, v, out, scale=None, offsets=None, clear=False):
     """Descriptor for q, k (B, H, n, dk) and v, out (B, H, n, dv), last dimension contiguous; with offsets (B + 1) the tensors
-    have one batch entry that holds the rows of all B sequences.  scale: 1 / sqrt(dk) by default.  grad_strides: three of each of dq, dk, dv."""
+    have one batch entry that holds the rows of all B sequences.  scale: 1 / sqrt(dk) by default.  clear: the forward writes zeros to rows of no sequence."""
     assert q.dim() == 4 and v.dim() == 4, "expect q, k (B, H, n, dk) and v, out (B, H, n, dv)"
     (N, H, n, dk), dv = q.shape, v.shape[3]
     assert k.shape == q.shape and v.shape == (N, H, n, dv) and out.shape == v.shape, "expect q, k (B, H, n, dk) and v, out (B, H, n, dv)"
@@ -499,18 +496,19 @@ def make_decay_desc(q, k, v, out, scale=None, offsets=None, grad_strides=_AS_THE
         B = offsets.numel() - 1
     return WersaDecayDesc.from_buffer_copy(_DECAY_DESC.pack(
         B, H, n, dk, dv, _dtype_code(q), offsets is not None, dk ** -0.5 if scale is None else scale,
-        qb, qh, qn, kb, kh, kn, vb, vh, vn, ob, oh, on, *grad_strides))
+        qb, qh, qn, kb, kh, kn, vb, vh, vn, ob, oh, on, clear))
 
 
 def _dense_like(x):
     """A new tensor of x's shape, with its dimensions in x's order in memory but none apart from or on another: x may be a slice, or windows that overlap."""
-    shape, strides = x.shape, x.stride()
-    (N, H, n, d), (b, h, r, _) = shape, strides
-    if not ((r == d and h == n * d or h == d and r == H * d) and b == H * n * d):   # (otherwise it is dense)
-        step, strides = d, [1] * 4
-        for i in sorted(range(3), key=x.stride):
-            strides[i] = step
-            step *= max(1, shape[i])
+    shape = N, H, n, d = x.shape
+    b, h, r, _ = x.stride()
+    if (r == d and h == n * d or h == d and r == H * d) and b == H * n * d:
+        return torch.empty_like(x)
+    step, strides = d, [1] * 4
+    for i in sorted(range(3), key=x.stride):
+        strides[i] = step
+        step *= max(1, shape[i])
     return torch.empty_strided(shape, strides, dtype=x.dtype, device=x.device)
 
 
@@ -572,10 +570,11 @@ def wersa_decay_forward(q, k, v, log_decay, scale=None, offsets=None, initial_st
     the caller's."""
     lib = load_library()
     clear = out is None and offsets is not None
-    q, k, v = _not_broadcast(q, stream), _not_broadcast(k, stream), _not_broadcast(v, stream)
+    if 0 in q.stride() or 0 in k.stride() or 0 in v.stride():
+        q, k, v = _not_broadcast(q, stream), _not_broadcast(k, stream), _not_broadcast(v, stream)
     if out is None:
         out = _dense_like(v)
-    desc = make_decay_desc(q, k, v, out, scale, offsets)
+    desc = make_decay_desc(q, k, v, out, scale, offsets, clear=clear)
     _check_log_decay(log_decay, desc)
     if want_state and final_state is None:
         assert slots is None, "with slots the states lie in a buffer of the caller's"
@@ -593,8 +592,6 @@ def wersa_decay_forward(q, k, v, log_decay, scale=None, offsets=None, initial_st
     _check(lib.wersa_decay_forward(ctypes.byref(desc), _addr(q), _addr(k), _addr(v), _addr(log_decay), _addr(offsets), _addr(initial_state),
                                    _addr(final_state), _addr(slots), rows, _addr(out), _addr(saved), _addr(workspace),
                                    0 if workspace is None else _nbytes(workspace), _stream(stream)))
-    if clear:
-        _check(lib.wersa_decay_clear(ctypes.byref(desc), _addr(offsets), _addr(out), _stream(stream)))
     return out, final_state, saved
 
 
@@ -610,7 +607,8 @@ def wersa_decay_backward(q, k, v, log_decay, dout, saved, scale=None, offsets=No
     for name, x in (("dq", q), ("dk", k), ("dv", v)):
         g = grads[name]
         assert g.shape == x.shape and g.dtype == x.dtype and g.stride(3) == 1, f"{name} has its tensor's shape and dtype, and a contiguous last dim"
-    desc = make_decay_desc(q, k, v, dout, scale, offsets, [s for name in ("dq", "dk", "dv") for s in grads[name].stride()[:3]])
+    desc = make_decay_desc(q, k, v, dout, scale, offsets)
+    _GRAD_STRIDES.pack_into(desc, WersaDecayDesc.stride_dq.offset, *(s for name in ("dq", "dk", "dv") for s in grads[name].stride()[:3]))
     _check_log_decay(log_decay, desc)
     _check_states(desc, None, initial_state, dfinal_state)
     sb = lib.wersa_decay_saved_bytes(ctypes.byref(desc))
@@ -642,7 +640,7 @@ def wersa_decay_step(q, k, v, log_decay, state, scale=None, slots=None, out=None
         (qb, qh, q1), (kb, kh, k1), (vb, vh, v1) = q.stride(), k.stride(), v.stride()
     assert q1 == k1 == v1 == o1 == 1, "expect a contiguous last dim"
     desc = WersaDecayDesc.from_buffer_copy(_DECAY_DESC.pack(B, H, 1, dk, dv, _dtype_code(q), 0, dk ** -0.5 if scale is None else scale,
-                                                            qb, qh, 0, kb, kh, 0, vb, vh, 0, ob, oh, 0, *_AS_THEIR_TENSORS))
+                                                            qb, qh, 0, kb, kh, 0, vb, vh, 0, ob, oh, 0, 0))
     _check_log_decay(log_decay, desc)
     rows = _check_states(desc, slots, state)
     _on_one_gpu(q, k, v, log_decay, state, slots, out)

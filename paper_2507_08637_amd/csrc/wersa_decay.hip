@@ -895,14 +895,41 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : 2) void back_bf16_kernel(W
   }
 }
 
+// Packed sequences lie one behind the other: rows of none are those before the first one and those behind the last one. Zeros to them, for nothing else writes them, in
+// up to three tensors. With a launch of their own (sequences of one segment) or beside the scan's workgroups, which costs no time of its own where there are no such rows.
+struct Outside {
+  void *to[3];              // the first one null: not wanted
+  Strides stride[3];
+  int width[3];
+  int element;
+};
+__device__ __forceinline__ void clear_outside(const Sequences &q, const Outside &a, int h, int group, int groups) {
+  typedef u32x4 u32x4_any __attribute__((aligned(2)));
+  const int first = q.begin(0), last = max(first, q.begin(q.B)), rows = first + q.n - last;
+#pragma unroll
+  for (int u = 0; u < 3; ++u) {
+    if (!a.to[u]) break;
+    const int per_row = a.width[u] * a.element / 16, at_once = (int)blockDim.x / per_row, mine = (int)threadIdx.x / per_row;   // pieces of 16 bytes; whole rows at a time
+    char *to = (char *)a.to[u] + h * a.stride[u].h * a.element + (int)threadIdx.x % per_row * 16;
+    if (mine < at_once)
+      for (int64_t i = (int64_t)group * at_once + mine; i < rows; i += (int64_t)groups * at_once)
+        *(u32x4_any *)(to + (i < first ? i : i + (last - first)) * a.stride[u].n * a.element) = u32x4{0, 0, 0, 0};
+  }
+}
+__global__ __launch_bounds__(256) void clear_kernel(Sequences seq, Outside a) { clear_outside(seq, a, blockIdx.y, blockIdx.x, gridDim.x); }
+
 // What the segments of a sequence add to the state, in place, to the states that they begin with: E values of a state per thread, over all
 // segments in their order (from the last one with `reverse`).  Few states are bound by the way to memory and back of each round of requests: rounds have many,
 // and a thread has one value, so that there are threads; many states (packed prompts) by the launch of their workgroups: four values then.  24 packed prompts, 16 heads
 // of 128 x 128: 77 us with one value; 8 slices of 64 x 64, 96 segments: 31 us with four values and rounds of eight.
 template <int E, int ROUND>
-__global__ __launch_bounds__(256) void scan_kernel(Walk a, float *local) {
+__global__ __launch_bounds__(256) void scan_kernel(Walk a, float *local, Outside outside) {
   typedef float V __attribute__((ext_vector_type(E)));
   const int h = blockIdx.y, b = blockIdx.z;
+  if (b == a.seq.B) {
+    clear_outside(a.seq, outside, h, blockIdx.x, gridDim.x);
+    return;
+  }
   const int64_t state_size = (int64_t)a.kw * a.vw, e = ((int64_t)blockIdx.x * blockDim.x + threadIdx.x) * E;
   if (e >= state_size) return;
   const int segs = a.seq.segments(b), have = a.seq.rows(b), own = cache_row(a, b);
@@ -925,26 +952,6 @@ __global__ __launch_bounds__(256) void scan_kernel(Walk a, float *local) {
       if (s0 + u < segs) *(V *)(p + s * step) = run;
       run = run * (s == segs - 1 ? tail : full) + x[u];
     }
-  }
-}
-
-// Packed sequences lie one behind the other: rows of none are those before the first one and those behind the last one. Zeros to them, for
-// nothing else writes them: 16 bytes to a thread, so far as there are any.
-struct Outside {
-  void *to[3];
-  Strides stride[3];
-  int width[3];             // bytes
-  int element;
-};
-__global__ __launch_bounds__(256) void clear_kernel(Sequences seq, Outside a) {
-  typedef u32x4 u32x4_any __attribute__((aligned(2)));
-  const int which = blockIdx.z, h = blockIdx.y, per_row = a.width[which] / 16;
-  const int first = seq.begin(0), last = max(first, min(max(seq.offsets[seq.B], 0), seq.n));
-  const int64_t pieces = (int64_t)(first + seq.n - last) * per_row;
-  char *to = (char *)a.to[which] + h * a.stride[which].h * a.element;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < pieces; i += (int64_t)gridDim.x * 256) {
-    const int64_t at = i / per_row, row = at < first ? at : at + (last - first);
-    *(u32x4_any *)(to + row * a.stride[which].n * a.element + i % per_row * 16) = u32x4{0, 0, 0, 0};
   }
 }
 
@@ -1120,7 +1127,7 @@ wersa_status validate(const wersa_decay_desc *c) {
   if (!c) return WERSA_ERR_INVALID_ARG;
   if (c->B < 1 || c->H < 1 || c->n < 0 || c->dk < 1 || c->dv < 1) return WERSA_ERR_INVALID_ARG;
   if (c->dtype != WERSA_F32 && c->dtype != WERSA_BF16) return WERSA_ERR_INVALID_ARG;
-  if (c->packed != 0 && c->packed != 1) return WERSA_ERR_INVALID_ARG;
+  if ((c->packed != 0 && c->packed != 1) || (c->clear != 0 && c->clear != 1)) return WERSA_ERR_INVALID_ARG;
   if (!(c->scale - c->scale == 0.f)) return WERSA_ERR_INVALID_ARG;   // not finite
   if (!strides_ok(c->stride_q, *c, c->dk) || !strides_ok(c->stride_k, *c, c->dk) || !strides_ok(c->stride_v, *c, c->dv) ||
       !strides_ok(c->stride_o, *c, c->dv))
@@ -1167,20 +1174,20 @@ bool launch_back(const wersa_decay_desc &c, const Walk &a, const Back &b, hipStr
   if (a.kw <= 64) return a.vw <= 64 ? launch_back_as<64, 64>(c, a, b, st) : launch_back_as<64, 128>(c, a, b, st);
   return a.vw <= 64 ? launch_back_as<128, 64>(c, a, b, st) : launch_back_as<128, 128>(c, a, b, st);
 }
-void launch_clear(const wersa_decay_desc &c, const Sequences &seq, int tensors, Outside a, hipStream_t st) {
-  if (!c.packed || c.n == 0) return;
-  a.element = c.dtype == WERSA_F32 ? 4 : 2;
-  const int64_t most = (int64_t)c.n * std::max(c.dk, c.dv) * a.element / 16;
-  const int64_t across = std::min<int64_t>((most + 255) / 256, std::max(1, 2048 / (c.H * tensors)));
-  for (int i = 0; i < tensors; ++i) a.width[i] *= a.element;
-  WERSA_STAGE("wersa_decay_clear", st, (clear_kernel<<<dim3((unsigned)across, c.H, tensors), 256, 0, st>>>(seq, a)));
-}
-void launch_scan(const Walk &a, float *local, hipStream_t st) {
+// Returns whether rows of no sequence are cleared.
+bool launch_scan(const Walk &a, float *local, const Outside &outside, hipStream_t st) {
   const int size = a.kw * a.vw;
+  const bool clear = outside.to[0] && a.seq.B < 65535;   // (blockIdx.z)
+  const int depth = a.seq.B + clear;
   if ((int64_t)size * a.H * a.seq.B >= 1 << 21)   // eight waves of four values to a SIMD
-    WERSA_STAGE("wersa_decay_scan", st, (scan_kernel<4, 8><<<dim3((size / 4 + 255) / 256, a.H, a.seq.B), 256, 0, st>>>(a, local)));
+    WERSA_STAGE("wersa_decay_scan", st, (scan_kernel<4, 8><<<dim3((size / 4 + 255) / 256, a.H, depth), 256, 0, st>>>(a, local, outside)));
   else
-    WERSA_STAGE("wersa_decay_scan", st, (scan_kernel<1, 32><<<dim3((size + 63) / 64, a.H, a.seq.B), 64, 0, st>>>(a, local)));
+    WERSA_STAGE("wersa_decay_scan", st, (scan_kernel<1, 32><<<dim3((size + 63) / 64, a.H, depth), 64, 0, st>>>(a, local, outside)));
+  return clear;
+}
+void launch_clear(const wersa_decay_desc &c, const Sequences &seq, const Outside &outside, hipStream_t st) {
+  const int64_t across = std::min<int64_t>(((int64_t)c.n * std::max(c.dk, c.dv) * outside.element / 16 + 255) / 256, std::max(1, 2048 / c.H));
+  WERSA_STAGE("wersa_decay_clear", st, (clear_kernel<<<dim3((unsigned)across, c.H), 256, 0, st>>>(seq, outside)));
 }
 
 }  // namespace
@@ -1221,25 +1228,19 @@ wersa_status wersa_decay_forward(const wersa_decay_desc *desc, const void *q, co
   a.heads_first = heads_first(c, a.seq);
   a.H = c.H, a.kw = c.dk, a.vw = c.dv, a.si = c.dv, a.sj = 1;
   a.intra = a.inter = c.scale, a.gain = 1.f;
+  Outside outside{{}, {}, {}, c.dtype == WERSA_F32 ? 4 : 2};
+  bool clear = c.packed && c.clear && c.n > 0;
+  if (clear) outside.to[0] = out, outside.stride[0] = a.so, outside.width[0] = c.dv;
   if (split) {
     float *local = (float *)(saved ? saved : workspace);
     a.fin = local;
     if (!launch_walk<true>(c, a, st)) return WERSA_ERR_LAUNCH;
-    launch_scan(a, local, st);
+    if (launch_scan(a, local, outside, st)) clear = false;
     a.init = local, a.by_slot = true;
   }
+  if (clear) launch_clear(c, a.seq, outside, st);
   a.fin = final_state;
   if (!launch_walk<false>(c, a, st)) return WERSA_ERR_LAUNCH;
-  return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
-}
-
-wersa_status wersa_decay_clear(const wersa_decay_desc *desc, const int32_t *offsets, void *out, void *hip_stream) {
-  const wersa_status vs = validate(desc);
-  if (vs != WERSA_OK) return vs;
-  const wersa_decay_desc &c = *desc;
-  if ((c.n > 0 && !out) || (c.packed != 0) != (offsets != nullptr)) return WERSA_ERR_INVALID_ARG;
-  if (const wersa_status ws = written(c.stride_o, c, c.dv)) return ws;
-  launch_clear(c, sequences(c, offsets), 1, Outside{{out}, {strides(c.stride_o, c, c.dv)}, {c.dv}, 0}, (hipStream_t)hip_stream);
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
 
@@ -1286,16 +1287,19 @@ wersa_status wersa_decay_backward(const wersa_decay_desc *desc, const void *q, c
   r.q = k, r.k = q, r.v = dout, r.o = dv;
   r.sq = sk, r.sk = sq, r.sv = so, r.so = sdv;
   r.kw = c.dk, r.vw = c.dv, r.si = c.dv, r.sj = 1;
+  Outside outside{{}, {}, {}, c.dtype == WERSA_F32 ? 4 : 2};
+  bool clear = c.packed && c.n > 0;
+  if (clear) outside = Outside{{dq, dk, dv}, {sdq, sdk, sdv}, {c.dk, c.dk, c.dv}, outside.element};
   if (split) {
     r.fin = (float *)workspace;
     if (!launch_walk<true>(c, r, st)) return WERSA_ERR_LAUNCH;
-    launch_scan(r, (float *)workspace, st);
+    if (launch_scan(r, (float *)workspace, outside, st)) clear = false;
     r.init = (const float *)workspace;
     r.by_slot = true;
   }
+  if (clear) launch_clear(c, a.seq, outside, st);
   r.fin = dinitial_state;
   if (!launch_back(c, r, Back{k, v, dk, dv, sk, sv, sdk, sdv}, st)) return WERSA_ERR_LAUNCH;
-  launch_clear(c, a.seq, 3, Outside{{dq, dk, dv}, {sdq, sdk, sdv}, {c.dk, c.dk, c.dv}, 0}, st);
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
 

@@ -137,7 +137,6 @@ Tensor attention(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor
 // Decay attention and the RMS norm, whose kernels for some thousand tokens take less than the host's part of a step.  128000 rows of 128, float32, forward and backward of the norm: 95 us
 // with a node in Python where the engine's thread runs near the caller's, 175 where it runs far; its kernels take 97.
 decltype(&wersa_decay_forward) decay_forward_fn = nullptr;
-decltype(&wersa_decay_clear) decay_clear_fn = nullptr;
 decltype(&wersa_decay_backward) decay_backward_fn = nullptr;
 decltype(&wersa_decay_workspace_bytes) decay_workspace_bytes_fn = nullptr;
 decltype(&wersa_decay_saved_bytes) decay_saved_bytes_fn = nullptr;
@@ -180,11 +179,11 @@ struct DecayAttention : torch::autograd::Function<DecayAttention> {
     std::memcpy(&d, desc.data(), sizeof(d));
     const Tensor out = dense_like(v);
     put_strides(d.stride_o, out);
+    d.clear = d.packed;
     const auto f32 = q.options().dtype(at::kFloat);
     const Tensor final_state = at::empty({d.B, d.H, d.dk, d.dv}, f32), saved = at::empty({saved_bytes / 4}, f32);
     check(decay_forward_fn(&d, in(q), in(k), in(v), floats(log_decay), (const int32_t *)in(offsets), (const float *)in(initial), floats_out(final_state), nullptr,
                            d.B, out.mutable_data_ptr(), saved.mutable_data_ptr(), nullptr, 0, stream(q)));
-    if (d.packed) check(decay_clear_fn(&d, (const int32_t *)in(offsets), out.mutable_data_ptr(), stream(q)));
     ctx->save_for_backward({q, k, v, log_decay, initial, offsets, saved});
     ctx->saved_data["desc"] = desc;
     ctx->set_materialize_grads(false);
@@ -289,15 +288,14 @@ PYBIND11_MODULE(_wersa_torch, m) {
   });
   m.def("attention", &attention);
   m.def("bind_causal", [](const std::vector<uintptr_t> &at) {
-    TORCH_CHECK(at.size() == 8, "eight entry points");
+    TORCH_CHECK(at.size() == 7, "seven entry points");
     decay_forward_fn = reinterpret_cast<decltype(decay_forward_fn)>(at[0]);
-    decay_clear_fn = reinterpret_cast<decltype(decay_clear_fn)>(at[1]);
-    decay_backward_fn = reinterpret_cast<decltype(decay_backward_fn)>(at[2]);
-    decay_workspace_bytes_fn = reinterpret_cast<decltype(decay_workspace_bytes_fn)>(at[3]);
-    decay_saved_bytes_fn = reinterpret_cast<decltype(decay_saved_bytes_fn)>(at[4]);
-    norm_forward_fn = reinterpret_cast<decltype(norm_forward_fn)>(at[5]);
-    norm_backward_fn = reinterpret_cast<decltype(norm_backward_fn)>(at[6]);
-    norm_workspace_bytes_fn = reinterpret_cast<decltype(norm_workspace_bytes_fn)>(at[7]);
+    decay_backward_fn = reinterpret_cast<decltype(decay_backward_fn)>(at[1]);
+    decay_workspace_bytes_fn = reinterpret_cast<decltype(decay_workspace_bytes_fn)>(at[2]);
+    decay_saved_bytes_fn = reinterpret_cast<decltype(decay_saved_bytes_fn)>(at[3]);
+    norm_forward_fn = reinterpret_cast<decltype(norm_forward_fn)>(at[4]);
+    norm_backward_fn = reinterpret_cast<decltype(norm_backward_fn)>(at[5]);
+    norm_workspace_bytes_fn = reinterpret_cast<decltype(norm_workspace_bytes_fn)>(at[6]);
   });
   m.def("decay_attention", &decay_attention);
   m.def("rms_norm", &rms_norm);
