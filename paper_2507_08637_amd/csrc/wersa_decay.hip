@@ -422,15 +422,15 @@ __global__ __launch_bounds__(64 * f32_waves(DK, DV)) void back_f32_kernel(Walk a
   f32x4 K[KT], V[CT];
   const TilePieces<DK, 4, PK, THREADS, false> qp(qr, 0, tid);
   const TilePieces<DV, 4, PV, THREADS, false> dp(dr, 0, tid);
-  const uint32_t kat = kr.offset(16 * part.t + c, 16 * g), vat = vr.offset(16 * part.t + c, 16 * g);
-  const uint32_t dkat = dkr.offset(16 * part.t + c, 16 * g), dvat = dvr.offset(16 * part.t + c, 16 * g);
+  // Places of own rows are formed where they are used: of four strides, they take registers that width 128 has not (229 us kept, 219 so, 16 slices of 8192 rows).
+  auto at_of = [&](const Rows &r) { return r.offset(16 * part.t + (int)opaque((uint32_t)c), 16 * g); };
   auto request = [&](int r0) {
     qp.template load<false>(qr, r0, rq);
     dp.template load<false>(dr, r0, rd);
   };
   auto request_own = [&](int r0) {
-    load_own_f32<DK>(kr, r0, kat, g, K);
-    load_own_f32<DV>(vr, r0, vat, g, V);
+    load_own_f32<DK>(kr, r0, at_of(kr), g, K);
+    load_own_f32<DV>(vr, r0, at_of(vr), g, V);
   };
   request(0);
   request_own(0);
@@ -445,9 +445,9 @@ __global__ __launch_bounds__(64 * f32_waves(DK, DV)) void back_f32_kernel(Walk a
       for (int ct = 0; ct < P4::CW; ++ct) *(f32x4 *)(Gt + (part.col0 + 16 * ct + c) * LK + part.row0 + 16 * rt + 4 * g) = G[rt][ct];
     __syncthreads();
     request(r0 + kChunk);
-    weighted_rows_f32<DV, P4::HALVES>(Ds, dvr, r0, dvat, vcol, part.t, g, c, [&](int ct) { return products_f32<DK>(Gt + vcol * LK, ct, K, g, c) * weights.reach; },
+    weighted_rows_f32<DV, P4::HALVES>(Ds, dvr, r0, at_of(dvr), vcol, part.t, g, c, [&](int ct) { return products_f32<DK>(Gt + vcol * LK, ct, K, g, c) * weights.reach; },
                                       [&](int jt) { return weights(products_f32<DK>(Qs, jt, K, g, c), jt); });
-    weighted_rows_f32<DK, P4::HALVES>(Qs, dkr, r0, dkat, kcol, part.t, g, c, [&](int kt) {   // G v: rows of G down the lanes, its columns four values apart in Gt
+    weighted_rows_f32<DK, P4::HALVES>(Qs, dkr, r0, at_of(dkr), kcol, part.t, g, c, [&](int kt) {   // G v: rows of G down the lanes, its columns four values apart in Gt
       f32x4 acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int j = 0; j < CT; ++j)
