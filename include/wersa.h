@@ -344,7 +344,8 @@ double wersa_peak_mfma(float *sink, int32_t reps, void *hip_stream);
 
 const char *wersa_status_string(wersa_status status);
 
-/* Library version, major*10000 + minor*100 + patch. */
+/* Library version, major*10000 + minor*100 + patch.  200: wersa_decay_desc has the gradients' strides and clear (a program built
+ * against an older header passes a shorter structure, and has to be built again). */
 int32_t wersa_version(void);
 
 #ifdef __cplusplus

@@ -42,3 +42,10 @@ def test_dense_like():
     for view in (x[:, :1].expand(2, 3, 10, 16), x[:1, :1].expand(2, 3, 10, 16), x[..., :1, :].expand(2, 3, 10, 16), torch.zeros(2, 3, 16, 1).mT):
         made = _dense_like(view)
         assert made.shape == view.shape and made.stride(3) == 1 and made.untyped_storage().nbytes() == made.numel() * 4
+
+
+def test_version_tells_the_descriptors_apart(lib):  # noqa: F811
+    """The gradients' strides and `clear` lie behind what the descriptor of version 100 had, 128 bytes."""
+    from paper_2507_08637_amd.binding import WersaDecayDesc
+    assert lib.wersa_version() >= 200
+    assert WersaDecayDesc.stride_dq.offset == 128 and WersaDecayDesc.clear.offset == 200 and ctypes.sizeof(WersaDecayDesc) == 208
