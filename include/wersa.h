@@ -244,7 +244,10 @@ int64_t wersa_block_workspace_offset(const wersa_desc *desc, int which);
  * wersa_decay_backward: the gradients of a scalar loss given those with respect to out and (dfinal_state, by sequence, may be
  * NULL) the final states; initial_state is by sequence; dinitial_state may be NULL.
  * Supported: dk, dv multiples of 16 up to 128; n up to 2^30 (0: the final state is the initial one); B, H up to 65535.
- * Arithmetic: states and every sum in float32.  The other conventions are those above.
+ * Arithmetic: states and every sum in float32.  For bf16 tensors the weighted products of a chunk's rows (64 of them) and the
+ * state as an operand of an output are rounded to bf16 once, as the output is: 2.3e-3 of an output in the 2-norm, where rounding the
+ * output alone leaves 1.7e-3; what goes into a state is not.  wersa_decay_step rounds its output only.  A row that is not finite reaches
+ * only what depends on it, which is then not finite, and may be NaN where the definition has an infinity.  The other conventions are those above.
  */
 typedef struct {
   int32_t B, H, n, dk, dv;
@@ -279,8 +282,8 @@ wersa_status wersa_decay_step(const wersa_decay_desc *desc, const void *q, const
  * Root-mean-square norm over the columns of a row, with the residual's addition before it:
  *   r = x + residual (kept in the tensors' type; with residual NULL r is x itself and nothing is written),
  *   y = r * rstd * weight,  rstd = 1 / sqrt(mean(r^2) + eps)
- * The norm reads the stream r as it is kept.  x and residual are (rows, cols) at row strides of their own, columns
- * contiguous; r, y, dy, dr and dx are dense.  weight is float32 [cols] or NULL (ones); rstd float32 [rows], NULL:
+ * The norm reads the stream r as it is kept.  x and residual are (rows, cols) at row strides of their own, at
+ * least cols, columns contiguous; r, y, dy, dr and dx are dense.  weight is float32 [cols] or NULL (ones); rstd float32 [rows], NULL:
  * not wanted.  wersa_rms_norm_eight_bit writes y in 8 bits (e4m3, largest value 448) and float32 scales [rows]:
  *   scale = max|y| / 448,  y8 = e4m3(y * (448 / max|y|)) to the nearest, ties to even;  a row of zeros has scale 1.  The bits are
  *   right for rows of any size; below max|y| = 448 * 2^-126 = 5e-36 the scale has fewer than 24 bits, down to zero.

@@ -315,7 +315,7 @@ __device__ __forceinline__ void weighted_rows_f32(const float *rows, const Rows 
 
 // Weights are formed as their transpose (the chunk's rows down the registers, own rows on the lanes), which is the layout that the product with V takes them in.
 // Eight waves at width 128, where LDS holds one workgroup to a compute unit: two to a SIMD, which form their rows' weights twice.
-// Up to width 32 near memory (128 slices of 4000 rows: 64 us, 4.1 TB/s), above by the matrix units: 32 slices of 8192 rows, width 64, 82 us, 3.3 TB/s; 16 slices, width 128, 136 us, 2.0 TB/s,
+// Up to width 32 near memory (128 slices of 4000 rows: 64 us, 4.1 TB/s), above by the matrix units: 32 slices of 8192 rows, width 64, 86 us, 3.1 TB/s; 16 slices, width 128, 136 us, 2.0 TB/s,
 // about 92 of the 157 TFLOP/s that float32 matrix instructions have at their nominal clock.
 constexpr int f32_waves(int dk, int dv) { return dk > 64 || dv > 64 ? 8 : 4; }
 template <int DK, int DV, bool STATES>
@@ -719,8 +719,9 @@ __device__ __forceinline__ void update_state(const Part<DK, DV> &part, f32x4 (&S
 }
 
 // As walk_f32_kernel, for bf16 tensors.  P and the state as an operand of the output are rounded to bf16, like the output (each 2^-9 of a result in the root mean square; P in two terms would
-// take the error of a result from 0.0023 to 0.0020 of it, for 4 %); what goes into the state is not.  Bound by memory: width 128, 32 slices of 65536 rows, 460 us, 4.7 TB/s (416 without the update
-// of the state; loads and stores alone 380 to 400); width 64, 8 slices of 131072, 100 us, 5.4 TB/s; forming states alone 213 us, 5.0 TB/s (199 without the products), and 57 us, 4.7 TB/s.
+// take the error of a result from 0.0023 to 0.0020 of it, for 4 %); what goes into the state is not.  Bound by memory: width 128, 32 slices of 65536 rows, 446 to 459 us on two cards, 4.7 TB/s
+// (without the update of the state 416 where it took 462; loads and stores alone 380 to 400); width 64, 8 slices of 131072, 89 to 96 us, 5.6 TB/s; forming states alone 211 to 214 us, 5.0 TB/s (199 without the
+// products), and 53 to 60 us, 4.5 to 5.1 TB/s.
 template <int DK, int DV, bool FULL, bool STATES, bool NT>
 __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) void walk_bf16_kernel(Walk a) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;   // pieces of a thread
@@ -807,7 +808,7 @@ __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : DK + DV <= 128 ? 3 : 2) vo
   if (fin) each_of_state(a, S, part, g, c, [&](float x, bool there, int64_t at) { if (there) fin[at] = x; return x; });
 }
 
-// As back_f32_kernel, for bf16 tensors.  Width 128, 32 slices of 65536 rows: 670 us, 4.8 TB/s (630 without the update of the state); two walks took 2 x 502.
+// As back_f32_kernel, for bf16 tensors.  Width 128, 32 slices of 65536 rows: 654 to 670 us on two cards, 4.8 to 4.9 TB/s (630 without the update of the state where it took 672); two walks took 2 x 502.
 template <int DK, int DV, bool FULL, bool NT>
 __global__ __launch_bounds__(256, DK + DV <= 64 ? 4 : 2) void back_bf16_kernel(Walk a, Back b) {
   constexpr int PK = kChunk * DK / 8 / 256, PV = kChunk * DV / 8 / 256;
