@@ -308,6 +308,75 @@ wersa_status wersa_rms_norm_backward(const wersa_norm_desc *desc, const void *r,
                                      const void *dy, const void *dr, void *dx, float *dweight, void *workspace,
                                      size_t workspace_bytes, void *hip_stream);
 
+/*
+ * Layer norm over the columns of a row, with the residual's addition before it (the conventions, types and limits of the RMS norm):
+ *   r = x + residual (kept in the tensors' type; with residual NULL r is x itself and nothing is written),
+ *   y = (r - m) * rstd * weight + bias,  m = mean(r),  rstd = 1 / sqrt(mean((r - m)^2) + eps)
+ * weight and bias are float32 [cols], either may be NULL (ones, zeros); stats is float32 [rows][2], m and rstd of each row, NULL: not wanted.
+ * wersa_layer_norm_backward: dx is the gradient of x and of the residual (dr: what reaches r from elsewhere, NULL: nothing); dweight and dbias
+ * (float32 [cols]) may each be NULL: not wanted; for either the workspace is needed.
+ */
+wersa_status wersa_layer_norm_forward(const wersa_norm_desc *desc, const void *x, const void *residual, const float *weight,
+                                      const float *bias, void *r, void *y, float *stats, void *hip_stream);
+size_t wersa_layer_norm_workspace_bytes(const wersa_norm_desc *desc);
+wersa_status wersa_layer_norm_backward(const wersa_norm_desc *desc, const void *r, const float *weight, const float *stats,
+                                       const void *dy, const void *dr, void *dx, float *dweight, float *dbias, void *workspace,
+                                       size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Rows of an embedding for tokens, and the gradient of its weights:
+ *   out[i] = scale * weight[token_i],   dweight[v] = scale * (sum of dout[i] over the places i with token_i = v)
+ * A token below 0 or from vocabulary on has no row: zeros in out, and no part in dweight (a batch's padding, rows that another device holds).
+ * tokens: device integers of token_bytes (4 or 8), contiguous.  weight (vocabulary, cols) at rows of stride_weight, out (tokens, cols) at rows of
+ * stride_out, at least cols; wersa_embedding_backward reads dout at stride_out and writes every row of dweight at stride_weight, those of tokens
+ * that are nowhere with zeros.  Columns contiguous; any element-aligned pointer is taken (the workspace: 256 bytes).  Types: dtype of out and dout,
+ * weight_dtype of weight and dweight.  Sums in float32, places in their order within pieces of the sorted list and these in theirs: the same bits every time.
+ * Supported: tokens below 2^31 (0: zeros in dweight), vocabulary below 2^31, cols up to 2^20.
+ */
+typedef struct {
+  int64_t tokens;
+  int32_t vocabulary, cols;
+  int32_t dtype, weight_dtype; /* wersa_dtype of out and dout, of weight and dweight */
+  int32_t token_bytes;
+  float scale;
+  int64_t stride_weight, stride_out;
+} wersa_embedding_desc;
+
+wersa_status wersa_embedding_forward(const wersa_embedding_desc *desc, const void *tokens, const void *weight, void *out,
+                                     void *hip_stream);
+size_t wersa_embedding_workspace_bytes(const wersa_embedding_desc *desc);
+wersa_status wersa_embedding_backward(const wersa_embedding_desc *desc, const void *tokens, const void *dout, void *dweight,
+                                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Logits before a token is chosen: penalties for tokens that were there before, biases, a mask of bits.  For each of B rows and each token v, in float32 and
+ * in this order:
+ *   v in the row's history:  z = z > 0 ? z / repetition : z * repetition
+ *                            z -= frequency * count + (count > 0 ? presence : 0),  count: how often v is in the history behind the prompt
+ *   biases:                  z += the biases of v, in their order
+ *   v not allowed:           z = -infinity, whatever it was (a row that allows nothing is all -infinity)
+ * logits and out are (B, vocabulary) at row strides of their own, columns contiguous, and may be the same buffer; any element-aligned pointer is taken.
+ *   history  int32 [history_rows][history_most] at rows of stride_history, or NULL; lengths int32 [history_rows] (clamped to 0 .. history_most) and
+ *            prompt_lengths int32 [history_rows] (NULL: none): how many tokens there are, and how many of the first of them are the
+ *            prompt.  slots int32 [B] or NULL: row b has history slots[b], or b; one below 0 or from history_rows on is none.
+ *   repetition, presence, frequency  float32 [B], each may be NULL (1, 0, 0).  repetition is above 0.
+ *   biases   how many a row has: bias_tokens int32 and bias_values float32 [B][biases] at rows of stride_bias (0: the same for every row).
+ *   mask     32-bit words [B][(vocabulary + 31) / 32] at rows of stride_mask (0: the same for every row) or NULL; token v is bit v % 32 of word v / 32,
+ *            1: allowed.
+ * Tokens outside 0 .. vocabulary - 1 in a history or among the biases are passed over.
+ * Supported: B up to 65535, biases up to 1023, history_most below 2^21.
+ */
+typedef struct {
+  int32_t B, vocabulary, dtype; /* wersa_dtype of logits and out */
+  int32_t history_rows, history_most, biases;
+  int64_t stride_logits, stride_out, stride_history, stride_bias, stride_mask;
+} wersa_logits_desc;
+
+wersa_status wersa_logits_adjust(const wersa_logits_desc *desc, const void *logits, const int32_t *history, const int32_t *lengths,
+                                 const int32_t *prompt_lengths, const int32_t *slots, const float *repetition,
+                                 const float *presence, const float *frequency, const int32_t *bias_tokens,
+                                 const float *bias_values, const uint32_t *mask, void *out, void *hip_stream);
+
 /* 1 if this descriptor runs on the MFMA path, 0 if on the generic path, -1 if rejected. */
 int32_t wersa_selected_path(const wersa_desc *desc);
 

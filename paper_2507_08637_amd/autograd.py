@@ -11,9 +11,11 @@ block, to x and the four weight matrices (float32 gradients cast to the weights'
     out, final_state = wersa_decay_attention(q, k, v, log_decay, scale, initial_state, offsets)
     y = wersa_rms_norm(x, weight, eps=eps)
     y, r = wersa_rms_norm(x, weight, residual, eps)
+    y[, r] = wersa_layer_norm(x, weight, bias[, residual], eps)
+    out = wersa_embedding(tokens, weight, scale, dtype)
 
 q, k (B, H, n, dk), v (B, H, n, dv), each with strides of its own; gradients flow to q, k, v and initial_state (log_decay
-is fixed: one that wants a gradient is refused).  x, residual (..., cols), weight float32 (cols) or None; gradients flow to all three.
+is fixed: one that wants a gradient is refused).  x, residual (..., cols), weight and bias float32 (cols) or None; gradients flow to all of them.
 """
 import ctypes
 import warnings
@@ -45,6 +47,8 @@ def _load_node():
         node.bind_causal([ctypes.cast(f, ctypes.c_void_p).value for f in (
             lib.wersa_decay_forward, lib.wersa_decay_backward, lib.wersa_decay_workspace_bytes, lib.wersa_decay_saved_bytes,
             lib.wersa_rms_norm_forward, lib.wersa_rms_norm_backward, lib.wersa_rms_norm_workspace_bytes)])
+        node.bind_layer_norm(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
+            lib.wersa_layer_norm_forward, lib.wersa_layer_norm_backward, lib.wersa_layer_norm_workspace_bytes)))
         _node = node
     return _node
 
@@ -188,3 +192,61 @@ def wersa_rms_norm(x, weight=None, residual=None, eps=1e-6):
     if len(shape) != 2:
         outs = [t.view(shape) for t in outs]
     return outs[0] if residual is None else tuple(outs)
+
+
+class _LayerNorm(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, weight, bias, residual, eps):
+        y, r, stats = binding.wersa_layer_norm_forward(x, weight, bias, residual=residual, eps=eps, want_stats=True)
+        ctx.save_for_backward(x if residual is None else r, weight, stats)
+        ctx.set_materialize_grads(False)
+        return y if residual is None else (y, r)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dy, dr=None):
+        r, weight, stats = ctx.saved_tensors
+        dense = lambda t: None if t is None else t.contiguous()
+        if dy is None:
+            dy = torch.zeros(r.shape, dtype=r.dtype, device=r.device)
+        needs = ctx.needs_input_grad
+        dx, dw, db = binding.wersa_layer_norm_backward(r, stats, dense(dy), weight, dense(dr), want_dweight=needs[1], want_dbias=needs[2])
+        return dx, dw, db, dx if needs[3] else None, None
+
+
+def wersa_layer_norm(x, weight=None, bias=None, residual=None, eps=1e-5):
+    """Layer norm over the last dimension: y, or (y, x + residual)."""
+    shape = x.shape
+    assert residual is None or residual.shape == shape, "the residual has x's shape and dtype"
+    x, residual = _as_rows(x), None if residual is None else _as_rows(residual)
+    node = _load_node() if _node is None else _node
+    if not node or torch.jit.is_tracing():
+        outs = _LayerNorm.apply(x, weight, bias, residual, eps)
+        outs = (outs,) if residual is None else outs
+    else:
+        binding.checked_layer_norm_args(x, weight, bias, residual)
+        outs = node.layer_norm(x, weight, bias, residual, eps)
+    if len(shape) != 2:
+        outs = [t.view(shape) for t in outs]
+    return outs[0] if residual is None else tuple(outs)
+
+
+class _Embedding(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, tokens, weight, scale, dtype):
+        ctx.save_for_backward(tokens)
+        ctx.scale, ctx.vocabulary, ctx.dtype = scale, weight.shape[0], weight.dtype
+        return binding.wersa_embedding_forward(tokens, weight, scale, dtype)
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout):
+        (tokens,) = ctx.saved_tensors
+        return None, binding.wersa_embedding_backward(tokens, dout.contiguous(), ctx.vocabulary, ctx.scale, ctx.dtype), None, None
+
+
+def wersa_embedding(tokens, weight, scale=1.0, dtype=None):
+    """scale * weight[tokens] of `dtype` (the weight's by default), zeros for tokens that have no row; the gradient of the weight is dense and of its dtype."""
+    assert weight.dim() == 2, "weight is (vocabulary, cols)"
+    tokens, weight = binding.checked_tokens(tokens), _as_rows(weight)
+    return _Embedding.apply(tokens, weight, float(scale), weight.dtype if dtype is None else dtype)

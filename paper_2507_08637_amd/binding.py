@@ -6,6 +6,7 @@ library's HIP kernels).  There is no CPU fallback: if the shared library is miss
 raises.
 """
 import ctypes
+import functools
 import os
 import struct
 
@@ -25,7 +26,9 @@ EXPORTS = ["wersa_workspace_bytes", "wersa_saved_bytes", "wersa_forward", "wersa
            "wersa_block_workspace_offset",
            "wersa_block_forward", "wersa_block_backward",
            "wersa_decay_workspace_bytes", "wersa_decay_saved_bytes", "wersa_decay_forward", "wersa_decay_backward", "wersa_decay_step",
-           "wersa_rms_norm_forward", "wersa_rms_norm_eight_bit", "wersa_rms_norm_workspace_bytes", "wersa_rms_norm_backward"]
+           "wersa_rms_norm_forward", "wersa_rms_norm_eight_bit", "wersa_rms_norm_workspace_bytes", "wersa_rms_norm_backward",
+           "wersa_layer_norm_forward", "wersa_layer_norm_workspace_bytes", "wersa_layer_norm_backward",
+           "wersa_embedding_forward", "wersa_embedding_workspace_bytes", "wersa_embedding_backward", "wersa_logits_adjust"]
 
 
 class WersaDesc(ctypes.Structure):
@@ -46,6 +49,17 @@ class WersaDecayDesc(ctypes.Structure):
 class WersaNormDesc(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float),
                 ("stride_x", ctypes.c_int64), ("stride_residual", ctypes.c_int64)]
+
+
+class WersaEmbeddingDesc(ctypes.Structure):
+    _fields_ = [("tokens", ctypes.c_int64), ("vocabulary", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("weight_dtype", ctypes.c_int32), ("token_bytes", ctypes.c_int32), ("scale", ctypes.c_float), ("stride_weight", ctypes.c_int64),
+                ("stride_out", ctypes.c_int64)]
+
+
+class WersaLogitsDesc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("B", "vocabulary", "dtype", "history_rows", "history_most", "biases")] + \
+               [(name, ctypes.c_int64) for name in ("stride_logits", "stride_out", "stride_history", "stride_bias", "stride_mask")]
 
 
 class WersaError(RuntimeError):
@@ -122,6 +136,21 @@ def load_library():
     lib.wersa_rms_norm_workspace_bytes.argtypes = [ndp]
     lib.wersa_rms_norm_backward.restype = ctypes.c_int
     lib.wersa_rms_norm_backward.argtypes = [ndp] + [vp] * 8 + [ctypes.c_size_t, vp]
+    lib.wersa_layer_norm_forward.restype = ctypes.c_int
+    lib.wersa_layer_norm_forward.argtypes = [ndp] + [vp] * 8
+    lib.wersa_layer_norm_workspace_bytes.restype = ctypes.c_size_t
+    lib.wersa_layer_norm_workspace_bytes.argtypes = [ndp]
+    lib.wersa_layer_norm_backward.restype = ctypes.c_int
+    lib.wersa_layer_norm_backward.argtypes = [ndp] + [vp] * 9 + [ctypes.c_size_t, vp]
+    edp = ctypes.POINTER(WersaEmbeddingDesc)
+    lib.wersa_embedding_forward.restype = ctypes.c_int
+    lib.wersa_embedding_forward.argtypes = [edp] + [vp] * 4
+    lib.wersa_embedding_workspace_bytes.restype = ctypes.c_size_t
+    lib.wersa_embedding_workspace_bytes.argtypes = [edp]
+    lib.wersa_embedding_backward.restype = ctypes.c_int
+    lib.wersa_embedding_backward.argtypes = [edp] + [vp] * 4 + [ctypes.c_size_t, vp]
+    lib.wersa_logits_adjust.restype = ctypes.c_int
+    lib.wersa_logits_adjust.argtypes = [ctypes.POINTER(WersaLogitsDesc)] + [vp] * 13
     lib.wersa_status_string.restype = ctypes.c_char_p
     lib.wersa_status_string.argtypes = [ctypes.c_int]
     lib.wersa_version.restype = ctypes.c_int32
@@ -728,6 +757,180 @@ def wersa_rms_norm_backward(r, rstd, dy, weight=None, dr=None, dx=None, want_dwe
     _check(lib.wersa_rms_norm_backward(ctypes.byref(desc), _addr(r), _addr(weight), _addr(rstd), _addr(dy), _addr(dr), _addr(dx), _addr(dweight),
                                        _addr(workspace), 0 if workspace is None else _nbytes(workspace), _stream(stream)))
     return dx, dweight
+
+
+# ---- layer norm with the residual's addition ---------------------------------------------------------
+
+def _on_current_gpu(first, *others):
+    """As _on_one_gpu, and the GPU whose stream the call goes to."""
+    _on_one_gpu(first, *others)
+    assert first.get_device() == torch.cuda.current_device(), "expect tensors on the current GPU"
+
+
+def _on_stream(entry):
+    """stream=s is the call within torch.cuda.stream(s): what it allocates belongs to that stream."""
+    @functools.wraps(entry)
+    def call(*args, stream=None, **kw):
+        if stream is None:
+            return entry(*args, **kw)
+        with torch.cuda.stream(stream):
+            return entry(*args, **kw)
+    return call
+
+
+def checked_layer_norm_args(x, weight, bias, residual):
+    checked_norm_args(x, weight, residual)
+    assert weight is None or weight.dim() == 1, "weight: float32, one per column"
+    if bias is not None:
+        assert bias.dim() == 1 and bias.dtype == torch.float32 and bias.is_contiguous() and bias.numel() == x.shape[1], "bias: float32, one per column"
+    _on_current_gpu(x, bias)
+
+
+@_on_stream
+def wersa_layer_norm_forward(x, weight=None, bias=None, residual=None, eps=1e-5, r=None, y=None, stats=None, want_stats=False):
+    """Returns (y, r, stats): r = x + residual (x itself without one), stats (rows, 2) float32, the mean and 1 / deviation of each row, or None."""
+    checked_layer_norm_args(x, weight, bias, residual)
+    desc, stream_out = _norm_args(x, weight, residual, eps, r)
+    y = x.new_empty(x.shape) if y is None else _dense(x, y, x.shape, x.dtype, "y")
+    if stats is not None:
+        _dense(x, stats, (x.shape[0], 2), torch.float32, "stats")
+    elif want_stats:
+        stats = x.new_empty((x.shape[0], 2), dtype=torch.float32)
+    _check(load_library().wersa_layer_norm_forward(ctypes.byref(desc), x.data_ptr(), _addr(residual), _addr(weight), _addr(bias), _addr(stream_out),
+                                                   y.data_ptr(), _addr(stats), _stream(None)))
+    return y, x if residual is None else stream_out, stats
+
+
+@_on_stream
+def wersa_layer_norm_backward(r, stats, dy, weight=None, dr=None, dx=None, want_dweight=True, want_dbias=True, dweight=None, dbias=None, workspace=None):
+    """Returns (dx, dweight, dbias): dx is the gradient of x and of the residual; dr: what reaches the stream r from elsewhere."""
+    lib = load_library()
+    desc, _ = _norm_args(r, weight, None, 0.0, None)
+    for t in (dy, dr):
+        assert t is None or (t.shape == r.shape and t.dtype == r.dtype and t.is_contiguous()), "dy and dr are dense, of r's shape and dtype"
+    _dense(r, stats, (r.shape[0], 2), torch.float32, "stats")
+    dx = r.new_empty(r.shape) if dx is None else _dense(r, dx, r.shape, r.dtype, "dx")
+
+    def sums(t, wanted, name):
+        if t is not None:
+            return _dense(r, t, r.shape[1:], torch.float32, name)
+        return r.new_empty(r.shape[1], dtype=torch.float32) if wanted else None
+    dweight, dbias = sums(dweight, want_dweight, "dweight"), sums(dbias, want_dbias, "dbias")
+    _on_current_gpu(r, dy, dr, workspace)
+    if workspace is None and (dweight is not None or dbias is not None):
+        workspace = _scratch(lib.wersa_layer_norm_workspace_bytes(ctypes.byref(desc)), r, None)
+    _check(lib.wersa_layer_norm_backward(ctypes.byref(desc), _addr(r), _addr(weight), _addr(stats), _addr(dy), _addr(dr), _addr(dx), _addr(dweight),
+                                         _addr(dbias), _addr(workspace), 0 if workspace is None else _nbytes(workspace), _stream(None)))
+    return dx, dweight, dbias
+
+
+# ---- rows of an embedding for tokens -------------------------------------------------------------------
+
+_EMBEDDING_DESC = struct.Struct("q5if2q")
+
+
+def make_embedding_desc(tokens, rows, row_stride, vocabulary, cols, dtype_of, weight_dtype_of, weight_stride, scale):
+    return WersaEmbeddingDesc.from_buffer_copy(_EMBEDDING_DESC.pack(tokens.numel(), vocabulary, cols, _dtype_code(dtype_of), _dtype_code(weight_dtype_of),
+                                                                    tokens.element_size(), scale, weight_stride, row_stride))
+
+
+def checked_tokens(tokens):
+    """Contiguous int32 or int64."""
+    assert tokens.dtype == torch.int64 or tokens.dtype == torch.int32, "tokens: int32 or int64"
+    return tokens if tokens.is_contiguous() else tokens.contiguous()
+
+
+def _rows_of(x, shape, name):
+    """Row stride of x, whose rows lie one after the other at one stride and do not share memory."""
+    assert x.shape == shape, f"{name} is {tuple(shape)}"
+    if x.is_contiguous():
+        return shape[-1]
+    flat = x.view(-1, shape[-1])   # (raises where there is no such stride)
+    assert flat.stride(1) == 1 and (flat.stride(0) >= shape[-1] or flat.shape[0] <= 1), f"{name} has contiguous columns and rows that do not share memory"
+    return flat.stride(0)
+
+
+@_on_stream
+def wersa_embedding_forward(tokens, weight, scale=1.0, dtype=None, out=None):
+    """tokens of any shape, weight (vocabulary, cols): out (*tokens.shape, cols) of `dtype` (the weight's by default) = scale * weight[tokens], zeros for
+    tokens that have no row."""
+    tokens = checked_tokens(tokens)
+    assert weight.dim() == 2, "weight is (vocabulary, cols)"
+    (vocabulary, cols), shape = weight.shape, tokens.shape + weight.shape[1:]
+    if out is None:
+        out = weight.new_empty(shape, dtype=weight.dtype if dtype is None else dtype)
+    assert dtype is None or out.dtype == dtype, "out is of another dtype"
+    desc = make_embedding_desc(tokens, shape, _rows_of(out, shape, "out"), vocabulary, cols, out, weight, _rows_of(weight, weight.shape, "weight"), scale)
+    _on_current_gpu(weight, tokens, out)
+    _check(load_library().wersa_embedding_forward(ctypes.byref(desc), tokens.data_ptr(), weight.data_ptr(), out.data_ptr(), _stream(None)))
+    return out
+
+
+@_on_stream
+def wersa_embedding_backward(tokens, dout, vocabulary, scale=1.0, dtype=torch.float32, dweight=None, workspace=None):
+    """dweight (vocabulary, cols) of `dtype`: the gradient of all rows, zeros for those of tokens that are nowhere."""
+    lib = load_library()
+    tokens, cols = checked_tokens(tokens), dout.shape[-1]
+    if dweight is None:
+        dweight = dout.new_empty((vocabulary, cols), dtype=dtype)
+    desc = make_embedding_desc(tokens, dout.shape, _rows_of(dout, tokens.shape + (cols,), "dout"), vocabulary, cols, dout, dweight,
+                               _rows_of(dweight, (vocabulary, cols), "dweight"), scale)
+    _on_current_gpu(dout, tokens, dweight, workspace)
+    if workspace is None:
+        workspace = _scratch(lib.wersa_embedding_workspace_bytes(ctypes.byref(desc)), dout, None)
+    _check(lib.wersa_embedding_backward(ctypes.byref(desc), tokens.data_ptr(), dout.data_ptr(), dweight.data_ptr(), workspace.data_ptr(), _nbytes(workspace),
+                                        _stream(None)))
+    return dweight
+
+
+# ---- logits before a token is chosen ---------------------------------------------------------------------
+
+_LOGITS_DESC = struct.Struct("6i5q")
+
+
+@_on_stream
+def wersa_logits_adjust(logits, history=None, lengths=None, prompt_lengths=None, slots=None, repetition=None, presence=None, frequency=None, bias_tokens=None,
+                        bias_values=None, mask=None, out=None):
+    """Returns out (a new tensor; out=logits: in place).  logits (B, vocabulary); history (B or slots, most) int32 with lengths and, where its first tokens are a
+    prompt, prompt_lengths; slots (B) says which row of these a row of logits has.  repetition, presence, frequency (B) float32.  bias_tokens int32 and
+    bias_values float32, (B, biases) or (biases).  mask int32, (B, words) or (words): a bit for each token, 1: allowed."""
+    assert logits.dim() == 2 and logits.stride(1) == 1, "expect (B, vocabulary) with contiguous columns"
+    B, vocabulary = logits.shape
+    if out is None:
+        out = logits.new_empty(logits.shape)
+    assert out.shape == logits.shape and out.dtype == logits.dtype and out.stride(1) == 1 and (out.stride(0) >= vocabulary or B <= 1), \
+        "out has the logits' shape and dtype, contiguous columns, and rows that do not share memory"
+    for name, t in (("repetition", repetition), ("presence", presence), ("frequency", frequency)):
+        assert t is None or (t.dtype == torch.float32 and t.is_contiguous() and t.numel() == B), f"{name}: float32, one per row"
+    rows = most = history_step = biases = bias_step = mask_step = 0
+    if history is not None:
+        assert history.dim() == 2 and history.dtype == torch.int32 and history.stride(1) == 1, "history: int32 (rows, most) with contiguous columns"
+        rows, most = history.shape
+        assert slots is not None or rows == B, "history: a row for each row of logits, or slots"
+        for name, t in (("lengths", lengths), ("prompt_lengths", prompt_lengths)):
+            assert (t is None and name != "lengths") or (t is not None and t.dtype == torch.int32 and t.is_contiguous() and t.numel() == rows), \
+                f"{name}: int32, one per row of the history"
+        assert slots is None or (slots.dtype == torch.int32 and slots.is_contiguous() and slots.numel() == B), "slots: int32, one per row"
+        history_step = history.stride(0)
+    else:
+        assert all(t is None for t in (lengths, prompt_lengths, slots, repetition, presence, frequency)), "penalties go by a history"
+    if bias_tokens is not None or bias_values is not None:
+        assert bias_tokens is not None and bias_values is not None and bias_tokens.dtype == torch.int32 and bias_values.dtype == torch.float32 and \
+            bias_tokens.is_contiguous() and bias_values.is_contiguous() and bias_tokens.shape == bias_values.shape and \
+            (bias_tokens.dim() == 1 or bias_tokens.dim() == 2 and bias_tokens.shape[0] == B), "biases: int32 tokens and float32 values, (B, biases) or (biases)"
+        biases = bias_tokens.shape[-1]
+        bias_step = biases if bias_tokens.dim() == 2 else 0
+    if mask is not None:
+        words = (vocabulary + 31) // 32
+        assert mask.dtype == torch.int32 and mask.stride(-1) == 1 and (mask.shape == (words,) or mask.shape == (B, words)), \
+            "mask: int32 words of 32 tokens, (B, words) or (words)"
+        mask_step = mask.stride(0) if mask.dim() == 2 else 0
+    _on_current_gpu(logits, out, history, lengths, prompt_lengths, slots, repetition, presence, frequency, bias_tokens, bias_values, mask)
+    desc = WersaLogitsDesc.from_buffer_copy(_LOGITS_DESC.pack(B, vocabulary, _dtype_code(logits), rows, most, biases, logits.stride(0), out.stride(0), history_step,
+                                                              bias_step, mask_step))
+    _check(load_library().wersa_logits_adjust(ctypes.byref(desc), *map(_addr, (logits, history, lengths, prompt_lengths, slots, repetition, presence, frequency,
+                                                                               bias_tokens, bias_values, mask, out)), _stream(None)))
+    return out
 
 
 def wersa_profile_enable(on, only=None):

@@ -1,0 +1,436 @@
+// Rows of an embedding for tokens, and the gradient of its weights by sorted tokens:
+//   out[i] = scale weight[token_i],   dweight[v] = scale (sum of dout[i] over the places i that hold token v)
+// A token outside 0 .. vocabulary - 1 has no row: zeros, and no part in the gradient.
+//
+// The gradient.  Places are sorted by token, stably (radix sort, up to nine bits a pass), and the sorted list is cut into pieces of equal length, however unequal the tokens'
+// counts: each piece adds up its rows of dout in order, a token that lies within a piece goes straight to dweight, what a piece has of a token that goes on
+// beyond it goes to the workspace and is added up afterwards in the order of the pieces.  dout is read once, dweight written once, no float atomics.
+#include "wersa_rows.h"
+
+namespace wersa {
+namespace {
+
+constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
+constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
+constexpr int kPiece = 32;            // sorted places of a piece
+constexpr int kFixBoundaries = 16;    // boundaries of pieces that a workgroup of the last step looks at
+constexpr int kClearRows = 16;        // rows that a workgroup of the clearing step looks at
+
+struct SortPlan {
+  int64_t tile;       // places of a workgroup, a multiple of kSortThreads
+  int tiles, passes, bits;   // bits of a pass's digit
+};
+// 64 workgroups, whose counts each of them adds up by itself; a wave's share stays below 2^15 steps' reach.
+SortPlan sort_plan(int64_t tokens, int vocabulary) {
+  SortPlan p;
+  int bits = 1;
+  while ((int64_t)1 << bits < vocabulary) ++bits;
+  p.passes = (bits + kDigitBits - 1) / kDigitBits;
+  p.bits = (bits + p.passes - 1) / p.passes;
+  const int64_t each = (tokens + 63) / 64;
+  p.tile = std::min<int64_t>((each + kSortThreads - 1) / kSortThreads * kSortThreads, 1 << 19);
+  p.tile = std::max<int64_t>(p.tile, kSortThreads);
+  p.tiles = (int)((tokens + p.tile - 1) / p.tile);
+  return p;
+}
+
+struct Workspace {
+  size_t count, counts, keys[2], places[2], partial, total;   // byte offsets
+};
+Workspace workspace_of(const wersa_embedding_desc &c) {
+  const SortPlan p = sort_plan(c.tokens, c.vocabulary);
+  Workspace w;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t was = at;
+    at += (bytes + 255) / 256 * 256;
+    return was;
+  };
+  w.count = take(4);
+  w.counts = take((size_t)p.tiles * kDigits * 4);
+  for (int i = 0; i < 2; ++i) w.keys[i] = take((size_t)c.tokens * 4), w.places[i] = take((size_t)c.tokens * 4);
+  w.partial = take((size_t)((c.tokens + kPiece - 1) / kPiece) * 2 * c.cols * 4);
+  w.total = at;
+  return w;
+}
+
+// Where a pass reads: the tokens themselves, or what the pass before it left.
+struct Source {
+  const void *tokens;
+  int token_bytes, vocabulary;
+  const uint32_t *keys, *places;    // null: the tokens
+};
+__device__ __forceinline__ bool read_source(const Source &s, int64_t i, uint32_t &key, uint32_t &place) {
+  if (s.keys) {
+    key = s.keys[i];
+    place = s.places[i];
+    return true;
+  }
+  const int64_t t = s.token_bytes == 8 ? ((const int64_t *)s.tokens)[i] : (int64_t)((const int32_t *)s.tokens)[i];
+  key = (uint32_t)t;
+  place = (uint32_t)i;
+  return t >= 0 && t < s.vocabulary;
+}
+
+// counts[tile][digit]
+__global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(Source s, const uint32_t *count, int64_t tokens, int64_t tile, int shift, int digits, uint32_t *counts) {
+  __shared__ uint32_t hist[kDigits];
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) hist[d] = 0;
+  __syncthreads();
+  const int64_t n = s.keys ? (int64_t)*count : tokens, begin = blockIdx.x * tile, end = min(begin + tile, n);
+  for (int64_t i = begin + threadIdx.x; i < end; i += kSortThreads) {
+    uint32_t key, place;
+    if (read_source(s, i, key, place)) atomicAdd(&hist[(key >> shift) & (digits - 1)], 1u);
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < digits; d += kSortThreads) counts[(int64_t)blockIdx.x * digits + d] = hist[d];
+}
+
+// Places go to where their digit begins, behind those of earlier tiles, of earlier waves and of earlier lanes: a stable order.  A wave takes 64 neighbours at a
+// time; the lanes of one digit find each other by one ballot per bit.
+__global__ __launch_bounds__(kSortThreads) void embedding_scatter_kernel(Source s, uint32_t *count, int64_t tokens, int64_t tile, int shift, int bits, const uint32_t *counts,
+                                                                         uint32_t *keys, uint32_t *places) {
+  __shared__ uint32_t start[kSortWaves][kDigits];
+  __shared__ uint32_t waves_sum[kSortWaves];
+  const int digits = 1 << bits, wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+  for (int i = threadIdx.x; i < kSortWaves * kDigits; i += kSortThreads) (&start[0][0])[i] = 0;
+  const int64_t n = s.keys ? (int64_t)*count : tokens;
+  const int64_t share = tile / kSortWaves, begin = blockIdx.x * tile + wave * share, end = min(begin + share, n);
+  __syncthreads();
+  for (int64_t i = begin + lane; i < end; i += 64) {
+    uint32_t key, place;
+    if (read_source(s, i, key, place)) atomicAdd(&start[wave][(key >> shift) & (digits - 1)], 1u);
+  }
+  // of digit threadIdx.x: all places, and those of earlier tiles
+  uint32_t all = 0, before = 0;
+  if ((int)threadIdx.x < digits) {
+#pragma unroll 8
+    for (int t = 0; t < (int)gridDim.x; ++t) {
+      const uint32_t c = counts[(int64_t)t * digits + threadIdx.x];
+      all += c;
+      before += t < (int)blockIdx.x ? c : 0;
+    }
+  }
+  uint32_t upto = all;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const uint32_t v = __shfl_up(upto, d);
+    if (lane >= d) upto += v;
+  }
+  if (lane == 63) waves_sum[wave] = upto;
+  __syncthreads();
+  uint32_t lower = 0, sum = 0;
+#pragma unroll
+  for (int w = 0; w < kSortWaves; ++w) {
+    lower += w < wave ? waves_sum[w] : 0;
+    sum += waves_sum[w];
+  }
+  if (!s.keys && blockIdx.x == 0 && threadIdx.x == 0) *count = sum;   // places that hold a row's token
+  if ((int)threadIdx.x < digits) {
+    uint32_t at = lower + upto - all + before;
+#pragma unroll
+    for (int w = 0; w < kSortWaves; ++w) {
+      const uint32_t c = start[w][threadIdx.x];
+      start[w][threadIdx.x] = at;
+      at += c;
+    }
+  }
+  __syncthreads();
+  for (int64_t i0 = begin; i0 < end; i0 += 64) {   // (the same for a wave's lanes)
+    uint32_t key = 0, place = 0;
+    const bool have = i0 + lane < end && read_source(s, i0 + lane, key, place);
+    const uint32_t digit = (key >> shift) & (digits - 1);
+    uint64_t same = __ballot(have);
+    for (int b = 0; b < bits; ++b) {
+      const uint64_t set = __ballot((digit >> b) & 1);
+      same &= (digit >> b) & 1 ? set : ~set;
+    }
+    if (have) {
+      const int first = __ffsll((unsigned long long)same) - 1;
+      const uint32_t rank = __popcll(same & (((uint64_t)1 << lane) - 1));
+      uint32_t at = 0;
+      if (lane == first) at = atomicAdd(&start[wave][digit], (uint32_t)__popcll(same));
+      at = __shfl(at, first) + rank;
+      keys[at] = key;
+      places[at] = place;
+    }
+  }
+}
+
+// First place in the sorted list whose token is not below `key`.
+__device__ __forceinline__ int64_t lower_bound(const uint32_t *keys, int64_t n, uint32_t key) {
+  int64_t lo = 0, hi = n;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) / 2;
+    if (keys[mid] < key) lo = mid + 1;
+    else hi = mid;
+  }
+  return lo;
+}
+
+struct SumJob {
+  const uint32_t *count, *keys, *places;
+  const void *dout;
+  void *dweight;
+  float *partial;            // [piece][2][cols]: of a token that began before the piece, of one that goes on behind it
+  int64_t stride_out, stride_weight;
+  int cols, vocabulary;
+  float scale;
+};
+
+template <typename T, int E> __device__ __forceinline__ void store_scaled(T *row, int col, int cols, const float (&v)[E], float scale) {
+#pragma unroll
+  for (int i0 = 0; i0 < E; i0 += 16 / (int)sizeof(T) < E ? 16 / (int)sizeof(T) : E) {
+    if constexpr (16 / (int)sizeof(T) <= E) {
+      float u[16 / sizeof(T)];
+#pragma unroll
+      for (int i = 0; i < 16 / (int)sizeof(T); ++i) u[i] = v[i0 + i] * scale;
+      store_piece<T, 16 / (int)sizeof(T)>(row, col + i0, cols, u);
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i)
+        if (col + i < cols) st(row + col + i, v[i] * scale);
+    }
+  }
+}
+
+// LANES threads to a piece, 16 bytes of a row of dout to a thread; blockIdx.z: further columns.
+template <typename T, typename W, int LANES>
+__global__ __launch_bounds__(256) void embedding_sum_kernel(SumJob a) {
+  constexpr int E = 16 / sizeof(T), AHEAD = 8;
+  const int64_t n = *a.count, piece = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / LANES) + threadIdx.x / LANES, begin = piece * kPiece, end = min(begin + kPiece, n);
+  const int col = (blockIdx.z * LANES + threadIdx.x % LANES) * E;
+  if (begin >= end || col >= a.cols) return;
+  float acc[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) acc[i] = 0.f;
+  uint32_t key = a.keys[begin];
+  bool head = begin > 0 && a.keys[begin - 1] == key;
+  const bool on = end < n && a.keys[end] == a.keys[end - 1];
+  float *partial = a.partial + piece * 2 * a.cols;
+  for (int64_t i0 = begin; i0 < end; i0 += AHEAD) {
+    uint32_t k[AHEAD];
+    u32x4 row[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int64_t at = min(i0 + i, end - 1);
+      k[i] = a.keys[at];
+      row[i] = load_raw((const T *)a.dout + (int64_t)a.places[at] * a.stride_out, col, a.cols);
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      if (i0 + i < end) {
+        if (k[i] != key) {
+          if (head) store_scaled<float, E>(partial, col, a.cols, acc, 1.f);
+          else store_scaled<W, E>((W *)a.dweight + (int64_t)key * a.stride_weight, col, a.cols, acc, a.scale);
+          head = false;
+          key = k[i];
+#pragma unroll
+          for (int j = 0; j < E; ++j) acc[j] = 0.f;
+        }
+        float v[E];
+        spread<T, E>(row[i], v);
+#pragma unroll
+        for (int j = 0; j < E; ++j) acc[j] += v[j];
+      }
+    }
+  }
+  if (head) store_scaled<float, E>(partial, col, a.cols, acc, 1.f);
+  else if (on) store_scaled<float, E>(partial + a.cols, col, a.cols, acc, 1.f);
+  else store_scaled<W, E>((W *)a.dweight + (int64_t)key * a.stride_weight, col, a.cols, acc, a.scale);
+}
+
+// Tokens that go on over boundaries of pieces, each at its first such boundary: the parts in the order of the pieces, four waves a quarter each.
+template <typename W>
+__global__ __launch_bounds__(256) void embedding_join_kernel(SumJob a) {
+  __shared__ float sums[4][4][64];
+  const int64_t n = *a.count;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, col = (blockIdx.y * 64 + lane) * 4;
+  const int64_t p0 = (int64_t)blockIdx.x * kFixBoundaries + 1;
+  bool mine = false;
+  if (lane < kFixBoundaries && (p0 + lane) * kPiece < n) {
+    const int64_t at = (p0 + lane) * kPiece;
+    const uint32_t key = a.keys[at];
+    mine = a.keys[at - 1] == key && (at == kPiece || a.keys[at - kPiece - 1] != key);
+  }
+  for (uint64_t todo = __ballot(mine); todo; todo &= todo - 1) {   // (every wave has the same)
+    const int64_t p = p0 + (__ffsll((unsigned long long)todo) - 1);
+    const uint32_t key = a.keys[p * kPiece];
+    const int64_t last = (lower_bound(a.keys, n, key + 1) - 1) / kPiece, parts = last - p + 2;   // the tail of piece p - 1 and the heads of p .. last
+    const int64_t from = parts * wave / 4, to = parts * (wave + 1) / 4;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int64_t i0 = from; i0 < to; i0 += 8) {
+      u32x4 row[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int64_t at = min(i0 + i, to - 1);
+        row[i] = load_raw(a.partial + (at == 0 ? (p - 1) * 2 + 1 : (p - 1 + at) * 2) * a.cols, col, a.cols);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (i0 + i < to) {
+          float v[4];
+          spread<float, 4>(row[i], v);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[j] += v[j];
+        }
+      }
+    }
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < 4; ++j) sums[wave][j][lane] = acc[j];
+    __syncthreads();
+    if (wave == 0 && col < a.cols) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j] = (sums[0][j][lane] + sums[1][j][lane]) + (sums[2][j][lane] + sums[3][j][lane]);
+      store_scaled<W, 4>((W *)a.dweight + (int64_t)key * a.stride_weight, col, a.cols, acc, a.scale);
+    }
+  }
+}
+
+// Rows of dweight whose token is nowhere: zeros.
+template <typename W>
+__global__ __launch_bounds__(256) void embedding_clear_kernel(SumJob a) {
+  __shared__ bool there[kClearRows];
+  const int64_t n = a.count ? (int64_t)*a.count : 0;
+  const int64_t row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kClearRows;
+  if (threadIdx.x < kClearRows) {
+    const int64_t row = row0 + threadIdx.x;
+    bool found = row >= a.vocabulary;
+    if (!found && n > 0) {
+      const int64_t at = lower_bound(a.keys, n, (uint32_t)row);
+      found = at < n && a.keys[at] == (uint32_t)row;
+    }
+    there[threadIdx.x] = found;
+  }
+  __syncthreads();
+  constexpr int E = 16 / sizeof(W);
+  float zeros[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) zeros[i] = 0.f;
+  for (int r = 0; r < kClearRows; ++r)
+    if (!there[r])
+      for (int col = threadIdx.x * E; col < a.cols; col += 256 * E) store_piece<W, E>((W *)a.dweight + (row0 + r) * a.stride_weight, col, a.cols, zeros);
+}
+
+// LANES threads to a row of out.
+template <typename T, typename W, int LANES>
+__global__ __launch_bounds__(256) void embedding_kernel(Source s, const void *weight, void *out, int64_t tokens, int64_t stride_weight, int64_t stride_out, int cols, float scale) {
+  constexpr int E = 16 / sizeof(T), EW = 16 / (int)sizeof(W);
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
+  if (row >= tokens) return;
+  uint32_t key, place;
+  const bool have = read_source(s, row, key, place);
+  const W *from = (const W *)weight + (have ? (int64_t)key : 0) * stride_weight;
+  T *to = (T *)out + row * stride_out;
+  for (int col = (threadIdx.x % LANES) * E; col < cols; col += LANES * E) {
+    float v[E];
+    if constexpr (EW <= E) {
+#pragma unroll
+      for (int i0 = 0; i0 < E; i0 += EW) {
+        float u[EW];
+        load_piece<W, EW>(from, col + i0, have ? cols : 0, u);
+#pragma unroll
+        for (int i = 0; i < EW; ++i) v[i0 + i] = u[i];
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = have && col + i < cols ? ld(from + col + i) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = have ? v[i] * scale : 0.f;
+    store_piece<T, E>(to, col, cols, v);
+  }
+}
+
+wersa_status validate(const wersa_embedding_desc *c) {
+  if (!c) return WERSA_ERR_INVALID_ARG;
+  if (c->tokens < 0 || c->vocabulary < 1 || c->cols < 1) return WERSA_ERR_INVALID_ARG;
+  for (const int32_t t : {c->dtype, c->weight_dtype})
+    if (t != WERSA_F32 && t != WERSA_BF16) return WERSA_ERR_INVALID_ARG;
+  if (c->token_bytes != 4 && c->token_bytes != 8) return WERSA_ERR_INVALID_ARG;
+  if ((c->tokens > 1 && c->stride_out < c->cols) || (c->vocabulary > 1 && c->stride_weight < c->cols)) return WERSA_ERR_INVALID_ARG;
+  if (c->tokens >= (int64_t)1 << 31 || c->cols > 1 << 20) return WERSA_ERR_UNSUPPORTED;
+  return WERSA_OK;
+}
+
+// Types of out and of the weights, and the threads of a row: one for each 16 bytes, as a power of two, 8 at least and a workgroup at most.
+template <typename F> void by_types(const wersa_embedding_desc &c, F f) {
+  auto lanes = [&](auto *t, auto *w) {
+    const int pieces = (int)(((int64_t)c.cols * sizeof(*t) + 15) / 16);
+    if (pieces <= 8) f(t, w, std::integral_constant<int, 8>{});
+    else if (pieces <= 16) f(t, w, std::integral_constant<int, 16>{});
+    else if (pieces <= 32) f(t, w, std::integral_constant<int, 32>{});
+    else if (pieces <= 64) f(t, w, std::integral_constant<int, 64>{});
+    else if (pieces <= 128) f(t, w, std::integral_constant<int, 128>{});
+    else f(t, w, std::integral_constant<int, 256>{});
+  };
+  float *f32 = nullptr;
+  bf16_t *b16 = nullptr;
+  if (c.dtype == WERSA_F32) c.weight_dtype == WERSA_F32 ? lanes(f32, f32) : lanes(f32, b16);
+  else c.weight_dtype == WERSA_F32 ? lanes(b16, f32) : lanes(b16, b16);
+}
+
+}  // namespace
+}  // namespace wersa
+
+using namespace wersa;
+
+extern "C" {
+
+wersa_status wersa_embedding_forward(const wersa_embedding_desc *desc, const void *tokens, const void *weight, void *out, void *hip_stream) {
+  const wersa_status vs = validate(desc);
+  if (vs != WERSA_OK) return vs;
+  if (desc->tokens == 0) return WERSA_OK;
+  if (!tokens || !weight || !out) return WERSA_ERR_INVALID_ARG;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const Source s{tokens, desc->token_bytes, desc->vocabulary, nullptr, nullptr};
+  by_types(*desc, [&](auto *t, auto *w, auto lanes) {
+    typedef typename std::remove_pointer<decltype(t)>::type T;
+    typedef typename std::remove_pointer<decltype(w)>::type W;
+    constexpr int L = decltype(lanes)::value;
+    WERSA_STAGE("wersa_embedding", st, (embedding_kernel<T, W, L><<<grid_of((desc->tokens + 256 / L - 1) / (256 / L)), 256, 0, st>>>(
+        s, weight, out, desc->tokens, desc->stride_weight, desc->stride_out, desc->cols, desc->scale)));
+  });
+  return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
+}
+
+size_t wersa_embedding_workspace_bytes(const wersa_embedding_desc *desc) { return validate(desc) == WERSA_OK ? workspace_of(*desc).total : 0; }
+
+wersa_status wersa_embedding_backward(const wersa_embedding_desc *desc, const void *tokens, const void *dout, void *dweight, void *workspace,
+                                      size_t workspace_bytes, void *hip_stream) {
+  const wersa_status vs = validate(desc);
+  if (vs != WERSA_OK) return vs;
+  if (!dweight || (desc->tokens > 0 && (!tokens || !dout))) return WERSA_ERR_INVALID_ARG;
+  if (desc->tokens > 0 && (!workspace || workspace_bytes < wersa_embedding_workspace_bytes(desc) || misaligned(workspace, 256))) return WERSA_ERR_WORKSPACE;
+  hipStream_t st = (hipStream_t)hip_stream;
+  char *ws = (char *)workspace;
+  const SortPlan p = sort_plan(desc->tokens, desc->vocabulary);
+  const Workspace at = workspace_of(*desc);
+  uint32_t *count = desc->tokens ? (uint32_t *)(ws + at.count) : nullptr, *counts = (uint32_t *)(ws + at.counts);
+  Source s{tokens, desc->token_bytes, desc->vocabulary, nullptr, nullptr};
+  for (int pass = 0; pass < p.passes && desc->tokens > 0; ++pass) {
+    uint32_t *keys = (uint32_t *)(ws + at.keys[pass & 1]), *places = (uint32_t *)(ws + at.places[pass & 1]);
+    WERSA_STAGE("wersa_embedding_count", st, (embedding_count_kernel<<<p.tiles, kSortThreads, 0, st>>>(s, count, desc->tokens, p.tile, pass * p.bits, 1 << p.bits, counts)));
+    WERSA_STAGE("wersa_embedding_scatter", st, (embedding_scatter_kernel<<<p.tiles, kSortThreads, 0, st>>>(s, count, desc->tokens, p.tile, pass * p.bits, p.bits, counts, keys, places)));
+    s.keys = keys, s.places = places;
+  }
+  const SumJob a{count, s.keys, s.places, dout, dweight, (float *)(ws + at.partial), desc->stride_out, desc->stride_weight, desc->cols, desc->vocabulary, desc->scale};
+  by_types(*desc, [&](auto *t, auto *w, auto lanes) {
+    typedef typename std::remove_pointer<decltype(t)>::type T;
+    typedef typename std::remove_pointer<decltype(w)>::type W;
+    constexpr int L = decltype(lanes)::value, E = 16 / sizeof(T);
+    WERSA_STAGE("wersa_embedding_clear", st, (embedding_clear_kernel<W><<<grid_of(((int64_t)desc->vocabulary + kClearRows - 1) / kClearRows), 256, 0, st>>>(a)));
+    if (desc->tokens == 0) return;
+    const int64_t pieces = (desc->tokens + kPiece - 1) / kPiece;
+    dim3 grid = grid_of((pieces + 256 / L - 1) / (256 / L));
+    grid.z = (desc->cols + L * E - 1) / (L * E);
+    WERSA_STAGE("wersa_embedding_sum", st, (embedding_sum_kernel<T, W, L><<<grid, 256, 0, st>>>(a)));
+    if (pieces > 1)
+      WERSA_STAGE("wersa_embedding_join", st,
+                  (embedding_join_kernel<W><<<dim3((unsigned)((pieces - 2) / kFixBoundaries + 1), (desc->cols + 255) / 256), 256, 0, st>>>(a)));
+  });
+  return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
+}
+
+}  // extern "C"

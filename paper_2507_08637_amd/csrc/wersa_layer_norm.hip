@@ -1,0 +1,279 @@
+// Layer norm over the columns of a row, with the residual's addition before it:
+//   r = x + residual (rounded to the tensors' type),  m = mean(r),  rstd = (mean((r - m)^2) + eps)^-1/2,  y = (r - m) rstd weight + bias
+// and its derivative.  Sums in float32.  Bound by memory: a row is read once and stays in registers, so that the variance is summed from centred
+// values in a second pass over these, at no cost in bytes (mean(r^2) - m^2 would lose the digits that a row far from zero has in common).
+#include "wersa_rows.h"
+
+namespace wersa {
+namespace {
+
+struct LayerJob {
+  const void *x, *residual;
+  const float *weight, *bias;
+  void *r, *y;
+  float *stats;             // [rows][2]: mean, rstd; null: not wanted
+  int64_t rows, stride_x, stride_residual;
+  int cols;
+  float eps;
+};
+
+// E values from column `col` on, zeros where there are none.
+template <int E> __device__ __forceinline__ void load_addends(const float *bias, int col, int cols, float (&b)[E]) {
+#pragma unroll
+  for (int i0 = 0; i0 < E; i0 += 4) {
+    float u[4] = {0.f, 0.f, 0.f, 0.f};
+    if (bias) load_piece<float, 4>(bias, col + i0, cols, u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) b[i0 + i] = u[i];
+  }
+}
+
+// LANES threads to a row, PIECES pieces of 16 bytes to a thread.
+template <typename T, int LANES, int PIECES>
+__global__ __launch_bounds__(256) void layer_norm_kernel(LayerJob a) {
+  constexpr int E = 16 / sizeof(T);
+  __shared__ float part[4];
+  const int t = threadIdx.x % LANES;
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
+  const bool ok = row < a.rows;   // (every thread stays for the sums)
+  const int cols = ok ? a.cols : 0;
+  const T *x = (const T *)a.x + (ok ? row : 0) * a.stride_x;
+  float v[PIECES][E];
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) load_piece<T, E>(x, (t + LANES * p) * E, cols, v[p]);
+  if (a.residual) {
+    const T *res = (const T *)a.residual + (ok ? row : 0) * a.stride_residual;
+    T *r = (T *)a.r + (ok ? row : 0) * a.cols;
+    float u[PIECES][E];
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) load_piece<T, E>(res, (t + LANES * p) * E, cols, u[p]);
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[p][i] = rounded<T>(v[p][i] + u[p][i]);
+      store_piece<T, E>(r, (t + LANES * p) * E, cols, v[p]);
+    }
+  }
+  float sum = 0.f;
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) s += v[p][i];
+    sum += s;
+  }
+  const float mean = row_sum<LANES>(sum, part) / (float)a.cols;
+  sum = 0.f;
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    float s = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      v[p][i] = (t + LANES * p) * E + i < a.cols ? v[p][i] - mean : 0.f;
+      s += v[p][i] * v[p][i];
+    }
+    sum += s;
+  }
+  const float rstd = rsqrtf(row_sum<LANES>(sum, part) / (float)a.cols + a.eps);
+  if (a.stats && ok && t == 0) {
+    a.stats[2 * row] = mean;
+    a.stats[2 * row + 1] = rstd;
+  }
+  T *y = (T *)a.y + (ok ? row : 0) * a.cols;
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    float w[E], b[E];
+    load_weights(a.weight, (t + LANES * p) * E, a.cols, w);
+    load_addends(a.bias, (t + LANES * p) * E, a.cols, b);
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[p][i] = v[p][i] * rstd * w[i] + b[i];
+    store_piece<T, E>(y, (t + LANES * p) * E, cols, v[p]);
+  }
+}
+
+constexpr int kBackGroups = 768;
+__host__ __device__ constexpr int back_groups(int columns) { return columns >= 32 ? 512 : kBackGroups; }   // columns of a thread
+
+struct LayerBackJob {
+  const void *r, *dy, *dr;
+  const float *weight, *stats;
+  void *dx;
+  float *partial;           // [workgroup][2][cols]: sums of dy xhat and of dy over its rows; null: not wanted
+  int64_t rows, stride_r;
+  int cols;
+};
+
+// dx = rstd (g - mean(g) - xhat mean(g xhat)) + dr with g = dy weight.  A workgroup takes rows from its index on, as many at a time as it holds, with the
+// weights of its columns and their sums in registers throughout.  All that a row needs is requested before the first of it is used.
+template <typename T, int LANES, int PIECES>
+__global__ __launch_bounds__(256, back_groups(PIECES * 16 / sizeof(T)) / 256) void layer_norm_back_kernel(LayerBackJob a) {
+  constexpr int E = 16 / sizeof(T), ROWS = 256 / LANES;
+  __shared__ float part[2][4];
+  __shared__ float sums[LANES == 256 ? 1 : 256 * 4];
+  const int t = threadIdx.x % LANES;
+  float w[PIECES][E], dw[PIECES][E], db[PIECES][E];
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    load_weights(a.weight, (t + LANES * p) * E, a.cols, w[p]);
+#pragma unroll
+    for (int i = 0; i < E; ++i) dw[p][i] = db[p][i] = 0.f;
+  }
+  for (int64_t row0 = (int64_t)blockIdx.x * ROWS; row0 < a.rows; row0 += (int64_t)gridDim.x * ROWS) {
+    const int64_t row = row0 + threadIdx.x / LANES, at = row < a.rows ? row : 0;
+    const int cols = row < a.rows ? a.cols : 0;
+    const T *r = (const T *)a.r + at * a.stride_r, *dy = (const T *)a.dy + at * a.cols, *dr = (const T *)a.dr + at * a.cols;
+    u32x4 rr[PIECES], rd[PIECES], ru[PIECES];
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      rr[p] = load_raw(r, (t + LANES * p) * E, cols);
+      rd[p] = load_raw(dy, (t + LANES * p) * E, cols);
+    }
+    if (a.dr) {
+#pragma unroll
+      for (int p = 0; p < PIECES; ++p) ru[p] = load_raw(dr, (t + LANES * p) * E, cols);
+    }
+    const float mean = a.stats[2 * at], rstd = a.stats[2 * at + 1];
+    float dot = 0.f, all = 0.f;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      float v[E], g[E], s = 0.f, u = 0.f;
+      spread<T, E>(rr[p], v);
+      spread<T, E>(rd[p], g);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        v[i] = (v[i] - mean) * rstd;     // (columns past the end: dy is zero there)
+        db[p][i] += g[i];
+        dw[p][i] += g[i] * v[i];
+        u += g[i] * w[p][i];
+        s += g[i] * w[p][i] * v[i];
+      }
+      dot += s;
+      all += u;
+    }
+    const float along = row_sum<LANES>(dot, part[0]) / (float)a.cols, level = row_sum<LANES>(all, part[1]) / (float)a.cols;
+    T *dx = (T *)a.dx + at * a.cols;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p) {
+      float v[E], g[E], u[E];
+      spread<T, E>(rr[p], v);
+      spread<T, E>(rd[p], g);
+      if (a.dr) spread<T, E>(ru[p], u);
+#pragma unroll
+      for (int i = 0; i < E; ++i) {
+        g[i] = rstd * (g[i] * w[p][i] - level - (v[i] - mean) * rstd * along);
+        if (a.dr) g[i] += u[i];
+      }
+      store_piece<T, E>(dx, (t + LANES * p) * E, cols, g);
+    }
+  }
+  if (!a.partial) return;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float *out = a.partial + ((int64_t)blockIdx.x * 2 + which) * a.cols;
+#pragma unroll
+    for (int p = 0; p < PIECES; ++p)
+#pragma unroll
+      for (int i0 = 0; i0 < E; i0 += 4) {
+        if (LANES < 256) {   // the rows of the workgroup
+          __syncthreads();
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sums[i * 256 + threadIdx.x] = which ? db[p][i0 + i] : dw[p][i0 + i];
+          __syncthreads();
+        }
+        if (threadIdx.x < LANES) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float s = which ? db[p][i0 + i] : dw[p][i0 + i];
+            if (LANES < 256) {
+#pragma unroll
+              for (int u = 1; u < ROWS; ++u) s += sums[i * 256 + u * LANES + threadIdx.x];
+            }
+            const int col = (t + LANES * p) * E + i0 + i;
+            if (col < a.cols) out[col] = s;
+          }
+        }
+      }
+  }
+}
+
+// Sums over the workgroups in order: 16 columns, 64 shares of the workgroups, all requests of a share at once.  blockIdx.y: the weight's, the bias's.
+__global__ __launch_bounds__(1024) void layer_norm_reduce_kernel(const float *partial, int groups, int cols, float *dweight, float *dbias) {
+  constexpr int SHARES = 64, EACH = kBackGroups / SHARES;
+  __shared__ float part[SHARES][17];
+  float *to = blockIdx.y ? dbias : dweight;
+  if (!to) return;
+  const int c = threadIdx.x % 16, s = threadIdx.x / 16, col = blockIdx.x * 16 + c;
+  float v[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) v[i] = col < cols && s + SHARES * i < groups ? partial[((int64_t)(s + SHARES * i) * 2 + blockIdx.y) * cols + col] : 0.f;
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) sum += v[i];
+  part[s][c] = sum;
+#pragma unroll
+  for (int d = SHARES / 2; d > 0; d /= 2) {
+    __syncthreads();
+    if (s < d) part[s][c] += part[s + d][c];
+  }
+  if (s == 0 && col < cols) to[col] = part[0][c];
+}
+
+wersa_status validate(const wersa_norm_desc *c) {
+  if (!c) return WERSA_ERR_INVALID_ARG;
+  if (c->rows < 0 || c->cols < 1 || !(c->eps >= 0.f)) return WERSA_ERR_INVALID_ARG;
+  if (c->dtype != WERSA_F32 && c->dtype != WERSA_BF16) return WERSA_ERR_INVALID_ARG;
+  if (c->rows > 1 && (c->stride_x < c->cols || c->stride_residual < c->cols)) return WERSA_ERR_INVALID_ARG;
+  if (c->cols > 8192 || c->rows > ((int64_t)1 << 31)) return WERSA_ERR_UNSUPPORTED;
+  return WERSA_OK;
+}
+
+}  // namespace
+}  // namespace wersa
+
+using namespace wersa;
+
+extern "C" {
+
+wersa_status wersa_layer_norm_forward(const wersa_norm_desc *desc, const void *x, const void *residual, const float *weight, const float *bias, void *r,
+                                      void *y, float *stats, void *hip_stream) {
+  const wersa_status vs = validate(desc);
+  if (vs != WERSA_OK) return vs;
+  if (desc->rows == 0) return WERSA_OK;
+  if (!x || !y || (residual && !r)) return WERSA_ERR_INVALID_ARG;
+  const LayerJob a{x, residual, weight, bias, r, y, stats, desc->rows, desc->stride_x, desc->stride_residual, desc->cols, desc->eps};
+  hipStream_t st = (hipStream_t)hip_stream;
+  by_width(desc->cols, desc->dtype, [&](auto *type, auto lanes, auto pieces) {
+    typedef typename std::remove_pointer<decltype(type)>::type T;
+    constexpr int L = decltype(lanes)::value, P = decltype(pieces)::value;
+    WERSA_STAGE("wersa_layer_norm", st, (layer_norm_kernel<T, L, P><<<grid_of((desc->rows + 256 / L - 1) / (256 / L)), 256, 0, st>>>(a)));
+  });
+  return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
+}
+
+size_t wersa_layer_norm_workspace_bytes(const wersa_norm_desc *desc) {
+  return validate(desc) == WERSA_OK ? (size_t)kBackGroups * 2 * desc->cols * sizeof(float) : 0;
+}
+
+wersa_status wersa_layer_norm_backward(const wersa_norm_desc *desc, const void *r, const float *weight, const float *stats, const void *dy, const void *dr,
+                                       void *dx, float *dweight, float *dbias, void *workspace, size_t workspace_bytes, void *hip_stream) {
+  const wersa_status vs = validate(desc);
+  if (vs != WERSA_OK) return vs;
+  if (desc->rows > 0 && (!r || !stats || !dy || !dx)) return WERSA_ERR_INVALID_ARG;
+  const bool sums = dweight || dbias;
+  if (sums && (!workspace || workspace_bytes < wersa_layer_norm_workspace_bytes(desc) || misaligned(workspace, 256))) return WERSA_ERR_WORKSPACE;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const LayerBackJob a{r, dy, dr, weight, stats, dx, sums ? (float *)workspace : nullptr, desc->rows, desc->stride_x, desc->cols};
+  int groups = 0;
+  by_width(desc->cols, desc->dtype, [&](auto *type, auto lanes, auto pieces) {
+    typedef typename std::remove_pointer<decltype(type)>::type T;
+    constexpr int L = decltype(lanes)::value, P = decltype(pieces)::value;
+    groups = (int)std::min<int64_t>(back_groups(P * 16 / sizeof(T)), (desc->rows + 256 / L - 1) / (256 / L));
+    if (groups > 0) WERSA_STAGE("wersa_layer_norm_back", st, (layer_norm_back_kernel<T, L, P><<<groups, 256, 0, st>>>(a)));
+  });
+  if (sums)
+    WERSA_STAGE("wersa_layer_norm_reduce", st,
+                layer_norm_reduce_kernel<<<dim3((desc->cols + 15) / 16, 2), 1024, 0, st>>>((const float *)workspace, groups, desc->cols, dweight, dbias));
+  return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,131 @@
+// Logits before a token is chosen: penalties for tokens that were there before, biases, a mask of bits.  For each row and token v, in float32 and in this order:
+//   z = logits;  v among the row's history: z = z > 0 ? z / repetition : z * repetition;  z -= frequency count + presence [count > 0], count: how often v
+//   is in the history behind the prompt;  z += the biases of v;  v not allowed: z = -inf
+// Bound by memory: logits are read and written once.  What a history says of a tile of the vocabulary is counted in LDS by the workgroup that has the tile,
+// which reads the whole history for it (a tile of logits is 32 KB of float32, a history of 8000 tokens as much, and it comes from the caches): no counts
+// in memory, which would be as large as the logits, and none to be kept from token to token.
+#include "wersa_rows.h"
+
+namespace wersa {
+namespace {
+
+constexpr int kTile = 8192, kThreads = 512;
+constexpr int kMostBiases = 1023, kMostHistory = (1 << 21) - 1;
+// A token's word in LDS: how often it is behind the prompt, whether it is in the prompt, and 1 + the place of its first bias.
+constexpr uint32_t kCount = kMostHistory, kPrompt = 1u << 21;
+constexpr int kBiasShift = 22;
+
+struct LogitsJob {
+  const void *logits;
+  void *out;
+  const int32_t *history, *lengths, *prompts, *slots, *bias_tokens;
+  const float *repetition, *presence, *frequency, *bias_values;
+  const uint32_t *mask;
+  int64_t stride_logits, stride_out, stride_history, stride_bias, stride_mask;
+  int vocabulary, history_rows, history_most, biases;
+};
+
+template <typename T>
+__global__ __launch_bounds__(kThreads) void logits_kernel(LogitsJob a) {
+  constexpr int E = 16 / sizeof(T);
+  __shared__ __attribute__((aligned(16))) uint32_t words[kTile];
+  __shared__ int32_t bias_token[kMostBiases + 1];
+  __shared__ float bias_value[kMostBiases + 1];
+  const int row = blockIdx.y, v0 = blockIdx.x * kTile, here = min(kTile, a.vocabulary - v0);
+  const T *logits = (const T *)a.logits + row * a.stride_logits + v0;
+  T *out = (T *)a.out + row * a.stride_out + v0;
+  const bool changed = a.history || a.biases > 0;
+  if (changed) {
+    for (int i = threadIdx.x; i < kTile / 4; i += kThreads) reinterpret_cast<u32x4 *>(words)[i] = u32x4{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < a.biases; i += kThreads) bias_token[i] = a.bias_tokens[row * a.stride_bias + i];
+    __syncthreads();
+  }
+  if (a.history) {
+    const int64_t at = a.slots ? (int64_t)a.slots[row] : row;
+    if (at >= 0 && at < a.history_rows) {
+      const int32_t *history = a.history + at * a.stride_history;
+      const int length = min(max(a.lengths[at], 0), a.history_most), prompt = a.prompts ? a.prompts[at] : 0;
+#pragma unroll 4
+      for (int i = threadIdx.x; i < length; i += kThreads) {
+        const uint32_t v = (uint32_t)history[i] - (uint32_t)v0;
+        if (v < (uint32_t)here) {
+          if (i < prompt) atomicOr(&words[v], kPrompt);
+          else atomicAdd(&words[v], 1u);
+        }
+      }
+    }
+  }
+  if (a.biases > 0) {   // a token's biases are added up by its first one, in their order
+    __syncthreads();
+    for (int i = threadIdx.x; i < a.biases; i += kThreads) {
+      const uint32_t v = (uint32_t)bias_token[i] - (uint32_t)v0;
+      bool first = v < (uint32_t)here;
+      for (int j = 0; j < i && first; ++j) first = bias_token[j] != bias_token[i];
+      if (first) {
+        float sum = 0.f;
+        for (int j = i; j < a.biases; ++j)
+          if (bias_token[j] == bias_token[i]) sum += a.bias_values[row * a.stride_bias + j];
+        bias_value[i + 1] = sum;
+        words[v] |= (uint32_t)(i + 1) << kBiasShift;   // (nobody else writes words now)
+      }
+    }
+  }
+  if (changed) __syncthreads();
+  const float repetition = a.repetition ? a.repetition[row] : 1.f, presence = a.presence ? a.presence[row] : 0.f, frequency = a.frequency ? a.frequency[row] : 0.f;
+  for (int col = threadIdx.x * E; col < here; col += kThreads * E) {
+    float z[E];
+    load_piece<T, E>(logits, col, here, z);
+    uint32_t allowed = ~0u;
+    if (a.mask) allowed = a.mask[row * a.stride_mask + (v0 + col) / 32] >> ((v0 + col) & 31);
+    uint32_t word[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) word[i] = changed ? words[col + i] : 0;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+      if (word[i] & (kCount | kPrompt)) {
+        const float count = (float)(word[i] & kCount);
+        z[i] = z[i] > 0.f ? z[i] / repetition : z[i] * repetition;
+        z[i] -= frequency * count + (count > 0.f ? presence : 0.f);
+      }
+      if (word[i] >> kBiasShift) z[i] += bias_value[word[i] >> kBiasShift];
+      if (!(allowed >> i & 1)) z[i] = -__builtin_huge_valf();
+    }
+    store_piece<T, E>(out, col, here, z);
+  }
+}
+
+wersa_status validate(const wersa_logits_desc *c) {
+  if (!c) return WERSA_ERR_INVALID_ARG;
+  if (c->B < 0 || c->vocabulary < 1 || c->history_rows < 0 || c->history_most < 0 || c->biases < 0) return WERSA_ERR_INVALID_ARG;
+  if (c->dtype != WERSA_F32 && c->dtype != WERSA_BF16) return WERSA_ERR_INVALID_ARG;
+  if (c->B > 1 && (c->stride_logits < 0 || c->stride_out < c->vocabulary || c->stride_bias < 0 || c->stride_mask < 0)) return WERSA_ERR_INVALID_ARG;
+  if (c->history_rows > 1 && c->stride_history < 0) return WERSA_ERR_INVALID_ARG;
+  if (c->B > 65535 || c->biases > kMostBiases || c->history_most > kMostHistory) return WERSA_ERR_UNSUPPORTED;
+  return WERSA_OK;
+}
+
+}  // namespace
+}  // namespace wersa
+
+using namespace wersa;
+
+extern "C" {
+
+wersa_status wersa_logits_adjust(const wersa_logits_desc *desc, const void *logits, const int32_t *history, const int32_t *lengths, const int32_t *prompt_lengths,
+                                 const int32_t *slots, const float *repetition, const float *presence, const float *frequency, const int32_t *bias_tokens,
+                                 const float *bias_values, const uint32_t *mask, void *out, void *hip_stream) {
+  const wersa_status vs = validate(desc);
+  if (vs != WERSA_OK) return vs;
+  if (desc->B == 0) return WERSA_OK;
+  if (!logits || !out || (history && !lengths) || (desc->biases > 0 && (!bias_tokens || !bias_values))) return WERSA_ERR_INVALID_ARG;
+  const LogitsJob a{logits, out, history, lengths, prompt_lengths, slots, bias_tokens, repetition, presence, frequency, bias_values, mask,
+                    desc->stride_logits, desc->stride_out, desc->stride_history, desc->stride_bias, desc->stride_mask,
+                    desc->vocabulary, desc->history_rows, desc->history_most, desc->biases};
+  hipStream_t st = (hipStream_t)hip_stream;
+  const dim3 grid((desc->vocabulary - 1) / kTile + 1, desc->B);
+  if (desc->dtype == WERSA_F32) WERSA_STAGE("wersa_logits", st, (logits_kernel<float><<<grid, kThreads, 0, st>>>(a)));
+  else WERSA_STAGE("wersa_logits", st, (logits_kernel<bf16_t><<<grid, kThreads, 0, st>>>(a)));
+  return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
+}
+
+}  // extern "C"

@@ -264,6 +264,57 @@ struct RmsNorm : torch::autograd::Function<RmsNorm> {
   }
 };
 
+decltype(&wersa_layer_norm_forward) layer_forward_fn = nullptr;
+decltype(&wersa_layer_norm_backward) layer_backward_fn = nullptr;
+decltype(&wersa_layer_norm_workspace_bytes) layer_workspace_bytes_fn = nullptr;
+
+// Gradients go to the inputs by their places among the arguments; needs_input_grad counts the tensors that there are.
+struct LayerNorm : torch::autograd::Function<LayerNorm> {
+  static variable_list forward(AutogradContext *ctx, const Tensor &x, const std::optional<Tensor> &weights, const std::optional<Tensor> &biases,
+                               const std::optional<Tensor> &added, double eps) {
+    const Tensor weight = or_none(weights), bias = or_none(biases), residual = or_none(added);
+    const int64_t rows = x.size(0), cols = x.size(1);
+    const wersa_norm_desc d{rows, (int32_t)cols, dtype_of(x), (float)eps, x.stride(0), residual.defined() ? residual.stride(0) : cols};
+    const Tensor y = at::empty({rows, cols}, x.options()), r = residual.defined() ? at::empty({rows, cols}, x.options()) : Tensor(),
+                 stats = at::empty({rows, 2}, x.options().dtype(at::kFloat));
+    check(layer_forward_fn(&d, in(x), in(residual), (const float *)in(weight), (const float *)in(bias), out_of(r), out_of(y), floats_out(stats), stream(x)));
+    ctx->save_for_backward({r.defined() ? r : x, weight, stats});
+    ctx->saved_data["bias"] = bias.defined();
+    ctx->set_materialize_grads(false);
+    return r.defined() ? variable_list{y, r} : variable_list{y};
+  }
+
+  static variable_list backward(AutogradContext *ctx, const variable_list &grads) {
+    once();
+    const variable_list t = ctx->get_saved_variables();
+    const Tensor &r = t[0], &weight = t[1], &stats = t[2];
+    require(r.dim() == 2 && r.stride(1) == 1 && dtype_of(r) >= 0 && (r.size(0) <= 1 || r.stride(0) >= r.size(1)) && holds_floats(stats, 2 * r.size(0)) &&
+                (!weight.defined() || holds_floats(weight, r.size(1))),
+            "expect the stream, the weight and the statistics as they were saved");
+    const int64_t rows = r.size(0), cols = r.size(1);
+    const Tensor dy = grads[0].defined() ? grads[0].contiguous() : at::zeros({rows, cols}, r.options());
+    const Tensor dr = grads.size() > 1 && grads[1].defined() ? grads[1].contiguous() : Tensor();
+    for (const Tensor *x : {&dy, &dr})
+      require(!x->defined() || (x->sizes() == r.sizes() && x->dtype() == r.dtype()), "gradients of other shapes or types than the outputs");
+    for (const Tensor &x : t) require(!x.defined() || x.device() == dy.device(), "saved tensors on another device");
+    const bool has_bias = ctx->saved_data["bias"].toBool(), wants_w = weight.defined() && ctx->needs_input_grad(1),
+               wants_b = has_bias && ctx->needs_input_grad(weight.defined() ? 2 : 1);
+    const wersa_norm_desc d{rows, (int32_t)cols, dtype_of(r), 0.f, r.stride(0), cols};
+    auto sums = [&](bool wanted) { return wanted ? at::empty({cols}, r.options().dtype(at::kFloat)) : Tensor(); };
+    const Tensor dx = at::empty({rows, cols}, r.options()), dw = sums(wants_w), db = sums(wants_b),
+                 ws = wants_w || wants_b ? scratch((int64_t)layer_workspace_bytes_fn(&d), r) : Tensor();
+    check(layer_backward_fn(&d, in(r), (const float *)in(weight), floats(stats), in(dy), in(dr), out_of(dx), (float *)out_of(dw), (float *)out_of(db),
+                            out_of(ws), ws.defined() ? ws.nbytes() : 0, stream(r)));
+    return {dx, dw, db, grads.size() > 1 && ctx->needs_input_grad(1 + weight.defined() + has_bias) ? dx : Tensor(), Tensor()};
+  }
+};
+
+variable_list layer_norm(const Tensor &x, const std::optional<Tensor> &weight, const std::optional<Tensor> &bias, const std::optional<Tensor> &residual,
+                         double eps) {
+  pybind11::gil_scoped_release nogil;
+  return LayerNorm::apply(x, weight, bias, residual, eps);
+}
+
 variable_list decay_attention(const Tensor &q, const Tensor &k, const Tensor &v, const Tensor &log_decay, const std::optional<Tensor> &initial,
                               const std::optional<Tensor> &offsets, const pybind11::bytes &desc, int64_t saved_bytes) {
   const std::string d = desc;
@@ -297,6 +348,12 @@ PYBIND11_MODULE(_wersa_torch, m) {
     norm_backward_fn = reinterpret_cast<decltype(norm_backward_fn)>(at[5]);
     norm_workspace_bytes_fn = reinterpret_cast<decltype(norm_workspace_bytes_fn)>(at[6]);
   });
+  m.def("bind_layer_norm", [](uintptr_t forward, uintptr_t backward, uintptr_t workspace_bytes) {
+    layer_forward_fn = reinterpret_cast<decltype(layer_forward_fn)>(forward);
+    layer_backward_fn = reinterpret_cast<decltype(layer_backward_fn)>(backward);
+    layer_workspace_bytes_fn = reinterpret_cast<decltype(layer_workspace_bytes_fn)>(workspace_bytes);
+  });
+  m.def("layer_norm", &layer_norm);
   m.def("decay_attention", &decay_attention);
   m.def("rms_norm", &rms_norm);
 }
