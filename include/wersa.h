@@ -279,6 +279,49 @@ wersa_status wersa_decay_step(const wersa_decay_desc *desc, const void *q, const
                               void *hip_stream);
 
 /*
+ * Gated linear recurrence, channel by channel (the causal operator whose decay the data choose, for decoders):
+ *   a_t = sigmoid(gate_t),  h_t = a_t h_{t-1} + (1 - a_t) x_t,  out_t = h_t
+ * over a whole sequence (wersa_recurrence_forward), its derivative (wersa_recurrence_backward), and one token at a time on a cache of states
+ * (wersa_recurrence_step).  x, gate and out are (B, n, C), each at strides of its own (batch, row; in elements; channels contiguous); dout is laid out by
+ * stride_o.  Any element-aligned pointer is taken.  What is only read may overlap or repeat itself (strides from 0 up); in out, dx and dgate rows and batch entries
+ * do not share memory.
+ *   packed   0: B sequences of n rows each; offsets is NULL.
+ *            1: B sequences of any lengths (zero among them) one behind the other in tensors with one batch entry of n rows, as for decay attention: sequence b
+ *               is rows offsets[b] .. offsets[b + 1] - 1; rows of no sequence are left in out as they are, or zeros with clear = 1, and zeros in dx and dgate.
+ *   states   float32 [state_slots][C], contiguous: initial_state, final_state and slots as for decay attention (slots in the forward and the step).
+ *   saved    what the forward leaves for the backward (wersa_recurrence_saved_bytes, 256-byte aligned); NULL: no backward follows.
+ *   workspace  scratch (256-byte aligned) in which workgroups pass states on: of one call at a time.
+ * wersa_recurrence_backward: the gradients given those with respect to out and (dfinal_state, by sequence, may be NULL) the final states; initial_state is by
+ * sequence; dinitial_state may be NULL, and is none of the buffers that are read.
+ * Supported: n up to 2^30 (0: the final state is the initial one), B up to 65535, C up to 2^20, B n C below 2^44.
+ * Arithmetic: states, gates and every sum in float32; what is written is rounded once.  A row that is not finite reaches only what depends on it, which is then not finite.
+ * The same bits every time.
+ */
+typedef struct {
+  int32_t B, n, C;
+  int32_t dtype;           /* wersa_dtype of x, gate, out and their gradients */
+  int32_t packed, clear;
+  int64_t stride_x[2], stride_gate[2], stride_o[2];
+  int64_t stride_dx[2], stride_dgate[2];   /* read by the backward alone */
+} wersa_recurrence_desc;
+
+size_t wersa_recurrence_workspace_bytes(const wersa_recurrence_desc *desc);
+size_t wersa_recurrence_saved_bytes(const wersa_recurrence_desc *desc);
+
+wersa_status wersa_recurrence_forward(const wersa_recurrence_desc *desc, const void *x, const void *gate, const int32_t *offsets,
+                                      const float *initial_state, float *final_state, const int32_t *slots, int32_t state_slots,
+                                      void *out, void *saved, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+wersa_status wersa_recurrence_backward(const wersa_recurrence_desc *desc, const void *x, const void *gate, const int32_t *offsets,
+                                       const float *initial_state, const void *dout, const float *dfinal_state, const void *saved,
+                                       void *dx, void *dgate, float *dinitial_state, void *workspace, size_t workspace_bytes,
+                                       void *hip_stream);
+
+/* One token of each of B sequences (desc->n = 1, not packed): the states are updated in place. */
+wersa_status wersa_recurrence_step(const wersa_recurrence_desc *desc, const void *x, const void *gate, float *state,
+                                   const int32_t *slots, int32_t state_slots, void *out, void *hip_stream);
+
+/*
  * Root-mean-square norm over the columns of a row, with the residual's addition before it:
  *   r = x + residual (kept in the tensors' type; with residual NULL r is x itself and nothing is written),
  *   y = r * rstd * weight,  rstd = 1 / sqrt(mean(r^2) + eps)

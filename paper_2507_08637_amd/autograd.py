@@ -13,6 +13,7 @@ block, to x and the four weight matrices (float32 gradients cast to the weights'
     y, r = wersa_rms_norm(x, weight, residual, eps)
     y[, r] = wersa_layer_norm(x, weight, bias[, residual], eps)
     out = wersa_embedding(tokens, weight, scale, dtype)
+    out, final_state = wersa_recurrence(x, gate, initial_state, offsets)
 
 q, k (B, H, n, dk), v (B, H, n, dv), each with strides of its own; gradients flow to q, k, v and initial_state (log_decay
 is fixed: one that wants a gradient is refused).  x, residual (..., cols), weight and bias float32 (cols) or None; gradients flow to all of them.
@@ -229,6 +230,36 @@ def wersa_layer_norm(x, weight=None, bias=None, residual=None, eps=1e-5):
     if len(shape) != 2:
         outs = [t.view(shape) for t in outs]
     return outs[0] if residual is None else tuple(outs)
+
+
+class _Recurrence(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, gate, initial_state, offsets):
+        out, final_state, saved = binding.wersa_recurrence_forward(x, gate, offsets, initial_state, want_state=True, want_saved=True)
+        ctx.save_for_backward(x, gate, initial_state, offsets, saved)
+        ctx.set_materialize_grads(False)
+        return out, final_state
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, dout, dfinal):
+        x, gate, initial_state, offsets, saved = ctx.saved_tensors
+        dout = torch.zeros(x.shape[2], dtype=x.dtype, device=x.device).expand(x.shape) if dout is None else _channels_side_by_side(dout)
+        g = binding.wersa_recurrence_backward(x, gate, dout, saved, offsets, initial_state, None if dfinal is None else dfinal.contiguous(),
+                                              want_dinitial=ctx.needs_input_grad[2])
+        return g["dx"], g["dgate"], g["dinitial_state"], None
+
+
+def _channels_side_by_side(x):
+    """x with contiguous channels (its other strides may be anything, 0 too)."""
+    return x if x.stride(-1) == 1 else x.contiguous()
+
+
+def wersa_recurrence(x, gate, initial_state=None, offsets=None):
+    """Gated linear recurrence: h_t = sigmoid(gate_t) h_{t-1} + (1 - sigmoid(gate_t)) x_t for each channel of x, gate (B, n, C).  Returns (out, final states (B, C) in
+    float32).  Rows of no sequence are zeros in out and in the gradients, whatever they hold."""
+    x, gate = _channels_side_by_side(x), _channels_side_by_side(gate)
+    return _Recurrence.apply(x, gate, initial_state, offsets)
 
 
 class _Embedding(torch.autograd.Function):

@@ -28,7 +28,8 @@ EXPORTS = ["wersa_workspace_bytes", "wersa_saved_bytes", "wersa_forward", "wersa
            "wersa_decay_workspace_bytes", "wersa_decay_saved_bytes", "wersa_decay_forward", "wersa_decay_backward", "wersa_decay_step",
            "wersa_rms_norm_forward", "wersa_rms_norm_eight_bit", "wersa_rms_norm_workspace_bytes", "wersa_rms_norm_backward",
            "wersa_layer_norm_forward", "wersa_layer_norm_workspace_bytes", "wersa_layer_norm_backward",
-           "wersa_embedding_forward", "wersa_embedding_workspace_bytes", "wersa_embedding_backward", "wersa_logits_adjust"]
+           "wersa_embedding_forward", "wersa_embedding_workspace_bytes", "wersa_embedding_backward", "wersa_logits_adjust",
+           "wersa_recurrence_workspace_bytes", "wersa_recurrence_saved_bytes", "wersa_recurrence_forward", "wersa_recurrence_backward", "wersa_recurrence_step"]
 
 
 class WersaDesc(ctypes.Structure):
@@ -55,6 +56,11 @@ class WersaEmbeddingDesc(ctypes.Structure):
     _fields_ = [("tokens", ctypes.c_int64), ("vocabulary", ctypes.c_int32), ("cols", ctypes.c_int32), ("dtype", ctypes.c_int32),
                 ("weight_dtype", ctypes.c_int32), ("token_bytes", ctypes.c_int32), ("scale", ctypes.c_float), ("stride_weight", ctypes.c_int64),
                 ("stride_out", ctypes.c_int64)]
+
+
+class WersaRecurrenceDesc(ctypes.Structure):
+    _fields_ = [(name, ctypes.c_int32) for name in ("B", "n", "C", "dtype", "packed", "clear")] + \
+               [(name, ctypes.c_int64 * 2) for name in ("stride_x", "stride_gate", "stride_o", "stride_dx", "stride_dgate")]
 
 
 class WersaLogitsDesc(ctypes.Structure):
@@ -149,6 +155,17 @@ def load_library():
     lib.wersa_embedding_workspace_bytes.argtypes = [edp]
     lib.wersa_embedding_backward.restype = ctypes.c_int
     lib.wersa_embedding_backward.argtypes = [edp] + [vp] * 4 + [ctypes.c_size_t, vp]
+    rdp = ctypes.POINTER(WersaRecurrenceDesc)
+    lib.wersa_recurrence_workspace_bytes.restype = ctypes.c_size_t
+    lib.wersa_recurrence_workspace_bytes.argtypes = [rdp]
+    lib.wersa_recurrence_saved_bytes.restype = ctypes.c_size_t
+    lib.wersa_recurrence_saved_bytes.argtypes = [rdp]
+    lib.wersa_recurrence_forward.restype = ctypes.c_int
+    lib.wersa_recurrence_forward.argtypes = [rdp] + [vp] * 6 + [ctypes.c_int32] + [vp] * 3 + [ctypes.c_size_t, vp]
+    lib.wersa_recurrence_backward.restype = ctypes.c_int
+    lib.wersa_recurrence_backward.argtypes = [rdp] + [vp] * 11 + [ctypes.c_size_t, vp]
+    lib.wersa_recurrence_step.restype = ctypes.c_int
+    lib.wersa_recurrence_step.argtypes = [rdp] + [vp] * 4 + [ctypes.c_int32, vp, vp]
     lib.wersa_logits_adjust.restype = ctypes.c_int
     lib.wersa_logits_adjust.argtypes = [ctypes.POINTER(WersaLogitsDesc)] + [vp] * 13
     lib.wersa_status_string.restype = ctypes.c_char_p
@@ -822,6 +839,126 @@ def wersa_layer_norm_backward(r, stats, dy, weight=None, dr=None, dx=None, want_
     _check(lib.wersa_layer_norm_backward(ctypes.byref(desc), _addr(r), _addr(weight), _addr(stats), _addr(dy), _addr(dr), _addr(dx), _addr(dweight),
                                          _addr(dbias), _addr(workspace), 0 if workspace is None else _nbytes(workspace), _stream(None)))
     return dx, dweight, dbias
+
+
+# ---- gated linear recurrence ---------------------------------------------------------------------------
+
+_RECURRENCE_DESC = struct.Struct("6i10q")
+_WHOLE = "expect x, gate and out (B, n, C)"
+
+
+def _channel_states(desc, slots, *states):
+    """float32 (rows, C); rows = B, or any number with slots (B).  Returns the rows."""
+    rows = desc.B
+    if slots is not None:
+        assert slots.dtype == torch.int32 and slots.is_contiguous() and slots.numel() == desc.B, "slots: int32, one per sequence"
+        rows = max([s.shape[0] for s in states if s is not None], default=0)
+    for s in states:
+        if s is not None:
+            assert s.shape == (rows, desc.C) and s.is_contiguous() and s.dtype == torch.float32, "states are contiguous float32 (sequences or slots, C)"
+    return rows
+
+
+def make_recurrence_desc(x, gate, out, offsets=None, clear=False, dx=None, dgate=None):
+    """Descriptor for x, gate, out (B, n, C), channels contiguous; with offsets (B + 1) the tensors have one batch entry with the rows of all B sequences."""
+    assert x.dim() == 3, _WHOLE
+    (N, n, C), dtype = x.shape, x.dtype
+    strides = []
+    for t in (x, gate, out, dx, dgate):
+        if t is None:
+            strides += (0, 0)
+            continue
+        assert t.shape == x.shape, _WHOLE
+        assert t.dtype == dtype, "x, gate, out and their gradients must share a dtype"
+        b, row, c = t.stride()
+        assert c == 1 or C == 1, "expect contiguous channels"
+        strides += (b, row)
+    B = N
+    if offsets is not None:
+        assert N == 1 and offsets.dim() == 1 and offsets.numel() >= 2 and offsets.dtype == torch.int32 and offsets.is_contiguous(), \
+            "packed sequences: tensors of one batch entry and int32 offsets (B + 1)"
+        B = offsets.numel() - 1
+    return WersaRecurrenceDesc.from_buffer_copy(_RECURRENCE_DESC.pack(B, n, C, _dtype_code(x), offsets is not None, clear, *strides))
+
+
+def checked_recurrence_desc(x, gate, out, offsets, initial_state, clear=False):
+    """(descriptor, bytes of saved, bytes of workspace) of a forward call without slots; the arguments are checked."""
+    lib = load_library()
+    desc = make_recurrence_desc(x, gate, out, offsets, clear)
+    _channel_states(desc, None, initial_state)
+    _on_current_gpu(x, gate, out, offsets, initial_state)
+    wb = lib.wersa_recurrence_workspace_bytes(ctypes.byref(desc))
+    if wb == 0:   # the precise status
+        _check(lib.wersa_recurrence_forward(ctypes.byref(desc), *([None] * 6), 0, *([None] * 3), 0, None))
+    return desc, lib.wersa_recurrence_saved_bytes(ctypes.byref(desc)), wb
+
+
+@_on_stream
+def wersa_recurrence_forward(x, gate, offsets=None, initial_state=None, final_state=None, slots=None, out=None, want_state=False, want_saved=False, saved=None,
+                             workspace=None):
+    """Returns (out, final_state, saved).  x, gate (B, n, C); states (B or slots, C) float32.  final_state: a buffer to write (the initial states' own, if wanted), or
+    want_state=True for a new one (else None); want_saved=True leaves what wersa_recurrence_backward needs (else None).  Rows of no sequence are zeros in a new out, and
+    left as they are in the caller's."""
+    lib = load_library()
+    clear = out is None and offsets is not None
+    if out is None:
+        out = x.new_empty(x.shape)
+    desc = make_recurrence_desc(x, gate, out, offsets, clear)
+    if want_state and final_state is None:
+        assert slots is None, "with slots the states lie in a buffer of the caller's"
+        final_state = x.new_empty((desc.B, desc.C), dtype=torch.float32)
+    rows = _channel_states(desc, slots, initial_state, final_state)
+    _on_current_gpu(x, gate, offsets, initial_state, final_state, slots, out, saved, workspace)
+    if saved is not None or want_saved:
+        sb = lib.wersa_recurrence_saved_bytes(ctypes.byref(desc))
+        if saved is None:
+            saved = x.new_empty(sb // 4, dtype=torch.float32)
+        assert _nbytes(saved) >= sb, f"saved buffer holds {_nbytes(saved)} bytes, wersa_recurrence_saved_bytes asks for {sb}"
+    if workspace is None:
+        workspace = _scratch(lib.wersa_recurrence_workspace_bytes(ctypes.byref(desc)), x, None)
+    _check(lib.wersa_recurrence_forward(ctypes.byref(desc), _addr(x), _addr(gate), _addr(offsets), _addr(initial_state), _addr(final_state), _addr(slots), rows,
+                                        _addr(out), _addr(saved), _addr(workspace), _nbytes(workspace), _stream(None)))
+    return out, final_state, saved
+
+
+@_on_stream
+def wersa_recurrence_backward(x, gate, dout, saved, offsets=None, initial_state=None, dfinal_state=None, want_dinitial=False, workspace=None, grads=None):
+    """Returns dict(dx, dgate, dinitial_state); rows of no sequence are zeros.  `grads` may be a dict from an earlier call, of any strides: its tensors are then
+    overwritten."""
+    lib = load_library()
+    if grads is None:
+        grads = dict(dx=x.new_empty(x.shape), dgate=x.new_empty(x.shape), dinitial_state=None)
+        if want_dinitial:
+            B = x.shape[0] if offsets is None else offsets.numel() - 1
+            grads["dinitial_state"] = x.new_empty((B, x.shape[2]), dtype=torch.float32)
+    desc = make_recurrence_desc(x, gate, dout, offsets, False, grads["dx"], grads["dgate"])
+    _channel_states(desc, None, initial_state, dfinal_state, grads["dinitial_state"])
+    sb = lib.wersa_recurrence_saved_bytes(ctypes.byref(desc))
+    assert saved.dtype == torch.float32 and saved.is_contiguous() and _nbytes(saved) >= sb, \
+        f"saved buffer holds {_nbytes(saved)} bytes, wersa_recurrence_saved_bytes asks for {sb}"
+    _on_current_gpu(x, gate, offsets, initial_state, dout, dfinal_state, saved, workspace, *grads.values())
+    if workspace is None:
+        workspace = _scratch(lib.wersa_recurrence_workspace_bytes(ctypes.byref(desc)), x, None)
+    _check(lib.wersa_recurrence_backward(ctypes.byref(desc), _addr(x), _addr(gate), _addr(offsets), _addr(initial_state), _addr(dout), _addr(dfinal_state),
+                                         _addr(saved), _addr(grads["dx"]), _addr(grads["dgate"]), _addr(grads["dinitial_state"]), _addr(workspace),
+                                         _nbytes(workspace), _stream(None)))
+    return grads
+
+
+@_on_stream
+def wersa_recurrence_step(x, gate, state, slots=None, out=None):
+    """One token of each of B sequences: x, gate (B, C), state (B or slots, C) float32, updated in place.  Returns out (B, C)."""
+    if out is None:
+        out = x.new_empty(x.shape)
+    assert x.dim() == 2 and gate.shape == x.shape and out.shape == x.shape, "expect x, gate and out (B, C)"
+    assert gate.dtype == x.dtype and out.dtype == x.dtype, "x, gate, out and their gradients must share a dtype"
+    (B, C), (xb, x1), (gb, g1), (ob, o1) = x.shape, x.stride(), gate.stride(), out.stride()
+    assert x1 == g1 == o1 == 1 or C == 1, "expect contiguous channels"
+    desc = WersaRecurrenceDesc.from_buffer_copy(_RECURRENCE_DESC.pack(B, 1, C, _dtype_code(x), 0, 0, xb, 0, gb, 0, ob, 0, 0, 0, 0, 0))
+    rows = _channel_states(desc, slots, state)
+    _on_current_gpu(x, gate, state, slots, out)
+    _check(load_library().wersa_recurrence_step(ctypes.byref(desc), x.data_ptr(), gate.data_ptr(), state.data_ptr(), _addr(slots), rows, out.data_ptr(), _stream(None)))
+    return out
 
 
 # ---- rows of an embedding for tokens -------------------------------------------------------------------

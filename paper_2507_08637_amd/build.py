@@ -11,7 +11,7 @@ LIB = os.path.join(HERE, "libwersa.so")
 NODE = os.path.join(HERE, "_wersa_torch.so")
 SOURCES = ["wersa_api.hip", "wersa_generic.hip", "wersa_profile.hip", "wersa_fast.hip",
            "wersa_block.hip", "wersa_split.hip", "wersa_decay.hip", "wersa_norm.hip", "wersa_layer_norm.hip",
-           "wersa_embedding.hip", "wersa_logits.hip"]
+           "wersa_embedding.hip", "wersa_logits.hip", "wersa_recurrence.hip"]
 FLAGS = ["-O3", "--offload-arch=gfx950", "-std=c++17", "-fPIC",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

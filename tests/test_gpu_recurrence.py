@@ -1,0 +1,343 @@
+"""The gated linear recurrence against its definition in float64, token by token.
+
+Tolerances, element by element, from the roundings of float32 (u = 2^-24).  A gate's a and 1 - a are off by at most (|gate| + 6) u of themselves (the exponent's rounding,
+the exponential, a sum, a reciprocal, a product); a itself, where it is near 1, by 3 u.  With M the recurrence on magnitudes, M_t = a M_{t-1} + (1 - a) |x|, a state is off by
+E_t = a E_{t-1} + u (6 a M_{t-1} + (|gate| + 8) (1 - a) |x| + 2 M_t): per row one product and one sum in the state and one product in the span's A.  Backwards the same
+with N_t = |dout_t| + a_{t+1} N_{t+1} and F_t = a_{t+1} F_{t+1} + u (6 a_{t+1} N_{t+1} + 2 N_t); dx and dgate are products of these with the gate's parts.
+For small |gate| a is off by more than 3 u of itself: 6 a covers |gate| up to 1 where gates are below zero, and gates further below zero have an a below e^-|gate|, at most 0.37: (|gate| + 6) a
+is taken in the place of 6 a.  A result in bfloat16 is rounded to 8 significant bits, 2^-8 of it at most.
+"""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+ROUND = {torch.float32: 0.0, torch.bfloat16: 1.01 * 2.0 ** -8}
+
+
+def make(N, n, C, B, dtype, seed=0, layout="dense"):
+    g = torch.Generator().manual_seed(seed)
+    normal = lambda *s: torch.randn(s, generator=g)
+    memory = torch.exp2(1 + 10 * torch.rand(C, generator=g))
+    p = dict(x=normal(N, n, C), gate=torch.log(memory) * (1 - 2.0 * (torch.rand(C, generator=g) < 0.15)) + 2 * normal(N, n, C), dout=normal(N, n, C),
+             initial=normal(B, C), dfinal=normal(B, C))
+    for k in ("x", "gate", "dout"):
+        p[k] = p[k].to(dtype)
+    return p
+
+
+def definition(p, spans, initial, dfinal, backward=True):
+    """spans: [(batch entry, begin, end)] of the sequences.  Values and bounds, in float64; rows of no sequence are zeros."""
+    x, gate, dout = (p[k].double() for k in ("x", "gate", "dout"))
+    v = {k: torch.zeros_like(x) for k in ("out", "dx", "dgate")}
+    e = {k: torch.zeros_like(x) for k in v}
+    B, C = len(spans), x.shape[2]
+    for k in ("final", "dinitial"):
+        v[k], e[k] = torch.zeros(B, C, dtype=torch.float64), torch.zeros(B, C, dtype=torch.float64)
+    for s, (b, lo, hi) in enumerate(spans):
+        h = initial[s].double() if initial is not None else torch.zeros(C, dtype=torch.float64)
+        M, E = h.abs(), torch.zeros_like(h)
+        past = []
+        for t in range(lo, hi):
+            g, xt = gate[b, t], x[b, t]
+            a, rest = torch.sigmoid(g), torch.sigmoid(-g)
+            past.append((h, M, E))
+            ga = torch.where(g < 0, g.abs(), torch.zeros_like(g)) + 6
+            nh = a * h + rest * xt
+            nM = a * M + rest * xt.abs()
+            E = a * E + U * (ga * a * M + (g.abs() + 8) * rest * xt.abs() + 2 * nM)
+            h, M = nh, nM
+            v["out"][b, t], e["out"][b, t] = h, E
+        v["final"][s], e["final"][s] = h, E
+        if not backward:
+            continue
+        carry = dfinal[s].double() if dfinal is not None else torch.zeros(C, dtype=torch.float64)
+        cN, cF = carry.abs(), torch.zeros_like(carry)
+        for t in range(hi - 1, lo - 1, -1):
+            g, xt, d = gate[b, t], x[b, t], dout[b, t]
+            a, rest = torch.sigmoid(g), torch.sigmoid(-g)
+            ga = torch.where(g < 0, g.abs(), torch.zeros_like(g)) + 6
+            G, N = d + carry, d.abs() + cN
+            F = cF + 2 * U * N
+            hp, Mp, Ep = past[t - lo]
+            away = Mp + xt.abs()
+            v["dx"][b, t], e["dx"][b, t] = rest * G, rest * (F + (g.abs() + 8) * U * N)
+            v["dgate"][b, t] = G * (hp - xt) * a * rest
+            e["dgate"][b, t] = a * rest * (F * away + N * (Ep + U * away) + (2 * g.abs() + 16) * U * N * away)
+            carry, cN, cF = a * G, a * N, a * F + U * ga * a * N
+        v["dinitial"][s], e["dinitial"][s] = carry, cF
+    return v, e
+
+
+def near(got, name, v, e, dtype):
+    got = got.detach().double().cpu()
+    assert got.shape == v[name].shape, name
+    rounding = ROUND[dtype] if name in ("out", "dx", "dgate") else 0.0
+    err, bound = (got - v[name]).abs(), 1.01 * e[name] * (1 + rounding) + rounding * v[name].abs() + 1e-37
+    assert (err <= bound).all(), (name, float((err / bound).max()))
+
+
+def run(p, dtype, B, offsets=None, state=True, fused=False):
+    """Forward and backward through the autograd entry."""
+    from paper_2507_08637_amd import autograd
+    x, gate = p["x"].cuda(), p["gate"].cuda()
+    if fused:
+        C = x.shape[2]
+        x, gate = torch.cat([x, gate], 2).split(C, 2)
+    ins = [t.detach().requires_grad_(True) for t in (x, gate)] + ([p["initial"].cuda().requires_grad_(True)] if state else [])
+    out, final = autograd.wersa_recurrence(ins[0], ins[1], ins[2] if state else None, offsets)
+    grads = torch.autograd.grad((out, final), ins, (p["dout"].cuda(), p["dfinal"].cuda()))
+    return dict(zip(("out", "final", "dx", "dgate", "dinitial"), (out, final, *grads)))
+
+
+SIZES = [(1, 1, 1), (1, 2, 3), (2, 7, 2), (3, 8, 31), (2, 9, 64), (1, 127, 65), (2, 128, 66), (1, 129, 128), (2, 255, 130), (1, 257, 200), (3, 300, 33), (1, 1000, 129),
+         (1, 4096, 64), (1, 4097, 72), (2, 4300, 40), (1, 8321, 68), (1, 3000, 520)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,n,C", SIZES)
+@pytest.mark.parametrize("state", [True, False])
+def test_whole_sequences(B, n, C, dtype, state):
+    p = make(B, n, C, B, dtype, n + C)
+    got = run(p, dtype, B, state=state, fused=n % 2 == 0)
+    v, e = definition(p, [(b, 0, n) for b in range(B)], p["initial"] if state else None, p["dfinal"])
+    for name in got:
+        near(got[name], name, v, e, dtype)
+
+
+PACKED = [([5], 0, 0), ([1, 0, 3], 0, 0), ([0, 0, 128, 0], 0, 0), ([128, 128], 0, 0), ([127, 1, 129, 0, 2], 3, 2), ([60] * 7, 0, 50), ([0, 700, 1, 1, 1, 0], 130, 140), ([1] * 40, 1, 0),
+          ([5000, 3, 0, 200], 10, 0), ([9, 4200, 4300], 0, 300), ([0, 0], 4, 4)]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("lengths,before,behind", PACKED)
+@pytest.mark.parametrize("C,state", [(66, True), (24, False), (133, True)])
+def test_packed(lengths, before, behind, C, dtype, state):
+    n, B = before + sum(lengths) + behind, len(lengths)
+    p = make(1, n, C, B, dtype, n + C)
+    spans, at = [], before
+    for length in lengths:
+        spans.append((0, at, at + length))
+        at += length
+    p["x"][0, :before], p["gate"][0, at:], p["dout"][0, at:], p["dout"][0, :before] = float("nan"), float("inf"), float("nan"), float("nan")    # rows of no sequence
+    offsets = torch.tensor([before] + [s[2] for s in spans], dtype=torch.int32, device="cuda")
+    got = run(p, dtype, B, offsets, state, fused=C == 66)
+    v, e = definition(p, spans, p["initial"] if state else None, p["dfinal"])
+    for name in got:
+        near(got[name], name, v, e, dtype)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("B,C", [(1, 1), (3, 5), (2, 64), (4, 130), (1, 1025), (300, 37)])
+def test_tokens(B, C, dtype):
+    """Token by token on a cache addressed by slots: the definition's sequence; other slots stay as they are, a sequence without one gives zeros."""
+    from paper_2507_08637_amd import binding
+    n = 6
+    p = make(B, n, C, B, dtype, C)
+    slots = torch.randperm(2 * B + 1, generator=torch.Generator().manual_seed(1))[:B].int()
+    cache = torch.full((2 * B + 1, C), 7.0, device="cuda")
+    cache[slots.long().cuda()] = p["initial"].cuda()
+    other = [i for i in range(2 * B + 1) if i not in slots.tolist()]
+    outs = [binding.wersa_recurrence_step(p["x"][:, t].cuda(), p["gate"][:, t].cuda(), cache, slots=slots.cuda()) for t in range(n)]
+    v, e = definition(p, [(b, 0, n) for b in range(B)], p["initial"], None, backward=False)
+    near(torch.stack(outs, 1), "out", v, e, dtype)
+    near(cache[slots.long().cuda()], "final", v, e, dtype)
+    assert (cache[other] == 7).all()
+    if B > 1:
+        slots[0], slots[1] = -1, 2 * B + 1
+        was = cache.clone()
+        out = binding.wersa_recurrence_step(p["x"][:, 0].cuda(), p["gate"][:, 0].cuda(), cache, slots=slots.cuda())
+        assert (out[:2] == 0).all() and torch.equal(cache[other], was[other])
+
+
+def test_prompts_into_slots_and_on():
+    """Packed prompts into a cache, states in place, then again from there: one sequence in two parts is the sequence."""
+    from paper_2507_08637_amd import binding
+    C, lengths = 72, [300, 0, 5, 140, 900]
+    p = make(1, sum(lengths), C, 5, torch.float32, 3)
+    offsets = torch.tensor([0, 300, 300, 305, 445, 1345], dtype=torch.int32, device="cuda")
+    slots = torch.tensor([4, 7, 0, -1, 2], dtype=torch.int32, device="cuda")
+    cache = torch.randn(9, C, generator=torch.Generator().manual_seed(1)).cuda()
+    start = cache.clone()
+    x, gate = p["x"].cuda(), p["gate"].cuda()
+    out, final, _ = binding.wersa_recurrence_forward(x, gate, offsets, initial_state=cache, final_state=cache, slots=slots)
+    assert final is cache
+    initial = torch.stack([start[4], start[7], start[0], torch.zeros(C, device="cuda"), start[2]]).cpu()
+    v, e = definition(p, [(0, 0, 300), (0, 300, 300), (0, 300, 305), (0, 305, 445), (0, 445, 1345)], initial, None, backward=False)
+    near(out, "out", v, e, torch.float32)
+    near(cache[[4, 7, 0, 2]], "final", {"final": v["final"][[0, 1, 2, 4]]}, {"final": e["final"][[0, 1, 2, 4]]}, torch.float32)
+    assert torch.equal(cache[[1, 3, 5, 6, 7, 8]], start[[1, 3, 5, 6, 7, 8]])
+    whole, last, _ = binding.wersa_recurrence_forward(x, gate, initial_state=start[:1], want_state=True)
+    state = start[:1].clone()
+    for i, j in ((0, 1), (1, 600), (600, 600), (600, 1345)):
+        part, _, _ = binding.wersa_recurrence_forward(x[:, i:j], gate[:, i:j], initial_state=state, final_state=state)
+        assert torch.allclose(part, whole[:, i:j], rtol=0, atol=2e-5)
+    assert torch.allclose(state, last, rtol=0, atol=2e-5)
+    # the first and the last of many tiles read and write one buffer
+    long = make(1, 9000, 40, 1, torch.float32, 4)
+    x, gate, state = long["x"].cuda(), long["gate"].cuda(), long["initial"].cuda()
+    want = binding.wersa_recurrence_forward(x, gate, initial_state=state.clone(), want_state=True)
+    got = binding.wersa_recurrence_forward(x, gate, initial_state=state, final_state=state)
+    assert torch.equal(got[0], want[0]) and torch.equal(state, want[1])
+
+
+def test_rows_of_no_sequence_in_the_callers_out():
+    from paper_2507_08637_amd import binding
+    x = torch.randn(1, 400, 34, device="cuda")
+    offsets = torch.tensor([13, 200, 390], dtype=torch.int32, device="cuda")
+    out = torch.full((1, 400, 50), 7.0, device="cuda")
+    binding.wersa_recurrence_forward(x, x, offsets, out=out[:, :, 9:43])
+    assert (out[0, :13] == 7).all() and (out[0, 390:] == 7).all() and (out[:, :, :9] == 7).all() and (out[:, :, 43:] == 7).all()
+    fresh, _, _ = binding.wersa_recurrence_forward(x, x, offsets)
+    assert torch.equal(fresh[0, 13:390], out[0, 13:390, 9:43]) and (fresh[0, :13] == 0).all() and (fresh[0, 390:] == 0).all()
+
+
+def test_offsets_out_of_range_are_clamped():
+    from paper_2507_08637_amd import binding
+    x = torch.randn(1, 300, 20, device="cuda")
+    a = binding.wersa_recurrence_forward(x, x, torch.tensor([-5, 150, 1000], dtype=torch.int32, device="cuda"), want_state=True)
+    b = binding.wersa_recurrence_forward(x, x, torch.tensor([0, 150, 300], dtype=torch.int32, device="cuda"), want_state=True)
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_layouts(dtype):
+    """Transposed batches, windows, broadcast values, channels that begin anywhere: the same bits as dense copies."""
+    from paper_2507_08637_amd import autograd, binding
+    g = torch.Generator(device="cuda").manual_seed(5)
+    normal = lambda *s: torch.randn(s, generator=g, device="cuda").to(dtype)
+    wide = normal(600, 3, 333)
+    x, gate = wide[:, :, 7:108].transpose(0, 1), wide[:, :, 200:301].transpose(0, 1)
+    dout = normal(600, 3, 101).transpose(0, 1)
+    want, want_final, saved = binding.wersa_recurrence_forward(x.contiguous(), gate.contiguous(), want_state=True, want_saved=True)
+    got, final, _ = binding.wersa_recurrence_forward(x, gate, want_state=True)
+    assert torch.equal(got, want) and torch.equal(final, want_final)
+    placed = torch.full((600, 3, 150), 7.0, dtype=dtype, device="cuda")
+    binding.wersa_recurrence_forward(x, gate, out=placed[:, :, 20:121].transpose(0, 1))
+    assert torch.equal(placed[:, :, 20:121].transpose(0, 1), want) and (placed[:, :, :20] == 7).all() and (placed[:, :, 121:] == 7).all()
+    grads = binding.wersa_recurrence_backward(x.contiguous(), gate.contiguous(), dout.contiguous(), saved)
+    both = torch.full((600, 3, 210), 7.0, dtype=dtype, device="cuda")
+    place = dict(dx=both[:, :, 1:102].transpose(0, 1), dgate=both[:, :, 103:204].transpose(0, 1), dinitial_state=torch.empty(3, 101, device="cuda"))
+    binding.wersa_recurrence_backward(x, gate, dout, saved, grads=place)
+    assert torch.equal(place["dx"], grads["dx"]) and torch.equal(place["dgate"], grads["dgate"]) and (both[:, :, 102] == 7).all()
+    # one row of values for all sequences and tokens, one gate for all channels' tokens
+    row, level = normal(1, 1, 101).requires_grad_(True), normal(3, 1, 101).requires_grad_(True)
+    out, _ = autograd.wersa_recurrence(row.expand(3, 600, 101), level.expand(3, 600, 101))
+    again, _ = autograd.wersa_recurrence(a := row.detach().expand(3, 600, 101).contiguous().requires_grad_(True), b := level.detach().expand(3, 600, 101).contiguous().requires_grad_(True))
+    assert torch.equal(out, again)
+    for x, y in zip(torch.autograd.grad(out, (row, level), dout), torch.autograd.grad(again, (a, b), dout)):
+        y = y.float().sum(1, keepdim=True) if x.shape[0] == 3 else y.float().sum((0, 1), keepdim=True)
+        assert (x.float() - y).norm() <= 2 ** -7 * y.norm()
+    flipped = torch.randn(2, 20, 50, device="cuda").transpose(1, 2)     # channels apart: copied
+    out, _ = autograd.wersa_recurrence(flipped, flipped)
+    assert torch.equal(out, autograd.wersa_recurrence(flipped.contiguous(), flipped.contiguous())[0])
+
+
+def test_parts_of_the_outputs():
+    from paper_2507_08637_amd import autograd
+    p = make(2, 200, 48, 2, torch.float32, 6)
+    ins = [p[k].cuda().requires_grad_(True) for k in ("x", "gate", "initial")]
+    out, final = autograd.wersa_recurrence(*ins)
+    whole = torch.autograd.grad((out, final), ins, (torch.ones_like(out), torch.zeros_like(final)), retain_graph=True)
+    alone = torch.autograd.grad(out, ins, torch.ones((), device="cuda").expand_as(out), retain_graph=True)
+    assert all(torch.equal(a, b) for a, b in zip(whole, alone))
+    (dx,) = torch.autograd.grad(final, ins[0], torch.ones_like(final), retain_graph=True)
+    assert torch.isfinite(dx).all() and (dx[:, -1] != 0).any()
+    (dg,) = torch.autograd.grad(out, ins[1], torch.ones_like(out), retain_graph=True)
+    assert torch.equal(dg, whole[1])
+    (d,) = torch.autograd.grad(out.square().sum(), ins[0], create_graph=True)
+    with pytest.raises(RuntimeError):
+        torch.autograd.grad(d.sum(), ins[0])
+
+
+def test_gradients_against_differences():
+    p = make(1, 150, 12, 1, torch.float32, 7)
+    got = run(p, torch.float32, 1)
+    gen = torch.Generator().manual_seed(8)
+
+    def loss(q):
+        v, _ = definition(q, [(0, 0, 150)], q["initial"], None, backward=False)
+        return float((v["out"] * q["dout"].double()).sum() + (v["final"] * q["dfinal"].double()).sum())
+    for name, grad in (("x", "dx"), ("gate", "dgate"), ("initial", "dinitial")):
+        way, h = torch.randn(p[name].shape, generator=gen, dtype=torch.float64), 1e-4
+        slope = (loss(dict(p, **{name: p[name].double() + h * way})) - loss(dict(p, **{name: p[name].double() - h * way}))) / (2 * h)
+        terms = got[grad].double().cpu() * way
+        assert abs(slope - float(terms.sum())) <= 1e-4 * float(terms.abs().sum()), name
+
+
+def test_what_is_not_finite_reaches_what_depends_on_it():
+    from paper_2507_08637_amd import binding
+    n, C = 9000, 8
+    x, gate = torch.randn(2, n, C, device="cuda"), torch.randn(2, n, C, device="cuda") + 2
+    x[0, 3000, 1], x[0, 4000, 2], gate[0, 5000, 3], gate[0, 100, 4], gate[0, 200, 5] = float("nan"), float("inf"), float("nan"), float("inf"), -float("inf")
+    out, final, _ = binding.wersa_recurrence_forward(x, gate, want_state=True)
+    finite = torch.isfinite(out)
+    assert finite[1].all()
+    for channel, row in ((1, 3000), (2, 4000), (3, 5000)):
+        assert finite[0, :row, channel].all() and not finite[0, row:, channel].any() and not torch.isfinite(final[0, channel])
+    assert finite[0, :, [0, 4, 5, 6, 7]].all()
+    assert out[0, 100, 4] == out[0, 99, 4] and out[0, 200, 5] == x[0, 200, 5]     # a gate that keeps all, one that keeps nothing
+    offsets = torch.tensor([0, 2500, 3500, 3501, n], dtype=torch.int32, device="cuda")
+    out, final, _ = binding.wersa_recurrence_forward(x[:1], gate[:1], offsets, want_state=True)
+    finite = torch.isfinite(out[0])
+    assert finite[:3000, 1].all() and not finite[3000:3500, 1].any() and finite[3500:, 1].all()
+    assert torch.equal(torch.isfinite(final), torch.tensor([[True] * 8, [True, False] + [True] * 6, [True] * 8, [True, True, False, False] + [True] * 4], device="cuda"))
+
+
+def test_gates_at_their_ends():
+    """Gates of 20 to 80 keep all but e^-gate, whose digits 1 - a would not have; the gradient of the values is that share."""
+    from paper_2507_08637_amd import autograd
+    gate = torch.linspace(20, 80, 61, device="cuda").expand(1, 3, 61).contiguous().requires_grad_(True)
+    x = torch.full((1, 3, 61), 2.0 ** 40, device="cuda", requires_grad=True)
+    out, _ = autograd.wersa_recurrence(x, gate)
+    share = torch.exp(-gate.detach()[0, 0].double())
+    assert ((out[0, 0].double() / 2 ** 40 / share - 1).abs() <= 100 * U).all()
+    (dx,) = torch.autograd.grad(out[:, 0].sum(), x)
+    assert ((dx[0, 0].double() / share - 1).abs() <= 100 * U).all() and (dx[0, 1:] == 0).all()
+
+
+def test_no_rows():
+    from paper_2507_08637_amd import autograd
+    x, h = torch.empty(2, 0, 40, device="cuda", requires_grad=True), torch.randn(2, 40, device="cuda", requires_grad=True)
+    out, final = autograd.wersa_recurrence(x, x, h)
+    assert out.shape == (2, 0, 40) and torch.equal(final, h)
+    dx, dh = torch.autograd.grad(final.sum(), (x, h), allow_unused=True)
+    assert torch.equal(dh, torch.ones_like(h))
+    out, final = autograd.wersa_recurrence(x, x)
+    assert (final == 0).all()
+
+
+def test_the_same_bits_every_time_on_several_streams_at_once():
+    from paper_2507_08637_amd import binding
+    p = {k: v.cuda() for k, v in make(3, 20000, 130, 3, torch.bfloat16, 9).items()}
+    want, want_final, saved = binding.wersa_recurrence_forward(p["x"], p["gate"], initial_state=p["initial"], want_state=True, want_saved=True)
+    grads = binding.wersa_recurrence_backward(p["x"], p["gate"], p["dout"], saved, initial_state=p["initial"], dfinal_state=p["dfinal"], want_dinitial=True)
+    torch.cuda.synchronize()
+    streams, results = [torch.cuda.Stream() for _ in range(3)], []
+    for _ in range(4):
+        for s in streams:
+            out, final, kept = binding.wersa_recurrence_forward(p["x"], p["gate"], initial_state=p["initial"], want_state=True, want_saved=True, stream=s)
+            results.append((out, final, binding.wersa_recurrence_backward(p["x"], p["gate"], p["dout"], kept, initial_state=p["initial"], dfinal_state=p["dfinal"],
+                                                                          want_dinitial=True, stream=s)))
+    torch.cuda.synchronize()
+    for out, final, g in results:
+        assert torch.equal(out, want) and torch.equal(final, want_final) and all(torch.equal(g[k], grads[k]) for k in grads)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_rows_past_32_bits(packed):
+    """2^21 + 300 rows of 2052: 4.3 G elements a tensor.  With a gate of 0 and values of 1 the state is 1 - 2^-t."""
+    from paper_2507_08637_amd import binding
+    n, C = (1 << 21) + 300, 2052
+    gate = torch.zeros(1, 1, C, dtype=torch.bfloat16, device="cuda").expand(1, n, C)
+    x = torch.ones(1, n, C, dtype=torch.bfloat16, device="cuda")
+    x[0, -2, -1] = 3
+    offsets = torch.tensor([0, n - 1, n], dtype=torch.int32, device="cuda") if packed else None
+    out, final, saved = binding.wersa_recurrence_forward(x, gate, offsets, want_state=True, want_saved=True)
+    assert (out[0, 100:-2] == 1).all() and (out[0, -2, :-1] == 1).all() and out[0, -2, -1] == 2 and (out[0, :3, -1] == torch.tensor([0.5, 0.75, 0.875], device="cuda")).all()
+    assert out[0, -1, -1] == (0.5 if packed else 1.5) and final[-1, -1] == (0.5 if packed else 1.5)
+    grads = dict(dx=x, dgate=torch.empty_like(x), dinitial_state=None)
+    binding.wersa_recurrence_backward(x.clone(), gate, torch.ones(1, 1, C, dtype=torch.bfloat16, device="cuda").expand(1, n, C), saved, offsets, grads=grads)
+    assert (grads["dx"][0, :-100] == 1).all() and (grads["dx"][0, -1] == 0.5).all() and (grads["dx"][0, -2] == (0.5 if packed else 0.75)).all()
+    assert grads["dgate"][0, -2, -1] == (2 * 0.25 * (-2) * (0.5 if packed else 0.75))
