@@ -16,13 +16,13 @@ namespace {
 
 constexpr int kThreads = 512, kLanes = 32, kSpans = kThreads / kLanes;   // spans of R rows that a tile has
 constexpr int kR = 8, kRows = kSpans * kR;
-constexpr int kGroup = 32;                // tiles of a group
+constexpr int kGroup = 16;                // tiles of a group
 constexpr int kWaves = kThreads / 64;
 constexpr uint32_t kNone = 0xffffffffu;   // what the workspace holds where nothing has been left; no number has these bits (NaNs are stored with others)
 constexpr int kPolls = 1 << 23;           // of a wait, some seconds: only a workspace that is written by others meanwhile comes to this
 
-// V channels of a row: raw bits as they came.
-template <typename T, int V> struct Raw { uint32_t u[V * sizeof(T) / 4]; };
+// V channels of a row: raw bits as they came (one of 2 bytes: in the lower half).
+template <typename T, int V> struct Raw { uint32_t u[V * sizeof(T) < 4 ? 1 : V * sizeof(T) / 4]; };
 
 struct Job {
   const void *x, *gate, *dout;
@@ -35,15 +35,15 @@ struct Job {
   uint64_t *spans;                    // [chain][tile][channels of a slab]: (A, H),
   uint32_t *states;                   // [chain][group][channels of a slab]: the state behind a group
   int64_t sx[2], sg[2], so[2], sdx[2], sdg[2];
-  int B, n, C, tiles, slabs, chains, state_slots, clear;
+  int B, n, C, tiles, slabs, chains, state_slots, clear, gathered;
 };
 
 template <typename T> __device__ __forceinline__ void gate_parts(float g, float &a, float &rest) {
   // e^-|g| with one rounding of the exponent for bfloat16 (|g| 2^-24 of it), for float32 with the exponent's low part
   constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596299e-8f, kLn2 = 0.69314718f;
-  const float m = fabsf(g), t = m * kLog2e;
+  const float m = sizeof(T) == 4 ? fminf(fabsf(g), 200.f) : fabsf(g), t = m * kLog2e;
   float e = __builtin_amdgcn_exp2f(-t);
-  if (sizeof(T) == 4 && m < 200.f) e -= e * (kLn2 * (fmaf(m, kLog2e, -t) + m * kLog2eLow));
+  if (sizeof(T) == 4) e = g != g ? g : e - e * (kLn2 * (fmaf(m, kLog2e, -t) + m * kLog2eLow));
   const float s = __builtin_amdgcn_rcpf(1.f + e), small = e * s;
   a = g >= 0.f ? s : small;
   rest = g >= 0.f ? small : s;
@@ -62,30 +62,92 @@ template <typename T, int V> __device__ __forceinline__ float channel(const Raw<
   return __uint_as_float(i & 1 ? p.u[i / 2] & 0xffff0000u : p.u[i / 2] << 16);
 }
 template <typename T, int V> struct __attribute__((packed, aligned(2))) AnyRaw { Raw<T, V> raw; };
-template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_channels(const T *p, int valid) {
-  if (valid >= V) return reinterpret_cast<const AnyRaw<T, V> *>(p)->raw;
-  Raw<T, V> r;
-#pragma unroll
-  for (int i = 0; i < (int)(V * sizeof(T) / 4); ++i) r.u[i] = 0;
-#pragma unroll
-  for (int i = 0; i < V; ++i)
-    if (i < valid) r.u[i * (int)sizeof(T) / 4] |= sizeof(T) == 4 ? __float_as_uint(ld(p + i)) : (__float_as_uint(ld(p + i)) >> 16) << 16 * (i & 1);
-  return r;
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> load_channels(const T *p) {
+  if constexpr (V * sizeof(T) < 4) return Raw<T, V>{{(uint32_t)*p}};
+  else return reinterpret_cast<const AnyRaw<T, V> *>(p)->raw;
+}
+// Lanes whose channels end beyond the row read the row's last V channels, and move their own ones to the front (`bits`: by how much; 0 for whole lanes and for those with none).
+template <typename T, int V> __device__ __forceinline__ void move_down(Raw<T, V> &r, int bits) {
+  if constexpr (V * sizeof(T) == 8) {
+    const uint64_t v = ((uint64_t)r.u[1] << 32 | r.u[0]) >> bits;
+    r.u[0] = (uint32_t)v, r.u[1] = (uint32_t)(v >> 32);
+  } else {
+    r.u[0] >>= bits;
+  }
 }
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 b16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t two_bf16(float lo, float hi) { return __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{lo, hi}, b16x2)); }
-template <typename T, int V> __device__ __forceinline__ void store_channels(T *p, int valid, const float (&v)[V]) {
-  if (valid >= V) {
-    AnyRaw<T, V> r;
+template <typename T, int V> __device__ __forceinline__ Raw<T, V> rounded_channels(const float (&v)[V]) {
+  Raw<T, V> r;
+  if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < (int)(V * sizeof(T) / 4); ++i) r.raw.u[i] = sizeof(T) == 4 ? __float_as_uint(v[i]) : two_bf16(v[2 * i], v[2 * i + 1 < V ? 2 * i + 1 : 0]);
-    *reinterpret_cast<AnyRaw<T, V> *>(p) = r;
+    for (int i = 0; i < V; ++i) r.u[i] = __float_as_uint(v[i]);
+  } else if constexpr (V == 1) {
+    r.u[0] = f32_to_bf16(v[0]);
   } else {
 #pragma unroll
-    for (int i = 0; i < V; ++i)
-      if (i < valid) st(p + i, v[i]);
+    for (int i = 0; i < V / 2; ++i) r.u[i] = two_bf16(v[2 * i], v[2 * i + 1]);
   }
+  return r;
+}
+template <typename T, int V> __device__ __forceinline__ void store_whole(T *p, const Raw<T, V> &r) {
+  if constexpr (V * sizeof(T) < 4) *p = (T)r.u[0];
+  else reinterpret_cast<AnyRaw<T, V> *>(p)->raw = r;
+}
+template <typename T, int V> __device__ __forceinline__ void store_part(T *p, int valid, const Raw<T, V> &r) {
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (i < valid) st(p + i, channel(r, i));
+}
+template <typename T, int V> __device__ __forceinline__ void store_channels(T *p, int valid, const float (&v)[V]) {
+  const Raw<T, V> r = rounded_channels<T, V>(v);
+  if (valid >= V) store_whole<T, V>(p, r);
+  else store_part<T, V>(p, valid, r);
+}
+// A thread's rows of one tensor, all at once at the end: a branch for each of them would have every row's values live at every branch.
+template <typename T, int V> __device__ __forceinline__ void store_rows(T *p, int64_t stride, int valid, const Raw<T, V> (&r)[kR], int unwritten) {
+  if (valid >= V && !unwritten) {
+#pragma unroll
+    for (int i = 0; i < kR; ++i) store_whole<T, V>(p + i * stride, r[i]);
+  } else if (valid > 0) {
+#pragma unroll
+    for (int i = 0; i < kR; ++i)
+      if (!(unwritten >> i & 1)) store_part<T, V>(p + i * stride, min(valid, V), r[i]);
+  }
+}
+
+// A thread's rows of one tensor: its channels, R rows from row0 on (the last row there is in the place of rows that are not there).
+template <typename T, int V>
+__device__ __forceinline__ void load_rows(const void *base, int64_t batch, const int64_t (&stride)[2], int c, int C, int row0, int n, bool whole, Raw<T, V> (&r)[kR]) {
+  const T *p = (const T *)base + batch * stride[0] + min(c, C - V);
+  if (whole) {
+    p += row0 * stride[1];
+#pragma unroll
+    for (int i = 0; i < kR; ++i) r[i] = load_channels<T, V>(p + i * stride[1]);
+  } else {
+#pragma unroll
+    for (int i = 0; i < kR; ++i) r[i] = load_channels<T, V>(p + min(row0 + i, n - 1) * stride[1]);
+  }
+}
+template <typename T, int V> __device__ __forceinline__ void move_rows(Raw<T, V> (&r)[kR], int valid) {
+  const int bits = valid > 0 && valid < V ? (V - valid) * (int)sizeof(T) * 8 : 0;
+#pragma unroll
+  for (int i = 0; i < kR; ++i) move_down<T, V>(r[i], bits);
+}
+
+// Values that are formed from these again afterwards, and are not to be kept meanwhile (the compiler would, in registers that there are not).
+template <int V> __device__ __forceinline__ void anew(float (&v)[kR][V]) {
+#pragma unroll
+  for (int r = 0; r < kR; ++r)
+#pragma unroll
+    for (int i = 0; i < V; ++i) asm volatile("" : "+v"(v[r][i]));
+}
+template <typename T, int V> __device__ __forceinline__ void anew(Raw<T, V> (&v)[kR]) {
+#pragma unroll
+  for (int r = 0; r < kR; ++r)
+#pragma unroll
+    for (uint32_t &u : v[r].u) asm volatile("" : "+v"(u));
 }
 
 // A span's (A, H).  A below 0: the state before the span does not reach its end (a sequence begins within), whatever it is.
@@ -101,52 +163,59 @@ __device__ __forceinline__ void leave(uint64_t *to, const Span &s) {
   __hip_atomic_store(to, (uint64_t)plain_bits(s.H) << 32 | plain_bits(s.A), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 __device__ __forceinline__ void leave(uint32_t *to, float h) { __hip_atomic_store(to, plain_bits(h), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ Span await(const uint64_t *from) {
-  for (int i = 0; i < kPolls; ++i) {
-    const uint64_t v = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if ((uint32_t)v != kNone) return Span{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))};
-    __builtin_amdgcn_s_sleep(1);
-  }
-  return Span{-1.f, __uint_as_float(0x7fc00000u)};
-}
+constexpr uint64_t kIdentity = 0x3f800000u;   // A = 1, H = 0
+__device__ __forceinline__ Span span_of(uint64_t v) { return Span{__uint_as_float((uint32_t)v), __uint_as_float((uint32_t)(v >> 32))}; }
 __device__ __forceinline__ float await(const uint32_t *from) {
-  for (int i = 0; i < kPolls; ++i) {
-    const uint32_t v = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    if (v != kNone) return __uint_as_float(v);
-    __builtin_amdgcn_s_sleep(1);
+  uint32_t v = kNone;
+#pragma unroll 1
+  for (int i = 0; i < kPolls && v == kNone; ++i) {
+    v = __hip_atomic_load(from, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (v == kNone) __builtin_amdgcn_s_sleep(1);
   }
-  return __uint_as_float(0x7fc00000u);
+  return __uint_as_float(v);
 }
 
-// The state before tile `at` of a chain (channels CH: those of threads below CH), which has left its (A, H): `begin` for the first one, whose (A, H) has it
-// in it (the first tile alone reads the initial states, before it leaves anything, so that the final ones may be written over them).
+// The state before tile `at` of a chain, for the threads below CH, whose channel's (A, H) over the tile is `all`: the state behind the group before, then the (A, H)
+// of its group's tiles before it, two to a wave.  `begin`: the state before the first tile, which has it in its (A, H) (that tile alone reads the initial states, before it
+// leaves anything, so that the final ones may be written over them).  What a tile leaves to others: its (A, H) at once, the last one of a group the state.
 template <int CH>
-__device__ __forceinline__ float state_before(const Job &a, int chain, int at, float begin, Span (*joined)[CH]) {
+__device__ __forceinline__ float state_before(const Job &a, int chain, int at, float begin, const Span &all, Span (*joined)[CH]) {
+  static_assert(kGroup <= 2 * kWaves, "two to a wave");
+  constexpr int EACH = CH < 64 ? 1 : CH / 64;
+  const int group = at / kGroup, count = at - group * kGroup, per_chain = (a.tiles + kGroup - 1) / kGroup, wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+  const bool mine = threadIdx.x < CH, on = at + 1 < a.tiles, ends = count == kGroup - 1;
+  if (mine && on && !ends) leave(a.spans + ((int64_t)chain * a.tiles + at) * CH + threadIdx.x, all);
   if (at == 0) return begin;
-  const int group = at / kGroup, from = group * kGroup, count = at - from, each = (count + kWaves - 1) / kWaves;
-  const int wave = threadIdx.x / 64, lane = threadIdx.x & 63, i0 = min(wave * each, count), i1 = min(i0 + each, count);
-  const uint64_t *spans = a.spans + ((int64_t)chain * a.tiles + from) * CH;
+  if (CH >= 64 || lane < CH) {
+    const uint64_t *from = a.spans + ((int64_t)chain * a.tiles + group * kGroup + 2 * wave) * CH + lane;
+    const int have = min(max(count - 2 * wave, 0), 2);
+    uint64_t v[2][EACH];
+#pragma unroll 1
+    for (int i = 0; i < kPolls; ++i) {
+      bool ready = true;
 #pragma unroll
-  for (int c = lane; c < CH; c += 64) {
-    Span s{1.f, 0.f};
-    for (int i = i0; i < i1; ++i) s = join(s, await(spans + (int64_t)i * CH + c));
-    joined[wave][c] = s;
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) v[j][e] = j < have ? __hip_atomic_load(from + j * CH + 64 * e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : kIdentity;
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int e = 0; e < EACH; ++e) ready &= (uint32_t)v[j][e] != kNone;
+      if (ready) break;
+      __builtin_amdgcn_s_sleep(1);
+    }
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) joined[wave][lane + 64 * e] = join(span_of(v[0][e]), span_of(v[1][e]));   // (what has not come is a NaN)
   }
   float h = 0.f;
-  if (threadIdx.x < CH && group > 0) h = await(a.states + ((int64_t)chain * ((a.tiles + kGroup - 1) / kGroup) + group - 1) * CH + threadIdx.x);
+  if (mine && group > 0) h = await(a.states + ((int64_t)chain * per_chain + group - 1) * CH + threadIdx.x);
   __syncthreads();
-  if (threadIdx.x < CH) {
+  if (mine) {
 #pragma unroll
     for (int w = 0; w < kWaves; ++w) h = after(joined[w][threadIdx.x], h);
+    if (ends && on) leave(a.states + ((int64_t)chain * per_chain + group) * CH + threadIdx.x, after(all, h));
   }
   return h;
-}
-// What tile `at` leaves to those behind it: (A, H) as soon as it has them; behind the last tile of a group the state, when the one before is known.
-template <int CH> __device__ __forceinline__ void leave_span(const Job &a, int chain, int at, const Span &s) {
-  if (at % kGroup != kGroup - 1 && at + 1 < a.tiles) leave(a.spans + ((int64_t)chain * a.tiles + at) * CH + threadIdx.x, s);
-}
-template <int CH> __device__ __forceinline__ void leave_state(const Job &a, int chain, int at, float h) {
-  if (at % kGroup == kGroup - 1 && at + 1 < a.tiles) leave(a.states + ((int64_t)chain * ((a.tiles + kGroup - 1) / kGroup) + at / kGroup) * CH + threadIdx.x, h);
 }
 
 // Packed sequences: what a row is.
@@ -169,6 +238,63 @@ __device__ __forceinline__ int64_t slot_of(const Job &a, int b) {   // below 0: 
   return s >= 0 && s < a.state_slots ? s : -1;
 }
 
+// Packed sequences' initial states, by slots, or by sequence where they have been gathered.
+__device__ __forceinline__ float first_state(const Job &a, int b, int c, bool there) {
+  if (!a.initial || !there) return 0.f;
+  const int64_t slot = a.gathered ? b : slot_of(a, b);
+  return slot >= 0 ? a.initial[slot * a.C + c] : 0.f;
+}
+
+template <int V> __device__ __forceinline__ void first_states(const Job &a, int kind, int c, int valid, float (&h)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) h[i] = first_state(a, kind & 0xffff, c + i, i < valid);
+}
+template <int V> __device__ __forceinline__ void last_gradients(const Job &a, int kind, int c, int valid, float (&g)[V]) {
+#pragma unroll
+  for (int i = 0; i < V; ++i) g[i] = a.dfinal && i < valid ? a.dfinal[(int64_t)(kind & 0xffff) * a.C + c + i] : 0.f;
+}
+
+// What a thread's rows are, a bit for each: not there (of no sequence, or past the end), not to be written, and (packed) the first and the last ones of sequences.
+struct Marks { int outside, unwritten, first, last; };
+template <bool PACKED> __device__ __forceinline__ Marks marks_of(const Job &a, int tile, int row0, int span, bool whole, int *kinds) {
+  Marks m{0, 0, 0, 0};
+  if (!whole) m.outside = m.unwritten = ~0 << min(max(a.n - row0, 0), kR) & ((1 << kR) - 1);
+  if (PACKED) {
+    int kind = 0;
+    if (threadIdx.x < kRows) kinds[threadIdx.x] = kind = tile * kRows + (int)threadIdx.x < a.n ? row_kind(a, tile * kRows + threadIdx.x) : kOutside;
+    if (__syncthreads_or(kind & (kFirst | kLast | kOutside))) {
+      m.outside = 0;
+#pragma unroll
+      for (int r = 0; r < kR; ++r) {
+        const int k = kinds[span * kR + r];
+        m.outside |= (k & kOutside ? 1 : 0) << r;
+        m.first |= (k & kFirst ? 1 : 0) << r;
+        m.last |= (k & kLast ? 1 : 0) << r;
+      }
+    }
+  }
+  return m;
+}
+// Rows that are not there: a gate that keeps the state, and nothing to add.
+template <typename T, int V> __device__ __forceinline__ void pass_over(const Marks &m, Raw<T, V> (&g)[kR], Raw<T, V> (&x)[kR]) {
+#pragma unroll
+  for (int r = 0; r < kR; ++r)
+    if (m.outside >> r & 1) {
+#pragma unroll
+      for (uint32_t &u : g[r].u) u = sizeof(T) == 4 ? 0x7f800000u : 0x7f807f80u;
+#pragma unroll
+      for (uint32_t &u : x[r].u) u = 0;
+    }
+}
+template <typename T, int V> __device__ __forceinline__ void clear_outside(const Marks &m, Raw<T, V> (&v)[kR]) {
+#pragma unroll
+  for (int r = 0; r < kR; ++r)
+    if (m.outside >> r & 1) {
+#pragma unroll
+      for (uint32_t &u : v[r].u) u = 0;
+    }
+}
+
 // Which tile of which chain a workgroup has.
 __device__ __forceinline__ bool next_tile(const Job &a, int &chain, int &at) {
   __shared__ uint32_t ticket;
@@ -186,7 +312,7 @@ __device__ __forceinline__ bool next_tile(const Job &a, int &chain, int &at) {
 }
 
 template <typename T, int V, bool PACKED>
-__global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Job a) {
+__global__ __launch_bounds__(kThreads, 6) void recurrence_kernel(Job a) {
   constexpr int CH = kLanes * V;
   __shared__ Span part[kSpans][CH], joined[kWaves][CH];
   __shared__ float before[CH];
@@ -194,54 +320,39 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Job a) {
   int chain, tile;
   if (!next_tile(a, chain, tile)) return;
   const int batch = chain / a.slabs, c0 = (chain % a.slabs) * CH, lane = threadIdx.x % kLanes, span = threadIdx.x / kLanes;
-  const int c = c0 + lane * V, valid = a.C - c, row0 = tile * kRows + span * kR, rows = min(max(a.n - row0, 0), kR);
-  const T *x = (const T *)a.x + batch * a.sx[0] + c, *gate = (const T *)a.gate + batch * a.sg[0] + c;
+  const int c = c0 + lane * V, valid = a.C - c, row0 = tile * kRows + span * kR;
+  const bool whole = (tile + 1) * (int64_t)kRows <= a.n;
   Raw<T, V> rx[kR], rg[kR];
-#pragma unroll
-  for (int r = 0; r < kR; ++r) {
-    const int64_t t = min(row0 + r, a.n - 1);
-    rx[r] = load_channels<T, V>(x + t * a.sx[1], valid);
-    rg[r] = load_channels<T, V>(gate + t * a.sg[1], valid);
+  load_rows<T, V>(a.gate, batch, a.sg, c, a.C, row0, a.n, whole, rg);
+  load_rows<T, V>(a.x, batch, a.sx, c, a.C, row0, a.n, whole, rx);
+  const Marks m = marks_of<PACKED>(a, tile, row0, span, whole, kinds);
+  if (a.C % V) {
+    move_rows<T, V>(rg, valid);
+    move_rows<T, V>(rx, valid);
   }
-  if (PACKED) {
-    for (int r = threadIdx.x; r < kRows; r += kThreads) kinds[r] = tile * kRows + r < a.n ? row_kind(a, tile * kRows + r) : kOutside;
-    __syncthreads();
-  }
-  float da[kR][V], db[kR][V];
+  if (m.outside) pass_over<T, V>(m, rg, rx);
+  float both[kR][V];    // a and 1 - a of each row
   Span s[V];
+  float h[V];
 #pragma unroll
-  for (int i = 0; i < V; ++i) s[i] = Span{1.f, 0.f};
+  for (int i = 0; i < V; ++i) s[i] = Span{1.f, 0.f}, h[i] = 0.f;
 #pragma unroll
   for (int r = 0; r < kR; ++r) {
-    const int kind = PACKED ? kinds[span * kR + r] : 0;
-    const bool live = PACKED ? !(kind & kOutside) : r < rows;
+    if (PACKED && (m.first >> r & 1)) first_states<V>(a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
+      const float g = channel(rg[r], i);
       float keep, rest;
-      gate_parts<T>(channel(rg[r], i), keep, rest);
-      da[r][i] = live ? keep : 1.f;
-      db[r][i] = live ? rest * channel(rx[r], i) : 0.f;
-    }
-    if (PACKED && (kind & kFirst) && live) {   // what the state before adds, if there is one; the row itself cuts off what came before
-      const int64_t slot = a.initial ? slot_of(a, kind & 0xffff) : -1;
-      if (slot >= 0) {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-          if (i < valid) db[r][i] = fmaf(da[r][i], a.initial[slot * a.C + c + i], db[r][i]);
-      }
-#pragma unroll
-      for (int i = 0; i < V; ++i) s[i] = Span{-1.f, db[r][i]};
-    } else {
-#pragma unroll
-      for (int i = 0; i < V; ++i) {
-        s[i].H = fmaf(da[r][i], s[i].H, db[r][i]);
-        if (!PACKED) s[i].A *= da[r][i];
-        else s[i].A = s[i].A < 0.f ? s[i].A : s[i].A * da[r][i];
-      }
+      gate_parts<T>(g, keep, rest);
+      both[r][i] = packed_parts(g, keep, rest);
+      h[i] = fmaf(keep, h[i], rest * channel(rx[r], i));
+      s[i].A *= keep;
     }
   }
+  anew(both);
+  anew<T, V>(rx);
 #pragma unroll
-  for (int i = 0; i < V; ++i) part[span][lane * V + i] = s[i];
+  for (int i = 0; i < V; ++i) part[span][lane * V + i] = Span{PACKED && m.first ? -1.f : s[i].A, h[i]};
   __syncthreads();
   float begin = 0.f;
   const int mine = c0 + threadIdx.x;
@@ -258,41 +369,40 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Job a) {
       if (slot >= 0) begin = a.initial[slot * a.C + mine];
     }
     if (tile == 0) all = Span{-1.f, after(all, begin)};
-    leave_span<CH>(a, chain, tile, all);
   }
-  const float h0 = state_before<CH>(a, chain, tile, begin, joined);
+  const float h0 = state_before<CH>(a, chain, tile, begin, all, joined);
   if (threadIdx.x < CH) {
     before[threadIdx.x] = h0;
-    leave_state<CH>(a, chain, tile, after(all, h0));
     if (a.saved && mine < a.C) a.saved[((int64_t)batch * a.tiles + tile) * a.C + mine] = h0;
   }
   __syncthreads();
-  float h[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) h[i] = after(part[span][lane * V + i], before[lane * V + i]);
-  T *out = (T *)a.out + batch * a.so[0] + c;
+  Raw<T, V> put[kR];
 #pragma unroll
   for (int r = 0; r < kR; ++r) {
-    const int kind = PACKED ? kinds[span * kR + r] : 0;
+    if (PACKED && (m.first >> r & 1)) first_states<V>(a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
-    for (int i = 0; i < V; ++i) h[i] = PACKED && (kind & kFirst) ? db[r][i] : fmaf(da[r][i], h[i], db[r][i]);
-    if (r < rows) {
-      if (!PACKED || !(kind & kOutside)) store_channels<T, V>(out + (row0 + r) * a.so[1], valid, h);
-      else if (a.clear) {
-        float zeros[V];
-#pragma unroll
-        for (int i = 0; i < V; ++i) zeros[i] = 0.f;
-        store_channels<T, V>(out + (row0 + r) * a.so[1], valid, zeros);
-      }
+    for (int i = 0; i < V; ++i) {
+      float keep, rest;
+      parts_of(both[r][i], keep, rest);
+      h[i] = fmaf(keep, h[i], rest * channel(rx[r], i));
     }
-    if (PACKED && (kind & kLast) && a.final) {
-      const int64_t slot = slot_of(a, kind & 0xffff);
+    put[r] = rounded_channels<T, V>(h);
+    if (PACKED && (m.last >> r & 1) && a.final) {
+      const int64_t slot = slot_of(a, kinds[span * kR + r] & 0xffff);
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if (slot >= 0 && i < valid) a.final[slot * a.C + c + i] = h[i];
     }
   }
-  if (!PACKED && a.final && rows > 0 && row0 + rows == a.n) {   // (rows past the end leave h as it is)
+  int unwritten = m.unwritten;
+  if (PACKED && m.outside) {
+    clear_outside<T, V>(m, put);
+    if (!a.clear) unwritten |= m.outside;
+  }
+  store_rows<T, V>((T *)a.out + batch * a.so[0] + row0 * a.so[1] + c, a.so[1], valid, put, unwritten);
+  if (!PACKED && a.final && row0 < a.n && row0 + kR >= a.n) {   // (rows past the end leave h as it is)
     const int64_t slot = slot_of(a, batch);
 #pragma unroll
     for (int i = 0; i < V; ++i)
@@ -304,12 +414,12 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_kernel(Job a) {
       const int channel_of = c0 + threadIdx.x % CH;
       const int64_t slot = slot_of(a, b);
       if (offset_of(a, b) >= offset_of(a, b + 1) && slot >= 0 && channel_of < a.C)
-        a.final[slot * a.C + channel_of] = a.initial ? a.initial[slot * a.C + channel_of] : 0.f;
+        a.final[slot * a.C + channel_of] = first_state(a, b, channel_of, true);
     }
   }
 }
 
-// Tiles from the last one to the first.  States are by sequence.
+// Tiles from the last one to the first.  States are by sequence.  With D_t = a_t (h_{t-1} - x_t), the gate's gradient is dx_t D_t.
 template <typename T, int V, bool PACKED>
 __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
   constexpr int CH = kLanes * V;
@@ -320,65 +430,58 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
   if (!next_tile(a, chain, at)) return;
   const int tile = a.tiles - 1 - at;
   const int batch = chain / a.slabs, c0 = (chain % a.slabs) * CH, lane = threadIdx.x % kLanes, span = threadIdx.x / kLanes;
-  const int c = c0 + lane * V, valid = a.C - c, row0 = tile * kRows + span * kR, rows = min(max(a.n - row0, 0), kR);
-  const T *x = (const T *)a.x + batch * a.sx[0] + c, *gate = (const T *)a.gate + batch * a.sg[0] + c, *dout = (const T *)a.dout + batch * a.so[0] + c;
+  const int c = c0 + lane * V, valid = a.C - c, row0 = tile * kRows + span * kR;
+  const bool whole = (tile + 1) * (int64_t)kRows <= a.n;
   Raw<T, V> rx[kR], rg[kR], rd[kR];
+  load_rows<T, V>(a.gate, batch, a.sg, c, a.C, row0, a.n, whole, rg);
+  load_rows<T, V>(a.x, batch, a.sx, c, a.C, row0, a.n, whole, rx);
+  load_rows<T, V>(a.dout, batch, a.so, c, a.C, row0, a.n, whole, rd);
+  const Marks m = marks_of<PACKED>(a, tile, row0, span, whole, kinds);
+  if (a.C % V) {
+    move_rows<T, V>(rg, valid);
+    move_rows<T, V>(rx, valid);
+    move_rows<T, V>(rd, valid);
+  }
+  if (m.outside) {
+    pass_over<T, V>(m, rg, rx);
+    clear_outside<T, V>(m, rd);
+  }
+  float both[kR][V], h[V], carry[V], A[V];    // both: a and 1 - a of each row
+#pragma unroll
+  for (int i = 0; i < V; ++i) A[i] = 1.f, h[i] = carry[i] = 0.f;
 #pragma unroll
   for (int r = 0; r < kR; ++r) {
-    const int64_t t = min(row0 + r, a.n - 1);
-    rg[r] = load_channels<T, V>(gate + t * a.sg[1], valid);
-    rx[r] = load_channels<T, V>(x + t * a.sx[1], valid);
-    rd[r] = load_channels<T, V>(dout + t * a.so[1], valid);
-  }
-  if (PACKED) {
-    for (int r = threadIdx.x; r < kRows; r += kThreads) kinds[r] = tile * kRows + r < a.n ? row_kind(a, tile * kRows + r) : kOutside;
-    __syncthreads();
-  }
-  float both[kR][V];    // a and 1 - a of each row (rows that are not there: a = 1)
-  Span s[V], b[V];
-#pragma unroll
-  for (int i = 0; i < V; ++i) s[i] = b[i] = Span{1.f, 0.f};
-#pragma unroll
-  for (int r = 0; r < kR; ++r) {
-    const int kind = PACKED ? kinds[span * kR + r] : 0;
-    const bool live = PACKED ? !(kind & kOutside) : r < rows;
-    const bool first = PACKED && live && (kind & kFirst);
+    if (PACKED && (m.first >> r & 1)) first_states<V>(a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float g = channel(rg[r], i);
       float keep, rest;
       gate_parts<T>(g, keep, rest);
-      both[r][i] = live ? packed_parts(g, keep, rest) : 0.f;
-      float add = live ? rest * channel(rx[r], i) : 0.f;
-      if (!live) keep = 1.f;
-      if (first) {
-        if (a.initial && i < valid) add = fmaf(keep, a.initial[(int64_t)(kind & 0xffff) * a.C + c + i], add);
-        s[i] = Span{-1.f, add};
-      } else {
-        s[i].H = fmaf(keep, s[i].H, add);
-        if (!PACKED) s[i].A *= keep;
-        else s[i].A = s[i].A < 0.f ? s[i].A : s[i].A * keep;
-      }
+      both[r][i] = packed_parts(g, keep, rest);
+      h[i] = fmaf(keep, h[i], rest * channel(rx[r], i));
+      A[i] *= keep;
     }
   }
+  anew(both);
 #pragma unroll
   for (int r = kR - 1; r >= 0; --r) {
-    const int kind = PACKED ? kinds[span * kR + r] : 0;
-    const bool live = PACKED ? !(kind & kOutside) : r < rows;
+    if (PACKED && (m.last >> r & 1)) last_gradients<V>(a, kinds[span * kR + r], c, valid, carry);   // (nothing else comes from behind a sequence)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      float keep, rest, d = live ? channel(rd[r], i) : 0.f;
+      float keep, rest;
       parts_of(both[r][i], keep, rest);
-      if (PACKED && (kind & kLast) && live && a.dfinal && i < valid) d += a.dfinal[(int64_t)(kind & 0xffff) * a.C + c + i];
-      b[i].H = keep * (d + b[i].H);
-      if (PACKED && live && (kind & kFirst)) b[i].H = 0.f;
+      carry[i] = keep * (channel(rd[r], i) + carry[i]);
+      if (PACKED && (m.first >> r & 1)) carry[i] = 0.f;
     }
   }
+  anew(both);
+  anew<T, V>(rx);
+  anew<T, V>(rd);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    b[i].A = s[i].A;
-    part[span][lane * V + i] = s[i];
-    back[span][lane * V + i] = b[i];
+    if (PACKED && m.first) A[i] = -1.f;
+    part[span][lane * V + i] = Span{A[i], h[i]};
+    back[span][lane * V + i] = Span{A[i], carry[i]};
   }
   __syncthreads();
   float begin = 0.f;
@@ -393,22 +496,18 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
     }
     if (!PACKED && at == 0 && a.dfinal && mine < a.C) begin = a.dfinal[(int64_t)batch * a.C + mine];
     if (at == 0) all = Span{-1.f, after(all, begin)};
-    leave_span<CH>(a, chain, at, all);
-    float h = mine < a.C ? a.saved[((int64_t)batch * a.tiles + tile) * a.C + mine] : 0.f;
+    float before_span = mine < a.C ? a.saved[((int64_t)batch * a.tiles + tile) * a.C + mine] : 0.f;
 #pragma unroll
-    for (int q = 0; q < kSpans; ++q) {    // the state before each span
+    for (int q = 0; q < kSpans; ++q) {
       const Span p = part[q][threadIdx.x];
-      part[q][threadIdx.x].H = h;
-      h = after(p, h);
+      part[q][threadIdx.x].H = before_span;
+      before_span = after(p, before_span);
     }
   }
-  const float g0 = state_before<CH>(a, chain, at, begin, joined);
-  if (threadIdx.x < CH) {
-    before[threadIdx.x] = g0;
-    leave_state<CH>(a, chain, at, after(all, g0));
-  }
+  const float g0 = state_before<CH>(a, chain, at, begin, all, joined);
+  if (threadIdx.x < CH) before[threadIdx.x] = g0;
   __syncthreads();
-  float h[V], carry[V], earlier[kR][V];    // earlier: the state before each row
+  float D[kR][V];
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     h[i] = part[span][lane * V + i].H;
@@ -416,44 +515,48 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
   }
 #pragma unroll
   for (int r = 0; r < kR; ++r) {
-    const int kind = PACKED ? kinds[span * kR + r] : 0;
+    if (PACKED && (m.first >> r & 1)) first_states<V>(a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       float keep, rest;
       parts_of(both[r][i], keep, rest);
-      if (PACKED && (kind & kFirst)) h[i] = a.initial && i < valid ? a.initial[(int64_t)(kind & 0xffff) * a.C + c + i] : 0.f;
-      earlier[r][i] = h[i];
-      h[i] = (PACKED ? !(kind & kOutside) : r < rows) ? fmaf(keep, h[i], rest * channel(rx[r], i)) : h[i];
+      const float x = channel(rx[r], i);
+      D[r][i] = keep * (h[i] - x);
+      h[i] = fmaf(keep, h[i], rest * x);
     }
   }
-  T *dx = (T *)a.dx + batch * a.sdx[0] + c, *dgate = (T *)a.dgate + batch * a.sdg[0] + c;
+  anew(both);
+  Raw<T, V> px[kR], pg[kR];
 #pragma unroll
   for (int r = kR - 1; r >= 0; --r) {
-    const int kind = PACKED ? kinds[span * kR + r] : 0;
-    const bool live = PACKED ? !(kind & kOutside) : r < rows;
+    if (PACKED && (m.last >> r & 1)) last_gradients<V>(a, kinds[span * kR + r], c, valid, carry);
     float gx[V], gg[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      float keep, rest, d = live ? channel(rd[r], i) : 0.f;
+      float keep, rest;
       parts_of(both[r][i], keep, rest);
-      if (PACKED && (kind & kLast) && live && a.dfinal && i < valid) d += a.dfinal[(int64_t)(kind & 0xffff) * a.C + c + i];
-      const float G = d + carry[i];
-      gx[i] = live ? rest * G : 0.f;
-      carry[i] = live ? keep * G : carry[i];
-      gg[i] = live ? gx[i] * keep * (earlier[r][i] - channel(rx[r], i)) : 0.f;
+      const float G = channel(rd[r], i) + carry[i];
+      gx[i] = rest * G;
+      gg[i] = gx[i] * D[r][i];
+      carry[i] = keep * G;
     }
-    if (r < rows) {
-      store_channels<T, V>(dx + (row0 + r) * a.sdx[1], valid, gx);
-      store_channels<T, V>(dgate + (row0 + r) * a.sdg[1], valid, gg);
-    }
-    if (PACKED && live && (kind & kFirst)) {
+    px[r] = rounded_channels<T, V>(gx);
+    pg[r] = rounded_channels<T, V>(gg);
+    if (PACKED && (m.first >> r & 1)) {
+      const int64_t to = (int64_t)(kinds[span * kR + r] & 0xffff) * a.C + c;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        if (a.dinitial && i < valid) a.dinitial[(int64_t)(kind & 0xffff) * a.C + c + i] = carry[i];
+        if (a.dinitial && i < valid) a.dinitial[to + i] = carry[i];
         carry[i] = 0.f;
       }
     }
   }
+  if (PACKED && m.outside) {
+    clear_outside<T, V>(m, px);
+    clear_outside<T, V>(m, pg);
+  }
+  store_rows<T, V>((T *)a.dx + batch * a.sdx[0] + row0 * a.sdx[1] + c, a.sdx[1], valid, px, m.unwritten);
+  store_rows<T, V>((T *)a.dgate + batch * a.sdg[0] + row0 * a.sdg[1] + c, a.sdg[1], valid, pg, m.unwritten);
   if (!PACKED && a.dinitial && row0 == 0) {
 #pragma unroll
     for (int i = 0; i < V; ++i)
@@ -482,24 +585,36 @@ __global__ __launch_bounds__(256) void recurrence_states_kernel(Job a, const flo
   }
 }
 
-// One token: four channels to a thread, blockIdx.y the sequence.
-template <typename T>
+// Initial states that lie where the final ones go, by sequence: a sequence may end before another thread has read where it begins.
+__global__ __launch_bounds__(256) void recurrence_gather_kernel(Job a, float *to) {
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)a.B * a.C; i += (int64_t)gridDim.x * 256) {
+    const int64_t slot = slot_of(a, (int)(i / a.C));
+    to[i] = slot >= 0 ? a.initial[slot * a.C + i % a.C] : 0.f;
+  }
+}
+
+// One token: V channels to a thread, blockIdx.y the sequence.
+template <typename T, int V>
 __global__ __launch_bounds__(256) void recurrence_step_kernel(Job a) {
-  constexpr int V = 4;
-  const int c = (blockIdx.x * 256 + threadIdx.x) * V, valid = a.C - c;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * V, valid = a.C - c, from = min(c, a.C - V);
   if (valid <= 0) return;
-  const int64_t slot = slot_of(a, blockIdx.y);
-  const Raw<T, V> rx = load_channels<T, V>((const T *)a.x + blockIdx.y * a.sx[0] + c, valid), rg = load_channels<T, V>((const T *)a.gate + blockIdx.y * a.sg[0] + c, valid);
-  float h[V];
-  Raw<float, V> state;
-  if (slot >= 0) state = load_channels<float, V>(a.final + slot * a.C + c, valid);
+  const int64_t slot = slot_of(a, blockIdx.y), bits = valid < V ? (V - valid) : 0;
+  Raw<T, V> rx = load_channels<T, V>((const T *)a.x + blockIdx.y * a.sx[0] + from), rg = load_channels<T, V>((const T *)a.gate + blockIdx.y * a.sg[0] + from);
+  move_down<T, V>(rx, (int)bits * (int)sizeof(T) * 8);
+  move_down<T, V>(rg, (int)bits * (int)sizeof(T) * 8);
+  float h[V], state[V];
+  float *states = a.final + (slot >= 0 ? slot : 0) * a.C + c;
+#pragma unroll
+  for (int i = 0; i < V; ++i) state[i] = slot >= 0 && i < valid ? states[i] : 0.f;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
     float keep, rest;
     gate_parts<float>(channel(rg, i), keep, rest);
-    h[i] = slot >= 0 ? fmaf(keep, channel(state, i), rest * channel(rx, i)) : 0.f;
+    h[i] = slot >= 0 ? fmaf(keep, state[i], rest * channel(rx, i)) : 0.f;
   }
-  if (slot >= 0) store_channels<float, V>(a.final + slot * a.C + c, valid, h);
+#pragma unroll
+  for (int i = 0; i < V; ++i)
+    if (slot >= 0 && i < valid) states[i] = h[i];
   store_channels<T, V>((T *)a.out + blockIdx.y * a.so[0] + c, valid, h);
 }
 
@@ -521,7 +636,7 @@ wersa_status validate(const wersa_recurrence_desc *c) {
     for (int i = 0; i < 2; ++i)
       if (s[i] < 0 || s[i] > most) return WERSA_ERR_INVALID_ARG;
   if (c->B > 65535 || c->n > 1 << 30 || c->C > 1 << 20) return WERSA_ERR_UNSUPPORTED;
-  const int64_t tiles = (c->n + kRows - 1) / kRows, chains = (int64_t)(c->packed ? 1 : c->B) * ((c->C + kLanes * 2 - 1) / (kLanes * 2));
+  const int64_t tiles = (c->n + kRows - 1) / kRows, chains = (int64_t)(c->packed ? 1 : c->B) * ((c->C + kLanes - 1) / kLanes);
   if (tiles * chains >= (int64_t)1 << 31) return WERSA_ERR_UNSUPPORTED;
   return WERSA_OK;
 }
@@ -531,11 +646,11 @@ bool written_apart(const wersa_recurrence_desc &c, std::initializer_list<const i
   return true;
 }
 
-// Channels of a lane: 8 bytes of a row, 4 where that is the whole row.
-int lane_channels(const wersa_recurrence_desc &c) { return c.dtype == WERSA_BF16 && c.C > kLanes * 2 ? 4 : 2; }
+// Channels of a lane: 8 bytes of a row, 4 where those of 32 lanes are the whole row; never more than a row has.
+int lane_channels(const wersa_recurrence_desc &c) { return c.C == 1 ? 1 : c.dtype == WERSA_BF16 && c.C > kLanes * 2 ? 4 : 2; }
 
 struct Layout {
-  size_t spans, states, total;   // byte offsets in the workspace; the counter comes first
+  size_t spans, states, initial, total;   // byte offsets in the workspace; the counter comes first
   int tiles, slabs, chains;
 };
 Layout layout_of(const wersa_recurrence_desc &c) {
@@ -545,9 +660,10 @@ Layout layout_of(const wersa_recurrence_desc &c) {
   l.slabs = (c.C + ch - 1) / ch;
   l.chains = l.slabs * (c.packed ? 1 : c.B);
   l.spans = 256;
+  const int groups = (l.tiles + kGroup - 1) / kGroup;
   l.states = l.spans + (size_t)l.chains * l.tiles * ch * 8;
-  l.total = l.states + ((size_t)l.chains * ((l.tiles + kGroup - 1) / kGroup) * ch * 4 + 255) / 256 * 256;
-  if (l.tiles <= 1) l.total = 256;
+  l.initial = l.tiles <= 1 ? 256 : l.states + ((size_t)l.chains * groups * ch * 4 + 255) / 256 * 256;
+  l.total = l.initial + (c.packed ? ((size_t)c.B * c.C * 4 + 255) / 256 * 256 : 0);
   return l;
 }
 
@@ -556,9 +672,10 @@ template <typename F> void by_type(const wersa_recurrence_desc &c, F f) {
     if (c.packed) f(type, v, std::true_type{});
     else f(type, v, std::false_type{});
   };
-  if (c.dtype == WERSA_F32) packed((float *)nullptr, std::integral_constant<int, 2>{});
-  else if (lane_channels(c) == 4) packed((bf16_t *)nullptr, std::integral_constant<int, 4>{});
-  else packed((bf16_t *)nullptr, std::integral_constant<int, 2>{});
+  const int v = lane_channels(c);
+  if (c.dtype == WERSA_F32) v == 1 ? packed((float *)nullptr, std::integral_constant<int, 1>{}) : packed((float *)nullptr, std::integral_constant<int, 2>{});
+  else if (v == 4) packed((bf16_t *)nullptr, std::integral_constant<int, 4>{});
+  else v == 2 ? packed((bf16_t *)nullptr, std::integral_constant<int, 2>{}) : packed((bf16_t *)nullptr, std::integral_constant<int, 1>{});
 }
 
 Job job_of(const wersa_recurrence_desc &c, const Layout &l, void *workspace) {
@@ -574,7 +691,7 @@ Job job_of(const wersa_recurrence_desc &c, const Layout &l, void *workspace) {
 
 void make_ready(const Layout &l, void *workspace, hipStream_t st) {
   if (l.tiles <= 1) return;
-  const int64_t count = (int64_t)(l.total / 16);
+  const int64_t count = (int64_t)(l.initial / 16);
   WERSA_STAGE("wersa_recurrence_ready", st, (recurrence_ready_kernel<<<(unsigned)std::min<int64_t>((count + 255) / 256, 1024), 256, 0, st>>>((u32x4 *)workspace, count)));
 }
 
@@ -607,7 +724,8 @@ wersa_status wersa_recurrence_forward(const wersa_recurrence_desc *desc, const v
   if (!written_apart(*desc, {desc->stride_o}) || (desc->packed != 0) != (offsets != nullptr) || (slots && state_slots < 0)) return WERSA_ERR_INVALID_ARG;
   if (desc->n > 0 && (!x || !gate || !out)) return WERSA_ERR_INVALID_ARG;
   const Layout l = layout_of(*desc);
-  if (l.tiles > 1 && (!workspace || workspace_bytes < l.total || misaligned(workspace, 256))) return WERSA_ERR_WORKSPACE;
+  const bool gathers = desc->packed && initial_state && initial_state == final_state;
+  if ((l.tiles > 1 || gathers) && (!workspace || workspace_bytes < l.total || misaligned(workspace, 256))) return WERSA_ERR_WORKSPACE;
   if (misaligned(saved, 256)) return WERSA_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)hip_stream;
   Job a = job_of(*desc, l, workspace);
@@ -615,6 +733,13 @@ wersa_status wersa_recurrence_forward(const wersa_recurrence_desc *desc, const v
   if (slots) a.state_slots = state_slots;
   if (desc->n == 0) return pass_states(a, initial_state, final_state, st);
   make_ready(l, workspace, st);
+  if (gathers) {
+    float *to = (float *)((char *)workspace + l.initial);
+    WERSA_STAGE("wersa_recurrence_gather", st,
+                (recurrence_gather_kernel<<<(unsigned)std::min<int64_t>(((int64_t)a.B * a.C + 255) / 256, 4096), 256, 0, st>>>(a, to)));
+    a.initial = to;
+    a.gathered = 1;
+  }
   by_type(*desc, [&](auto *type, auto v, auto packed) {
     typedef typename std::remove_pointer<decltype(type)>::type T;
     WERSA_STAGE("wersa_recurrence", st, (recurrence_kernel<T, decltype(v)::value, decltype(packed)::value><<<grid_of((int64_t)l.chains * l.tiles), kThreads, 0, st>>>(a)));
@@ -655,9 +780,11 @@ wersa_status wersa_recurrence_step(const wersa_recurrence_desc *desc, const void
   Job a = job_of(*desc, layout_of(*desc), nullptr);
   a.x = x, a.gate = gate, a.final = state, a.slots = slots, a.out = out;
   if (slots) a.state_slots = state_slots;
-  const dim3 grid((desc->C + 1023) / 1024, desc->B);
-  if (desc->dtype == WERSA_F32) WERSA_STAGE("wersa_recurrence_step", st, (recurrence_step_kernel<float><<<grid, 256, 0, st>>>(a)));
-  else WERSA_STAGE("wersa_recurrence_step", st, (recurrence_step_kernel<bf16_t><<<grid, 256, 0, st>>>(a)));
+  by_type(*desc, [&](auto *type, auto v, auto) {
+    typedef typename std::remove_pointer<decltype(type)>::type T;
+    constexpr int V = decltype(v)::value;
+    WERSA_STAGE("wersa_recurrence_step", st, (recurrence_step_kernel<T, V><<<dim3((desc->C + 256 * V - 1) / (256 * V), desc->B), 256, 0, st>>>(a)));
+  });
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
 
