@@ -35,7 +35,7 @@ struct Job {
   uint64_t *spans;                    // [chain][tile][channels of a slab]: (A, H),
   uint32_t *states;                   // [chain][group][channels of a slab]: the state behind a group
   int64_t sx[2], sg[2], so[2], sdx[2], sdg[2];
-  int B, n, C, tiles, slabs, chains, state_slots, clear, gathered;
+  int B, n, C, tiles, slabs, chains, state_slots, clear;
 };
 
 template <typename T> __device__ __forceinline__ void gate_parts(float g, float &a, float &rest) {
@@ -150,6 +150,13 @@ template <typename T, int V> __device__ __forceinline__ void anew(Raw<T, V> (&v)
     for (uint32_t &u : v[r].u) asm volatile("" : "+v"(u));
 }
 
+// A value that is formed here, and not behind the rows to come, which would keep what it is formed from.
+__device__ __forceinline__ void here(float &v) { asm volatile("" : "+v"(v)); }
+template <typename T, int V> __device__ __forceinline__ void here(Raw<T, V> &v) {
+#pragma unroll
+  for (uint32_t &u : v.u) asm volatile("" : "+v"(u));
+}
+
 // A span's (A, H).  A below 0: the state before the span does not reach its end (a sequence begins within), whatever it is.
 struct Span { float A, H; };
 __device__ __forceinline__ float after(const Span &s, float h) { return s.A < 0.f ? s.H : fmaf(s.A, h, s.H); }
@@ -221,14 +228,14 @@ __device__ __forceinline__ float state_before(const Job &a, int chain, int at, f
 // Packed sequences: what a row is.
 constexpr int kFirst = 1 << 16, kLast = 1 << 17, kOutside = 1 << 18;   // beside the sequence's number
 __device__ __forceinline__ int offset_of(const Job &a, int b) { return min(max(a.offsets[b], 0), a.n); }
-__device__ __forceinline__ int row_kind(const Job &a, int t) {
-  int lo = 0, hi = a.B;     // the last sequence that begins at or before row t
+template <typename F> __device__ __forceinline__ int row_kind(int B, int t, F offset) {
+  int lo = 0, hi = B;     // the last sequence that begins at or before row t
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
-    if (offset_of(a, mid) <= t) lo = mid;
+    if (offset(mid) <= t) lo = mid;
     else hi = mid;
   }
-  const int begin = offset_of(a, lo), end = offset_of(a, lo + 1);
+  const int begin = offset(lo), end = offset(lo + 1);
   if (t < begin || t >= end) return kOutside;
   return lo | (t == begin ? kFirst : 0) | (t == end - 1 ? kLast : 0);
 }
@@ -238,38 +245,58 @@ __device__ __forceinline__ int64_t slot_of(const Job &a, int b) {   // below 0: 
   return s >= 0 && s < a.state_slots ? s : -1;
 }
 
-// Packed sequences' initial states, by slots, or by sequence where they have been gathered.
-__device__ __forceinline__ float first_state(const Job &a, int b, int c, bool there) {
-  if (!a.initial || !there) return 0.f;
-  const int64_t slot = a.gathered ? b : slot_of(a, b);
-  return slot >= 0 ? a.initial[slot * a.C + c] : 0.f;
+// V states from `p` on, of which `valid` are a row's; none: zeros.
+typedef float f32x4 __attribute__((ext_vector_type(4), aligned(4)));
+template <int V> __device__ __forceinline__ void load_states(const float *p, int valid, float (&h)[V]) {
+  if (V == 4 && valid >= V) {
+    const f32x4 v = *reinterpret_cast<const f32x4 *>(p);
+#pragma unroll
+    for (int i = 0; i < V; ++i) h[i] = v[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) h[i] = i < valid ? p[i] : 0.f;
+  }
+}
+// Packed sequences' initial states and final states' gradients, by sequence.
+template <int V> __device__ __forceinline__ void states_of(const float *states, const Job &a, int kind, int c, int valid, float (&h)[V]) {
+  if (states) load_states<V>(states + (int64_t)(kind & 0xffff) * a.C + c, valid, h);
+  else {
+#pragma unroll
+    for (int i = 0; i < V; ++i) h[i] = 0.f;
+  }
 }
 
-template <int V> __device__ __forceinline__ void first_states(const Job &a, int kind, int c, int valid, float (&h)[V]) {
-#pragma unroll
-  for (int i = 0; i < V; ++i) h[i] = first_state(a, kind & 0xffff, c + i, i < valid);
-}
-template <int V> __device__ __forceinline__ void last_gradients(const Job &a, int kind, int c, int valid, float (&g)[V]) {
-#pragma unroll
-  for (int i = 0; i < V; ++i) g[i] = a.dfinal && i < valid ? a.dfinal[(int64_t)(kind & 0xffff) * a.C + c + i] : 0.f;
-}
-
-// What a thread's rows are, a bit for each: not there (of no sequence, or past the end), not to be written, and (packed) the first and the last ones of sequences.
-struct Marks { int outside, unwritten, first, last; };
-template <bool PACKED> __device__ __forceinline__ Marks marks_of(const Job &a, int tile, int row0, int span, bool whole, int *kinds) {
-  Marks m{0, 0, 0, 0};
-  if (!whole) m.outside = m.unwritten = ~0 << min(max(a.n - row0, 0), kR) & ((1 << kR) - 1);
+// What a thread's rows are, a bit for each: not there (of no sequence, or past the end), and (packed) the first and the last ones of sequences.
+struct Marks {
+  int bits;
+  __device__ bool outside(int r) const { return bits >> r & 1; }
+  __device__ bool first(int r) const { return bits >> (8 + r) & 1; }
+  __device__ bool last(int r) const { return bits >> (16 + r) & 1; }
+  __device__ int all_outside() const { return bits & 0xff; }
+  __device__ int any_first() const { return bits & 0xff00; }
+};
+__device__ __forceinline__ int rows_past(const Job &a, int row0) { return ~0 << min(max(a.n - row0, 0), kR) & ((1 << kR) - 1); }
+// near: offset threadIdx.x, where there are so few that each thread has one (the search goes through LDS then: a chain of loads from memory takes 2 us).
+template <bool PACKED> __device__ __forceinline__ Marks marks_of(const Job &a, int tile, int row0, int span, bool whole, int near, int *offsets, int *kinds) {
+  static_assert(kR == 8, "eight bits each");
+  Marks m{whole ? 0 : rows_past(a, row0)};
   if (PACKED) {
     int kind = 0;
-    if (threadIdx.x < kRows) kinds[threadIdx.x] = kind = tile * kRows + (int)threadIdx.x < a.n ? row_kind(a, tile * kRows + threadIdx.x) : kOutside;
+    const int t = tile * kRows + threadIdx.x;
+    if (a.B < kThreads) {
+      offsets[threadIdx.x] = near;
+      __syncthreads();
+      if (threadIdx.x < kRows) kind = t < a.n ? row_kind(a.B, t, [&](int b) { return offsets[b]; }) : kOutside;
+    } else if (threadIdx.x < kRows) {
+      kind = t < a.n ? row_kind(a.B, t, [&](int b) { return offset_of(a, b); }) : kOutside;
+    }
+    if (threadIdx.x < kRows) kinds[threadIdx.x] = kind;
     if (__syncthreads_or(kind & (kFirst | kLast | kOutside))) {
-      m.outside = 0;
+      m.bits = 0;
 #pragma unroll
       for (int r = 0; r < kR; ++r) {
         const int k = kinds[span * kR + r];
-        m.outside |= (k & kOutside ? 1 : 0) << r;
-        m.first |= (k & kFirst ? 1 : 0) << r;
-        m.last |= (k & kLast ? 1 : 0) << r;
+        m.bits |= ((k & kOutside ? 1 : 0) | (k & kFirst ? 1 << 8 : 0) | (k & kLast ? 1 << 16 : 0)) << r;
       }
     }
   }
@@ -279,7 +306,7 @@ template <bool PACKED> __device__ __forceinline__ Marks marks_of(const Job &a, i
 template <typename T, int V> __device__ __forceinline__ void pass_over(const Marks &m, Raw<T, V> (&g)[kR], Raw<T, V> (&x)[kR]) {
 #pragma unroll
   for (int r = 0; r < kR; ++r)
-    if (m.outside >> r & 1) {
+    if (m.outside(r)) {
 #pragma unroll
       for (uint32_t &u : g[r].u) u = sizeof(T) == 4 ? 0x7f800000u : 0x7f807f80u;
 #pragma unroll
@@ -289,7 +316,7 @@ template <typename T, int V> __device__ __forceinline__ void pass_over(const Mar
 template <typename T, int V> __device__ __forceinline__ void clear_outside(const Marks &m, Raw<T, V> (&v)[kR]) {
 #pragma unroll
   for (int r = 0; r < kR; ++r)
-    if (m.outside >> r & 1) {
+    if (m.outside(r)) {
 #pragma unroll
       for (uint32_t &u : v[r].u) u = 0;
     }
@@ -312,25 +339,26 @@ __device__ __forceinline__ bool next_tile(const Job &a, int &chain, int &at) {
 }
 
 template <typename T, int V, bool PACKED>
-__global__ __launch_bounds__(kThreads, 6) void recurrence_kernel(Job a) {
+__global__ __launch_bounds__(kThreads, PACKED ? 4 : 6) void recurrence_kernel(Job a) {
   constexpr int CH = kLanes * V;
   __shared__ Span part[kSpans][CH], joined[kWaves][CH];
   __shared__ float before[CH];
-  __shared__ int kinds[PACKED ? kRows : 1];
+  __shared__ int kinds[PACKED ? kRows : 1], offsets[PACKED ? kThreads : 1];
   int chain, tile;
   if (!next_tile(a, chain, tile)) return;
   const int batch = chain / a.slabs, c0 = (chain % a.slabs) * CH, lane = threadIdx.x % kLanes, span = threadIdx.x / kLanes;
   const int c = c0 + lane * V, valid = a.C - c, row0 = tile * kRows + span * kR;
   const bool whole = (tile + 1) * (int64_t)kRows <= a.n;
+  const int near = PACKED && (int)threadIdx.x <= a.B ? offset_of(a, threadIdx.x) : 0;
   Raw<T, V> rx[kR], rg[kR];
   load_rows<T, V>(a.gate, batch, a.sg, c, a.C, row0, a.n, whole, rg);
   load_rows<T, V>(a.x, batch, a.sx, c, a.C, row0, a.n, whole, rx);
-  const Marks m = marks_of<PACKED>(a, tile, row0, span, whole, kinds);
+  const Marks m = marks_of<PACKED>(a, tile, row0, span, whole, near, offsets, kinds);
   if (a.C % V) {
     move_rows<T, V>(rg, valid);
     move_rows<T, V>(rx, valid);
   }
-  if (m.outside) pass_over<T, V>(m, rg, rx);
+  if (m.all_outside()) pass_over<T, V>(m, rg, rx);
   float both[kR][V];    // a and 1 - a of each row
   Span s[V];
   float h[V];
@@ -338,21 +366,21 @@ __global__ __launch_bounds__(kThreads, 6) void recurrence_kernel(Job a) {
   for (int i = 0; i < V; ++i) s[i] = Span{1.f, 0.f}, h[i] = 0.f;
 #pragma unroll
   for (int r = 0; r < kR; ++r) {
-    if (PACKED && (m.first >> r & 1)) first_states<V>(a, kinds[span * kR + r], c, valid, h);
+    if (PACKED && m.first(r)) states_of<V>(a.initial, a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float g = channel(rg[r], i);
       float keep, rest;
       gate_parts<T>(g, keep, rest);
       both[r][i] = packed_parts(g, keep, rest);
+      here(both[r][i]);
       h[i] = fmaf(keep, h[i], rest * channel(rx[r], i));
       s[i].A *= keep;
     }
   }
-  anew(both);
   anew<T, V>(rx);
 #pragma unroll
-  for (int i = 0; i < V; ++i) part[span][lane * V + i] = Span{PACKED && m.first ? -1.f : s[i].A, h[i]};
+  for (int i = 0; i < V; ++i) part[span][lane * V + i] = Span{PACKED && m.any_first() ? -1.f : s[i].A, h[i]};
   __syncthreads();
   float begin = 0.f;
   const int mine = c0 + threadIdx.x;
@@ -381,7 +409,7 @@ __global__ __launch_bounds__(kThreads, 6) void recurrence_kernel(Job a) {
   Raw<T, V> put[kR];
 #pragma unroll
   for (int r = 0; r < kR; ++r) {
-    if (PACKED && (m.first >> r & 1)) first_states<V>(a, kinds[span * kR + r], c, valid, h);
+    if (PACKED && m.first(r)) states_of<V>(a.initial, a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       float keep, rest;
@@ -389,17 +417,18 @@ __global__ __launch_bounds__(kThreads, 6) void recurrence_kernel(Job a) {
       h[i] = fmaf(keep, h[i], rest * channel(rx[r], i));
     }
     put[r] = rounded_channels<T, V>(h);
-    if (PACKED && (m.last >> r & 1) && a.final) {
+    here<T, V>(put[r]);
+    if (PACKED && m.last(r) && a.final) {
       const int64_t slot = slot_of(a, kinds[span * kR + r] & 0xffff);
 #pragma unroll
       for (int i = 0; i < V; ++i)
         if (slot >= 0 && i < valid) a.final[slot * a.C + c + i] = h[i];
     }
   }
-  int unwritten = m.unwritten;
-  if (PACKED && m.outside) {
+  int unwritten = whole ? 0 : rows_past(a, row0);
+  if (PACKED && m.all_outside()) {
     clear_outside<T, V>(m, put);
-    if (!a.clear) unwritten |= m.outside;
+    if (!a.clear) unwritten |= m.all_outside();
   }
   store_rows<T, V>((T *)a.out + batch * a.so[0] + row0 * a.so[1] + c, a.so[1], valid, put, unwritten);
   if (!PACKED && a.final && row0 < a.n && row0 + kR >= a.n) {   // (rows past the end leave h as it is)
@@ -414,7 +443,7 @@ __global__ __launch_bounds__(kThreads, 6) void recurrence_kernel(Job a) {
       const int channel_of = c0 + threadIdx.x % CH;
       const int64_t slot = slot_of(a, b);
       if (offset_of(a, b) >= offset_of(a, b + 1) && slot >= 0 && channel_of < a.C)
-        a.final[slot * a.C + channel_of] = first_state(a, b, channel_of, true);
+        a.final[slot * a.C + channel_of] = a.initial ? a.initial[(int64_t)b * a.C + channel_of] : 0.f;
     }
   }
 }
@@ -425,24 +454,25 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
   constexpr int CH = kLanes * V;
   __shared__ Span part[kSpans][CH], back[kSpans][CH], joined[kWaves][CH];
   __shared__ float before[CH];
-  __shared__ int kinds[PACKED ? kRows : 1];
+  __shared__ int kinds[PACKED ? kRows : 1], offsets[PACKED ? kThreads : 1];
   int chain, at;
   if (!next_tile(a, chain, at)) return;
   const int tile = a.tiles - 1 - at;
   const int batch = chain / a.slabs, c0 = (chain % a.slabs) * CH, lane = threadIdx.x % kLanes, span = threadIdx.x / kLanes;
   const int c = c0 + lane * V, valid = a.C - c, row0 = tile * kRows + span * kR;
   const bool whole = (tile + 1) * (int64_t)kRows <= a.n;
+  const int near = PACKED && (int)threadIdx.x <= a.B ? offset_of(a, threadIdx.x) : 0;
   Raw<T, V> rx[kR], rg[kR], rd[kR];
   load_rows<T, V>(a.gate, batch, a.sg, c, a.C, row0, a.n, whole, rg);
   load_rows<T, V>(a.x, batch, a.sx, c, a.C, row0, a.n, whole, rx);
   load_rows<T, V>(a.dout, batch, a.so, c, a.C, row0, a.n, whole, rd);
-  const Marks m = marks_of<PACKED>(a, tile, row0, span, whole, kinds);
+  const Marks m = marks_of<PACKED>(a, tile, row0, span, whole, near, offsets, kinds);
   if (a.C % V) {
     move_rows<T, V>(rg, valid);
     move_rows<T, V>(rx, valid);
     move_rows<T, V>(rd, valid);
   }
-  if (m.outside) {
+  if (m.all_outside()) {
     pass_over<T, V>(m, rg, rx);
     clear_outside<T, V>(m, rd);
   }
@@ -451,27 +481,27 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
   for (int i = 0; i < V; ++i) A[i] = 1.f, h[i] = carry[i] = 0.f;
 #pragma unroll
   for (int r = 0; r < kR; ++r) {
-    if (PACKED && (m.first >> r & 1)) first_states<V>(a, kinds[span * kR + r], c, valid, h);
+    if (PACKED && m.first(r)) states_of<V>(a.initial, a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float g = channel(rg[r], i);
       float keep, rest;
       gate_parts<T>(g, keep, rest);
       both[r][i] = packed_parts(g, keep, rest);
+      here(both[r][i]);
       h[i] = fmaf(keep, h[i], rest * channel(rx[r], i));
       A[i] *= keep;
     }
   }
-  anew(both);
 #pragma unroll
   for (int r = kR - 1; r >= 0; --r) {
-    if (PACKED && (m.last >> r & 1)) last_gradients<V>(a, kinds[span * kR + r], c, valid, carry);   // (nothing else comes from behind a sequence)
+    if (PACKED && m.last(r)) states_of<V>(a.dfinal, a, kinds[span * kR + r], c, valid, carry);   // (nothing else comes from behind a sequence)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       float keep, rest;
       parts_of(both[r][i], keep, rest);
       carry[i] = keep * (channel(rd[r], i) + carry[i]);
-      if (PACKED && (m.first >> r & 1)) carry[i] = 0.f;
+      if (PACKED && m.first(r)) carry[i] = 0.f;
     }
   }
   anew(both);
@@ -479,7 +509,7 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
   anew<T, V>(rd);
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    if (PACKED && m.first) A[i] = -1.f;
+    if (PACKED && m.any_first()) A[i] = -1.f;
     part[span][lane * V + i] = Span{A[i], h[i]};
     back[span][lane * V + i] = Span{A[i], carry[i]};
   }
@@ -515,13 +545,14 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
   }
 #pragma unroll
   for (int r = 0; r < kR; ++r) {
-    if (PACKED && (m.first >> r & 1)) first_states<V>(a, kinds[span * kR + r], c, valid, h);
+    if (PACKED && m.first(r)) states_of<V>(a.initial, a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       float keep, rest;
       parts_of(both[r][i], keep, rest);
       const float x = channel(rx[r], i);
       D[r][i] = keep * (h[i] - x);
+      here(D[r][i]);
       h[i] = fmaf(keep, h[i], rest * x);
     }
   }
@@ -529,7 +560,7 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
   Raw<T, V> px[kR], pg[kR];
 #pragma unroll
   for (int r = kR - 1; r >= 0; --r) {
-    if (PACKED && (m.last >> r & 1)) last_gradients<V>(a, kinds[span * kR + r], c, valid, carry);
+    if (PACKED && m.last(r)) states_of<V>(a.dfinal, a, kinds[span * kR + r], c, valid, carry);
     float gx[V], gg[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
@@ -542,7 +573,9 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
     }
     px[r] = rounded_channels<T, V>(gx);
     pg[r] = rounded_channels<T, V>(gg);
-    if (PACKED && (m.first >> r & 1)) {
+    here<T, V>(px[r]);
+    here<T, V>(pg[r]);
+    if (PACKED && m.first(r)) {
       const int64_t to = (int64_t)(kinds[span * kR + r] & 0xffff) * a.C + c;
 #pragma unroll
       for (int i = 0; i < V; ++i) {
@@ -551,12 +584,13 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
       }
     }
   }
-  if (PACKED && m.outside) {
+  const int unwritten = whole ? 0 : rows_past(a, row0);
+  if (PACKED && m.all_outside()) {
     clear_outside<T, V>(m, px);
     clear_outside<T, V>(m, pg);
   }
-  store_rows<T, V>((T *)a.dx + batch * a.sdx[0] + row0 * a.sdx[1] + c, a.sdx[1], valid, px, m.unwritten);
-  store_rows<T, V>((T *)a.dgate + batch * a.sdg[0] + row0 * a.sdg[1] + c, a.sdg[1], valid, pg, m.unwritten);
+  store_rows<T, V>((T *)a.dx + batch * a.sdx[0] + row0 * a.sdx[1] + c, a.sdx[1], valid, px, unwritten);
+  store_rows<T, V>((T *)a.dgate + batch * a.sdg[0] + row0 * a.sdg[1] + c, a.sdg[1], valid, pg, unwritten);
   if (!PACKED && a.dinitial && row0 == 0) {
 #pragma unroll
     for (int i = 0; i < V; ++i)
@@ -585,7 +619,7 @@ __global__ __launch_bounds__(256) void recurrence_states_kernel(Job a, const flo
   }
 }
 
-// Initial states that lie where the final ones go, by sequence: a sequence may end before another thread has read where it begins.
+// Initial states by sequence, where they are addressed by slots or lie where the final ones go (a sequence may end before another thread has read where it begins).
 __global__ __launch_bounds__(256) void recurrence_gather_kernel(Job a, float *to) {
   for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < (int64_t)a.B * a.C; i += (int64_t)gridDim.x * 256) {
     const int64_t slot = slot_of(a, (int)(i / a.C));
@@ -724,7 +758,7 @@ wersa_status wersa_recurrence_forward(const wersa_recurrence_desc *desc, const v
   if (!written_apart(*desc, {desc->stride_o}) || (desc->packed != 0) != (offsets != nullptr) || (slots && state_slots < 0)) return WERSA_ERR_INVALID_ARG;
   if (desc->n > 0 && (!x || !gate || !out)) return WERSA_ERR_INVALID_ARG;
   const Layout l = layout_of(*desc);
-  const bool gathers = desc->packed && initial_state && initial_state == final_state;
+  const bool gathers = desc->packed && initial_state && (slots || initial_state == final_state);
   if ((l.tiles > 1 || gathers) && (!workspace || workspace_bytes < l.total || misaligned(workspace, 256))) return WERSA_ERR_WORKSPACE;
   if (misaligned(saved, 256)) return WERSA_ERR_WORKSPACE;
   hipStream_t st = (hipStream_t)hip_stream;
@@ -738,7 +772,6 @@ wersa_status wersa_recurrence_forward(const wersa_recurrence_desc *desc, const v
     WERSA_STAGE("wersa_recurrence_gather", st,
                 (recurrence_gather_kernel<<<(unsigned)std::min<int64_t>(((int64_t)a.B * a.C + 255) / 256, 4096), 256, 0, st>>>(a, to)));
     a.initial = to;
-    a.gathered = 1;
   }
   by_type(*desc, [&](auto *type, auto v, auto packed) {
     typedef typename std::remove_pointer<decltype(type)>::type T;
