@@ -48,8 +48,10 @@ def _load_node():
         node.bind_causal([ctypes.cast(f, ctypes.c_void_p).value for f in (
             lib.wersa_decay_forward, lib.wersa_decay_backward, lib.wersa_decay_workspace_bytes, lib.wersa_decay_saved_bytes,
             lib.wersa_rms_norm_forward, lib.wersa_rms_norm_backward, lib.wersa_rms_norm_workspace_bytes)])
-        node.bind_layer_norm(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-            lib.wersa_layer_norm_forward, lib.wersa_layer_norm_backward, lib.wersa_layer_norm_workspace_bytes)))
+        node.bind_decoder([ctypes.cast(f, ctypes.c_void_p).value for f in (
+            lib.wersa_layer_norm_forward, lib.wersa_layer_norm_backward, lib.wersa_layer_norm_workspace_bytes,
+            lib.wersa_recurrence_forward, lib.wersa_recurrence_backward, lib.wersa_recurrence_workspace_bytes, lib.wersa_recurrence_saved_bytes,
+            lib.wersa_embedding_forward, lib.wersa_embedding_backward, lib.wersa_embedding_workspace_bytes)])
         _node = node
     return _node
 
@@ -259,7 +261,11 @@ def wersa_recurrence(x, gate, initial_state=None, offsets=None):
     """Gated linear recurrence: h_t = sigmoid(gate_t) h_{t-1} + (1 - sigmoid(gate_t)) x_t for each channel of x, gate (B, n, C).  Returns (out, final states (B, C) in
     float32).  Rows of no sequence are zeros in out and in the gradients, whatever they hold."""
     x, gate = _channels_side_by_side(x), _channels_side_by_side(gate)
-    return _Recurrence.apply(x, gate, initial_state, offsets)
+    node = _load_node() if _node is None else _node
+    if not node or torch.jit.is_tracing():
+        return _Recurrence.apply(x, gate, initial_state, offsets)
+    desc, saved_bytes, workspace = binding.checked_recurrence_desc(x, gate, offsets, initial_state)
+    return tuple(node.recurrence(x, gate, initial_state, offsets, bytes(desc), saved_bytes, workspace))
 
 
 class _Embedding(torch.autograd.Function):
@@ -280,4 +286,7 @@ def wersa_embedding(tokens, weight, scale=1.0, dtype=None):
     """scale * weight[tokens] of `dtype` (the weight's by default), zeros for tokens that have no row; the gradient of the weight is dense and of its dtype."""
     assert weight.dim() == 2, "weight is (vocabulary, cols)"
     tokens, weight = binding.checked_tokens(tokens), _as_rows(weight)
-    return _Embedding.apply(tokens, weight, float(scale), weight.dtype if dtype is None else dtype)
+    node = _load_node() if _node is None else _node
+    if not node or torch.jit.is_tracing():
+        return _Embedding.apply(tokens, weight, float(scale), weight.dtype if dtype is None else dtype)
+    return node.embedding(tokens, weight, scale, binding.checked_embedding_types(tokens, weight, dtype))

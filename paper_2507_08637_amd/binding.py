@@ -881,12 +881,12 @@ def make_recurrence_desc(x, gate, out, offsets=None, clear=False, dx=None, dgate
     return WersaRecurrenceDesc.from_buffer_copy(_RECURRENCE_DESC.pack(B, n, C, _dtype_code(x), offsets is not None, clear, *strides))
 
 
-def checked_recurrence_desc(x, gate, out, offsets, initial_state, clear=False):
-    """(descriptor, bytes of saved, bytes of workspace) of a forward call without slots; the arguments are checked."""
+def checked_recurrence_desc(x, gate, offsets, initial_state):
+    """(descriptor, bytes of saved, bytes of workspace) of a forward call, whose output's strides the caller fills in; the arguments are checked."""
     lib = load_library()
-    desc = make_recurrence_desc(x, gate, out, offsets, clear)
+    desc = make_recurrence_desc(x, gate, None, offsets)
     _channel_states(desc, None, initial_state)
-    _on_current_gpu(x, gate, out, offsets, initial_state)
+    _on_current_gpu(x, gate, offsets, initial_state)
     wb = lib.wersa_recurrence_workspace_bytes(ctypes.byref(desc))
     if wb == 0:   # the precise status
         _check(lib.wersa_recurrence_forward(ctypes.byref(desc), *([None] * 6), 0, *([None] * 3), 0, None))
@@ -985,6 +985,17 @@ def _rows_of(x, shape, name):
     flat = x.view(-1, shape[-1])   # (raises where there is no such stride)
     assert flat.stride(1) == 1 and (flat.stride(0) >= shape[-1] or flat.shape[0] <= 1), f"{name} has contiguous columns and rows that do not share memory"
     return flat.stride(0)
+
+
+def checked_embedding_types(tokens, weight, dtype):
+    """The code of out's type; the arguments are checked."""
+    _dtype_code(weight)
+    _on_current_gpu(weight, tokens)
+    if dtype is None:
+        return _dtype_code(weight)
+    if dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("dtype must be float32 or bfloat16")
+    return WERSA_F32 if dtype == torch.float32 else WERSA_BF16
 
 
 @_on_stream

@@ -309,6 +309,116 @@ struct LayerNorm : torch::autograd::Function<LayerNorm> {
   }
 };
 
+decltype(&wersa_recurrence_forward) recurrence_forward_fn = nullptr;
+decltype(&wersa_recurrence_backward) recurrence_backward_fn = nullptr;
+decltype(&wersa_recurrence_workspace_bytes) recurrence_workspace_bytes_fn = nullptr;
+decltype(&wersa_recurrence_saved_bytes) recurrence_saved_bytes_fn = nullptr;
+
+struct Recurrence : torch::autograd::Function<Recurrence> {
+  static variable_list forward(AutogradContext *ctx, const Tensor &x, const Tensor &gate, const std::optional<Tensor> &initial_state,
+                               const std::optional<Tensor> &sequences, const std::string &desc, int64_t saved_bytes, int64_t workspace) {
+    const Tensor initial = or_none(initial_state), offsets = or_none(sequences);
+    wersa_recurrence_desc d;
+    TORCH_CHECK(desc.size() == sizeof(d), "descriptor of another size");
+    std::memcpy(&d, desc.data(), sizeof(d));
+    const Tensor out = at::empty(x.sizes(), x.options());
+    d.stride_o[0] = out.stride(0), d.stride_o[1] = out.stride(1);
+    d.clear = d.packed;
+    const auto f32 = x.options().dtype(at::kFloat);
+    const Tensor final_state = at::empty({d.B, d.C}, f32), saved = at::empty({saved_bytes / 4}, f32), ws = scratch(workspace, x);
+    check(recurrence_forward_fn(&d, in(x), in(gate), (const int32_t *)in(offsets), (const float *)in(initial), floats_out(final_state), nullptr, d.B, out_of(out),
+                                out_of(saved), ws.mutable_data_ptr(), ws.nbytes(), stream(x)));
+    ctx->save_for_backward({x, gate, initial, offsets, saved});
+    ctx->saved_data["desc"] = desc;
+    ctx->set_materialize_grads(false);
+    return {out, final_state};
+  }
+
+  // As above, the call is described by the tensors that are there now.  `saved` does not depend on their strides.
+  static variable_list backward(AutogradContext *ctx, const variable_list &grads) {
+    once();
+    const variable_list t = ctx->get_saved_variables();
+    const Tensor &x = t[0], &gate = t[1], &initial = t[2], &offsets = t[3], &saved = t[4];
+    wersa_recurrence_desc d;
+    std::memcpy(&d, ctx->saved_data["desc"].toStringRef().data(), sizeof(d));
+    const int64_t N = d.packed ? 1 : d.B;
+    for (const Tensor *y : {&x, &gate})
+      require(y->dim() == 3 && y->sizes() == at::IntArrayRef({N, d.n, d.C}) && dtype_of(*y) == d.dtype && (y->stride(2) == 1 || d.C == 1),
+              "expect x and gate as they were saved: (B, n, C) with contiguous channels");
+    auto states = [&](const Tensor &y) { return !y.defined() || holds_floats(y, (int64_t)d.B * d.C); };
+    require(states(initial) && holds_floats(saved, (int64_t)recurrence_saved_bytes_fn(&d) / 4) &&
+                (offsets.defined() ? d.packed && offsets.scalar_type() == at::kInt && offsets.is_contiguous() && offsets.numel() == d.B + 1 : !d.packed),
+            "expect the states and the offsets as they were saved");
+    Tensor dout = grads[0], dfinal = grads[1];
+    if (!dout.defined()) dout = at::zeros({d.C}, x.options()).expand(x.sizes());
+    if (dout.dim() == 3 && dout.stride(2) != 1) dout = dout.contiguous();
+    if (dfinal.defined()) dfinal = dfinal.contiguous();
+    require(dout.sizes() == x.sizes() && dout.dtype() == x.dtype() && states(dfinal), "gradients of other shapes or types than the outputs");
+    for (const Tensor &y : t) require(!y.defined() || y.device() == dout.device(), "saved tensors on another device");
+    const Tensor dx = at::empty(x.sizes(), x.options()), dgate = at::empty(x.sizes(), x.options()),
+                 dinitial = initial.defined() && ctx->needs_input_grad(2) ? at::empty_like(initial) : Tensor();
+    auto put = [](int64_t *to, const Tensor &y) { to[0] = y.stride(0), to[1] = y.stride(1); };
+    put(d.stride_x, x);
+    put(d.stride_gate, gate);
+    put(d.stride_o, dout);
+    put(d.stride_dx, dx);
+    put(d.stride_dgate, dgate);
+    const Tensor ws = scratch((int64_t)recurrence_workspace_bytes_fn(&d), x);
+    check(recurrence_backward_fn(&d, in(x), in(gate), (const int32_t *)in(offsets), (const float *)in(initial), in(dout), (const float *)in(dfinal),
+                                 saved.const_data_ptr(), out_of(dx), out_of(dgate), (float *)out_of(dinitial), ws.mutable_data_ptr(), ws.nbytes(), stream(x)));
+    return {dx, dgate, dinitial, Tensor(), Tensor(), Tensor(), Tensor()};
+  }
+};
+
+variable_list recurrence(const Tensor &x, const Tensor &gate, const std::optional<Tensor> &initial, const std::optional<Tensor> &offsets,
+                         const pybind11::bytes &desc, int64_t saved_bytes, int64_t workspace) {
+  const std::string d = desc;
+  pybind11::gil_scoped_release nogil;
+  return Recurrence::apply(x, gate, initial, offsets, d, saved_bytes, workspace);
+}
+
+decltype(&wersa_embedding_forward) embedding_forward_fn = nullptr;
+decltype(&wersa_embedding_backward) embedding_backward_fn = nullptr;
+decltype(&wersa_embedding_workspace_bytes) embedding_workspace_bytes_fn = nullptr;
+
+struct Embedding : torch::autograd::Function<Embedding> {
+  static Tensor forward(AutogradContext *ctx, const Tensor &tokens, const Tensor &weight, double scale, int64_t dtype) {
+    std::vector<int64_t> shape = tokens.sizes().vec();
+    const int64_t cols = weight.size(1);
+    shape.push_back(cols);
+    const Tensor out = at::empty(shape, weight.options().dtype(dtype == WERSA_F32 ? at::kFloat : at::kBFloat16));
+    const wersa_embedding_desc d{tokens.numel(), (int32_t)weight.size(0), (int32_t)cols, (int32_t)dtype, dtype_of(weight), (int32_t)tokens.element_size(),
+                                 (float)scale, weight.stride(0), cols};
+    check(embedding_forward_fn(&d, in(tokens), in(weight), out_of(out), stream(weight)));
+    ctx->save_for_backward({tokens});
+    ctx->saved_data["vocabulary"] = weight.size(0);
+    ctx->saved_data["dtype"] = (int64_t)dtype_of(weight);
+    ctx->saved_data["scale"] = scale;
+    return out;
+  }
+
+  static variable_list backward(AutogradContext *ctx, const variable_list &grads) {
+    once();
+    const variable_list t = ctx->get_saved_variables();
+    const Tensor &tokens = t[0], dout = grads[0].contiguous();
+    require((tokens.scalar_type() == at::kInt || tokens.scalar_type() == at::kLong) && tokens.is_contiguous() && dout.dim() == tokens.dim() + 1 &&
+                dout.sizes().slice(0, tokens.dim()) == tokens.sizes() && dtype_of(dout) >= 0 && tokens.device() == dout.device(),
+            "expect the tokens as they were saved");
+    const int64_t vocabulary = ctx->saved_data["vocabulary"].toInt(), dtype = ctx->saved_data["dtype"].toInt(), cols = dout.size(-1);
+    const wersa_embedding_desc d{tokens.numel(), (int32_t)vocabulary, (int32_t)cols, dtype_of(dout), (int32_t)dtype, (int32_t)tokens.element_size(),
+                                 (float)ctx->saved_data["scale"].toDouble(), cols, cols};
+    const Tensor dweight = at::empty({vocabulary, cols}, dout.options().dtype(dtype == WERSA_F32 ? at::kFloat : at::kBFloat16)),
+                 ws = scratch((int64_t)embedding_workspace_bytes_fn(&d), dout);
+    check(embedding_backward_fn(&d, in(tokens), in(dout), out_of(dweight), out_of(ws), ws.nbytes(), stream(dout)));
+    return {Tensor(), dweight, Tensor(), Tensor()};
+  }
+};
+
+Tensor embedding(const Tensor &tokens, const Tensor &weight, double scale, int64_t dtype) {
+  pybind11::gil_scoped_release nogil;
+  return Embedding::apply(tokens, weight, scale, dtype);
+}
+
 variable_list layer_norm(const Tensor &x, const std::optional<Tensor> &weight, const std::optional<Tensor> &bias, const std::optional<Tensor> &residual,
                          double eps) {
   pybind11::gil_scoped_release nogil;
@@ -348,11 +458,21 @@ PYBIND11_MODULE(_wersa_torch, m) {
     norm_backward_fn = reinterpret_cast<decltype(norm_backward_fn)>(at[5]);
     norm_workspace_bytes_fn = reinterpret_cast<decltype(norm_workspace_bytes_fn)>(at[6]);
   });
-  m.def("bind_layer_norm", [](uintptr_t forward, uintptr_t backward, uintptr_t workspace_bytes) {
-    layer_forward_fn = reinterpret_cast<decltype(layer_forward_fn)>(forward);
-    layer_backward_fn = reinterpret_cast<decltype(layer_backward_fn)>(backward);
-    layer_workspace_bytes_fn = reinterpret_cast<decltype(layer_workspace_bytes_fn)>(workspace_bytes);
+  m.def("bind_decoder", [](const std::vector<uintptr_t> &at) {
+    TORCH_CHECK(at.size() == 10, "ten entry points");
+    layer_forward_fn = reinterpret_cast<decltype(layer_forward_fn)>(at[0]);
+    layer_backward_fn = reinterpret_cast<decltype(layer_backward_fn)>(at[1]);
+    layer_workspace_bytes_fn = reinterpret_cast<decltype(layer_workspace_bytes_fn)>(at[2]);
+    recurrence_forward_fn = reinterpret_cast<decltype(recurrence_forward_fn)>(at[3]);
+    recurrence_backward_fn = reinterpret_cast<decltype(recurrence_backward_fn)>(at[4]);
+    recurrence_workspace_bytes_fn = reinterpret_cast<decltype(recurrence_workspace_bytes_fn)>(at[5]);
+    recurrence_saved_bytes_fn = reinterpret_cast<decltype(recurrence_saved_bytes_fn)>(at[6]);
+    embedding_forward_fn = reinterpret_cast<decltype(embedding_forward_fn)>(at[7]);
+    embedding_backward_fn = reinterpret_cast<decltype(embedding_backward_fn)>(at[8]);
+    embedding_workspace_bytes_fn = reinterpret_cast<decltype(embedding_workspace_bytes_fn)>(at[9]);
   });
+  m.def("recurrence", &recurrence);
+  m.def("embedding", &embedding);
   m.def("layer_norm", &layer_norm);
   m.def("decay_attention", &decay_attention);
   m.def("rms_norm", &rms_norm);
