@@ -12,8 +12,8 @@ namespace {
 
 constexpr int kDigitBits = 9, kDigits = 1 << kDigitBits;
 constexpr int kSortThreads = 1024, kSortWaves = kSortThreads / 64;
-constexpr int kPiece = 32;            // sorted places of a piece
-constexpr int kFixBoundaries = 16;    // boundaries of pieces that a workgroup of the last step looks at
+constexpr int kRowsAhead = 2;         // rows of out that a thread has in flight
+constexpr size_t kCached = (size_t)256 << 20;   // bytes that the last-level cache holds: a larger dout, read once, is read past it
 constexpr int kClearRows = 16;        // rows that a workgroup of the clearing step looks at
 
 struct SortPlan {
@@ -34,6 +34,72 @@ SortPlan sort_plan(int64_t tokens, int vocabulary) {
   return p;
 }
 
+// A thread has four neighbouring columns, or two times four, so that rows of either type are read and written in whole lines.
+template <typename T> struct Quad { uint32_t u[sizeof(T)]; };
+template <typename T> struct __attribute__((packed, aligned(2))) AnyQuad { Quad<T> q; };
+typedef uint32_t words2 __attribute__((ext_vector_type(2), aligned(2)));
+typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(2)));
+template <typename T> __device__ __forceinline__ float value(const Quad<T> &q, int i) {
+  if (sizeof(T) == 4) return __uint_as_float(q.u[i]);
+  return __uint_as_float(i & 1 ? q.u[i / 2] & 0xffff0000u : q.u[i / 2] << 16);
+}
+template <bool PAST, typename T> __device__ __forceinline__ Quad<T> load_quad(const T *row, int col, int cols) {
+  Quad<T> q = {};
+  if (col + 4 <= cols) {
+    if constexpr (sizeof(T) == 4) {
+      const words4 *p = reinterpret_cast<const words4 *>(row + col);
+      const words4 v = PAST ? __builtin_nontemporal_load(p) : *p;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q.u[i] = v[i];
+    } else {
+      const words2 *p = reinterpret_cast<const words2 *>(row + col);
+      const words2 v = PAST ? __builtin_nontemporal_load(p) : *p;
+      q.u[0] = v[0], q.u[1] = v[1];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (col + i < cols) q.u[i * (int)sizeof(T) / 4] |= sizeof(T) == 4 ? __float_as_uint(ld(row + col + i)) : (__float_as_uint(ld(row + col + i)) >> 16) << 16 * (i & 1);
+  }
+  return q;
+}
+template <typename T> __device__ __forceinline__ void store_quad(T *row, int col, int cols, const float (&v)[4], float scale) {
+  if (col + 4 <= cols) {
+    if constexpr (sizeof(T) == 4) {
+      words4 w;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i] * scale);
+      *reinterpret_cast<words4 *>(row + col) = w;
+    } else {
+      words2 w;
+#pragma unroll
+      for (int i = 0; i < 2; ++i) w[i] = (uint32_t)f32_to_bf16(v[2 * i] * scale) | (uint32_t)f32_to_bf16(v[2 * i + 1] * scale) << 16;
+      *reinterpret_cast<words2 *>(row + col) = w;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (col + i < cols) st(row + col + i, v[i] * scale);
+  }
+}
+template <typename T> constexpr int kQuads = sizeof(T) == 4 ? 1 : 2;   // of a thread: 16 bytes of a row of out
+
+// Threads of a row: one for each 16 bytes of out, as a power of two, 8 at least and a workgroup at most.
+int lanes_of(const wersa_embedding_desc &c) {
+  const int64_t pieces = ((int64_t)c.cols * (c.dtype == WERSA_F32 ? 4 : 2) + 15) / 16;
+  int lanes = 8;
+  while (lanes < 256 && lanes < pieces) lanes *= 2;
+  return lanes;
+}
+// Sorted places of a piece: as many as leave two workgroups to a compute unit (longer pieces have fewer parts to join), between 8 and 128.
+int piece_of(const wersa_embedding_desc &c) {
+  const int lanes = lanes_of(c), e = c.dtype == WERSA_F32 ? 4 : 8;
+  const int64_t slabs = (c.cols + lanes * e - 1) / (lanes * e), each = c.tokens * lanes * slabs / (256 * 512);
+  int piece = 8;
+  while (piece < 128 && piece * 2 <= each) piece *= 2;
+  return piece;
+}
+
 struct Workspace {
   size_t count, counts, keys[2], places[2], partial, total;   // byte offsets
 };
@@ -49,7 +115,7 @@ Workspace workspace_of(const wersa_embedding_desc &c) {
   w.count = take(4);
   w.counts = take((size_t)p.tiles * kDigits * 4);
   for (int i = 0; i < 2; ++i) w.keys[i] = take((size_t)c.tokens * 4), w.places[i] = take((size_t)c.tokens * 4);
-  w.partial = take((size_t)((c.tokens + kPiece - 1) / kPiece) * 2 * c.cols * 4);
+  w.partial = take((size_t)((c.tokens + piece_of(c) - 1) / piece_of(c)) * 2 * c.cols * 4);
   w.total = at;
   return w;
 }
@@ -91,7 +157,7 @@ __global__ __launch_bounds__(kSortThreads) void embedding_count_kernel(Source s,
 __global__ __launch_bounds__(kSortThreads) void embedding_scatter_kernel(Source s, uint32_t *count, int64_t tokens, int64_t tile, int shift, int bits, const uint32_t *counts,
                                                                          uint32_t *keys, uint32_t *places) {
   __shared__ uint32_t start[kSortWaves][kDigits];
-  __shared__ uint32_t waves_sum[kSortWaves];
+  __shared__ uint32_t waves_sum[kSortWaves], counted[2][kSortThreads];
   const int digits = 1 << bits, wave = threadIdx.x / 64, lane = threadIdx.x & 63;
   for (int i = threadIdx.x; i < kSortWaves * kDigits; i += kSortThreads) (&start[0][0])[i] = 0;
   const int64_t n = s.keys ? (int64_t)*count : tokens;
@@ -101,15 +167,22 @@ __global__ __launch_bounds__(kSortThreads) void embedding_scatter_kernel(Source 
     uint32_t key, place;
     if (read_source(s, i, key, place)) atomicAdd(&start[wave][(key >> shift) & (digits - 1)], 1u);
   }
-  // of digit threadIdx.x: all places, and those of earlier tiles
+  // of each digit: all places, and those of earlier tiles, the tiles shared out among as many threads as there are for a digit
   uint32_t all = 0, before = 0;
-  if ((int)threadIdx.x < digits) {
+  {
+    const int digit = threadIdx.x & (digits - 1), shares = kSortThreads >> bits;
 #pragma unroll 8
-    for (int t = 0; t < (int)gridDim.x; ++t) {
-      const uint32_t c = counts[(int64_t)t * digits + threadIdx.x];
+    for (int t = threadIdx.x >> bits; t < (int)gridDim.x; t += shares) {
+      const uint32_t c = counts[(int64_t)t * digits + digit];
       all += c;
       before += t < (int)blockIdx.x ? c : 0;
     }
+    counted[0][threadIdx.x] = all;
+    counted[1][threadIdx.x] = before;
+    __syncthreads();
+    all = before = 0;
+    if ((int)threadIdx.x < digits)
+      for (int i = threadIdx.x; i < kSortThreads; i += digits) all += counted[0][i], before += counted[1][i];
   }
   uint32_t upto = all;
 #pragma unroll
@@ -174,118 +247,97 @@ struct SumJob {
   void *dweight;
   float *partial;            // [piece][2][cols]: of a token that began before the piece, of one that goes on behind it
   int64_t stride_out, stride_weight;
-  int cols, vocabulary;
+  int cols, vocabulary, piece;
   float scale;
 };
 
-template <typename T, int E> __device__ __forceinline__ void store_scaled(T *row, int col, int cols, const float (&v)[E], float scale) {
-#pragma unroll
-  for (int i0 = 0; i0 < E; i0 += 16 / (int)sizeof(T) < E ? 16 / (int)sizeof(T) : E) {
-    if constexpr (16 / (int)sizeof(T) <= E) {
-      float u[16 / sizeof(T)];
-#pragma unroll
-      for (int i = 0; i < 16 / (int)sizeof(T); ++i) u[i] = v[i0 + i] * scale;
-      store_piece<T, 16 / (int)sizeof(T)>(row, col + i0, cols, u);
-    } else {
-#pragma unroll
-      for (int i = 0; i < E; ++i)
-        if (col + i < cols) st(row + col + i, v[i] * scale);
-    }
-  }
-}
-
-// LANES threads to a piece, 16 bytes of a row of dout to a thread; blockIdx.z: further columns.
-template <typename T, typename W, int LANES>
+// LANES threads to a piece; blockIdx.z: further columns.  PAST: dout is more than the last-level cache holds.
+template <typename T, typename W, int LANES, bool PAST>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(SumJob a) {
-  constexpr int E = 16 / sizeof(T), AHEAD = 8;
-  const int64_t n = *a.count, piece = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / LANES) + threadIdx.x / LANES, begin = piece * kPiece, end = min(begin + kPiece, n);
-  const int col = (blockIdx.z * LANES + threadIdx.x % LANES) * E;
+  constexpr int Q = kQuads<T>, AHEAD = 8;
+  const int64_t n = *a.count, piece = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / LANES) + threadIdx.x / LANES, begin = piece * a.piece, end = min(begin + a.piece, n);
+  const int col = (blockIdx.z * LANES * Q + threadIdx.x % LANES) * 4;
   if (begin >= end || col >= a.cols) return;
-  float acc[E];
-#pragma unroll
-  for (int i = 0; i < E; ++i) acc[i] = 0.f;
+  float acc[Q][4] = {};
   uint32_t key = a.keys[begin];
   bool head = begin > 0 && a.keys[begin - 1] == key;
   const bool on = end < n && a.keys[end] == a.keys[end - 1];
   float *partial = a.partial + piece * 2 * a.cols;
+  const auto put = [&](bool tail) {
+#pragma unroll
+    for (int q = 0; q < Q; ++q) {
+      const int at = col + q * LANES * 4;
+      if (head) store_quad<float>(partial, at, a.cols, acc[q], 1.f);
+      else if (tail) store_quad<float>(partial + a.cols, at, a.cols, acc[q], 1.f);
+      else store_quad<W>((W *)a.dweight + (int64_t)key * a.stride_weight, at, a.cols, acc[q], a.scale);
+    }
+  };
   for (int64_t i0 = begin; i0 < end; i0 += AHEAD) {
     uint32_t k[AHEAD];
-    u32x4 row[AHEAD];
+    Quad<T> row[AHEAD][Q];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       const int64_t at = min(i0 + i, end - 1);
       k[i] = a.keys[at];
-      row[i] = load_raw((const T *)a.dout + (int64_t)a.places[at] * a.stride_out, col, a.cols);
+      const T *from = (const T *)a.dout + (int64_t)a.places[at] * a.stride_out;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) row[i][q] = load_quad<PAST, T>(from, col + q * LANES * 4, a.cols);
     }
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       if (i0 + i < end) {
         if (k[i] != key) {
-          if (head) store_scaled<float, E>(partial, col, a.cols, acc, 1.f);
-          else store_scaled<W, E>((W *)a.dweight + (int64_t)key * a.stride_weight, col, a.cols, acc, a.scale);
+          put(false);
           head = false;
           key = k[i];
 #pragma unroll
-          for (int j = 0; j < E; ++j) acc[j] = 0.f;
-        }
-        float v[E];
-        spread<T, E>(row[i], v);
+          for (int q = 0; q < Q; ++q)
 #pragma unroll
-        for (int j = 0; j < E; ++j) acc[j] += v[j];
+            for (int j = 0; j < 4; ++j) acc[q][j] = 0.f;
+        }
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[q][j] += value(row[i][q], j);
       }
     }
   }
-  if (head) store_scaled<float, E>(partial, col, a.cols, acc, 1.f);
-  else if (on) store_scaled<float, E>(partial + a.cols, col, a.cols, acc, 1.f);
-  else store_scaled<W, E>((W *)a.dweight + (int64_t)key * a.stride_weight, col, a.cols, acc, a.scale);
+  put(on);
 }
 
-// Tokens that go on over boundaries of pieces, each at its first such boundary: the parts in the order of the pieces, four waves a quarter each.
+// Tokens that go on over boundaries of pieces, each at its first such boundary, a wave to a boundary and 256 columns: the parts in the order of the pieces.
 template <typename W>
 __global__ __launch_bounds__(256) void embedding_join_kernel(SumJob a) {
-  __shared__ float sums[4][4][64];
-  const int64_t n = *a.count;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x / 64, col = (blockIdx.y * 64 + lane) * 4;
-  const int64_t p0 = (int64_t)blockIdx.x * kFixBoundaries + 1;
-  bool mine = false;
-  if (lane < kFixBoundaries && (p0 + lane) * kPiece < n) {
-    const int64_t at = (p0 + lane) * kPiece;
-    const uint32_t key = a.keys[at];
-    mine = a.keys[at - 1] == key && (at == kPiece || a.keys[at - kPiece - 1] != key);
+  constexpr int AHEAD = 16;
+  const int64_t n = *a.count, p = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 4 + threadIdx.x / 64 + 1, at = p * a.piece;
+  const int lane = threadIdx.x & 63, col = (blockIdx.z * 64 + lane) * 4;
+  if (at >= n) return;
+  const uint32_t key = a.keys[at];
+  if (a.keys[at - 1] != key || (at > a.piece && a.keys[at - a.piece - 1] == key)) return;
+  int64_t parts = 1;   // the tail of piece p - 1 and the heads of p, p + 1 ... as far as the token goes
+  for (bool more = true; more;) {
+    const int64_t next = at + (parts - 1 + lane) * a.piece;
+    const uint64_t same = __ballot(next < n && a.keys[next < n ? next : at] == key);
+    parts += same == ~0ull ? 64 : __ffsll((unsigned long long)~same) - 1;
+    more = same == ~0ull;
   }
-  for (uint64_t todo = __ballot(mine); todo; todo &= todo - 1) {   // (every wave has the same)
-    const int64_t p = p0 + (__ffsll((unsigned long long)todo) - 1);
-    const uint32_t key = a.keys[p * kPiece];
-    const int64_t last = (lower_bound(a.keys, n, key + 1) - 1) / kPiece, parts = last - p + 2;   // the tail of piece p - 1 and the heads of p .. last
-    const int64_t from = parts * wave / 4, to = parts * (wave + 1) / 4;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-    for (int64_t i0 = from; i0 < to; i0 += 8) {
-      u32x4 row[8];
+  float acc[4] = {0.f, 0.f, 0.f, 0.f};
+  for (int64_t i0 = 0; i0 < parts; i0 += AHEAD) {
+    Quad<float> row[AHEAD];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int64_t at = min(i0 + i, to - 1);
-        row[i] = load_raw(a.partial + (at == 0 ? (p - 1) * 2 + 1 : (p - 1 + at) * 2) * a.cols, col, a.cols);
-      }
+    for (int i = 0; i < AHEAD; ++i) {
+      const int64_t part = min(i0 + i, parts - 1);
+      row[i] = load_quad<false, float>(a.partial + (part == 0 ? (p - 1) * 2 + 1 : (p - 1 + part) * 2) * a.cols, col, a.cols);
+    }
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (i0 + i < to) {
-          float v[4];
-          spread<float, 4>(row[i], v);
+    for (int i = 0; i < AHEAD; ++i) {
+      if (i0 + i < parts) {
 #pragma unroll
-          for (int j = 0; j < 4; ++j) acc[j] += v[j];
-        }
+        for (int j = 0; j < 4; ++j) acc[j] += value(row[i], j);
       }
     }
-    __syncthreads();
-#pragma unroll
-    for (int j = 0; j < 4; ++j) sums[wave][j][lane] = acc[j];
-    __syncthreads();
-    if (wave == 0 && col < a.cols) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j] = (sums[0][j][lane] + sums[1][j][lane]) + (sums[2][j][lane] + sums[3][j][lane]);
-      store_scaled<W, 4>((W *)a.dweight + (int64_t)key * a.stride_weight, col, a.cols, acc, a.scale);
-    }
   }
+  store_quad<W>((W *)a.dweight + (int64_t)key * a.stride_weight, col, a.cols, acc, a.scale);
 }
 
 // Rows of dweight whose token is nowhere: zeros.
@@ -313,33 +365,31 @@ __global__ __launch_bounds__(256) void embedding_clear_kernel(SumJob a) {
       for (int col = threadIdx.x * E; col < a.cols; col += 256 * E) store_piece<W, E>((W *)a.dweight + (row0 + r) * a.stride_weight, col, a.cols, zeros);
 }
 
-// LANES threads to a row of out.
+// LANES threads to a row of out, kRowsAhead rows to a thread.
 template <typename T, typename W, int LANES>
 __global__ __launch_bounds__(256) void embedding_kernel(Source s, const void *weight, void *out, int64_t tokens, int64_t stride_weight, int64_t stride_out, int cols, float scale) {
-  constexpr int E = 16 / sizeof(T), EW = 16 / (int)sizeof(W);
-  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / LANES) + threadIdx.x / LANES;
-  if (row >= tokens) return;
-  uint32_t key, place;
-  const bool have = read_source(s, row, key, place);
-  const W *from = (const W *)weight + (have ? (int64_t)key : 0) * stride_weight;
-  T *to = (T *)out + row * stride_out;
-  for (int col = (threadIdx.x % LANES) * E; col < cols; col += LANES * E) {
-    float v[E];
-    if constexpr (EW <= E) {
+  constexpr int Q = kQuads<T>, GROUPS = 256 / LANES;
+  const int64_t row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (GROUPS * kRowsAhead) + threadIdx.x / LANES;
+  uint32_t key[kRowsAhead], place;
+  bool have[kRowsAhead];
 #pragma unroll
-      for (int i0 = 0; i0 < E; i0 += EW) {
-        float u[EW];
-        load_piece<W, EW>(from, col + i0, have ? cols : 0, u);
+  for (int r = 0; r < kRowsAhead; ++r) have[r] = row0 + r * GROUPS < tokens && read_source(s, row0 + r * GROUPS, key[r], place);
+  for (int col = threadIdx.x % LANES * 4; col < cols; col += LANES * Q * 4) {
+    Quad<W> q[kRowsAhead][Q];
 #pragma unroll
-        for (int i = 0; i < EW; ++i) v[i0 + i] = u[i];
+    for (int r = 0; r < kRowsAhead; ++r)
+#pragma unroll
+      for (int i = 0; i < Q; ++i)
+        q[r][i] = load_quad<false, W>((const W *)weight + (have[r] ? (int64_t)key[r] : 0) * stride_weight, col + i * LANES * 4, have[r] ? cols : 0);
+#pragma unroll
+    for (int r = 0; r < kRowsAhead; ++r)
+#pragma unroll
+      for (int i = 0; i < Q; ++i) {
+        float v[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = have[r] ? value(q[r][i], j) : 0.f;
+        if (row0 + r * GROUPS < tokens) store_quad<T>((T *)out + (row0 + r * GROUPS) * stride_out, col + i * LANES * 4, cols, v, have[r] ? scale : 1.f);
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < E; ++i) v[i] = have && col + i < cols ? ld(from + col + i) : 0.f;
-    }
-#pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = have ? v[i] * scale : 0.f;
-    store_piece<T, E>(to, col, cols, v);
   }
 }
 
@@ -354,16 +404,17 @@ wersa_status validate(const wersa_embedding_desc *c) {
   return WERSA_OK;
 }
 
-// Types of out and of the weights, and the threads of a row: one for each 16 bytes, as a power of two, 8 at least and a workgroup at most.
+// Types of out and of the weights, and the threads of a row.
 template <typename F> void by_types(const wersa_embedding_desc &c, F f) {
   auto lanes = [&](auto *t, auto *w) {
-    const int pieces = (int)(((int64_t)c.cols * sizeof(*t) + 15) / 16);
-    if (pieces <= 8) f(t, w, std::integral_constant<int, 8>{});
-    else if (pieces <= 16) f(t, w, std::integral_constant<int, 16>{});
-    else if (pieces <= 32) f(t, w, std::integral_constant<int, 32>{});
-    else if (pieces <= 64) f(t, w, std::integral_constant<int, 64>{});
-    else if (pieces <= 128) f(t, w, std::integral_constant<int, 128>{});
-    else f(t, w, std::integral_constant<int, 256>{});
+    switch (lanes_of(c)) {
+      case 8: return f(t, w, std::integral_constant<int, 8>{});
+      case 16: return f(t, w, std::integral_constant<int, 16>{});
+      case 32: return f(t, w, std::integral_constant<int, 32>{});
+      case 64: return f(t, w, std::integral_constant<int, 64>{});
+      case 128: return f(t, w, std::integral_constant<int, 128>{});
+      default: return f(t, w, std::integral_constant<int, 256>{});
+    }
   };
   float *f32 = nullptr;
   bf16_t *b16 = nullptr;
@@ -389,7 +440,7 @@ wersa_status wersa_embedding_forward(const wersa_embedding_desc *desc, const voi
     typedef typename std::remove_pointer<decltype(t)>::type T;
     typedef typename std::remove_pointer<decltype(w)>::type W;
     constexpr int L = decltype(lanes)::value;
-    WERSA_STAGE("wersa_embedding", st, (embedding_kernel<T, W, L><<<grid_of((desc->tokens + 256 / L - 1) / (256 / L)), 256, 0, st>>>(
+    WERSA_STAGE("wersa_embedding", st, (embedding_kernel<T, W, L><<<grid_of((desc->tokens + 256 / L * kRowsAhead - 1) / (256 / L * kRowsAhead)), 256, 0, st>>>(
         s, weight, out, desc->tokens, desc->stride_weight, desc->stride_out, desc->cols, desc->scale)));
   });
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
@@ -415,20 +466,23 @@ wersa_status wersa_embedding_backward(const wersa_embedding_desc *desc, const vo
     WERSA_STAGE("wersa_embedding_scatter", st, (embedding_scatter_kernel<<<p.tiles, kSortThreads, 0, st>>>(s, count, desc->tokens, p.tile, pass * p.bits, p.bits, counts, keys, places)));
     s.keys = keys, s.places = places;
   }
-  const SumJob a{count, s.keys, s.places, dout, dweight, (float *)(ws + at.partial), desc->stride_out, desc->stride_weight, desc->cols, desc->vocabulary, desc->scale};
+  const SumJob a{count, s.keys, s.places, dout, dweight, (float *)(ws + at.partial), desc->stride_out, desc->stride_weight, desc->cols, desc->vocabulary, piece_of(*desc), desc->scale};
   by_types(*desc, [&](auto *t, auto *w, auto lanes) {
     typedef typename std::remove_pointer<decltype(t)>::type T;
     typedef typename std::remove_pointer<decltype(w)>::type W;
-    constexpr int L = decltype(lanes)::value, E = 16 / sizeof(T);
+    constexpr int L = decltype(lanes)::value, E = 4 * kQuads<T>;
     WERSA_STAGE("wersa_embedding_clear", st, (embedding_clear_kernel<W><<<grid_of(((int64_t)desc->vocabulary + kClearRows - 1) / kClearRows), 256, 0, st>>>(a)));
     if (desc->tokens == 0) return;
-    const int64_t pieces = (desc->tokens + kPiece - 1) / kPiece;
+    const int64_t pieces = (desc->tokens + a.piece - 1) / a.piece;
     dim3 grid = grid_of((pieces + 256 / L - 1) / (256 / L));
     grid.z = (desc->cols + L * E - 1) / (L * E);
-    WERSA_STAGE("wersa_embedding_sum", st, (embedding_sum_kernel<T, W, L><<<grid, 256, 0, st>>>(a)));
-    if (pieces > 1)
-      WERSA_STAGE("wersa_embedding_join", st,
-                  (embedding_join_kernel<W><<<dim3((unsigned)((pieces - 2) / kFixBoundaries + 1), (desc->cols + 255) / 256), 256, 0, st>>>(a)));
+    const auto sum = (size_t)desc->tokens * desc->cols * sizeof(T) > kCached ? embedding_sum_kernel<T, W, L, true> : embedding_sum_kernel<T, W, L, false>;
+    WERSA_STAGE("wersa_embedding_sum", st, (sum<<<grid, 256, 0, st>>>(a)));
+    if (pieces > 1) {
+      dim3 joins = grid_of((pieces - 1 + 3) / 4);
+      joins.z = (desc->cols + 255) / 256;
+      WERSA_STAGE("wersa_embedding_join", st, (embedding_join_kernel<W><<<joins, 256, 0, st>>>(a)));
+    }
   });
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }

@@ -15,6 +15,9 @@ constexpr int kMostBiases = 1023, kMostHistory = (1 << 21) - 1;
 constexpr uint32_t kCount = kMostHistory, kPrompt = 1u << 21;
 constexpr int kBiasShift = 22;
 
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 struct LogitsJob {
   const void *logits;
   void *out;
@@ -25,71 +28,111 @@ struct LogitsJob {
   int vocabulary, history_rows, history_most, biases;
 };
 
+// Dynamic LDS: the words of the tile, and where there are biases their tokens, values and sums.  What memory gives is requested before the first of it is waited for.
 template <typename T>
-__global__ __launch_bounds__(kThreads) void logits_kernel(LogitsJob a) {
-  constexpr int E = 16 / sizeof(T);
-  __shared__ __attribute__((aligned(16))) uint32_t words[kTile];
-  __shared__ int32_t bias_token[kMostBiases + 1];
-  __shared__ float bias_value[kMostBiases + 1];
+__global__ __launch_bounds__(kThreads, 8) void logits_kernel(LogitsJob a) {
+  constexpr int E = 16 / sizeof(T), PIECES = kTile / (kThreads * E), AHEAD = 8;
+  extern __shared__ __attribute__((aligned(16))) uint32_t lds[];
+  uint32_t *words = lds;
+  int32_t *bias_token = (int32_t *)(lds + kTile);
+  const int slots_of_bias = (a.biases + 3) / 4 * 4;
+  float *bias_value = (float *)(bias_token + slots_of_bias), *bias_sum = bias_value + slots_of_bias;
   const int row = blockIdx.y, v0 = blockIdx.x * kTile, here = min(kTile, a.vocabulary - v0);
   const T *logits = (const T *)a.logits + row * a.stride_logits + v0;
   T *out = (T *)a.out + row * a.stride_out + v0;
   const bool changed = a.history || a.biases > 0;
-  if (changed) {
-    for (int i = threadIdx.x; i < kTile / 4; i += kThreads) reinterpret_cast<u32x4 *>(words)[i] = u32x4{0, 0, 0, 0};
-    for (int i = threadIdx.x; i < a.biases; i += kThreads) bias_token[i] = a.bias_tokens[row * a.stride_bias + i];
-    __syncthreads();
-  }
+  const int32_t *history = nullptr;
+  int length = 0, prompt = 0;
   if (a.history) {
     const int64_t at = a.slots ? (int64_t)a.slots[row] : row;
     if (at >= 0 && at < a.history_rows) {
-      const int32_t *history = a.history + at * a.stride_history;
-      const int length = min(max(a.lengths[at], 0), a.history_most), prompt = a.prompts ? a.prompts[at] : 0;
-#pragma unroll 4
-      for (int i = threadIdx.x; i < length; i += kThreads) {
-        const uint32_t v = (uint32_t)history[i] - (uint32_t)v0;
-        if (v < (uint32_t)here) {
-          if (i < prompt) atomicOr(&words[v], kPrompt);
-          else atomicAdd(&words[v], 1u);
-        }
-      }
+      history = a.history + at * a.stride_history;
+      length = min(max(a.lengths[at], 0), a.history_most);
+      prompt = a.prompts ? a.prompts[at] : 0;
     }
+  }
+  int32_t said[AHEAD];
+#pragma unroll
+  for (int k = 0; k < AHEAD; ++k) said[k] = (int)threadIdx.x + k * kThreads < length ? history[threadIdx.x + k * kThreads] : -1;
+  u32x4 raw[PIECES];
+  uint32_t allowed[PIECES];
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    const int col = (threadIdx.x + p * kThreads) * E;
+    raw[p] = load_raw(logits, col, here);
+    allowed[p] = a.mask && col < here ? a.mask[row * a.stride_mask + (v0 + col) / 32] >> ((v0 + col) & 31) : ~0u;
+  }
+  if (changed) {
+    for (int i = threadIdx.x; i < kTile / 4; i += kThreads) reinterpret_cast<u32x4 *>(words)[i] = u32x4{0, 0, 0, 0};
+    for (int i = threadIdx.x; i < slots_of_bias; i += kThreads) {
+      bias_token[i] = i < a.biases ? a.bias_tokens[row * a.stride_bias + i] : -1;
+      bias_value[i] = i < a.biases ? a.bias_values[row * a.stride_bias + i] : 0.f;
+    }
+    __syncthreads();
+    const auto count = [&](int i, int32_t token) {
+      const uint32_t v = (uint32_t)token - (uint32_t)v0;
+      if (v < (uint32_t)here) {
+        if (i < prompt) atomicOr(&words[v], kPrompt);
+        else atomicAdd(&words[v], 1u);
+      }
+    };
+#pragma unroll
+    for (int k = 0; k < AHEAD; ++k) count(threadIdx.x + k * kThreads, said[k]);   // (-1 is in no tile)
+#pragma unroll 4
+    for (int i = threadIdx.x + AHEAD * kThreads; i < length; i += kThreads) count(i, history[i]);
   }
   if (a.biases > 0) {   // a token's biases are added up by its first one, in their order
     __syncthreads();
     for (int i = threadIdx.x; i < a.biases; i += kThreads) {
-      const uint32_t v = (uint32_t)bias_token[i] - (uint32_t)v0;
-      bool first = v < (uint32_t)here;
-      for (int j = 0; j < i && first; ++j) first = bias_token[j] != bias_token[i];
+      const int token = bias_token[i];
+      const uint32_t v = (uint32_t)token - (uint32_t)v0;
+      if (v >= (uint32_t)here) continue;
+      bool first = true;
+      float sum = 0.f;
+#pragma unroll 4
+      for (int j0 = 0; j0 < a.biases; j0 += 4) {
+        const i32x4 t = *reinterpret_cast<const i32x4 *>(bias_token + j0);
+        const f32x4 b = *reinterpret_cast<const f32x4 *>(bias_value + j0);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          if (t[k] == token) {
+            first &= j0 + k >= i;
+            sum += b[k];
+          }
+        }
+      }
       if (first) {
-        float sum = 0.f;
-        for (int j = i; j < a.biases; ++j)
-          if (bias_token[j] == bias_token[i]) sum += a.bias_values[row * a.stride_bias + j];
-        bias_value[i + 1] = sum;
+        bias_sum[i] = sum;
         words[v] |= (uint32_t)(i + 1) << kBiasShift;   // (nobody else writes words now)
       }
     }
   }
   if (changed) __syncthreads();
   const float repetition = a.repetition ? a.repetition[row] : 1.f, presence = a.presence ? a.presence[row] : 0.f, frequency = a.frequency ? a.frequency[row] : 0.f;
-  for (int col = threadIdx.x * E; col < here; col += kThreads * E) {
+#pragma unroll
+  for (int p = 0; p < PIECES; ++p) {
+    const int col = (threadIdx.x + p * kThreads) * E;
     float z[E];
-    load_piece<T, E>(logits, col, here, z);
-    uint32_t allowed = ~0u;
-    if (a.mask) allowed = a.mask[row * a.stride_mask + (v0 + col) / 32] >> ((v0 + col) & 31);
-    uint32_t word[E];
+    spread<T, E>(raw[p], z);
+    if (changed) {
+      uint32_t word[E], any = 0;
 #pragma unroll
-    for (int i = 0; i < E; ++i) word[i] = changed ? words[col + i] : 0;
+      for (int i = 0; i < E; ++i) any |= word[i] = words[col + i];
+      if (any) {
 #pragma unroll
-    for (int i = 0; i < E; ++i) {
-      if (word[i] & (kCount | kPrompt)) {
-        const float count = (float)(word[i] & kCount);
-        z[i] = z[i] > 0.f ? z[i] / repetition : z[i] * repetition;
-        z[i] -= frequency * count + (count > 0.f ? presence : 0.f);
+        for (int i = 0; i < E; ++i) {
+          if (word[i] & (kCount | kPrompt)) {
+            const float count = (float)(word[i] & kCount);
+            z[i] = z[i] > 0.f ? z[i] / repetition : z[i] * repetition;
+            z[i] -= frequency * count + (count > 0.f ? presence : 0.f);
+          }
+          if (word[i] >> kBiasShift) z[i] += bias_sum[(word[i] >> kBiasShift) - 1];
+        }
       }
-      if (word[i] >> kBiasShift) z[i] += bias_value[word[i] >> kBiasShift];
-      if (!(allowed >> i & 1)) z[i] = -__builtin_huge_valf();
     }
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (!(allowed[p] >> i & 1)) z[i] = -__builtin_huge_valf();
     store_piece<T, E>(out, col, here, z);
   }
 }
@@ -123,8 +166,9 @@ wersa_status wersa_logits_adjust(const wersa_logits_desc *desc, const void *logi
                     desc->vocabulary, desc->history_rows, desc->history_most, desc->biases};
   hipStream_t st = (hipStream_t)hip_stream;
   const dim3 grid((desc->vocabulary - 1) / kTile + 1, desc->B);
-  if (desc->dtype == WERSA_F32) WERSA_STAGE("wersa_logits", st, (logits_kernel<float><<<grid, kThreads, 0, st>>>(a)));
-  else WERSA_STAGE("wersa_logits", st, (logits_kernel<bf16_t><<<grid, kThreads, 0, st>>>(a)));
+  const size_t lds = (history || desc->biases > 0 ? kTile * 4 : 0) + (size_t)(desc->biases + 3) / 4 * 4 * 12;   // below 45 KB
+  if (desc->dtype == WERSA_F32) WERSA_STAGE("wersa_logits", st, (logits_kernel<float><<<grid, kThreads, lds, st>>>(a)));
+  else WERSA_STAGE("wersa_logits", st, (logits_kernel<bf16_t><<<grid, kThreads, lds, st>>>(a)));
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
 
