@@ -1,12 +1,14 @@
 """A small decoder of linear-time layers: what the causal operators are for, together.
 
-    python -m paper_2507_08637_amd.decoder [--steps 200] [--eight-bit]
+    python -m paper_2507_08637_amd.decoder [--steps 200] [--eight-bit] [--mixing decay,recurrence] [--norm layer] [--repetition 1.3]
 
 trains it on sequences of two tokens that take turns, takes a batch of packed prompts of unequal lengths into a cache of states
 and goes on token by token, for a prompt's length no more than for any other.  A layer is
     h, r = norm(x + r);  q, k, v = h Wqkv;  x = norm_per_head(decay attention(q, k, v)) Wo
     h, r = norm(x + r);  x = silu(h Wup) Wdown
-with the residual stream r added where it is normed next.  The decays are fixed: memories from 8 tokens to 1024.
+with the residual stream r added where it is normed next.  The decays are fixed: memories from 8 tokens to 1024.  A layer whose mixing is the gated recurrence has
+    v, g = h Wvg + (0, bias);  x = recurrence(v, g) Wo
+in their place, with a memory for each channel that the tokens choose; its biases begin at the same range.  norm: "rms", or "layer" with a bias.
 Products with weights are torch's; with eight_bit, serving has the norms leave 8 bits with a scale for each row, and the
 weights in 8 bits with a scale for each column.
 """
@@ -18,48 +20,79 @@ from . import autograd, binding
 
 
 class Decoder(torch.nn.Module):
-    def __init__(self, vocabulary=64, hidden=256, heads=4, layers=2, dtype=torch.bfloat16, device="cuda"):
+    def __init__(self, vocabulary=64, hidden=256, heads=4, layers=2, dtype=torch.bfloat16, device="cuda", mixing="decay", norm="rms"):
+        """mixing: "decay" or "recurrence", or one of them for each layer (they take turns where there are fewer than layers)."""
         super().__init__()
-        self.heads, self.width, self.hidden, self.dtype = heads, hidden // heads, hidden, dtype
+        kinds = (mixing,) if isinstance(mixing, str) else tuple(mixing)
+        assert kinds and set(kinds) <= {"decay", "recurrence"}, "mixing is decay, recurrence, or a list of these"
+        assert norm in ("rms", "layer"), "norm is rms or layer"
+        self.heads, self.width, self.hidden, self.dtype, self.norm = heads, hidden // heads, hidden, dtype, norm
         param = lambda *shape, scale=1.0: torch.nn.Parameter(scale * torch.randn(*shape, device=device))
-        ones = lambda: torch.nn.Parameter(torch.ones(hidden, device=device))
+        ones, zeros = (lambda f=f: torch.nn.Parameter(f(hidden, device=device)) for f in (torch.ones, torch.zeros))
         self.embedding = param(vocabulary, hidden)
         self.layers = torch.nn.ModuleList()
-        for _ in range(layers):
+        for i in range(layers):
             layer = torch.nn.Module()
+            layer.mixing = kinds[i % len(kinds)]
             layer.norm_mix, layer.norm_mlp = ones(), ones()
-            layer.qkv, layer.out = param(hidden, 3 * hidden, scale=hidden ** -0.5), param(hidden, hidden, scale=hidden ** -0.5)
+            if norm == "layer":
+                layer.norm_mix_bias, layer.norm_mlp_bias = zeros(), zeros()
+            if layer.mixing == "recurrence":
+                layer.gate_bias = torch.nn.Parameter(torch.linspace(3, 10, hidden, device=device) * 0.6931)
+            layer.qkv, layer.out = param(hidden, (3 if layer.mixing == "decay" else 2) * hidden, scale=hidden ** -0.5), param(hidden, hidden, scale=hidden ** -0.5)
             layer.up, layer.down = param(hidden, 2 * hidden, scale=hidden ** -0.5), param(2 * hidden, hidden, scale=(2 * hidden) ** -0.5)
             self.layers.append(layer)
         self.norm_last, self.head = ones(), param(hidden, vocabulary, scale=hidden ** -0.5)
+        if norm == "layer":
+            self.norm_last_bias = zeros()
         memory = torch.exp2(3 + 7 * torch.arange(heads, device=device) / max(1, heads - 1))
         self.register_buffer("log_decay", torch.log1p(-1 / memory))
 
     def cache(self, slots):
         """States of `slots` sequences, for each layer."""
-        return [torch.zeros(slots, self.heads, self.width, self.width, device=self.log_decay.device) for _ in self.layers]
+        shape = {"decay": (self.heads, self.width, self.width), "recurrence": (self.hidden,)}
+        return [torch.zeros(slots, *shape[layer.mixing], device=self.log_decay.device) for layer in self.layers]
 
     def _heads(self, qkv):
         """(B, n, 3 hidden) as q, k, v (B, heads, n, width), by stride."""
         return qkv.unflatten(-1, (3, self.heads, self.width)).permute(2, 0, 3, 1, 4).unbind(0)
 
+    def _gates(self, layer, both):
+        """(..., 2 hidden) as values and gates."""
+        v, g = both.split(self.hidden, -1)
+        return v, g + layer.gate_bias.to(self.dtype)
+
     # ---- training: whole sequences, all of them at once
+    def _train_norm(self, x, module, name, r):
+        weight = getattr(module, name)
+        if self.norm == "layer":
+            out = autograd.wersa_layer_norm(x, weight, getattr(module, name + "_bias"), residual=r)
+        else:
+            out = autograd.wersa_rms_norm(x, weight, residual=r)
+        return (out, x) if r is None else out
+
     def forward(self, tokens):
         """(B, n) -> logits (B, n, vocabulary)."""
-        x, r = self.embedding[tokens].to(self.dtype), None
+        x, r = autograd.wersa_embedding(tokens, self.embedding, dtype=self.dtype), None
         for layer in self.layers:
-            h, r = (autograd.wersa_rms_norm(x, layer.norm_mix), x) if r is None else autograd.wersa_rms_norm(x, layer.norm_mix, residual=r)
-            o, _ = autograd.wersa_decay_attention(*self._heads(h @ layer.qkv.to(self.dtype)), self.log_decay)
-            o = autograd.wersa_rms_norm(o.transpose(1, 2)).flatten(2)
-            h, r = autograd.wersa_rms_norm(o @ layer.out.to(self.dtype), layer.norm_mlp, residual=r)
+            h, r = self._train_norm(x, layer, "norm_mix", r)
+            h = h @ layer.qkv.to(self.dtype)
+            if layer.mixing == "recurrence":
+                o, _ = autograd.wersa_recurrence(*self._gates(layer, h))
+            else:
+                o, _ = autograd.wersa_decay_attention(*self._heads(h), self.log_decay)
+                o = autograd.wersa_rms_norm(o.transpose(1, 2)).flatten(2)
+            h, r = self._train_norm(o @ layer.out.to(self.dtype), layer, "norm_mlp", r)
             x = torch.nn.functional.silu(h @ layer.up.to(self.dtype)) @ layer.down.to(self.dtype)
-        h, r = autograd.wersa_rms_norm(x, self.norm_last, residual=r)
+        h, r = self._train_norm(x, self, "norm_last", r)
         return (h @ self.head.to(self.dtype)).float()
 
     # ---- serving: the weights laid out once, a cache of states, prompts and then tokens
     @torch.no_grad()
     def serving(self, eight_bit=False):
         """The weights as prefill() and step() take them: in the model's type, and those that follow a norm of the stream with eight_bit in 8 bits, a scale for each column."""
+        assert not eight_bit or self.norm == "rms", "the layer norm does not leave 8 bits"
+
         def after_norm(w):
             if not eight_bit:
                 return w.to(self.dtype), None
@@ -69,33 +102,43 @@ class Decoder(torch.nn.Module):
         return ([dict(qkv=after_norm(x.qkv), out=x.out.to(self.dtype), up=after_norm(x.up), down=x.down.to(self.dtype)) for x in self.layers],
                 after_norm(self.head))
 
-    def _normed(self, x, weight, r, w):
+    def _normed(self, x, module, name, r, w):
         """norm(x + r) times w, and the stream."""
-        w, scale = w
+        (w, scale), weight = w, getattr(module, name)
+        if self.norm == "layer":
+            y, r, _ = binding.wersa_layer_norm_forward(x, weight, getattr(module, name + "_bias"), residual=r)
+            return y @ w, r
         if scale is None:
             y, r, _ = binding.wersa_rms_norm_forward(x, weight, residual=r)
             return y @ w, r
         y, r, rows = binding.wersa_rms_norm_eight_bit(x, weight, residual=r)
         return torch._scaled_mm(y, w, scale_a=rows[:, None], scale_b=scale, out_dtype=self.dtype), r
 
-    def _serve(self, tokens, weights, attend):
-        """Logits (rows, vocabulary) of rows of tokens; attend(layer's number, q, k, v (1, heads, rows, width)) gives (1, heads, rows, width)."""
+    def _serve(self, tokens, weights, attend, recur):
+        """Logits (rows, vocabulary) of rows of tokens; attend(layer's number, q, k, v (1, heads, rows, width)) gives (1, heads, rows, width), recur(layer's number,
+        values, gates (rows, hidden)) gives (rows, hidden)."""
         layers, head = weights
-        x, r = self.embedding[tokens].to(self.dtype), None
+        x, r = binding.wersa_embedding_forward(tokens, self.embedding, dtype=self.dtype), None
         for i, (layer, w) in enumerate(zip(self.layers, layers)):
-            qkv, r = self._normed(x, layer.norm_mix, r, w["qkv"])
-            o = attend(i, *self._heads(qkv[None]))
-            o, _, _ = binding.wersa_rms_norm_forward(o.transpose(1, 2).reshape(-1, self.width))
-            h, r = self._normed(o.view(-1, self.hidden) @ w["out"], layer.norm_mlp, r, w["up"])
+            mixed, r = self._normed(x, layer, "norm_mix", r, w["qkv"])
+            if layer.mixing == "recurrence":
+                o = recur(i, *self._gates(layer, mixed))
+            else:
+                o = attend(i, *self._heads(mixed[None]))
+                o, _, _ = binding.wersa_rms_norm_forward(o.transpose(1, 2).reshape(-1, self.width))
+            h, r = self._normed(o.view(-1, self.hidden) @ w["out"], layer, "norm_mlp", r, w["up"])
             x = torch.nn.functional.silu(h) @ w["down"]
-        return self._normed(x, self.norm_last, r, head)[0].float()
+        return self._normed(x, self, "norm_last", r, head)[0].float()
 
     @torch.no_grad()
     def prefill(self, tokens, offsets, cache, slots, weights):
         """Prompts one behind the other: tokens (all), offsets (prompts + 1) and slots (prompts) int32.  Leaves their states in the cache; logits of every token."""
         def attend(i, q, k, v):
             return binding.wersa_decay_forward(q, k, v, self.log_decay, offsets=offsets, final_state=cache[i], slots=slots)[0]
-        return self._serve(tokens, weights, attend)
+
+        def recur(i, v, g):
+            return binding.wersa_recurrence_forward(v[None], g[None], offsets=offsets, final_state=cache[i], slots=slots)[0][0]
+        return self._serve(tokens, weights, attend, recur)
 
     @torch.no_grad()
     def step(self, tokens, cache, slots, weights):
@@ -103,7 +146,10 @@ class Decoder(torch.nn.Module):
         def attend(i, q, k, v):
             q, k, v = (x[0].transpose(0, 1) for x in (q, k, v))
             return binding.wersa_decay_step(q, k, v, self.log_decay, cache[i], slots=slots).transpose(0, 1)[None]
-        return self._serve(tokens, weights, attend)
+
+        def recur(i, v, g):
+            return binding.wersa_recurrence_step(v, g, cache[i], slots=slots)
+        return self._serve(tokens, weights, attend, recur)
 
 
 def batch(sequences, n, vocabulary, period, generator):
@@ -129,18 +175,41 @@ def train(model, steps, sequences=16, n=128, period=2, seed=0, report=None):
     return losses
 
 
-def generate(model, prompts, tokens, eight_bit=False):
-    """The most likely continuation, `tokens` long, of each prompt (a list of 1-D tensors): (prompts, tokens)."""
+def generate(model, prompts, tokens, eight_bit=False, repetition=1.0, presence=0.0, frequency=0.0, biases=None, allowed=None):
+    """The most likely continuation, `tokens` long, of each prompt (a list of 1-D tensors): (prompts, tokens).  repetition, presence, frequency: penalties for tokens that were
+    there before (the latter two: in the continuation); biases: {token: what is added to its logit}; allowed(step): the mask of the tokens that may come at a step, 32 to a
+    word, for all prompts or for each (None: any)."""
     assert prompts and all(len(p) > 0 for p in prompts), "a prompt has at least one token to go on from"
     device, B = model.log_decay.device, len(prompts)
     lengths = torch.tensor([len(p) for p in prompts])
     offsets = torch.cat([torch.zeros(1, dtype=torch.long), lengths.cumsum(0)]).to(torch.int32).to(device)
     slots = torch.arange(B, dtype=torch.int32, device=device)
     weights, cache = model.serving(eight_bit), model.cache(B)
-    logits = model.prefill(torch.cat(prompts), offsets, cache, slots, weights)[offsets[1:].long() - 1]
-    out = [logits.argmax(1)]
-    for _ in range(tokens - 1):
-        out.append(model.step(out[-1], cache, slots, weights).argmax(1))
+    adjust = {}
+    if repetition != 1 or presence or frequency:
+        history = torch.zeros(B, int(lengths.max()) + tokens, dtype=torch.int32, device=device)
+        for row, prompt in zip(history, prompts):
+            row[:len(prompt)] = prompt
+        each = lambda v: torch.full((B,), float(v), device=device)
+        prompt_lengths = lengths.to(torch.int32).to(device)
+        adjust.update(history=history, lengths=prompt_lengths.clone(), prompt_lengths=prompt_lengths, repetition=each(repetition), presence=each(presence),
+                      frequency=each(frequency))
+    if biases:
+        adjust.update(bias_tokens=torch.tensor(list(biases), dtype=torch.int32, device=device),
+                      bias_values=torch.tensor([float(v) for v in biases.values()], device=device))
+    out = []
+    for i in range(tokens):
+        if i == 0:
+            logits = model.prefill(torch.cat(prompts), offsets, cache, slots, weights)[offsets[1:].long() - 1]
+        else:
+            logits = model.step(out[-1], cache, slots, weights)
+        mask = allowed(i) if allowed else None
+        if adjust or mask is not None:
+            binding.wersa_logits_adjust(logits, mask=mask, out=logits, **adjust)
+        out.append(logits.argmax(1))
+        if "history" in adjust:
+            adjust["history"].scatter_(1, adjust["lengths"].long()[:, None], out[-1].to(torch.int32)[:, None])
+            adjust["lengths"] += 1
     return torch.stack(out, 1)
 
 
@@ -148,14 +217,17 @@ def main():
     parser = argparse.ArgumentParser(description=__doc__.split("\n")[0])
     parser.add_argument("--steps", type=int, default=200)
     parser.add_argument("--eight-bit", action="store_true", help="serve with activations and weights in 8 bits")
+    parser.add_argument("--mixing", default="decay", help="decay, recurrence, or a list of these that takes turns, with commas")
+    parser.add_argument("--norm", default="rms", choices=["rms", "layer"])
+    parser.add_argument("--repetition", type=float, default=1.0, help="penalty for tokens that were there before")
     args = parser.parse_args()
     torch.manual_seed(0)
-    model = Decoder()
+    model = Decoder(mixing=args.mixing.split(","), norm=args.norm)
     train(model, args.steps, report=50)
     generator = torch.Generator(device="cuda").manual_seed(1)
     rows = batch(4, 64, model.embedding.shape[0], 2, generator)
     prompts = [row[:length] for row, length in zip(rows, (17, 40, 23, 31))]
-    out = generate(model, prompts, 16, args.eight_bit)
+    out = generate(model, prompts, 16, args.eight_bit, repetition=args.repetition)
     for row, prompt, got in zip(rows, prompts, out):
         want = row[len(prompt):len(prompt) + 16]
         print(f"prompt of {len(prompt)}: {int((got == want).sum())} of 16 tokens as they repeat")
