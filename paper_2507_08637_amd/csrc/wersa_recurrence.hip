@@ -38,24 +38,25 @@ struct Job {
   int B, n, C, tiles, slabs, chains, state_slots, clear;
 };
 
-template <typename T> __device__ __forceinline__ void gate_parts(float g, float &a, float &rest) {
+// A gate as one register: the smaller of a and 1 - a, with all its digits, and the gate's sign, which says which of them it is.
+template <typename T> __device__ __forceinline__ float signed_share(float g) {
   // e^-|g| with one rounding of the exponent for bfloat16 (|g| 2^-24 of it), for float32 with the exponent's low part
   constexpr float kLog2e = 1.44269504f, kLog2eLow = 1.92596299e-8f, kLn2 = 0.69314718f;
   const float m = sizeof(T) == 4 ? fminf(fabsf(g), 200.f) : fabsf(g), t = m * kLog2e;
   float e = __builtin_amdgcn_exp2f(-t);
   if (sizeof(T) == 4) e = g != g ? g : e - e * (kLn2 * (fmaf(m, kLog2e, -t) + m * kLog2eLow));
-  const float s = __builtin_amdgcn_rcpf(1.f + e), small = e * s;
-  a = g >= 0.f ? s : small;
-  rest = g >= 0.f ? small : s;
+  return copysignf(e * __builtin_amdgcn_rcpf(1.f + e), g);
 }
-// The smaller of a and 1 - a with the sign of the gate: both of them from one register, each with all its digits.
-__device__ __forceinline__ void parts_of(float s, float &a, float &rest) {
-  const float small = fabsf(s), big = 1.f - small;
-  const bool keeps = !(__float_as_uint(s) >> 31);
-  a = keeps ? big : small;
-  rest = keeps ? small : big;
+__device__ __forceinline__ bool keeps(float s) { return !(__float_as_uint(s) >> 31); }
+// a h + (1 - a) x from the nearer of the two on: one rounding of the result, where a rounded 1 - a would be off by 2^-25 of h at every row of a long memory.
+__device__ __forceinline__ float next_state(float s, float h, float x) {
+  const float near = keeps(s) ? h : x, far = keeps(s) ? x : h;
+  return fmaf(fabsf(s), far - near, near);
 }
-__device__ __forceinline__ float packed_parts(float g, float a, float rest) { return g >= 0.f ? rest : -a; }
+// a v, with one rounding.
+__device__ __forceinline__ float kept(float s, float v) { return keeps(s) ? fmaf(-fabsf(s), v, v) : fabsf(s) * v; }
+// 1 - a.
+__device__ __forceinline__ float taken(float s) { return keeps(s) ? fabsf(s) : 1.f - fabsf(s); }
 
 template <typename T, int V> __device__ __forceinline__ float channel(const Raw<T, V> &p, int i) {
   if (sizeof(T) == 4) return __uint_as_float(p.u[i]);
@@ -359,7 +360,7 @@ __global__ __launch_bounds__(kThreads, PACKED ? 4 : 6) void recurrence_kernel(Jo
     move_rows<T, V>(rx, valid);
   }
   if (m.all_outside()) pass_over<T, V>(m, rg, rx);
-  float both[kR][V];    // a and 1 - a of each row
+  float both[kR][V];    // a and 1 - a of each row, as one register
   Span s[V];
   float h[V];
 #pragma unroll
@@ -370,12 +371,10 @@ __global__ __launch_bounds__(kThreads, PACKED ? 4 : 6) void recurrence_kernel(Jo
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float g = channel(rg[r], i);
-      float keep, rest;
-      gate_parts<T>(g, keep, rest);
-      both[r][i] = packed_parts(g, keep, rest);
+      both[r][i] = signed_share<T>(g);
       here(both[r][i]);
-      h[i] = fmaf(keep, h[i], rest * channel(rx[r], i));
-      s[i].A *= keep;
+      h[i] = next_state(both[r][i], h[i], channel(rx[r], i));
+      s[i].A = kept(both[r][i], s[i].A);
     }
   }
   anew<T, V>(rx);
@@ -412,9 +411,7 @@ __global__ __launch_bounds__(kThreads, PACKED ? 4 : 6) void recurrence_kernel(Jo
     if (PACKED && m.first(r)) states_of<V>(a.initial, a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      float keep, rest;
-      parts_of(both[r][i], keep, rest);
-      h[i] = fmaf(keep, h[i], rest * channel(rx[r], i));
+      h[i] = next_state(both[r][i], h[i], channel(rx[r], i));
     }
     put[r] = rounded_channels<T, V>(h);
     here<T, V>(put[r]);
@@ -476,7 +473,7 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
     pass_over<T, V>(m, rg, rx);
     clear_outside<T, V>(m, rd);
   }
-  float both[kR][V], h[V], carry[V], A[V];    // both: a and 1 - a of each row
+  float both[kR][V], h[V], carry[V], A[V];    // both: a and 1 - a of each row, as one register
 #pragma unroll
   for (int i = 0; i < V; ++i) A[i] = 1.f, h[i] = carry[i] = 0.f;
 #pragma unroll
@@ -485,12 +482,10 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
 #pragma unroll
     for (int i = 0; i < V; ++i) {
       const float g = channel(rg[r], i);
-      float keep, rest;
-      gate_parts<T>(g, keep, rest);
-      both[r][i] = packed_parts(g, keep, rest);
+      both[r][i] = signed_share<T>(g);
       here(both[r][i]);
-      h[i] = fmaf(keep, h[i], rest * channel(rx[r], i));
-      A[i] *= keep;
+      h[i] = next_state(both[r][i], h[i], channel(rx[r], i));
+      A[i] = kept(both[r][i], A[i]);
     }
   }
 #pragma unroll
@@ -498,9 +493,7 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
     if (PACKED && m.last(r)) states_of<V>(a.dfinal, a, kinds[span * kR + r], c, valid, carry);   // (nothing else comes from behind a sequence)
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      float keep, rest;
-      parts_of(both[r][i], keep, rest);
-      carry[i] = keep * (channel(rd[r], i) + carry[i]);
+      carry[i] = kept(both[r][i], channel(rd[r], i) + carry[i]);
       if (PACKED && m.first(r)) carry[i] = 0.f;
     }
   }
@@ -548,12 +541,10 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
     if (PACKED && m.first(r)) states_of<V>(a.initial, a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      float keep, rest;
-      parts_of(both[r][i], keep, rest);
       const float x = channel(rx[r], i);
-      D[r][i] = keep * (h[i] - x);
+      D[r][i] = kept(both[r][i], h[i] - x);
       here(D[r][i]);
-      h[i] = fmaf(keep, h[i], rest * x);
+      h[i] = next_state(both[r][i], h[i], x);
     }
   }
   anew(both);
@@ -564,12 +555,10 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
     float gx[V], gg[V];
 #pragma unroll
     for (int i = 0; i < V; ++i) {
-      float keep, rest;
-      parts_of(both[r][i], keep, rest);
       const float G = channel(rd[r], i) + carry[i];
-      gx[i] = rest * G;
+      gx[i] = taken(both[r][i]) * G;
       gg[i] = gx[i] * D[r][i];
-      carry[i] = keep * G;
+      carry[i] = kept(both[r][i], G);
     }
     px[r] = rounded_channels<T, V>(gx);
     pg[r] = rounded_channels<T, V>(gg);
@@ -642,9 +631,7 @@ __global__ __launch_bounds__(256) void recurrence_step_kernel(Job a) {
   for (int i = 0; i < V; ++i) state[i] = slot >= 0 && i < valid ? states[i] : 0.f;
 #pragma unroll
   for (int i = 0; i < V; ++i) {
-    float keep, rest;
-    gate_parts<float>(channel(rg, i), keep, rest);
-    h[i] = slot >= 0 ? fmaf(keep, state[i], rest * channel(rx, i)) : 0.f;
+    h[i] = slot >= 0 ? next_state(signed_share<float>(channel(rg, i)), state[i], channel(rx, i)) : 0.f;
   }
 #pragma unroll
   for (int i = 0; i < V; ++i)
