@@ -16,7 +16,7 @@ namespace {
 
 constexpr int kThreads = 512, kLanes = 32, kSpans = kThreads / kLanes;   // spans of R rows that a tile has
 constexpr int kR = 8, kRows = kSpans * kR;
-constexpr int kGroup = 16;                // tiles of a group
+constexpr size_t kCached = (size_t)32 << 20;   // bytes that the second-level caches hold: a larger output is written past them
 constexpr int kWaves = kThreads / 64;
 constexpr uint32_t kNone = 0xffffffffu;   // what the workspace holds where nothing has been left; no number has these bits (NaNs are stored with others)
 constexpr int kPolls = 1 << 23;           // of a wait, some seconds: only a workspace that is written by others meanwhile comes to this
@@ -35,7 +35,7 @@ struct Job {
   uint64_t *spans;                    // [chain][tile][channels of a slab]: (A, H),
   uint32_t *states;                   // [chain][group][channels of a slab]: the state behind a group
   int64_t sx[2], sg[2], so[2], sdx[2], sdg[2];
-  int B, n, C, tiles, slabs, chains, state_slots, clear;
+  int B, n, C, tiles, slabs, chains, state_slots, clear, group, past;
 };
 
 // A gate as one register: the smaller of a and 1 - a, with all its digits, and the gate's sign, which says which of them it is.
@@ -107,10 +107,18 @@ template <typename T, int V> __device__ __forceinline__ void store_channels(T *p
   else store_part<T, V>(p, valid, r);
 }
 // A thread's rows of one tensor, all at once at the end: a branch for each of them would have every row's values live at every branch.
-template <typename T, int V> __device__ __forceinline__ void store_rows(T *p, int64_t stride, int valid, const Raw<T, V> (&r)[kR], int unwritten) {
+template <typename T, int V> __device__ __forceinline__ void store_rows(T *p, int64_t stride, int valid, const Raw<T, V> (&r)[kR], int unwritten, bool past) {
   if (valid >= V && !unwritten) {
+    if (V * sizeof(T) == 8 && past) {
+      typedef uint32_t words2 __attribute__((ext_vector_type(2), aligned(2)));
+      asm volatile("" ::: "memory");   // (else these become one with the others, and lose what they are)
 #pragma unroll
-    for (int i = 0; i < kR; ++i) store_whole<T, V>(p + i * stride, r[i]);
+      for (int i = 0; i < kR; ++i) __builtin_nontemporal_store(words2{r[i].u[0], r[i].u[sizeof(r[i].u) / 4 - 1]}, reinterpret_cast<words2 *>(p + i * stride));
+      asm volatile("" ::: "memory");
+    } else {
+#pragma unroll
+      for (int i = 0; i < kR; ++i) store_whole<T, V>(p + i * stride, r[i]);
+    }
   } else if (valid > 0) {
 #pragma unroll
     for (int i = 0; i < kR; ++i)
@@ -184,36 +192,43 @@ __device__ __forceinline__ float await(const uint32_t *from) {
 }
 
 // The state before tile `at` of a chain, for the threads below CH, whose channel's (A, H) over the tile is `all`: the state behind the group before, then the (A, H)
-// of its group's tiles before it, two to a wave.  `begin`: the state before the first tile, which has it in its (A, H) (that tile alone reads the initial states, before it
+// of its group's tiles before it, a share of them to each wave.  `begin`: the state before the first tile, which has it in its (A, H) (that tile alone reads the initial states, before it
 // leaves anything, so that the final ones may be written over them).  What a tile leaves to others: its (A, H) at once, the last one of a group the state.
 template <int CH>
 __device__ __forceinline__ float state_before(const Job &a, int chain, int at, float begin, const Span &all, Span (*joined)[CH]) {
-  static_assert(kGroup <= 2 * kWaves, "two to a wave");
   constexpr int EACH = CH < 64 ? 1 : CH / 64;
-  const int group = at / kGroup, count = at - group * kGroup, per_chain = (a.tiles + kGroup - 1) / kGroup, wave = threadIdx.x / 64, lane = threadIdx.x & 63;
-  const bool mine = threadIdx.x < CH, on = at + 1 < a.tiles, ends = count == kGroup - 1;
+  const int group = at / a.group, count = at - group * a.group, per_chain = (a.tiles + a.group - 1) / a.group, wave = threadIdx.x / 64, lane = threadIdx.x & 63;
+  const bool mine = threadIdx.x < CH, on = at + 1 < a.tiles, ends = count == a.group - 1;
   if (mine && on && !ends) leave(a.spans + ((int64_t)chain * a.tiles + at) * CH + threadIdx.x, all);
   if (at == 0) return begin;
   if (CH >= 64 || lane < CH) {
-    const uint64_t *from = a.spans + ((int64_t)chain * a.tiles + group * kGroup + 2 * wave) * CH + lane;
-    const int have = min(max(count - 2 * wave, 0), 2);
-    uint64_t v[2][EACH];
+    const int share = a.group / kWaves, first = wave * share, have = min(max(count - first, 0), share);
+    const uint64_t *from = a.spans + ((int64_t)chain * a.tiles + group * a.group + first) * CH + lane;
+    Span s[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) s[e] = Span{1.f, 0.f};
 #pragma unroll 1
-    for (int i = 0; i < kPolls; ++i) {
-      bool ready = true;
+    for (int k = 0; k < have; k += 2, from += 2 * CH) {
+      uint64_t v[2][EACH];
+#pragma unroll 1
+      for (int i = 0; i < kPolls; ++i) {
+        bool ready = true;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) v[j][e] = j < have ? __hip_atomic_load(from + j * CH + 64 * e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : kIdentity;
+          for (int e = 0; e < EACH; ++e) v[j][e] = k + j < have ? __hip_atomic_load(from + j * CH + 64 * e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : kIdentity;
 #pragma unroll
-      for (int j = 0; j < 2; ++j)
+        for (int j = 0; j < 2; ++j)
 #pragma unroll
-        for (int e = 0; e < EACH; ++e) ready &= (uint32_t)v[j][e] != kNone;
-      if (ready) break;
-      __builtin_amdgcn_s_sleep(1);
+          for (int e = 0; e < EACH; ++e) ready &= (uint32_t)v[j][e] != kNone;
+        if (ready) break;
+        __builtin_amdgcn_s_sleep(1);
+      }
+#pragma unroll
+      for (int e = 0; e < EACH; ++e) s[e] = join(s[e], join(span_of(v[0][e]), span_of(v[1][e])));   // (what has not come is a NaN)
     }
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) joined[wave][lane + 64 * e] = join(span_of(v[0][e]), span_of(v[1][e]));   // (what has not come is a NaN)
+    for (int e = 0; e < EACH; ++e) joined[wave][lane + 64 * e] = s[e];
   }
   float h = 0.f;
   if (mine && group > 0) h = await(a.states + ((int64_t)chain * per_chain + group - 1) * CH + threadIdx.x);
@@ -427,7 +442,7 @@ __global__ __launch_bounds__(kThreads, PACKED ? 4 : 6) void recurrence_kernel(Jo
     clear_outside<T, V>(m, put);
     if (!a.clear) unwritten |= m.all_outside();
   }
-  store_rows<T, V>((T *)a.out + batch * a.so[0] + row0 * a.so[1] + c, a.so[1], valid, put, unwritten);
+  store_rows<T, V>((T *)a.out + batch * a.so[0] + row0 * a.so[1] + c, a.so[1], valid, put, unwritten, a.past);
   if (!PACKED && a.final && row0 < a.n && row0 + kR >= a.n) {   // (rows past the end leave h as it is)
     const int64_t slot = slot_of(a, batch);
 #pragma unroll
@@ -578,8 +593,8 @@ __global__ __launch_bounds__(kThreads, 4) void recurrence_back_kernel(Job a) {
     clear_outside<T, V>(m, px);
     clear_outside<T, V>(m, pg);
   }
-  store_rows<T, V>((T *)a.dx + batch * a.sdx[0] + row0 * a.sdx[1] + c, a.sdx[1], valid, px, unwritten);
-  store_rows<T, V>((T *)a.dgate + batch * a.sdg[0] + row0 * a.sdg[1] + c, a.sdg[1], valid, pg, unwritten);
+  store_rows<T, V>((T *)a.dx + batch * a.sdx[0] + row0 * a.sdx[1] + c, a.sdx[1], valid, px, unwritten, a.past);
+  store_rows<T, V>((T *)a.dgate + batch * a.sdg[0] + row0 * a.sdg[1] + c, a.sdg[1], valid, pg, unwritten, a.past);
   if (!PACKED && a.dinitial && row0 == 0) {
 #pragma unroll
     for (int i = 0; i < V; ++i)
@@ -670,9 +685,13 @@ bool written_apart(const wersa_recurrence_desc &c, std::initializer_list<const i
 // Channels of a lane: 8 bytes of a row, 4 where those of 32 lanes are the whole row; never more than a row has.
 int lane_channels(const wersa_recurrence_desc &c) { return c.C == 1 ? 1 : c.dtype == WERSA_BF16 && c.C > kLanes * 2 ? 4 : 2; }
 
+// Tiles of a group.  A chain's groups follow one another, 1 us each: the fewer chains there are, the longer they may take.  131072 rows of 64 channels in bf16: 65 us with
+// groups of 16, 41 with 32; of 1024 channels, forward and backward, 449 and 472, since each tile looks at half of its group.
+int group_of(int chains) { return chains >= 8 ? 16 : chains >= 3 ? 32 : 64; }
+
 struct Layout {
   size_t spans, states, initial, total;   // byte offsets in the workspace; the counter comes first
-  int tiles, slabs, chains;
+  int tiles, slabs, chains, group;
 };
 Layout layout_of(const wersa_recurrence_desc &c) {
   Layout l;
@@ -681,7 +700,8 @@ Layout layout_of(const wersa_recurrence_desc &c) {
   l.slabs = (c.C + ch - 1) / ch;
   l.chains = l.slabs * (c.packed ? 1 : c.B);
   l.spans = 256;
-  const int groups = (l.tiles + kGroup - 1) / kGroup;
+  l.group = group_of(l.chains);
+  const int groups = (l.tiles + l.group - 1) / l.group;
   l.states = l.spans + (size_t)l.chains * l.tiles * ch * 8;
   l.initial = l.tiles <= 1 ? 256 : l.states + ((size_t)l.chains * groups * ch * 4 + 255) / 256 * 256;
   l.total = l.initial + (c.packed ? ((size_t)c.B * c.C * 4 + 255) / 256 * 256 : 0);
@@ -702,7 +722,8 @@ template <typename F> void by_type(const wersa_recurrence_desc &c, F f) {
 Job job_of(const wersa_recurrence_desc &c, const Layout &l, void *workspace) {
   Job a{};
   a.B = c.B, a.n = c.n, a.C = c.C, a.clear = c.clear, a.state_slots = c.B;
-  a.tiles = l.tiles, a.slabs = l.slabs, a.chains = l.chains;
+  a.tiles = l.tiles, a.slabs = l.slabs, a.chains = l.chains, a.group = l.group;
+  a.past = (size_t)(c.packed ? 1 : c.B) * c.n * c.C * (c.dtype == WERSA_F32 ? 4 : 2) > kCached;
   for (int i = 0; i < 2; ++i) a.sx[i] = c.stride_x[i], a.sg[i] = c.stride_gate[i], a.so[i] = c.stride_o[i], a.sdx[i] = c.stride_dx[i], a.sdg[i] = c.stride_dgate[i];
   char *ws = (char *)workspace;
   a.counter = (uint32_t *)ws;
