@@ -17,6 +17,25 @@ struct LayerJob {
   float eps;
 };
 
+// Tensors larger than the last-level cache: what is written once, or read for the last time, passes by the caches (PAST), which keep their room for what comes again.
+// 131072 rows of 2048 in bf16 with a residual: forward 386 us for 404, forward and backward 761 for 824; the forward's reads, or its stream, past them as well: no gain.
+constexpr size_t kCached = (size_t)256 << 20;
+template <bool PAST, typename T> __device__ __forceinline__ u32x4 load_last(const T *row, int col, int cols) {
+  if (PAST && col + 16 / (int)sizeof(T) <= cols) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any *>(row + col));
+  return load_raw(row, col, cols);
+}
+template <bool PAST, typename T, int E> __device__ __forceinline__ void store_once(T *row, int col, int cols, const float (&v)[E]) {
+  if (PAST && col + E <= cols) {
+    u32x4 p;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      p[i] = E == 4 ? __float_as_uint(v[i]) : (uint32_t)f32_to_bf16(v[2 * i % E]) | (uint32_t)f32_to_bf16(v[(2 * i + 1) % E]) << 16;
+    __builtin_nontemporal_store(p, reinterpret_cast<u32x4_any *>(row + col));
+  } else {
+    store_piece<T, E>(row, col, cols, v);
+  }
+}
+
 // E values from column `col` on, zeros where there are none.
 template <int E> __device__ __forceinline__ void load_addends(const float *bias, int col, int cols, float (&b)[E]) {
 #pragma unroll
@@ -29,7 +48,7 @@ template <int E> __device__ __forceinline__ void load_addends(const float *bias,
 }
 
 // LANES threads to a row, PIECES pieces of 16 bytes to a thread.
-template <typename T, int LANES, int PIECES>
+template <typename T, int LANES, int PIECES, bool PAST>
 __global__ __launch_bounds__(256) void layer_norm_kernel(LayerJob a) {
   constexpr int E = 16 / sizeof(T);
   __shared__ float part[4];
@@ -87,7 +106,7 @@ __global__ __launch_bounds__(256) void layer_norm_kernel(LayerJob a) {
     load_addends(a.bias, (t + LANES * p) * E, a.cols, b);
 #pragma unroll
     for (int i = 0; i < E; ++i) v[p][i] = v[p][i] * rstd * w[i] + b[i];
-    store_piece<T, E>(y, (t + LANES * p) * E, cols, v[p]);
+    store_once<PAST, T, E>(y, (t + LANES * p) * E, cols, v[p]);
   }
 }
 
@@ -105,7 +124,7 @@ struct LayerBackJob {
 
 // dx = rstd (g - mean(g) - xhat mean(g xhat)) + dr with g = dy weight.  A workgroup takes rows from its index on, as many at a time as it holds, with the
 // weights of its columns and their sums in registers throughout.  All that a row needs is requested before the first of it is used.
-template <typename T, int LANES, int PIECES>
+template <typename T, int LANES, int PIECES, bool PAST>
 __global__ __launch_bounds__(256, back_groups(PIECES * 16 / sizeof(T)) / 256) void layer_norm_back_kernel(LayerBackJob a) {
   constexpr int E = 16 / sizeof(T), ROWS = 256 / LANES;
   __shared__ float part[2][4];
@@ -125,12 +144,12 @@ __global__ __launch_bounds__(256, back_groups(PIECES * 16 / sizeof(T)) / 256) vo
     u32x4 rr[PIECES], rd[PIECES], ru[PIECES];
 #pragma unroll
     for (int p = 0; p < PIECES; ++p) {
-      rr[p] = load_raw(r, (t + LANES * p) * E, cols);
-      rd[p] = load_raw(dy, (t + LANES * p) * E, cols);
+      rr[p] = load_last<PAST>(r, (t + LANES * p) * E, cols);
+      rd[p] = load_last<PAST>(dy, (t + LANES * p) * E, cols);
     }
     if (a.dr) {
 #pragma unroll
-      for (int p = 0; p < PIECES; ++p) ru[p] = load_raw(dr, (t + LANES * p) * E, cols);
+      for (int p = 0; p < PIECES; ++p) ru[p] = load_last<PAST>(dr, (t + LANES * p) * E, cols);
     }
     const float mean = a.stats[2 * at], rstd = a.stats[2 * at + 1];
     float dot = 0.f, all = 0.f;
@@ -163,7 +182,7 @@ __global__ __launch_bounds__(256, back_groups(PIECES * 16 / sizeof(T)) / 256) vo
         g[i] = rstd * (g[i] * w[p][i] - level - (v[i] - mean) * rstd * along);
         if (a.dr) g[i] += u[i];
       }
-      store_piece<T, E>(dx, (t + LANES * p) * E, cols, g);
+      store_once<PAST, T, E>(dx, (t + LANES * p) * E, cols, g);
     }
   }
   if (!a.partial) return;
@@ -245,7 +264,8 @@ wersa_status wersa_layer_norm_forward(const wersa_norm_desc *desc, const void *x
   by_width(desc->cols, desc->dtype, [&](auto *type, auto lanes, auto pieces) {
     typedef typename std::remove_pointer<decltype(type)>::type T;
     constexpr int L = decltype(lanes)::value, P = decltype(pieces)::value;
-    WERSA_STAGE("wersa_layer_norm", st, (layer_norm_kernel<T, L, P><<<grid_of((desc->rows + 256 / L - 1) / (256 / L)), 256, 0, st>>>(a)));
+    const auto kernel = (size_t)desc->rows * desc->cols * sizeof(T) > kCached ? layer_norm_kernel<T, L, P, true> : layer_norm_kernel<T, L, P, false>;
+    WERSA_STAGE("wersa_layer_norm", st, (kernel<<<grid_of((desc->rows + 256 / L - 1) / (256 / L)), 256, 0, st>>>(a)));
   });
   return hipGetLastError() == hipSuccess ? WERSA_OK : WERSA_ERR_LAUNCH;
 }
@@ -268,7 +288,8 @@ wersa_status wersa_layer_norm_backward(const wersa_norm_desc *desc, const void *
     typedef typename std::remove_pointer<decltype(type)>::type T;
     constexpr int L = decltype(lanes)::value, P = decltype(pieces)::value;
     groups = (int)std::min<int64_t>(back_groups(P * 16 / sizeof(T)), (desc->rows + 256 / L - 1) / (256 / L));
-    if (groups > 0) WERSA_STAGE("wersa_layer_norm_back", st, (layer_norm_back_kernel<T, L, P><<<groups, 256, 0, st>>>(a)));
+    const auto kernel = (size_t)desc->rows * desc->cols * sizeof(T) > kCached ? layer_norm_back_kernel<T, L, P, true> : layer_norm_back_kernel<T, L, P, false>;
+    if (groups > 0) WERSA_STAGE("wersa_layer_norm_back", st, (kernel<<<groups, 256, 0, st>>>(a)));
   });
   if (sums)
     WERSA_STAGE("wersa_layer_norm_reduce", st,
