@@ -275,6 +275,7 @@ template <int V> __device__ __forceinline__ void load_states(const float *p, int
 }
 // Packed sequences' initial states and final states' gradients, by sequence.
 template <int V> __device__ __forceinline__ void states_of(const float *states, const Job &a, int kind, int c, int valid, float (&h)[V]) {
+  asm volatile("" : "+v"(c));   // (the address is formed here, not kept for all rows)
   if (states) load_states<V>(states + (int64_t)(kind & 0xffff) * a.C + c, valid, h);
   else {
 #pragma unroll
@@ -355,7 +356,7 @@ __device__ __forceinline__ bool next_tile(const Job &a, int &chain, int &at) {
 }
 
 template <typename T, int V, bool PACKED>
-__global__ __launch_bounds__(kThreads, PACKED ? 4 : 6) void recurrence_kernel(Job a) {
+__global__ __launch_bounds__(kThreads, 6) void recurrence_kernel(Job a) {
   constexpr int CH = kLanes * V;
   __shared__ Span part[kSpans][CH], joined[kWaves][CH];
   __shared__ float before[CH];
@@ -431,10 +432,12 @@ __global__ __launch_bounds__(kThreads, PACKED ? 4 : 6) void recurrence_kernel(Jo
     put[r] = rounded_channels<T, V>(h);
     here<T, V>(put[r]);
     if (PACKED && m.last(r) && a.final) {
+      int at = c;
+      asm volatile("" : "+v"(at));
       const int64_t slot = slot_of(a, kinds[span * kR + r] & 0xffff);
 #pragma unroll
       for (int i = 0; i < V; ++i)
-        if (slot >= 0 && i < valid) a.final[slot * a.C + c + i] = h[i];
+        if (slot >= 0 && i < valid) a.final[slot * a.C + at + i] = h[i];
     }
   }
   int unwritten = whole ? 0 : rows_past(a, row0);
