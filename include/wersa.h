@@ -293,7 +293,8 @@ wersa_status wersa_decay_step(const wersa_decay_desc *desc, const void *q, const
  *   workspace  scratch (256-byte aligned) in which workgroups pass states on: of one call at a time.
  * wersa_recurrence_backward: the gradients given those with respect to out and (dfinal_state, by sequence, may be NULL) the final states; initial_state is by
  * sequence; dinitial_state may be NULL, and is none of the buffers that are read.
- * Supported: n up to 2^30 (0: the final state is the initial one), B up to 65535, C up to 2^20, B n C below 2^44.
+ * out, dx and dgate are none of the tensors that are read.
+ * Supported: n up to 2^30 (0: the final state is the initial one), B up to 65535, C up to 2^20, B n C below 2^43.
  * Arithmetic: states, gates and every sum in float32; what is written is rounded once.  A row that is not finite reaches only what depends on it, which is then not finite.
  * The same bits every time.
  */
@@ -459,7 +460,7 @@ double wersa_peak_mfma(float *sink, int32_t reps, void *hip_stream);
 
 const char *wersa_status_string(wersa_status status);
 
-/* Library version, major*10000 + minor*100 + patch.  200: wersa_decay_desc has the gradients' strides and clear (a program built
+/* Library version, major*10000 + minor*100 + patch.  300: wersa_recurrence_*, wersa_layer_norm_*, wersa_embedding_*, wersa_logits_adjust.  200: wersa_decay_desc has the gradients' strides and clear (a program built
  * against an older header passes a shorter structure, and has to be built again). */
 int32_t wersa_version(void);
 

@@ -204,6 +204,6 @@ const char *wersa_status_string(wersa_status status) {
   }
 }
 
-int32_t wersa_version(void) { return 200; }
+int32_t wersa_version(void) { return 300; }
 
 }  // extern "C"

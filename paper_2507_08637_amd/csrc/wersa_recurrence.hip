@@ -356,7 +356,7 @@ __device__ __forceinline__ bool next_tile(const Job &a, int &chain, int &at) {
 }
 
 template <typename T, int V, bool PACKED>
-__global__ __launch_bounds__(kThreads, 6) void recurrence_kernel(Job a) {
+__global__ __launch_bounds__(kThreads, PACKED && V == 4 ? 4 : 6) void recurrence_kernel(Job a) {
   constexpr int CH = kLanes * V;
   __shared__ Span part[kSpans][CH], joined[kWaves][CH];
   __shared__ float before[CH];
@@ -381,18 +381,23 @@ __global__ __launch_bounds__(kThreads, 6) void recurrence_kernel(Job a) {
   float h[V];
 #pragma unroll
   for (int i = 0; i < V; ++i) s[i] = Span{1.f, 0.f}, h[i] = 0.f;
+  // Waves of which no row begins or ends a sequence have loops of their own: branches at every row would have the rows one after the other.
+  const bool marked = PACKED && __any(m.bits);
+  const auto form = [&](auto marks) {
 #pragma unroll
-  for (int r = 0; r < kR; ++r) {
-    if (PACKED && m.first(r)) states_of<V>(a.initial, a, kinds[span * kR + r], c, valid, h);
+    for (int r = 0; r < kR; ++r) {
+      if (decltype(marks)::value && m.first(r)) states_of<V>(a.initial, a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      const float g = channel(rg[r], i);
-      both[r][i] = signed_share<T>(g);
-      here(both[r][i]);
-      h[i] = next_state(both[r][i], h[i], channel(rx[r], i));
-      s[i].A = kept(both[r][i], s[i].A);
+      for (int i = 0; i < V; ++i) {
+        both[r][i] = signed_share<T>(channel(rg[r], i));
+        here(both[r][i]);
+        h[i] = next_state(both[r][i], h[i], channel(rx[r], i));
+        s[i].A = kept(both[r][i], s[i].A);
+      }
     }
-  }
+  };
+  if (PACKED && marked) form(std::integral_constant<bool, PACKED>{});
+  else form(std::false_type{});
   anew<T, V>(rx);
 #pragma unroll
   for (int i = 0; i < V; ++i) part[span][lane * V + i] = Span{PACKED && m.any_first() ? -1.f : s[i].A, h[i]};
@@ -422,24 +427,26 @@ __global__ __launch_bounds__(kThreads, 6) void recurrence_kernel(Job a) {
 #pragma unroll
   for (int i = 0; i < V; ++i) h[i] = after(part[span][lane * V + i], before[lane * V + i]);
   Raw<T, V> put[kR];
+  const auto give = [&](auto marks) {
 #pragma unroll
-  for (int r = 0; r < kR; ++r) {
-    if (PACKED && m.first(r)) states_of<V>(a.initial, a, kinds[span * kR + r], c, valid, h);
+    for (int r = 0; r < kR; ++r) {
+      if (decltype(marks)::value && m.first(r)) states_of<V>(a.initial, a, kinds[span * kR + r], c, valid, h);
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-      h[i] = next_state(both[r][i], h[i], channel(rx[r], i));
+      for (int i = 0; i < V; ++i) h[i] = next_state(both[r][i], h[i], channel(rx[r], i));
+      put[r] = rounded_channels<T, V>(h);
+      here<T, V>(put[r]);
+      if (decltype(marks)::value && m.last(r) && a.final) {
+        int at = c;
+        asm volatile("" : "+v"(at));
+        const int64_t slot = slot_of(a, kinds[span * kR + r] & 0xffff);
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+          if (slot >= 0 && i < valid) a.final[slot * a.C + at + i] = h[i];
+      }
     }
-    put[r] = rounded_channels<T, V>(h);
-    here<T, V>(put[r]);
-    if (PACKED && m.last(r) && a.final) {
-      int at = c;
-      asm volatile("" : "+v"(at));
-      const int64_t slot = slot_of(a, kinds[span * kR + r] & 0xffff);
-#pragma unroll
-      for (int i = 0; i < V; ++i)
-        if (slot >= 0 && i < valid) a.final[slot * a.C + at + i] = h[i];
-    }
-  }
+  };
+  if (PACKED && marked) give(std::integral_constant<bool, PACKED>{});
+  else give(std::false_type{});
   int unwritten = whole ? 0 : rows_past(a, row0);
   if (PACKED && m.all_outside()) {
     clear_outside<T, V>(m, put);
