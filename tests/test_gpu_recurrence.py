@@ -341,3 +341,54 @@ def test_rows_past_32_bits(packed):
     binding.wersa_recurrence_backward(x.clone(), gate, torch.ones(1, 1, C, dtype=torch.bfloat16, device="cuda").expand(1, n, C), saved, offsets, grads=grads)
     assert (grads["dx"][0, :-100] == 1).all() and (grads["dx"][0, -1] == 0.5).all() and (grads["dx"][0, -2] == (0.5 if packed else 0.75)).all()
     assert grads["dgate"][0, -2, -1] == (2 * 0.25 * (-2) * (0.5 if packed else 0.75))
+
+
+@pytest.mark.parametrize("dtype,B,n,C", [(torch.bfloat16, 2, 9000, 300), (torch.float32, 3, 5000, 130), (torch.bfloat16, 1, 60000, 64)])
+def test_passes_on_other_values_in_turn(dtype, B, n, C):
+    """What one pass leaves in memory that the next one gets says nothing to it: forward and backward on two sets of values in turn, nothing waited for in between."""
+    from paper_2507_08637_amd import autograd
+    sets = []
+    for seed in (1, 2):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        normal = lambda *s: torch.randn(s, generator=g, device="cuda")
+        sets.append([(3 * normal(B, n, C)).to(dtype).requires_grad_(True), (4 + normal(B, n, C)).to(dtype).requires_grad_(True), normal(B, C).requires_grad_(True),
+                     normal(B, n, C).to(dtype), normal(B, C)])
+
+    def run(x, gate, h0, dout, dfinal):
+        out, final = autograd.wersa_recurrence(x, gate, h0)
+        return [out.detach(), final.detach(), *torch.autograd.grad((out, final), (x, gate, h0), (dout, dfinal))]
+    want = []
+    for s in sets:
+        want.append([t.clone() for t in run(*s)])
+        torch.cuda.synchronize()
+    for _ in range(10):
+        first, second, third = run(*sets[0]), run(*sets[1]), run(*sets[0])
+        for got, ref in ((first, want[0]), (second, want[1]), (third, want[0])):
+            assert all(torch.equal(a, b) for a, b in zip(got, ref))
+
+
+def test_two_recorded_graphs_of_one_pool_in_turn():
+    from paper_2507_08637_amd import binding
+    sets, graphs, outs, pool = [], [], [], torch.cuda.graph_pool_handle()
+    for seed in (1, 2):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        sets.append([torch.randn(2, 6000, 130, generator=g, device="cuda").bfloat16() for _ in range(3)])
+
+    def run(x, gate, dout):
+        out, final, saved = binding.wersa_recurrence_forward(x, gate, want_state=True, want_saved=True)
+        return [out, final, *(v for v in binding.wersa_recurrence_backward(x, gate, dout, saved).values() if v is not None)]
+    want = [[t.clone() for t in run(*s)] for s in sets]
+    kept = []
+    for s in sets:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, pool=pool):
+            got = run(*s)
+            kept.append([t.clone() for t in got])
+        graphs.append(graph)
+        outs.append(kept[-1])
+    for i in (0, 1, 0, 0, 1, 1, 0):
+        for t in outs[i]:
+            t.fill_(float("nan"))
+        graphs[i].replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs[i], want[i])), i
