@@ -92,6 +92,7 @@ int lanes_of(const wersa_embedding_desc &c) {
   return lanes;
 }
 // Sorted places of a piece: as many as leave two workgroups to a compute unit (longer pieces have fewer parts to join), between 8 and 128.
+// 31999 places of 512 columns in float32: sums 21 us and joins 10; with four workgroups to a unit 22 and 12; with one, before long runs were shared out, 27 and 13.5 for 20 and 20.
 int piece_of(const wersa_embedding_desc &c) {
   const int lanes = lanes_of(c), e = c.dtype == WERSA_F32 ? 4 : 8;
   const int64_t slabs = (c.cols + lanes * e - 1) / (lanes * e), each = c.tokens * lanes * slabs / (256 * 512);
@@ -251,7 +252,8 @@ struct SumJob {
   float scale;
 };
 
-// LANES threads to a piece; blockIdx.z: further columns.  PAST: dout is more than the last-level cache holds.
+// LANES threads to a piece; blockIdx.z: further columns.  PAST: dout is more than the last-level cache holds.  Bound by memory: 131072 places of 2048 columns in bf16
+// 171 to 177 us, 744 MB at 4.3 TB/s; with 16 rows ahead 251, with 4 178; dout through the caches 209.
 template <typename T, typename W, int LANES, bool PAST>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(SumJob a) {
   constexpr int Q = kQuads<T>, AHEAD = 8;
@@ -307,6 +309,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(SumJob a) {
 
 // Tokens that go on over boundaries of pieces, each at its first such boundary: the parts in the order of the pieces.  A workgroup looks at kJoinWaves boundaries and 256
 // columns: a wave joins the token of its own one where that has up to kAlone parts, and all of them share out what has more.
+// Bound by the longest run of parts: 31999 places 6.6 to 6.8 us.
 constexpr int kJoinWaves = 8, kAlone = 32;
 struct Parts { int64_t p; int count; uint32_t key; };
 __device__ __forceinline__ void add_parts(const SumJob &a, const Parts &of, int from, int to, int col, float (&acc)[4]) {
@@ -375,7 +378,7 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embedding_join_kernel(SumJob 
   }
 }
 
-// Rows of dweight whose token is nowhere: zeros.
+// Rows of dweight whose token is nowhere: zeros.  Bound by memory: 310 MiB in 48 to 50 us.
 template <typename W>
 __global__ __launch_bounds__(256) void embedding_clear_kernel(SumJob a) {
   __shared__ bool there[kClearRows];
@@ -400,7 +403,8 @@ __global__ __launch_bounds__(256) void embedding_clear_kernel(SumJob a) {
       for (int col = threadIdx.x * E; col < a.cols; col += 256 * E) store_piece<W, E>((W *)a.dweight + (row0 + r) * a.stride_weight, col, a.cols, zeros);
 }
 
-// LANES threads to a row of out, kRowsAhead rows to a thread.
+// LANES threads to a row of out, kRowsAhead rows to a thread.  Bound by memory: 131072 places of 2048 columns, bf16 from float32, 199 to 219 us: 512 MiB are written, and 663 MB
+// read past the L2 caches, each of which has a copy of the rows that come often (the distinct rows have 213 MB).
 template <typename T, typename W, int LANES>
 __global__ __launch_bounds__(256) void embedding_kernel(Source s, const void *weight, void *out, int64_t tokens, int64_t stride_weight, int64_t stride_out, int cols, float scale) {
   constexpr int Q = kQuads<T>, GROUPS = 256 / LANES;

@@ -18,7 +18,7 @@ struct LayerJob {
 };
 
 // Tensors larger than the last-level cache: what is written once, or read for the last time, passes by the caches (PAST), which keep their room for what comes again.
-// 131072 rows of 2048 in bf16 with a residual: forward 386 us for 404, forward and backward 761 for 824; the forward's reads, or its stream, past them as well: no gain.
+// 131072 rows of 2048 in bf16 with a residual: forward 386 us for 404, forward and backward 761 for 824; the forward's reads past them as well: 379, and 810 for 799 before the backward had its own.
 constexpr size_t kCached = (size_t)256 << 20;
 template <bool PAST, typename T> __device__ __forceinline__ u32x4 load_last(const T *row, int col, int cols) {
   if (PAST && col + 16 / (int)sizeof(T) <= cols) return __builtin_nontemporal_load(reinterpret_cast<const u32x4_any *>(row + col));
@@ -47,7 +47,8 @@ template <int E> __device__ __forceinline__ void load_addends(const float *bias,
   }
 }
 
-// LANES threads to a row, PIECES pieces of 16 bytes to a thread.
+// LANES threads to a row, PIECES pieces of 16 bytes to a thread.  Bound by memory: 131072 rows of 2048 in bf16 with a residual 392 to 448 us, 2.15 GB at 4.8 to 5.5 TB/s;
+// 128000 of 128 in float32 42 to 45 us.
 template <typename T, int LANES, int PIECES, bool PAST>
 __global__ __launch_bounds__(256) void layer_norm_kernel(LayerJob a) {
   constexpr int E = 16 / sizeof(T);
@@ -124,6 +125,7 @@ struct LayerBackJob {
 
 // dx = rstd (g - mean(g) - xhat mean(g xhat)) + dr with g = dy weight.  A workgroup takes rows from its index on, as many at a time as it holds, with the
 // weights of its columns and their sums in registers throughout.  All that a row needs is requested before the first of it is used.
+// Bound by memory: 131072 rows of 2048 in bf16 368 to 388 us, 128000 of 128 in float32 41 to 43.
 template <typename T, int LANES, int PIECES, bool PAST>
 __global__ __launch_bounds__(256, back_groups(PIECES * 16 / sizeof(T)) / 256) void layer_norm_back_kernel(LayerBackJob a) {
   constexpr int E = 16 / sizeof(T), ROWS = 256 / LANES;

@@ -29,6 +29,8 @@ struct LogitsJob {
 };
 
 // Dynamic LDS: the words of the tile, and where there are biases their tokens, values and sums.  What memory gives is requested before the first of it is waited for.
+// Bound by the history, which every tile counts: 256 rows of 131072 in float32, histories up to 8000, 65 to 67 us (an earlier form of 85 us took 60 without histories); with
+// tiles of 12288 69 for 68, of 4096 and 512 threads 99 for 77.  One row of 32768: 6.0 to 6.5 us, the way of a workgroup.
 template <typename T>
 __global__ __launch_bounds__(kThreads, 8) void logits_kernel(LogitsJob a) {
   constexpr int E = 16 / sizeof(T), PIECES = kTile / (kThreads * E), AHEAD = 8;
