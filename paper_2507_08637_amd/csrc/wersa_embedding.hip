@@ -252,12 +252,42 @@ struct SumJob {
   float scale;
 };
 
-// LANES threads to a piece; blockIdx.z: further columns.  PAST: dout is more than the last-level cache holds.  Bound by memory: 131072 places of 2048 columns in bf16
-// 171 to 177 us, 744 MB at 4.3 TB/s; with 16 rows ahead 251, with 4 178; dout through the caches 209.
+// Rows of dweight whose token is nowhere: zeros, kClearRows rows to a workgroup.  They need the sorted list only, and lie in the launch of the sums: sorting, sums and zeros
+// with the lookup 458 us for 467 with a launch of their own (131072 places, 65536 rows of 2048 columns), 74 for 81 (31999, 50021 of 512).
+template <typename W> __device__ __forceinline__ void clear_rows(const SumJob &a, int64_t row0) {
+  __shared__ bool there[kClearRows];
+  const int64_t n = a.count ? (int64_t)*a.count : 0;
+  if (threadIdx.x < kClearRows) {
+    const int64_t row = row0 + threadIdx.x;
+    bool found = row >= a.vocabulary;
+    if (!found && n > 0) {
+      const int64_t at = lower_bound(a.keys, n, (uint32_t)row);
+      found = at < n && a.keys[at] == (uint32_t)row;
+    }
+    there[threadIdx.x] = found;
+  }
+  __syncthreads();
+  constexpr int E = 16 / sizeof(W);
+  float zeros[E];
+#pragma unroll
+  for (int i = 0; i < E; ++i) zeros[i] = 0.f;
+  for (int r = 0; r < kClearRows; ++r)
+    if (!there[r])
+      for (int col = threadIdx.x * E; col < a.cols; col += 256 * E) store_piece<W, E>((W *)a.dweight + (row0 + r) * a.stride_weight, col, a.cols, zeros);
+}
+
+// LANES threads to a piece; blockIdx.z: further columns, the last one the rows that are cleared.  PAST: dout is more than the last-level cache holds.  Bound by memory: 131072 places of 2048 columns in bf16,
+// sums alone, 171 to 177 us, 744 MB at 4.3 TB/s; with 16 rows ahead 251, with 4 178; dout through the caches 209.
 template <typename T, typename W, int LANES, bool PAST>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(SumJob a) {
   constexpr int Q = kQuads<T>, AHEAD = 8;
-  const int64_t n = *a.count, piece = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (256 / LANES) + threadIdx.x / LANES, begin = piece * a.piece, end = min(begin + a.piece, n);
+  const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x;
+  if (blockIdx.z == gridDim.z - 1) {
+    if (block * kClearRows < a.vocabulary) clear_rows<W>(a, block * kClearRows);
+    return;
+  }
+  if (!a.count) return;
+  const int64_t n = *a.count, piece = block * (256 / LANES) + threadIdx.x / LANES, begin = piece * a.piece, end = min(begin + a.piece, n);
   const int col = (blockIdx.z * LANES * Q + threadIdx.x % LANES) * 4;
   if (begin >= end || col >= a.cols) return;
   float acc[Q][4] = {};
@@ -378,31 +408,6 @@ __global__ __launch_bounds__(kJoinWaves * 64) void embedding_join_kernel(SumJob 
   }
 }
 
-// Rows of dweight whose token is nowhere: zeros.  Bound by memory: 310 MiB in 48 to 50 us.
-template <typename W>
-__global__ __launch_bounds__(256) void embedding_clear_kernel(SumJob a) {
-  __shared__ bool there[kClearRows];
-  const int64_t n = a.count ? (int64_t)*a.count : 0;
-  const int64_t row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * kClearRows;
-  if (threadIdx.x < kClearRows) {
-    const int64_t row = row0 + threadIdx.x;
-    bool found = row >= a.vocabulary;
-    if (!found && n > 0) {
-      const int64_t at = lower_bound(a.keys, n, (uint32_t)row);
-      found = at < n && a.keys[at] == (uint32_t)row;
-    }
-    there[threadIdx.x] = found;
-  }
-  __syncthreads();
-  constexpr int E = 16 / sizeof(W);
-  float zeros[E];
-#pragma unroll
-  for (int i = 0; i < E; ++i) zeros[i] = 0.f;
-  for (int r = 0; r < kClearRows; ++r)
-    if (!there[r])
-      for (int col = threadIdx.x * E; col < a.cols; col += 256 * E) store_piece<W, E>((W *)a.dweight + (row0 + r) * a.stride_weight, col, a.cols, zeros);
-}
-
 // LANES threads to a row of out, kRowsAhead rows to a thread.  Bound by memory: 131072 places of 2048 columns, bf16 from float32, 199 to 219 us: 512 MiB are written, and 663 MB
 // read past the L2 caches, each of which has a copy of the rows that come often (the distinct rows have 213 MB).
 template <typename T, typename W, int LANES>
@@ -510,11 +515,9 @@ wersa_status wersa_embedding_backward(const wersa_embedding_desc *desc, const vo
     typedef typename std::remove_pointer<decltype(t)>::type T;
     typedef typename std::remove_pointer<decltype(w)>::type W;
     constexpr int L = decltype(lanes)::value, E = 4 * kQuads<T>;
-    WERSA_STAGE("wersa_embedding_clear", st, (embedding_clear_kernel<W><<<grid_of(((int64_t)desc->vocabulary + kClearRows - 1) / kClearRows), 256, 0, st>>>(a)));
-    if (desc->tokens == 0) return;
-    const int64_t pieces = (desc->tokens + a.piece - 1) / a.piece;
-    dim3 grid = grid_of((pieces + 256 / L - 1) / (256 / L));
-    grid.z = (desc->cols + L * E - 1) / (L * E);
+    const int64_t pieces = (desc->tokens + a.piece - 1) / a.piece, clears = ((int64_t)desc->vocabulary + kClearRows - 1) / kClearRows;
+    dim3 grid = grid_of(std::max((pieces + 256 / L - 1) / (256 / L), clears));
+    grid.z = (desc->cols + L * E - 1) / (L * E) + 1;
     const auto sum = (size_t)desc->tokens * desc->cols * sizeof(T) > kCached ? embedding_sum_kernel<T, W, L, true> : embedding_sum_kernel<T, W, L, false>;
     WERSA_STAGE("wersa_embedding_sum", st, (sum<<<grid, 256, 0, st>>>(a)));
     if (pieces > 1) {
