@@ -11,7 +11,7 @@ namespace {
 
 constexpr int kTile = 8192, kThreads = 512;
 constexpr int kMostBiases = 1023, kMostHistory = (1 << 21) - 1;
-// A token's word in LDS: how often it is behind the prompt, whether it is in the prompt, and 1 + the place of its first bias.
+// A token's word in LDS: how often it is behind the prompt, whether it is in the prompt, and kMostBiases - the place of its first bias (0: none).
 constexpr uint32_t kCount = kMostHistory, kPrompt = 1u << 21;
 constexpr int kBiasShift = 22;
 
@@ -29,8 +29,9 @@ struct LogitsJob {
 };
 
 // Dynamic LDS: the words of the tile, and where there are biases their tokens, values and sums.  What memory gives is requested before the first of it is waited for.
-// Bound by the history, which every tile counts: 256 rows of 131072 in float32, histories up to 8000, 65 to 67 us (an earlier form of 85 us took 60 without histories); with
-// tiles of 12288 69 for 68, of 4096 and 512 threads 99 for 77.  One row of 32768: 6.0 to 6.5 us, the way of a workgroup.
+// Bound by the history, which every tile counts: 256 rows of 131072 in float32, histories up to 8000 and 100 biases, 65 to 67 us.  With biases of different tokens 60 us, without
+// histories 49 to 51, without biases 55, the mask alone 44.  Each bias looking through all of them took 67 for 60, and 6.3 us for 6.7 on one row of 32768 (a barrier less); tiles of
+// 12288 69 us for 68, of 4096 and 512 threads 99 for 77, both on an earlier form.
 template <typename T>
 __global__ __launch_bounds__(kThreads, 8) void logits_kernel(LogitsJob a) {
   constexpr int E = 16 / sizeof(T), PIECES = kTile / (kThreads * E), AHEAD = 8;
@@ -83,29 +84,35 @@ __global__ __launch_bounds__(kThreads, 8) void logits_kernel(LogitsJob a) {
 #pragma unroll 4
     for (int i = threadIdx.x + AHEAD * kThreads; i < length; i += kThreads) count(i, history[i]);
   }
-  if (a.biases > 0) {   // a token's biases are added up by its first one, in their order
+  if (a.biases > 0) {   // a token's first bias stands for all of them (the most of kMostBiases - i); counts do not change any more
     __syncthreads();
+    bool again = false;
     for (int i = threadIdx.x; i < a.biases; i += kThreads) {
-      const int token = bias_token[i];
-      const uint32_t v = (uint32_t)token - (uint32_t)v0;
+      const uint32_t v = (uint32_t)bias_token[i] - (uint32_t)v0;
       if (v >= (uint32_t)here) continue;
-      bool first = true;
-      float sum = 0.f;
+      atomicMax(&words[v], (words[v] & (kCount | kPrompt)) | (uint32_t)(kMostBiases - i) << kBiasShift);
+      bias_sum[i] = bias_value[i];
+    }
+    __syncthreads();
+    const auto first = [&](int i, uint32_t v) { return words[v] >> kBiasShift == (uint32_t)(kMostBiases - i); };
+    for (int i = threadIdx.x; i < a.biases; i += kThreads) {
+      const uint32_t v = (uint32_t)bias_token[i] - (uint32_t)v0;
+      again |= v < (uint32_t)here && !first(i, v);
+    }
+    if (__syncthreads_or(again)) {   // a tile with a token that has several: its first one adds them up in their order
+      for (int i = threadIdx.x; i < a.biases; i += kThreads) {
+        const int token = bias_token[i];
+        const uint32_t v = (uint32_t)token - (uint32_t)v0;
+        if (v >= (uint32_t)here || !first(i, v)) continue;
+        float sum = 0.f;
 #pragma unroll 4
-      for (int j0 = 0; j0 < a.biases; j0 += 4) {
-        const i32x4 t = *reinterpret_cast<const i32x4 *>(bias_token + j0);
-        const f32x4 b = *reinterpret_cast<const f32x4 *>(bias_value + j0);
+        for (int j0 = i / 4 * 4; j0 < a.biases; j0 += 4) {
+          const i32x4 t = *reinterpret_cast<const i32x4 *>(bias_token + j0);
+          const f32x4 b = *reinterpret_cast<const f32x4 *>(bias_value + j0);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          if (t[k] == token) {
-            first &= j0 + k >= i;
-            sum += b[k];
-          }
+          for (int k = 0; k < 4; ++k) sum += t[k] == token ? b[k] : 0.f;
         }
-      }
-      if (first) {
         bias_sum[i] = sum;
-        words[v] |= (uint32_t)(i + 1) << kBiasShift;   // (nobody else writes words now)
       }
     }
   }
@@ -128,7 +135,7 @@ __global__ __launch_bounds__(kThreads, 8) void logits_kernel(LogitsJob a) {
             z[i] = z[i] > 0.f ? z[i] / repetition : z[i] * repetition;
             z[i] -= frequency * count + (count > 0.f ? presence : 0.f);
           }
-          if (word[i] >> kBiasShift) z[i] += bias_sum[(word[i] >> kBiasShift) - 1];
+          if (word[i] >> kBiasShift) z[i] += bias_sum[kMostBiases - (int)(word[i] >> kBiasShift)];
         }
       }
     }

@@ -157,3 +157,13 @@ def test_rows_past_32_bits():
     tokens, values = torch.full((B, 1), vocabulary - 2, dtype=torch.int32, device="cuda"), torch.full((B, 1), 2.0, device="cuda")
     out = binding.wersa_logits_adjust(logits, bias_tokens=tokens, bias_values=values, mask=mask, out=logits)
     assert out[-1, -1] == -math.inf and (out[:, -2] == 3).all() and (out[:-1, -1] == 1).all() and (out[-1, :-2] == 1).all()
+
+
+@pytest.mark.parametrize("repeated", [False, True])
+def test_biases_all_over_the_vocabulary(repeated):
+    p = make(2, 20011, 500, 300, torch.float32, 5)
+    g = torch.Generator().manual_seed(6)
+    p["bias_tokens"] = torch.stack([torch.randperm(20011, generator=g)[:300] for _ in range(2)]).int()
+    if repeated:   # one token of the second tile, thrice
+        p["bias_tokens"][1, [7, 130, 299]] = 12345
+    check(p, call(p), torch.float32)
